@@ -35,28 +35,28 @@ def listed():
 
     return [
         # one token of width 768 in each of 4 replicas: the call's latency
-        dropout("dropout fwd, one token", "fwd", 4, 768, "bf16", 0.1, residual=True),
+        dropout("dropout fwd one token", "fwd", 4, 768, "bf16", 0.1, residual=True),
         # 32 images of 197 tokens of width 768, 8 replicas: the end of a transformer sub-layer
-        dropout("dropout fwd, vit batch", "fwd", 8, 32 * 197 * 768, "bf16", 0.1, residual=True),
+        dropout("dropout fwd vit batch", "fwd", 8, 32 * 197 * 768, "bf16", 0.1, residual=True),
         # an odd length in fp32: a classifier head's features
-        dropout("dropout bwd, odd fp32", "bwd", 3, 1_000_003, "f32", 0.5),
+        dropout("dropout bwd odd fp32", "bwd", 3, 1_000_003, "f32", 0.5),
         # the largest: 64 images, 16 replicas
-        dropout("dropout bwd, large", "bwd", 16, 64 * 197 * 768, "bf16", 0.1),
+        dropout("dropout bwd large", "bwd", 16, 64 * 197 * 768, "bf16", 0.1),
         # one token again
-        norm("layernorm fwd, one token", "fwd", 4, 1, 768, "bf16"),
+        norm("layernorm fwd one token", "fwd", 4, 1, 768, "bf16"),
         # long sequences of a wide model
-        norm("layernorm fwd, wide", "fwd", 4, 8192, 4096, "bf16"),
+        norm("layernorm fwd wide", "fwd", 4, 8192, 4096, "bf16"),
         # one image, rows of odd length inside a padded buffer, gamma and beta at an odd place of the vector
-        norm("layernorm bwd, odd fp32", "bwd", 3, 197, 1001, "f32", pad=6, lead=11),
+        norm("layernorm bwd odd fp32", "bwd", 3, 197, 1001, "f32", pad=6, lead=11),
         # 32 images, 8 replicas
-        norm("layernorm bwd, vit batch", "bwd", 8, 32 * 197, 768, "bf16"),
+        norm("layernorm bwd vit batch", "bwd", 8, 32 * 197, 768, "bf16"),
         # a few tokens against all weights: bound by the weights' bytes; weights at an odd place
-        ffn("ffn fwd, few tokens", "fwd", 4, 5, 768, 2048, "bf16", "silu", lead=3),
+        ffn("ffn fwd few tokens", "fwd", 4, 5, 768, 2048, "bf16", "silu", lead=3),
         # one micro-batch of a mid-sized model
-        ffn("ffn fwd, large", "fwd", 4, 4096, 2048, 5632, "bf16", "silu"),
+        ffn("ffn fwd large", "fwd", 4, 4096, 2048, 5632, "bf16", "silu"),
         # 8 images in each of 2 replicas, a hidden width that is not a multiple of any tile
-        ffn("ffn bwd, ragged", "bwd", 2, 8 * 197, 768, 2050, "f16", "gelu"),
-        ffn("ffn bwd, large", "bwd", 4, 4096, 2048, 5632, "bf16", "silu"),
+        ffn("ffn bwd ragged", "bwd", 2, 8 * 197, 768, 2050, "f16", "gelu"),
+        ffn("ffn bwd large", "bwd", 4, 4096, 2048, 5632, "bf16", "silu"),
     ]
 
 
