@@ -255,6 +255,71 @@ grawa_status grawa_step_host_typed(grawa_dtype dtype, grawa_variant variant, voi
                                    const int64_t *layer_offsets, int n_layers, void *center_out,
                                    grawa_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Replica operators: layers of the local phase (the forward and backward passes whose accumulated
+ * gradients the step entry points read) run for all M workers in one call.  The paper leaves the
+ * model to the caller; these operators exist for callers who keep M replicas as flat vectors on one
+ * GPU: a layer's weights are read in place, at any element offset inside the workers' parameter
+ * vectors, and its gradients are written to, or added to (G_k = sum over samples, Eq. 3), the
+ * workers' gradient vectors.
+ *
+ *   - Tables (x, y, gamma, ...) are HOST arrays of M DEVICE pointers on the current device, elements
+ *     stored in `dtype`, aligned to the element size; 16-byte aligned rows take the vector kernels.
+ *     Tables are read during the call only.
+ *   - Arithmetic is fp32 on exactly widened elements; each stored value is rounded to nearest-even once.
+ *   - No output may overlap another buffer of the call (rows of one row stride that lie between each
+ *     other do not overlap); overlap visible from the pointers is rejected.  Elements between the end
+ *     of a row and the next row are neither read nor written.
+ *   - Work is enqueued on `stream`, nothing synchronises, no call allocates device memory or keeps
+ *     anything for the next one, and results are bitwise reproducible.  Calls may be captured into a
+ *     CUDA graph.  A workspace belongs to its call until the call's work is done: calls (or replays of
+ *     captured calls) that may overlap on the GPU need different ones.
+ */
+
+/* Dropout with an optional residual, on n elements a worker:
+ *   y_m[j] = residual_m[j] + (w >= floor(p 2^32 + 1/2) ? x_m[j] / (1 - p) : 0)
+ * with w the 32-bit word j mod 4 of Philox4x32-10 (Salmon et al., SC'11) at
+ *   counter = (b low, b high + (m << 24), o low, o high),  b = floor(j / 4),  key = (seed low, seed high)
+ * and o = offset + *offset_counter.  The mask is a function of (seed, o, m, j) alone, independent of
+ * type, alignment and launch shape: the backward pass computes it again, nothing is stored.
+ * p in [0, 1).  residual may be NULL.  offset_counter: DEVICE, one uint64, or NULL (0): it is read when
+ * the work runs, so that replays of a captured call can use new masks.  y_m may be the same buffer as
+ * x_m or residual_m.  A dropped element does not enter the result, whatever it holds. */
+grawa_status grawa_dropout_forward(grawa_dtype dtype, const void *const *x, const void *const *residual,
+                                   void *const *y, int64_t n, int M, float p, uint64_t seed, uint64_t offset,
+                                   const uint64_t *offset_counter, grawa_stream_t stream);
+
+/* dx_m[j] = (w >= floor(p 2^32 + 1/2) ? dy_m[j] / (1 - p) : 0), the mask of the forward call with the same
+ * p, seed, offset and counter.  (The residual's gradient is dy itself.)  dx_m may be the same buffer as dy_m. */
+grawa_status grawa_dropout_backward(grawa_dtype dtype, const void *const *dy, void *const *dx, int64_t n, int M, float p,
+                                    uint64_t seed, uint64_t offset, const uint64_t *offset_counter,
+                                    grawa_stream_t stream);
+
+/* Layer norm of every row:  mu = mean x, s = 1 / sqrt(mean (x - mu)^2 + eps), y = gamma (x - mu) s + beta.
+ * x, y: `rows` rows of `cols` elements, x_stride / y_stride elements from row to row (>= cols).
+ * gamma, beta: cols elements a worker; either may be NULL (1 and 0).  mean, rstd: DEVICE, fp32, `rows`
+ * values a worker, for the backward pass; both or neither.  eps >= 0.  rows = 0 is a no-op. */
+grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void *const *x, const void *const *gamma,
+                                     const void *const *beta, void *const *y, float *const *mean, float *const *rstd,
+                                     int64_t rows, int64_t cols, int64_t x_stride, int64_t y_stride, int M, float eps,
+                                     grawa_stream_t stream);
+
+/* Its gradients, with h = (x - mu) s and g = dy gamma:
+ *   dx = s (g - mean g - h mean(g h)),  dgamma = sum over rows of dy h,  dbeta = sum over rows of dy.
+ * dy has row stride y_stride; x and dx x_stride.  gamma as in the forward call.  dx, dgamma, dbeta: any of
+ * them may be NULL, not all.  accumulate != 0 adds dgamma and dbeta to what the buffers hold (one rounding
+ * of the sum), 0 overwrites it; rows = 0 overwrites with zeros.
+ * workspace: DEVICE scratch, 16-byte aligned, of grawa_layernorm_backward_workspace_bytes(...) bytes (0
+ * without dgamma and dbeta: it may then be NULL); it needs no particular contents. */
+grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void *const *dy, const void *const *x,
+                                      const void *const *gamma, const float *const *mean, const float *const *rstd,
+                                      void *const *dx, void *const *dgamma, void *const *dbeta, int64_t rows, int64_t cols,
+                                      int64_t x_stride, int64_t y_stride, int M, int accumulate, void *workspace,
+                                      size_t workspace_bytes, grawa_stream_t stream);
+
+/* Bytes of scratch grawa_layernorm_backward needs (0 for few rows, and on invalid arguments). */
+size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M);
+
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not
  * exceed it (for example M = 16 workers of up to 134 million elements each). */
 #define GRAWA_STATIC_MAX_PARTIALS 131072

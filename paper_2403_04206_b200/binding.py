@@ -103,6 +103,17 @@ def library() -> ctypes.CDLL:
     lib.grawa_selftest_bounded_wait.restype = ci
     lib.grawa_collect_kernel_times.argtypes = [vp, vp, vp, vp]
     lib.grawa_collect_kernel_times.restype = ci
+    u64 = ctypes.c_uint64
+    lib.grawa_dropout_forward.argtypes = [ci, vp, vp, vp, i64, ci, cf, u64, u64, vp, vp]
+    lib.grawa_dropout_forward.restype = ci
+    lib.grawa_dropout_backward.argtypes = [ci, vp, vp, i64, ci, cf, u64, u64, vp, vp]
+    lib.grawa_dropout_backward.restype = ci
+    lib.grawa_layernorm_forward.argtypes = [ci] + [vp] * 6 + [i64] * 4 + [ci, cf, vp]
+    lib.grawa_layernorm_forward.restype = ci
+    lib.grawa_layernorm_backward.argtypes = [ci] + [vp] * 8 + [i64] * 4 + [ci, ci, vp, ctypes.c_size_t, vp]
+    lib.grawa_layernorm_backward.restype = ci
+    lib.grawa_layernorm_backward_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.grawa_layernorm_backward_workspace_bytes.restype = ctypes.c_size_t
     _lib = lib
     return lib
 
@@ -428,6 +439,155 @@ def grawa_sumsq_static(grads, sumsq_out, *, stream=None, n=None) -> None:
         n = _numel(grads[0]) if M else 0
     _raise(library().grawa_sumsq_static(_ptr_array(grads), n, M, _addr(sumsq_out), _stream(stream)),
            "grawa_sumsq_static")
+
+
+# ------------------------------------------------------------------ replica operators
+
+def _table(bufs, M, shape, dtype, name, optional=False):
+    """Pointer table of M device tensors of one dtype, one shape and the current device (a 2-D one may have
+    padded rows); with it the row stride.  None gives a NULL table where that is allowed."""
+    if bufs is None and optional:
+        return None, 0
+    if len(bufs) != M:
+        raise ValueError(f"{name}: one entry per worker is needed ({M}), got {len(bufs)}")
+    import torch
+    device = torch.cuda.current_device()
+    out = (ctypes.c_void_p * M)()
+    stride = shape[-1]
+    for m, t in enumerate(bufs):
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if t.get_device() != device:
+            raise ValueError(f"{name}: expected tensors on the current CUDA device ({device}), got {t.device}")
+        if t.shape != shape:
+            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+        if len(shape) == 2 and shape[0] > 1:
+            s = t.stride()
+            if s[1] != 1 and shape[1] > 1:
+                raise ValueError(f"{name}: the elements of a row must be contiguous")
+            if m and s[0] != stride:
+                raise ValueError(f"{name}: all workers need one row stride")
+            stride = s[0]
+        elif not t.is_contiguous():
+            raise ValueError(f"{name}: tensors must be contiguous")
+        out[m] = t.data_ptr()
+    return out, stride
+
+
+def _flat_table(bufs, M, n, dtype, name, optional=False):
+    """Pointer table of M contiguous device tensors of n elements, of any shape."""
+    if bufs is None and optional:
+        return None
+    if len(bufs) != M:
+        raise ValueError(f"{name}: one entry per worker is needed ({M}), got {len(bufs)}")
+    import torch
+    device = torch.cuda.current_device()
+    out = (ctypes.c_void_p * M)()
+    for m, t in enumerate(bufs):
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if t.get_device() != device:
+            raise ValueError(f"{name}: expected tensors on the current CUDA device ({device}), got {t.device}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous tensors of {n} elements")
+        out[m] = t.data_ptr()
+    return out
+
+
+def _storage(bufs) -> int:
+    if len(bufs) == 0:
+        raise ValueError("at least one worker is needed")
+    key = str(bufs[0].dtype)
+    if key not in _DTYPES or not hasattr(bufs[0], "get_device"):
+        raise TypeError(f"expected CUDA tensors of float32, bfloat16 or float16, got {key}")
+    return _DTYPES[key]
+
+
+def _scratch(workspace, need, stream):
+    """The caller's workspace, or one from torch's allocator that is tied to the call's stream.  Returns the
+    tensor (to be kept until the call is enqueued), its address and its size."""
+    if workspace is None and need:
+        import torch
+        s = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(_stream(stream))
+        if s.cuda_stream == torch.cuda.current_stream().cuda_stream:
+            workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+        else:
+            with torch.cuda.stream(s):
+                workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+    if workspace is None:
+        return None, None, 0
+    return workspace, _addr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _counter(offset_counter):
+    if offset_counter is None or isinstance(offset_counter, int):
+        return offset_counter
+    if offset_counter.element_size() != 8 or offset_counter.is_floating_point():
+        raise TypeError("offset_counter: expected a 64-bit integer device tensor")
+    return _addr(offset_counter)
+
+
+def grawa_dropout_forward(x, y, p, seed, offset=0, *, residual=None, offset_counter=None, stream=None) -> None:
+    """y = residual + dropout(x) for all workers (lists of device tensors of equal size); the mask is a function
+    of (seed, offset + counter, worker, element) and never stored; see grawa_dropout_forward in grawa.h."""
+    dt, M = _storage(x), len(x)
+    n, kind = x[0].numel(), x[0].dtype
+    _raise(library().grawa_dropout_forward(dt, _flat_table(x, M, n, kind, "x"), _flat_table(residual, M, n, kind, "residual", True),
+                                           _flat_table(y, M, n, kind, "y"), n, M, float(p), int(seed), int(offset), _counter(offset_counter),
+                                           _stream(stream)), "grawa_dropout_forward")
+
+
+def grawa_dropout_backward(dy, dx, p, seed, offset=0, *, offset_counter=None, stream=None) -> None:
+    """dx = dy where the forward call with these p, seed, offset and counter kept the element, scaled; else 0."""
+    dt, M = _storage(dy), len(dy)
+    n, kind = dy[0].numel(), dy[0].dtype
+    _raise(library().grawa_dropout_backward(dt, _flat_table(dy, M, n, kind, "dy"), _flat_table(dx, M, n, kind, "dx"), n, M, float(p),
+                                            int(seed), int(offset), _counter(offset_counter), _stream(stream)), "grawa_dropout_backward")
+
+
+def grawa_layernorm_forward(x, gamma, beta, y, eps=1e-5, *, mean=None, rstd=None, stream=None) -> None:
+    """Layer norm of the rows of each worker's x ([rows, cols], rows may be padded) into y; gamma and beta ([cols])
+    may be None; mean and rstd ([rows] float32) are filled for the backward pass when given."""
+    import torch
+    dt, M = _storage(x), len(x)
+    shape, kind = x[0].shape, x[0].dtype
+    if len(shape) != 2:
+        raise ValueError("x: expected 2-D tensors [rows, cols]")
+    rows, cols = shape
+    xt, xs = _table(x, M, shape, kind, "x")
+    yt, ys = _table(y, M, shape, kind, "y")
+    _raise(library().grawa_layernorm_forward(
+        dt, xt, _flat_table(gamma, M, cols, kind, "gamma", True), _flat_table(beta, M, cols, kind, "beta", True), yt,
+        _flat_table(mean, M, rows, torch.float32, "mean", True), _flat_table(rstd, M, rows, torch.float32, "rstd", True),
+        rows, cols, xs, ys, M, float(eps), _stream(stream)), "grawa_layernorm_forward")
+
+
+def grawa_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, *, accumulate=False, workspace=None, stream=None) -> None:
+    """Gradients of grawa_layernorm_forward; dx, dgamma and dbeta may each be None.  accumulate adds dgamma and dbeta
+    to what the buffers hold.  dx needs x's row stride.  Without a workspace the call takes one from torch's allocator."""
+    import torch
+    lib, dt, M = library(), _storage(x), len(x)
+    shape, kind = x[0].shape, x[0].dtype
+    if len(shape) != 2:
+        raise ValueError("x: expected 2-D tensors [rows, cols]")
+    rows, cols = shape
+    xt, xs = _table(x, M, shape, kind, "x")
+    yt, ys = _table(dy, M, shape, kind, "dy")
+    dxt, dxs = _table(dx, M, shape, kind, "dx", True)
+    if dxt is not None and dxs != xs:
+        raise ValueError("dx: expected the row stride of x")
+    tables = [_flat_table(gamma, M, cols, kind, "gamma", True), _flat_table(mean, M, rows, torch.float32, "mean"),
+              _flat_table(rstd, M, rows, torch.float32, "rstd"), dxt, _flat_table(dgamma, M, cols, kind, "dgamma", True),
+              _flat_table(dbeta, M, cols, kind, "dbeta", True)]
+    need = lib.grawa_layernorm_backward_workspace_bytes(rows, cols, M) if dgamma is not None or dbeta is not None else 0
+    keep, ws, ws_bytes = _scratch(workspace, need, stream)
+    _raise(lib.grawa_layernorm_backward(dt, yt, xt, *tables, rows, cols, xs, ys, M, 1 if accumulate else 0, ws, ws_bytes,
+                                        _stream(stream)), "grawa_layernorm_backward")
+    del keep
+
+
+def grawa_layernorm_backward_workspace_bytes(rows: int, cols: int, M: int) -> int:
+    return int(library().grawa_layernorm_backward_workspace_bytes(rows, cols, M))
 
 
 def grawa_workspace_bytes(n: int, M: int, layer_offsets=None) -> int:

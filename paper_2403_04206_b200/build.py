@@ -13,7 +13,12 @@ DEBUG_LIB_PATH = os.path.join(_HERE, "libgrawa_debug_bounds.so")
 TRACE_LIB_PATH = os.path.join(_HERE, "libgrawa_trace.so")
 SOURCES = [os.path.join(CSRC, "grawa.cu")]
 HEADERS = [os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "center_pull_bulk.cuh"), os.path.join(CSRC, "kernels_16bit.cuh"), os.path.join(CSRC, "center_pull_staged_any.cuh"),
-           os.path.join(_ROOT, "include", "grawa.h")]
+           os.path.join(CSRC, "host_common.h"), os.path.join(_ROOT, "include", "grawa.h")]
+# The replica operators have no debug or trace code of their own: one object, linked into every variant.
+OPS_OBJECT = os.path.join(_HERE, "_build", "replica_ops.o")
+OPS_SOURCE = os.path.join(CSRC, "replica_ops.cu")
+OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "dropout.cuh", "layernorm.cuh", "host_common.h")] + [
+    os.path.join(_ROOT, "include", "grawa.h")]
 
 # IEEE arithmetic throughout: no fast-math.
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -31,16 +36,33 @@ def is_stale(path: str = LIB_PATH) -> bool:
     if not os.path.exists(path):
         return True
     t = os.path.getmtime(path)
-    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS)
+    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS + [OPS_SOURCE] + OPS_HEADERS)
+
+
+def _run(cmd) -> str:
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+    return res.stderr
+
+
+def _build_ops(force: bool, verbose: bool = False) -> str:
+    """The object of the replica operators, compiled when missing or older than its sources."""
+    if force or not os.path.exists(OPS_OBJECT) or any(os.path.getmtime(p) > os.path.getmtime(OPS_OBJECT) for p in [OPS_SOURCE] + OPS_HEADERS):
+        os.makedirs(os.path.dirname(OPS_OBJECT), exist_ok=True)
+        tmp = OPS_OBJECT + f".tmp{os.getpid()}.o"
+        flags = [f for f in NVCC_FLAGS if f != "-shared"] + (["-Xptxas", "-v"] if verbose else [])
+        log = _run([_nvcc()] + flags + ["-c", "-o", tmp, OPS_SOURCE])
+        if verbose:
+            print(log)
+        os.replace(tmp, OPS_OBJECT)
+    return OPS_OBJECT
 
 
 def _build_variant(path: str, define: str, force: bool) -> str:
     if force or is_stale(path):
         tmp = path + f".tmp{os.getpid()}"
-        cmd = [_nvcc()] + NVCC_FLAGS + [define, "-o", tmp] + SOURCES
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        if res.returncode != 0:
-            raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+        _run([_nvcc()] + NVCC_FLAGS + [define, "-o", tmp] + SOURCES + [_build_ops(False)])
         os.replace(tmp, path)
     return path
 
@@ -55,12 +77,10 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
         return _build_variant(TRACE_LIB_PATH, "-DGRAWA_TRACE", force)
     if force or is_stale():
         tmp = LIB_PATH + f".tmp{os.getpid()}"
-        cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
-        res = subprocess.run(cmd, capture_output=True, text=True)
-        if res.returncode != 0:
-            raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+        ops = _build_ops(force, verbose)
+        log = _run([_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES + [ops])
         if verbose:
-            print(res.stderr)
+            print(log)
         os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

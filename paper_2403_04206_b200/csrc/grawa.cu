@@ -14,6 +14,7 @@
 #include <string>
 #include <vector>
 
+#include "host_common.h"
 #include "kernels.cuh"
 #include "center_pull_bulk.cuh"
 #include "kernels_16bit.cuh"
@@ -25,7 +26,7 @@ static_assert(kMaxWorkers == GRAWA_MAX_WORKERS, "header and kernels disagree on 
 
 // ------------------------------------------------------------------ process-wide state
 static std::mutex g_mutex;
-static std::atomic<int64_t> g_launches{0};
+std::atomic<int64_t> g_launches{0};            // shared with replica_ops.cu
 static int64_t g_sumsq_tile = 8192;
 static int64_t g_pull_tile = 0;           // 0 = one pass of the register kernel, pull_pass_elems(M)
 static int64_t g_pull_variant = 0;
@@ -41,19 +42,13 @@ static int64_t g_sumsq_ctas_per_sm = 0;   // 0 = one CTA per work item
 static int64_t g_pull_ctas_per_sm = 0;    // 0 = one CTA per work item
 static thread_local std::string t_cuda_error;
 
-static grawa_status cuda_fail(cudaError_t err, const char* what)
+grawa_status cuda_fail(cudaError_t err, const char* what)
 {
     char buf[512];
     std::snprintf(buf, sizeof buf, "%s: %s (%s)", what, cudaGetErrorString(err), cudaGetErrorName(err));
     t_cuda_error = buf;
     return GRAWA_ERR_CUDA;
 }
-
-#define GRAWA_CUDA_TRY(expr)                                        \
-    do {                                                            \
-        cudaError_t err__ = (expr);                                 \
-        if (err__ != cudaSuccess) return cuda_fail(err__, #expr);   \
-    } while (0)
 
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

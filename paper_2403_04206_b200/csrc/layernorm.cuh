@@ -1,0 +1,405 @@
+// Layer norm over the rows of all M workers' activations, forward and backward.
+//
+//   forward   mu = mean x, s = (mean (x - mu)^2 + eps)^-1/2, y = gamma (x - mu) s + beta
+//   backward  h = (x - mu) s, g = dy gamma
+//             dx = s (g - mean g - h mean(g h)),  dgamma = sum over rows dy h,  dbeta = sum over rows dy
+//
+// Both directions are bound by memory: 2 (forward) and 3 (backward) elements of traffic per element.  A
+// row is read once and stays in registers, so the variance is the mean of the squared deviations from
+// the finished mean (two passes over registers), not a difference of two large sums.
+//
+// Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in at most 32 (forward) or 16 to
+// 32 (backward) elements a thread; longer rows are read again from L2 instead.
+#pragma once
+#include "replica_common.cuh"
+
+namespace grawa {
+namespace replica {
+
+struct NormForwardArgs {
+    In x, gamma, beta;
+    Out y, mean, rstd;
+    long long rows, x_stride, y_stride;
+    int cols;
+    float eps;
+    int has_gamma, has_beta, has_stats;
+};
+
+struct NormBackwardArgs {
+    In dy, x, gamma, mean, rstd;
+    Out dx, dgamma, dbeta;
+    float* partial;                        // [M][parts][2][cols] when parts > 1
+    long long rows, x_stride, y_stride;
+    int cols, parts;
+    int has_gamma, has_dx, has_dgamma, has_dbeta, accumulate;
+};
+
+constexpr int kNormThreads = 128;          // CTA of the kernels that give a row to some lanes of a warp
+constexpr int kNormMaxBlock = 512;         // largest CTA of the kernels that give a row to a CTA
+constexpr int kNormLongThreads = 512;      // CTA of the kernels for rows that do not fit in registers
+
+// Sum over the LPR lanes of a row, or (LPR = 0) over the CTA.  `buf` alternates between calls: a CTA needs
+// one barrier per call, because a slot is written again only two calls later.
+template <int LPR>
+__device__ __forceinline__ float2 row_sum(float2 v, int buf)
+{
+    if constexpr (LPR > 0) {
+        return make_float2(lanes_sum<LPR>(v.x), lanes_sum<LPR>(v.y));
+    } else {
+        __shared__ float2 part[2][kNormMaxBlock / 32];
+        v = make_float2(lanes_sum<32>(v.x), lanes_sum<32>(v.y));
+        if ((threadIdx.x & 31) == 0) part[buf][threadIdx.x >> 5] = v;
+        __syncthreads();
+        float2 t = make_float2(0.0f, 0.0f);
+        for (unsigned w = 0; w < blockDim.x / 32; ++w) { t.x += part[buf][w].x; t.y += part[buf][w].y; }
+        return t;
+    }
+}
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v, int buf)
+{
+    if constexpr (LPR > 0) return lanes_sum<LPR>(v);
+    else return row_sum<0>(make_float2(v, 0.0f), buf).x;
+}
+
+// LPR = 8 or 32: that many lanes hold a row, kNormThreads / LPR rows a CTA; LPR = 0: the CTA holds it.
+// A thread holds EPT elements in words of VE.
+template <typename T, int VE, int EPT, int LPR>
+__global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
+layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    constexpr int NV = EPT / VE;
+    using W = WordOf<T, VE>;
+    const int m = blockIdx.y;
+    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
+    const long long row = LPR ? static_cast<long long>(blockIdx.x) * (kNormThreads / (LPR ? LPR : 1)) + threadIdx.x / (LPR ? LPR : 1) : blockIdx.x;
+    const bool live = row < a.rows;
+    const int words = live ? a.cols / VE : 0;                 // a group without a row keeps its warp company
+    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + (live ? row : 0) * a.x_stride);
+
+    W xw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (lane + i * lanes < words) xw[i] = x[lane + i * lanes];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (lane + i * lanes >= words) continue;
+        float f[VE];
+        unpack<T, VE>(xw[i], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) sum += f[e];
+    }
+    const float mean = row_sum<LPR>(sum, 0) / a.cols;
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (lane + i * lanes >= words) continue;
+        float f[VE];
+        unpack<T, VE>(xw[i], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) squares = fmaf(f[e] - mean, f[e] - mean, squares);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<LPR>(squares, 1) / a.cols + a.eps);
+    if (!live) return;
+    if (a.has_stats && lane == 0) {
+        static_cast<float*>(a.mean.p[m])[row] = mean;
+        static_cast<float*>(a.rstd.p[m])[row] = rstd;
+    }
+    const W* gamma = static_cast<const W*>(a.gamma.p[m]);
+    const W* beta = static_cast<const W*>(a.beta.p[m]);
+    const T* gamma1 = static_cast<const T*>(a.gamma.p[m]);
+    const T* beta1 = static_cast<const T*>(a.beta.p[m]);
+    const bool words_ok = ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) % sizeof(W)) == 0;
+    W* y = reinterpret_cast<W*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = lane + i * lanes;
+        if (at >= words) continue;
+        float f[VE], g[VE], b[VE] = {};
+#pragma unroll
+        for (int e = 0; e < VE; ++e) g[e] = 1.0f;
+        if (words_ok) {
+            if (a.has_gamma) unpack<T, VE>(gamma[at], g);
+            if (a.has_beta) unpack<T, VE>(beta[at], b);
+        } else {                                              // parameters inside a flat vector stand anywhere
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                if (a.has_gamma) g[e] = widen(gamma1[at * VE + e]);
+                if (a.has_beta) b[e] = widen(beta1[at * VE + e]);
+            }
+        }
+        unpack<T, VE>(xw[i], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) f[e] = fmaf((f[e] - mean) * rstd, g[e], b[e]);
+        y[at] = pack<T, VE>(f);
+    }
+}
+
+// Rows longer than a CTA's registers: a CTA per row, three reads of it (the second and third from L2).
+template <typename T, int VE>
+__global__ void __launch_bounds__(kNormLongThreads)
+layernorm_forward_long_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    using W = WordOf<T, VE>;
+    const int m = blockIdx.y, words = a.cols / VE;
+    const long long row = blockIdx.x;
+    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + row * a.x_stride);
+    const T* gamma = static_cast<const T*>(a.gamma.p[m]);
+    const T* beta = static_cast<const T*>(a.beta.p[m]);
+    W* y = reinterpret_cast<W*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride);
+    float sum = 0.0f, f[VE];
+    for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
+        unpack<T, VE>(x[at], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) sum += f[e];
+    }
+    const float mean = row_sum<0>(sum, 0) / a.cols;
+    float squares = 0.0f;
+    for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
+        unpack<T, VE>(x[at], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) squares = fmaf(f[e] - mean, f[e] - mean, squares);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<0>(squares, 1) / a.cols + a.eps);
+    if (a.has_stats && threadIdx.x == 0) {
+        static_cast<float*>(a.mean.p[m])[row] = mean;
+        static_cast<float*>(a.rstd.p[m])[row] = rstd;
+    }
+    for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
+        unpack<T, VE>(x[at], f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            f[e] = fmaf((f[e] - mean) * rstd, a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f, a.has_beta ? widen(beta[at * VE + e]) : 0.0f);
+        y[at] = pack<T, VE>(f);
+    }
+}
+
+// One column's finished gradients: added to what the worker's gradient vector holds, or put in its place.
+template <typename T>
+__device__ __forceinline__ void store_gradients(const NormBackwardArgs& a, int m, int col, float dg, float db)
+{
+    if (a.has_dgamma) {
+        T* d = static_cast<T*>(a.dgamma.p[m]) + col;
+        *d = narrow<T>(a.accumulate ? widen(*d) + dg : dg);
+    }
+    if (a.has_dbeta) {
+        T* d = static_cast<T*>(a.dbeta.p[m]) + col;
+        *d = narrow<T>(a.accumulate ? widen(*d) + db : db);
+    }
+}
+
+// A worker's column sums over the rows of one CTA: to the CTA's place in `partial`, or, when it is the
+// worker's only CTA, to the gradients themselves.
+template <typename T>
+__device__ __forceinline__ void store_column(const NormBackwardArgs& a, int m, int part, int col, float dg, float db)
+{
+    if (a.parts == 1) {
+        store_gradients<T>(a, m, col, dg, db);
+    } else {
+        float* p = a.partial + (static_cast<size_t>(m) * a.parts + part) * 2 * a.cols + col;
+        p[0] = dg;
+        p[a.cols] = db;
+    }
+}
+
+// gridDim.x CTAs a worker go through its rows in turn; a thread keeps the sums of its own columns in
+// registers over all of them, so the weights' gradients cost one small table at the end and no atomics
+// (the split depends on the sizes alone: the same bits every time).
+template <typename T, int VE, int EPT, int LPR>
+__global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
+layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    constexpr int NV = EPT / VE;
+    constexpr int GROUPS = LPR ? kNormThreads / (LPR ? LPR : 1) : 1;
+    using W = WordOf<T, VE>;
+    const int m = blockIdx.y;
+    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
+    const int group = LPR ? threadIdx.x / (LPR ? LPR : 1) : 0;
+    const int words = a.cols / VE;
+    const T* gamma = static_cast<const T*>(a.gamma.p[m]);
+    const float* means = static_cast<const float*>(a.mean.p[m]);
+    const float* rstds = static_cast<const float*>(a.rstd.p[m]);
+    const float inv = 1.0f / a.cols;
+
+    T gm[EPT];
+    float dg[EPT], db[EPT];
+#pragma unroll
+    for (int k = 0; k < EPT; ++k) {
+        const int at = lane + k / VE * lanes;
+        gm[k] = a.has_gamma && at < words ? gamma[at * VE + k % VE] : narrow<T>(1.0f);
+        dg[k] = db[k] = 0.0f;
+    }
+    int buf = 0;
+    for (long long base = static_cast<long long>(blockIdx.x) * GROUPS; base < a.rows; base += static_cast<long long>(gridDim.x) * GROUPS) {
+        const long long row = base + group;
+        const bool live = row < a.rows;
+        const int w_end = live ? words : 0;
+        const long long r = live ? row : 0;
+        const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + r * a.x_stride);
+        const W* dy = reinterpret_cast<const W*>(static_cast<const T*>(a.dy.p[m]) + r * a.y_stride);
+        W xw[NV], yw[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lane + i * lanes < w_end) { xw[i] = x[lane + i * lanes]; yw[i] = dy[lane + i * lanes]; }
+        const float mean = means[r], rstd = rstds[r];
+        float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (lane + i * lanes >= w_end) continue;
+            float f[VE], d[VE];
+            unpack<T, VE>(xw[i], f);
+            unpack<T, VE>(yw[i], d);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float h = (f[e] - mean) * rstd, g = d[e] * widen(gm[i * VE + e]);
+                s.x += g;
+                s.y = fmaf(g, h, s.y);
+                dg[i * VE + e] = fmaf(d[e], h, dg[i * VE + e]);
+                db[i * VE + e] += d[e];
+            }
+        }
+        if (a.has_dx) {
+            s = row_sum<LPR>(s, buf);
+            buf ^= 1;
+            const float mg = s.x * inv, mgh = s.y * inv;
+            W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + r * a.x_stride);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (lane + i * lanes >= w_end) continue;
+                float f[VE], d[VE];
+                unpack<T, VE>(xw[i], f);
+                unpack<T, VE>(yw[i], d);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const float h = (f[e] - mean) * rstd;
+                    f[e] = (fmaf(d[e], widen(gm[i * VE + e]), -mg) - h * mgh) * rstd;
+                }
+                dx[lane + i * lanes] = pack<T, VE>(f);
+            }
+        }
+    }
+    if (!a.has_dgamma && !a.has_dbeta) return;
+    if constexpr (LPR == 0) {
+#pragma unroll
+        for (int k = 0; k < EPT; ++k) {
+            const int at = lane + k / VE * lanes;
+            if (at < words) store_column<T>(a, m, blockIdx.x, at * VE + k % VE, dg[k], db[k]);
+        }
+    } else {
+        // groups of rows: first the groups of a warp, then the warps in order, through shared memory
+        __shared__ float2 acc[LPR * EPT];
+#pragma unroll
+        for (int k = 0; k < EPT; ++k)
+#pragma unroll
+            for (int d = LPR; d < 32; d <<= 1) {
+                dg[k] += __shfl_xor_sync(0xffffffffu, dg[k], d);
+                db[k] += __shfl_xor_sync(0xffffffffu, db[k], d);
+            }
+        const int warp = threadIdx.x >> 5;
+        for (int turn = 0; turn < kNormThreads / 32; ++turn) {
+            if (warp == turn && (threadIdx.x & 31) < LPR) {
+#pragma unroll
+                for (int k = 0; k < EPT; ++k) {
+                    float2 v = make_float2(dg[k], db[k]);
+                    if (turn) { v.x += acc[k * LPR + lane].x; v.y += acc[k * LPR + lane].y; }
+                    acc[k * LPR + lane] = v;
+                }
+            }
+            __syncthreads();
+        }
+        for (int j = threadIdx.x; j < LPR * EPT; j += kNormThreads) {
+            const int at = j % LPR + j / LPR / VE * LPR, col = at * VE + j / LPR % VE;
+            if (at < words) store_column<T>(a, m, blockIdx.x, col, acc[j].x, acc[j].y);
+        }
+    }
+}
+
+// Rows that do not fit in a CTA's registers: dx by a CTA per row (dy and x are read again from L2) ...
+template <typename T, int VE>
+__global__ void __launch_bounds__(kNormLongThreads)
+layernorm_backward_long_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    using W = WordOf<T, VE>;
+    const int m = blockIdx.y, words = a.cols / VE;
+    const long long row = blockIdx.x;
+    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + row * a.x_stride);
+    const W* dy = reinterpret_cast<const W*>(static_cast<const T*>(a.dy.p[m]) + row * a.y_stride);
+    const T* gamma = static_cast<const T*>(a.gamma.p[m]);
+    W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + row * a.x_stride);
+    const float mean = static_cast<const float*>(a.mean.p[m])[row], rstd = static_cast<const float*>(a.rstd.p[m])[row];
+    float f[VE], d[VE];
+    float2 s = make_float2(0.0f, 0.0f);
+    for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
+        unpack<T, VE>(x[at], f);
+        unpack<T, VE>(dy[at], d);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            const float g = d[e] * (a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f);
+            s.x += g;
+            s.y = fmaf(g, (f[e] - mean) * rstd, s.y);
+        }
+    }
+    s = row_sum<0>(s, 0);
+    const float mg = s.x / a.cols, mgh = s.y / a.cols;
+    for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
+        unpack<T, VE>(x[at], f);
+        unpack<T, VE>(dy[at], d);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            const float g = d[e] * (a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f);
+            f[e] = (g - mg - (f[e] - mean) * rstd * mgh) * rstd;
+        }
+        dx[at] = pack<T, VE>(f);
+    }
+}
+
+// ... and the weights' gradients by a thread per column, gridDim.z parts of the rows.
+template <typename T>
+__global__ void __launch_bounds__(kNormThreads)
+layernorm_columns_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    const int m = blockIdx.y, col = blockIdx.x * kNormThreads + threadIdx.x, part = blockIdx.z;
+    if (col >= a.cols) return;
+    const T* x = static_cast<const T*>(a.x.p[m]) + col;
+    const T* dy = static_cast<const T*>(a.dy.p[m]) + col;
+    const float* means = static_cast<const float*>(a.mean.p[m]);
+    const float* rstds = static_cast<const float*>(a.rstd.p[m]);
+    float dg = 0.0f, db = 0.0f;
+#pragma unroll 4
+    for (long long row = part; row < a.rows; row += a.parts) {
+        const float d = widen(dy[row * a.y_stride]);
+        dg = fmaf(d, (widen(x[row * a.x_stride]) - means[row]) * rstds[row], dg);
+        db += d;
+    }
+    store_column<T>(a, m, part, col, dg, db);
+}
+
+// The parts' column sums, added in a fixed order: 32 columns a CTA, kFinishGroups threads a column.
+constexpr int kFinishGroups = 16;
+template <typename T>
+__global__ void __launch_bounds__(32 * kFinishGroups)
+layernorm_finish_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float2 acc[kFinishGroups][32];
+    const int m = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    float2 s = make_float2(0.0f, 0.0f);
+    if (col < a.cols) {
+        const float* p = a.partial + static_cast<size_t>(m) * a.parts * 2 * a.cols + col;
+#pragma unroll 4
+        for (int i = group; i < a.parts; i += kFinishGroups) {
+            s.x += p[static_cast<size_t>(i) * 2 * a.cols];
+            s.y += p[static_cast<size_t>(i) * 2 * a.cols + a.cols];
+        }
+    }
+    acc[group][lane] = s;
+    __syncthreads();
+    if (group != 0 || col >= a.cols) return;
+#pragma unroll
+    for (int g = 1; g < kFinishGroups; ++g) { s.x += acc[g][lane].x; s.y += acc[g][lane].y; }
+    store_gradients<T>(a, m, col, s.x, s.y);
+}
+
+}  // namespace replica
+}  // namespace grawa

@@ -1,0 +1,77 @@
+// Host-side checks of the replica operators: worker counts, pointers, and overlap of row-strided buffers.
+#pragma once
+#include "host_common.h"
+
+#include <algorithm>
+#include <cstdint>
+
+namespace grawa {
+namespace replica {
+
+inline bool dtype_known(grawa_dtype d) { return d == GRAWA_F32 || d == GRAWA_BF16 || d == GRAWA_F16; }
+inline int64_t type_bytes(grawa_dtype d) { return d == GRAWA_F32 ? 4 : 2; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// The buffers of a call.  add() takes one buffer a worker, `rows` rows of `cols` elements `stride` elements
+// apart; clash() says whether an output shares a byte with any other buffer of the call.  Rows that lie
+// between the rows of another buffer of the same stride are no overlap.
+class Buffers {
+public:
+    static constexpr int kMost = 10 * GRAWA_MAX_WORKERS;
+
+    // false: a NULL entry, or one that is not aligned to its element size
+    bool add(const void* const* table, int M, int64_t rows, int64_t cols, int64_t stride, int64_t elem, bool output)
+    {
+        for (int m = 0; m < M; ++m) {
+            if (rows == 0 || cols == 0) continue;                   // nothing is read or written: any address will do
+            if (table[m] == nullptr || !aligned(table[m], static_cast<size_t>(elem))) return false;
+            const uintptr_t lo = reinterpret_cast<uintptr_t>(table[m]);
+            const uintptr_t stride_bytes = static_cast<uintptr_t>(stride * elem), row_bytes = static_cast<uintptr_t>(cols * elem);
+            item_[count_++] = Item{lo, lo + static_cast<uintptr_t>(rows - 1) * stride_bytes + row_bytes, rows > 1 ? stride_bytes : 0, row_bytes, output};
+        }
+        return true;
+    }
+    bool clash()
+    {
+        std::sort(item_, item_ + count_, [](const Item& a, const Item& b) { return a.lo < b.lo; });
+        for (int i = 0; i < count_; ++i)
+            for (int j = i + 1; j < count_ && item_[j].lo < item_[i].hi; ++j) {
+                if (!item_[i].output && !item_[j].output) continue;
+                if (item_[i].stride && item_[i].stride == item_[j].stride) {
+                    const uintptr_t d = (item_[j].lo - item_[i].lo) % item_[i].stride;
+                    if (d >= item_[i].row && d + item_[j].row <= item_[i].stride) continue;
+                }
+                return true;
+            }
+        return false;
+    }
+
+private:
+    struct Item { uintptr_t lo, hi, stride, row; bool output; };
+    Item item_[kMost];
+    int count_ = 0;
+};
+
+// One launch over grid (gx, gy, gz); `dependent`: its launch may overlap the end of the kernel in front of it
+// on the stream, whose results it waits for by itself.
+template <typename... KArgs, typename... Args>
+grawa_status launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool dependent, const Args&... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(block));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    GRAWA_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    ++g_launches;
+    return GRAWA_OK;
+}
+
+}  // namespace replica
+}  // namespace grawa
