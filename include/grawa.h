@@ -320,6 +320,43 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void *const *dy, 
 /* Bytes of scratch grawa_layernorm_backward needs (0 for few rows, and on invalid arguments). */
 size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M);
 
+/* Activation of the gate. */
+typedef enum grawa_activation { GRAWA_SILU = 0, GRAWA_GELU = 1 /* with erf */, GRAWA_RELU = 2 } grawa_activation;
+
+/* Gated feed-forward product:  a = x Wg^T,  u = x Wu^T,  h = act(a) u, all workers in one kernel on the
+ * tensor cores.  x: [rows][d_in], w_gate and w_up: [d_hidden][d_in], h: [rows][d_hidden], contiguous.
+ * gate_out, up_out: [rows][d_hidden], a and u for the backward pass; both or neither (NULL).
+ * dtype GRAWA_BF16 or GRAWA_F16 (the tensor cores' operands; fp32 is refused), accumulation in fp32, every
+ * output rounded once.  rows = 0 is a no-op; d_in, d_hidden >= 1.
+ * workspace: DEVICE scratch, 256-byte aligned, of grawa_gated_ffn_workspace_bytes(...) bytes, NULL when that is 0. */
+grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, const void *const *x,
+                                     const void *const *w_gate, const void *const *w_up, void *const *h,
+                                     void *const *gate_out, void *const *up_out, int64_t rows, int64_t d_in,
+                                     int64_t d_hidden, int M, void *workspace, size_t workspace_bytes,
+                                     grawa_stream_t stream);
+
+/* Its gradients from dh and the forward call's a (gate) and u (up), with da = dh u act'(a) and du = dh act(a):
+ *   dx = da Wg + du Wu,  dWg = da^T x,  dWu = du^T x.
+ * da and du are rounded to `dtype` on the way (the tensor cores' operands).  dx may be NULL, dw_gate and dw_up
+ * both may be, not all three.  accumulate != 0 adds dw_gate and dw_up to what the buffers hold (one rounding of
+ * the sum), 0 overwrites them; rows = 0 overwrites with zeros.  The slope of GRAWA_RELU at 0 is 0. */
+grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, const void *const *dh,
+                                      const void *const *x, const void *const *w_gate, const void *const *w_up,
+                                      const void *const *gate, const void *const *up, void *const *dx,
+                                      void *const *dw_gate, void *const *dw_up, int64_t rows, int64_t d_in,
+                                      int64_t d_hidden, int M, int accumulate, void *workspace, size_t workspace_bytes,
+                                      grawa_stream_t stream);
+
+/* Bytes of scratch of a forward (backward = 0) or backward call.  `aligned` != 0: x, w_gate and w_up of every
+ * worker are 16-byte aligned; they are then read in place when d_in is a multiple of 8 (a forward call needs
+ * no scratch), and otherwise laid out again in the scratch.  A backward call also keeps da and du there.
+ * 0 on invalid arguments. */
+size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned);
+
+/* Synchronises `stream` and reports whether a bounded device wait of a gated feed-forward call on the current
+ * device ran out since the last report: GRAWA_OK, or GRAWA_ERR_TIMEOUT (that call's outputs are incomplete). */
+grawa_status grawa_gated_ffn_status(grawa_stream_t stream);
+
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not
  * exceed it (for example M = 16 workers of up to 134 million elements each). */
 #define GRAWA_STATIC_MAX_PARTIALS 131072

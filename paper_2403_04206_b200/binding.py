@@ -114,6 +114,15 @@ def library() -> ctypes.CDLL:
     lib.grawa_layernorm_backward.restype = ci
     lib.grawa_layernorm_backward_workspace_bytes.argtypes = [i64, i64, ci]
     lib.grawa_layernorm_backward_workspace_bytes.restype = ctypes.c_size_t
+    sz = ctypes.c_size_t
+    lib.grawa_gated_ffn_forward.argtypes = [ci, ci] + [vp] * 6 + [i64] * 3 + [ci, vp, sz, vp]
+    lib.grawa_gated_ffn_forward.restype = ci
+    lib.grawa_gated_ffn_backward.argtypes = [ci, ci] + [vp] * 9 + [i64] * 3 + [ci, ci, vp, sz, vp]
+    lib.grawa_gated_ffn_backward.restype = ci
+    lib.grawa_gated_ffn_workspace_bytes.argtypes = [i64] * 3 + [ci] * 3
+    lib.grawa_gated_ffn_workspace_bytes.restype = sz
+    lib.grawa_gated_ffn_status.argtypes = [vp]
+    lib.grawa_gated_ffn_status.restype = ci
     _lib = lib
     return lib
 
@@ -588,6 +597,62 @@ def grawa_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, *, acc
 
 def grawa_layernorm_backward_workspace_bytes(rows: int, cols: int, M: int) -> int:
     return int(library().grawa_layernorm_backward_workspace_bytes(rows, cols, M))
+
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _ffn_sizes(x, w_gate):
+    if len(x[0].shape) != 2 or len(w_gate) == 0 or len(w_gate[0].shape) != 2 or w_gate[0].shape[1] != x[0].shape[1]:
+        raise ValueError("expected x [rows, d_in] and weights [d_hidden, d_in]")
+    return x[0].shape[0], x[0].shape[1], w_gate[0].shape[0]
+
+
+def _aligned16(*tables) -> int:
+    return 0 if any(p % 16 for t in tables for p in t if p) else 1
+
+
+def grawa_gated_ffn_forward(x, w_gate, w_up, h, *, activation="silu", gate_out=None, up_out=None, workspace=None, stream=None) -> None:
+    """h = act(x w_gate^T) * (x w_up^T) for each worker's x [rows, d_in], weights [d_hidden, d_in] (views into the flat
+    parameter vectors will do), bfloat16 or float16; gate_out and up_out receive the two products for the backward pass."""
+    lib, dt, M, kind = library(), _storage(x), len(x), x[0].dtype
+    rows, d_in, d_hidden = _ffn_sizes(x, w_gate)
+    act = _ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
+    xt, gt, ut = (_flat_table(v, M, n, kind, name) for v, n, name in
+                  ((x, rows * d_in, "x"), (w_gate, d_hidden * d_in, "w_gate"), (w_up, d_hidden * d_in, "w_up")))
+    outs = [_flat_table(v, M, rows * d_hidden, kind, name, name != "h") for v, name in ((h, "h"), (gate_out, "gate_out"), (up_out, "up_out"))]
+    need = lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, _aligned16(xt, gt, ut))
+    keep, ws, ws_bytes = _scratch(workspace, need, stream)
+    _raise(lib.grawa_gated_ffn_forward(dt, act, xt, gt, ut, *outs, rows, d_in, d_hidden, M, ws, ws_bytes, _stream(stream)),
+           "grawa_gated_ffn_forward")
+    del keep
+
+
+def grawa_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, *, activation="silu", accumulate=False, workspace=None,
+                             stream=None) -> None:
+    """Gradients of grawa_gated_ffn_forward from dh and its gate_out and up_out; dx may be None, dw_gate and dw_up both may be.
+    accumulate adds the weights' gradients to what the buffers hold.  Without a workspace the call takes one from torch's allocator."""
+    lib, dt, M, kind = library(), _storage(x), len(x), x[0].dtype
+    rows, d_in, d_hidden = _ffn_sizes(x, w_gate)
+    act = _ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
+    narrow, wide, weight = rows * d_in, rows * d_hidden, d_hidden * d_in
+    t = [_flat_table(v, M, n, kind, name, name[0] == "d" and name != "dh") for v, n, name in
+         ((dh, wide, "dh"), (x, narrow, "x"), (w_gate, weight, "w_gate"), (w_up, weight, "w_up"), (gate, wide, "gate"), (up, wide, "up"),
+          (dx, narrow, "dx"), (dw_gate, weight, "dw_gate"), (dw_up, weight, "dw_up"))]
+    need = lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, _aligned16(t[1], t[2], t[3]))
+    keep, ws, ws_bytes = _scratch(workspace, need, stream)
+    _raise(lib.grawa_gated_ffn_backward(dt, act, *t, rows, d_in, d_hidden, M, 1 if accumulate else 0, ws, ws_bytes, _stream(stream)),
+           "grawa_gated_ffn_backward")
+    del keep
+
+
+def grawa_gated_ffn_workspace_bytes(rows: int, d_in: int, d_hidden: int, M: int, backward: bool = False, aligned: bool = True) -> int:
+    return int(library().grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1 if backward else 0, 1 if aligned else 0))
+
+
+def grawa_gated_ffn_status(stream=None) -> int:
+    """Synchronises the stream and returns 0, or -5 when a bounded wait of a gated feed-forward call ran out."""
+    return int(library().grawa_gated_ffn_status(_stream(stream)))
 
 
 def grawa_workspace_bytes(n: int, M: int, layer_offsets=None) -> int:

@@ -17,7 +17,7 @@ HEADERS = [os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "center_pull_bu
 # The replica operators have no debug or trace code of their own: one object, linked into every variant.
 OPS_OBJECT = os.path.join(_HERE, "_build", "replica_ops.o")
 OPS_SOURCE = os.path.join(CSRC, "replica_ops.cu")
-OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "dropout.cuh", "layernorm.cuh", "host_common.h")] + [
+OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "dropout.cuh", "layernorm.cuh", "gated_ffn.cuh", "host_common.h")] + [
     os.path.join(_ROOT, "include", "grawa.h")]
 
 # IEEE arithmetic throughout: no fast-math.

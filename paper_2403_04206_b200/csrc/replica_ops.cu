@@ -1,9 +1,13 @@
 // Host side of the replica operators: argument checks, the choice of a kernel, launches, and their part of
 // the C ABI in include/grawa.h.  No call allocates device memory or keeps anything from one call to the next.
+#include <cudaTypedefs.h>
+
 #include <cmath>
 #include <cstring>
+#include <utility>
 
 #include "dropout.cuh"
+#include "gated_ffn.cuh"
 #include "layernorm.cuh"
 #include "replica_host.h"
 
@@ -179,6 +183,139 @@ static grawa_status norm_forward(const NormForwardArgs& a, int M, int ve, cudaSt
     return launch_norm_forward<T, 1>(a, M, stream);
 }
 
+// ------------------------------------------------------------------ gated feed-forward product
+
+// The driver's encoder of tensor maps, looked up once through the runtime (the library does not link the driver).
+static grawa_status map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out)
+{
+    static const auto found = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+        if (err == cudaSuccess && (q != cudaDriverEntryPointSuccess || fn == nullptr)) err = cudaErrorNotSupported;
+        return std::make_pair(err, reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn));
+    }();
+    GRAWA_CUDA_TRY(found.first);
+    *out = found.second;
+    return GRAWA_OK;
+}
+
+// Map of a matrix [depth][rows][cols] of 16-bit elements with rows `pitch` elements apart, for boxes of 64
+// columns (128 bytes, the swizzle's width) by box_rows rows.  The base is 16-byte aligned, the pitch a
+// multiple of 8 elements, and every box starts at a multiple of 64 columns.
+static grawa_status encode_map(CUtensorMap* map, grawa_dtype dtype, const void* base, int64_t depth, int64_t rows, int64_t cols, int64_t pitch,
+                               int box_rows)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+    const grawa_status st = map_encoder(&encode);
+    if (st != GRAWA_OK) return st;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(depth)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(pitch) * 2, static_cast<cuuint64_t>(pitch) * 2 * rows};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
+    const CUresult res = encode(map, dtype == GRAWA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, depth ? 3 : 2,
+                                const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return res == CUDA_SUCCESS ? GRAWA_OK : cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+// One operand of all workers as TMA can read it: in place, or laid out again in the workspace.
+struct Operand {
+    const void* base[GRAWA_MAX_WORKERS];
+    int64_t rows, cols, pitch;
+};
+
+// A bump allocator over the caller's workspace; with a NULL base it only counts.
+struct Scratch {
+    char* base;
+    size_t used = 0;
+    void* take(size_t bytes)
+    {
+        void* p = base ? base + used : nullptr;
+        used += (bytes + 255) / 256 * 256;
+        return p;
+    }
+};
+
+static int64_t pitch_of(int64_t cols) { return ceil_div(cols, 8) * 8; }
+static bool in_place(int64_t cols, bool is_aligned) { return cols % 8 == 0 && is_aligned; }
+
+// Scratch of one operand: nothing when it is read in place.
+static void* operand_scratch(Scratch& s, int64_t rows, int64_t cols, int M, bool is_aligned)
+{
+    return in_place(cols, is_aligned) ? nullptr : s.take(static_cast<size_t>(M) * rows * pitch_of(cols) * 2);
+}
+
+static grawa_status make_operand(Operand* op, const void* const* table, int64_t rows, int64_t cols, int M, void* scratch, cudaStream_t stream)
+{
+    op->rows = rows; op->cols = cols; op->pitch = pitch_of(cols);
+    if (in_place(cols, all_aligned(table, M, 16))) {
+        for (int m = 0; m < M; ++m) op->base[m] = table[m];
+        return GRAWA_OK;
+    }
+    PackArgs a{};
+    copy_table(a.from, table, M);
+    a.to = static_cast<unsigned short*>(scratch);
+    a.rows = rows; a.cols = static_cast<int>(cols); a.pitch = static_cast<int>(op->pitch);
+    for (int m = 0; m < M; ++m) op->base[m] = a.to + static_cast<size_t>(m) * rows * op->pitch;
+    return launch(pack_rows_kernel, dim3(static_cast<unsigned>(ceil_div(rows * (op->pitch / 8), kGatedThreads)), M), kGatedThreads, 0, stream, false, a);
+}
+
+template <typename T, int MODE>
+static grawa_status launch_gemm(const GemmArgs& a, cudaStream_t stream)
+{
+    const int64_t tiles = static_cast<int64_t>(a.workers) * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
+    if (tiles > 0x7fffffff - kSms) return GRAWA_ERR_TOO_LARGE;
+    GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
+    return launch(gemm_kernel<T, MODE>, dim3(static_cast<unsigned>(std::min<int64_t>(tiles, kSms))), kGemmThreads, kGemmSmem, stream, false, a);
+}
+
+template <int MODE>
+static grawa_status launch_gemm(grawa_dtype dtype, const GemmArgs& a, cudaStream_t stream)
+{
+    return dtype == GRAWA_BF16 ? launch_gemm<__nv_bfloat16, MODE>(a, stream) : launch_gemm<__half, MODE>(a, stream);
+}
+
+// Outputs of [rows][cols] for the workers [first, first + count); whether they take 16-byte stores.
+static void set_outputs(GemmArgs& a, int slot, void* const* table, int first, int count)
+{
+    for (int w = 0; w < count; ++w) {
+        a.out[slot][w] = table ? table[first + w] : nullptr;
+        a.words = a.words && aligned(a.out[slot][w], 16);
+    }
+}
+
+static bool ffn_shape_ok(int64_t rows, int64_t d_in, int64_t d_hidden, int M)
+{
+    constexpr int64_t kMost = int64_t{1} << 24;
+    return M >= 1 && M <= GRAWA_MAX_WORKERS && rows >= 0 && rows <= kMost && d_in >= 1 && d_in <= kMost && d_hidden >= 1 && d_hidden <= kMost &&
+           d_in * d_hidden <= (int64_t{1} << 40) && rows * std::max(d_in, d_hidden) <= (int64_t{1} << 38);
+}
+
+static bool ffn_kinds_ok(grawa_dtype dtype, grawa_activation act)
+{
+    return (dtype == GRAWA_BF16 || dtype == GRAWA_F16) && (act == GRAWA_SILU || act == GRAWA_GELU || act == GRAWA_RELU);
+}
+
+// The places of a call's scratch, in the order in which they are taken.
+struct FfnScratch {
+    void *x, *w_gate, *w_up, *da, *du;
+    size_t bytes;
+};
+static FfnScratch ffn_scratch(void* base, int64_t rows, int64_t d_in, int64_t d_hidden, int M, bool x_ok, bool w_ok, bool backward)
+{
+    Scratch s{static_cast<char*>(base)};
+    FfnScratch f{};
+    f.x = operand_scratch(s, rows, d_in, M, x_ok);
+    f.w_gate = operand_scratch(s, d_hidden, d_in, M, w_ok);
+    f.w_up = operand_scratch(s, d_hidden, d_in, M, w_ok);
+    if (backward) {
+        f.da = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
+        f.du = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
+    }
+    f.bytes = s.used;
+    return f;
+}
+
 }  // namespace replica
 }  // namespace grawa
 
@@ -282,6 +419,156 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     if (dtype == GRAWA_BF16) return norm_backward<__nv_bfloat16>(a, M, ve, stream);
     if (dtype == GRAWA_F16) return norm_backward<__half>(a, M, ve, stream);
     return norm_backward<float>(a, M, ve, stream);
+}
+
+size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned)
+{
+    if (!ffn_shape_ok(rows, d_in, d_hidden, M) || rows == 0) return 0;
+    return ffn_scratch(nullptr, rows, d_in, d_hidden, M, aligned != 0, aligned != 0, backward != 0).bytes;
+}
+
+grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, const void* const* x, const void* const* w_gate,
+                                     const void* const* w_up, void* const* h, void* const* gate_out, void* const* up_out, int64_t rows,
+                                     int64_t d_in, int64_t d_hidden, int M, void* workspace, size_t workspace_bytes, grawa_stream_t stream)
+{
+    if (!ffn_kinds_ok(dtype, act) || !x || !w_gate || !w_up || !h || (gate_out == nullptr) != (up_out == nullptr)) return GRAWA_ERR_INVALID_ARG;
+    if (!ffn_shape_ok(rows, d_in, d_hidden, M)) return GRAWA_ERR_INVALID_ARG;
+    if (rows == 0) return GRAWA_OK;
+    Buffers b;
+    if (!b.add(x, M, 1, rows * d_in, rows * d_in, 2, false) || !b.add(w_gate, M, 1, d_in * d_hidden, d_in * d_hidden, 2, false) ||
+        !b.add(w_up, M, 1, d_in * d_hidden, d_in * d_hidden, 2, false) || !b.add(h, M, 1, rows * d_hidden, rows * d_hidden, 2, true))
+        return GRAWA_ERR_INVALID_ARG;
+    if (gate_out && (!b.add(gate_out, M, 1, rows * d_hidden, rows * d_hidden, 2, true) ||
+                     !b.add(up_out, M, 1, rows * d_hidden, rows * d_hidden, 2, true))) return GRAWA_ERR_INVALID_ARG;
+    const FfnScratch f = ffn_scratch(workspace, rows, d_in, d_hidden, M, all_aligned(x, M, 16), all_aligned(w_gate, M, 16) && all_aligned(w_up, M, 16), false);
+    if (f.bytes) {
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < f.bytes) return GRAWA_ERR_WORKSPACE;
+        const void* ws = workspace;
+        if (!b.add(&ws, 1, 1, static_cast<int64_t>(f.bytes), static_cast<int64_t>(f.bytes), 1, true)) return GRAWA_ERR_INVALID_ARG;
+    }
+    if (b.clash()) return GRAWA_ERR_INVALID_ARG;
+
+    Operand xo, go, uo;
+    grawa_status st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
+    if (st == GRAWA_OK) st = make_operand(&go, w_gate, d_hidden, d_in, M, f.w_gate, stream);
+    if (st == GRAWA_OK) st = make_operand(&uo, w_up, d_hidden, d_in, M, f.w_up, stream);
+    for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
+        GemmArgs a{};
+        a.workers = std::min(kGemmWorkers, M - first);
+        a.first_worker = first;
+        a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_hidden, kTileN / 2));
+        a.k_blocks = static_cast<int>(ceil_div(d_in, kTileK));
+        a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_hidden);
+        a.activation = act;
+        a.words = d_hidden % 8 == 0;
+        set_outputs(a, 0, h, first, a.workers);
+        set_outputs(a, 1, gate_out, first, a.workers);
+        set_outputs(a, 2, up_out, first, a.workers);
+        for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
+            st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kTileM);
+            if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kTileN / 2);
+            if (st == GRAWA_OK) st = encode_map(&a.per[2][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kTileN / 2);
+        }
+        if (st == GRAWA_OK) st = launch_gemm<kForward>(dtype, a, stream);
+    }
+    return st;
+}
+
+grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, const void* const* dh, const void* const* x,
+                                      const void* const* w_gate, const void* const* w_up, const void* const* gate, const void* const* up,
+                                      void* const* dx, void* const* dw_gate, void* const* dw_up, int64_t rows, int64_t d_in, int64_t d_hidden,
+                                      int M, int accumulate, void* workspace, size_t workspace_bytes, grawa_stream_t stream)
+{
+    if (!ffn_kinds_ok(dtype, act) || !dh || !x || !w_gate || !w_up || !gate || !up) return GRAWA_ERR_INVALID_ARG;
+    if ((dw_gate == nullptr) != (dw_up == nullptr) || (!dx && !dw_gate) || !ffn_shape_ok(rows, d_in, d_hidden, M)) return GRAWA_ERR_INVALID_ARG;
+    const int64_t weights = d_in * d_hidden;
+    Buffers b;
+    for (const void* const* t : {dh, gate, up})
+        if (!b.add(t, M, rows, d_hidden, d_hidden, 2, false)) return GRAWA_ERR_INVALID_ARG;
+    if (!b.add(x, M, rows, d_in, d_in, 2, false)) return GRAWA_ERR_INVALID_ARG;
+    if (!b.add(w_gate, M, 1, weights, weights, 2, false) || !b.add(w_up, M, 1, weights, weights, 2, false)) return GRAWA_ERR_INVALID_ARG;
+    if (dx && !b.add(dx, M, rows, d_in, d_in, 2, true)) return GRAWA_ERR_INVALID_ARG;
+    if (dw_gate && (!b.add(dw_gate, M, 1, weights, weights, 2, true) || !b.add(dw_up, M, 1, weights, weights, 2, true))) return GRAWA_ERR_INVALID_ARG;
+    const FfnScratch f = ffn_scratch(workspace, rows, d_in, d_hidden, M, all_aligned(x, M, 16), all_aligned(w_gate, M, 16) && all_aligned(w_up, M, 16), true);
+    if (rows > 0) {
+        if (!workspace || !aligned(workspace, 256) || workspace_bytes < f.bytes) return GRAWA_ERR_WORKSPACE;
+        const void* ws = workspace;
+        if (!b.add(&ws, 1, 1, static_cast<int64_t>(f.bytes), static_cast<int64_t>(f.bytes), 1, true)) return GRAWA_ERR_INVALID_ARG;
+    }
+    if (b.clash()) return GRAWA_ERR_INVALID_ARG;
+    if (rows == 0) {                                          // sums over no rows
+        for (int m = 0; m < M && dw_gate && !accumulate; ++m) {
+            GRAWA_CUDA_TRY(cudaMemsetAsync(dw_gate[m], 0, static_cast<size_t>(weights) * 2, stream));
+            GRAWA_CUDA_TRY(cudaMemsetAsync(dw_up[m], 0, static_cast<size_t>(weights) * 2, stream));
+        }
+        return GRAWA_OK;
+    }
+
+    const int64_t pitch = pitch_of(d_hidden);
+    GatedGradArgs e{};
+    copy_table(e.dh, dh, M);
+    copy_table(e.gate, gate, M);
+    copy_table(e.up, up, M);
+    e.da = f.da; e.du = f.du;
+    e.rows = rows; e.cols = static_cast<int>(d_hidden); e.pitch = static_cast<int>(pitch);
+    e.activation = act;
+    e.words = d_hidden % 8 == 0 && all_aligned(dh, M, 16) && all_aligned(gate, M, 16) && all_aligned(up, M, 16);
+    const dim3 grid(static_cast<unsigned>(ceil_div(rows * (pitch / 8), kGatedThreads)), M);
+    grawa_status st = dtype == GRAWA_BF16 ? launch(gated_grad_kernel<__nv_bfloat16>, grid, kGatedThreads, 0, stream, false, e)
+                                          : launch(gated_grad_kernel<__half>, grid, kGatedThreads, 0, stream, false, e);
+    Operand xo, go, uo;
+    if (dx) {
+        if (st == GRAWA_OK) st = make_operand(&go, w_gate, d_hidden, d_in, M, f.w_gate, stream);
+        if (st == GRAWA_OK) st = make_operand(&uo, w_up, d_hidden, d_in, M, f.w_up, stream);
+        for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
+            GemmArgs a{};
+            a.workers = std::min(kGemmWorkers, M - first);
+            a.first_worker = first;
+            a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_in, kTileN));
+            a.k_blocks = static_cast<int>(ceil_div(d_hidden, kTileK));
+            a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_in);
+            a.words = d_in % 8 == 0;
+            set_outputs(a, 0, dx, first, a.workers);
+            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kTileM);
+            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kTileM);
+            for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
+                st = encode_map(&a.per[0][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kTileK);
+                if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kTileK);
+            }
+            if (st == GRAWA_OK) st = launch_gemm<kInputGrad>(dtype, a, stream);
+        }
+    }
+    if (dw_gate) {
+        if (st == GRAWA_OK) st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
+        for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
+            GemmArgs a{};
+            a.workers = std::min(kGemmWorkers, M - first);
+            a.first_worker = first;
+            a.m_tiles = static_cast<int>(ceil_div(d_hidden, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_in, kTileN));
+            a.k_blocks = static_cast<int>(ceil_div(rows, kTileK));
+            a.rows = static_cast<int>(d_hidden); a.cols = static_cast<int>(d_in);
+            a.words = d_in % 8 == 0;
+            a.accumulate = accumulate != 0;
+            set_outputs(a, 0, dw_gate, first, a.workers);
+            set_outputs(a, 1, dw_up, first, a.workers);
+            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kTileK);
+            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kTileK);
+            for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kTileK);
+            if (st == GRAWA_OK) st = launch_gemm<kWeightGrad>(dtype, a, stream);
+        }
+    }
+    return st;
+}
+
+grawa_status grawa_gated_ffn_status(grawa_stream_t stream)
+{
+    int word = 0, zero = 0;
+    GRAWA_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, g_ffn_status, sizeof word, 0, cudaMemcpyDeviceToHost, stream));
+    GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
+    if (word == 0) return GRAWA_OK;
+    GRAWA_CUDA_TRY(cudaMemcpyToSymbolAsync(g_ffn_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, stream));
+    GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
+    return GRAWA_ERR_TIMEOUT;
 }
 
 }  // extern "C"

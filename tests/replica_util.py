@@ -80,3 +80,46 @@ def layernorm_backward64(dy, x, gamma, mean, rstd):
     # column sums: at most rows + 64 additions, and four roundings of each term
     n = (rows + 68) * EPS32
     return (dx, rstd * e), ((dy * h).sum(0), n * (dy * h).abs().sum(0)), (dy.sum(0), n * dy.abs().sum(0))
+
+
+def activation64(name, a):
+    """Value and slope of the gate's activation."""
+    if name == "silu":
+        s = torch.sigmoid(a)
+        return a * s, s * (1.0 + a * (1.0 - s))
+    if name == "gelu":
+        c = 0.5 * (1.0 + torch.erf(a * 0.5 ** 0.5))
+        return a * c, c + a * torch.exp(-0.5 * a * a) / (2.0 * np.pi) ** 0.5
+    return torch.clamp(a, min=0.0), (a > 0).double()
+
+
+ACC = 2.0 ** -23          # one addition of the tensor cores' fp32 accumulation, which may truncate
+FAST = 2.0 ** -20         # relative error of an activation of magnitude one: a few units of the fast exponential and quotient
+
+
+def gated_ffn64(act, x, wg, wu):
+    """(h, error), (a, error), (u, error) with the arithmetic's share of the errors."""
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    k = x.shape[1] * ACC
+    a, u = x @ wg.T, x @ wu.T
+    ea, eu = k * (x.abs() @ wg.abs().T), k * (x.abs() @ wu.abs().T)
+    f, _ = activation64(act, a)
+    # slopes are below 1.13; the exponential's relative error grows with its argument
+    h = f * u
+    return (h, 1.13 * ea * u.abs() + f.abs() * eu + 1.13 * ea * eu + FAST * (1 + a.abs()) * h.abs()), (a, ea), (u, eu)
+
+
+def gated_ffn_backward64(act, dh, x, wg, wu, a, u, kind):
+    """(dx, error), (dwg, error), (dwu, error) for given 16-bit a and u."""
+    dh, x, wg, wu, a, u = (t.double() for t in (dh, x, wg, wu, a, u))
+    f, slope = activation64(act, a)
+    da, du = dh * u * slope, dh * f
+    # each of da and du carries its fp32 arithmetic and one rounding to the storage type
+    ea = HALF_ULP[kind] * da.abs() + FAST * (1 + a.abs()) * (dh * u).abs() * 1.13 + TINY[kind]
+    eu = HALF_ULP[kind] * du.abs() + FAST * (1 + a.abs()) * du.abs() + TINY[kind]
+    rows, hidden = dh.shape
+    out = []
+    out.append((da @ wg + du @ wu, ea @ wg.abs() + eu @ wu.abs() + 2 * hidden * ACC * (da.abs() @ wg.abs() + du.abs() @ wu.abs())))
+    for d, e in ((da, ea), (du, eu)):
+        out.append((d.T @ x, e.T @ x.abs() + rows * ACC * (d.abs().T @ x.abs())))
+    return out

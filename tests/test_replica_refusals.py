@@ -72,3 +72,33 @@ def test_layernorm_backward_refusals():
 def test_workspace_does_not_grow_with_the_rows_without_end(rows, cols, M):
     # at most 16 CTAs an SM's worth of column sums, whatever the rows
     assert grawa.grawa_layernorm_backward_workspace_bytes(rows, cols, M) <= max(148 * 16, M) * 2 * 4 * cols
+
+
+def ffn_forward(dtype=1, act=0, x=X, wg=R, wu=D, h=Y, gate=E, up=F, rows=64, d_in=64, hidden=64, M=2, ws=None, ws_bytes=0):
+    return grawa.library().grawa_gated_ffn_forward(dtype, act, x, wg, wu, h, gate, up, rows, d_in, hidden, M, ws, ws_bytes, None)
+
+
+def ffn_backward(dtype=1, act=0, dh=X, x=R, wg=D, wu=Y, gate=E, up=F, dx=G, dwg=H, dwu=table(0x90_0000_0000), rows=64, d_in=64, hidden=64, M=2, acc=0,
+                 ws=0xa0_0000_0000, ws_bytes=1 << 30):
+    return grawa.library().grawa_gated_ffn_backward(dtype, act, dh, x, wg, wu, gate, up, dx, dwg, dwu, rows, d_in, hidden, M, acc, ws, ws_bytes, None)
+
+
+def test_gated_ffn_refusals():
+    size = grawa.grawa_gated_ffn_workspace_bytes
+    assert ffn_forward(rows=0) == OK and ffn_backward(rows=0, acc=1) == OK
+    assert size(64, 64, 64, 2) == 0 and size(64, 60, 64, 2) > 0 and size(64, 64, 64, 2, aligned=False) > 0
+    assert size(64, 64, 64, 2, backward=True) == 2 * 2 * 64 * 64 * 2 and size(0, 64, 64, 2, backward=True) == 0
+    assert size(-1, 64, 64, 2, True) == 0 and size(64, 0, 64, 2, True) == 0 and size(64, 64, 64, 65, True) == 0
+    for kw in (dict(dtype=0), dict(dtype=3), dict(act=3), dict(act=-1), dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(gate=None),
+               dict(up=None), dict(rows=-1), dict(d_in=0), dict(hidden=0), dict(M=0), dict(M=65), dict(rows=1 << 25), dict(d_in=1 << 25),
+               dict(d_in=1 << 22, hidden=1 << 22), dict(x=NULLS), dict(wu=NULLS), dict(h=NULLS), dict(up=NULLS), dict(h=X), dict(h=R), dict(gate=Y),
+               dict(up=E), dict(x=table(0x10_0000_0001)), dict(h=table(X[1] + 8190))):
+        assert ffn_forward(**kw) == BAD, kw
+    for kw in (dict(d_in=60), dict(x=table(X[0] + 2)), dict(wg=table(R[0] + 8)), dict(d_in=60, ws=0xa0_0000_0000, ws_bytes=size(64, 60, 64, 2) - 1),
+               dict(d_in=60, ws=0xa0_0000_0010, ws_bytes=1 << 30)):
+        assert ffn_forward(**kw) == NO_SPACE, kw
+    for kw in (dict(dtype=0), dict(act=9), dict(dh=None), dict(gate=None), dict(up=None), dict(dwg=None), dict(dwu=None), dict(dx=None, dwg=None, dwu=None),
+               dict(dx=X), dict(dx=R), dict(dwg=D), dict(dwu=H), dict(ws=X[0] - 256), dict(ws=H[0])):
+        assert ffn_backward(**kw) == BAD, kw
+    for kw in (dict(ws=None), dict(ws_bytes=size(64, 64, 64, 2, True) - 1), dict(ws=0xa0_0000_0080), dict(wu=table(Y[0] + 2), ws_bytes=size(64, 64, 64, 2, True))):
+        assert ffn_backward(**kw) == NO_SPACE, kw
