@@ -452,86 +452,60 @@ def grawa_sumsq_static(grads, sumsq_out, *, stream=None, n=None) -> None:
 
 # ------------------------------------------------------------------ replica operators
 
-def _table(bufs, M, shape, dtype, name, optional=False):
-    """Pointer table of M device tensors of one dtype, one shape and the current device (a 2-D one may have
-    padded rows); with it the row stride.  None gives a NULL table where that is allowed."""
-    if bufs is None and optional:
-        return None, 0
-    if len(bufs) != M:
-        raise ValueError(f"{name}: one entry per worker is needed ({M}), got {len(bufs)}")
+_marshal = None
+_ROWS, _OPTIONAL, _FLOAT32 = 1, 2, 4          # modes of a table, as in csrc/marshal.cpp
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _tables(first, specs):
+    """Storage type code, then pointer table and row stride of each spec (name, tensors or None, rows, cols, mode), from the
+    native marshaller, which checks types, sizes, contiguity and that all tensors are on the current device; last the device."""
+    global _marshal
     import torch
-    device = torch.cuda.current_device()
-    out = (ctypes.c_void_p * M)()
-    stride = shape[-1]
-    for m, t in enumerate(bufs):
-        if t.dtype is not dtype:
-            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-        if t.get_device() != device:
-            raise ValueError(f"{name}: expected tensors on the current CUDA device ({device}), got {t.device}")
-        if t.shape != shape:
-            raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-        if len(shape) == 2 and shape[0] > 1:
-            s = t.stride()
-            if s[1] != 1 and shape[1] > 1:
-                raise ValueError(f"{name}: the elements of a row must be contiguous")
-            if m and s[0] != stride:
-                raise ValueError(f"{name}: all workers need one row stride")
-            stride = s[0]
-        elif not t.is_contiguous():
-            raise ValueError(f"{name}: tensors must be contiguous")
-        out[m] = t.data_ptr()
-    return out, stride
+    if _marshal is None:
+        _build.build_marshal()
+        from . import _marshal as native
+        _marshal = native
+        torch.cuda.init()
+    device = torch._C._cuda_getDevice()
+    return _marshal.tables(first, device, specs) + (device,)
 
 
-def _flat_table(bufs, M, n, dtype, name, optional=False):
-    """Pointer table of M contiguous device tensors of n elements, of any shape."""
-    if bufs is None and optional:
-        return None
-    if len(bufs) != M:
-        raise ValueError(f"{name}: one entry per worker is needed ({M}), got {len(bufs)}")
-    import torch
-    device = torch.cuda.current_device()
-    out = (ctypes.c_void_p * M)()
-    for m, t in enumerate(bufs):
-        if t.dtype is not dtype:
-            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-        if t.get_device() != device:
-            raise ValueError(f"{name}: expected tensors on the current CUDA device ({device}), got {t.device}")
-        if t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"{name}: expected contiguous tensors of {n} elements")
-        out[m] = t.data_ptr()
-    return out
+def _stream_on(stream, device) -> int:
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream)
 
 
-def _storage(bufs) -> int:
-    if len(bufs) == 0:
-        raise ValueError("at least one worker is needed")
-    key = str(bufs[0].dtype)
-    if key not in _DTYPES or not hasattr(bufs[0], "get_device"):
-        raise TypeError(f"expected CUDA tensors of float32, bfloat16 or float16, got {key}")
-    return _DTYPES[key]
+def _matrix_shape(t, name):
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name}: expected 2-D tensors")
+    return shape
 
 
 def _scratch(workspace, need, stream):
-    """The caller's workspace, or one from torch's allocator that is tied to the call's stream.  Returns the
-    tensor (to be kept until the call is enqueued), its address and its size."""
-    if workspace is None and need:
-        import torch
-        s = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(_stream(stream))
-        if s.cuda_stream == torch.cuda.current_stream().cuda_stream:
-            workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
-        else:
-            with torch.cuda.stream(s):
-                workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+    """The caller's workspace, or one from torch's allocator that is tied to the call's stream."""
+    if workspace is not None or not need:
+        return workspace
+    import torch
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream))):
+        return torch.empty(need, dtype=torch.uint8, device="cuda")
+
+
+def _scratch_args(workspace):
     if workspace is None:
-        return None, None, 0
-    return workspace, _addr(workspace), workspace.numel() * workspace.element_size()
+        return None, 0
+    return _addr(workspace), workspace.numel() * workspace.element_size()
 
 
 def _counter(offset_counter):
     if offset_counter is None or isinstance(offset_counter, int):
         return offset_counter
-    if offset_counter.element_size() != 8 or offset_counter.is_floating_point():
+    if offset_counter.element_size() != 8 or offset_counter.is_floating_point() or not offset_counter.is_cuda:
         raise TypeError("offset_counter: expected a 64-bit integer device tensor")
     return _addr(offset_counter)
 
@@ -539,111 +513,98 @@ def _counter(offset_counter):
 def grawa_dropout_forward(x, y, p, seed, offset=0, *, residual=None, offset_counter=None, stream=None) -> None:
     """y = residual + dropout(x) for all workers (lists of device tensors of equal size); the mask is a function
     of (seed, offset + counter, worker, element) and never stored; see grawa_dropout_forward in grawa.h."""
-    dt, M = _storage(x), len(x)
-    n, kind = x[0].numel(), x[0].dtype
-    _raise(library().grawa_dropout_forward(dt, _flat_table(x, M, n, kind, "x"), _flat_table(residual, M, n, kind, "residual", True),
-                                           _flat_table(y, M, n, kind, "y"), n, M, float(p), int(seed), int(offset), _counter(offset_counter),
-                                           _stream(stream)), "grawa_dropout_forward")
+    n = x[0].numel()
+    code, xt, _, rt, _, yt, _, dev = _tables(x, (("x", x, n, 1, 0), ("residual", residual, n, 1, _OPTIONAL), ("y", y, n, 1, 0)))
+    status = library().grawa_dropout_forward(code, xt, rt, yt, n, len(x), p, seed, offset, _counter(offset_counter), _stream_on(stream, dev))
+    _raise(status, "grawa_dropout_forward")
 
 
 def grawa_dropout_backward(dy, dx, p, seed, offset=0, *, offset_counter=None, stream=None) -> None:
     """dx = dy where the forward call with these p, seed, offset and counter kept the element, scaled; else 0."""
-    dt, M = _storage(dy), len(dy)
-    n, kind = dy[0].numel(), dy[0].dtype
-    _raise(library().grawa_dropout_backward(dt, _flat_table(dy, M, n, kind, "dy"), _flat_table(dx, M, n, kind, "dx"), n, M, float(p),
-                                            int(seed), int(offset), _counter(offset_counter), _stream(stream)), "grawa_dropout_backward")
+    n = dy[0].numel()
+    code, yt, _, xt, _, dev = _tables(dy, (("dy", dy, n, 1, 0), ("dx", dx, n, 1, 0)))
+    status = library().grawa_dropout_backward(code, yt, xt, n, len(dy), p, seed, offset, _counter(offset_counter), _stream_on(stream, dev))
+    _raise(status, "grawa_dropout_backward")
 
 
 def grawa_layernorm_forward(x, gamma, beta, y, eps=1e-5, *, mean=None, rstd=None, stream=None) -> None:
     """Layer norm of the rows of each worker's x ([rows, cols], rows may be padded) into y; gamma and beta ([cols])
     may be None; mean and rstd ([rows] float32) are filled for the backward pass when given."""
-    import torch
-    dt, M = _storage(x), len(x)
-    shape, kind = x[0].shape, x[0].dtype
-    if len(shape) != 2:
-        raise ValueError("x: expected 2-D tensors [rows, cols]")
-    rows, cols = shape
-    xt, xs = _table(x, M, shape, kind, "x")
-    yt, ys = _table(y, M, shape, kind, "y")
-    _raise(library().grawa_layernorm_forward(
-        dt, xt, _flat_table(gamma, M, cols, kind, "gamma", True), _flat_table(beta, M, cols, kind, "beta", True), yt,
-        _flat_table(mean, M, rows, torch.float32, "mean", True), _flat_table(rstd, M, rows, torch.float32, "rstd", True),
-        rows, cols, xs, ys, M, float(eps), _stream(stream)), "grawa_layernorm_forward")
+    rows, cols = _matrix_shape(x[0], "x")
+    code, xt, xs, gt, _, bt, _, yt, ys, mt, _, rt, _, dev = _tables(x, (
+        ("x", x, rows, cols, _ROWS), ("gamma", gamma, cols, 1, _OPTIONAL), ("beta", beta, cols, 1, _OPTIONAL), ("y", y, rows, cols, _ROWS),
+        ("mean", mean, rows, 1, _OPTIONAL | _FLOAT32), ("rstd", rstd, rows, 1, _OPTIONAL | _FLOAT32)))
+    status = library().grawa_layernorm_forward(code, xt, gt, bt, yt, mt, rt, rows, cols, xs, ys, len(x), eps, _stream_on(stream, dev))
+    _raise(status, "grawa_layernorm_forward")
 
 
 def grawa_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, *, accumulate=False, workspace=None, stream=None) -> None:
     """Gradients of grawa_layernorm_forward; dx, dgamma and dbeta may each be None.  accumulate adds dgamma and dbeta
     to what the buffers hold.  dx needs x's row stride.  Without a workspace the call takes one from torch's allocator."""
-    import torch
-    lib, dt, M = library(), _storage(x), len(x)
-    shape, kind = x[0].shape, x[0].dtype
-    if len(shape) != 2:
-        raise ValueError("x: expected 2-D tensors [rows, cols]")
-    rows, cols = shape
-    xt, xs = _table(x, M, shape, kind, "x")
-    yt, ys = _table(dy, M, shape, kind, "dy")
-    dxt, dxs = _table(dx, M, shape, kind, "dx", True)
-    if dxt is not None and dxs != xs:
+    lib, M = library(), len(x)
+    rows, cols = _matrix_shape(x[0], "x")
+    code, yt, ys, xt, xs, gt, _, mt, _, rt, _, dxt, dxs, dgt, _, dbt, _, dev = _tables(x, (
+        ("dy", dy, rows, cols, _ROWS), ("x", x, rows, cols, _ROWS), ("gamma", gamma, cols, 1, _OPTIONAL), ("mean", mean, rows, 1, _FLOAT32),
+        ("rstd", rstd, rows, 1, _FLOAT32), ("dx", dx, rows, cols, _ROWS | _OPTIONAL), ("dgamma", dgamma, cols, 1, _OPTIONAL),
+        ("dbeta", dbeta, cols, 1, _OPTIONAL)))
+    if dx is not None and dxs != xs:
         raise ValueError("dx: expected the row stride of x")
-    tables = [_flat_table(gamma, M, cols, kind, "gamma", True), _flat_table(mean, M, rows, torch.float32, "mean"),
-              _flat_table(rstd, M, rows, torch.float32, "rstd"), dxt, _flat_table(dgamma, M, cols, kind, "dgamma", True),
-              _flat_table(dbeta, M, cols, kind, "dbeta", True)]
     need = lib.grawa_layernorm_backward_workspace_bytes(rows, cols, M) if dgamma is not None or dbeta is not None else 0
-    keep, ws, ws_bytes = _scratch(workspace, need, stream)
-    _raise(lib.grawa_layernorm_backward(dt, yt, xt, *tables, rows, cols, xs, ys, M, 1 if accumulate else 0, ws, ws_bytes,
-                                        _stream(stream)), "grawa_layernorm_backward")
-    del keep
+    keep = _scratch(workspace, need, stream)
+    status = lib.grawa_layernorm_backward(code, yt, xt, gt, mt, rt, dxt, dgt, dbt, rows, cols, xs, ys, M, 1 if accumulate else 0,
+                                          *_scratch_args(keep), _stream_on(stream, dev))
+    _raise(status, "grawa_layernorm_backward")
 
 
 def grawa_layernorm_backward_workspace_bytes(rows: int, cols: int, M: int) -> int:
     return int(library().grawa_layernorm_backward_workspace_bytes(rows, cols, M))
 
 
-_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
-
-
 def _ffn_sizes(x, w_gate):
-    if len(x[0].shape) != 2 or len(w_gate) == 0 or len(w_gate[0].shape) != 2 or w_gate[0].shape[1] != x[0].shape[1]:
-        raise ValueError("expected x [rows, d_in] and weights [d_hidden, d_in]")
-    return x[0].shape[0], x[0].shape[1], w_gate[0].shape[0]
+    rows, d_in = _matrix_shape(x[0], "x")
+    d_hidden, of_weights = _matrix_shape(w_gate[0], "w_gate")
+    if of_weights != d_in:
+        raise ValueError(f"expected x [rows, d_in] and weights [d_hidden, d_in], got {d_in} and {of_weights} columns")
+    return rows, d_in, d_hidden
 
 
-def _aligned16(*tables) -> int:
-    return 0 if any(p % 16 for t in tables for p in t if p) else 1
+def _all_aligned(*tables) -> int:
+    return 0 if any(t.data_ptr() % 16 for table in tables for t in table) else 1
 
 
 def grawa_gated_ffn_forward(x, w_gate, w_up, h, *, activation="silu", gate_out=None, up_out=None, workspace=None, stream=None) -> None:
     """h = act(x w_gate^T) * (x w_up^T) for each worker's x [rows, d_in], weights [d_hidden, d_in] (views into the flat
     parameter vectors will do), bfloat16 or float16; gate_out and up_out receive the two products for the backward pass."""
-    lib, dt, M, kind = library(), _storage(x), len(x), x[0].dtype
+    lib, M = library(), len(x)
     rows, d_in, d_hidden = _ffn_sizes(x, w_gate)
     act = _ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
-    xt, gt, ut = (_flat_table(v, M, n, kind, name) for v, n, name in
-                  ((x, rows * d_in, "x"), (w_gate, d_hidden * d_in, "w_gate"), (w_up, d_hidden * d_in, "w_up")))
-    outs = [_flat_table(v, M, rows * d_hidden, kind, name, name != "h") for v, name in ((h, "h"), (gate_out, "gate_out"), (up_out, "up_out"))]
-    need = lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, _aligned16(xt, gt, ut))
-    keep, ws, ws_bytes = _scratch(workspace, need, stream)
-    _raise(lib.grawa_gated_ffn_forward(dt, act, xt, gt, ut, *outs, rows, d_in, d_hidden, M, ws, ws_bytes, _stream(stream)),
-           "grawa_gated_ffn_forward")
-    del keep
+    code, xt, _, gt, _, ut, _, ht, _, got, _, uot, _, dev = _tables(x, (
+        ("x", x, rows, d_in, 0), ("w_gate", w_gate, d_hidden, d_in, 0), ("w_up", w_up, d_hidden, d_in, 0), ("h", h, rows, d_hidden, 0),
+        ("gate_out", gate_out, rows, d_hidden, _OPTIONAL), ("up_out", up_out, rows, d_hidden, _OPTIONAL)))
+    keep = workspace
+    if keep is None:
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, _all_aligned(x, w_gate, w_up)), stream)
+    status = lib.grawa_gated_ffn_forward(code, act, xt, gt, ut, ht, got, uot, rows, d_in, d_hidden, M, *_scratch_args(keep), _stream_on(stream, dev))
+    _raise(status, "grawa_gated_ffn_forward")
 
 
 def grawa_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, *, activation="silu", accumulate=False, workspace=None,
                              stream=None) -> None:
     """Gradients of grawa_gated_ffn_forward from dh and its gate_out and up_out; dx may be None, dw_gate and dw_up both may be.
     accumulate adds the weights' gradients to what the buffers hold.  Without a workspace the call takes one from torch's allocator."""
-    lib, dt, M, kind = library(), _storage(x), len(x), x[0].dtype
+    lib, M = library(), len(x)
     rows, d_in, d_hidden = _ffn_sizes(x, w_gate)
     act = _ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
-    narrow, wide, weight = rows * d_in, rows * d_hidden, d_hidden * d_in
-    t = [_flat_table(v, M, n, kind, name, name[0] == "d" and name != "dh") for v, n, name in
-         ((dh, wide, "dh"), (x, narrow, "x"), (w_gate, weight, "w_gate"), (w_up, weight, "w_up"), (gate, wide, "gate"), (up, wide, "up"),
-          (dx, narrow, "dx"), (dw_gate, weight, "dw_gate"), (dw_up, weight, "dw_up"))]
-    need = lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, _aligned16(t[1], t[2], t[3]))
-    keep, ws, ws_bytes = _scratch(workspace, need, stream)
-    _raise(lib.grawa_gated_ffn_backward(dt, act, *t, rows, d_in, d_hidden, M, 1 if accumulate else 0, ws, ws_bytes, _stream(stream)),
-           "grawa_gated_ffn_backward")
-    del keep
+    t = _tables(x, (
+        ("dh", dh, rows, d_hidden, 0), ("x", x, rows, d_in, 0), ("w_gate", w_gate, d_hidden, d_in, 0), ("w_up", w_up, d_hidden, d_in, 0),
+        ("gate", gate, rows, d_hidden, 0), ("up", up, rows, d_hidden, 0), ("dx", dx, rows, d_in, _OPTIONAL),
+        ("dw_gate", dw_gate, d_hidden, d_in, _OPTIONAL), ("dw_up", dw_up, d_hidden, d_in, _OPTIONAL)))
+    keep = workspace
+    if keep is None:
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, _all_aligned(x, w_gate, w_up)), stream)
+    status = lib.grawa_gated_ffn_backward(t[0], act, *t[1:-1:2], rows, d_in, d_hidden, M, 1 if accumulate else 0, *_scratch_args(keep),
+                                          _stream_on(stream, t[-1]))
+    _raise(status, "grawa_gated_ffn_backward")
 
 
 def grawa_gated_ffn_workspace_bytes(rows: int, d_in: int, d_hidden: int, M: int, backward: bool = False, aligned: bool = True) -> int:

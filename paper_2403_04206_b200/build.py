@@ -20,6 +20,10 @@ OPS_SOURCE = os.path.join(CSRC, "replica_ops.cu")
 OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "dropout.cuh", "layernorm.cuh", "gated_ffn.cuh", "host_common.h")] + [
     os.path.join(_ROOT, "include", "grawa.h")]
 
+# The binding's marshaller of pointer tables (a CPython module that reads torch tensors).
+MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
+MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
+
 # IEEE arithmetic throughout: no fast-math.
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]
@@ -42,7 +46,7 @@ def is_stale(path: str = LIB_PATH) -> bool:
 def _run(cmd) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+        raise RuntimeError("compilation failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
     return res.stderr
 
 
@@ -57,6 +61,20 @@ def _build_ops(force: bool, verbose: bool = False) -> str:
             print(log)
         os.replace(tmp, OPS_OBJECT)
     return OPS_OBJECT
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compiles the marshaller when missing or older than its source; returns its path."""
+    if force or not os.path.exists(MARSHAL_PATH) or os.path.getmtime(MARSHAL_SOURCE) > os.path.getmtime(MARSHAL_PATH):
+        import sysconfig
+        import torch
+        base = os.path.dirname(torch.__file__)
+        tmp = MARSHAL_PATH + f".tmp{os.getpid()}"
+        _run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + os.path.join(base, "include"),
+              "-I" + os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I" + sysconfig.get_paths()["include"],
+              MARSHAL_SOURCE, "-o", tmp, "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+        os.replace(tmp, MARSHAL_PATH)
+    return MARSHAL_PATH
 
 
 def _build_variant(path: str, define: str, force: bool) -> str:

@@ -30,14 +30,13 @@ static bool all_aligned(const void* const* table, int M, size_t bytes)
 // ------------------------------------------------------------------ dropout
 
 template <typename T>
-static grawa_status launch_dropout(const DropoutArgs& a, int M, bool vec, cudaStream_t stream)
+static grawa_status launch_dropout(const DropoutArgs& a, int M, bool vec, bool residual, cudaStream_t stream)
 {
-    constexpr int kCols = 2;
-    const int64_t per_cta = static_cast<int64_t>(kDropThreads) * kCols * (vec ? 16 / static_cast<int>(sizeof(T)) : 4);
-    const int64_t ctas = ceil_div(a.n, per_cta);
+    const int64_t ctas = ceil_div(a.n, kDropThreads * kDropCols * (16 / static_cast<int>(sizeof(T))));
     if (ctas > 0x7fffffff) return GRAWA_ERR_INVALID_ARG;
-    return launch(vec ? dropout_kernel<T, true, kCols> : dropout_kernel<T, false, kCols>, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0,
-                  stream, false, a);
+    auto* const kernel = vec ? (residual ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>)
+                             : (residual ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>);
+    return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0, stream, false, a);
 }
 
 // `in` and `r` may each be the same buffer as `out` (every element is read before it is written, by one thread).
@@ -69,16 +68,16 @@ static grawa_status dropout(grawa_dtype dtype, const void* const* in, const void
     copy_table(a.r, r, M);
     copy_table(a.y, out, M);
     a.n = n;
-    a.seed = seed;
+    for (unsigned round = 0; round < 10; ++round)
+        a.keys[round] = make_uint2(static_cast<unsigned>(seed) + round * 0x9E3779B9u, static_cast<unsigned>(seed >> 32) + round * 0xBB67AE85u);
     a.offset = offset;
     a.counter = reinterpret_cast<const unsigned long long*>(counter);
     a.threshold = static_cast<unsigned>(std::floor(static_cast<double>(p) * 4294967296.0 + 0.5));
     a.scale = static_cast<float>(1.0 / (1.0 - static_cast<double>(p)));
-    a.residual = r != nullptr;
     const bool vec = all_aligned(in, M, 16) && all_aligned(r, M, 16) && all_aligned(out, M, 16);
-    if (dtype == GRAWA_BF16) return launch_dropout<__nv_bfloat16>(a, M, vec, stream);
-    if (dtype == GRAWA_F16) return launch_dropout<__half>(a, M, vec, stream);
-    return launch_dropout<float>(a, M, vec, stream);
+    if (dtype == GRAWA_BF16) return launch_dropout<__nv_bfloat16>(a, M, vec, r != nullptr, stream);
+    if (dtype == GRAWA_F16) return launch_dropout<__half>(a, M, vec, r != nullptr, stream);
+    return launch_dropout<float>(a, M, vec, r != nullptr, stream);
 }
 
 // ------------------------------------------------------------------ layer norm

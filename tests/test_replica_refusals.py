@@ -102,3 +102,20 @@ def test_gated_ffn_refusals():
         assert ffn_backward(**kw) == BAD, kw
     for kw in (dict(ws=None), dict(ws_bytes=size(64, 64, 64, 2, True) - 1), dict(ws=0xa0_0000_0080), dict(wu=table(Y[0] + 2), ws_bytes=size(64, 64, 64, 2, True))):
         assert ffn_backward(**kw) == NO_SPACE, kw
+
+
+def test_the_marshaller_names_the_wrong_table():
+    import torch
+    from paper_2403_04206_b200 import build
+    build.build_marshal()
+    from paper_2403_04206_b200 import _marshal
+    x = [torch.zeros(4, 8) for _ in range(2)]
+    for first, specs, error, word in (
+            (x, (("x", x, 4, 8, 1),), ValueError, "current CUDA device"), (x, (("y", None, 4, 8, 0),), TypeError, "y: expected a list"),
+            (x, (("y", x[:1], 4, 8, 0),), ValueError, "one entry per worker"), (x, (("y", [1, 2], 4, 8, 0),), TypeError, "expected tensors"),
+            (x, (("y", [t.half() for t in x], 4, 8, 0),), TypeError, "expected Float, got Half"),
+            ([t.double() for t in x], (), TypeError, "float32, bfloat16 or float16"), ([], (), ValueError, "workers"),
+            (x * 40, (), ValueError, "1 to 64 workers"), (7, (), TypeError, "len"), (x, (("y", 3, 4, 8, 0),), TypeError, "list of tensors")):
+        with pytest.raises(error, match=word):
+            _marshal.tables(first, 0, specs)
+    assert _marshal.tables(x, 0, (("r", None, 4, 8, 2),)) == (0, 0, 8)
