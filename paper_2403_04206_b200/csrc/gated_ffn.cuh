@@ -5,11 +5,14 @@
 //             dx = da Wg + du Wu                                         (one product over both halves)
 //             dWg = da^T x, dWu = du^T x                                 (one launch)
 //
-// All three products run in gemm_kernel: a persistent CTA per SM walks over 128 x 256 tiles; one thread
-// fetches operand tiles by TMA into a ring of shared-memory stages, one thread issues tcgen05.mma, four
-// warps bring finished accumulators from tensor memory to global memory while the next tile is computed
-// (two accumulators of 256 columns take turns).  The forward tile holds 128 columns of a beside the same
-// 128 columns of u, so the activation and the product are taken in the epilogue.
+// All three products run in gemm_kernel: a persistent pair of CTAs (a cluster) per two SMs walks over 256 x 256
+// tiles; each CTA holds 128 rows of A and 128 of the 256 columns of B, so a byte in shared memory feeds twice
+// the products that it feeds in a single CTA (whose 128 x 256 tiles were bound by shared memory: tensor pipe 65
+// to 76 % busy).  In each CTA one thread fetches operand tiles by TMA into a ring of shared-memory stages; one
+// thread of the pair issues tcgen05.mma for both; eight warps of each bring finished accumulators from tensor
+// memory to global memory while the next tile is computed (two accumulators of 256 columns take turns).  The
+// forward tile holds 128 columns of a beside the same 128 columns of u, so the activation and the product are
+// taken in the epilogue.
 //
 // Operands are read in the order in which they stand: rows whose products run along the contiguous index
 // are "K-major" tiles, the others (weights in dx, both operands in dW) "MN-major" tiles of 64 contiguous
@@ -31,13 +34,14 @@ enum Activation { kSilu = 0, kGelu = 1, kRelu = 2 };
 enum GemmMode { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
 
 constexpr int kGemmWorkers = 16;            // workers a launch (their tensor maps travel as kernel parameters)
-constexpr int kTileM = 128, kTileN = 256, kTileK = 64;
-constexpr int kStages = 4;
-constexpr int kABytes = kTileM * kTileK * 2, kBBytes = kTileN * kTileK * 2;
+constexpr int kTileM = 256, kTileN = 256, kTileK = 64;      // of a pair
+constexpr int kHalf = 128;                  // rows of A, and columns of B, that a CTA of the pair holds
+constexpr int kStages = 5;
+constexpr int kABytes = kHalf * kTileK * 2, kBBytes = kHalf * kTileK * 2;
 constexpr int kStageBytes = kABytes + kBBytes;
-constexpr int kGemmSmem = kStages * kStageBytes + 1024;     // 1024: the swizzle pattern wants aligned stages
-constexpr int kGemmThreads = 192;           // warp 0: copies, warp 1: products, warps 2..5: results
-constexpr int kTileGroup = 16;              // tiles along M that are walked through together, for L2
+constexpr int kGemmSmem = kStages * kStageBytes + 8 * 4096 + 1024;     // + results on their way out; the swizzle wants aligned stages
+constexpr int kGemmThreads = 320;           // warp 0: copies, warp 1: products, warps 2..9: results
+constexpr int kTileGroup = 8;               // tiles along M that are walked through together, for L2
 
 struct GemmArgs {
     // kForward: per = x, Wg, Wu.  kInputGrad: common = da, du of all workers, per = Wg, Wu.
@@ -67,9 +71,17 @@ __device__ __forceinline__ void barrier_init(unsigned bar, unsigned count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
-__device__ __forceinline__ void barrier_arrive(unsigned bar)
+// The same place of shared memory in the first CTA of the pair.
+__device__ __forceinline__ unsigned in_leader(unsigned address)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    unsigned r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(address));
+    return r;
+}
+// Arrival at a barrier of either CTA of the pair.
+__device__ __forceinline__ void barrier_arrive(unsigned cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes)
 {
@@ -80,7 +92,7 @@ __device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity)
     unsigned ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
@@ -102,58 +114,58 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
         }
     }
 }
+// Copies into this CTA's shared memory that complete on a barrier of the pair's first CTA.
 __device__ __forceinline__ void copy_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
                  "r"(x), "r"(y), "r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ void copy_3d(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
                  "r"(x), "r"(y), "r"(z), "r"(bar)
                  : "memory");
 }
-// A 16 x 16-bit step of the product: D (+)= A B^T, both operands in shared memory, D in tensor memory.
+// A step of 16 along the sum: D (+)= A B^T, each CTA's halves of both operands in its shared memory, its rows
+// of D in its tensor memory.
 __device__ __forceinline__ void mma_step(unsigned d, unsigned long long a, unsigned long long b, unsigned shape, bool add)
 {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(shape), "r"(add ? 1u : 0u)
         : "memory");
 }
-// The barrier completes when every product this thread has issued so far is done.
+// Arrives at this barrier in both CTAs when every product this thread has issued so far is done.
 __device__ __forceinline__ void mma_commit(unsigned bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"(static_cast<unsigned short>(3))
+                 : "memory");
 }
-// 32 columns of this warp's 32 lanes: a thread gets one row's 32 neighbouring values, which may be used after
-// accumulator_wait (the values pass through it, so that no use can move in front of it).
-__device__ __forceinline__ void accumulator_load(unsigned address, unsigned (&r)[32])
+__device__ __forceinline__ void pair_sync()
 {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-          "=r"(r[30]), "=r"(r[31])
-        : "r"(address));
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void accumulator_wait(unsigned (&r)[32], float (&v)[32])
+// 8 columns of this warp's 32 lanes: a thread gets one row's 8 neighbouring values, which may be used after
+// accumulator_wait (the values pass through it, so that no use can move in front of it).
+__device__ __forceinline__ void accumulator_load(unsigned address, unsigned (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(address));
+}
+__device__ __forceinline__ void accumulator_wait(unsigned (&r)[8], float (&v)[8])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]),
-                   "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
-                   "+r"(r[30]), "+r"(r[31])
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
                  :
                  : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void order_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void order_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -176,6 +188,20 @@ __device__ __forceinline__ float activation(int kind, float a)
     if (kind == kSilu) return __fdividef(a, 1.0f + __expf(-a));
     if (kind == kGelu) return 0.5f * a * (1.0f + erff(a * 0.70710678118654752f));
     return a <= 0.0f ? 0.0f : a;
+}
+// v <- act(v) u, the kind decided once for 8 values.
+__device__ __forceinline__ void gated_product(int kind, float (&v)[8], const float (&u)[8])
+{
+    if (kind == kSilu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = activation(kSilu, v[e]) * u[e];
+    } else if (kind == kGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = activation(kGelu, v[e]) * u[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = activation(kRelu, v[e]) * u[e];
+    }
 }
 // Value and slope.
 __device__ __forceinline__ float2 activation_slope(int kind, float a)
@@ -211,33 +237,59 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& a, int t)
     return r;
 }
 
-// 32 neighbouring results of one row, columns [col, col + 32).
-template <typename T>
-__device__ __forceinline__ void store_results(const GemmArgs& a, void* base, int row, int col, float (&v)[32], bool add)
+// Results go to memory by way of a warp's own 4 KB of shared memory, 32 rows by 64 columns of 16 bits: a thread
+// has a row of the accumulator, but whole 128-byte rows are what global memory takes well.  The 16-byte pieces
+// of a row are permuted so that neither direction meets bank conflicts.  The loops over an accumulator's columns
+// stay rolled, 8 columns a turn: two warps an SM quarter cannot hide the instruction fetches of code that runs
+// once (unrolled over 64 columns, a forward tile's results took 22 thousand cycles, longer than its products).
+constexpr int kStoreCols = 64;
+constexpr int kStoreBytes = 32 * kStoreCols * 2;
+
+__device__ __forceinline__ uint4* store_slot(unsigned char* stage, int row, int piece)
 {
+    return reinterpret_cast<uint4*>(stage + row * 128 + ((piece ^ (row & 7)) * 16));
+}
+
+// Outputs that do not take 16-byte accesses: element by element, neighbouring lanes at neighbouring columns.
+template <typename T, bool TO_MEMORY>
+__device__ __noinline__ void move_elements(unsigned char* stage, T* out, int rows, int cols, int pitch)
+{
+    const int lane = threadIdx.x & 31;
+    for (int r = 0; r < rows; ++r)
+        for (int c = lane; c < cols; c += 32) {
+            T* at = out + static_cast<size_t>(r) * pitch + c;
+            T* in = reinterpret_cast<T*>(store_slot(stage, r, c / 8)) + c % 8;
+            if (TO_MEMORY) *at = *in;
+            else *in = *at;
+        }
+}
+
+// Between the stage and rows [row, row + 32), columns [col, col + 64) of an output, inside its edges.
+template <typename T, bool TO_MEMORY>
+__device__ __forceinline__ void move_stage(const GemmArgs& a, unsigned char* stage, void* base, int row, int col)
+{
+    const int lane = threadIdx.x & 31;
     T* out = static_cast<T*>(base) + static_cast<size_t>(row) * a.cols + col;
+    __syncwarp();
     if (a.words) {                                            // a.cols is a multiple of 8
-        uint4* o = reinterpret_cast<uint4*>(out);
+        const int piece = lane % 8, first = lane / 8;
+        if (col + piece * 8 < a.cols) {
+            uint4* at = reinterpret_cast<uint4*>(out + static_cast<size_t>(first) * a.cols + piece * 8);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (col + 8 * q >= a.cols) break;
-            if (add) {
-                float held[8];
-                unpack<T, 8>(o[q], held);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[8 * q + e] += held[e];
+            for (int i = 0; i < 8; ++i, at += a.cols / 2) {   // 4 rows further
+                if (row + first + 4 * i >= a.rows) break;
+                if (TO_MEMORY) *at = *store_slot(stage, first + 4 * i, piece);
+                else *store_slot(stage, first + 4 * i, piece) = *at;
             }
-            o[q] = pack<T, 8>(v + 8 * q);
         }
     } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (col + e < a.cols) out[e] = narrow<T>(add ? widen(out[e]) + v[e] : v[e]);
+        move_elements<T, TO_MEMORY>(stage, out, min(32, a.rows - row), min(kStoreCols, a.cols - col), a.cols);
     }
+    __syncwarp();
 }
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs a)
 {
     extern __shared__ unsigned char raw[];
@@ -245,68 +297,76 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     __shared__ unsigned tmem_slot;
     __shared__ int gave_up;
 
+    // full and ready are used in the pair's first CTA only, empty, done and drain in each
     const unsigned ring = (smem_address(raw) + 1023u) & ~1023u;
     const unsigned full = smem_address(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, ready = done + 16, drain = ready + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     const int halves = MODE == kInputGrad ? 2 : 1;            // products that add up in one accumulator
     const int blocks = a.k_blocks * halves;
     const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
+    const int first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
-        for (int s = 0; s < 2; ++s) { barrier_init(done + 8 * s, 1); barrier_init(ready + 8 * s, 4); }   // ready: one arrival a warp
+        for (int s = 0; s < 2; ++s) { barrier_init(done + 8 * s, 1); barrier_init(ready + 8 * s, 16); }  // ready: one arrival a warp of the pair
         barrier_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {                                          // all 512 columns: two accumulators of 256
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_address(&tmem_slot)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (warp == 1) {                                          // all 512 columns of both: two accumulators of 256
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_address(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     order_before();
     __syncthreads();
+    pair_sync();                                              // both CTAs' barriers are ready before either is used
     order_after();
     const unsigned tmem = tmem_slot;
 
     if (warp == 0 && lane == 0) {
+        const unsigned leader_full = in_leader(full);
         int fills = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+        for (int t = first; t < tiles && ok; t += stride) {
             const Tile tile = tile_of<MODE>(a, t);
-            const int m0 = tile.m * kTileM, n0 = tile.n * (MODE == kForward ? kTileN / 2 : kTileN);
+            const int m0 = tile.m * kTileM + rank * kHalf;
+            const int n0 = MODE == kForward ? tile.n * kHalf : tile.n * kTileN + rank * kHalf;
             for (int kb = 0; kb < blocks; ++kb, ++fills) {
                 const int s = fills % kStages;
                 if (fills >= kStages && !barrier_wait(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) { ok = false; break; }
-                const unsigned bar = full + 8 * s, sa = ring + s * kStageBytes, sb = sa + kABytes;
+                const unsigned bar = leader_full + 8 * s, sa = ring + s * kStageBytes, sb = sa + kABytes;
                 const int half = MODE == kInputGrad ? kb / a.k_blocks : tile.half;
                 const int k0 = (MODE == kInputGrad ? kb % a.k_blocks : kb) * kTileK;
-                barrier_expect(bar, kStageBytes);
+                if (rank == 0) barrier_expect(full + 8 * s, 2 * kStageBytes);           // the bytes of both CTAs
                 if (MODE == kForward) {
                     copy_2d(sa, &a.per[0][tile.worker], k0, m0, bar);
-                    copy_2d(sb, &a.per[1][tile.worker], k0, n0, bar);
-                    copy_2d(sb + kBBytes / 2, &a.per[2][tile.worker], k0, n0, bar);
+                    copy_2d(sb, &a.per[1 + rank][tile.worker], k0, n0, bar);            // a's columns in one CTA, u's in the other
                 } else if (MODE == kInputGrad) {
                     copy_3d(sa, &a.common[half], k0, m0, a.first_worker + tile.worker, bar);
 #pragma unroll
-                    for (int i = 0; i < kTileN / 64; ++i) copy_2d(sb + i * 8192, &a.per[half][tile.worker], n0 + 64 * i, k0, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[half][tile.worker], n0 + 64 * i, k0, bar);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kTileM / 64; ++i) copy_3d(sa + i * 8192, &a.common[half], m0 + 64 * i, k0, a.first_worker + tile.worker, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_3d(sa + i * 8192, &a.common[half], m0 + 64 * i, k0, a.first_worker + tile.worker, bar);
 #pragma unroll
-                    for (int i = 0; i < kTileN / 64; ++i) copy_2d(sb + i * 8192, &a.per[0][tile.worker], n0 + 64 * i, k0, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[0][tile.worker], n0 + 64 * i, k0, bar);
                 }
             }
         }
-        if (!ok)                                              // copies in flight still write shared memory
+        // The last arrivals at this CTA's barriers come before it leaves.
+        if (ok)
+            for (int f = max(0, fills - kStages); f < fills && ok; ++f) ok = barrier_wait(empty + 8 * (f % kStages), (f / kStages) & 1, &gave_up);
+        // After a wait ran out, copies in flight still write shared memory: the first CTA sees those of both.
+        if (!ok && rank == 0)
             for (int f = max(0, fills - kStages); f < fills; ++f) barrier_wait(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1 && lane == 0 && rank == 0) {
         constexpr bool kAMn = MODE == kWeightGrad, kBMn = MODE != kForward;
         constexpr unsigned shape = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
                                    (kTileN >> 3) << 17 | (kTileM >> 4) << 24;
         constexpr unsigned a_step = (kAMn ? 2048 : 32) >> 4, b_step = (kBMn ? 2048 : 32) >> 4;   // 16 k further
         int used = 0, turn = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++turn) {
+        for (int t = first; t < tiles && ok; t += stride, ++turn) {
             const unsigned d = tmem + (turn & 1) * kTileN;
             if (turn >= 2 && !barrier_wait(ready + 8 * (turn & 1), (turn / 2 - 1) & 1, &gave_up)) { ok = false; break; }
             order_after();
@@ -328,57 +388,73 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         }
     } else if (warp >= 2) {
         const int quarter = warp & 3;                         // the lanes of tensor memory that this warp may read
+        const int part = (warp - 2) / 4;                      // its half of the columns
+        const unsigned leader_ready = in_leader(ready);
+        unsigned char* stage = raw + (ring - smem_address(raw)) + kStages * kStageBytes + (warp - 2) * kStoreBytes;
         int turn = 0;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++turn) {
+        for (int t = first; t < tiles; t += stride, ++turn) {
             const Tile tile = tile_of<MODE>(a, t);
             if (!barrier_wait(done + 8 * (turn & 1), (turn / 2) & 1, &gave_up)) break;
             __syncwarp();
             order_after();
             const unsigned d = tmem + (turn & 1) * kTileN + (static_cast<unsigned>(quarter * 32) << 16);
-            const int row = tile.m * kTileM + quarter * 32 + lane;
+            const int row = tile.m * kTileM + rank * kHalf + quarter * 32;
             if (MODE == kForward) {
-                const int n0 = tile.n * (kTileN / 2);
+                const int c = part * kStoreCols, col = tile.n * kHalf + c;
 #pragma unroll 1
-                for (int c = 0; c < kTileN / 2 && n0 + c < a.cols; c += 32) {
-                    unsigned gr[32], ur[32];
-                    float g[32], u[32];
-                    accumulator_load(d + c, gr);
-                    accumulator_load(d + kTileN / 2 + c, ur);
-                    accumulator_wait(gr, g);
-                    accumulator_wait(ur, u);
-                    if (row < a.rows) {
-                        if (a.out[1][tile.worker]) {
-                            store_results<T>(a, a.out[1][tile.worker], row, n0 + c, g, false);
-                            store_results<T>(a, a.out[2][tile.worker], row, n0 + c, u, false);
+                for (int out = 2; out >= 0; --out) {          // u, a, h
+                    if (a.out[out][tile.worker] == nullptr || row >= a.rows || col >= a.cols) continue;
+#pragma unroll 1
+                    for (int q = 0; q < kStoreCols / 8; ++q) {
+                        unsigned first[8], second[8];
+                        float v[8], u[8];
+                        accumulator_load(d + c + q * 8 + (out == 2 ? kHalf : 0), first);
+                        if (out == 0) accumulator_load(d + c + q * 8 + kHalf, second);
+                        accumulator_wait(first, v);
+                        if (out == 0) {
+                            accumulator_wait(second, u);
+                            gated_product(a.activation, v, u);
                         }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) g[e] = activation(a.activation, g[e]) * u[e];
-                        store_results<T>(a, a.out[0][tile.worker], row, n0 + c, g, false);
+                        *store_slot(stage, lane, q) = pack<T, 8>(v);
                     }
-                    __syncwarp();
+                    move_stage<T, true>(a, stage, a.out[out][tile.worker], row, col);
                 }
             } else {
-                const int n0 = tile.n * kTileN;
+                void* out = a.out[tile.half][tile.worker];
+                const bool add = MODE == kWeightGrad && a.accumulate;
 #pragma unroll 1
-                for (int c = 0; c < kTileN && n0 + c < a.cols; c += 32) {
-                    unsigned r[32];
-                    float v[32];
-                    accumulator_load(d + c, r);
-                    accumulator_wait(r, v);
-                    if (row < a.rows) store_results<T>(a, a.out[tile.half][tile.worker], row, n0 + c, v, a.accumulate != 0);
-                    __syncwarp();
+                for (int c = part * kHalf; c < (part + 1) * kHalf; c += kStoreCols) {
+                    const int col = tile.n * kTileN + c;
+                    if (row >= a.rows || col >= a.cols) break;
+                    if (add) move_stage<T, false>(a, stage, out, row, col);
+#pragma unroll 1
+                    for (int q = 0; q < kStoreCols / 8; ++q) {
+                        unsigned r[8];
+                        float v[8];
+                        accumulator_load(d + c + q * 8, r);
+                        accumulator_wait(r, v);
+                        if (add) {
+                            float held[8];
+                            unpack<T, 8>(*store_slot(stage, lane, q), held);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] += held[e];
+                        }
+                        *store_slot(stage, lane, q) = pack<T, 8>(v);
+                    }
+                    move_stage<T, true>(a, stage, out, row, col);
                 }
             }
             order_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(ready + 8 * (turn & 1));
+            if (lane == 0) barrier_arrive(leader_ready + 8 * (turn & 1));
         }
     }
     __syncwarp();
     order_before();
     __syncthreads();
+    pair_sync();                                              // neither CTA leaves while the other may reach into it
     order_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // ------------------------------------------------------------------ elementwise parts

@@ -265,7 +265,7 @@ static grawa_status launch_gemm(const GemmArgs& a, cudaStream_t stream)
     const int64_t tiles = static_cast<int64_t>(a.workers) * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
     if (tiles > 0x7fffffff - kSms) return GRAWA_ERR_TOO_LARGE;
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
-    return launch(gemm_kernel<T, MODE>, dim3(static_cast<unsigned>(std::min<int64_t>(tiles, kSms))), kGemmThreads, kGemmSmem, stream, false, a);
+    return launch(gemm_kernel<T, MODE>, dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, kSms / 2))), kGemmThreads, kGemmSmem, stream, false, a);
 }
 
 template <int MODE>
@@ -455,7 +455,7 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
         GemmArgs a{};
         a.workers = std::min(kGemmWorkers, M - first);
         a.first_worker = first;
-        a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_hidden, kTileN / 2));
+        a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_hidden, kHalf));
         a.k_blocks = static_cast<int>(ceil_div(d_in, kTileK));
         a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_hidden);
         a.activation = act;
@@ -464,9 +464,9 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
         set_outputs(a, 1, gate_out, first, a.workers);
         set_outputs(a, 2, up_out, first, a.workers);
         for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
-            st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kTileM);
-            if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kTileN / 2);
-            if (st == GRAWA_OK) st = encode_map(&a.per[2][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kTileN / 2);
+            st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kHalf);
+            if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kHalf);
+            if (st == GRAWA_OK) st = encode_map(&a.per[2][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kHalf);
         }
         if (st == GRAWA_OK) st = launch_gemm<kForward>(dtype, a, stream);
     }
@@ -528,8 +528,8 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
             a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_in);
             a.words = d_in % 8 == 0;
             set_outputs(a, 0, dx, first, a.workers);
-            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kTileM);
-            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kTileM);
+            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kHalf);
+            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kHalf);
             for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
                 st = encode_map(&a.per[0][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kTileK);
                 if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kTileK);
