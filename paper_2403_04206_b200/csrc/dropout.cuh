@@ -61,13 +61,13 @@ __device__ __forceinline__ float dropped(float x, float r, unsigned w, const Dro
 }
 
 constexpr int kDropThreads = 256;
-constexpr int kDropCols = 2;                // columns of 16 bytes a thread
 
-// A CTA handles a chunk of kDropThreads * kDropCols columns of 16 bytes, a thread kDropCols of them; the
+// A CTA handles a chunk of kDropThreads * kDropCols columns of 16 bytes, a thread kDropCols of them (4, which
+// shares the head of the rounds and the addresses, where that leaves many chunks for every SM; else 1); the
 // threads of a warp take neighbouring columns.  Whole chunks of 16-byte aligned buffers (VEC) go by vector
 // accesses without bounds checks, the last chunk and unaligned buffers element by element; the counters
 // are the same.
-template <typename T, bool VEC, bool RESIDUAL>
+template <typename T, int kDropCols, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(kDropThreads)
 dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
@@ -108,14 +108,35 @@ dropout_kernel(const __grid_constant__ DropoutArgs a)
             reinterpret_cast<uint4*>(y)[at] = pack<T, VE>(f);
         }
     } else {
+        // A thread computes the words of a block of four elements; through shared memory they reach the lanes that
+        // hold the elements, which are neighbours of their neighbours'.
+        __shared__ uint4 words[kDropThreads / 32][32];
         const int n = static_cast<int>(min(a.n - begin, static_cast<long long>(kChunk)));
-        for (int b = threadIdx.x; b * 4 < n; b += kDropThreads) {
-            const uint4 v = philox(low + b, head, a.keys);
-            const unsigned w[4] = {v.x, v.y, v.z, v.w};
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+        constexpr int kGroups = kChunk / (kDropThreads * 4), kBatch = kGroups < 4 ? kGroups : 4;   // of 128 elements, a warp's
+        for (int g = 0; g < kGroups; g += kBatch) {
+            const int first = (warp * kGroups + g) * 128;
+            if (first >= n) break;
+            T xe[kBatch * 4], re[kBatch * 4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = b * 4 + e;
-                if (j < n) y[j] = narrow<T>(dropped(widen(x[j]), RESIDUAL ? widen(r[j]) : 0.0f, w[e], a));
+            for (int e = 0; e < kBatch * 4; ++e) {            // all loads of the batch first
+                const int j = first + e * 32 + lane;
+                if (j < n) {
+                    xe[e] = x[j];
+                    if (RESIDUAL) re[e] = r[j];
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                __syncwarp();
+                words[warp][lane] = philox(low + (first + b * 128) / 4 + lane, head, a.keys);
+                __syncwarp();
+                const unsigned* w = reinterpret_cast<const unsigned*>(words[warp]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = first + b * 128 + e * 32 + lane;
+                    if (j < n) y[j] = narrow<T>(dropped(widen(xe[b * 4 + e]), RESIDUAL ? widen(re[b * 4 + e]) : 0.0f, w[e * 32 + lane], a));
+                }
             }
         }
     }

@@ -8,8 +8,9 @@
 // row is read once and stays in registers, so the variance is the mean of the squared deviations from
 // the finished mean (two passes over registers), not a difference of two large sums.
 //
-// Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in at most 32 (forward) or 16 to
-// 32 (backward) elements a thread; longer rows are read again from L2 instead.
+// Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in its registers; a warp alone holds
+// up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
+// rows are read again from L2 instead.
 #pragma once
 #include "replica_common.cuh"
 
@@ -21,7 +22,7 @@ struct NormForwardArgs {
     Out y, mean, rstd;
     long long rows, x_stride, y_stride;
     int cols;
-    float eps;
+    float eps, inv_cols;
     int has_gamma, has_beta, has_stats;
 };
 
@@ -31,6 +32,7 @@ struct NormBackwardArgs {
     float* partial;                        // [M][parts][2][cols] when parts > 1
     long long rows, x_stride, y_stride;
     int cols, parts;
+    float inv_cols;
     int has_gamma, has_dx, has_dgamma, has_dbeta, accumulate;
 };
 
@@ -40,6 +42,21 @@ constexpr int kNormLongThreads = 512;      // CTA of the kernels for rows that d
 
 // Sum over the LPR lanes of a row, or (LPR = 0) over the CTA.  `buf` alternates between calls: a CTA needs
 // one barrier per call, because a slot is written again only two calls later.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v, int buf)
+{
+    if constexpr (LPR > 0) {
+        return lanes_sum<LPR>(v);
+    } else {
+        __shared__ float part[2][kNormMaxBlock / 32];
+        v = lanes_sum<32>(v);
+        if ((threadIdx.x & 31) == 0) part[buf][threadIdx.x >> 5] = v;
+        __syncthreads();
+        float t = 0.0f;
+        for (unsigned w = 0; w < blockDim.x / 32; ++w) t += part[buf][w];
+        return t;
+    }
+}
 template <int LPR>
 __device__ __forceinline__ float2 row_sum(float2 v, int buf)
 {
@@ -55,52 +72,49 @@ __device__ __forceinline__ float2 row_sum(float2 v, int buf)
         return t;
     }
 }
-template <int LPR>
-__device__ __forceinline__ float row_sum(float v, int buf)
+
+// 1 / sqrt(v): the fast estimate and one step of Newton's iteration.  (v = 0, a constant row with eps = 0, gives
+// infinity like the plain expression.)
+__device__ __forceinline__ float inverse_root(float v)
 {
-    if constexpr (LPR > 0) return lanes_sum<LPR>(v);
-    else return row_sum<0>(make_float2(v, 0.0f), buf).x;
+    const float r = rsqrtf(v);
+    return v > 0.0f && v < 1e30f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
 // LPR = 8 or 32: that many lanes hold a row, kNormThreads / LPR rows a CTA; LPR = 0: the CTA holds it.
-// A thread holds EPT elements in words of VE.
-template <typename T, int VE, int EPT, int LPR>
+// A thread holds NV words of VE elements.
+template <typename T, int VE, int NV, int LPR>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
 layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
-    constexpr int NV = EPT / VE;
     using W = WordOf<T, VE>;
     const int m = blockIdx.y;
     const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
     const long long row = LPR ? static_cast<long long>(blockIdx.x) * (kNormThreads / (LPR ? LPR : 1)) + threadIdx.x / (LPR ? LPR : 1) : blockIdx.x;
     const bool live = row < a.rows;
-    const int words = live ? a.cols / VE : 0;                 // a group without a row keeps its warp company
+    if (LPR == 32 && !live) return;                           // a whole warp
+    const int words = live ? a.cols / VE : 0;                 // a group of 8 without a row keeps its warp company
     const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + (live ? row : 0) * a.x_stride);
 
     W xw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (lane + i * lanes < words) xw[i] = x[lane + i * lanes];
-    float sum = 0.0f;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (lane + i * lanes < words) add_elements<T, VE>(xw[i], sum);
+    const float mean = row_sum<LPR>(sum[0] + sum[1], 0) * a.inv_cols;
+    float square[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (lane + i * lanes >= words) continue;
         float f[VE];
-        unpack<T, VE>(xw[i], f);
+        shifted<T, VE>(xw[i], -mean, f);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sum += f[e];
+        for (int e = 0; e < VE; ++e) square[e % 2] = fmaf(f[e], f[e], square[e % 2]);
     }
-    const float mean = row_sum<LPR>(sum, 0) / a.cols;
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (lane + i * lanes >= words) continue;
-        float f[VE];
-        unpack<T, VE>(xw[i], f);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) squares = fmaf(f[e] - mean, f[e] - mean, squares);
-    }
-    const float rstd = 1.0f / sqrtf(row_sum<LPR>(squares, 1) / a.cols + a.eps);
+    const float rstd = inverse_root(fmaf(row_sum<LPR>(square[0] + square[1], 1), a.inv_cols, a.eps));
     if (!live) return;
     if (a.has_stats && lane == 0) {
         static_cast<float*>(a.mean.p[m])[row] = mean;
@@ -110,29 +124,33 @@ layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
     const W* beta = static_cast<const W*>(a.beta.p[m]);
     const T* gamma1 = static_cast<const T*>(a.gamma.p[m]);
     const T* beta1 = static_cast<const T*>(a.beta.p[m]);
-    const bool words_ok = ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) % sizeof(W)) == 0;
+    const bool words_ok = a.has_gamma && a.has_beta && ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) % sizeof(W)) == 0;
     W* y = reinterpret_cast<W*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride);
+    if (words_ok) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = lane + i * lanes;
-        if (at >= words) continue;
-        float f[VE], g[VE], b[VE] = {};
+        for (int i = 0; i < NV; ++i) {
+            const int at = lane + i * lanes;
+            if (at >= words) continue;
+            float f[VE], g[VE], b[VE];
+            unpack<T, VE>(gamma[at], g);
+            unpack<T, VE>(beta[at], b);
+            shifted<T, VE>(xw[i], -mean, f);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) g[e] = 1.0f;
-        if (words_ok) {
-            if (a.has_gamma) unpack<T, VE>(gamma[at], g);
-            if (a.has_beta) unpack<T, VE>(beta[at], b);
-        } else {                                              // parameters inside a flat vector stand anywhere
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                if (a.has_gamma) g[e] = widen(gamma1[at * VE + e]);
-                if (a.has_beta) b[e] = widen(beta1[at * VE + e]);
-            }
+            for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
+            y[at] = pack<T, VE>(f);
         }
-        unpack<T, VE>(xw[i], f);
+    } else {                                                  // parameters inside a flat vector stand anywhere, or there are none
 #pragma unroll
-        for (int e = 0; e < VE; ++e) f[e] = fmaf((f[e] - mean) * rstd, g[e], b[e]);
-        y[at] = pack<T, VE>(f);
+        for (int i = 0; i < NV; ++i) {
+            const int at = lane + i * lanes;
+            if (at >= words) continue;
+            float f[VE];
+            shifted<T, VE>(xw[i], -mean, f);
+#pragma unroll
+            for (int e = 0; e < VE; ++e)
+                f[e] = fmaf(f[e] * rstd, a.has_gamma ? widen(gamma1[at * VE + e]) : 1.0f, a.has_beta ? widen(beta1[at * VE + e]) : 0.0f);
+            y[at] = pack<T, VE>(f);
+        }
     }
 }
 
@@ -154,14 +172,14 @@ layernorm_forward_long_kernel(const __grid_constant__ NormForwardArgs a)
 #pragma unroll
         for (int e = 0; e < VE; ++e) sum += f[e];
     }
-    const float mean = row_sum<0>(sum, 0) / a.cols;
+    const float mean = row_sum<0>(sum, 0) * a.inv_cols;
     float squares = 0.0f;
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
         unpack<T, VE>(x[at], f);
 #pragma unroll
         for (int e = 0; e < VE; ++e) squares = fmaf(f[e] - mean, f[e] - mean, squares);
     }
-    const float rstd = 1.0f / sqrtf(row_sum<0>(squares, 1) / a.cols + a.eps);
+    const float rstd = inverse_root(fmaf(row_sum<0>(squares, 1), a.inv_cols, a.eps));
     if (a.has_stats && threadIdx.x == 0) {
         static_cast<float*>(a.mean.p[m])[row] = mean;
         static_cast<float*>(a.rstd.p[m])[row] = rstd;
@@ -203,6 +221,16 @@ __device__ __forceinline__ void store_column(const NormBackwardArgs& a, int m, i
     }
 }
 
+// Rows under way: 16-byte words are staged through shared memory by asynchronous copies, kNormDepth rows ahead of
+// the one that is computed (registers are full of column sums; one row ahead in registers left the SM waiting
+// for memory), each thread its own words, so that no barrier is needed.
+template <typename T, int VE, int EPT> struct NormStage {
+    static constexpr bool staged = VE * sizeof(T) == 16;
+    static constexpr int words = EPT / VE;
+    static constexpr int depth = words <= 3 ? 4 : words <= 4 ? 3 : 2;
+    static constexpr size_t bytes_a_thread = staged ? depth * 2 * words * 16 : 0;
+};
+
 // gridDim.x CTAs a worker go through its rows in turn; a thread keeps the sums of its own columns in
 // registers over all of them, so the weights' gradients cost one small table at the end and no atomics
 // (the split depends on the sizes alone: the same bits every time).
@@ -210,49 +238,80 @@ template <typename T, int VE, int EPT, int LPR>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
 layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 {
+    using Stage = NormStage<T, VE, EPT>;
     constexpr int NV = EPT / VE;
     constexpr int GROUPS = LPR ? kNormThreads / (LPR ? LPR : 1) : 1;
     using W = WordOf<T, VE>;
+    extern __shared__ uint4 ring[];                           // [depth][x, dy][NV][threads]
     const int m = blockIdx.y;
     const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
     const int group = LPR ? threadIdx.x / (LPR ? LPR : 1) : 0;
     const int words = a.cols / VE;
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
+    const T* xs = static_cast<const T*>(a.x.p[m]);
+    const T* dys = static_cast<const T*>(a.dy.p[m]);
     const float* means = static_cast<const float*>(a.mean.p[m]);
     const float* rstds = static_cast<const float*>(a.rstd.p[m]);
-    const float inv = 1.0f / a.cols;
 
-    T gm[EPT];
-    float dg[EPT], db[EPT];
+    float gm[EPT], dg[EPT], db[EPT];
 #pragma unroll
     for (int k = 0; k < EPT; ++k) {
         const int at = lane + k / VE * lanes;
-        gm[k] = a.has_gamma && at < words ? gamma[at * VE + k % VE] : narrow<T>(1.0f);
+        gm[k] = a.has_gamma && at < words ? widen(gamma[at * VE + k % VE]) : 1.0f;
         dg[k] = db[k] = 0.0f;
     }
-    int buf = 0;
-    for (long long base = static_cast<long long>(blockIdx.x) * GROUPS; base < a.rows; base += static_cast<long long>(gridDim.x) * GROUPS) {
-        const long long row = base + group;
-        const bool live = row < a.rows;
-        const int w_end = live ? words : 0;
-        const long long r = live ? row : 0;
-        const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + r * a.x_stride);
-        const W* dy = reinterpret_cast<const W*>(static_cast<const T*>(a.dy.p[m]) + r * a.y_stride);
-        W xw[NV], yw[NV];
+    const long long stride = static_cast<long long>(gridDim.x) * GROUPS;
+    long long row = static_cast<long long>(blockIdx.x) * GROUPS + group;
+    const auto fetch = [&](int slot, long long r) {
+        if (r < a.rows) {
+            const W* x = reinterpret_cast<const W*>(xs + r * a.x_stride) + lane;
+            const W* dy = reinterpret_cast<const W*>(dys + r * a.y_stride) + lane;
+            uint4* to = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (lane + i * lanes < w_end) { xw[i] = x[lane + i * lanes]; yw[i] = dy[lane + i * lanes]; }
-        const float mean = means[r], rstd = rstds[r];
+            for (int i = 0; i < NV; ++i)
+                if (lane + i * lanes < words) {
+                    copy_async16(to + i * blockDim.x, x + i * lanes);
+                    copy_async16(to + (NV + i) * blockDim.x, dy + i * lanes);
+                }
+        }
+        copy_async_commit();                                  // a group a row, also where there is none
+    };
+    if constexpr (Stage::staged) {
+#pragma unroll
+        for (int d = 0; d < Stage::depth - 1; ++d) fetch(d, row + d * stride);
+    }
+    int buf = 0, slot = 0;
+    float mean = row < a.rows ? means[row] : 0.0f, rstd = row < a.rows ? rstds[row] : 0.0f;
+    for (; row - group < a.rows; row += stride) {             // the same turns for all groups of the CTA
+        const int w_end = row < a.rows ? words : 0;
+        W xw[NV], dw[NV];
+        if constexpr (Stage::staged) {
+            fetch(slot == 0 ? Stage::depth - 1 : slot - 1, row + (Stage::depth - 1) * stride);
+            copy_async_wait<Stage::depth - 1>();
+            const uint4* from = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (lane + i * lanes < w_end) { xw[i] = from[i * blockDim.x]; dw[i] = from[(NV + i) * blockDim.x]; }
+            slot = slot + 1 == Stage::depth ? 0 : slot + 1;
+        } else {
+            const W* x = reinterpret_cast<const W*>(xs + row * a.x_stride) + lane;
+            const W* dy = reinterpret_cast<const W*>(dys + row * a.y_stride) + lane;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (lane + i * lanes < w_end) { xw[i] = x[i * lanes]; dw[i] = dy[i * lanes]; }
+        }
+        const bool more = row + stride < a.rows;
+        const float next_mean = more ? means[row + stride] : 0.0f, next_rstd = more ? rstds[row + stride] : 0.0f;
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (lane + i * lanes >= w_end) continue;
             float f[VE], d[VE];
-            unpack<T, VE>(xw[i], f);
-            unpack<T, VE>(yw[i], d);
+            shifted<T, VE>(xw[i], -mean, f);
+            unpack<T, VE>(dw[i], d);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
-                const float h = (f[e] - mean) * rstd, g = d[e] * widen(gm[i * VE + e]);
+                const float h = f[e] * rstd, g = d[e] * gm[i * VE + e];
                 s.x += g;
                 s.y = fmaf(g, h, s.y);
                 dg[i * VE + e] = fmaf(d[e], h, dg[i * VE + e]);
@@ -262,23 +321,23 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
         if (a.has_dx) {
             s = row_sum<LPR>(s, buf);
             buf ^= 1;
-            const float mg = s.x * inv, mgh = s.y * inv;
-            W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + r * a.x_stride);
+            const float mg = -s.x * a.inv_cols * rstd, mgh = -s.y * a.inv_cols * rstd * rstd;
+            W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + row * a.x_stride) + lane;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (lane + i * lanes >= w_end) continue;
                 float f[VE], d[VE];
-                unpack<T, VE>(xw[i], f);
-                unpack<T, VE>(yw[i], d);
+                shifted<T, VE>(xw[i], -mean, f);
+                unpack<T, VE>(dw[i], d);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const float h = (f[e] - mean) * rstd;
-                    f[e] = (fmaf(d[e], widen(gm[i * VE + e]), -mg) - h * mgh) * rstd;
-                }
-                dx[lane + i * lanes] = pack<T, VE>(f);
+                for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e], mgh, mg));
+                dx[i * lanes] = pack<T, VE>(f);
             }
         }
+        mean = next_mean;
+        rstd = next_rstd;
     }
+    if constexpr (Stage::staged) copy_async_wait<0>();
     if (!a.has_dgamma && !a.has_dbeta) return;
     if constexpr (LPR == 0) {
 #pragma unroll
@@ -341,7 +400,7 @@ layernorm_backward_long_kernel(const __grid_constant__ NormBackwardArgs a)
         }
     }
     s = row_sum<0>(s, 0);
-    const float mg = s.x / a.cols, mgh = s.y / a.cols;
+    const float mg = s.x * a.inv_cols, mgh = s.y * a.inv_cols;
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
         unpack<T, VE>(x[at], f);
         unpack<T, VE>(dy[at], d);

@@ -89,6 +89,64 @@ __device__ __forceinline__ WordOf<T, VE> pack(const float* o)
     }
 }
 
+// o[e] = element e + c, and acc[e % 2] += element e.  For 16-bit elements these are single instructions that
+// take the 16-bit source as it is (widened exactly, one rounding), so nothing is unpacked first.
+__device__ __forceinline__ void pair_add(unsigned w, float c, float* o, __nv_bfloat16)
+{
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %3;\n\tadd.rn.f32.bf16 %1, h, %3;\n\t}"
+        : "=f"(o[0]), "=f"(o[1]) : "r"(w), "f"(c));
+}
+__device__ __forceinline__ void pair_add(unsigned w, float c, float* o, __half)
+{
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %3;\n\tadd.rn.f32.f16 %1, h, %3;\n\t}"
+        : "=f"(o[0]), "=f"(o[1]) : "r"(w), "f"(c));
+}
+__device__ __forceinline__ void pair_sum(unsigned w, float* acc, __nv_bfloat16)
+{
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}"
+        : "+f"(acc[0]), "+f"(acc[1]) : "r"(w));
+}
+__device__ __forceinline__ void pair_sum(unsigned w, float* acc, __half)
+{
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t}"
+        : "+f"(acc[0]), "+f"(acc[1]) : "r"(w));
+}
+template <typename T, int VE>
+__device__ __forceinline__ void shifted(const WordOf<T, VE>& w, float c, float* o)
+{
+    if constexpr (sizeof(T) == 2 && VE == 8) {
+        pair_add(w.x, c, o, T{}); pair_add(w.y, c, o + 2, T{}); pair_add(w.z, c, o + 4, T{}); pair_add(w.w, c, o + 6, T{});
+    } else if constexpr (sizeof(T) == 2 && VE == 2) {
+        pair_add(w, c, o, T{});
+    } else {
+        unpack<T, VE>(w, o);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) o[e] += c;
+    }
+}
+template <typename T, int VE>
+__device__ __forceinline__ void add_elements(const WordOf<T, VE>& w, float (&acc)[2])
+{
+    if constexpr (sizeof(T) == 2 && VE == 8) {
+        pair_sum(w.x, acc, T{}); pair_sum(w.y, acc, T{}); pair_sum(w.z, acc, T{}); pair_sum(w.w, acc, T{});
+    } else if constexpr (sizeof(T) == 2 && VE == 2) {
+        pair_sum(w, acc, T{});
+    } else {
+        float o[VE];
+        unpack<T, VE>(w, o);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e % 2] += o[e];
+    }
+}
+
+// 16 bytes from global to shared memory behind this thread's back; a thread waits for its own copies.
+__device__ __forceinline__ void copy_async16(void* shared, const void* global)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<unsigned>(__cvta_generic_to_shared(shared))), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
 // Sum over groups of LPR neighbouring lanes (a power of two up to 32); every lane gets it.  All 32 lanes take part.
 template <int LPR>
 __device__ __forceinline__ float lanes_sum(float v)

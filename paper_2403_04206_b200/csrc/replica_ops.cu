@@ -29,14 +29,21 @@ static bool all_aligned(const void* const* table, int M, size_t bytes)
 
 // ------------------------------------------------------------------ dropout
 
+template <typename T, int COLS>
+static grawa_status launch_dropout(const DropoutArgs& a, int M, bool vec, bool residual, cudaStream_t stream)
+{
+    const int64_t ctas = ceil_div(a.n, kDropThreads * COLS * (16 / static_cast<int>(sizeof(T))));
+    if (ctas > 0x7fffffff) return GRAWA_ERR_INVALID_ARG;
+    auto* const kernel = vec ? (residual ? dropout_kernel<T, COLS, true, true> : dropout_kernel<T, COLS, true, false>)
+                             : (residual ? dropout_kernel<T, COLS, false, true> : dropout_kernel<T, COLS, false, false>);
+    return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0, stream, false, a);
+}
+
 template <typename T>
 static grawa_status launch_dropout(const DropoutArgs& a, int M, bool vec, bool residual, cudaStream_t stream)
 {
-    const int64_t ctas = ceil_div(a.n, kDropThreads * kDropCols * (16 / static_cast<int>(sizeof(T))));
-    if (ctas > 0x7fffffff) return GRAWA_ERR_INVALID_ARG;
-    auto* const kernel = vec ? (residual ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>)
-                             : (residual ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>);
-    return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0, stream, false, a);
+    const int64_t columns = ceil_div(a.n, kDropThreads * (16 / static_cast<int>(sizeof(T)))) * M;
+    return columns >= 4 * 16 * kSms ? launch_dropout<T, 4>(a, M, vec, residual, stream) : launch_dropout<T, 1>(a, M, vec, residual, stream);
 }
 
 // `in` and `r` may each be the same buffer as `out` (every element is read before it is written, by one thread).
@@ -109,16 +116,25 @@ static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStr
     const auto lanes = [&](auto kernel, int lpr) {
         return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, false, a);
     };
-    const auto block = [&](auto kernel, int ept) {
-        return launch(kernel, dim3(static_cast<unsigned>(a.rows), M), static_cast<int>(ceil_div(a.cols, 32 * ept)) * 32, 0, stream, false, a);
-    };
-    if (a.cols <= 64) return lanes(layernorm_forward_kernel<T, VE, 8, 8>, 8);
-    if (a.cols <= 256) return lanes(layernorm_forward_kernel<T, VE, 8, 32>, 32);
-    if (a.cols <= 512) return lanes(layernorm_forward_kernel<T, VE, 16, 32>, 32);
-    if (a.cols <= 768) return lanes(layernorm_forward_kernel<T, VE, 24, 32>, 32);
-    if (a.cols <= 1024) return lanes(layernorm_forward_kernel<T, VE, 32, 32>, 32);
-    if (a.cols <= kLongForward / 2) return block(layernorm_forward_kernel<T, VE, 16, 0>, 16);
-    if (a.cols <= kLongForward) return block(layernorm_forward_kernel<T, VE, 32, 0>, 32);
+    if (a.cols <= 64) return lanes(layernorm_forward_kernel<T, VE, 8 / VE, 8>, 8);
+    // A warp a row, as long as a lane's words fit in its registers.
+    const int64_t per_lane = ceil_div(a.cols / VE, 32);
+    if constexpr (VE >= 4) {
+        if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, VE, 1, 32>, 32);
+        if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, VE, 2, 32>, 32);
+        if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, VE, 3, 32>, 32);
+        if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, VE, 4, 32>, 32);
+        if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, VE, 6, 32>, 32);
+        if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, VE, 8, 32>, 32);
+        if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, VE, 12, 32>, 32);
+        if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, VE, 16, 32>, 32);
+    } else {
+        if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, VE, 8, 32>, 32);
+        if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, VE, 16, 32>, 32);
+        if (per_lane <= 32) return lanes(layernorm_forward_kernel<T, VE, 32, 32>, 32);
+    }
+    if (a.cols <= kLongForward)
+        return launch(layernorm_forward_kernel<T, VE, 32 / VE, 0>, dim3(static_cast<unsigned>(a.rows), M), static_cast<int>(ceil_div(a.cols, 32 * 32)) * 32, 0, stream, false, a);
     return launch(layernorm_forward_long_kernel<T, VE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
 }
 
@@ -128,7 +144,7 @@ static int norm_groups(int64_t cols) { return cols <= 64 ? kNormThreads / 8 : co
 // CTAs a worker's rows are split over in the backward pass (a rule on the sizes alone, so that the order of
 // the additions does not change from call to call).  Few rows go to one CTA, which then writes the
 // gradients itself: the second launch costs more than a few rows one after the other.
-static int norm_parts(int64_t rows, int64_t cols, int M)
+static int norm_parts(int64_t rows, int64_t cols, int M, int64_t elem)
 {
     if (cols > kLongBackward) {
         const int64_t want = std::max<int64_t>(1, 8 * kSms / std::max<int64_t>(1, M * ceil_div(cols, kNormThreads)));
@@ -136,22 +152,30 @@ static int norm_parts(int64_t rows, int64_t cols, int M)
     }
     const int64_t steps = ceil_div(rows, norm_groups(cols));
     if (steps <= 4) return 1;
-    const int64_t threads = cols <= 1024 ? kNormThreads : ceil_div(cols, 32 * 16) * 32;
-    const int64_t resident = kSms * std::max<int64_t>(1, 512 / threads);
-    return static_cast<int>(std::max<int64_t>(1, std::min(steps, resident / M)));
+    // as many CTAs as their registers and stages let an SM hold at once
+    const bool narrow = elem == 2;
+    const int64_t per_sm = cols <= 256 ? 6 : cols <= 512 ? (narrow ? 5 : 4) : cols <= 768 ? (narrow ? 4 : 3) : cols <= 1024 ? (narrow ? 3 : 2)
+                           : 512 / (ceil_div(cols, 32 * 16) * 32);
+    return static_cast<int>(std::max<int64_t>(1, std::min(steps, kSms * per_sm / M)));
+}
+
+template <typename T, int VE, int EPT, int LPR>
+static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
+{
+    const size_t smem = NormStage<T, VE, EPT>::bytes_a_thread * block;
+    if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(layernorm_backward_kernel<T, VE, EPT, LPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    return launch(layernorm_backward_kernel<T, VE, EPT, LPR>, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a);
 }
 
 template <typename T, int VE>
 static grawa_status launch_norm_backward(const NormBackwardArgs& a, int M, cudaStream_t stream)
 {
-    const dim3 grid(static_cast<unsigned>(a.parts), M);
-    const int block = static_cast<int>(ceil_div(a.cols, 32 * 16)) * 32;
-    if (a.cols <= 64) return launch(layernorm_backward_kernel<T, VE, 8, 8>, grid, kNormThreads, 0, stream, false, a);
-    if (a.cols <= 256) return launch(layernorm_backward_kernel<T, VE, 8, 32>, grid, kNormThreads, 0, stream, false, a);
-    if (a.cols <= 512) return launch(layernorm_backward_kernel<T, VE, 16, 32>, grid, kNormThreads, 0, stream, false, a);
-    if (a.cols <= 768) return launch(layernorm_backward_kernel<T, VE, 24, 32>, grid, kNormThreads, 0, stream, false, a);
-    if (a.cols <= 1024) return launch(layernorm_backward_kernel<T, VE, 32, 32>, grid, kNormThreads, 0, stream, false, a);
-    if (a.cols <= kLongBackward) return launch(layernorm_backward_kernel<T, VE, 16, 0>, grid, block, 0, stream, false, a);
+    if (a.cols <= 64) return launch_norm_rows<T, VE, 8, 8>(a, M, kNormThreads, stream);
+    if (a.cols <= 256) return launch_norm_rows<T, VE, 8, 32>(a, M, kNormThreads, stream);
+    if (a.cols <= 512) return launch_norm_rows<T, VE, 16, 32>(a, M, kNormThreads, stream);
+    if (a.cols <= 768) return launch_norm_rows<T, VE, 24, 32>(a, M, kNormThreads, stream);
+    if (a.cols <= 1024) return launch_norm_rows<T, VE, 32, 32>(a, M, kNormThreads, stream);
+    if (a.cols <= kLongBackward) return launch_norm_rows<T, VE, 16, 0>(a, M, static_cast<int>(ceil_div(a.cols, 32 * 16)) * 32, stream);
     if (a.has_dx) {
         const grawa_status st = launch(layernorm_backward_long_kernel<T, VE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
         if (st != GRAWA_OK) return st;
@@ -359,7 +383,7 @@ grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void* const* x, co
     copy_table(a.rstd, rstd, M);
     a.rows = rows; a.cols = static_cast<int>(cols);
     a.x_stride = x_stride; a.y_stride = y_stride;
-    a.eps = eps;
+    a.eps = eps; a.inv_cols = 1.0f / static_cast<float>(cols);
     a.has_gamma = gamma != nullptr; a.has_beta = beta != nullptr; a.has_stats = mean != nullptr;
     const int ve = word_elems(elem, cols, x_stride, y_stride, x, y, nullptr, M);
     if (dtype == GRAWA_BF16) return norm_forward<__nv_bfloat16>(a, M, ve, stream);
@@ -370,7 +394,7 @@ grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void* const* x, co
 size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M)
 {
     if (!shape_ok(rows, cols, cols, cols, M, 4)) return 0;
-    const int parts = norm_parts(rows, cols, M);
+    const int parts = norm_parts(rows, cols, M, 2);            // 16-bit storage takes the most
     return parts == 1 ? 0 : static_cast<size_t>(M) * parts * 2 * cols * sizeof(float);
 }
 
@@ -409,9 +433,9 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     copy_table(a.dgamma, dgamma, M);
     copy_table(a.dbeta, dbeta, M);
     a.partial = static_cast<float*>(workspace);
-    a.rows = rows; a.cols = static_cast<int>(cols);
+    a.rows = rows; a.cols = static_cast<int>(cols); a.inv_cols = 1.0f / static_cast<float>(cols);
     a.x_stride = x_stride; a.y_stride = y_stride;
-    a.parts = rows == 0 ? 0 : norm_parts(rows, cols, M);
+    a.parts = rows == 0 ? 0 : norm_parts(rows, cols, M, elem);
     a.has_gamma = gamma != nullptr; a.has_dx = dx != nullptr; a.has_dgamma = dgamma != nullptr; a.has_dbeta = dbeta != nullptr;
     a.accumulate = accumulate != 0;
     const int ve = word_elems(elem, cols, x_stride, y_stride, x, dy, dx, M);
