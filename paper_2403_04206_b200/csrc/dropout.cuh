@@ -95,8 +95,8 @@ dropout_kernel(const __grid_constant__ DropoutArgs a)
         for (int c = 0; c < kDropCols; ++c) {
             const unsigned at = threadIdx.x + c * kDropThreads;
             float f[VE], g[VE] = {};
-            unpack<T, VE>(xw[c], f);
-            if (RESIDUAL) unpack<T, VE>(rw[c], g);
+            unpack<T>(xw[c], f);
+            if (RESIDUAL) unpack<T>(rw[c], g);
 #pragma unroll
             for (int q = 0; q < VE / 4; ++q) {
                 const uint4 w = philox(low + at * (VE / 4) + q, head, a.keys);
@@ -105,7 +105,7 @@ dropout_kernel(const __grid_constant__ DropoutArgs a)
                 f[4 * q + 2] = dropped(f[4 * q + 2], g[4 * q + 2], w.z, a);
                 f[4 * q + 3] = dropped(f[4 * q + 3], g[4 * q + 3], w.w, a);
             }
-            reinterpret_cast<uint4*>(y)[at] = pack<T, VE>(f);
+            reinterpret_cast<uint4*>(y)[at] = pack<T>(f);
         }
     } else {
         // A thread computes the words of a block of four elements; through shared memory they reach the lanes that

@@ -415,7 +415,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                             accumulator_wait(second, u);
                             gated_product(a.activation, v, u);
                         }
-                        *store_slot(stage, lane, q) = pack<T, 8>(v);
+                        *store_slot(stage, lane, q) = pack<T>(v);
                     }
                     move_stage<T, true>(a, stage, a.out[out][tile.worker], row, col);
                 }
@@ -435,11 +435,11 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                         accumulator_wait(r, v);
                         if (add) {
                             float held[8];
-                            unpack<T, 8>(*store_slot(stage, lane, q), held);
+                            unpack<T>(*store_slot(stage, lane, q), held);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) v[e] += held[e];
                         }
-                        *store_slot(stage, lane, q) = pack<T, 8>(v);
+                        *store_slot(stage, lane, q) = pack<T>(v);
                     }
                     move_stage<T, true>(a, stage, out, row, col);
                 }
@@ -463,35 +463,35 @@ struct GatedGradArgs {
     In dh, gate, up;
     void *da, *du;                         // [M][rows][pitch]
     long long rows;
-    int cols, pitch, activation, words;
+    int cols, pitch, activation;
 };
 
 constexpr int kGatedThreads = 256;
 
-// da = dh u act'(a), du = dh act(a): bound by memory, 5 elements of traffic an element.  A thread handles 8
-// neighbouring elements of a row.
-template <typename T>
+// da = dh u act'(a), du = dh act(a): bound by memory, 5 elements of traffic an element.  WORDS: a thread handles 8
+// neighbouring elements of a row (16-byte accesses); else a warp handles 256, lane by lane.
+template <typename T, bool WORDS>
 __global__ void __launch_bounds__(kGatedThreads)
 gated_grad_kernel(const __grid_constant__ GatedGradArgs a)
 {
-    const int m = blockIdx.y, per_row = a.pitch / 8;
+    const int m = blockIdx.y, lane = threadIdx.x & 31, per_row = WORDS ? a.pitch / 8 : (a.pitch + 255) / 256 * 32;
     const long long at = static_cast<long long>(blockIdx.x) * kGatedThreads + threadIdx.x;
-    if (at >= a.rows * per_row) return;
     const long long row = at / per_row;
-    const int col = static_cast<int>(at % per_row) * 8;
+    if (row >= a.rows) return;
+    const int col = WORDS ? static_cast<int>(at % per_row) * 8 : static_cast<int>(at % per_row) / 32 * 256 + lane;
     const long long in = row * a.cols + col;
     const T* dh = static_cast<const T*>(a.dh.p[m]) + in;
     const T* gate = static_cast<const T*>(a.gate.p[m]) + in;
     const T* up = static_cast<const T*>(a.up.p[m]) + in;
     float d[8] = {}, g[8] = {}, u[8] = {};
-    if (a.words) {
-        unpack<T, 8>(*reinterpret_cast<const uint4*>(dh), d);
-        unpack<T, 8>(*reinterpret_cast<const uint4*>(gate), g);
-        unpack<T, 8>(*reinterpret_cast<const uint4*>(up), u);
+    if (WORDS) {
+        unpack<T>(*reinterpret_cast<const uint4*>(dh), d);
+        unpack<T>(*reinterpret_cast<const uint4*>(gate), g);
+        unpack<T>(*reinterpret_cast<const uint4*>(up), u);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (col + e < a.cols) { d[e] = widen(dh[e]); g[e] = widen(gate[e]); u[e] = widen(up[e]); }
+            if (col + 32 * e < a.cols) { d[e] = widen(dh[32 * e]); g[e] = widen(gate[32 * e]); u[e] = widen(up[32 * e]); }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -500,18 +500,28 @@ gated_grad_kernel(const __grid_constant__ GatedGradArgs a)
         g[e] = d[e] * f.x;
     }
     const size_t out = (static_cast<size_t>(m) * a.rows + row) * a.pitch + col;
-    *reinterpret_cast<uint4*>(static_cast<T*>(a.da) + out) = pack<T, 8>(u);
-    *reinterpret_cast<uint4*>(static_cast<T*>(a.du) + out) = pack<T, 8>(g);
+    T* da = static_cast<T*>(a.da) + out;
+    T* du = static_cast<T*>(a.du) + out;
+    if (WORDS) {
+        *reinterpret_cast<uint4*>(da) = pack<T>(u);
+        *reinterpret_cast<uint4*>(du) = pack<T>(g);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (col + 32 * e < a.cols) { da[32 * e] = narrow<T>(u[e]); du[32 * e] = narrow<T>(g[e]); }
+    }
 }
 
 struct PackArgs {
-    In from;
-    unsigned short* to;                    // [M][rows][pitch]
+    In from[2];
+    unsigned short* to[2];                 // [M][rows][pitch]
     long long rows;
     int cols, pitch;
 };
 
-// Rows of 16-bit elements at any address, laid out again with 16-byte aligned rows, as TMA wants them.
+// Rows of 16-bit elements at any address, laid out again with 16-byte aligned rows, as TMA wants them: gridDim.z
+// operands of one shape.  A thread makes one 16-byte word of the result from the two aligned words that hold its
+// elements (each of which holds at least one of them, so nothing outside the operand's own words is read).
 static __global__ void __launch_bounds__(kGatedThreads)
 pack_rows_kernel(const __grid_constant__ PackArgs a)
 {
@@ -519,13 +529,9 @@ pack_rows_kernel(const __grid_constant__ PackArgs a)
     const long long at = static_cast<long long>(blockIdx.x) * kGatedThreads + threadIdx.x;
     if (at >= a.rows * per_row) return;
     const long long row = at / per_row;
-    const int col = static_cast<int>(at % per_row) * 8;
-    const unsigned short* from = static_cast<const unsigned short*>(a.from.p[m]) + row * a.cols + col;
-    unsigned short v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = col + e < a.cols ? from[e] : static_cast<unsigned short>(0);
-    *reinterpret_cast<uint4*>(a.to + (static_cast<size_t>(m) * a.rows + row) * a.pitch + col) =
-        make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    const int col = static_cast<int>(at % per_row) * 8, count = min(8, a.cols - col);
+    const uint4 v = load_halves(static_cast<const unsigned short*>(a.from[blockIdx.z].p[m]) + row * a.cols + col, count);
+    *reinterpret_cast<uint4*>(a.to[blockIdx.z] + (static_cast<size_t>(m) * a.rows + row) * a.pitch + col) = v;
 }
 
 }  // namespace replica

@@ -10,7 +10,8 @@
 //
 // Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in its registers; a warp alone holds
 // up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
-// rows are read again from L2 instead.
+// rows are read again from L2 instead.  WHOLE kernels are for rows of whole 16-byte words at 16-byte boundaries;
+// the others put the words of rows of any length and address together from aligned ones.
 #pragma once
 #include "replica_common.cuh"
 
@@ -29,9 +30,10 @@ struct NormForwardArgs {
 struct NormBackwardArgs {
     In dy, x, gamma, mean, rstd;
     Out dx, dgamma, dbeta;
-    float* partial;                        // [M][parts][2][cols] when parts > 1
+    float* partial;                        // [M][parts][2][slots] when parts > 1
     long long rows, x_stride, y_stride;
     int cols, parts;
+    int slots, lanes, word;                // slot j of a part holds the column that slot_column(j) names
     float inv_cols;
     int has_gamma, has_dx, has_dgamma, has_dbeta, accumulate;
 };
@@ -81,115 +83,235 @@ __device__ __forceinline__ float inverse_root(float v)
     return v > 0.0f && v < 1e30f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
+// Rows are read and written once, with the streaming hint (4 x 8192 x 4096 bf16: 95 us, 103 to 113 us without).
+// Word `at` of a row whose end is `left` elements behind the word's start; behind the end it holds zeros.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ uint4 load_word(const T* row, int at, int left)
+{
+    if constexpr (WHOLE) return __ldcs(reinterpret_cast<const uint4*>(row) + at);
+    else return load_halves(reinterpret_cast<const unsigned short*>(row + at * kWordElems<T>), min(left, kWordElems<T>) * static_cast<int>(sizeof(T) / 2));
+}
+
+// Whole words, or single elements.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void read_elements(const T* row, int at, float* f)
+{
+    if constexpr (WHOLE) unpack<T>(reinterpret_cast<const uint4*>(row)[at], f);
+    else f[0] = widen(row[at]);
+}
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void write_elements(T* row, int at, const float* f)
+{
+    if constexpr (WHOLE) reinterpret_cast<uint4*>(row)[at] = pack<T>(f);
+    else row[at] = narrow<T>(f[0]);
+}
+
 // LPR = 8 or 32: that many lanes hold a row, kNormThreads / LPR rows a CTA; LPR = 0: the CTA holds it.
-// A thread holds NV words of VE elements.
-template <typename T, int VE, int NV, int LPR>
+// A thread holds NV words.
+template <typename T, int NV, int LPR, bool WHOLE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
 layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
-    using W = WordOf<T, VE>;
+    constexpr int VE = kWordElems<T>, LANES = LPR ? LPR : 32, HALVES = sizeof(T) / 2;
     const int m = blockIdx.y;
-    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
-    const long long row = LPR ? static_cast<long long>(blockIdx.x) * (kNormThreads / (LPR ? LPR : 1)) + threadIdx.x / (LPR ? LPR : 1) : blockIdx.x;
+    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % LANES : threadIdx.x;
+    const long long row = LPR ? static_cast<long long>(blockIdx.x) * (kNormThreads / LANES) + threadIdx.x / LANES : blockIdx.x;
     const bool live = row < a.rows;
     if (LPR == 32 && !live) return;                           // a whole warp
-    const int words = live ? a.cols / VE : 0;                 // a group of 8 without a row keeps its warp company
-    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + (live ? row : 0) * a.x_stride);
+    const int cols = live ? a.cols : 0, words = (cols + VE - 1) / VE;     // a group of 8 without a row keeps its warp company
+    const T* x = static_cast<const T*>(a.x.p[m]) + (live ? row : 0) * a.x_stride;
 
-    W xw[NV];
+    uint4 xw[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (lane + i * lanes < words) xw[i] = x[lane + i * lanes];
+    for (int i = 0; i < NV; ++i) {
+        const int at = lane + i * lanes;
+        if (at < words) xw[i] = load_word<T, WHOLE>(x, at, cols - at * VE);
+    }
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (lane + i * lanes < words) add_elements<T, VE>(xw[i], sum);
+        if (lane + i * lanes < words) add_elements<T>(xw[i], sum);
     const float mean = row_sum<LPR>(sum[0] + sum[1], 0) * a.inv_cols;
     float square[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (lane + i * lanes >= words) continue;
+        const int at = lane + i * lanes;
+        if (at >= words) continue;
         float f[VE];
-        shifted<T, VE>(xw[i], -mean, f);
+        shifted<T>(xw[i], -mean, f);
+        if (!WHOLE && at * VE + VE > cols) {                  // the row ends inside this word
+#pragma unroll
+            for (int e = 0; e < VE; ++e)
+                if (at * VE + e >= cols) f[e] = 0.0f;
+        }
 #pragma unroll
         for (int e = 0; e < VE; ++e) square[e % 2] = fmaf(f[e], f[e], square[e % 2]);
     }
     const float rstd = inverse_root(fmaf(row_sum<LPR>(square[0] + square[1], 1), a.inv_cols, a.eps));
-    if (!live) return;
-    if (a.has_stats && lane == 0) {
+    if (a.has_stats && lane == 0 && live) {
         static_cast<float*>(a.mean.p[m])[row] = mean;
         static_cast<float*>(a.rstd.p[m])[row] = rstd;
     }
-    const W* gamma = static_cast<const W*>(a.gamma.p[m]);
-    const W* beta = static_cast<const W*>(a.beta.p[m]);
-    const T* gamma1 = static_cast<const T*>(a.gamma.p[m]);
-    const T* beta1 = static_cast<const T*>(a.beta.p[m]);
-    const bool words_ok = a.has_gamma && a.has_beta && ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) % sizeof(W)) == 0;
-    W* y = reinterpret_cast<W*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride);
-    if (words_ok) {
+    const T* gamma = static_cast<const T*>(a.gamma.p[m]);
+    const T* beta = static_cast<const T*>(a.beta.p[m]);
+    unsigned short* y = reinterpret_cast<unsigned short*>(static_cast<T*>(a.y.p[m]) + (live ? row : 0) * a.y_stride);
+    if constexpr (WHOLE) {
+        // parameters inside a flat vector stand anywhere, or there are none
+        const bool words_ok = a.has_gamma && a.has_beta && skip_of(gamma) == 0 && skip_of(beta) == 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = lane + i * lanes;
             if (at >= words) continue;
             float f[VE], g[VE], b[VE];
-            unpack<T, VE>(gamma[at], g);
-            unpack<T, VE>(beta[at], b);
-            shifted<T, VE>(xw[i], -mean, f);
+            if (words_ok) {
+                unpack<T>(reinterpret_cast<const uint4*>(gamma)[at], g);
+                unpack<T>(reinterpret_cast<const uint4*>(beta)[at], b);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    g[e] = a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f;
+                    b[e] = a.has_beta ? widen(beta[at * VE + e]) : 0.0f;
+                }
+            }
+            shifted<T>(xw[i], -mean, f);
 #pragma unroll
             for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
-            y[at] = pack<T, VE>(f);
+            __stcs(reinterpret_cast<uint4*>(y) + at, pack<T>(f));
         }
-    } else {                                                  // parameters inside a flat vector stand anywhere, or there are none
+    } else {
+        const unsigned skip = skip_of(y);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = lane + i * lanes;
-            if (at >= words) continue;
-            float f[VE];
-            shifted<T, VE>(xw[i], -mean, f);
+            const int at = lane + i * lanes, left = cols - at * VE;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (at < words) {
+                float f[VE], g[VE], b[VE] = {};
 #pragma unroll
-            for (int e = 0; e < VE; ++e)
-                f[e] = fmaf(f[e] * rstd, a.has_gamma ? widen(gamma1[at * VE + e]) : 1.0f, a.has_beta ? widen(beta1[at * VE + e]) : 0.0f);
-            y[at] = pack<T, VE>(f);
+                for (int e = 0; e < VE; ++e) g[e] = 1.0f;
+                if (a.has_gamma) unpack<T>(load_word<T, false>(gamma, at, left), g);
+                if (a.has_beta) unpack<T>(load_word<T, false>(beta, at, left), b);
+                shifted<T>(xw[i], -mean, f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
+                v = pack<T>(f);
+            }
+            store_halves(y, at, threadIdx.x % LANES, LANES, cols * HALVES, v, skip);
         }
     }
 }
 
-// Rows longer than a CTA's registers: a CTA per row, three reads of it (the second and third from L2).
-template <typename T, int VE>
+// Short rows by the thousand, 16-byte aligned, a warp a row: a warp goes through rows with the next ones on their way
+// to shared memory, each lane its own words (no barriers).  For rows of one or two words a lane, whose loads
+// alone do not keep memory busy (8 x 18554 rows of 256 bf16: 48 us with a warp for every row, 32 us so); longer
+// rows have loads enough in flight, and lose with the fewer warps that the stages leave room for.
+constexpr int kAheadDepth = 4, kAheadCtas = 6;                // rows ahead, and CTAs an SM takes
+template <typename T, int NV>
+__global__ void __launch_bounds__(kNormThreads)
+layernorm_forward_short_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    constexpr int VE = kWordElems<T>, kWarps = kNormThreads / 32;
+    __shared__ uint4 ring[kAheadDepth][NV][kNormThreads];
+    const int m = blockIdx.y, lane = threadIdx.x % 32, words = a.cols / VE;
+    const T* xs = static_cast<const T*>(a.x.p[m]);
+    const uint4* gamma = static_cast<const uint4*>(a.gamma.p[m]) + lane;            // aligned, and whole words, as the host has checked
+    const uint4* beta = static_cast<const uint4*>(a.beta.p[m]) + lane;
+    const int stride = gridDim.x * kWarps;
+    const auto fetch = [&](int slot, long long row) {
+        if (row < a.rows) {
+            const uint4* x = reinterpret_cast<const uint4*>(xs + row * a.x_stride) + lane;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (lane + i * 32 < words) copy_async16(&ring[slot][i][threadIdx.x], x + i * 32);
+        }
+        copy_async_commit();                                  // a group a row, also where there is none
+    };
+    long long row = static_cast<long long>(blockIdx.x) * kWarps + threadIdx.x / 32;
+#pragma unroll
+    for (int d = 0; d < kAheadDepth - 1; ++d) fetch(d, row + static_cast<long long>(d) * stride);
+    uint4 gw[NV], bw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (lane + i * 32 < words) { gw[i] = gamma[i * 32]; bw[i] = beta[i * 32]; }
+    for (int slot = 0; row < a.rows; row += stride, slot = (slot + 1) % kAheadDepth) {
+        fetch((slot + kAheadDepth - 1) % kAheadDepth, row + static_cast<long long>(kAheadDepth - 1) * stride);
+        copy_async_wait<kAheadDepth - 1>();
+        uint4 xw[NV];
+        float sum[2] = {0.0f, 0.0f}, square[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (lane + i * 32 >= words) continue;
+            xw[i] = ring[slot][i][threadIdx.x];
+            add_elements<T>(xw[i], sum);
+        }
+        const float mean = lanes_sum<32>(sum[0] + sum[1]) * a.inv_cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (lane + i * 32 >= words) continue;
+            float f[VE];
+            shifted<T>(xw[i], -mean, f);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) square[e % 2] = fmaf(f[e], f[e], square[e % 2]);
+        }
+        const float rstd = inverse_root(fmaf(lanes_sum<32>(square[0] + square[1]), a.inv_cols, a.eps));
+        if (a.has_stats && lane == 0) {
+            static_cast<float*>(a.mean.p[m])[row] = mean;
+            static_cast<float*>(a.rstd.p[m])[row] = rstd;
+        }
+        uint4* y = reinterpret_cast<uint4*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride) + lane;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (lane + i * 32 >= words) continue;
+            float f[VE], g[VE], b[VE];
+            unpack<T>(gw[i], g);
+            unpack<T>(bw[i], b);
+            shifted<T>(xw[i], -mean, f);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
+            __stcs(y + i * 32, pack<T>(f));
+        }
+    }
+    copy_async_wait<0>();
+}
+
+// Rows longer than a CTA's registers: a CTA per row, three reads of it (the second and third from L2), by words, or
+// element by element (neighbouring threads at neighbouring elements).
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormLongThreads)
 layernorm_forward_long_kernel(const __grid_constant__ NormForwardArgs a)
 {
-    using W = WordOf<T, VE>;
+    constexpr int VE = WHOLE ? kWordElems<T> : 1;
     const int m = blockIdx.y, words = a.cols / VE;
     const long long row = blockIdx.x;
-    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + row * a.x_stride);
+    const T* x = static_cast<const T*>(a.x.p[m]) + row * a.x_stride;
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
     const T* beta = static_cast<const T*>(a.beta.p[m]);
-    W* y = reinterpret_cast<W*>(static_cast<T*>(a.y.p[m]) + row * a.y_stride);
-    float sum = 0.0f, f[VE];
+    T* y = static_cast<T*>(a.y.p[m]) + row * a.y_stride;
+    float f[VE], sum = 0.0f, square = 0.0f;
+#pragma unroll 4
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
-        unpack<T, VE>(x[at], f);
+        read_elements<T, WHOLE>(x, at, f);
 #pragma unroll
         for (int e = 0; e < VE; ++e) sum += f[e];
     }
     const float mean = row_sum<0>(sum, 0) * a.inv_cols;
-    float squares = 0.0f;
+#pragma unroll 4
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
-        unpack<T, VE>(x[at], f);
+        read_elements<T, WHOLE>(x, at, f);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) squares = fmaf(f[e] - mean, f[e] - mean, squares);
+        for (int e = 0; e < VE; ++e) square = fmaf(f[e] - mean, f[e] - mean, square);
     }
-    const float rstd = inverse_root(fmaf(row_sum<0>(squares, 1), a.inv_cols, a.eps));
+    const float rstd = inverse_root(fmaf(row_sum<0>(square, 1), a.inv_cols, a.eps));
     if (a.has_stats && threadIdx.x == 0) {
         static_cast<float*>(a.mean.p[m])[row] = mean;
         static_cast<float*>(a.rstd.p[m])[row] = rstd;
     }
+#pragma unroll 2
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
-        unpack<T, VE>(x[at], f);
+        read_elements<T, WHOLE>(x, at, f);
 #pragma unroll
         for (int e = 0; e < VE; ++e)
             f[e] = fmaf((f[e] - mean) * rstd, a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f, a.has_beta ? widen(beta[at * VE + e]) : 0.0f);
-        y[at] = pack<T, VE>(f);
+        write_elements<T, WHOLE>(y, at, f);
     }
 }
 
@@ -207,46 +329,51 @@ __device__ __forceinline__ void store_gradients(const NormBackwardArgs& a, int m
     }
 }
 
-// A worker's column sums over the rows of one CTA: to the CTA's place in `partial`, or, when it is the
-// worker's only CTA, to the gradients themselves.
+// A worker's column sums over the rows of one CTA go to the CTA's place in `partial`, or, when it is the
+// worker's only CTA, to the gradients themselves.  The sums stand in the order of the threads that hold them
+// (by columns, a warp's stores would touch 32 sectors each): slot (i, lane) of element i of a thread.
+__device__ __forceinline__ int slot_column(const NormBackwardArgs& a, int j)
+{
+    const int i = j / a.lanes, lane = j % a.lanes;
+    return (lane + i / a.word * a.lanes) * a.word + i % a.word;
+}
 template <typename T>
-__device__ __forceinline__ void store_column(const NormBackwardArgs& a, int m, int part, int col, float dg, float db)
+__device__ __forceinline__ void store_slot_sums(const NormBackwardArgs& a, int m, int part, int slot, float dg, float db)
 {
     if (a.parts == 1) {
-        store_gradients<T>(a, m, col, dg, db);
+        const int col = slot_column(a, slot);
+        if (col < a.cols) store_gradients<T>(a, m, col, dg, db);
     } else {
-        float* p = a.partial + (static_cast<size_t>(m) * a.parts + part) * 2 * a.cols + col;
+        float* p = a.partial + (static_cast<size_t>(m) * a.parts + part) * 2 * a.slots + slot;
         p[0] = dg;
-        p[a.cols] = db;
+        p[a.slots] = db;
     }
 }
 
-// Rows under way: 16-byte words are staged through shared memory by asynchronous copies, kNormDepth rows ahead of
-// the one that is computed (registers are full of column sums; one row ahead in registers left the SM waiting
-// for memory), each thread its own words, so that no barrier is needed.
-template <typename T, int VE, int EPT> struct NormStage {
-    static constexpr bool staged = VE * sizeof(T) == 16;
-    static constexpr int words = EPT / VE;
-    static constexpr int depth = words <= 3 ? 4 : words <= 4 ? 3 : 2;
-    static constexpr size_t bytes_a_thread = staged ? depth * 2 * words * 16 : 0;
+// Whole rows under way are staged through shared memory by asynchronous copies, `depth` - 1 rows ahead of the one
+// that is computed (registers are full of column sums; one row ahead in registers left the SM waiting for memory),
+// each thread its own words, so that no barrier is needed.
+template <int NV> struct NormStage {
+    static constexpr int depth = NV <= 3 ? 4 : NV <= 4 ? 3 : 2;
+    static constexpr size_t bytes_a_thread = depth * 2 * NV * 16;
 };
+// CTAs of kNormThreads that an SM is to hold, by a thread's elements (three registers each, and the words).
+constexpr int norm_ctas(int elems, int bytes) { return elems <= 8 ? 6 : elems <= 16 ? (bytes == 2 ? 5 : 4) : elems <= 24 ? (bytes == 2 ? 4 : 3) : (bytes == 2 ? 3 : 2); }
 
 // gridDim.x CTAs a worker go through its rows in turn; a thread keeps the sums of its own columns in
 // registers over all of them, so the weights' gradients cost one small table at the end and no atomics
 // (the split depends on the sizes alone: the same bits every time).
-template <typename T, int VE, int EPT, int LPR>
-__global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
+template <typename T, int NV, int LPR, bool WHOLE>
+__global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock, LPR == 32 ? norm_ctas(NV * kWordElems<T>, sizeof(T)) : 1)
 layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    using Stage = NormStage<T, VE, EPT>;
-    constexpr int NV = EPT / VE;
-    constexpr int GROUPS = LPR ? kNormThreads / (LPR ? LPR : 1) : 1;
-    using W = WordOf<T, VE>;
+    constexpr int VE = kWordElems<T>, EPT = NV * VE, LANES = LPR ? LPR : 32, HALVES = sizeof(T) / 2;
+    constexpr int GROUPS = LPR ? kNormThreads / LANES : 1, DEPTH = NormStage<NV>::depth;
     extern __shared__ uint4 ring[];                           // [depth][x, dy][NV][threads]
     const int m = blockIdx.y;
-    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % (LPR ? LPR : 1) : threadIdx.x;
-    const int group = LPR ? threadIdx.x / (LPR ? LPR : 1) : 0;
-    const int words = a.cols / VE;
+    const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % LANES : threadIdx.x;
+    const int group = LPR ? threadIdx.x / LANES : 0;
+    const int words = (a.cols + VE - 1) / VE;
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
     const T* xs = static_cast<const T*>(a.x.p[m]);
     const T* dys = static_cast<const T*>(a.dy.p[m]);
@@ -255,60 +382,71 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 
     float gm[EPT], dg[EPT], db[EPT];
 #pragma unroll
-    for (int k = 0; k < EPT; ++k) {
-        const int at = lane + k / VE * lanes;
-        gm[k] = a.has_gamma && at < words ? widen(gamma[at * VE + k % VE]) : 1.0f;
-        dg[k] = db[k] = 0.0f;
+    for (int i = 0; i < NV; ++i) {
+        const int at = lane + i * lanes;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) gm[i * VE + e] = 1.0f;
+        if (a.has_gamma && at < words) unpack<T>(load_word<T, false>(gamma, at, a.cols - at * VE), gm + i * VE);
     }
+#pragma unroll
+    for (int k = 0; k < EPT; ++k) dg[k] = db[k] = 0.0f;
     const long long stride = static_cast<long long>(gridDim.x) * GROUPS;
     long long row = static_cast<long long>(blockIdx.x) * GROUPS + group;
     const auto fetch = [&](int slot, long long r) {
         if (r < a.rows) {
-            const W* x = reinterpret_cast<const W*>(xs + r * a.x_stride) + lane;
-            const W* dy = reinterpret_cast<const W*>(dys + r * a.y_stride) + lane;
+            const T* x = xs + r * a.x_stride;
+            const T* dy = dys + r * a.y_stride;
             uint4* to = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (lane + i * lanes < words) {
-                    copy_async16(to + i * blockDim.x, x + i * lanes);
-                    copy_async16(to + (NV + i) * blockDim.x, dy + i * lanes);
+            for (int i = 0; i < NV; ++i) {
+                const int at = lane + i * lanes;
+                if (at < words) {
+                    copy_async16(to + i * blockDim.x, x + at * VE);
+                    copy_async16(to + (NV + i) * blockDim.x, dy + at * VE);
                 }
+            }
         }
         copy_async_commit();                                  // a group a row, also where there is none
     };
-    if constexpr (Stage::staged) {
+    if constexpr (WHOLE) {
 #pragma unroll
-        for (int d = 0; d < Stage::depth - 1; ++d) fetch(d, row + d * stride);
+        for (int d = 0; d < DEPTH - 1; ++d) fetch(d, row + d * stride);
     }
     int buf = 0, slot = 0;
     float mean = row < a.rows ? means[row] : 0.0f, rstd = row < a.rows ? rstds[row] : 0.0f;
     for (; row - group < a.rows; row += stride) {             // the same turns for all groups of the CTA
-        const int w_end = row < a.rows ? words : 0;
-        W xw[NV], dw[NV];
-        if constexpr (Stage::staged) {
-            fetch(slot == 0 ? Stage::depth - 1 : slot - 1, row + (Stage::depth - 1) * stride);
-            copy_async_wait<Stage::depth - 1>();
+        const bool live = row < a.rows;
+        const int w_end = live ? words : 0;
+        uint4 xw[NV], dw[NV];
+        if constexpr (WHOLE) {
+            fetch(slot == 0 ? DEPTH - 1 : slot - 1, row + (DEPTH - 1) * stride);
+            copy_async_wait<DEPTH - 1>();
             const uint4* from = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (lane + i * lanes < w_end) { xw[i] = from[i * blockDim.x]; dw[i] = from[(NV + i) * blockDim.x]; }
-            slot = slot + 1 == Stage::depth ? 0 : slot + 1;
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
         } else {
-            const W* x = reinterpret_cast<const W*>(xs + row * a.x_stride) + lane;
-            const W* dy = reinterpret_cast<const W*>(dys + row * a.y_stride) + lane;
+            const T* x = xs + (live ? row : 0) * a.x_stride;
+            const T* dy = dys + (live ? row : 0) * a.y_stride;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (lane + i * lanes < w_end) { xw[i] = x[i * lanes]; dw[i] = dy[i * lanes]; }
+            for (int i = 0; i < NV; ++i) {
+                const int at = lane + i * lanes;
+                if (at >= w_end) continue;
+                xw[i] = load_word<T, false>(x, at, a.cols - at * VE);
+                dw[i] = load_word<T, false>(dy, at, a.cols - at * VE);
+            }
         }
         const bool more = row + stride < a.rows;
         const float next_mean = more ? means[row + stride] : 0.0f, next_rstd = more ? rstds[row + stride] : 0.0f;
+        // (Behind the end of a row dy is zero, and with it every term of the sums.)
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (lane + i * lanes >= w_end) continue;
             float f[VE], d[VE];
-            shifted<T, VE>(xw[i], -mean, f);
-            unpack<T, VE>(dw[i], d);
+            shifted<T>(xw[i], -mean, f);
+            unpack<T>(dw[i], d);
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 const float h = f[e] * rstd, g = d[e] * gm[i * VE + e];
@@ -322,29 +460,35 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
             s = row_sum<LPR>(s, buf);
             buf ^= 1;
             const float mg = -s.x * a.inv_cols * rstd, mgh = -s.y * a.inv_cols * rstd * rstd;
-            W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + row * a.x_stride) + lane;
+            unsigned short* dx = reinterpret_cast<unsigned short*>(static_cast<T*>(a.dx.p[m]) + (live ? row : 0) * a.x_stride);
+            const unsigned skip = WHOLE ? 0u : skip_of(dx);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (lane + i * lanes >= w_end) continue;
-                float f[VE], d[VE];
-                shifted<T, VE>(xw[i], -mean, f);
-                unpack<T, VE>(dw[i], d);
+                const int at = lane + i * lanes;
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (at < w_end) {
+                    float f[VE], d[VE];
+                    shifted<T>(xw[i], -mean, f);
+                    unpack<T>(dw[i], d);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e], mgh, mg));
-                dx[i * lanes] = pack<T, VE>(f);
+                    for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e], mgh, mg));
+                    v = pack<T>(f);
+                }
+                if constexpr (WHOLE) {
+                    if (at < w_end) reinterpret_cast<uint4*>(dx)[at] = v;
+                } else {
+                    store_halves(dx, at, threadIdx.x % LANES, LANES, live ? a.cols * HALVES : 0, v, skip);
+                }
             }
         }
         mean = next_mean;
         rstd = next_rstd;
     }
-    if constexpr (Stage::staged) copy_async_wait<0>();
+    if constexpr (WHOLE) copy_async_wait<0>();
     if (!a.has_dgamma && !a.has_dbeta) return;
     if constexpr (LPR == 0) {
 #pragma unroll
-        for (int k = 0; k < EPT; ++k) {
-            const int at = lane + k / VE * lanes;
-            if (at < words) store_column<T>(a, m, blockIdx.x, at * VE + k % VE, dg[k], db[k]);
-        }
+        for (int k = 0; k < EPT; ++k) store_slot_sums<T>(a, m, blockIdx.x, k * lanes + lane, dg[k], db[k]);
     } else {
         // groups of rows: first the groups of a warp, then the warps in order, through shared memory
         __shared__ float2 acc[LPR * EPT];
@@ -367,31 +511,29 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
             }
             __syncthreads();
         }
-        for (int j = threadIdx.x; j < LPR * EPT; j += kNormThreads) {
-            const int at = j % LPR + j / LPR / VE * LPR, col = at * VE + j / LPR % VE;
-            if (at < words) store_column<T>(a, m, blockIdx.x, col, acc[j].x, acc[j].y);
-        }
+        for (int j = threadIdx.x; j < LPR * EPT; j += kNormThreads) store_slot_sums<T>(a, m, blockIdx.x, j, acc[j].x, acc[j].y);
     }
 }
 
 // Rows that do not fit in a CTA's registers: dx by a CTA per row (dy and x are read again from L2) ...
-template <typename T, int VE>
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormLongThreads)
 layernorm_backward_long_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    using W = WordOf<T, VE>;
+    constexpr int VE = WHOLE ? kWordElems<T> : 1;
     const int m = blockIdx.y, words = a.cols / VE;
     const long long row = blockIdx.x;
-    const W* x = reinterpret_cast<const W*>(static_cast<const T*>(a.x.p[m]) + row * a.x_stride);
-    const W* dy = reinterpret_cast<const W*>(static_cast<const T*>(a.dy.p[m]) + row * a.y_stride);
+    const T* x = static_cast<const T*>(a.x.p[m]) + row * a.x_stride;
+    const T* dy = static_cast<const T*>(a.dy.p[m]) + row * a.y_stride;
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
-    W* dx = reinterpret_cast<W*>(static_cast<T*>(a.dx.p[m]) + row * a.x_stride);
+    T* dx = static_cast<T*>(a.dx.p[m]) + row * a.x_stride;
     const float mean = static_cast<const float*>(a.mean.p[m])[row], rstd = static_cast<const float*>(a.rstd.p[m])[row];
     float f[VE], d[VE];
     float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 4
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
-        unpack<T, VE>(x[at], f);
-        unpack<T, VE>(dy[at], d);
+        read_elements<T, WHOLE>(x, at, f);
+        read_elements<T, WHOLE>(dy, at, d);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             const float g = d[e] * (a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f);
@@ -401,40 +543,60 @@ layernorm_backward_long_kernel(const __grid_constant__ NormBackwardArgs a)
     }
     s = row_sum<0>(s, 0);
     const float mg = s.x * a.inv_cols, mgh = s.y * a.inv_cols;
+#pragma unroll 2
     for (int at = threadIdx.x; at < words; at += kNormLongThreads) {
-        unpack<T, VE>(x[at], f);
-        unpack<T, VE>(dy[at], d);
+        read_elements<T, WHOLE>(x, at, f);
+        read_elements<T, WHOLE>(dy, at, d);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             const float g = d[e] * (a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f);
             f[e] = (g - mg - (f[e] - mean) * rstd * mgh) * rstd;
         }
-        dx[at] = pack<T, VE>(f);
+        write_elements<T, WHOLE>(dx, at, f);
     }
 }
 
-// ... and the weights' gradients by a thread per column, gridDim.z parts of the rows.
-template <typename T>
+// ... and the weights' gradients by columns, gridDim.z parts of the rows: a warp takes 32 neighbouring words (or
+// elements) of a row, and the warps of a CTA take rows in turn.
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormThreads)
 layernorm_columns_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    const int m = blockIdx.y, col = blockIdx.x * kNormThreads + threadIdx.x, part = blockIdx.z;
-    if (col >= a.cols) return;
-    const T* x = static_cast<const T*>(a.x.p[m]) + col;
-    const T* dy = static_cast<const T*>(a.dy.p[m]) + col;
+    constexpr int VE = WHOLE ? kWordElems<T> : 1, kWarps = kNormThreads / 32;
+    __shared__ float2 acc[kWarps][32 * VE];
+    const int m = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = blockIdx.x * 32 + lane, part = blockIdx.z;
     const float* means = static_cast<const float*>(a.mean.p[m]);
     const float* rstds = static_cast<const float*>(a.rstd.p[m]);
-    float dg = 0.0f, db = 0.0f;
+    float dg[VE] = {}, db[VE] = {};
+    if (at < a.cols / VE) {
+        const T* x = static_cast<const T*>(a.x.p[m]);
+        const T* dy = static_cast<const T*>(a.dy.p[m]);
 #pragma unroll 4
-    for (long long row = part; row < a.rows; row += a.parts) {
-        const float d = widen(dy[row * a.y_stride]);
-        dg = fmaf(d, (widen(x[row * a.x_stride]) - means[row]) * rstds[row], dg);
-        db += d;
+        for (long long row = part * kWarps + warp; row < a.rows; row += static_cast<long long>(a.parts) * kWarps) {
+            float f[VE], d[VE];
+            read_elements<T, WHOLE>(x + row * a.x_stride, at, f);
+            read_elements<T, WHOLE>(dy + row * a.y_stride, at, d);
+            const float mean = means[row], rstd = rstds[row];
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                dg[e] = fmaf(d[e], (f[e] - mean) * rstd, dg[e]);
+                db[e] += d[e];
+            }
+        }
     }
-    store_column<T>(a, m, part, col, dg, db);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) acc[warp][e * 32 + lane] = make_float2(dg[e], db[e]);
+    __syncthreads();
+    for (int j = threadIdx.x; j < 32 * VE; j += kNormThreads) {
+        float2 s = acc[0][j];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) { s.x += acc[w][j].x; s.y += acc[w][j].y; }
+        const int col = (blockIdx.x * 32 + j % 32) * VE + j / 32;
+        if (col < a.cols) store_slot_sums<T>(a, m, part, col, s.x, s.y);            // (a slot a column)
+    }
 }
 
-// The parts' column sums, added in a fixed order: 32 columns a CTA, kFinishGroups threads a column.
+// The parts' column sums, added in a fixed order: 32 slots a CTA, kFinishGroups threads a slot.
 constexpr int kFinishGroups = 16;
 template <typename T>
 __global__ void __launch_bounds__(32 * kFinishGroups)
@@ -442,19 +604,21 @@ layernorm_finish_kernel(const __grid_constant__ NormBackwardArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float2 acc[kFinishGroups][32];
-    const int m = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    const int m = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x >> 5, slot = blockIdx.x * 32 + lane;
     float2 s = make_float2(0.0f, 0.0f);
-    if (col < a.cols) {
-        const float* p = a.partial + static_cast<size_t>(m) * a.parts * 2 * a.cols + col;
+    if (slot < a.slots) {
+        const float* p = a.partial + static_cast<size_t>(m) * a.parts * 2 * a.slots + slot;
 #pragma unroll 4
         for (int i = group; i < a.parts; i += kFinishGroups) {
-            s.x += p[static_cast<size_t>(i) * 2 * a.cols];
-            s.y += p[static_cast<size_t>(i) * 2 * a.cols + a.cols];
+            s.x += p[static_cast<size_t>(i) * 2 * a.slots];
+            s.y += p[static_cast<size_t>(i) * 2 * a.slots + a.slots];
         }
     }
     acc[group][lane] = s;
     __syncthreads();
-    if (group != 0 || col >= a.cols) return;
+    if (group != 0 || slot >= a.slots) return;
+    const int col = slot_column(a, slot);
+    if (col >= a.cols) return;
 #pragma unroll
     for (int g = 1; g < kFinishGroups; ++g) { s.x += acc[g][lane].x; s.y += acc[g][lane].y; }
     store_gradients<T>(a, m, col, s.x, s.y);

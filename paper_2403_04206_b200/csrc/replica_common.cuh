@@ -16,12 +16,8 @@ constexpr int kSms = 148;              // a B200; the shapes of the persistent g
 struct In { const void* p[kWorkers]; };
 struct Out { void* p[kWorkers]; };
 
-// The word that carries VE elements of T: 16, 4 or 2 bytes.
-template <int BYTES> struct Word;
-template <> struct Word<16> { using type = uint4; };
-template <> struct Word<4> { using type = unsigned; };
-template <> struct Word<2> { using type = unsigned short; };
-template <typename T, int VE> using WordOf = typename Word<VE * static_cast<int>(sizeof(T))>::type;
+// Elements travel in words of 16 bytes: 8 of 16 bits, 4 of 32.
+template <typename T> constexpr int kWordElems = 16 / static_cast<int>(sizeof(T));
 
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -53,40 +49,22 @@ __device__ __forceinline__ unsigned pack_pair(float lo, float hi, __half)
     return *reinterpret_cast<const unsigned*>(&v);
 }
 
-template <typename T, int VE>
-__device__ __forceinline__ void unpack(const WordOf<T, VE>& w, float* o)
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& w, float* o)
 {
     if constexpr (sizeof(T) == 4) {
-        if constexpr (VE == 4) {
-            o[0] = __uint_as_float(w.x); o[1] = __uint_as_float(w.y); o[2] = __uint_as_float(w.z); o[3] = __uint_as_float(w.w);
-        } else {
-            o[0] = __uint_as_float(w);
-        }
-    } else if constexpr (VE == 8) {
-        unpack_pair(w.x, o, T{}); unpack_pair(w.y, o + 2, T{}); unpack_pair(w.z, o + 4, T{}); unpack_pair(w.w, o + 6, T{});
-    } else if constexpr (VE == 2) {
-        unpack_pair(w, o, T{});
+        o[0] = __uint_as_float(w.x); o[1] = __uint_as_float(w.y); o[2] = __uint_as_float(w.z); o[3] = __uint_as_float(w.w);
     } else {
-        o[0] = widen(*reinterpret_cast<const T*>(&w));
+        unpack_pair(w.x, o, T{}); unpack_pair(w.y, o + 2, T{}); unpack_pair(w.z, o + 4, T{}); unpack_pair(w.w, o + 6, T{});
     }
 }
-
-template <typename T, int VE>
-__device__ __forceinline__ WordOf<T, VE> pack(const float* o)
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float* o)
 {
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (VE == 4)
-            return make_uint4(__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
-        else
-            return __float_as_uint(o[0]);
-    } else if constexpr (VE == 8) {
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
+    else
         return make_uint4(pack_pair(o[0], o[1], T{}), pack_pair(o[2], o[3], T{}), pack_pair(o[4], o[5], T{}), pack_pair(o[6], o[7], T{}));
-    } else if constexpr (VE == 2) {
-        return pack_pair(o[0], o[1], T{});
-    } else {
-        const T v = narrow<T>(o[0]);
-        return *reinterpret_cast<const unsigned short*>(&v);
-    }
 }
 
 // o[e] = element e + c, and acc[e % 2] += element e.  For 16-bit elements these are single instructions that
@@ -111,31 +89,102 @@ __device__ __forceinline__ void pair_sum(unsigned w, float* acc, __half)
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t}"
         : "+f"(acc[0]), "+f"(acc[1]) : "r"(w));
 }
-template <typename T, int VE>
-__device__ __forceinline__ void shifted(const WordOf<T, VE>& w, float c, float* o)
+template <typename T>
+__device__ __forceinline__ void shifted(const uint4& w, float c, float* o)
 {
-    if constexpr (sizeof(T) == 2 && VE == 8) {
+    if constexpr (sizeof(T) == 2) {
         pair_add(w.x, c, o, T{}); pair_add(w.y, c, o + 2, T{}); pair_add(w.z, c, o + 4, T{}); pair_add(w.w, c, o + 6, T{});
-    } else if constexpr (sizeof(T) == 2 && VE == 2) {
-        pair_add(w, c, o, T{});
     } else {
-        unpack<T, VE>(w, o);
+        unpack<T>(w, o);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) o[e] += c;
+        for (int e = 0; e < 4; ++e) o[e] += c;
     }
 }
-template <typename T, int VE>
-__device__ __forceinline__ void add_elements(const WordOf<T, VE>& w, float (&acc)[2])
+template <typename T>
+__device__ __forceinline__ void add_elements(const uint4& w, float (&acc)[2])
 {
-    if constexpr (sizeof(T) == 2 && VE == 8) {
+    if constexpr (sizeof(T) == 2) {
         pair_sum(w.x, acc, T{}); pair_sum(w.y, acc, T{}); pair_sum(w.z, acc, T{}); pair_sum(w.w, acc, T{});
-    } else if constexpr (sizeof(T) == 2 && VE == 2) {
-        pair_sum(w, acc, T{});
     } else {
-        float o[VE];
-        unpack<T, VE>(w, o);
+        float o[4];
+        unpack<T>(w, o);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) acc[e % 2] += o[e];
+        for (int e = 0; e < 4; ++e) acc[e % 2] += o[e];
+    }
+}
+
+// Words at addresses of any alignment, in halves (16 bits): a word of 8 halves lies in one or two aligned words.
+// The 8 halves from half `skip` (0..7) on of the 16 halves (lo, hi).
+__device__ __forceinline__ uint4 shift_halves(const uint4& lo, const uint4& hi, unsigned skip)
+{
+    const unsigned w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    unsigned t[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {                             // by whole 32-bit words, two steps of a binary shift
+        const unsigned a = skip & 4 ? w[i + 2] : w[i], b = skip & 4 ? w[i + 3 < 8 ? i + 3 : 7] : w[i + 1];
+        t[i] = skip & 2 ? b : a;
+    }
+    const unsigned bits = (skip & 1) * 16;
+    return make_uint4(__funnelshift_r(t[0], t[1], bits), __funnelshift_r(t[1], t[2], bits), __funnelshift_r(t[2], t[3], bits),
+                      __funnelshift_r(t[3], t[4], bits));
+}
+// The first `count` (1 to 8) halves of v, zeros behind them.
+__device__ __forceinline__ uint4 keep_halves(uint4 v, int count)
+{
+    if (count < 8) {
+        unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (2 * i + 1 >= count) w[i] = 2 * i >= count ? 0u : w[i] & 0xffffu;
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+__device__ __forceinline__ unsigned skip_of(const void* p) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15) / 2; }
+
+// `count` (1 to 8) halves from p on, zeros behind them, from the aligned words that hold them (each of which holds
+// at least one of them).
+__device__ __forceinline__ uint4 load_halves(const unsigned short* p, int count)
+{
+    const unsigned skip = skip_of(p);
+    const uint4* word = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~static_cast<uintptr_t>(15));
+    const uint4 lo = word[0];
+    const uint4 hi = static_cast<int>(skip) + count > 8 ? word[1] : make_uint4(0, 0, 0, 0);
+    return keep_halves(shift_halves(lo, hi, skip), count);
+}
+
+// Stores of a row of `halves` halves whose words stand in order in neighbouring lanes: lane l of a segment of `lanes`
+// neighbouring lanes holds word `at` = (the segment's first) + l, v; lanes behind the row's last word hold none.  All
+// 32 lanes of the warp call it.  Where the row does not start on a 16-byte boundary, a lane stores the aligned word
+// that its halves share with the lane in front; what is left at the ends of a segment goes half by half.
+// (Rows of one warp may start at different offsets, so every lane takes part in the exchange whether it needs it or not.)
+__device__ __forceinline__ void store_halves(unsigned short* row, int at, int lane, int lanes, int halves, const uint4& v, unsigned skip)
+{
+    const int count = min(8, halves - 8 * at);
+    const uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1),
+                                    __shfl_up_sync(0xffffffffu, v.z, 1), __shfl_up_sync(0xffffffffu, v.w, 1));
+    if (skip == 0) {
+        if (count == 8) {
+            *reinterpret_cast<uint4*>(row + 8 * at) = v;
+        } else if (count > 0) {
+            const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < count) row[8 * at + e] = static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16));
+        }
+        return;
+    }
+    if (count <= 0) return;
+    const int own = 8 - static_cast<int>(skip);               // halves of v in the aligned word that v begins in
+    const bool joined = lane > 0 && count >= own;
+    const bool passed = lane + 1 < lanes && halves - 8 * (at + 1) >= own;          // the rest of v goes with the next lane's word
+    if (joined) *reinterpret_cast<uint4*>(row + 8 * at - static_cast<int>(skip)) = shift_halves(before, v, own);
+    if (!joined || !passed) {
+        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+        const int from = joined ? own : 0, to = passed ? min(count, own) : count;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= from && e < to) row[8 * at + e] = static_cast<unsigned short>(w[e / 2] >> (e % 2 * 16));
     }
 }
 

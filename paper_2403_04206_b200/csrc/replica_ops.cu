@@ -89,16 +89,10 @@ static grawa_status dropout(grawa_dtype dtype, const void* const* in, const void
 
 // ------------------------------------------------------------------ layer norm
 
-// Elements per word: 16 bytes, else 4, else one element, whatever the rows' bases, strides and length allow.
-static int word_elems(int64_t elem, int64_t cols, int64_t stride_a, int64_t stride_b, const void* const* a, const void* const* b, const void* const* c, int M)
+// Are all rows of a row-strided operand whole 16-byte words at 16-byte boundaries?
+static bool rows_whole(const void* const* table, int M, int64_t rows, int64_t cols, int64_t stride, int64_t elem)
 {
-    for (int64_t bytes : {int64_t{16}, int64_t{4}}) {
-        if (bytes <= elem) break;
-        const int64_t ve = bytes / elem;
-        if (cols % ve || stride_a % ve || stride_b % ve) continue;
-        if (all_aligned(a, M, bytes) && all_aligned(b, M, bytes) && all_aligned(c, M, bytes)) return static_cast<int>(ve);
-    }
-    return 1;
+    return cols * elem % 16 == 0 && (rows <= 1 || stride * elem % 16 == 0) && all_aligned(table, M, 16);
 }
 
 static bool shape_ok(int64_t rows, int64_t cols, int64_t x_stride, int64_t y_stride, int M, int64_t elem)
@@ -108,102 +102,125 @@ static bool shape_ok(int64_t rows, int64_t cols, int64_t x_stride, int64_t y_str
     return x_stride >= cols && y_stride >= cols && x_stride <= most / std::max<int64_t>(1, rows) && y_stride <= most / std::max<int64_t>(1, rows);
 }
 
-constexpr int kLongForward = kNormMaxBlock * 32, kLongBackward = kNormMaxBlock * 16;   // longest rows held in registers
+template <typename T, int NV>
+static grawa_status launch_norm_short(const NormForwardArgs& a, int M, cudaStream_t stream)
+{
+    const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows, kNormThreads / 32), static_cast<int64_t>(kSms) * kAheadCtas / M));
+    return launch(layernorm_forward_short_kernel<T, NV>, dim3(static_cast<unsigned>(ctas), M), kNormThreads, 0, stream, false, a);
+}
 
-template <typename T, int VE>
+template <typename T, bool WHOLE>
 static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStream_t stream)
 {
+    constexpr int VE = kWordElems<T>;
+    const int64_t words = ceil_div(a.cols, VE), per_lane = ceil_div(words, 32);
     const auto lanes = [&](auto kernel, int lpr) {
         return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, false, a);
     };
-    if (a.cols <= 64) return lanes(layernorm_forward_kernel<T, VE, 8 / VE, 8>, 8);
-    // A warp a row, as long as a lane's words fit in its registers.
-    const int64_t per_lane = ceil_div(a.cols / VE, 32);
-    if constexpr (VE >= 4) {
-        if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, VE, 1, 32>, 32);
-        if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, VE, 2, 32>, 32);
-        if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, VE, 3, 32>, 32);
-        if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, VE, 4, 32>, 32);
-        if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, VE, 6, 32>, 32);
-        if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, VE, 8, 32>, 32);
-        if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, VE, 12, 32>, 32);
-        if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, VE, 16, 32>, 32);
-    } else {
-        if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, VE, 8, 32>, 32);
-        if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, VE, 16, 32>, 32);
-        if (per_lane <= 32) return lanes(layernorm_forward_kernel<T, VE, 32, 32>, 32);
-    }
-    if (a.cols <= kLongForward)
-        return launch(layernorm_forward_kernel<T, VE, 32 / VE, 0>, dim3(static_cast<unsigned>(a.rows), M), static_cast<int>(ceil_div(a.cols, 32 * 32)) * 32, 0, stream, false, a);
-    return launch(layernorm_forward_long_kernel<T, VE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+    if (words <= 8) return lanes(layernorm_forward_kernel<T, 1, 8, WHOLE>, 8);
+    if (WHOLE && per_lane <= 2 && a.has_gamma && a.has_beta && a.rows * M >= 32 * kSms * kAheadCtas &&
+        all_aligned(a.gamma.p, M, 16) && all_aligned(a.beta.p, M, 16))
+        return per_lane == 1 ? launch_norm_short<T, 1>(a, M, stream) : launch_norm_short<T, 2>(a, M, stream);
+    if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, 1, 32, WHOLE>, 32);
+    if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, 2, 32, WHOLE>, 32);
+    if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, 3, 32, WHOLE>, 32);
+    if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, 4, 32, WHOLE>, 32);
+    if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, 6, 32, WHOLE>, 32);
+    if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, 8, 32, WHOLE>, 32);
+    if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, 12, 32, WHOLE>, 32);
+    if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, 16, 32, WHOLE>, 32);
+    constexpr int kBlockWords = 4;                            // a thread's, where a CTA holds the row
+    if (words <= kNormMaxBlock * kBlockWords)
+        return launch(layernorm_forward_kernel<T, kBlockWords, 0, WHOLE>, dim3(static_cast<unsigned>(a.rows), M),
+                      static_cast<int>(ceil_div(words, 32 * kBlockWords)) * 32, 0, stream, false, a);
+    return launch(layernorm_forward_long_kernel<T, WHOLE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
 }
 
-// Rows that a CTA of the register kernels handles at a time.
-static int norm_groups(int64_t cols) { return cols <= 64 ? kNormThreads / 8 : cols <= 1024 ? kNormThreads / 32 : 1; }
+// How the backward pass lays a row out: NV words in each of `lanes` lanes (8, 32, or a CTA's threads), rows too long for
+// that apart.
+struct NormLayout {
+    int words, lanes;                                         // words of a lane; 0: the row is too long
+};
+static NormLayout norm_layout(int64_t cols, int64_t elem)
+{
+    const int64_t words = ceil_div(cols * elem, 16);
+    const int step = elem == 4 ? 2 : 1;                       // words of 8 elements
+    const int block_words = 2 * step, warp_words = 4 * step;
+    if (words <= 8) return {1, 8};
+    if (words <= 32 * warp_words) return {static_cast<int>(ceil_div(words, 32 * step)) * step, 32};
+    if (words <= kNormMaxBlock * block_words) return {block_words, static_cast<int>(ceil_div(words, 32 * block_words)) * 32};
+    return {0, 0};
+}
+// Slots of a part's column sums: one for every element of every thread, whether there is a column for it or not.
+static int64_t norm_slots(int64_t cols, int64_t elem)
+{
+    const NormLayout l = norm_layout(cols, elem);
+    return l.words ? static_cast<int64_t>(l.words) * l.lanes * (16 / elem) : cols;
+}
 
 // CTAs a worker's rows are split over in the backward pass (a rule on the sizes alone, so that the order of
 // the additions does not change from call to call).  Few rows go to one CTA, which then writes the
 // gradients itself: the second launch costs more than a few rows one after the other.
 static int norm_parts(int64_t rows, int64_t cols, int M, int64_t elem)
 {
-    if (cols > kLongBackward) {
-        const int64_t want = std::max<int64_t>(1, 8 * kSms / std::max<int64_t>(1, M * ceil_div(cols, kNormThreads)));
+    const NormLayout l = norm_layout(cols, elem);
+    if (l.words == 0) {
+        const int64_t want = 16 * kSms / (M * ceil_div(cols, 256));                 // CTAs of the column kernel
         return static_cast<int>(std::max<int64_t>(1, std::min(want, ceil_div(rows, 32))));
     }
-    const int64_t steps = ceil_div(rows, norm_groups(cols));
+    const int64_t steps = l.lanes > 32 ? rows : ceil_div(rows, kNormThreads / l.lanes);
     if (steps <= 4) return 1;
     // as many CTAs as their registers and stages let an SM hold at once
-    const bool narrow = elem == 2;
-    const int64_t per_sm = cols <= 256 ? 6 : cols <= 512 ? (narrow ? 5 : 4) : cols <= 768 ? (narrow ? 4 : 3) : cols <= 1024 ? (narrow ? 3 : 2)
-                           : 512 / (ceil_div(cols, 32 * 16) * 32);
+    const int elems = l.words * (16 / static_cast<int>(elem));
+    const int64_t per_sm = l.lanes > 32 ? std::max(1, 512 / l.lanes) : norm_ctas(elems, static_cast<int>(elem));
     return static_cast<int>(std::max<int64_t>(1, std::min(steps, kSms * per_sm / M)));
 }
 
-template <typename T, int VE, int EPT, int LPR>
+template <typename T, int NV, int LPR, bool WHOLE>
 static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
 {
-    const size_t smem = NormStage<T, VE, EPT>::bytes_a_thread * block;
-    if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(layernorm_backward_kernel<T, VE, EPT, LPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    return launch(layernorm_backward_kernel<T, VE, EPT, LPR>, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a);
+    auto* const kernel = layernorm_backward_kernel<T, NV, LPR, WHOLE>;
+    const size_t smem = WHOLE ? NormStage<NV>::bytes_a_thread * block : 0;
+    if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    return launch(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a);
 }
 
-template <typename T, int VE>
+template <typename T, bool WHOLE>
 static grawa_status launch_norm_backward(const NormBackwardArgs& a, int M, cudaStream_t stream)
 {
-    if (a.cols <= 64) return launch_norm_rows<T, VE, 8, 8>(a, M, kNormThreads, stream);
-    if (a.cols <= 256) return launch_norm_rows<T, VE, 8, 32>(a, M, kNormThreads, stream);
-    if (a.cols <= 512) return launch_norm_rows<T, VE, 16, 32>(a, M, kNormThreads, stream);
-    if (a.cols <= 768) return launch_norm_rows<T, VE, 24, 32>(a, M, kNormThreads, stream);
-    if (a.cols <= 1024) return launch_norm_rows<T, VE, 32, 32>(a, M, kNormThreads, stream);
-    if (a.cols <= kLongBackward) return launch_norm_rows<T, VE, 16, 0>(a, M, static_cast<int>(ceil_div(a.cols, 32 * 16)) * 32, stream);
+    const NormLayout l = norm_layout(a.cols, sizeof(T));      // its words are one of the kernels below
+    constexpr int kStep = sizeof(T) == 4 ? 2 : 1;
+    if (l.lanes == 8) return launch_norm_rows<T, 1, 8, WHOLE>(a, M, kNormThreads, stream);
+    if (l.lanes == 32) {
+        if (l.words == kStep) return launch_norm_rows<T, kStep, 32, WHOLE>(a, M, kNormThreads, stream);
+        if (l.words == 2 * kStep) return launch_norm_rows<T, 2 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
+        if (l.words == 3 * kStep) return launch_norm_rows<T, 3 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
+        return launch_norm_rows<T, 4 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
+    }
+    if (l.lanes > 32) return launch_norm_rows<T, 2 * kStep, 0, WHOLE>(a, M, l.lanes, stream);
     if (a.has_dx) {
-        const grawa_status st = launch(layernorm_backward_long_kernel<T, VE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+        const grawa_status st = launch(layernorm_backward_long_kernel<T, WHOLE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
         if (st != GRAWA_OK) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
-    return launch(layernorm_columns_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.cols, kNormThreads)), M, a.parts), kNormThreads, 0, stream, false, a);
+    return launch(layernorm_columns_kernel<T, WHOLE>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32 * (WHOLE ? kWordElems<T> : 1))), M, a.parts), kNormThreads, 0, stream, false, a);
 }
 
 template <typename T>
-static grawa_status norm_backward(const NormBackwardArgs& a, int M, int ve, cudaStream_t stream)
+static grawa_status norm_backward(const NormBackwardArgs& a, int M, bool whole, cudaStream_t stream)
 {
     if (a.rows > 0) {
-        grawa_status st;
-        if (ve == 16 / static_cast<int>(sizeof(T))) st = launch_norm_backward<T, 16 / static_cast<int>(sizeof(T))>(a, M, stream);
-        else if (sizeof(T) == 2 && ve == 2) st = launch_norm_backward<T, sizeof(T) == 2 ? 2 : 1>(a, M, stream);
-        else st = launch_norm_backward<T, 1>(a, M, stream);
+        const grawa_status st = whole ? launch_norm_backward<T, true>(a, M, stream) : launch_norm_backward<T, false>(a, M, stream);
         if (st != GRAWA_OK || a.parts == 1) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
-    return launch(layernorm_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32)), M), 32 * kFinishGroups, 0, stream, true, a);
+    return launch(layernorm_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.slots, 32)), M), 32 * kFinishGroups, 0, stream, true, a);
 }
 
 template <typename T>
-static grawa_status norm_forward(const NormForwardArgs& a, int M, int ve, cudaStream_t stream)
+static grawa_status norm_forward(const NormForwardArgs& a, int M, bool whole, cudaStream_t stream)
 {
-    if (ve == 16 / static_cast<int>(sizeof(T))) return launch_norm_forward<T, 16 / static_cast<int>(sizeof(T))>(a, M, stream);
-    if (sizeof(T) == 2 && ve == 2) return launch_norm_forward<T, sizeof(T) == 2 ? 2 : 1>(a, M, stream);
-    return launch_norm_forward<T, 1>(a, M, stream);
+    return whole ? launch_norm_forward<T, true>(a, M, stream) : launch_norm_forward<T, false>(a, M, stream);
 }
 
 // ------------------------------------------------------------------ gated feed-forward product
@@ -268,19 +285,37 @@ static void* operand_scratch(Scratch& s, int64_t rows, int64_t cols, int M, bool
     return in_place(cols, is_aligned) ? nullptr : s.take(static_cast<size_t>(M) * rows * pitch_of(cols) * 2);
 }
 
+// Operands of one shape: those that cannot be read in place are laid out again, all in one launch.
+static grawa_status make_operands(Operand* const* ops, const void* const* const* tables, void* const* scratch, int count, int64_t rows, int64_t cols, int M,
+                                  cudaStream_t stream)
+{
+    PackArgs a{};
+    int packed = 0;
+    for (int i = 0; i < count; ++i) {
+        Operand& op = *ops[i];
+        op.rows = rows; op.cols = cols; op.pitch = pitch_of(cols);
+        const bool stays = in_place(cols, all_aligned(tables[i], M, 16));
+        unsigned short* to = static_cast<unsigned short*>(scratch[i]);
+        for (int m = 0; m < M; ++m) op.base[m] = stays ? tables[i][m] : to + static_cast<size_t>(m) * rows * op.pitch;
+        if (stays) continue;
+        copy_table(a.from[packed], tables[i], M);
+        a.to[packed++] = to;
+    }
+    if (packed == 0) return GRAWA_OK;
+    a.rows = rows; a.cols = static_cast<int>(cols); a.pitch = static_cast<int>(pitch_of(cols));
+    return launch(pack_rows_kernel, dim3(static_cast<unsigned>(ceil_div(rows * (a.pitch / 8), kGatedThreads)), M, packed), kGatedThreads, 0, stream, false, a);
+}
 static grawa_status make_operand(Operand* op, const void* const* table, int64_t rows, int64_t cols, int M, void* scratch, cudaStream_t stream)
 {
-    op->rows = rows; op->cols = cols; op->pitch = pitch_of(cols);
-    if (in_place(cols, all_aligned(table, M, 16))) {
-        for (int m = 0; m < M; ++m) op->base[m] = table[m];
-        return GRAWA_OK;
-    }
-    PackArgs a{};
-    copy_table(a.from, table, M);
-    a.to = static_cast<unsigned short*>(scratch);
-    a.rows = rows; a.cols = static_cast<int>(cols); a.pitch = static_cast<int>(op->pitch);
-    for (int m = 0; m < M; ++m) op->base[m] = a.to + static_cast<size_t>(m) * rows * op->pitch;
-    return launch(pack_rows_kernel, dim3(static_cast<unsigned>(ceil_div(rows * (op->pitch / 8), kGatedThreads)), M), kGatedThreads, 0, stream, false, a);
+    return make_operands(&op, &table, &scratch, 1, rows, cols, M, stream);
+}
+static grawa_status make_weights(Operand* gate, Operand* up, const void* const* w_gate, const void* const* w_up, int64_t d_hidden, int64_t d_in, int M,
+                                 void* gate_scratch, void* up_scratch, cudaStream_t stream)
+{
+    Operand* const ops[2] = {gate, up};
+    const void* const* const tables[2] = {w_gate, w_up};
+    void* const scratch[2] = {gate_scratch, up_scratch};
+    return make_operands(ops, tables, scratch, 2, d_hidden, d_in, M, stream);
 }
 
 template <typename T, int MODE>
@@ -385,17 +420,21 @@ grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void* const* x, co
     a.x_stride = x_stride; a.y_stride = y_stride;
     a.eps = eps; a.inv_cols = 1.0f / static_cast<float>(cols);
     a.has_gamma = gamma != nullptr; a.has_beta = beta != nullptr; a.has_stats = mean != nullptr;
-    const int ve = word_elems(elem, cols, x_stride, y_stride, x, y, nullptr, M);
-    if (dtype == GRAWA_BF16) return norm_forward<__nv_bfloat16>(a, M, ve, stream);
-    if (dtype == GRAWA_F16) return norm_forward<__half>(a, M, ve, stream);
-    return norm_forward<float>(a, M, ve, stream);
+    const bool whole = rows_whole(x, M, rows, cols, x_stride, elem) && rows_whole(y, M, rows, cols, y_stride, elem);
+    if (dtype == GRAWA_BF16) return norm_forward<__nv_bfloat16>(a, M, whole, stream);
+    if (dtype == GRAWA_F16) return norm_forward<__half>(a, M, whole, stream);
+    return norm_forward<float>(a, M, whole, stream);
 }
 
 size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M)
 {
     if (!shape_ok(rows, cols, cols, cols, M, 4)) return 0;
-    const int parts = norm_parts(rows, cols, M, 2);            // 16-bit storage takes the most
-    return parts == 1 ? 0 : static_cast<size_t>(M) * parts * 2 * cols * sizeof(float);
+    size_t most = 0;                                          // of the storage types
+    for (const int64_t elem : {int64_t{2}, int64_t{4}}) {
+        const int parts = norm_parts(rows, cols, M, elem);
+        if (parts > 1) most = std::max(most, static_cast<size_t>(M) * parts * 2 * norm_slots(cols, elem) * sizeof(float));
+    }
+    return most;
 }
 
 grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, const void* const* x, const void* const* gamma,
@@ -416,7 +455,8 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     if (dgamma && !b.add(dgamma, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     if (dbeta && !b.add(dbeta, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     const bool weights = dgamma || dbeta;
-    const size_t need = weights ? grawa_layernorm_backward_workspace_bytes(rows, cols, M) : 0;
+    const int parts = norm_parts(rows, cols, M, elem);
+    const size_t need = weights && rows > 0 && parts > 1 ? grawa_layernorm_backward_workspace_bytes(rows, cols, M) : 0;
     if (need) {
         if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return GRAWA_ERR_WORKSPACE;
         const void* ws = workspace;
@@ -435,13 +475,18 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     a.partial = static_cast<float*>(workspace);
     a.rows = rows; a.cols = static_cast<int>(cols); a.inv_cols = 1.0f / static_cast<float>(cols);
     a.x_stride = x_stride; a.y_stride = y_stride;
-    a.parts = rows == 0 ? 0 : norm_parts(rows, cols, M, elem);
+    a.parts = rows == 0 ? 0 : parts;
     a.has_gamma = gamma != nullptr; a.has_dx = dx != nullptr; a.has_dgamma = dgamma != nullptr; a.has_dbeta = dbeta != nullptr;
     a.accumulate = accumulate != 0;
-    const int ve = word_elems(elem, cols, x_stride, y_stride, x, dy, dx, M);
-    if (dtype == GRAWA_BF16) return norm_backward<__nv_bfloat16>(a, M, ve, stream);
-    if (dtype == GRAWA_F16) return norm_backward<__half>(a, M, ve, stream);
-    return norm_backward<float>(a, M, ve, stream);
+    const bool whole = rows_whole(x, M, rows, cols, x_stride, elem) && rows_whole(dy, M, rows, cols, y_stride, elem) &&
+                       (!dx || rows_whole(dx, M, rows, cols, x_stride, elem));
+    const NormLayout l = norm_layout(cols, elem);
+    a.slots = static_cast<int>(norm_slots(cols, elem));
+    a.lanes = l.words ? l.lanes : a.slots;
+    a.word = l.words ? static_cast<int>(16 / elem) : 1;
+    if (dtype == GRAWA_BF16) return norm_backward<__nv_bfloat16>(a, M, whole, stream);
+    if (dtype == GRAWA_F16) return norm_backward<__half>(a, M, whole, stream);
+    return norm_backward<float>(a, M, whole, stream);
 }
 
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned)
@@ -473,8 +518,7 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
 
     Operand xo, go, uo;
     grawa_status st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
-    if (st == GRAWA_OK) st = make_operand(&go, w_gate, d_hidden, d_in, M, f.w_gate, stream);
-    if (st == GRAWA_OK) st = make_operand(&uo, w_up, d_hidden, d_in, M, f.w_up, stream);
+    if (st == GRAWA_OK) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
     for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
         GemmArgs a{};
         a.workers = std::min(kGemmWorkers, M - first);
@@ -535,14 +579,16 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
     e.da = f.da; e.du = f.du;
     e.rows = rows; e.cols = static_cast<int>(d_hidden); e.pitch = static_cast<int>(pitch);
     e.activation = act;
-    e.words = d_hidden % 8 == 0 && all_aligned(dh, M, 16) && all_aligned(gate, M, 16) && all_aligned(up, M, 16);
-    const dim3 grid(static_cast<unsigned>(ceil_div(rows * (pitch / 8), kGatedThreads)), M);
-    grawa_status st = dtype == GRAWA_BF16 ? launch(gated_grad_kernel<__nv_bfloat16>, grid, kGatedThreads, 0, stream, false, e)
-                                          : launch(gated_grad_kernel<__half>, grid, kGatedThreads, 0, stream, false, e);
+    const bool words = d_hidden % 8 == 0 && all_aligned(dh, M, 16) && all_aligned(gate, M, 16) && all_aligned(up, M, 16);
+    const int64_t threads = rows * (words ? pitch / 8 : ceil_div(pitch, 256) * 32);
+    const auto elementwise = [&](auto kernel) {
+        return launch(kernel, dim3(static_cast<unsigned>(ceil_div(threads, kGatedThreads)), M), kGatedThreads, 0, stream, false, e);
+    };
+    grawa_status st = dtype == GRAWA_BF16 ? (words ? elementwise(gated_grad_kernel<__nv_bfloat16, true>) : elementwise(gated_grad_kernel<__nv_bfloat16, false>))
+                                          : (words ? elementwise(gated_grad_kernel<__half, true>) : elementwise(gated_grad_kernel<__half, false>));
     Operand xo, go, uo;
     if (dx) {
-        if (st == GRAWA_OK) st = make_operand(&go, w_gate, d_hidden, d_in, M, f.w_gate, stream);
-        if (st == GRAWA_OK) st = make_operand(&uo, w_up, d_hidden, d_in, M, f.w_up, stream);
+        if (st == GRAWA_OK) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
         for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
             GemmArgs a{};
             a.workers = std::min(kGemmWorkers, M - first);
