@@ -10,8 +10,7 @@
 //
 // Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in its registers; a warp alone holds
 // up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
-// rows are read again from L2 instead.  WHOLE kernels are for rows of whole 16-byte words at 16-byte boundaries;
-// the others put the words of rows of any length and address together from aligned ones.
+// rows are read again from L2 instead.
 #pragma once
 #include "replica_common.cuh"
 
@@ -83,14 +82,59 @@ __device__ __forceinline__ float inverse_root(float v)
     return v > 0.0f && v < 1e30f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
-// Rows are read and written once, with the streaming hint (4 x 8192 x 4096 bf16: 95 us, 103 to 113 us without).
-// Word `at` of a row whose end is `left` elements behind the word's start; behind the end it holds zeros.
-template <typename T, bool WHOLE>
-__device__ __forceinline__ uint4 load_word(const T* row, int at, int left)
-{
-    if constexpr (WHOLE) return __ldcs(reinterpret_cast<const uint4*>(row) + at);
-    else return load_halves(reinterpret_cast<const unsigned short*>(row + at * kWordElems<T>), min(left, kWordElems<T>) * static_cast<int>(sizeof(T) / 2));
-}
+// How rows are read and written, by the alignment that all rows of a call share:
+//   kWhole   whole 16-byte words at 16-byte boundaries.  With the streaming hint, as rows are used once (forward of
+//            4 x 8192 x 4096 bf16: 95 us, 103 to 113 us without).
+//   kUnits   units of 4 bytes (fp32 rows anywhere; 16-bit rows of even length at even addresses): a lane's four
+//            units of a word are `lanes` units apart, so that a warp's accesses are contiguous.
+//   kHalves  16-bit rows anywhere: 16-byte words put together from aligned ones.  (Single 2-byte accesses took
+//            1.8 to 2 times as long: 8 x 4745 rows of 1001 bf16, forward 117 us, here 65 us.)
+enum RowMode { kWhole = 0, kUnits = 1, kHalves = 2 };
+
+template <typename T, int MODE>
+struct Rows {
+    static constexpr int VE = kWordElems<T>, EU = 4 / static_cast<int>(sizeof(T)), HALVES = sizeof(T) / 2;
+    static constexpr int WORD = MODE == kUnits ? EU : VE;     // neighbouring elements of a lane
+
+    // The column of element e of a lane's word i.
+    static __device__ __forceinline__ int column(int i, int e, int lane, int lanes)
+    {
+        if constexpr (MODE == kUnits) return ((i * 4 + e / EU) * lanes + lane) * EU + e % EU;
+        else return (i * lanes + lane) * VE + e;
+    }
+    static __device__ __forceinline__ bool any(int i, int lane, int lanes, int cols) { return column(i, 0, lane, lanes) < cols; }
+
+    // Word i of a lane that has any() of it; behind the end of the row it holds zeros.
+    static __device__ __forceinline__ uint4 load(const T* row, int i, int lane, int lanes, int cols)
+    {
+        if constexpr (MODE == kWhole) {
+            return __ldcs(reinterpret_cast<const uint4*>(row) + i * lanes + lane);
+        } else if constexpr (MODE == kUnits) {
+            const unsigned* u = reinterpret_cast<const unsigned*>(row) + i * 4 * lanes + lane;
+            const int units = cols / EU - i * 4 * lanes - lane;
+            return make_uint4(u[0], lanes < units ? u[lanes] : 0u, 2 * lanes < units ? u[2 * lanes] : 0u, 3 * lanes < units ? u[3 * lanes] : 0u);
+        } else {
+            const int at = (i * lanes + lane) * VE;
+            return load_halves(reinterpret_cast<const unsigned short*>(row + at), min(cols - at, VE) * HALVES);
+        }
+    }
+    // Its counterpart; with kHalves all lanes of a warp call it, and `segment` neighbouring lanes hold neighbouring words.
+    static __device__ __forceinline__ void store(T* row, int i, int lane, int lanes, int cols, const uint4& v, int segment)
+    {
+        if constexpr (MODE == kWhole) {
+            if (any(i, lane, lanes, cols)) __stcs(reinterpret_cast<uint4*>(row) + i * lanes + lane, v);
+        } else if constexpr (MODE == kUnits) {
+            unsigned* u = reinterpret_cast<unsigned*>(row) + i * 4 * lanes + lane;
+            const int units = cols / EU - i * 4 * lanes - lane;
+            if (0 < units) u[0] = v.x;
+            if (lanes < units) u[lanes] = v.y;
+            if (2 * lanes < units) u[2 * lanes] = v.z;
+            if (3 * lanes < units) u[3 * lanes] = v.w;
+        } else {
+            store_halves(reinterpret_cast<unsigned short*>(row), i * lanes + lane, lane % segment, segment, cols * HALVES, v, skip_of(row));
+        }
+    }
+};
 
 // Whole words, or single elements.
 template <typename T, bool WHOLE>
@@ -108,41 +152,39 @@ __device__ __forceinline__ void write_elements(T* row, int at, const float* f)
 
 // LPR = 8 or 32: that many lanes hold a row, kNormThreads / LPR rows a CTA; LPR = 0: the CTA holds it.
 // A thread holds NV words.
-template <typename T, int NV, int LPR, bool WHOLE>
+template <typename T, int NV, int LPR, int MODE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
 layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
-    constexpr int VE = kWordElems<T>, LANES = LPR ? LPR : 32, HALVES = sizeof(T) / 2;
+    using R = Rows<T, MODE>;
+    constexpr int VE = R::VE, LANES = LPR ? LPR : 32;
     const int m = blockIdx.y;
     const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % LANES : threadIdx.x;
     const long long row = LPR ? static_cast<long long>(blockIdx.x) * (kNormThreads / LANES) + threadIdx.x / LANES : blockIdx.x;
     const bool live = row < a.rows;
     if (LPR == 32 && !live) return;                           // a whole warp
-    const int cols = live ? a.cols : 0, words = (cols + VE - 1) / VE;     // a group of 8 without a row keeps its warp company
+    const int cols = live ? a.cols : 0;                       // a group of 8 without a row keeps its warp company
     const T* x = static_cast<const T*>(a.x.p[m]) + (live ? row : 0) * a.x_stride;
 
     uint4 xw[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = lane + i * lanes;
-        if (at < words) xw[i] = load_word<T, WHOLE>(x, at, cols - at * VE);
-    }
+    for (int i = 0; i < NV; ++i)
+        if (R::any(i, lane, lanes, cols)) xw[i] = R::load(x, i, lane, lanes, cols);
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (lane + i * lanes < words) add_elements<T>(xw[i], sum);
+        if (R::any(i, lane, lanes, cols)) add_elements<T>(xw[i], sum);
     const float mean = row_sum<LPR>(sum[0] + sum[1], 0) * a.inv_cols;
     float square[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = lane + i * lanes;
-        if (at >= words) continue;
+        if (!R::any(i, lane, lanes, cols)) continue;
         float f[VE];
         shifted<T>(xw[i], -mean, f);
-        if (!WHOLE && at * VE + VE > cols) {                  // the row ends inside this word
+        if (MODE != kWhole && R::column(i, VE - 1, lane, lanes) >= cols) {          // the row ends inside this word
 #pragma unroll
             for (int e = 0; e < VE; ++e)
-                if (at * VE + e >= cols) f[e] = 0.0f;
+                if (R::column(i, e, lane, lanes) >= cols) f[e] = 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < VE; ++e) square[e % 2] = fmaf(f[e], f[e], square[e % 2]);
@@ -154,49 +196,37 @@ layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
     }
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
     const T* beta = static_cast<const T*>(a.beta.p[m]);
-    unsigned short* y = reinterpret_cast<unsigned short*>(static_cast<T*>(a.y.p[m]) + (live ? row : 0) * a.y_stride);
-    if constexpr (WHOLE) {
-        // parameters inside a flat vector stand anywhere, or there are none
-        const bool words_ok = a.has_gamma && a.has_beta && skip_of(gamma) == 0 && skip_of(beta) == 0;
+    T* y = static_cast<T*>(a.y.p[m]) + (live ? row : 0) * a.y_stride;
+    // parameters inside a flat vector stand anywhere, or there are none
+    const bool by_words = MODE == kWhole && a.has_gamma && a.has_beta && skip_of(gamma) == 0 && skip_of(beta) == 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = lane + i * lanes;
-            if (at >= words) continue;
+    for (int i = 0; i < NV; ++i) {
+        const bool here = R::any(i, lane, lanes, cols);
+        if (MODE != kHalves && !here) continue;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (here) {
             float f[VE], g[VE], b[VE];
-            if (words_ok) {
-                unpack<T>(reinterpret_cast<const uint4*>(gamma)[at], g);
-                unpack<T>(reinterpret_cast<const uint4*>(beta)[at], b);
+            if (by_words) {
+                unpack<T>(reinterpret_cast<const uint4*>(gamma)[i * lanes + lane], g);
+                unpack<T>(reinterpret_cast<const uint4*>(beta)[i * lanes + lane], b);
+            } else if (MODE == kHalves && a.has_gamma && a.has_beta) {
+                unpack<T>(R::load(gamma, i, lane, lanes, cols), g);
+                unpack<T>(R::load(beta, i, lane, lanes, cols), b);
             } else {
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    g[e] = a.has_gamma ? widen(gamma[at * VE + e]) : 1.0f;
-                    b[e] = a.has_beta ? widen(beta[at * VE + e]) : 0.0f;
+                    const int col = R::column(i, e, lane, lanes);
+                    const bool in = MODE == kWhole || col < cols;
+                    g[e] = a.has_gamma && in ? widen(gamma[col]) : 1.0f;
+                    b[e] = a.has_beta && in ? widen(beta[col]) : 0.0f;
                 }
             }
             shifted<T>(xw[i], -mean, f);
 #pragma unroll
             for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
-            __stcs(reinterpret_cast<uint4*>(y) + at, pack<T>(f));
+            v = pack<T>(f);
         }
-    } else {
-        const unsigned skip = skip_of(y);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = lane + i * lanes, left = cols - at * VE;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (at < words) {
-                float f[VE], g[VE], b[VE] = {};
-#pragma unroll
-                for (int e = 0; e < VE; ++e) g[e] = 1.0f;
-                if (a.has_gamma) unpack<T>(load_word<T, false>(gamma, at, left), g);
-                if (a.has_beta) unpack<T>(load_word<T, false>(beta, at, left), b);
-                shifted<T>(xw[i], -mean, f);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) f[e] = fmaf(f[e] * rstd, g[e], b[e]);
-                v = pack<T>(f);
-            }
-            store_halves(y, at, threadIdx.x % LANES, LANES, cols * HALVES, v, skip);
-        }
+        R::store(y, i, lane, lanes, cols, v, LANES);
     }
 }
 
@@ -363,17 +393,17 @@ constexpr int norm_ctas(int elems, int bytes) { return elems <= 8 ? 6 : elems <=
 // gridDim.x CTAs a worker go through its rows in turn; a thread keeps the sums of its own columns in
 // registers over all of them, so the weights' gradients cost one small table at the end and no atomics
 // (the split depends on the sizes alone: the same bits every time).
-template <typename T, int NV, int LPR, bool WHOLE>
+template <typename T, int NV, int LPR, int MODE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock, LPR == 32 ? norm_ctas(NV * kWordElems<T>, sizeof(T)) : 1)
 layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    constexpr int VE = kWordElems<T>, EPT = NV * VE, LANES = LPR ? LPR : 32, HALVES = sizeof(T) / 2;
-    constexpr int GROUPS = LPR ? kNormThreads / LANES : 1, DEPTH = NormStage<NV>::depth;
+    using R = Rows<T, MODE>;
+    constexpr int VE = R::VE, EPT = NV * VE, LANES = LPR ? LPR : 32, GROUPS = LPR ? kNormThreads / LANES : 1;
+    constexpr int DEPTH = NormStage<NV>::depth;
     extern __shared__ uint4 ring[];                           // [depth][x, dy][NV][threads]
     const int m = blockIdx.y;
     const int lanes = LPR ? LPR : blockDim.x, lane = LPR ? threadIdx.x % LANES : threadIdx.x;
     const int group = LPR ? threadIdx.x / LANES : 0;
-    const int words = (a.cols + VE - 1) / VE;
     const T* gamma = static_cast<const T*>(a.gamma.p[m]);
     const T* xs = static_cast<const T*>(a.x.p[m]);
     const T* dys = static_cast<const T*>(a.dy.p[m]);
@@ -382,60 +412,51 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 
     float gm[EPT], dg[EPT], db[EPT];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = lane + i * lanes;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) gm[i * VE + e] = 1.0f;
-        if (a.has_gamma && at < words) unpack<T>(load_word<T, false>(gamma, at, a.cols - at * VE), gm + i * VE);
+    for (int k = 0; k < EPT; ++k) {
+        const int col = R::column(k / VE, k % VE, lane, lanes);
+        gm[k] = a.has_gamma && col < a.cols ? widen(gamma[col]) : 1.0f;
+        dg[k] = db[k] = 0.0f;
     }
-#pragma unroll
-    for (int k = 0; k < EPT; ++k) dg[k] = db[k] = 0.0f;
     const long long stride = static_cast<long long>(gridDim.x) * GROUPS;
     long long row = static_cast<long long>(blockIdx.x) * GROUPS + group;
     const auto fetch = [&](int slot, long long r) {
         if (r < a.rows) {
-            const T* x = xs + r * a.x_stride;
-            const T* dy = dys + r * a.y_stride;
+            const uint4* x = reinterpret_cast<const uint4*>(xs + r * a.x_stride) + lane;
+            const uint4* dy = reinterpret_cast<const uint4*>(dys + r * a.y_stride) + lane;
             uint4* to = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int at = lane + i * lanes;
-                if (at < words) {
-                    copy_async16(to + i * blockDim.x, x + at * VE);
-                    copy_async16(to + (NV + i) * blockDim.x, dy + at * VE);
+            for (int i = 0; i < NV; ++i)
+                if (R::any(i, lane, lanes, a.cols)) {
+                    copy_async16(to + i * blockDim.x, x + i * lanes);
+                    copy_async16(to + (NV + i) * blockDim.x, dy + i * lanes);
                 }
-            }
         }
         copy_async_commit();                                  // a group a row, also where there is none
     };
-    if constexpr (WHOLE) {
+    if constexpr (MODE == kWhole) {
 #pragma unroll
         for (int d = 0; d < DEPTH - 1; ++d) fetch(d, row + d * stride);
     }
     int buf = 0, slot = 0;
     float mean = row < a.rows ? means[row] : 0.0f, rstd = row < a.rows ? rstds[row] : 0.0f;
     for (; row - group < a.rows; row += stride) {             // the same turns for all groups of the CTA
-        const bool live = row < a.rows;
-        const int w_end = live ? words : 0;
+        const int cols = row < a.rows ? a.cols : 0;
+        const long long r = row < a.rows ? row : 0;
         uint4 xw[NV], dw[NV];
-        if constexpr (WHOLE) {
+        if constexpr (MODE == kWhole) {
             fetch(slot == 0 ? DEPTH - 1 : slot - 1, row + (DEPTH - 1) * stride);
             copy_async_wait<DEPTH - 1>();
             const uint4* from = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (lane + i * lanes < w_end) { xw[i] = from[i * blockDim.x]; dw[i] = from[(NV + i) * blockDim.x]; }
+                if (R::any(i, lane, lanes, cols)) { xw[i] = from[i * blockDim.x]; dw[i] = from[(NV + i) * blockDim.x]; }
             slot = slot + 1 == DEPTH ? 0 : slot + 1;
         } else {
-            const T* x = xs + (live ? row : 0) * a.x_stride;
-            const T* dy = dys + (live ? row : 0) * a.y_stride;
+            const T* x = xs + r * a.x_stride;
+            const T* dy = dys + r * a.y_stride;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int at = lane + i * lanes;
-                if (at >= w_end) continue;
-                xw[i] = load_word<T, false>(x, at, a.cols - at * VE);
-                dw[i] = load_word<T, false>(dy, at, a.cols - at * VE);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (R::any(i, lane, lanes, cols)) { xw[i] = R::load(x, i, lane, lanes, cols); dw[i] = R::load(dy, i, lane, lanes, cols); }
         }
         const bool more = row + stride < a.rows;
         const float next_mean = more ? means[row + stride] : 0.0f, next_rstd = more ? rstds[row + stride] : 0.0f;
@@ -443,7 +464,7 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (lane + i * lanes >= w_end) continue;
+            if (!R::any(i, lane, lanes, cols)) continue;
             float f[VE], d[VE];
             shifted<T>(xw[i], -mean, f);
             unpack<T>(dw[i], d);
@@ -460,13 +481,11 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
             s = row_sum<LPR>(s, buf);
             buf ^= 1;
             const float mg = -s.x * a.inv_cols * rstd, mgh = -s.y * a.inv_cols * rstd * rstd;
-            unsigned short* dx = reinterpret_cast<unsigned short*>(static_cast<T*>(a.dx.p[m]) + (live ? row : 0) * a.x_stride);
-            const unsigned skip = WHOLE ? 0u : skip_of(dx);
+            T* dx = static_cast<T*>(a.dx.p[m]) + r * a.x_stride;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int at = lane + i * lanes;
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (at < w_end) {
+                if (R::any(i, lane, lanes, cols)) {
                     float f[VE], d[VE];
                     shifted<T>(xw[i], -mean, f);
                     unpack<T>(dw[i], d);
@@ -474,17 +493,13 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
                     for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e], mgh, mg));
                     v = pack<T>(f);
                 }
-                if constexpr (WHOLE) {
-                    if (at < w_end) reinterpret_cast<uint4*>(dx)[at] = v;
-                } else {
-                    store_halves(dx, at, threadIdx.x % LANES, LANES, live ? a.cols * HALVES : 0, v, skip);
-                }
+                R::store(dx, i, lane, lanes, cols, v, LANES);
             }
         }
         mean = next_mean;
         rstd = next_rstd;
     }
-    if constexpr (WHOLE) copy_async_wait<0>();
+    if constexpr (MODE == kWhole) copy_async_wait<0>();
     if (!a.has_dgamma && !a.has_dbeta) return;
     if constexpr (LPR == 0) {
 #pragma unroll

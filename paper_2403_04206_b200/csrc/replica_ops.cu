@@ -89,10 +89,10 @@ static grawa_status dropout(grawa_dtype dtype, const void* const* in, const void
 
 // ------------------------------------------------------------------ layer norm
 
-// Are all rows of a row-strided operand whole 16-byte words at 16-byte boundaries?
-static bool rows_whole(const void* const* table, int M, int64_t rows, int64_t cols, int64_t stride, int64_t elem)
+// Do all rows of a row-strided operand start on, and last for, multiples of `bytes`?
+static bool rows_by(const void* const* table, int M, int64_t rows, int64_t cols, int64_t stride, int64_t elem, int64_t bytes)
 {
-    return cols * elem % 16 == 0 && (rows <= 1 || stride * elem % 16 == 0) && all_aligned(table, M, 16);
+    return cols * elem % bytes == 0 && (rows <= 1 || stride * elem % bytes == 0) && all_aligned(table, M, static_cast<size_t>(bytes));
 }
 
 static bool shape_ok(int64_t rows, int64_t cols, int64_t x_stride, int64_t y_stride, int M, int64_t elem)
@@ -109,7 +109,7 @@ static grawa_status launch_norm_short(const NormForwardArgs& a, int M, cudaStrea
     return launch(layernorm_forward_short_kernel<T, NV>, dim3(static_cast<unsigned>(ctas), M), kNormThreads, 0, stream, false, a);
 }
 
-template <typename T, bool WHOLE>
+template <typename T, int MODE>
 static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStream_t stream)
 {
     constexpr int VE = kWordElems<T>;
@@ -117,23 +117,23 @@ static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStr
     const auto lanes = [&](auto kernel, int lpr) {
         return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, false, a);
     };
-    if (words <= 8) return lanes(layernorm_forward_kernel<T, 1, 8, WHOLE>, 8);
-    if (WHOLE && per_lane <= 2 && a.has_gamma && a.has_beta && a.rows * M >= 32 * kSms * kAheadCtas &&
+    if (words <= 8) return lanes(layernorm_forward_kernel<T, 1, 8, MODE>, 8);
+    if (MODE == kWhole && per_lane <= 2 && a.has_gamma && a.has_beta && a.rows * M >= 32 * kSms * kAheadCtas &&
         all_aligned(a.gamma.p, M, 16) && all_aligned(a.beta.p, M, 16))
         return per_lane == 1 ? launch_norm_short<T, 1>(a, M, stream) : launch_norm_short<T, 2>(a, M, stream);
-    if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, 1, 32, WHOLE>, 32);
-    if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, 2, 32, WHOLE>, 32);
-    if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, 3, 32, WHOLE>, 32);
-    if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, 4, 32, WHOLE>, 32);
-    if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, 6, 32, WHOLE>, 32);
-    if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, 8, 32, WHOLE>, 32);
-    if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, 12, 32, WHOLE>, 32);
-    if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, 16, 32, WHOLE>, 32);
+    if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, 1, 32, MODE>, 32);
+    if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, 2, 32, MODE>, 32);
+    if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, 3, 32, MODE>, 32);
+    if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, 4, 32, MODE>, 32);
+    if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, 6, 32, MODE>, 32);
+    if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, 8, 32, MODE>, 32);
+    if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, 12, 32, MODE>, 32);
+    if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, 16, 32, MODE>, 32);
     constexpr int kBlockWords = 4;                            // a thread's, where a CTA holds the row
     if (words <= kNormMaxBlock * kBlockWords)
-        return launch(layernorm_forward_kernel<T, kBlockWords, 0, WHOLE>, dim3(static_cast<unsigned>(a.rows), M),
+        return launch(layernorm_forward_kernel<T, kBlockWords, 0, MODE>, dim3(static_cast<unsigned>(a.rows), M),
                       static_cast<int>(ceil_div(words, 32 * kBlockWords)) * 32, 0, stream, false, a);
-    return launch(layernorm_forward_long_kernel<T, WHOLE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+    return launch(layernorm_forward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
 }
 
 // How the backward pass lays a row out: NV words in each of `lanes` lanes (8, 32, or a CTA's threads), rows too long for
@@ -176,41 +176,44 @@ static int norm_parts(int64_t rows, int64_t cols, int M, int64_t elem)
     return static_cast<int>(std::max<int64_t>(1, std::min(steps, kSms * per_sm / M)));
 }
 
-template <typename T, int NV, int LPR, bool WHOLE>
+template <typename T, int NV, int LPR, int MODE>
 static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
 {
-    auto* const kernel = layernorm_backward_kernel<T, NV, LPR, WHOLE>;
-    const size_t smem = WHOLE ? NormStage<NV>::bytes_a_thread * block : 0;
+    auto* const kernel = layernorm_backward_kernel<T, NV, LPR, MODE>;
+    const size_t smem = MODE == kWhole ? NormStage<NV>::bytes_a_thread * block : 0;
     if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     return launch(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a);
 }
 
-template <typename T, bool WHOLE>
+template <typename T, int MODE>
 static grawa_status launch_norm_backward(const NormBackwardArgs& a, int M, cudaStream_t stream)
 {
     const NormLayout l = norm_layout(a.cols, sizeof(T));      // its words are one of the kernels below
     constexpr int kStep = sizeof(T) == 4 ? 2 : 1;
-    if (l.lanes == 8) return launch_norm_rows<T, 1, 8, WHOLE>(a, M, kNormThreads, stream);
+    if (l.lanes == 8) return launch_norm_rows<T, 1, 8, MODE>(a, M, kNormThreads, stream);
     if (l.lanes == 32) {
-        if (l.words == kStep) return launch_norm_rows<T, kStep, 32, WHOLE>(a, M, kNormThreads, stream);
-        if (l.words == 2 * kStep) return launch_norm_rows<T, 2 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
-        if (l.words == 3 * kStep) return launch_norm_rows<T, 3 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
-        return launch_norm_rows<T, 4 * kStep, 32, WHOLE>(a, M, kNormThreads, stream);
+        if (l.words == kStep) return launch_norm_rows<T, kStep, 32, MODE>(a, M, kNormThreads, stream);
+        if (l.words == 2 * kStep) return launch_norm_rows<T, 2 * kStep, 32, MODE>(a, M, kNormThreads, stream);
+        if (l.words == 3 * kStep) return launch_norm_rows<T, 3 * kStep, 32, MODE>(a, M, kNormThreads, stream);
+        return launch_norm_rows<T, 4 * kStep, 32, MODE>(a, M, kNormThreads, stream);
     }
-    if (l.lanes > 32) return launch_norm_rows<T, 2 * kStep, 0, WHOLE>(a, M, l.lanes, stream);
+    if (l.lanes > 32) return launch_norm_rows<T, 2 * kStep, 0, MODE>(a, M, l.lanes, stream);
     if (a.has_dx) {
-        const grawa_status st = launch(layernorm_backward_long_kernel<T, WHOLE>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+        const grawa_status st = launch(layernorm_backward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
         if (st != GRAWA_OK) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
-    return launch(layernorm_columns_kernel<T, WHOLE>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32 * (WHOLE ? kWordElems<T> : 1))), M, a.parts), kNormThreads, 0, stream, false, a);
+    return launch(layernorm_columns_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32 * (MODE == kWhole ? kWordElems<T> : 1))), M, a.parts), kNormThreads, 0, stream, false, a);
 }
 
 template <typename T>
-static grawa_status norm_backward(const NormBackwardArgs& a, int M, bool whole, cudaStream_t stream)
+static grawa_status norm_backward(const NormBackwardArgs& a, int M, RowMode mode, cudaStream_t stream)
 {
     if (a.rows > 0) {
-        const grawa_status st = whole ? launch_norm_backward<T, true>(a, M, stream) : launch_norm_backward<T, false>(a, M, stream);
+        grawa_status st;
+        if (mode == kWhole) st = launch_norm_backward<T, kWhole>(a, M, stream);
+        else if (sizeof(T) == 4 || mode == kUnits) st = launch_norm_backward<T, kUnits>(a, M, stream);
+        else st = launch_norm_backward<T, sizeof(T) == 4 ? kUnits : kHalves>(a, M, stream);
         if (st != GRAWA_OK || a.parts == 1) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
@@ -218,9 +221,11 @@ static grawa_status norm_backward(const NormBackwardArgs& a, int M, bool whole, 
 }
 
 template <typename T>
-static grawa_status norm_forward(const NormForwardArgs& a, int M, bool whole, cudaStream_t stream)
+static grawa_status norm_forward(const NormForwardArgs& a, int M, RowMode mode, cudaStream_t stream)
 {
-    return whole ? launch_norm_forward<T, true>(a, M, stream) : launch_norm_forward<T, false>(a, M, stream);
+    if (mode == kWhole) return launch_norm_forward<T, kWhole>(a, M, stream);
+    if (sizeof(T) == 4 || mode == kUnits) return launch_norm_forward<T, kUnits>(a, M, stream);
+    return launch_norm_forward<T, sizeof(T) == 4 ? kUnits : kHalves>(a, M, stream);
 }
 
 // ------------------------------------------------------------------ gated feed-forward product
@@ -420,10 +425,11 @@ grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void* const* x, co
     a.x_stride = x_stride; a.y_stride = y_stride;
     a.eps = eps; a.inv_cols = 1.0f / static_cast<float>(cols);
     a.has_gamma = gamma != nullptr; a.has_beta = beta != nullptr; a.has_stats = mean != nullptr;
-    const bool whole = rows_whole(x, M, rows, cols, x_stride, elem) && rows_whole(y, M, rows, cols, y_stride, elem);
-    if (dtype == GRAWA_BF16) return norm_forward<__nv_bfloat16>(a, M, whole, stream);
-    if (dtype == GRAWA_F16) return norm_forward<__half>(a, M, whole, stream);
-    return norm_forward<float>(a, M, whole, stream);
+    const auto by = [&](int64_t bytes) { return rows_by(x, M, rows, cols, x_stride, elem, bytes) && rows_by(y, M, rows, cols, y_stride, elem, bytes); };
+    const RowMode mode = by(16) ? kWhole : by(4) ? kUnits : kHalves;
+    if (dtype == GRAWA_BF16) return norm_forward<__nv_bfloat16>(a, M, mode, stream);
+    if (dtype == GRAWA_F16) return norm_forward<__half>(a, M, mode, stream);
+    return norm_forward<float>(a, M, mode, stream);
 }
 
 size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M)
@@ -478,15 +484,18 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     a.parts = rows == 0 ? 0 : parts;
     a.has_gamma = gamma != nullptr; a.has_dx = dx != nullptr; a.has_dgamma = dgamma != nullptr; a.has_dbeta = dbeta != nullptr;
     a.accumulate = accumulate != 0;
-    const bool whole = rows_whole(x, M, rows, cols, x_stride, elem) && rows_whole(dy, M, rows, cols, y_stride, elem) &&
-                       (!dx || rows_whole(dx, M, rows, cols, x_stride, elem));
+    const auto by = [&](int64_t bytes) {
+        return rows_by(x, M, rows, cols, x_stride, elem, bytes) && rows_by(dy, M, rows, cols, y_stride, elem, bytes) &&
+               (!dx || rows_by(dx, M, rows, cols, x_stride, elem, bytes));
+    };
+    const RowMode mode = by(16) ? kWhole : by(4) ? kUnits : kHalves;
     const NormLayout l = norm_layout(cols, elem);
     a.slots = static_cast<int>(norm_slots(cols, elem));
     a.lanes = l.words ? l.lanes : a.slots;
-    a.word = l.words ? static_cast<int>(16 / elem) : 1;
-    if (dtype == GRAWA_BF16) return norm_backward<__nv_bfloat16>(a, M, whole, stream);
-    if (dtype == GRAWA_F16) return norm_backward<__half>(a, M, whole, stream);
-    return norm_backward<float>(a, M, whole, stream);
+    a.word = l.words == 0 ? 1 : static_cast<int>((mode == kUnits ? 4 : 16) / elem);
+    if (dtype == GRAWA_BF16) return norm_backward<__nv_bfloat16>(a, M, mode, stream);
+    if (dtype == GRAWA_F16) return norm_backward<__half>(a, M, mode, stream);
+    return norm_backward<float>(a, M, mode, stream);
 }
 
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned)
