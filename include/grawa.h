@@ -348,9 +348,9 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
                                       grawa_stream_t stream);
 
 /* Bytes of scratch of a forward (backward = 0) or backward call.  `aligned` != 0: x, w_gate and w_up of every
- * worker are 16-byte aligned; they are then read in place when d_in is a multiple of 8 (a forward call needs
- * no scratch), and otherwise laid out again in the scratch.  A backward call also keeps da and du there.
- * 0 on invalid arguments. */
+ * worker are 16-byte aligned; they are then read in place when d_in is a multiple of 8, and otherwise laid out
+ * again in the scratch (but not by a forward call of up to 8 rows).  Sums that are split among the SMs keep their
+ * parts there, and a backward call da and du.  0 on invalid arguments. */
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned);
 
 /* Synchronises `stream` and reports whether a bounded device wait of a gated feed-forward call on the current

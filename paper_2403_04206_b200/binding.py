@@ -458,8 +458,9 @@ _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 
 def _tables(first, specs):
-    """Storage type code, then pointer table and row stride of each spec (name, tensors or None, rows, cols, mode), from the
-    native marshaller, which checks types, sizes, contiguity and that all tensors are on the current device; last the device."""
+    """Storage type code, then pointer table and row stride (of contiguous tensors: the low bits of their addresses) of each
+    spec (name, tensors or None, rows, cols, mode), from the native marshaller, which checks types, sizes, contiguity and that
+    all tensors are on the current device; last the device."""
     global _marshal
     import torch
     if _marshal is None:
@@ -568,22 +569,18 @@ def _ffn_sizes(x, w_gate):
     return rows, d_in, d_hidden
 
 
-def _all_aligned(*tables) -> int:
-    return 0 if any(t.data_ptr() % 16 for table in tables for t in table) else 1
-
-
 def grawa_gated_ffn_forward(x, w_gate, w_up, h, *, activation="silu", gate_out=None, up_out=None, workspace=None, stream=None) -> None:
     """h = act(x w_gate^T) * (x w_up^T) for each worker's x [rows, d_in], weights [d_hidden, d_in] (views into the flat
     parameter vectors will do), bfloat16 or float16; gate_out and up_out receive the two products for the backward pass."""
     lib, M = library(), len(x)
     rows, d_in, d_hidden = _ffn_sizes(x, w_gate)
     act = _ACTIVATIONS[activation] if isinstance(activation, str) else int(activation)
-    code, xt, _, gt, _, ut, _, ht, _, got, _, uot, _, dev = _tables(x, (
+    code, xt, xa, gt, ga, ut, ua, ht, _, got, _, uot, _, dev = _tables(x, (
         ("x", x, rows, d_in, 0), ("w_gate", w_gate, d_hidden, d_in, 0), ("w_up", w_up, d_hidden, d_in, 0), ("h", h, rows, d_hidden, 0),
         ("gate_out", gate_out, rows, d_hidden, _OPTIONAL), ("up_out", up_out, rows, d_hidden, _OPTIONAL)))
     keep = workspace
     if keep is None:
-        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, _all_aligned(x, w_gate, w_up)), stream)
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, 0 if xa | ga | ua else 1), stream)
     status = lib.grawa_gated_ffn_forward(code, act, xt, gt, ut, ht, got, uot, rows, d_in, d_hidden, M, *_scratch_args(keep), _stream_on(stream, dev))
     _raise(status, "grawa_gated_ffn_forward")
 
@@ -601,7 +598,7 @@ def grawa_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, 
         ("dw_gate", dw_gate, d_hidden, d_in, _OPTIONAL), ("dw_up", dw_up, d_hidden, d_in, _OPTIONAL)))
     keep = workspace
     if keep is None:
-        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, _all_aligned(x, w_gate, w_up)), stream)
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, 0 if t[4] | t[6] | t[8] else 1), stream)
     status = lib.grawa_gated_ffn_backward(t[0], act, *t[1:-1:2], rows, d_in, d_hidden, M, 1 if accumulate else 0, *_scratch_args(keep),
                                           _stream_on(stream, t[-1]))
     _raise(status, "grawa_gated_ffn_backward")

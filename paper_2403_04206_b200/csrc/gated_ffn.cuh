@@ -1,6 +1,6 @@
 // The gated feed-forward product of all M workers on the tensor cores, and its gradients.
 //
-//   forward   a = x Wg^T, u = x Wu^T, h = act(a) u                      (one kernel)
+//   forward   a = x Wg^T, u = x Wu^T, h = act(a) u                      (one kernel; two where the sum is split)
 //   backward  da = dh u act'(a), du = dh act(a)                          (one elementwise kernel)
 //             dx = da Wg + du Wu                                         (one product over both halves)
 //             dWg = da^T x, dWu = du^T x                                 (one launch)
@@ -20,6 +20,9 @@
 // by TMA.  Accumulation is fp32; da and du are rounded to the storage type once, because the tensor cores
 // take 16-bit operands (their rounding errors are independent and average out over the sums).
 //
+// Where a product has fewer tiles than there are pairs of SMs, its sum is split among them and the parts, in fp32,
+// are added by a second kernel in a fixed order.
+//
 // Every wait is bounded: a CTA whose wait runs out records it in g_ffn_status, waits (bounded) for its own
 // copies and products in flight, frees its tensor memory and returns.
 #pragma once
@@ -36,7 +39,7 @@ enum GemmMode { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
 constexpr int kGemmWorkers = 16;            // workers a launch (their tensor maps travel as kernel parameters)
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;      // of a pair
 constexpr int kHalf = 128;                  // rows of A, and columns of B, that a CTA of the pair holds
-constexpr int kStages = 5;
+constexpr int kStages = 6;
 constexpr int kABytes = kHalf * kTileK * 2, kBBytes = kHalf * kTileK * 2;
 constexpr int kStageBytes = kABytes + kBBytes;
 constexpr int kGemmSmem = kStages * kStageBytes + 8 * 4096 + 1024;     // + results on their way out; the swizzle wants aligned stages
@@ -49,8 +52,10 @@ struct GemmArgs {
     CUtensorMap common[2];
     CUtensorMap per[3][kGemmWorkers];
     void* out[3][kGemmWorkers];             // kForward: h, a, u (a and u may be NULL).  kInputGrad: dx.  kWeightGrad: dWg, dWu.
+    float* partial;                         // splits > 1: [split][tile][256 columns][256 rows]
     int workers, first_worker;
     int m_tiles, n_tiles, k_blocks;         // k_blocks: of one half
+    int splits, split_blocks;               // parts of the sum, and blocks of each
     int rows, cols;                         // of an output
     int activation, accumulate, words;      // words: outputs take 16-byte stores
 };
@@ -183,10 +188,22 @@ template <> struct TypeCode<__nv_bfloat16> { static constexpr unsigned value = 1
 
 // ------------------------------------------------------------------ activation
 
+// The normal distribution's cdf and density at a.  erf by formula 7.1.26 of Abramowitz and Stegun, "Handbook of
+// Mathematical Functions" (Hastings): 1 - erf(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x), x >= 0, to
+// 1.5e-7; it shares the exponential with the density, and gives small values at large negative a without
+// cancellation.  (With the library's erf the elementwise kernel was bound by instructions: 3.2 million
+// elements in each of 2 workers, 18.6 us.)
+__device__ __forceinline__ float2 normal_distribution(float a)
+{
+    const float x = fabsf(a) * 0.70710678118654752f, t = __fdividef(1.0f, fmaf(0.3275911f, x, 1.0f)), e = __expf(-0.5f * a * a);
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * q * e;
+    return make_float2(a >= 0.0f ? 1.0f - tail : tail, 0.39894228040143268f * e);
+}
 __device__ __forceinline__ float activation(int kind, float a)
 {
     if (kind == kSilu) return __fdividef(a, 1.0f + __expf(-a));
-    if (kind == kGelu) return 0.5f * a * (1.0f + erff(a * 0.70710678118654752f));
+    if (kind == kGelu) return a * normal_distribution(a).x;
     return a <= 0.0f ? 0.0f : a;
 }
 // v <- act(v) u, the kind decided once for 8 values.
@@ -211,8 +228,8 @@ __device__ __forceinline__ float2 activation_slope(int kind, float a)
         return make_float2(a * s, s * (1.0f + a * (1.0f - s)));
     }
     if (kind == kGelu) {
-        const float c = 0.5f * (1.0f + erff(a * 0.70710678118654752f));
-        return make_float2(a * c, fmaf(a * 0.39894228040143268f, __expf(-0.5f * a * a), c));
+        const float2 d = normal_distribution(a);
+        return make_float2(a * d.x, fmaf(a, d.y, d.x));
     }
     return make_float2(a <= 0.0f ? 0.0f : a, a > 0.0f ? 1.0f : 0.0f);
 }
@@ -303,7 +320,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     const int halves = MODE == kInputGrad ? 2 : 1;            // products that add up in one accumulator
     const int blocks = a.k_blocks * halves;
-    const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
+    const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles, units = tiles * a.splits;
     const int first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
@@ -321,17 +338,19 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     __syncthreads();
     pair_sync();                                              // both CTAs' barriers are ready before either is used
     order_after();
+    asm volatile("griddepcontrol.wait;" ::: "memory");        // what is in front on the stream has written the operands
     const unsigned tmem = tmem_slot;
 
     if (warp == 0 && lane == 0) {
         const unsigned leader_full = in_leader(full);
         int fills = 0;
         bool ok = true;
-        for (int t = first; t < tiles && ok; t += stride) {
-            const Tile tile = tile_of<MODE>(a, t);
+        for (int t = first; t < units && ok; t += stride) {
+            const Tile tile = tile_of<MODE>(a, t % tiles);
+            const int begin = t / tiles * a.split_blocks, end = min(blocks, begin + a.split_blocks);
             const int m0 = tile.m * kTileM + rank * kHalf;
             const int n0 = MODE == kForward ? tile.n * kHalf : tile.n * kTileN + rank * kHalf;
-            for (int kb = 0; kb < blocks; ++kb, ++fills) {
+            for (int kb = begin; kb < end; ++kb, ++fills) {
                 const int s = fills % kStages;
                 if (fills >= kStages && !barrier_wait(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) { ok = false; break; }
                 const unsigned bar = leader_full + 8 * s, sa = ring + s * kStageBytes, sb = sa + kABytes;
@@ -366,18 +385,19 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         constexpr unsigned a_step = (kAMn ? 2048 : 32) >> 4, b_step = (kBMn ? 2048 : 32) >> 4;   // 16 k further
         int used = 0, turn = 0;
         bool ok = true;
-        for (int t = first; t < tiles && ok; t += stride, ++turn) {
+        for (int t = first; t < units && ok; t += stride, ++turn) {
+            const int begin = t / tiles * a.split_blocks, end = min(blocks, begin + a.split_blocks);
             const unsigned d = tmem + (turn & 1) * kTileN;
             if (turn >= 2 && !barrier_wait(ready + 8 * (turn & 1), (turn / 2 - 1) & 1, &gave_up)) { ok = false; break; }
             order_after();
-            for (int kb = 0; kb < blocks; ++kb, ++used) {
+            for (int kb = begin; kb < end; ++kb, ++used) {
                 const int s = used % kStages;
                 if (!barrier_wait(full + 8 * s, (used / kStages) & 1, &gave_up)) { ok = false; break; }
                 order_after();
                 const unsigned sa = ring + s * kStageBytes, sb = sa + kABytes;
                 const unsigned long long da = matrix_descriptor(sa, kAMn ? 8192 : 16), db = matrix_descriptor(sb, kBMn ? 8192 : 16);
 #pragma unroll
-                for (int k = 0; k < kTileK / 16; ++k) mma_step(d, da + k * a_step, db + k * b_step, shape, kb > 0 || k > 0);
+                for (int k = 0; k < kTileK / 16; ++k) mma_step(d, da + k * a_step, db + k * b_step, shape, kb > begin || k > 0);
                 mma_commit(empty + 8 * s);
             }
             if (ok) mma_commit(done + 8 * (turn & 1));
@@ -392,14 +412,26 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         const unsigned leader_ready = in_leader(ready);
         unsigned char* stage = raw + (ring - smem_address(raw)) + kStages * kStageBytes + (warp - 2) * kStoreBytes;
         int turn = 0;
-        for (int t = first; t < tiles; t += stride, ++turn) {
-            const Tile tile = tile_of<MODE>(a, t);
+        for (int t = first; t < units; t += stride, ++turn) {
+            const Tile tile = tile_of<MODE>(a, t % tiles);
             if (!barrier_wait(done + 8 * (turn & 1), (turn / 2) & 1, &gave_up)) break;
             __syncwarp();
             order_after();
             const unsigned d = tmem + (turn & 1) * kTileN + (static_cast<unsigned>(quarter * 32) << 16);
             const int row = tile.m * kTileM + rank * kHalf + quarter * 32;
-            if (MODE == kForward) {
+            if (a.splits > 1) {                               // a part of the sum, as it stands: a warp's 32 rows side by side
+                float* to = a.partial + static_cast<size_t>(t) * kTileM * kTileN + rank * kHalf + quarter * 32 + lane;
+#pragma unroll 1
+                for (int c = part * kHalf; c < (part + 1) * kHalf && row < a.rows; c += 8) {
+                    if ((MODE == kForward ? tile.n * kHalf + c % kHalf : tile.n * kTileN + c) >= a.cols) break;
+                    unsigned r[8];
+                    float v[8];
+                    accumulator_load(d + c, r);
+                    accumulator_wait(r, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[(c + e) * kTileM] = v[e];
+                }
+            } else if (MODE == kForward) {
                 const int c = part * kStoreCols, col = tile.n * kHalf + c;
 #pragma unroll 1
                 for (int out = 2; out >= 0; --out) {          // u, a, h
@@ -457,6 +489,165 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
+// The parts of split sums, added in their order, and what the epilogue would have done with the sum.  A CTA takes 32 rows
+// by 32 columns of a tile (of a and of u in the forward pass), through shared memory to rows.
+constexpr int kJoinThreads = 256;
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kJoinThreads)
+gemm_join_kernel(const __grid_constant__ GemmArgs a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float sums[MODE == kForward ? 2 : 1][32][33];
+    const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
+    const Tile tile = tile_of<MODE>(a, blockIdx.x);
+    const int r0 = blockIdx.y * 32, c0 = blockIdx.z * 32, row0 = tile.m * kTileM + r0, col0 = tile.n * (MODE == kForward ? kHalf : kTileN) + c0;
+    if (row0 >= a.rows || col0 >= a.cols) return;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const float* from = a.partial + static_cast<size_t>(blockIdx.x) * kTileM * kTileN + r0 + lane;
+    const size_t step = static_cast<size_t>(tiles) * kTileM * kTileN;
+    constexpr int kSums = MODE == kForward ? 8 : 4;           // of a thread: 4 columns, of a and of u
+    float s[kSums] = {};
+    if (row0 + lane < a.rows) {
+        // (Columns behind the edge were not written; their sums are not used.)
+#pragma unroll 4
+        for (int p = 0; p < a.splits; ++p)
+#pragma unroll
+            for (int j = 0; j < kSums; ++j) {
+                const int c = warp * 4 + j % 4;
+                if (col0 + c < a.cols) s[j] += __ldcs(from + p * step + static_cast<size_t>(j / 4 * kHalf + c0 + c) * kTileM);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < kSums; ++j) sums[j / 4][lane][warp * 4 + j % 4] = s[j];
+    __syncthreads();
+    for (int j = threadIdx.x; j < 32 * 32; j += kJoinThreads) {
+        const int r = j / 32, c = j % 32;
+        if (row0 + r >= a.rows || col0 + c >= a.cols) continue;
+        const size_t at = static_cast<size_t>(row0 + r) * a.cols + col0 + c;
+        if (MODE == kForward) {
+            const float g = sums[0][r][c], u = sums[MODE == kForward ? 1 : 0][r][c];
+            if (a.out[1][tile.worker]) {
+                static_cast<T*>(a.out[1][tile.worker])[at] = narrow<T>(g);
+                static_cast<T*>(a.out[2][tile.worker])[at] = narrow<T>(u);
+            }
+            static_cast<T*>(a.out[0][tile.worker])[at] = narrow<T>(activation(a.activation, g) * u);
+        } else {
+            T* out = static_cast<T*>(a.out[tile.half][tile.worker]) + at;
+            *out = narrow<T>(MODE == kWeightGrad && a.accumulate ? widen(*out) + sums[0][r][c] : sums[0][r][c]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ a few rows
+
+// For a few rows the product is a pass over the weights: a CTA takes neighbouring columns of a and u, a warp two of
+// them at a time, its lanes neighbouring 16-byte words of the four weight rows, against the rows of x in shared
+// memory.  Products of 16-bit elements are exact in the fp32 multiply-add that takes them as they are.  Weights are
+// read where they stand, at any alignment (the tensor cores' path would lay them out again first).
+struct FewArgs {
+    In x, w_gate, w_up;
+    Out h, gate, up;                       // gate and up may be NULL
+    int rows, d_in, d_hidden, activation;
+};
+constexpr int kFewThreads = 256, kFewRows = 8;
+
+__device__ __forceinline__ void multiply_add(float& acc, unsigned x, unsigned w, __nv_bfloat16)
+{
+    asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %1;\n\tmov.b32 {c, d}, %2;\n\tfma.rn.f32.bf16 %0, a, c, %0;\n\tfma.rn.f32.bf16 %0, b, d, %0;\n\t}"
+        : "+f"(acc) : "r"(x), "r"(w));
+}
+__device__ __forceinline__ void multiply_add(float& acc, unsigned x, unsigned w, __half)
+{
+    asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %1;\n\tmov.b32 {c, d}, %2;\n\tfma.rn.f32.f16 %0, a, c, %0;\n\tfma.rn.f32.f16 %0, b, d, %0;\n\t}"
+        : "+f"(acc) : "r"(x), "r"(w));
+}
+
+// COLS: columns of a CTA, 32, or 16 where that leaves too few CTAs to keep memory busy.
+template <typename T, int ROWS, int COLS, bool WHOLE>
+__global__ void __launch_bounds__(kFewThreads, COLS == 16 ? (ROWS <= 4 ? 4 : 3) : 2)
+gated_few_kernel(const __grid_constant__ FewArgs a)
+{
+    constexpr int P = ROWS <= 1 ? 1 : ROWS <= 2 ? 2 : ROWS <= 4 ? 4 : 8;           // rows, to a power of two
+    extern __shared__ uint4 xs[];                             // [ROWS][words]
+    __shared__ float sums[2][P][COLS];
+    const int m = blockIdx.y, col0 = blockIdx.x * COLS, words = (a.d_in + 7) / 8;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const unsigned short* x = static_cast<const unsigned short*>(a.x.p[m]);
+    for (int j = threadIdx.x; j < ROWS * words; j += kFewThreads) {
+        const int r = j / words, at = j % words * 8;
+        xs[j] = r < a.rows ? load_halves(x + static_cast<size_t>(r) * a.d_in + at, min(8, a.d_in - at)) : make_uint4(0, 0, 0, 0);
+    }
+    bool staged = false;
+    for (int c = warp * 2; c < COLS && col0 + c < a.d_hidden; c += kFewThreads / 32 * 2) {
+        const unsigned short* rows[4];                        // gate and up rows of two columns (one twice at the edge)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            rows[i] = static_cast<const unsigned short*>(i & 1 ? a.w_up.p[m] : a.w_gate.p[m]) + static_cast<size_t>(min(col0 + c + i / 2, a.d_hidden - 1)) * a.d_in;
+        const auto weights = [&](uint4 (&w)[4], int k) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (WHOLE) w[i] = __ldcs(reinterpret_cast<const uint4*>(rows[i]) + k);
+                else w[i] = load_halves(rows[i] + 8 * k, min(8, a.d_in - 8 * k));
+            }
+        };
+        float v[2][2 * P] = {};
+        uint4 w[4];
+        if (lane < words) weights(w, lane);                   // on their way while x is staged
+        if (!staged) __syncthreads();
+        staged = true;
+#pragma unroll 1
+        for (int k = lane; k < words; k += 32) {
+            uint4 next[4];
+            if (k + 32 < words) weights(next, k + 32);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const uint4 in = xs[r * words + k];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float& acc = v[i / 2][(i & 1) * P + r];
+                    multiply_add(acc, in.x, w[i].x, T{});
+                    multiply_add(acc, in.y, w[i].y, T{});
+                    multiply_add(acc, in.z, w[i].z, T{});
+                    multiply_add(acc, in.w, w[i].w, T{});
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = next[i];
+        }
+        // The lanes' sums, halving the values a lane holds at every step; the lane's number says which is left.
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            int index = 0, d = 16;
+#pragma unroll
+            for (int half = P; half >= 1; half /= 2, d /= 2) {
+                const bool upper = lane & d;
+#pragma unroll
+                for (int i = 0; i < half; ++i) {
+                    const float mine = upper ? v[j][half + i] : v[j][i], other = upper ? v[j][i] : v[j][half + i];
+                    v[j][i] = mine + __shfl_xor_sync(0xffffffffu, other, d);
+                }
+                index = index * 2 + (upper ? 1 : 0);
+            }
+#pragma unroll
+            for (int e = d; e >= 1; e /= 2) v[j][0] += __shfl_xor_sync(0xffffffffu, v[j][0], e);
+            if ((lane & (2 * d - 1)) == 0) (&sums[0][0][0])[index * COLS + c + j] = v[j][0];
+        }
+    }
+    if (!staged) __syncthreads();                             // a warp without columns
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.rows * COLS; j += kFewThreads) {
+        const int r = j / COLS, c = j % COLS;
+        if (col0 + c >= a.d_hidden) continue;
+        const float g = sums[0][r][c], u = sums[1][r][c];
+        const size_t at = static_cast<size_t>(r) * a.d_hidden + col0 + c;
+        if (a.gate.p[m]) {
+            static_cast<T*>(a.gate.p[m])[at] = narrow<T>(g);
+            static_cast<T*>(a.up.p[m])[at] = narrow<T>(u);
+        }
+        static_cast<T*>(a.h.p[m])[at] = narrow<T>(activation(a.activation, g) * u);
+    }
+}
+
 // ------------------------------------------------------------------ elementwise parts
 
 struct GatedGradArgs {
@@ -468,26 +659,35 @@ struct GatedGradArgs {
 
 constexpr int kGatedThreads = 256;
 
-// da = dh u act'(a), du = dh act(a): bound by memory, 5 elements of traffic an element.  WORDS: a thread handles 8
-// neighbouring elements of a row (16-byte accesses); else a warp handles 256, lane by lane.
-template <typename T, bool WORDS>
+// da = dh u act'(a), du = dh act(a): bound by memory, 5 elements of traffic an element.  A thread handles 8 elements:
+// STEP = 8 neighbouring ones of a row (16-byte accesses), or pairs (4 bytes) or single ones, 32 pairs or elements apart, so
+// that a warp's accesses are contiguous.
+template <typename T, int STEP>
 __global__ void __launch_bounds__(kGatedThreads)
 gated_grad_kernel(const __grid_constant__ GatedGradArgs a)
 {
-    const int m = blockIdx.y, lane = threadIdx.x & 31, per_row = WORDS ? a.pitch / 8 : (a.pitch + 255) / 256 * 32;
+    const int m = blockIdx.y, lane = threadIdx.x & 31, per_row = STEP == 8 ? a.pitch / 8 : (a.pitch + 255) / 256 * 32;
     const long long at = static_cast<long long>(blockIdx.x) * kGatedThreads + threadIdx.x;
     const long long row = at / per_row;
     if (row >= a.rows) return;
-    const int col = WORDS ? static_cast<int>(at % per_row) * 8 : static_cast<int>(at % per_row) / 32 * 256 + lane;
+    const int col = STEP == 8 ? static_cast<int>(at % per_row) * 8 : static_cast<int>(at % per_row) / 32 * 256 + lane * STEP;
     const long long in = row * a.cols + col;
     const T* dh = static_cast<const T*>(a.dh.p[m]) + in;
     const T* gate = static_cast<const T*>(a.gate.p[m]) + in;
     const T* up = static_cast<const T*>(a.up.p[m]) + in;
     float d[8] = {}, g[8] = {}, u[8] = {};
-    if (WORDS) {
+    if constexpr (STEP == 8) {
         unpack<T>(*reinterpret_cast<const uint4*>(dh), d);
         unpack<T>(*reinterpret_cast<const uint4*>(gate), g);
         unpack<T>(*reinterpret_cast<const uint4*>(up), u);
+    } else if constexpr (STEP == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + 64 * e < a.cols) {
+                unpack_pair(*reinterpret_cast<const unsigned*>(dh + 64 * e), d + 2 * e, T{});
+                unpack_pair(*reinterpret_cast<const unsigned*>(gate + 64 * e), g + 2 * e, T{});
+                unpack_pair(*reinterpret_cast<const unsigned*>(up + 64 * e), u + 2 * e, T{});
+            }
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -502,9 +702,16 @@ gated_grad_kernel(const __grid_constant__ GatedGradArgs a)
     const size_t out = (static_cast<size_t>(m) * a.rows + row) * a.pitch + col;
     T* da = static_cast<T*>(a.da) + out;
     T* du = static_cast<T*>(a.du) + out;
-    if (WORDS) {
+    if constexpr (STEP == 8) {
         *reinterpret_cast<uint4*>(da) = pack<T>(u);
         *reinterpret_cast<uint4*>(du) = pack<T>(g);
+    } else if constexpr (STEP == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + 64 * e < a.cols) {
+                *reinterpret_cast<unsigned*>(da + 64 * e) = pack_pair(u[2 * e], u[2 * e + 1], T{});
+                *reinterpret_cast<unsigned*>(du + 64 * e) = pack_pair(g[2 * e], g[2 * e + 1], T{});
+            }
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)

@@ -22,7 +22,8 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 }
 
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
-// padded, all with one row stride; else contiguous tensors of rows * cols elements.
+// padded, all with one row stride; else contiguous tensors of rows * cols elements, and in place of the stride the bits
+// below 16 that any of the addresses has.
 bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kind, int device, uint64_t* address, int64_t* stride)
 {
     const char* name;
@@ -31,7 +32,7 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
     int mode;
     if (!PyArg_ParseTuple(spec, "sOLLi", &name, &bufs, &rows, &cols, &mode)) return false;
     *address = 0;
-    *stride = cols;
+    *stride = (mode & kRows) ? cols : 0;
     if (bufs == Py_None) return (mode & kOptional) ? true : fail(PyExc_TypeError, name, "expected a list of tensors, got None");
     PyObject* list = PySequence_Fast(bufs, "expected a list of tensors");
     if (list == nullptr) return false;
@@ -63,6 +64,7 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
             break;
         }
         t_tables[index][m] = reinterpret_cast<uint64_t>(t.data_ptr());
+        if (!(mode & kRows)) *stride |= static_cast<int64_t>(t_tables[index][m] & 15);
     }
     Py_DECREF(list);
     *address = reinterpret_cast<uint64_t>(t_tables[index]);
@@ -70,7 +72,7 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
 }
 
 // tables(first, device, specs): the storage type code of `first` (a list of tensors, one a worker) and, for each
-// spec, the address of its pointer table (0 for None) and its row stride.
+// spec, the address of its pointer table (0 for None) and its row stride, or the low bits of its addresses.
 PyObject* tables(PyObject*, PyObject* args)
 {
     PyObject *first, *specs;

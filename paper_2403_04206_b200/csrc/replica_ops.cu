@@ -323,19 +323,110 @@ static grawa_status make_weights(Operand* gate, Operand* up, const void* const* 
     return make_operands(ops, tables, scratch, 2, d_hidden, d_in, M, stream);
 }
 
+// How a product of `tiles` tiles, each of `blocks` steps along its sum, is laid over the pairs of SMs: the number of parts
+// that the sum is split into, by an estimate of the time in microseconds (a step 0.3, a tile's start and results 3; a second
+// kernel 3, and the parts written and read at 5 TB/s), measured on products of 8 to 74 tiles.
+static int gemm_splits(int64_t tiles, int64_t blocks, double tile_bytes)
+{
+    const int64_t pairs = kSms / 2;
+    if (tiles >= pairs) return 1;
+    const auto time = [&](int64_t s) {
+        const double steps = static_cast<double>(ceil_div(tiles * s, pairs) * ceil_div(blocks, s));
+        return steps * 0.3 + 3.0 + (s > 1 ? 3.0 + static_cast<double>(tiles * s) * 2.0 * tile_bytes / 5e6 : 0.0);
+    };
+    int64_t best = 1;
+    for (int64_t s = 2; s <= std::min<int64_t>(blocks, 16); ++s)
+        if (time(s) < time(best)) best = s;
+    return static_cast<int>(best);
+}
+
+// One launch's share of a product: the grid of tiles and the split of its sum.
+struct GemmPlan {
+    int m_tiles, n_tiles, blocks, splits, split_blocks;
+    size_t partial_bytes;
+};
+static GemmPlan gemm_plan(int mode, int workers, int64_t out_rows, int64_t out_cols, int64_t sum)
+{
+    GemmPlan p{};
+    p.m_tiles = static_cast<int>(ceil_div(out_rows, kTileM));
+    p.n_tiles = static_cast<int>(ceil_div(out_cols, mode == kForward ? kHalf : kTileN));
+    p.blocks = static_cast<int>(ceil_div(sum, kTileK));
+    const int64_t tiles = static_cast<int64_t>(workers) * (mode == kWeightGrad ? 2 : 1) * p.m_tiles * p.n_tiles;
+    const int64_t all = p.blocks * (mode == kInputGrad ? 2 : 1);
+    const double rows_used = static_cast<double>(std::min<int64_t>(ceil_div(out_rows, 32) * 32, kTileM));
+    const int64_t splits = gemm_splits(tiles, all, rows_used * kTileN * 4);
+    p.split_blocks = static_cast<int>(ceil_div(all, splits));
+    p.splits = static_cast<int>(ceil_div(all, p.split_blocks));
+    p.partial_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * kTileM * kTileN * sizeof(float) : 0;
+    return p;
+}
+// Scratch for the parts of a product of M workers (its launches use it one after the other).
+static size_t gemm_partial_bytes(int mode, int M, int64_t out_rows, int64_t out_cols, int64_t sum)
+{
+    size_t most = 0;
+    for (int first = 0; first < M; first += kGemmWorkers)
+        most = std::max(most, gemm_plan(mode, std::min(kGemmWorkers, M - first), out_rows, out_cols, sum).partial_bytes);
+    return most;
+}
+static void set_plan(GemmArgs& a, int mode, int64_t out_rows, int64_t out_cols, int64_t sum, void* partial)
+{
+    const GemmPlan p = gemm_plan(mode, a.workers, out_rows, out_cols, sum);
+    a.m_tiles = p.m_tiles; a.n_tiles = p.n_tiles; a.k_blocks = p.blocks;
+    a.splits = p.splits; a.split_blocks = p.split_blocks;
+    a.partial = static_cast<float*>(partial);
+    a.rows = static_cast<int>(out_rows); a.cols = static_cast<int>(out_cols);
+}
+
 template <typename T, int MODE>
 static grawa_status launch_gemm(const GemmArgs& a, cudaStream_t stream)
 {
     const int64_t tiles = static_cast<int64_t>(a.workers) * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
-    if (tiles > 0x7fffffff - kSms) return GRAWA_ERR_TOO_LARGE;
+    if (tiles * a.splits > 0x7fffffff - kSms) return GRAWA_ERR_TOO_LARGE;
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
-    return launch(gemm_kernel<T, MODE>, dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, kSms / 2))), kGemmThreads, kGemmSmem, stream, false, a);
+    const grawa_status st = launch(gemm_kernel<T, MODE>, dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles * a.splits, kSms / 2))), kGemmThreads,
+                                   kGemmSmem, stream, true, a);
+    if (st != GRAWA_OK || a.splits == 1) return st;
+    return launch(gemm_join_kernel<T, MODE>, dim3(static_cast<unsigned>(tiles), kTileM / 32, (MODE == kForward ? kHalf : kTileN) / 32), kJoinThreads, 0,
+                  stream, true, a);
 }
 
 template <int MODE>
 static grawa_status launch_gemm(grawa_dtype dtype, const GemmArgs& a, cudaStream_t stream)
 {
     return dtype == GRAWA_BF16 ? launch_gemm<__nv_bfloat16, MODE>(a, stream) : launch_gemm<__half, MODE>(a, stream);
+}
+
+// Up to 4 rows, or 8 where the weights would have to be laid out again, go by the kernel for a few rows, if their x fits
+// in shared memory.  (8 workers, 4096 -> 8192, bf16: 1 row 171 us, 8 rows 299 us against 251 on the tensor cores,
+// and 407 us against 251 and as much again for the layout when the weights are not aligned.)
+static bool takes_few(int64_t rows, int64_t d_in, bool w_ok)
+{
+    return rows <= (in_place(d_in, w_ok) ? kFewRows / 2 : kFewRows) && rows * ceil_div(d_in, 8) * 16 <= 96 * 1024;
+}
+
+template <typename T, int ROWS, int COLS, bool WHOLE>
+static grawa_status launch_few(const FewArgs& a, int M, cudaStream_t stream)
+{
+    auto* const kernel = gated_few_kernel<T, ROWS, COLS, WHOLE>;
+    const size_t smem = static_cast<size_t>(ROWS) * ceil_div(a.d_in, 8) * 16;
+    GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.d_hidden, COLS)), M), kFewThreads, smem, stream, false, a);
+}
+template <typename T, int ROWS>
+static grawa_status launch_few(const FewArgs& a, int M, bool whole, cudaStream_t stream)
+{
+    const bool narrow_ctas = ceil_div(a.d_hidden, 32) * M < 4 * kSms;
+    if (narrow_ctas) return whole ? launch_few<T, ROWS, 16, true>(a, M, stream) : launch_few<T, ROWS, 16, false>(a, M, stream);
+    return whole ? launch_few<T, ROWS, 32, true>(a, M, stream) : launch_few<T, ROWS, 32, false>(a, M, stream);
+}
+template <typename T>
+static grawa_status launch_few(const FewArgs& a, int M, bool whole, cudaStream_t stream)
+{
+    if (a.rows == 1) return launch_few<T, 1>(a, M, whole, stream);
+    if (a.rows == 2) return launch_few<T, 2>(a, M, whole, stream);
+    if (a.rows <= 4) return launch_few<T, 4>(a, M, whole, stream);
+    if (a.rows <= 6) return launch_few<T, 6>(a, M, whole, stream);
+    return launch_few<T, 8>(a, M, whole, stream);
 }
 
 // Outputs of [rows][cols] for the workers [first, first + count); whether they take 16-byte stores.
@@ -361,19 +452,23 @@ static bool ffn_kinds_ok(grawa_dtype dtype, grawa_activation act)
 
 // The places of a call's scratch, in the order in which they are taken.
 struct FfnScratch {
-    void *x, *w_gate, *w_up, *da, *du;
+    void *x, *w_gate, *w_up, *da, *du, *partial;
     size_t bytes;
 };
 static FfnScratch ffn_scratch(void* base, int64_t rows, int64_t d_in, int64_t d_hidden, int M, bool x_ok, bool w_ok, bool backward)
 {
     Scratch s{static_cast<char*>(base)};
     FfnScratch f{};
+    if (rows == 0 || (!backward && takes_few(rows, d_in, w_ok))) return f;
     f.x = operand_scratch(s, rows, d_in, M, x_ok);
     f.w_gate = operand_scratch(s, d_hidden, d_in, M, w_ok);
     f.w_up = operand_scratch(s, d_hidden, d_in, M, w_ok);
     if (backward) {
         f.da = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
         f.du = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
+        f.partial = s.take(std::max(gemm_partial_bytes(kInputGrad, M, rows, d_in, d_hidden), gemm_partial_bytes(kWeightGrad, M, d_hidden, d_in, rows)));
+    } else {
+        f.partial = s.take(gemm_partial_bytes(kForward, M, rows, d_hidden, d_in));
     }
     f.bytes = s.used;
     return f;
@@ -525,6 +620,20 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
     }
     if (b.clash()) return GRAWA_ERR_INVALID_ARG;
 
+    const bool w_ok = all_aligned(w_gate, M, 16) && all_aligned(w_up, M, 16);
+    if (takes_few(rows, d_in, w_ok)) {
+        FewArgs a{};
+        copy_table(a.x, x, M);
+        copy_table(a.w_gate, w_gate, M);
+        copy_table(a.w_up, w_up, M);
+        copy_table(a.h, h, M);
+        copy_table(a.gate, gate_out, M);
+        copy_table(a.up, up_out, M);
+        a.rows = static_cast<int>(rows); a.d_in = static_cast<int>(d_in); a.d_hidden = static_cast<int>(d_hidden);
+        a.activation = act;
+        const bool whole = in_place(d_in, w_ok);
+        return dtype == GRAWA_BF16 ? launch_few<__nv_bfloat16>(a, M, whole, stream) : launch_few<__half>(a, M, whole, stream);
+    }
     Operand xo, go, uo;
     grawa_status st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
     if (st == GRAWA_OK) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
@@ -532,9 +641,7 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
         GemmArgs a{};
         a.workers = std::min(kGemmWorkers, M - first);
         a.first_worker = first;
-        a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_hidden, kHalf));
-        a.k_blocks = static_cast<int>(ceil_div(d_in, kTileK));
-        a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_hidden);
+        set_plan(a, kForward, rows, d_hidden, d_in, f.partial);
         a.activation = act;
         a.words = d_hidden % 8 == 0;
         set_outputs(a, 0, h, first, a.workers);
@@ -588,13 +695,19 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
     e.da = f.da; e.du = f.du;
     e.rows = rows; e.cols = static_cast<int>(d_hidden); e.pitch = static_cast<int>(pitch);
     e.activation = act;
-    const bool words = d_hidden % 8 == 0 && all_aligned(dh, M, 16) && all_aligned(gate, M, 16) && all_aligned(up, M, 16);
-    const int64_t threads = rows * (words ? pitch / 8 : ceil_div(pitch, 256) * 32);
+    const auto by = [&](size_t bytes) {
+        return d_hidden * 2 % static_cast<int64_t>(bytes) == 0 && all_aligned(dh, M, bytes) && all_aligned(gate, M, bytes) && all_aligned(up, M, bytes);
+    };
+    const int step = by(16) ? 8 : by(4) ? 2 : 1;
+    const int64_t threads = rows * (step == 8 ? pitch / 8 : ceil_div(pitch, 256) * 32);
     const auto elementwise = [&](auto kernel) {
         return launch(kernel, dim3(static_cast<unsigned>(ceil_div(threads, kGatedThreads)), M), kGatedThreads, 0, stream, false, e);
     };
-    grawa_status st = dtype == GRAWA_BF16 ? (words ? elementwise(gated_grad_kernel<__nv_bfloat16, true>) : elementwise(gated_grad_kernel<__nv_bfloat16, false>))
-                                          : (words ? elementwise(gated_grad_kernel<__half, true>) : elementwise(gated_grad_kernel<__half, false>));
+    const auto of_type = [&](auto type) {
+        using T = decltype(type);
+        return step == 8 ? elementwise(gated_grad_kernel<T, 8>) : step == 2 ? elementwise(gated_grad_kernel<T, 2>) : elementwise(gated_grad_kernel<T, 1>);
+    };
+    grawa_status st = dtype == GRAWA_BF16 ? of_type(__nv_bfloat16{}) : of_type(__half{});
     Operand xo, go, uo;
     if (dx) {
         if (st == GRAWA_OK) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
@@ -602,9 +715,7 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
             GemmArgs a{};
             a.workers = std::min(kGemmWorkers, M - first);
             a.first_worker = first;
-            a.m_tiles = static_cast<int>(ceil_div(rows, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_in, kTileN));
-            a.k_blocks = static_cast<int>(ceil_div(d_hidden, kTileK));
-            a.rows = static_cast<int>(rows); a.cols = static_cast<int>(d_in);
+            set_plan(a, kInputGrad, rows, d_in, d_hidden, f.partial);
             a.words = d_in % 8 == 0;
             set_outputs(a, 0, dx, first, a.workers);
             st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kHalf);
@@ -622,9 +733,7 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
             GemmArgs a{};
             a.workers = std::min(kGemmWorkers, M - first);
             a.first_worker = first;
-            a.m_tiles = static_cast<int>(ceil_div(d_hidden, kTileM)); a.n_tiles = static_cast<int>(ceil_div(d_in, kTileN));
-            a.k_blocks = static_cast<int>(ceil_div(rows, kTileK));
-            a.rows = static_cast<int>(d_hidden); a.cols = static_cast<int>(d_in);
+            set_plan(a, kWeightGrad, d_hidden, d_in, rows, f.partial);
             a.words = d_in % 8 == 0;
             a.accumulate = accumulate != 0;
             set_outputs(a, 0, dw_gate, first, a.workers);

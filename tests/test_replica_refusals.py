@@ -118,4 +118,4 @@ def test_the_marshaller_names_the_wrong_table():
             (x * 40, (), ValueError, "1 to 64 workers"), (7, (), TypeError, "len"), (x, (("y", 3, 4, 8, 0),), TypeError, "list of tensors")):
         with pytest.raises(error, match=word):
             _marshal.tables(first, 0, specs)
-    assert _marshal.tables(x, 0, (("r", None, 4, 8, 2),)) == (0, 0, 8)
+    assert _marshal.tables(x, 0, (("r", None, 4, 8, 2),)) == (0, 0, 0)
