@@ -2,8 +2,8 @@
 //
 //   forward   a = x Wg^T, u = x Wu^T, h = act(a) u                      (one kernel; two where the sum is split)
 //   backward  da = dh u act'(a), du = dh act(a)                          (one elementwise kernel)
-//             dx = da Wg + du Wu                                         (one product over both halves)
-//             dWg = da^T x, dWu = du^T x                                 (one launch)
+//             dx = da Wg + du Wu, dWg = da^T x, dWu = du^T x             (one kernel where their operands fit in L2
+//                                                                         together, else two)
 //
 // All three products run in gemm_kernel: a persistent pair of CTAs (a cluster) per two SMs walks over 256 x 256
 // tiles; each CTA holds 128 rows of A and 128 of the 256 columns of B, so a byte in shared memory feeds twice
@@ -34,7 +34,7 @@ namespace grawa {
 namespace replica {
 
 enum Activation { kSilu = 0, kGelu = 1, kRelu = 2 };
-enum GemmMode { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
+enum GemmPartName { kInputGrad = 0, kWeightGrad = 1 };     // the two products of the backward pass
 
 constexpr int kGemmWorkers = 16;            // workers a launch (their tensor maps travel as kernel parameters)
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;      // of a pair
@@ -46,18 +46,26 @@ constexpr int kGemmSmem = kStages * kStageBytes + 8 * 4096 + 1024;     // + resu
 constexpr int kGemmThreads = 320;           // warp 0: copies, warp 1: products, warps 2..9: results
 constexpr int kTileGroup = 8;               // tiles along M that are walked through together, for L2
 
-struct GemmArgs {
-    // kForward: per = x, Wg, Wu.  kInputGrad: common = da, du of all workers, per = Wg, Wu.
-    // kWeightGrad: common = da, du, per = x.
-    CUtensorMap common[2];
-    CUtensorMap per[3][kGemmWorkers];
-    void* out[3][kGemmWorkers];             // kForward: h, a, u (a and u may be NULL).  kInputGrad: dx.  kWeightGrad: dWg, dWu.
+// A product: its grid of tiles, and the split of its sum.  A unit of work is one part of one tile's sum.
+struct GemmPart {
     float* partial;                         // splits > 1: [split][tile][256 columns][256 rows]
+    int m_tiles, n_tiles, tiles, units;     // units = tiles * splits
+    int half_blocks, blocks;                // steps of kTileK along the sum: of one half (dx adds two products), and of all
+    int splits, split_blocks;               // parts of the sum, and steps of each
+    int rows, cols, words;                  // of an output; words: outputs take 16-byte stores
+};
+
+struct GemmArgs {
+    // forward: per = x, Wg, Wu.  Backward: common = da, du as dx takes them, then as the weights' gradients do, of
+    // all workers; per = Wg, Wu, x.
+    CUtensorMap common[4];
+    CUtensorMap per[3][kGemmWorkers];
+    void* out[3][kGemmWorkers];             // forward: h, a, u (a and u may be NULL).  Backward: dx, dWg, dWu.
+    GemmPart part[2];                       // forward: one.  Backward: kInputGrad, kWeightGrad; without units where not wanted
+    // Pair p of CTAs takes units p, p + pairs, ... of part `lead`, then the other part's units [share[p], share[p + 1]).
+    int lead, share[kSms / 2 + 1];
     int workers, first_worker;
-    int m_tiles, n_tiles, k_blocks;         // k_blocks: of one half
-    int splits, split_blocks;               // parts of the sum, and blocks of each
-    int rows, cols;                         // of an output
-    int activation, accumulate, words;      // words: outputs take 16-byte stores
+    int activation, accumulate;
 };
 
 __device__ int g_ffn_status = 0;            // 1: a wait ran out since the word was read
@@ -236,22 +244,42 @@ __device__ __forceinline__ float2 activation_slope(int kind, float a)
 
 // ------------------------------------------------------------------ the product
 
-struct Tile { int worker, half, m, n; };
+struct Unit { int part, slot, worker, half, m, n, begin, end; };   // slot: the unit's place in its part; [begin, end): steps of the sum
 
 // Tiles of one worker and half stand together; inside, kTileGroup tiles along M are walked through before
 // the next one along N, so that the operands of the tiles in flight stay in L2.
-template <int MODE>
-__device__ __forceinline__ Tile tile_of(const GemmArgs& a, int t)
+template <bool FORWARD>
+__device__ __forceinline__ Unit unit_of(const GemmArgs& a, int part, int slot)
 {
-    const int per = a.m_tiles * a.n_tiles, whole = t / per, in = t % per;
-    Tile r;
-    r.worker = MODE == kWeightGrad ? whole / 2 : whole;
-    r.half = MODE == kWeightGrad ? whole % 2 : 0;
-    const int group = in / (kTileGroup * a.n_tiles), first = group * kTileGroup, high = min(kTileGroup, a.m_tiles - first);
-    const int at = in - group * kTileGroup * a.n_tiles;
-    r.m = first + at % high;
-    r.n = at / high;
-    return r;
+    const GemmPart& p = a.part[part];
+    const int t = slot % p.tiles, per = p.m_tiles * p.n_tiles, whole = t / per, in = t % per, halves = !FORWARD && part == kWeightGrad ? 2 : 1;
+    Unit u;
+    u.part = part;
+    u.slot = slot;
+    u.worker = whole / halves;
+    u.half = whole % halves;
+    const int group = in / (kTileGroup * p.n_tiles), first = group * kTileGroup, high = min(kTileGroup, p.m_tiles - first);
+    const int at = in - group * kTileGroup * p.n_tiles;
+    u.m = first + at % high;
+    u.n = at / high;
+    u.begin = slot / p.tiles * p.split_blocks;
+    u.end = min(p.blocks, u.begin + p.split_blocks);
+    return u;
+}
+// The pair's unit number `turn`; false when it has no more.
+template <bool FORWARD>
+__device__ __forceinline__ bool next_unit(const GemmArgs& a, int turn, Unit& u)
+{
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2, units = a.part[a.lead].units, own = units > pair ? (units - pair + pairs - 1) / pairs : 0;
+    if (turn < own) {
+        u = unit_of<FORWARD>(a, a.lead, pair + turn * pairs);
+        return true;
+    }
+    if (FORWARD) return false;
+    const int slot = a.share[pair] + turn - own;
+    if (slot >= a.share[pair + 1]) return false;
+    u = unit_of<FORWARD>(a, 1 - a.lead, slot);
+    return true;
 }
 
 // Results go to memory by way of a warp's own 4 KB of shared memory, 32 rows by 64 columns of 16 bits: a thread
@@ -267,23 +295,35 @@ __device__ __forceinline__ uint4* store_slot(unsigned char* stage, int row, int 
     return reinterpret_cast<uint4*>(stage + row * 128 + ((piece ^ (row & 7)) * 16));
 }
 
-// Outputs that do not take 16-byte accesses: element by element, neighbouring lanes at neighbouring columns.
-template <typename T, bool TO_MEMORY>
-__device__ __noinline__ void move_elements(unsigned char* stage, T* out, int rows, int cols, int pitch)
+// Outputs that do not take 16-byte accesses: pairs of elements where they stand on 4-byte boundaries, else single ones,
+// neighbouring lanes at neighbouring columns, 8 rows under way at a time.  STEP: 16-bit elements of an access.
+template <typename W, int STEP, bool TO_MEMORY>
+__device__ __noinline__ void move_elements(unsigned char* stage, unsigned short* out, int rows, int cols, int pitch)
 {
     const int lane = threadIdx.x & 31;
-    for (int r = 0; r < rows; ++r)
-        for (int c = lane; c < cols; c += 32) {
-            T* at = out + static_cast<size_t>(r) * pitch + c;
-            T* in = reinterpret_cast<T*>(store_slot(stage, r, c / 8)) + c % 8;
-            if (TO_MEMORY) *at = *in;
-            else *in = *at;
+    for (int c = lane * STEP; c < cols; c += 32 * STEP)
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            W v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = r0 + i;
+                if (r >= rows) continue;
+                if (TO_MEMORY) v[i] = *reinterpret_cast<const W*>(reinterpret_cast<const unsigned short*>(store_slot(stage, r, c / 8)) + c % 8);
+                else v[i] = *reinterpret_cast<const W*>(out + static_cast<size_t>(r) * pitch + c);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = r0 + i;
+                if (r >= rows) continue;
+                if (TO_MEMORY) *reinterpret_cast<W*>(out + static_cast<size_t>(r) * pitch + c) = v[i];
+                else *reinterpret_cast<W*>(reinterpret_cast<unsigned short*>(store_slot(stage, r, c / 8)) + c % 8) = v[i];
+            }
         }
 }
 
 // Between the stage and rows [row, row + 32), columns [col, col + 64) of an output, inside its edges.
 template <typename T, bool TO_MEMORY>
-__device__ __forceinline__ void move_stage(const GemmArgs& a, unsigned char* stage, void* base, int row, int col)
+__device__ __forceinline__ void move_stage(const GemmPart& a, unsigned char* stage, void* base, int row, int col)
 {
     const int lane = threadIdx.x & 31;
     T* out = static_cast<T*>(base) + static_cast<size_t>(row) * a.cols + col;
@@ -300,12 +340,15 @@ __device__ __forceinline__ void move_stage(const GemmArgs& a, unsigned char* sta
             }
         }
     } else {
-        move_elements<T, TO_MEMORY>(stage, out, min(32, a.rows - row), min(kStoreCols, a.cols - col), a.cols);
+        unsigned short* at = reinterpret_cast<unsigned short*>(out);
+        const int rows = min(32, a.rows - row), cols = min(kStoreCols, a.cols - col);
+        if (a.cols % 2 == 0 && reinterpret_cast<uintptr_t>(at) % 4 == 0) move_elements<unsigned, 2, TO_MEMORY>(stage, at, rows, cols, a.cols);
+        else move_elements<unsigned short, 1, TO_MEMORY>(stage, at, rows, cols, a.cols);
     }
     __syncwarp();
 }
 
-template <typename T, int MODE>
+template <typename T, bool FORWARD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs a)
 {
@@ -318,10 +361,6 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     const unsigned ring = (smem_address(raw) + 1023u) & ~1023u;
     const unsigned full = smem_address(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, ready = done + 16, drain = ready + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
-    const int halves = MODE == kInputGrad ? 2 : 1;            // products that add up in one accumulator
-    const int blocks = a.k_blocks * halves;
-    const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles, units = tiles * a.splits;
-    const int first = blockIdx.x / 2, stride = gridDim.x / 2;
 
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -341,34 +380,33 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     asm volatile("griddepcontrol.wait;" ::: "memory");        // what is in front on the stream has written the operands
     const unsigned tmem = tmem_slot;
 
+    Unit u;
     if (warp == 0 && lane == 0) {
         const unsigned leader_full = in_leader(full);
         int fills = 0;
         bool ok = true;
-        for (int t = first; t < units && ok; t += stride) {
-            const Tile tile = tile_of<MODE>(a, t % tiles);
-            const int begin = t / tiles * a.split_blocks, end = min(blocks, begin + a.split_blocks);
-            const int m0 = tile.m * kTileM + rank * kHalf;
-            const int n0 = MODE == kForward ? tile.n * kHalf : tile.n * kTileN + rank * kHalf;
-            for (int kb = begin; kb < end; ++kb, ++fills) {
+        for (int turn = 0; ok && next_unit<FORWARD>(a, turn, u); ++turn) {
+            const int m0 = u.m * kTileM + rank * kHalf;
+            const int n0 = FORWARD ? u.n * kHalf : u.n * kTileN + rank * kHalf;
+            const int half_blocks = a.part[u.part].half_blocks;
+            for (int kb = u.begin; kb < u.end; ++kb, ++fills) {
                 const int s = fills % kStages;
                 if (fills >= kStages && !barrier_wait(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) { ok = false; break; }
                 const unsigned bar = leader_full + 8 * s, sa = ring + s * kStageBytes, sb = sa + kABytes;
-                const int half = MODE == kInputGrad ? kb / a.k_blocks : tile.half;
-                const int k0 = (MODE == kInputGrad ? kb % a.k_blocks : kb) * kTileK;
                 if (rank == 0) barrier_expect(full + 8 * s, 2 * kStageBytes);           // the bytes of both CTAs
-                if (MODE == kForward) {
-                    copy_2d(sa, &a.per[0][tile.worker], k0, m0, bar);
-                    copy_2d(sb, &a.per[1 + rank][tile.worker], k0, n0, bar);            // a's columns in one CTA, u's in the other
-                } else if (MODE == kInputGrad) {
-                    copy_3d(sa, &a.common[half], k0, m0, a.first_worker + tile.worker, bar);
+                if (FORWARD) {
+                    copy_2d(sa, &a.per[0][u.worker], kb * kTileK, m0, bar);
+                    copy_2d(sb, &a.per[1 + rank][u.worker], kb * kTileK, n0, bar);      // a's columns in one CTA, u's in the other
+                } else if (u.part == kInputGrad) {
+                    const int half = kb >= half_blocks, k0 = (kb - half * half_blocks) * kTileK;
+                    copy_3d(sa, &a.common[half], k0, m0, a.first_worker + u.worker, bar);
 #pragma unroll
-                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[half][tile.worker], n0 + 64 * i, k0, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[half][u.worker], n0 + 64 * i, k0, bar);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kHalf / 64; ++i) copy_3d(sa + i * 8192, &a.common[half], m0 + 64 * i, k0, a.first_worker + tile.worker, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_3d(sa + i * 8192, &a.common[2 + u.half], m0 + 64 * i, kb * kTileK, a.first_worker + u.worker, bar);
 #pragma unroll
-                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[0][tile.worker], n0 + 64 * i, k0, bar);
+                    for (int i = 0; i < kHalf / 64; ++i) copy_2d(sb + i * 8192, &a.per[2][u.worker], n0 + 64 * i, kb * kTileK, bar);
                 }
             }
         }
@@ -379,25 +417,24 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         if (!ok && rank == 0)
             for (int f = max(0, fills - kStages); f < fills; ++f) barrier_wait(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
     } else if (warp == 1 && lane == 0 && rank == 0) {
-        constexpr bool kAMn = MODE == kWeightGrad, kBMn = MODE != kForward;
-        constexpr unsigned shape = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kAMn ? 1u : 0u) << 15 | (kBMn ? 1u : 0u) << 16 |
-                                   (kTileN >> 3) << 17 | (kTileM >> 4) << 24;
-        constexpr unsigned a_step = (kAMn ? 2048 : 32) >> 4, b_step = (kBMn ? 2048 : 32) >> 4;   // 16 k further
-        int used = 0, turn = 0;
+        constexpr unsigned kShape = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTileN >> 3) << 17 | (kTileM >> 4) << 24;
+        constexpr unsigned kAMn = 1u << 15, kBMn = 1u << 16, kAlongK = 32 >> 4, kAlongMn = 2048 >> 4;   // 16 k further in a K- or an MN-major tile
+        int used = 0;
         bool ok = true;
-        for (int t = first; t < units && ok; t += stride, ++turn) {
-            const int begin = t / tiles * a.split_blocks, end = min(blocks, begin + a.split_blocks);
+        for (int turn = 0; ok && next_unit<FORWARD>(a, turn, u); ++turn) {
+            const bool a_mn = !FORWARD && u.part == kWeightGrad, b_mn = !FORWARD;
+            const unsigned shape = kShape | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u), a_step = a_mn ? kAlongMn : kAlongK, b_step = b_mn ? kAlongMn : kAlongK;
             const unsigned d = tmem + (turn & 1) * kTileN;
             if (turn >= 2 && !barrier_wait(ready + 8 * (turn & 1), (turn / 2 - 1) & 1, &gave_up)) { ok = false; break; }
             order_after();
-            for (int kb = begin; kb < end; ++kb, ++used) {
+            for (int kb = u.begin; kb < u.end; ++kb, ++used) {
                 const int s = used % kStages;
                 if (!barrier_wait(full + 8 * s, (used / kStages) & 1, &gave_up)) { ok = false; break; }
                 order_after();
                 const unsigned sa = ring + s * kStageBytes, sb = sa + kABytes;
-                const unsigned long long da = matrix_descriptor(sa, kAMn ? 8192 : 16), db = matrix_descriptor(sb, kBMn ? 8192 : 16);
+                const unsigned long long da = matrix_descriptor(sa, a_mn ? 8192 : 16), db = matrix_descriptor(sb, b_mn ? 8192 : 16);
 #pragma unroll
-                for (int k = 0; k < kTileK / 16; ++k) mma_step(d, da + k * a_step, db + k * b_step, shape, kb > begin || k > 0);
+                for (int k = 0; k < kTileK / 16; ++k) mma_step(d, da + k * a_step, db + k * b_step, shape, kb > u.begin || k > 0);
                 mma_commit(empty + 8 * s);
             }
             if (ok) mma_commit(done + 8 * (turn & 1));
@@ -408,22 +445,21 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         }
     } else if (warp >= 2) {
         const int quarter = warp & 3;                         // the lanes of tensor memory that this warp may read
-        const int part = (warp - 2) / 4;                      // its half of the columns
+        const int half = (warp - 2) / 4;                      // its half of the columns
         const unsigned leader_ready = in_leader(ready);
         unsigned char* stage = raw + (ring - smem_address(raw)) + kStages * kStageBytes + (warp - 2) * kStoreBytes;
-        int turn = 0;
-        for (int t = first; t < units; t += stride, ++turn) {
-            const Tile tile = tile_of<MODE>(a, t % tiles);
+        for (int turn = 0; next_unit<FORWARD>(a, turn, u); ++turn) {
+            const GemmPart& p = a.part[u.part];
             if (!barrier_wait(done + 8 * (turn & 1), (turn / 2) & 1, &gave_up)) break;
             __syncwarp();
             order_after();
             const unsigned d = tmem + (turn & 1) * kTileN + (static_cast<unsigned>(quarter * 32) << 16);
-            const int row = tile.m * kTileM + rank * kHalf + quarter * 32;
-            if (a.splits > 1) {                               // a part of the sum, as it stands: a warp's 32 rows side by side
-                float* to = a.partial + static_cast<size_t>(t) * kTileM * kTileN + rank * kHalf + quarter * 32 + lane;
+            const int row = u.m * kTileM + rank * kHalf + quarter * 32;
+            if (p.splits > 1) {                               // a part of the sum, as it stands: a warp's 32 rows side by side
+                float* to = p.partial + static_cast<size_t>(u.slot) * kTileM * kTileN + rank * kHalf + quarter * 32 + lane;
 #pragma unroll 1
-                for (int c = part * kHalf; c < (part + 1) * kHalf && row < a.rows; c += 8) {
-                    if ((MODE == kForward ? tile.n * kHalf + c % kHalf : tile.n * kTileN + c) >= a.cols) break;
+                for (int c = half * kHalf; c < (half + 1) * kHalf && row < p.rows; c += 8) {
+                    if ((FORWARD ? u.n * kHalf + c % kHalf : u.n * kTileN + c) >= p.cols) break;
                     unsigned r[8];
                     float v[8];
                     accumulator_load(d + c, r);
@@ -431,34 +467,34 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) to[(c + e) * kTileM] = v[e];
                 }
-            } else if (MODE == kForward) {
-                const int c = part * kStoreCols, col = tile.n * kHalf + c;
+            } else if (FORWARD) {
+                const int c = half * kStoreCols, col = u.n * kHalf + c;
 #pragma unroll 1
                 for (int out = 2; out >= 0; --out) {          // u, a, h
-                    if (a.out[out][tile.worker] == nullptr || row >= a.rows || col >= a.cols) continue;
+                    if (a.out[out][u.worker] == nullptr || row >= p.rows || col >= p.cols) continue;
 #pragma unroll 1
                     for (int q = 0; q < kStoreCols / 8; ++q) {
                         unsigned first[8], second[8];
-                        float v[8], u[8];
+                        float v[8], up[8];
                         accumulator_load(d + c + q * 8 + (out == 2 ? kHalf : 0), first);
                         if (out == 0) accumulator_load(d + c + q * 8 + kHalf, second);
                         accumulator_wait(first, v);
                         if (out == 0) {
-                            accumulator_wait(second, u);
-                            gated_product(a.activation, v, u);
+                            accumulator_wait(second, up);
+                            gated_product(a.activation, v, up);
                         }
                         *store_slot(stage, lane, q) = pack<T>(v);
                     }
-                    move_stage<T, true>(a, stage, a.out[out][tile.worker], row, col);
+                    move_stage<T, true>(p, stage, a.out[out][u.worker], row, col);
                 }
             } else {
-                void* out = a.out[tile.half][tile.worker];
-                const bool add = MODE == kWeightGrad && a.accumulate;
+                void* out = a.out[u.part == kInputGrad ? 0 : 1 + u.half][u.worker];
+                const bool add = u.part == kWeightGrad && a.accumulate;
 #pragma unroll 1
-                for (int c = part * kHalf; c < (part + 1) * kHalf; c += kStoreCols) {
-                    const int col = tile.n * kTileN + c;
-                    if (row >= a.rows || col >= a.cols) break;
-                    if (add) move_stage<T, false>(a, stage, out, row, col);
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c += kStoreCols) {
+                    const int col = u.n * kTileN + c;
+                    if (row >= p.rows || col >= p.cols) break;
+                    if (add) move_stage<T, false>(p, stage, out, row, col);
 #pragma unroll 1
                     for (int q = 0; q < kStoreCols / 8; ++q) {
                         unsigned r[8];
@@ -473,7 +509,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                         }
                         *store_slot(stage, lane, q) = pack<T>(v);
                     }
-                    move_stage<T, true>(a, stage, out, row, col);
+                    move_stage<T, true>(p, stage, out, row, col);
                 }
             }
             order_before();
@@ -492,29 +528,28 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
 // The parts of split sums, added in their order, and what the epilogue would have done with the sum.  A CTA takes 32 rows
 // by 32 columns of a tile (of a and of u in the forward pass), through shared memory to rows.
 constexpr int kJoinThreads = 256;
-template <typename T, int MODE>
+template <typename T, bool FORWARD>
 __global__ void __launch_bounds__(kJoinThreads)
-gemm_join_kernel(const __grid_constant__ GemmArgs a)
+gemm_join_kernel(const __grid_constant__ GemmArgs a, int part)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    __shared__ float sums[MODE == kForward ? 2 : 1][32][33];
-    const int tiles = a.workers * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
-    const Tile tile = tile_of<MODE>(a, blockIdx.x);
-    const int r0 = blockIdx.y * 32, c0 = blockIdx.z * 32, row0 = tile.m * kTileM + r0, col0 = tile.n * (MODE == kForward ? kHalf : kTileN) + c0;
-    if (row0 >= a.rows || col0 >= a.cols) return;
+    constexpr int kSums = FORWARD ? 8 : 4;                    // of a thread: 4 columns, of a and of u
+    __shared__ float sums[FORWARD ? 2 : 1][32][33];
+    const GemmPart& p = a.part[part];
+    const Unit t = unit_of<FORWARD>(a, part, blockIdx.x);
+    const int r0 = blockIdx.y * 32, c0 = blockIdx.z * 32, row0 = t.m * kTileM + r0, col0 = t.n * (FORWARD ? kHalf : kTileN) + c0;
+    if (row0 >= p.rows || col0 >= p.cols) return;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const float* from = a.partial + static_cast<size_t>(blockIdx.x) * kTileM * kTileN + r0 + lane;
-    const size_t step = static_cast<size_t>(tiles) * kTileM * kTileN;
-    constexpr int kSums = MODE == kForward ? 8 : 4;           // of a thread: 4 columns, of a and of u
+    const float* from = p.partial + static_cast<size_t>(blockIdx.x) * kTileM * kTileN + r0 + lane;
+    const size_t step = static_cast<size_t>(p.tiles) * kTileM * kTileN;
     float s[kSums] = {};
-    if (row0 + lane < a.rows) {
-        // (Columns behind the edge were not written; their sums are not used.)
+    if (row0 + lane < p.rows) {
 #pragma unroll 4
-        for (int p = 0; p < a.splits; ++p)
+        for (int i = 0; i < p.splits; ++i)
 #pragma unroll
             for (int j = 0; j < kSums; ++j) {
                 const int c = warp * 4 + j % 4;
-                if (col0 + c < a.cols) s[j] += __ldcs(from + p * step + static_cast<size_t>(j / 4 * kHalf + c0 + c) * kTileM);
+                if (col0 + c < p.cols) s[j] += __ldcs(from + i * step + static_cast<size_t>(j / 4 * kHalf + c0 + c) * kTileM);
             }
     }
 #pragma unroll
@@ -522,18 +557,18 @@ gemm_join_kernel(const __grid_constant__ GemmArgs a)
     __syncthreads();
     for (int j = threadIdx.x; j < 32 * 32; j += kJoinThreads) {
         const int r = j / 32, c = j % 32;
-        if (row0 + r >= a.rows || col0 + c >= a.cols) continue;
-        const size_t at = static_cast<size_t>(row0 + r) * a.cols + col0 + c;
-        if (MODE == kForward) {
-            const float g = sums[0][r][c], u = sums[MODE == kForward ? 1 : 0][r][c];
-            if (a.out[1][tile.worker]) {
-                static_cast<T*>(a.out[1][tile.worker])[at] = narrow<T>(g);
-                static_cast<T*>(a.out[2][tile.worker])[at] = narrow<T>(u);
+        if (row0 + r >= p.rows || col0 + c >= p.cols) continue;
+        const size_t at = static_cast<size_t>(row0 + r) * p.cols + col0 + c;
+        if (FORWARD) {
+            const float g = sums[0][r][c], u = sums[FORWARD ? 1 : 0][r][c];
+            if (a.out[1][t.worker]) {
+                static_cast<T*>(a.out[1][t.worker])[at] = narrow<T>(g);
+                static_cast<T*>(a.out[2][t.worker])[at] = narrow<T>(u);
             }
-            static_cast<T*>(a.out[0][tile.worker])[at] = narrow<T>(activation(a.activation, g) * u);
+            static_cast<T*>(a.out[0][t.worker])[at] = narrow<T>(activation(a.activation, g) * u);
         } else {
-            T* out = static_cast<T*>(a.out[tile.half][tile.worker]) + at;
-            *out = narrow<T>(MODE == kWeightGrad && a.accumulate ? widen(*out) + sums[0][r][c] : sums[0][r][c]);
+            T* out = static_cast<T*>(a.out[part == kInputGrad ? 0 : 1 + t.half][t.worker]) + at;
+            *out = narrow<T>(part == kWeightGrad && a.accumulate ? widen(*out) + sums[0][r][c] : sums[0][r][c]);
         }
     }
 }

@@ -323,77 +323,148 @@ static grawa_status make_weights(Operand* gate, Operand* up, const void* const* 
     return make_operands(ops, tables, scratch, 2, d_hidden, d_in, M, stream);
 }
 
-// How a product of `tiles` tiles, each of `blocks` steps along its sum, is laid over the pairs of SMs: the number of parts
-// that the sum is split into, by an estimate of the time in microseconds (a step 0.3, a tile's start and results 3; a second
-// kernel 3, and the parts written and read at 5 TB/s), measured on products of 8 to 74 tiles.
-static int gemm_splits(int64_t tiles, int64_t blocks, double tile_bytes)
+// The number of parts that the sum of a product of `tiles` tiles, of `blocks` steps each, is split into: by an estimate of
+// the time in microseconds (a step 0.4, a tile's start and results 3; a second kernel 3, and the parts written and
+// read at 5 TB/s).
+static int64_t gemm_splits(int64_t tiles, int64_t blocks, double tile_bytes)
 {
     const int64_t pairs = kSms / 2;
     if (tiles >= pairs) return 1;
     const auto time = [&](int64_t s) {
         const double steps = static_cast<double>(ceil_div(tiles * s, pairs) * ceil_div(blocks, s));
-        return steps * 0.3 + 3.0 + (s > 1 ? 3.0 + static_cast<double>(tiles * s) * 2.0 * tile_bytes / 5e6 : 0.0);
+        return steps * 0.4 + 3.0 + (s > 1 ? 3.0 + static_cast<double>(tiles * s) * 2.0 * tile_bytes / 5e6 : 0.0);
     };
     int64_t best = 1;
     for (int64_t s = 2; s <= std::min<int64_t>(blocks, 16); ++s)
         if (time(s) < time(best)) best = s;
-    return static_cast<int>(best);
+    return best;
 }
 
-// One launch's share of a product: the grid of tiles and the split of its sum.
-struct GemmPlan {
-    int m_tiles, n_tiles, blocks, splits, split_blocks;
-    size_t partial_bytes;
-};
-static GemmPlan gemm_plan(int mode, int workers, int64_t out_rows, int64_t out_cols, int64_t sum)
+// A product of [out_rows][out_cols] results for each of `copies` matrices: its tiles, with `halves` sums of `sum` elements
+// that add up in one result.  Splits are set apart (set_splits).
+static GemmPart gemm_part(int64_t copies, int64_t out_rows, int64_t out_cols, int tile_cols, int64_t sum, int halves)
 {
-    GemmPlan p{};
+    GemmPart p{};
     p.m_tiles = static_cast<int>(ceil_div(out_rows, kTileM));
-    p.n_tiles = static_cast<int>(ceil_div(out_cols, mode == kForward ? kHalf : kTileN));
-    p.blocks = static_cast<int>(ceil_div(sum, kTileK));
-    const int64_t tiles = static_cast<int64_t>(workers) * (mode == kWeightGrad ? 2 : 1) * p.m_tiles * p.n_tiles;
-    const int64_t all = p.blocks * (mode == kInputGrad ? 2 : 1);
-    const double rows_used = static_cast<double>(std::min<int64_t>(ceil_div(out_rows, 32) * 32, kTileM));
-    const int64_t splits = gemm_splits(tiles, all, rows_used * kTileN * 4);
-    p.split_blocks = static_cast<int>(ceil_div(all, splits));
-    p.splits = static_cast<int>(ceil_div(all, p.split_blocks));
-    p.partial_bytes = p.splits > 1 ? static_cast<size_t>(tiles) * p.splits * kTileM * kTileN * sizeof(float) : 0;
+    p.n_tiles = static_cast<int>(ceil_div(out_cols, tile_cols));
+    p.tiles = p.units = static_cast<int>(copies * p.m_tiles * p.n_tiles);
+    p.half_blocks = static_cast<int>(ceil_div(sum, kTileK));
+    p.blocks = p.split_blocks = p.half_blocks * halves;
+    p.splits = 1;
+    p.rows = static_cast<int>(out_rows);
+    p.cols = static_cast<int>(out_cols);
     return p;
 }
-// Scratch for the parts of a product of M workers (its launches use it one after the other).
-static size_t gemm_partial_bytes(int mode, int M, int64_t out_rows, int64_t out_cols, int64_t sum)
+static void set_splits(GemmPart& p, int64_t splits)
+{
+    p.split_blocks = static_cast<int>(ceil_div(p.blocks, splits));
+    p.splits = static_cast<int>(ceil_div(p.blocks, p.split_blocks));
+    p.units = p.tiles * p.splits;
+}
+static size_t partial_bytes(const GemmPart& p) { return p.splits > 1 ? static_cast<size_t>(p.units) * kTileM * kTileN * sizeof(float) : 0; }
+// What the results of a tile come to in fp32 (rows behind the edge are not written).
+static double tile_bytes(const GemmPart& p) { return std::min(kTileM, (p.rows + 31) / 32 * 32) * static_cast<double>(kTileN) * 4.0; }
+
+static GemmPart forward_part(int workers, int64_t rows, int64_t d_in, int64_t d_hidden)
+{
+    GemmPart p = gemm_part(workers, rows, d_hidden, kHalf, d_in, 1);
+    set_splits(p, gemm_splits(p.tiles, p.blocks, tile_bytes(p)));
+    return p;
+}
+
+// The two products of a backward pass.  Where all their operands and results fit in L2 together, one launch takes both:
+// the pairs of SMs then share out the steps of both evenly, where two launches leave many idle at the end of each
+// (2 x 1576 tokens, 768 -> 2050: 66 steps for 42 pairs, then 25 steps for 108 tiles on 74 pairs).
+struct BackwardPlan {
+    GemmPart part[2];
+    bool together;
+};
+static BackwardPlan backward_plan(int workers, int64_t rows, int64_t d_in, int64_t d_hidden, bool want_dx, bool want_dw)
+{
+    BackwardPlan b{};
+    if (want_dx) b.part[kInputGrad] = gemm_part(workers, rows, d_in, kTileN, d_hidden, 2);
+    if (want_dw) b.part[kWeightGrad] = gemm_part(2 * workers, d_hidden, d_in, kTileN, rows, 1);
+    constexpr double kFitsL2 = 96e6;
+    const double bytes = 2.0 * workers * (2.0 * rows * d_hidden + 4.0 * d_hidden * d_in + 2.0 * rows * d_in);
+    b.together = want_dx && want_dw && bytes <= kFitsL2;
+    if (b.together) {
+        // no unit much longer than an even share of all the steps: a sum is split where that saves more than joining its
+        // parts costs (and not into units of less than 8 steps)
+        const int64_t all = static_cast<int64_t>(b.part[0].tiles) * b.part[0].blocks + static_cast<int64_t>(b.part[1].tiles) * b.part[1].blocks;
+        const int64_t share = std::max<int64_t>(8, ceil_div(all, kSms / 2)) * 5 / 4;
+        for (GemmPart& p : b.part) set_splits(p, ceil_div(p.blocks, share));
+    } else {
+        for (GemmPart& p : b.part)
+            if (p.tiles) set_splits(p, gemm_splits(p.tiles, p.blocks, tile_bytes(p)));
+    }
+    return b;
+}
+
+// Scratch for the parts of split sums (the launches of a call use it one after the other), with whatever gradients the
+// call wants.
+static size_t forward_partial_bytes(int M, int64_t rows, int64_t d_in, int64_t d_hidden)
+{
+    size_t most = 0;
+    for (int first = 0; first < M; first += kGemmWorkers) most = std::max(most, partial_bytes(forward_part(std::min(kGemmWorkers, M - first), rows, d_in, d_hidden)));
+    return most;
+}
+static size_t backward_partial_bytes(int M, int64_t rows, int64_t d_in, int64_t d_hidden)
 {
     size_t most = 0;
     for (int first = 0; first < M; first += kGemmWorkers)
-        most = std::max(most, gemm_plan(mode, std::min(kGemmWorkers, M - first), out_rows, out_cols, sum).partial_bytes);
+        for (int want = 1; want < 4; ++want) {
+            const BackwardPlan b = backward_plan(std::min(kGemmWorkers, M - first), rows, d_in, d_hidden, want & 1, want & 2);
+            most = std::max(most, partial_bytes(b.part[0]) + partial_bytes(b.part[1]));
+        }
     return most;
 }
-static void set_plan(GemmArgs& a, int mode, int64_t out_rows, int64_t out_cols, int64_t sum, void* partial)
+
+// Shares the units of both parts out among the pairs: the longer ones in turn, then the shorter ones so that all pairs
+// come to about the same number of steps (a unit counts for 2 more, and for at least the 7 that its results take).
+static void set_shares(GemmArgs& a, int pairs)
 {
-    const GemmPlan p = gemm_plan(mode, a.workers, out_rows, out_cols, sum);
-    a.m_tiles = p.m_tiles; a.n_tiles = p.n_tiles; a.k_blocks = p.blocks;
-    a.splits = p.splits; a.split_blocks = p.split_blocks;
-    a.partial = static_cast<float*>(partial);
-    a.rows = static_cast<int>(out_rows); a.cols = static_cast<int>(out_cols);
+    const auto length = [](const GemmPart& p) { return std::max(7, p.split_blocks) + 2; };
+    a.lead = a.part[1].units == 0 || (a.part[0].units > 0 && length(a.part[0]) >= length(a.part[1])) ? 0 : 1;
+    const GemmPart &lead = a.part[a.lead], &rest = a.part[1 - a.lead];
+    if (rest.units == 0) return;                              // all shares are empty
+    const int64_t len = length(rest);
+    const auto load = [&](int p) { return static_cast<int64_t>(lead.units > p ? (lead.units - p + pairs - 1) / pairs : 0) * length(lead); };
+    const auto takes = [&](int p, int64_t level) { return std::max<int64_t>(0, (level - load(p)) / len); };
+    int64_t low = 0, high = load(0) + len * (rest.units + 1);  // the lowest level at which the pairs take all units
+    while (low < high) {
+        const int64_t level = (low + high) / 2;
+        int64_t taken = 0;
+        for (int p = 0; p < pairs; ++p) taken += takes(p, level);
+        if (taken >= rest.units) high = level;
+        else low = level + 1;
+    }
+    int64_t at = 0;
+    for (int p = 0; p < pairs; ++p) {
+        a.share[p] = static_cast<int>(at);
+        at = std::min<int64_t>(rest.units, at + takes(p, low));
+    }
+    a.share[pairs] = rest.units;
 }
 
-template <typename T, int MODE>
-static grawa_status launch_gemm(const GemmArgs& a, cudaStream_t stream)
+template <typename T, bool FORWARD>
+static grawa_status launch_gemm(GemmArgs& a, cudaStream_t stream)
 {
-    const int64_t tiles = static_cast<int64_t>(a.workers) * (MODE == kWeightGrad ? 2 : 1) * a.m_tiles * a.n_tiles;
-    if (tiles * a.splits > 0x7fffffff - kSms) return GRAWA_ERR_TOO_LARGE;
-    GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
-    const grawa_status st = launch(gemm_kernel<T, MODE>, dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles * a.splits, kSms / 2))), kGemmThreads,
-                                   kGemmSmem, stream, true, a);
-    if (st != GRAWA_OK || a.splits == 1) return st;
-    return launch(gemm_join_kernel<T, MODE>, dim3(static_cast<unsigned>(tiles), kTileM / 32, (MODE == kForward ? kHalf : kTileN) / 32), kJoinThreads, 0,
-                  stream, true, a);
+    const int64_t units = static_cast<int64_t>(a.part[0].units) + a.part[1].units;
+    if (units == 0) return GRAWA_OK;
+    const int pairs = static_cast<int>(std::min<int64_t>(units, kSms / 2));
+    set_shares(a, pairs);
+    GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, FORWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
+    grawa_status st = launch(gemm_kernel<T, FORWARD>, dim3(static_cast<unsigned>(2 * pairs)), kGemmThreads, kGemmSmem, stream, true, a);
+    for (int part = 0; part < 2 && st == GRAWA_OK; ++part)
+        if (a.part[part].splits > 1)
+            st = launch(gemm_join_kernel<T, FORWARD>, dim3(static_cast<unsigned>(a.part[part].tiles), kTileM / 32, (FORWARD ? kHalf : kTileN) / 32), kJoinThreads,
+                        0, stream, true, a, part);
+    return st;
 }
-
-template <int MODE>
-static grawa_status launch_gemm(grawa_dtype dtype, const GemmArgs& a, cudaStream_t stream)
+template <bool FORWARD>
+static grawa_status launch_gemm(grawa_dtype dtype, GemmArgs& a, cudaStream_t stream)
 {
-    return dtype == GRAWA_BF16 ? launch_gemm<__nv_bfloat16, MODE>(a, stream) : launch_gemm<__half, MODE>(a, stream);
+    return dtype == GRAWA_BF16 ? launch_gemm<__nv_bfloat16, FORWARD>(a, stream) : launch_gemm<__half, FORWARD>(a, stream);
 }
 
 // Up to 4 rows, or 8 where the weights would have to be laid out again, go by the kernel for a few rows, if their x fits
@@ -429,13 +500,15 @@ static grawa_status launch_few(const FewArgs& a, int M, bool whole, cudaStream_t
     return launch_few<T, 8>(a, M, whole, stream);
 }
 
-// Outputs of [rows][cols] for the workers [first, first + count); whether they take 16-byte stores.
-static void set_outputs(GemmArgs& a, int slot, void* const* table, int first, int count)
+// Outputs of the workers [first, first + count); whether they take 16-byte stores.
+static bool set_outputs(GemmArgs& a, int slot, void* const* table, int first, int count)
 {
+    bool words = true;
     for (int w = 0; w < count; ++w) {
         a.out[slot][w] = table ? table[first + w] : nullptr;
-        a.words = a.words && aligned(a.out[slot][w], 16);
+        words = words && aligned(a.out[slot][w], 16);
     }
+    return words;
 }
 
 static bool ffn_shape_ok(int64_t rows, int64_t d_in, int64_t d_hidden, int M)
@@ -466,9 +539,9 @@ static FfnScratch ffn_scratch(void* base, int64_t rows, int64_t d_in, int64_t d_
     if (backward) {
         f.da = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
         f.du = s.take(static_cast<size_t>(M) * rows * pitch_of(d_hidden) * 2);
-        f.partial = s.take(std::max(gemm_partial_bytes(kInputGrad, M, rows, d_in, d_hidden), gemm_partial_bytes(kWeightGrad, M, d_hidden, d_in, rows)));
+        f.partial = s.take(backward_partial_bytes(M, rows, d_in, d_hidden));
     } else {
-        f.partial = s.take(gemm_partial_bytes(kForward, M, rows, d_hidden, d_in));
+        f.partial = s.take(forward_partial_bytes(M, rows, d_in, d_hidden));
     }
     f.bytes = s.used;
     return f;
@@ -641,18 +714,20 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
         GemmArgs a{};
         a.workers = std::min(kGemmWorkers, M - first);
         a.first_worker = first;
-        set_plan(a, kForward, rows, d_hidden, d_in, f.partial);
         a.activation = act;
-        a.words = d_hidden % 8 == 0;
-        set_outputs(a, 0, h, first, a.workers);
-        set_outputs(a, 1, gate_out, first, a.workers);
-        set_outputs(a, 2, up_out, first, a.workers);
+        GemmPart& p = a.part[0];
+        p = forward_part(a.workers, rows, d_in, d_hidden);
+        p.partial = static_cast<float*>(f.partial);
+        p.words = d_hidden % 8 == 0;
+        p.words = set_outputs(a, 0, h, first, a.workers) && p.words;
+        p.words = set_outputs(a, 1, gate_out, first, a.workers) && p.words;
+        p.words = set_outputs(a, 2, up_out, first, a.workers) && p.words;
         for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
             st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kHalf);
             if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kHalf);
             if (st == GRAWA_OK) st = encode_map(&a.per[2][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kHalf);
         }
-        if (st == GRAWA_OK) st = launch_gemm<kForward>(dtype, a, stream);
+        if (st == GRAWA_OK) st = launch_gemm<true>(dtype, a, stream);
     }
     return st;
 }
@@ -709,39 +784,43 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
     };
     grawa_status st = dtype == GRAWA_BF16 ? of_type(__nv_bfloat16{}) : of_type(__half{});
     Operand xo, go, uo;
-    if (dx) {
-        if (st == GRAWA_OK) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
-        for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
-            GemmArgs a{};
-            a.workers = std::min(kGemmWorkers, M - first);
-            a.first_worker = first;
-            set_plan(a, kInputGrad, rows, d_in, d_hidden, f.partial);
-            a.words = d_in % 8 == 0;
-            set_outputs(a, 0, dx, first, a.workers);
-            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kHalf);
-            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kHalf);
-            for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
+    if (st == GRAWA_OK && dx) st = make_weights(&go, &uo, w_gate, w_up, d_hidden, d_in, M, f.w_gate, f.w_up, stream);
+    if (st == GRAWA_OK && dw_gate) st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
+    for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
+        GemmArgs a{};
+        a.workers = std::min(kGemmWorkers, M - first);
+        a.first_worker = first;
+        a.accumulate = accumulate != 0;
+        const BackwardPlan plan = backward_plan(a.workers, rows, d_in, d_hidden, dx != nullptr, dw_gate != nullptr);
+        GemmPart parts[2] = {plan.part[0], plan.part[1]};
+        parts[0].partial = static_cast<float*>(f.partial);
+        parts[1].partial = parts[0].partial + partial_bytes(parts[0]) / sizeof(float);
+        const bool whole = d_in % 8 == 0;
+        parts[0].words = set_outputs(a, 0, dx, first, a.workers) && whole;
+        parts[1].words = set_outputs(a, 1, dw_gate, first, a.workers) && whole;
+        parts[1].words = set_outputs(a, 2, dw_up, first, a.workers) && parts[1].words;
+        const void* const halves[2] = {f.da, f.du};
+        for (int i = 0; i < 2 && st == GRAWA_OK; ++i) {
+            st = encode_map(&a.common[i], dtype, halves[i], M, rows, d_hidden, pitch, kHalf);
+            if (st == GRAWA_OK) st = encode_map(&a.common[2 + i], dtype, halves[i], M, rows, d_hidden, pitch, kTileK);
+        }
+        for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) {
+            if (dx) {
                 st = encode_map(&a.per[0][w], dtype, go.base[first + w], 0, d_hidden, d_in, go.pitch, kTileK);
                 if (st == GRAWA_OK) st = encode_map(&a.per[1][w], dtype, uo.base[first + w], 0, d_hidden, d_in, uo.pitch, kTileK);
             }
-            if (st == GRAWA_OK) st = launch_gemm<kInputGrad>(dtype, a, stream);
+            if (st == GRAWA_OK && dw_gate) st = encode_map(&a.per[2][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kTileK);
         }
-    }
-    if (dw_gate) {
-        if (st == GRAWA_OK) st = make_operand(&xo, x, rows, d_in, M, f.x, stream);
-        for (int first = 0; first < M && st == GRAWA_OK; first += kGemmWorkers) {
-            GemmArgs a{};
-            a.workers = std::min(kGemmWorkers, M - first);
-            a.first_worker = first;
-            set_plan(a, kWeightGrad, d_hidden, d_in, rows, f.partial);
-            a.words = d_in % 8 == 0;
-            a.accumulate = accumulate != 0;
-            set_outputs(a, 0, dw_gate, first, a.workers);
-            set_outputs(a, 1, dw_up, first, a.workers);
-            st = encode_map(&a.common[0], dtype, f.da, M, rows, d_hidden, pitch, kTileK);
-            if (st == GRAWA_OK) st = encode_map(&a.common[1], dtype, f.du, M, rows, d_hidden, pitch, kTileK);
-            for (int w = 0; w < a.workers && st == GRAWA_OK; ++w) st = encode_map(&a.per[0][w], dtype, xo.base[first + w], 0, rows, d_in, xo.pitch, kTileK);
-            if (st == GRAWA_OK) st = launch_gemm<kWeightGrad>(dtype, a, stream);
+        if (plan.together) {
+            a.part[0] = parts[0];
+            a.part[1] = parts[1];
+            if (st == GRAWA_OK) st = launch_gemm<false>(dtype, a, stream);
+        } else {
+            for (int i = 0; i < 2 && st == GRAWA_OK; ++i) {
+                a.part[i] = parts[i];
+                a.part[1 - i] = GemmPart{};
+                st = launch_gemm<false>(dtype, a, stream);
+            }
         }
     }
     return st;
