@@ -108,6 +108,22 @@ def test_captured_call_takes_a_new_mask_from_the_counter(grawa):
             assert torch.equal(y[m], torch.where(keep, x[m] * 2, torch.zeros_like(x[m])))
 
 
+def test_no_elements_and_two_streams_at_once(grawa):
+    empty = [torch.empty(0, device="cuda")]
+    grawa.grawa_dropout_forward(empty, empty, 0.5, 1, 2, residual=empty)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    n, p = 3_000_001, 0.2
+    x = values(2, n, torch.bfloat16, 12)
+    y = [torch.empty_like(t) for t in x]
+    torch.cuda.synchronize()
+    for k, s in enumerate(streams):
+        grawa.grawa_dropout_forward([x[k]], [y[k]], p, SEED + k, OFFSET, stream=s)
+    torch.cuda.synchronize()
+    for k in range(2):
+        keep = keep_mask(SEED + k, OFFSET, 0, n, p).cuda()
+        assert torch.equal(y[k] != 0, keep & (x[k] != 0))
+
+
 def test_elements_past_two_to_the_31(grawa):
     n, p = 2 ** 31 + 1029, 0.5
     x = torch.ones(n, dtype=torch.bfloat16, device="cuda")

@@ -89,6 +89,67 @@ def test_backward_on_integers(grawa, kind, lead, rows, d_in, hidden):
     assert (c.grads[:, :lead] == 5.0).all()                    # what stands in front of the layer stays
 
 
+# sums long enough beside few tiles that they are split (forward; dx; the weights' gradients), operands larger together
+# than L2 (two launches in the backward pass), few rows against weights in rows of every alignment
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("lead", [0, 3])
+@pytest.mark.parametrize("rows,d_in,hidden", [(64, 4096, 256), (100, 4100, 130), (64, 200, 4096), (70, 201, 3001), (4096, 200, 130), (5000, 136, 72), (4096, 2048, 2816)])
+def test_split_sums_on_integers(grawa, rows, d_in, hidden, lead, accumulate):
+    kind = torch.bfloat16
+    c = Case(1, rows, d_in, hidden, kind, rows + hidden, True, lead)
+    if accumulate:
+        h, a, u = c.forward(grawa, "relu")
+        wa, wu = c.x[0].double() @ c.wg[0].double().T, c.x[0].double() @ c.wu[0].double().T
+        same(a[0], wa, kind, "gate")
+        same(u[0], wu, kind, "up")
+        same(h[0], torch.clamp(wa, min=0) * wu, kind, "h")
+    held = 5.0 if accumulate else 0.0
+    for dx_too in (True, False):
+        c.grads.fill_(5.0)
+        dx, dwg, dwu = c.backward(grawa, "relu", dx=dx_too, accumulate=accumulate)
+        dh, x, a, u = (t[0].double() for t in (c.dh, c.x, c.a, c.u))
+        da, du = dh * u * (a > 0), dh * a
+        if dx_too:
+            same(dx[0], da @ c.wg[0].double() + du @ c.wu[0].double(), kind, "dx")
+        same(dwg[0], held + da.T @ x, kind, "dw_gate")
+        same(dwu[0], held + du.T @ x, kind, "dw_up")
+        assert (c.grads[:, :lead] == 5.0).all()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows", range(1, 10))
+@pytest.mark.parametrize("d_in,hidden,lead", [(768, 80, 0), (768, 80, 1), (97, 33, 0), (260, 40, 2), (2056, 3, 5), (8, 2000, 0), (12288, 17, 0)])
+def test_few_rows_on_integers(grawa, kind, rows, d_in, hidden, lead):
+    c = Case(3, rows, d_in, hidden, kind, rows + d_in, True, lead)
+    h, a, u = c.forward(grawa, "relu")
+    for m in range(c.M):
+        wa, wu = c.x[m].double() @ c.wg[m].double().T, c.x[m].double() @ c.wu[m].double().T
+        same(a[m], wa, kind, "gate")
+        same(u[m], wu, kind, "up")
+        same(h[m], torch.clamp(wa, min=0) * wu, kind, "h")
+
+
+@pytest.mark.parametrize("rows,d_in,hidden", [(3, 40, 50), (130, 100, 264), (257, 70, 131)])
+@pytest.mark.parametrize("shift", [0, 1, 2])
+def test_nothing_is_written_around_the_outputs(grawa, rows, d_in, hidden, shift):
+    kind = torch.float16
+    c = Case(1, rows, d_in, hidden, kind, 11, True)
+
+    def guarded(n):
+        return torch.full((n + 128,), 3.0, dtype=kind, device="cuda")
+
+    full = [guarded(rows * hidden) for _ in range(3)] + [guarded(rows * d_in)] + [guarded(d_in * hidden) for _ in range(2)]
+    shapes = [(rows, hidden)] * 3 + [(rows, d_in)] + [(hidden, d_in)] * 2
+    h, a, u, dx, dwg, dwu = ([t[64 + shift:64 + shift + r * k].view(r, k)] for t, (r, k) in zip(full, shapes))
+    grawa.grawa_gated_ffn_forward(c.x, c.wg, c.wu, h, activation="relu", gate_out=a, up_out=u)
+    grawa.grawa_gated_ffn_backward(c.dh, c.x, c.wg, c.wu, c.a, c.u, dx, dwg, dwu, activation="relu")
+    wa = c.x[0].double() @ c.wg[0].double().T
+    same(a[0], wa, kind, "gate")
+    same(dwu[0], (c.dh[0].double() * c.a[0].double()).T @ c.x[0].double(), kind, "dw_up")
+    for t, (r, k) in zip(full, shapes):
+        assert (t[:64 + shift] == 3.0).all() and (t[64 + shift + r * k:] == 3.0).all()
+
+
 @pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
 @pytest.mark.parametrize("rows,d_in,hidden", [(1, 768, 512), (6, 264, 200), (33, 100, 77), (197, 768, 640), (300, 1024, 515)])

@@ -96,6 +96,21 @@ def test_padded_rows_and_parameters_at_odd_places(grawa, kind, cols, pad, lead):
     check_backward(grawa, d, mean, rstd, kind, pad)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("cols,pad", [(100, 0), (256, 0), (250, 0), (251, 0), (512, 0), (1025, 1)])
+def test_many_short_rows(grawa, kind, cols, pad):
+    """Enough rows that every warp takes several, in every way of reading them."""
+    d = make(2, 30011, cols, kind, cols, pad)
+    mean, rstd = check_forward(grawa, d, kind, pad)
+    check_backward(grawa, d, mean, rstd, kind, pad)
+
+
+def test_most_workers(grawa):
+    d = make(64, 9, 72, torch.bfloat16, 3)
+    mean, rstd = check_forward(grawa, d, torch.bfloat16)
+    check_backward(grawa, d, mean, rstd, torch.bfloat16)
+
+
 @pytest.mark.parametrize("cols", [40, 768, 3000, 9000])
 def test_without_parameters_and_partial_gradients(grawa, cols):
     kind = torch.bfloat16
