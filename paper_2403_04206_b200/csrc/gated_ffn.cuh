@@ -28,6 +28,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "replica_common.cuh"
 
 namespace grawa {
@@ -575,105 +577,122 @@ gemm_join_kernel(const __grid_constant__ GemmArgs a, int part)
 
 // ------------------------------------------------------------------ a few rows
 
-// For a few rows the product is a pass over the weights: a CTA takes neighbouring columns of a and u, a warp two of
-// them at a time, its lanes neighbouring 16-byte words of the four weight rows, against the rows of x in shared
-// memory.  Products of 16-bit elements are exact in the fp32 multiply-add that takes them as they are.  Weights are
-// read where they stand, at any alignment (the tensor cores' path would lay them out again first).
+// For a few rows the product is a pass over the weights, which no 256-row tile makes faster: a CTA takes 16 neighbouring
+// columns of a and u, its warps steps of 32 along the sum in turn, and the products are 16 x 8 x 16 ones of the warp-wide
+// matrix instruction (multiply-adds of the plain cores, two products an instruction, were the bound from 2 rows on:
+// 4 x 5 tokens, 768 -> 2048, 11.3 us).  As the order along the sum is free, a lane's operands are 16 neighbouring bytes of
+// a row, in the weights and in x alike: four lanes read 64 bytes of a row, where they stand, at any alignment (the
+// tcgen05 path would lay unaligned weights out again first).  x comes from the L1 cache.
 struct FewArgs {
     In x, w_gate, w_up;
     Out h, gate, up;                       // gate and up may be NULL
     int rows, d_in, d_hidden, activation;
 };
-constexpr int kFewThreads = 256, kFewRows = 8;
+constexpr int kFewThreads = 256, kFewCols = 16, kFewRows = 16;
 
-__device__ __forceinline__ void multiply_add(float& acc, unsigned x, unsigned w, __nv_bfloat16)
+// d (16 x 8) += a (16 x 16) b (16 x 8)
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1, __nv_bfloat16)
 {
-    asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %1;\n\tmov.b32 {c, d}, %2;\n\tfma.rn.f32.bf16 %0, a, c, %0;\n\tfma.rn.f32.bf16 %0, b, d, %0;\n\t}"
-        : "+f"(acc) : "r"(x), "r"(w));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void multiply_add(float& acc, unsigned x, unsigned w, __half)
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1, __half)
 {
-    asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %1;\n\tmov.b32 {c, d}, %2;\n\tfma.rn.f32.f16 %0, a, c, %0;\n\tfma.rn.f32.f16 %0, b, d, %0;\n\t}"
-        : "+f"(acc) : "r"(x), "r"(w));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// COLS: columns of a CTA, 32, or 16 where that leaves too few CTAs to keep memory busy.
-template <typename T, int ROWS, int COLS, bool WHOLE>
-__global__ void __launch_bounds__(kFewThreads, COLS == 16 ? (ROWS <= 4 ? 4 : 3) : 2)
+// How the operands are read:
+//   kFewWhole    x and the weights in whole 16-byte words at 16-byte boundaries;
+//   kFewShifted  weight rows of whole words that start anywhere (a layer inside a flat vector): all rows of a matrix start
+//                `skip` halves behind a boundary, so their aligned words are read as they are, against words of x that
+//                start `skip` halves early (8 x 1 token, 4096 -> 8192: 342 us with every word put together from two);
+//   kFewAny      rows of any length: every word put together.
+enum FewMode { kFewAny = 0, kFewWhole = 1, kFewShifted = 2 };
+
+// Word j of a row of n halves (a multiple of 8) that is cut `skip` halves in front of its start and every 8 from there;
+// the row is taken as a ring, so that word 0 begins with the `skip` halves that are left at its end.
+__device__ __forceinline__ uint4 cut_word(const unsigned short* row, int j, int n, unsigned skip)
+{
+    if (j > 0 || skip == 0) return load_halves(row + 8 * j - static_cast<int>(skip), 8);
+    return shift_halves(load_halves(row + n - 8, 8), load_halves(row, 8), 8 - skip);
+}
+
+// NT: groups of 8 rows of x.
+template <typename T, int NT, int MODE>
+__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 4 : MODE == kFewShifted ? 2 : 3)
 gated_few_kernel(const __grid_constant__ FewArgs a)
 {
-    constexpr int P = ROWS <= 1 ? 1 : ROWS <= 2 ? 2 : ROWS <= 4 ? 4 : 8;           // rows, to a power of two
-    extern __shared__ uint4 xs[];                             // [ROWS][words]
-    __shared__ float sums[2][P][COLS];
-    const int m = blockIdx.y, col0 = blockIdx.x * COLS, words = (a.d_in + 7) / 8;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const unsigned short* x = static_cast<const unsigned short*>(a.x.p[m]);
-    for (int j = threadIdx.x; j < ROWS * words; j += kFewThreads) {
-        const int r = j / words, at = j % words * 8;
-        xs[j] = r < a.rows ? load_halves(x + static_cast<size_t>(r) * a.d_in + at, min(8, a.d_in - at)) : make_uint4(0, 0, 0, 0);
-    }
-    bool staged = false;
-    for (int c = warp * 2; c < COLS && col0 + c < a.d_hidden; c += kFewThreads / 32 * 2) {
-        const unsigned short* rows[4];                        // gate and up rows of two columns (one twice at the edge)
+    constexpr int kWarps = kFewThreads / 32;
+    __shared__ float sums[kWarps][2][NT * 8][kFewCols + 1];
+    const int m = blockIdx.y, col0 = blockIdx.x * kFewCols;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, line = lane / 4, piece = lane % 4;
+    const unsigned short* w[4];                               // of this lane: gate and up rows of columns `line` and line + 8
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            rows[i] = static_cast<const unsigned short*>(i & 1 ? a.w_up.p[m] : a.w_gate.p[m]) + static_cast<size_t>(min(col0 + c + i / 2, a.d_hidden - 1)) * a.d_in;
-        const auto weights = [&](uint4 (&w)[4], int k) {
+    for (int i = 0; i < 4; ++i)                               // (at the edge the last column again)
+        w[i] = static_cast<const unsigned short*>(i & 1 ? a.w_up.p[m] : a.w_gate.p[m]) +
+               static_cast<size_t>(min(col0 + line + i / 2 * 8, a.d_hidden - 1)) * a.d_in;
+    const unsigned short* x = static_cast<const unsigned short*>(a.x.p[m]) + static_cast<size_t>(line) * a.d_in;
+    const unsigned skip[2] = {MODE == kFewShifted ? skip_of(w[0]) : 0u, MODE == kFewShifted ? skip_of(w[1]) : 0u};
+    const int words = (a.d_in + 7) / 8;
+    float acc[2][NT][4] = {};
+    const auto step = [&](int k0, auto first) {               // first: the step with word 0
+        const int k = k0 + piece, count = min(8, a.d_in - 8 * k);
+        const bool cut = MODE == kFewShifted && decltype(first)::value && k == 0;
+        uint4 v[4], in[2][NT];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (WHOLE) w[i] = __ldcs(reinterpret_cast<const uint4*>(rows[i]) + k);
-                else w[i] = load_halves(rows[i] + 8 * k, min(8, a.d_in - 8 * k));
+        for (int i = 0; i < 4; ++i) {
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (k < words) {
+                if constexpr (MODE == kFewAny) v[i] = load_halves(w[i] + 8 * k, count);
+                else if (cut) v[i] = cut_word(w[i], 0, a.d_in, skip[i & 1]);
+                else v[i] = __ldcs(reinterpret_cast<const uint4*>(w[i] - skip[i & 1]) + k);
             }
-        };
-        float v[2][2 * P] = {};
-        uint4 w[4];
-        if (lane < words) weights(w, lane);                   // on their way while x is staged
-        if (!staged) __syncthreads();
-        staged = true;
-#pragma unroll 1
-        for (int k = lane; k < words; k += 32) {
-            uint4 next[4];
-            if (k + 32 < words) weights(next, k + 32);
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const uint4 in = xs[r * words + k];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float& acc = v[i / 2][(i & 1) * P + r];
-                    multiply_add(acc, in.x, w[i].x, T{});
-                    multiply_add(acc, in.y, w[i].y, T{});
-                    multiply_add(acc, in.z, w[i].z, T{});
-                    multiply_add(acc, in.w, w[i].w, T{});
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = next[i];
         }
-        // The lanes' sums, halving the values a lane holds at every step; the lane's number says which is left.
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            int index = 0, d = 16;
-#pragma unroll
-            for (int half = P; half >= 1; half /= 2, d /= 2) {
-                const bool upper = lane & d;
-#pragma unroll
-                for (int i = 0; i < half; ++i) {
-                    const float mine = upper ? v[j][half + i] : v[j][i], other = upper ? v[j][i] : v[j][half + i];
-                    v[j][i] = mine + __shfl_xor_sync(0xffffffffu, other, d);
-                }
-                index = index * 2 + (upper ? 1 : 0);
+        for (int t = 0; t < NT; ++t) {
+            in[0][t] = in[1][t] = make_uint4(0, 0, 0, 0);
+            if (k < words && t * 8 + line < a.rows) {
+                const unsigned short* row = x + static_cast<size_t>(t) * 8 * a.d_in;
+                if constexpr (MODE == kFewAny) in[0][t] = load_halves(row + 8 * k, count);
+                else if constexpr (MODE == kFewWhole) in[0][t] = reinterpret_cast<const uint4*>(row)[k];
+                else if (cut) in[0][t] = cut_word(row, 0, a.d_in, skip[0]);
+                else in[0][t] = load_halves(row + 8 * k - static_cast<int>(skip[0]), 8);
+                in[1][t] = in[0][t];
+                if (MODE == kFewShifted && skip[1] != skip[0]) in[1][t] = cut_word(row, k, a.d_in, skip[1]);
             }
-#pragma unroll
-            for (int e = d; e >= 1; e /= 2) v[j][0] += __shfl_xor_sync(0xffffffffu, v[j][0], e);
-            if ((lane & (2 * d - 1)) == 0) (&sums[0][0][0])[index * COLS + c + j] = v[j][0];
         }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {                     // gate, up
+                mma_16x8x16(acc[i][t], v[i].x, v[i + 2].x, v[i].y, v[i + 2].y, in[i][t].x, in[i][t].y, T{});
+                mma_16x8x16(acc[i][t], v[i].z, v[i + 2].z, v[i].w, v[i + 2].w, in[i][t].z, in[i][t].w, T{});
+            }
+    };
+    int k0 = warp * 4;
+    if (MODE == kFewShifted && warp == 0) {
+        step(0, std::true_type{});
+        k0 = kWarps * 4;
     }
-    if (!staged) __syncthreads();                             // a warp without columns
+#pragma unroll 2
+    for (; k0 < words; k0 += kWarps * 4) step(k0, std::false_type{});
+    // the warps' parts of the sums, added in their order
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[warp][i][t * 8 + piece * 2 + e % 2][line + e / 2 * 8] = acc[i][t][e];
     __syncthreads();
-    for (int j = threadIdx.x; j < a.rows * COLS; j += kFewThreads) {
-        const int r = j / COLS, c = j % COLS;
+    for (int j = threadIdx.x; j < a.rows * kFewCols; j += kFewThreads) {
+        const int r = j / kFewCols, c = j % kFewCols;
         if (col0 + c >= a.d_hidden) continue;
-        const float g = sums[0][r][c], u = sums[1][r][c];
+        float g = 0.0f, u = 0.0f;
+#pragma unroll
+        for (int p = 0; p < kWarps; ++p) { g += sums[p][0][r][c]; u += sums[p][1][r][c]; }
         const size_t at = static_cast<size_t>(r) * a.d_hidden + col0 + c;
         if (a.gate.p[m]) {
             static_cast<T*>(a.gate.p[m])[at] = narrow<T>(g);

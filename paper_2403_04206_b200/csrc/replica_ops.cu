@@ -467,37 +467,20 @@ static grawa_status launch_gemm(grawa_dtype dtype, GemmArgs& a, cudaStream_t str
     return dtype == GRAWA_BF16 ? launch_gemm<__nv_bfloat16, FORWARD>(a, stream) : launch_gemm<__half, FORWARD>(a, stream);
 }
 
-// Up to 4 rows, or 8 where the weights would have to be laid out again, go by the kernel for a few rows, if their x fits
-// in shared memory.  (8 workers, 4096 -> 8192, bf16: 1 row 171 us, 8 rows 299 us against 251 on the tensor cores,
-// and 407 us against 251 and as much again for the layout when the weights are not aligned.)
-static bool takes_few(int64_t rows, int64_t d_in, bool w_ok)
-{
-    return rows <= (in_place(d_in, w_ok) ? kFewRows / 2 : kFewRows) && rows * ceil_div(d_in, 8) * 16 <= 96 * 1024;
-}
+// Up to kFewRows rows go by the kernel for a few rows.  (4 workers, 2048 -> 5632, bf16: 31 us for 1 row and 39 for 16,
+// against 55 and 50 by the tensor cores' tiles; 24 rows 67 against 49.)
+static bool takes_few(int64_t rows) { return rows <= kFewRows; }
 
-template <typename T, int ROWS, int COLS, bool WHOLE>
-static grawa_status launch_few(const FewArgs& a, int M, cudaStream_t stream)
+template <typename T, int NT>
+static grawa_status launch_few(const FewArgs& a, int M, FewMode mode, cudaStream_t stream)
 {
-    auto* const kernel = gated_few_kernel<T, ROWS, COLS, WHOLE>;
-    const size_t smem = static_cast<size_t>(ROWS) * ceil_div(a.d_in, 8) * 16;
-    GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.d_hidden, COLS)), M), kFewThreads, smem, stream, false, a);
-}
-template <typename T, int ROWS>
-static grawa_status launch_few(const FewArgs& a, int M, bool whole, cudaStream_t stream)
-{
-    const bool narrow_ctas = ceil_div(a.d_hidden, 32) * M < 4 * kSms;
-    if (narrow_ctas) return whole ? launch_few<T, ROWS, 16, true>(a, M, stream) : launch_few<T, ROWS, 16, false>(a, M, stream);
-    return whole ? launch_few<T, ROWS, 32, true>(a, M, stream) : launch_few<T, ROWS, 32, false>(a, M, stream);
+    auto* const kernel = mode == kFewWhole ? gated_few_kernel<T, NT, kFewWhole> : mode == kFewShifted ? gated_few_kernel<T, NT, kFewShifted> : gated_few_kernel<T, NT, kFewAny>;
+    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.d_hidden, kFewCols)), M), kFewThreads, 0, stream, false, a);
 }
 template <typename T>
-static grawa_status launch_few(const FewArgs& a, int M, bool whole, cudaStream_t stream)
+static grawa_status launch_few(const FewArgs& a, int M, FewMode mode, cudaStream_t stream)
 {
-    if (a.rows == 1) return launch_few<T, 1>(a, M, whole, stream);
-    if (a.rows == 2) return launch_few<T, 2>(a, M, whole, stream);
-    if (a.rows <= 4) return launch_few<T, 4>(a, M, whole, stream);
-    if (a.rows <= 6) return launch_few<T, 6>(a, M, whole, stream);
-    return launch_few<T, 8>(a, M, whole, stream);
+    return a.rows <= 8 ? launch_few<T, 1>(a, M, mode, stream) : launch_few<T, 2>(a, M, mode, stream);
 }
 
 // Outputs of the workers [first, first + count); whether they take 16-byte stores.
@@ -532,7 +515,7 @@ static FfnScratch ffn_scratch(void* base, int64_t rows, int64_t d_in, int64_t d_
 {
     Scratch s{static_cast<char*>(base)};
     FfnScratch f{};
-    if (rows == 0 || (!backward && takes_few(rows, d_in, w_ok))) return f;
+    if (rows == 0 || (!backward && takes_few(rows))) return f;
     f.x = operand_scratch(s, rows, d_in, M, x_ok);
     f.w_gate = operand_scratch(s, d_hidden, d_in, M, w_ok);
     f.w_up = operand_scratch(s, d_hidden, d_in, M, w_ok);
@@ -693,8 +676,7 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
     }
     if (b.clash()) return GRAWA_ERR_INVALID_ARG;
 
-    const bool w_ok = all_aligned(w_gate, M, 16) && all_aligned(w_up, M, 16);
-    if (takes_few(rows, d_in, w_ok)) {
+    if (takes_few(rows)) {
         FewArgs a{};
         copy_table(a.x, x, M);
         copy_table(a.w_gate, w_gate, M);
@@ -704,8 +686,9 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
         copy_table(a.up, up_out, M);
         a.rows = static_cast<int>(rows); a.d_in = static_cast<int>(d_in); a.d_hidden = static_cast<int>(d_hidden);
         a.activation = act;
-        const bool whole = in_place(d_in, w_ok);
-        return dtype == GRAWA_BF16 ? launch_few<__nv_bfloat16>(a, M, whole, stream) : launch_few<__half>(a, M, whole, stream);
+        const bool all = all_aligned(x, M, 16) && all_aligned(w_gate, M, 16) && all_aligned(w_up, M, 16);
+        const FewMode mode = d_in % 8 ? kFewAny : all ? kFewWhole : kFewShifted;
+        return dtype == GRAWA_BF16 ? launch_few<__nv_bfloat16>(a, M, mode, stream) : launch_few<__half>(a, M, mode, stream);
     }
     Operand xo, go, uo;
     grawa_status st = make_operand(&xo, x, rows, d_in, M, f.x, stream);

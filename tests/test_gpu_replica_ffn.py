@@ -117,8 +117,8 @@ def test_split_sums_on_integers(grawa, rows, d_in, hidden, lead, accumulate):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("rows", range(1, 10))
-@pytest.mark.parametrize("d_in,hidden,lead", [(768, 80, 0), (768, 80, 1), (97, 33, 0), (260, 40, 2), (2056, 3, 5), (8, 2000, 0), (12288, 17, 0)])
+@pytest.mark.parametrize("rows", [1, 2, 3, 5, 7, 8, 9, 15, 16, 17])
+@pytest.mark.parametrize("d_in,hidden,lead", [(768, 80, 0), (768, 80, 1), (97, 33, 0), (260, 40, 2), (2056, 3, 5), (8, 2000, 0), (8, 70, 3), (16, 65, 7), (12288, 17, 0), (4096, 48, 6)])
 def test_few_rows_on_integers(grawa, kind, rows, d_in, hidden, lead):
     c = Case(3, rows, d_in, hidden, kind, rows + d_in, True, lead)
     h, a, u = c.forward(grawa, "relu")
