@@ -317,7 +317,7 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void *const *dy, 
                                       int64_t x_stride, int64_t y_stride, int M, int accumulate, void *workspace,
                                       size_t workspace_bytes, grawa_stream_t stream);
 
-/* Bytes of scratch grawa_layernorm_backward needs (0 for few rows, and on invalid arguments). */
+/* Bytes of scratch grawa_layernorm_backward needs (0 for up to some 200 rows, and on invalid arguments). */
 size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M);
 
 /* Activation of the gate. */

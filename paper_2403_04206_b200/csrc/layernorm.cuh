@@ -12,6 +12,8 @@
 // up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
 // rows are read again from L2 instead.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "replica_common.cuh"
 
 namespace grawa {
@@ -33,6 +35,7 @@ struct NormBackwardArgs {
     long long rows, x_stride, y_stride;
     int cols, parts;
     int slots, lanes, word;                // slot j of a part holds the column that slot_column(j) names
+    int cluster;                           // the parts are the CTAs of one cluster, which adds them up itself
     float inv_cols;
     int has_gamma, has_dx, has_dgamma, has_dbeta, accumulate;
 };
@@ -392,7 +395,8 @@ constexpr int norm_ctas(int elems, int bytes) { return elems <= 8 ? 6 : elems <=
 
 // gridDim.x CTAs a worker go through its rows in turn; a thread keeps the sums of its own columns in
 // registers over all of them, so the weights' gradients cost one small table at the end and no atomics
-// (the split depends on the sizes alone: the same bits every time).
+// (the split depends on the sizes alone: the same bits every time).  A moderate number of rows goes to one cluster of CTAs
+// a worker, whose CTAs read each other's sums from shared memory: no table and no second launch.
 template <typename T, int NV, int LPR, int MODE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock, LPR == 32 ? norm_ctas(NV * kWordElems<T>, sizeof(T)) : 1)
 layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
@@ -501,12 +505,21 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
     }
     if constexpr (MODE == kWhole) copy_async_wait<0>();
     if (!a.has_dgamma && !a.has_dbeta) return;
+    float2* sums;                                             // the CTA's, by slots, where they pass through shared memory
     if constexpr (LPR == 0) {
+        if (!a.cluster) {
 #pragma unroll
-        for (int k = 0; k < EPT; ++k) store_slot_sums<T>(a, m, blockIdx.x, k * lanes + lane, dg[k], db[k]);
+            for (int k = 0; k < EPT; ++k) store_slot_sums<T>(a, m, blockIdx.x, k * lanes + lane, dg[k], db[k]);
+            return;
+        }
+        __syncthreads();                                      // the stages have been read
+        sums = reinterpret_cast<float2*>(ring);
+#pragma unroll
+        for (int k = 0; k < EPT; ++k) sums[k * lanes + lane] = make_float2(dg[k], db[k]);
     } else {
-        // groups of rows: first the groups of a warp, then the warps in order, through shared memory
+        // groups of rows: first the groups of a warp, then the warps in order
         __shared__ float2 acc[LPR * EPT];
+        sums = acc;
 #pragma unroll
         for (int k = 0; k < EPT; ++k)
 #pragma unroll
@@ -526,8 +539,25 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
             }
             __syncthreads();
         }
-        for (int j = threadIdx.x; j < LPR * EPT; j += kNormThreads) store_slot_sums<T>(a, m, blockIdx.x, j, acc[j].x, acc[j].y);
+        if (!a.cluster) {
+            for (int j = threadIdx.x; j < LPR * EPT; j += kNormThreads) store_slot_sums<T>(a, m, blockIdx.x, j, acc[j].x, acc[j].y);
+            return;
+        }
     }
+    // A cluster: every CTA adds up its share of the slots over all CTAs, in their order, and finishes them.
+    const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    cluster.sync();
+    for (int j = blockIdx.x * blockDim.x + threadIdx.x; j < a.slots; j += gridDim.x * blockDim.x) {
+        float2 s = make_float2(0.0f, 0.0f);
+        for (unsigned p = 0; p < gridDim.x; ++p) {
+            const float2 v = cluster.map_shared_rank(sums, p)[j];
+            s.x += v.x;
+            s.y += v.y;
+        }
+        const int col = slot_column(a, j);
+        if (col < a.cols) store_gradients<T>(a, m, col, s.x, s.y);
+    }
+    cluster.sync();                                           // no CTA leaves while its sums are read
 }
 
 // Rows that do not fit in a CTA's registers: dx by a CTA per row (dy and x are read again from L2) ...

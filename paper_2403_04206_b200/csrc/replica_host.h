@@ -53,24 +53,37 @@ private:
     int count_ = 0;
 };
 
-// One launch over grid (gx, gy, gz); `dependent`: its launch may overlap the end of the kernel in front of it
-// on the stream, whose results it waits for by itself.
+// One launch over grid (gx, gy, gz), in clusters of `cluster` CTAs along x.  `dependent`: its launch may overlap the end of
+// the kernel in front of it on the stream, whose results it waits for by itself.
 template <typename... KArgs, typename... Args>
-grawa_status launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool dependent, const Args&... args)
+grawa_status launch_clusters(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool dependent, unsigned cluster,
+                             const Args&... args)
 {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(static_cast<unsigned>(block));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    if (dependent) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = cluster;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = dependent ? 1 : 0;
     GRAWA_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     ++g_launches;
     return GRAWA_OK;
+}
+template <typename... KArgs, typename... Args>
+grawa_status launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool dependent, const Args&... args)
+{
+    return launch_clusters(kernel, grid, block, smem, stream, dependent, 1u, args...);
 }
 
 }  // namespace replica

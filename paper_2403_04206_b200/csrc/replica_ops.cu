@@ -159,30 +159,35 @@ static int64_t norm_slots(int64_t cols, int64_t elem)
 }
 
 // CTAs a worker's rows are split over in the backward pass (a rule on the sizes alone, so that the order of
-// the additions does not change from call to call).  Few rows go to one CTA, which then writes the
-// gradients itself: the second launch costs more than a few rows one after the other.
-static int norm_parts(int64_t rows, int64_t cols, int M, int64_t elem)
+// the additions does not change from call to call).  Few rows go to one CTA, and a moderate number to one
+// cluster, which then write the gradients themselves: the second launch costs more than a few rows one after
+// the other (called from Python, the second launch and its scratch take 6 us of the host's time).
+constexpr int kMostCluster = 8, kClusterSteps = 8;            // CTAs, and turns of each (some 0.8 us)
+struct NormSplit { int parts; bool cluster; };
+static NormSplit norm_split(int64_t rows, int64_t cols, int M, int64_t elem)
 {
     const NormLayout l = norm_layout(cols, elem);
     if (l.words == 0) {
         const int64_t want = 16 * kSms / (M * ceil_div(cols, 256));                 // CTAs of the column kernel
-        return static_cast<int>(std::max<int64_t>(1, std::min(want, ceil_div(rows, 32))));
+        return {static_cast<int>(std::max<int64_t>(1, std::min(want, ceil_div(rows, 32)))), false};
     }
     const int64_t steps = l.lanes > 32 ? rows : ceil_div(rows, kNormThreads / l.lanes);
-    if (steps <= 4) return 1;
+    if (steps <= 4) return {1, false};
+    if (steps <= kMostCluster * kClusterSteps) return {static_cast<int>(std::min<int64_t>(kMostCluster, ceil_div(steps, 2))), true};
     // as many CTAs as their registers and stages let an SM hold at once
     const int elems = l.words * (16 / static_cast<int>(elem));
     const int64_t per_sm = l.lanes > 32 ? std::max(1, 512 / l.lanes) : norm_ctas(elems, static_cast<int>(elem));
-    return static_cast<int>(std::max<int64_t>(1, std::min(steps, kSms * per_sm / M)));
+    return {static_cast<int>(std::max<int64_t>(1, std::min(steps, kSms * per_sm / M))), false};
 }
 
 template <typename T, int NV, int LPR, int MODE>
 static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
 {
     auto* const kernel = layernorm_backward_kernel<T, NV, LPR, MODE>;
-    const size_t smem = MODE == kWhole ? NormStage<NV>::bytes_a_thread * block : 0;
+    size_t smem = MODE == kWhole ? NormStage<NV>::bytes_a_thread * block : 0;
+    if (LPR == 0 && a.cluster) smem = std::max(smem, sizeof(float2) * a.slots);
     if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    return launch(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a);
+    return launch_clusters(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a.cluster ? a.parts : 1u, a);
 }
 
 template <typename T, int MODE>
@@ -214,7 +219,7 @@ static grawa_status norm_backward(const NormBackwardArgs& a, int M, RowMode mode
         if (mode == kWhole) st = launch_norm_backward<T, kWhole>(a, M, stream);
         else if (sizeof(T) == 4 || mode == kUnits) st = launch_norm_backward<T, kUnits>(a, M, stream);
         else st = launch_norm_backward<T, sizeof(T) == 4 ? kUnits : kHalves>(a, M, stream);
-        if (st != GRAWA_OK || a.parts == 1) return st;
+        if (st != GRAWA_OK || a.parts == 1 || a.cluster) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
     return launch(layernorm_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.slots, 32)), M), 32 * kFinishGroups, 0, stream, true, a);
@@ -588,8 +593,8 @@ size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int 
     if (!shape_ok(rows, cols, cols, cols, M, 4)) return 0;
     size_t most = 0;                                          // of the storage types
     for (const int64_t elem : {int64_t{2}, int64_t{4}}) {
-        const int parts = norm_parts(rows, cols, M, elem);
-        if (parts > 1) most = std::max(most, static_cast<size_t>(M) * parts * 2 * norm_slots(cols, elem) * sizeof(float));
+        const NormSplit s = norm_split(rows, cols, M, elem);
+        if (s.parts > 1 && !s.cluster) most = std::max(most, static_cast<size_t>(M) * s.parts * 2 * norm_slots(cols, elem) * sizeof(float));
     }
     return most;
 }
@@ -612,8 +617,8 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     if (dgamma && !b.add(dgamma, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     if (dbeta && !b.add(dbeta, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     const bool weights = dgamma || dbeta;
-    const int parts = norm_parts(rows, cols, M, elem);
-    const size_t need = weights && rows > 0 && parts > 1 ? grawa_layernorm_backward_workspace_bytes(rows, cols, M) : 0;
+    const NormSplit split = norm_split(rows, cols, M, elem);
+    const size_t need = weights && rows > 0 && split.parts > 1 && !split.cluster ? grawa_layernorm_backward_workspace_bytes(rows, cols, M) : 0;
     if (need) {
         if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return GRAWA_ERR_WORKSPACE;
         const void* ws = workspace;
@@ -632,7 +637,8 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     a.partial = static_cast<float*>(workspace);
     a.rows = rows; a.cols = static_cast<int>(cols); a.inv_cols = 1.0f / static_cast<float>(cols);
     a.x_stride = x_stride; a.y_stride = y_stride;
-    a.parts = rows == 0 ? 0 : parts;
+    a.parts = rows == 0 ? 0 : split.parts;
+    a.cluster = split.cluster;
     a.has_gamma = gamma != nullptr; a.has_dx = dx != nullptr; a.has_dgamma = dgamma != nullptr; a.has_dbeta = dbeta != nullptr;
     a.accumulate = accumulate != 0;
     const auto by = [&](int64_t bytes) {
