@@ -165,22 +165,24 @@ __device__ __forceinline__ void pair_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// 8 columns of this warp's 32 lanes: a thread gets one row's 8 neighbouring values, which may be used after
+// 16 columns of this warp's 32 lanes: a thread gets one row's 16 neighbouring values, which may be used after
 // accumulator_wait (the values pass through it, so that no use can move in front of it).
-__device__ __forceinline__ void accumulator_load(unsigned address, unsigned (&r)[8])
+__device__ __forceinline__ void accumulator_load(unsigned address, unsigned (&r)[16])
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(address));
 }
-__device__ __forceinline__ void accumulator_wait(unsigned (&r)[8], float (&v)[8])
+__device__ __forceinline__ void accumulator_wait(unsigned (&r)[16], float (&v)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
                  :
                  : "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void order_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void order_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -216,18 +218,18 @@ __device__ __forceinline__ float activation(int kind, float a)
     if (kind == kGelu) return a * normal_distribution(a).x;
     return a <= 0.0f ? 0.0f : a;
 }
-// v <- act(v) u, the kind decided once for 8 values.
-__device__ __forceinline__ void gated_product(int kind, float (&v)[8], const float (&u)[8])
+// v <- act(v) u, the kind decided once for 16 values.
+__device__ __forceinline__ void gated_product(int kind, float (&v)[16], const float (&u)[16])
 {
     if (kind == kSilu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = activation(kSilu, v[e]) * u[e];
+        for (int e = 0; e < 16; ++e) v[e] = activation(kSilu, v[e]) * u[e];
     } else if (kind == kGelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = activation(kGelu, v[e]) * u[e];
+        for (int e = 0; e < 16; ++e) v[e] = activation(kGelu, v[e]) * u[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = activation(kRelu, v[e]) * u[e];
+        for (int e = 0; e < 16; ++e) v[e] = activation(kRelu, v[e]) * u[e];
     }
 }
 // Value and slope.
@@ -287,7 +289,7 @@ __device__ __forceinline__ bool next_unit(const GemmArgs& a, int turn, Unit& u)
 // Results go to memory by way of a warp's own 4 KB of shared memory, 32 rows by 64 columns of 16 bits: a thread
 // has a row of the accumulator, but whole 128-byte rows are what global memory takes well.  The 16-byte pieces
 // of a row are permuted so that neither direction meets bank conflicts.  The loops over an accumulator's columns
-// stay rolled, 8 columns a turn: two warps an SM quarter cannot hide the instruction fetches of code that runs
+// stay rolled, 16 columns a turn: two warps an SM quarter cannot hide the instruction fetches of code that runs
 // once (unrolled over 64 columns, a forward tile's results took 22 thousand cycles, longer than its products).
 constexpr int kStoreCols = 64;
 constexpr int kStoreBytes = 32 * kStoreCols * 2;
@@ -460,14 +462,14 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
             if (p.splits > 1) {                               // a part of the sum, as it stands: a warp's 32 rows side by side
                 float* to = p.partial + static_cast<size_t>(u.slot) * kTileM * kTileN + rank * kHalf + quarter * 32 + lane;
 #pragma unroll 1
-                for (int c = half * kHalf; c < (half + 1) * kHalf && row < p.rows; c += 8) {
+                for (int c = half * kHalf; c < (half + 1) * kHalf && row < p.rows; c += 16) {
                     if ((FORWARD ? u.n * kHalf + c % kHalf : u.n * kTileN + c) >= p.cols) break;
-                    unsigned r[8];
-                    float v[8];
+                    unsigned r[16];
+                    float v[16];
                     accumulator_load(d + c, r);
                     accumulator_wait(r, v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) to[(c + e) * kTileM] = v[e];
+                    for (int e = 0; e < 16; ++e) to[(c + e) * kTileM] = v[e];
                 }
             } else if (FORWARD) {
                 const int c = half * kStoreCols, col = u.n * kHalf + c;
@@ -475,9 +477,9 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                 for (int out = 2; out >= 0; --out) {          // u, a, h
                     if (a.out[out][u.worker] == nullptr || row >= p.rows || col >= p.cols) continue;
 #pragma unroll 1
-                    for (int q = 0; q < kStoreCols / 8; ++q) {
-                        unsigned first[8], second[8];
-                        float v[8], up[8];
+                    for (int q = 0; q < kStoreCols / 8; q += 2) {
+                        unsigned first[16], second[16];
+                        float v[16], up[16];
                         accumulator_load(d + c + q * 8 + (out == 2 ? kHalf : 0), first);
                         if (out == 0) accumulator_load(d + c + q * 8 + kHalf, second);
                         accumulator_wait(first, v);
@@ -486,6 +488,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                             gated_product(a.activation, v, up);
                         }
                         *store_slot(stage, lane, q) = pack<T>(v);
+                        *store_slot(stage, lane, q + 1) = pack<T>(v + 8);
                     }
                     move_stage<T, true>(p, stage, a.out[out][u.worker], row, col);
                 }
@@ -498,18 +501,20 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
                     if (row >= p.rows || col >= p.cols) break;
                     if (add) move_stage<T, false>(p, stage, out, row, col);
 #pragma unroll 1
-                    for (int q = 0; q < kStoreCols / 8; ++q) {
-                        unsigned r[8];
-                        float v[8];
+                    for (int q = 0; q < kStoreCols / 8; q += 2) {
+                        unsigned r[16];
+                        float v[16];
                         accumulator_load(d + c + q * 8, r);
                         accumulator_wait(r, v);
                         if (add) {
-                            float held[8];
+                            float held[16];
                             unpack<T>(*store_slot(stage, lane, q), held);
+                            unpack<T>(*store_slot(stage, lane, q + 1), held + 8);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] += held[e];
+                            for (int e = 0; e < 16; ++e) v[e] += held[e];
                         }
                         *store_slot(stage, lane, q) = pack<T>(v);
+                        *store_slot(stage, lane, q + 1) = pack<T>(v + 8);
                     }
                     move_stage<T, true>(p, stage, out, row, col);
                 }
