@@ -317,8 +317,10 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void *const *dy, 
                                       int64_t x_stride, int64_t y_stride, int M, int accumulate, void *workspace,
                                       size_t workspace_bytes, grawa_stream_t stream);
 
-/* Bytes of scratch grawa_layernorm_backward needs (0 for up to some 200 rows, and on invalid arguments). */
-size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M);
+/* Bytes of scratch grawa_layernorm_backward needs, for every storage type (0 for few rows, and on invalid
+ * arguments).  `aligned` != 0: the rows of x, dy and dx are whole 16-byte words at 16-byte boundaries, for every
+ * worker; some 200 rows of up to 1024 elements then need none. */
+size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M, int aligned);
 
 /* Activation of the gate. */
 typedef enum grawa_activation { GRAWA_SILU = 0, GRAWA_GELU = 1 /* with erf */, GRAWA_RELU = 2 } grawa_activation;

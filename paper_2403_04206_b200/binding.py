@@ -112,7 +112,7 @@ def library() -> ctypes.CDLL:
     lib.grawa_layernorm_forward.restype = ci
     lib.grawa_layernorm_backward.argtypes = [ci] + [vp] * 8 + [i64] * 4 + [ci, ci, vp, ctypes.c_size_t, vp]
     lib.grawa_layernorm_backward.restype = ci
-    lib.grawa_layernorm_backward_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.grawa_layernorm_backward_workspace_bytes.argtypes = [i64, i64, ci, ci]
     lib.grawa_layernorm_backward_workspace_bytes.restype = ctypes.c_size_t
     sz = ctypes.c_size_t
     lib.grawa_gated_ffn_forward.argtypes = [ci, ci] + [vp] * 6 + [i64] * 3 + [ci, vp, sz, vp]
@@ -458,9 +458,9 @@ _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 
 def _tables(first, specs):
-    """Storage type code, then pointer table and row stride (of contiguous tensors: the low bits of their addresses) of each
-    spec (name, tensors or None, rows, cols, mode), from the native marshaller, which checks types, sizes, contiguity and that
-    all tensors are on the current device; last the device."""
+    """Storage type code, then pointer table and layout (16 * row stride + the low 4 bits of the addresses; stride 0 for contiguous
+    tensors) of each spec (name, tensors or None, rows, cols, mode), from the native marshaller, which checks types, sizes,
+    contiguity and that all tensors are on the current device; last the device."""
     global _marshal
     import torch
     if _marshal is None:
@@ -535,7 +535,7 @@ def grawa_layernorm_forward(x, gamma, beta, y, eps=1e-5, *, mean=None, rstd=None
     code, xt, xs, gt, _, bt, _, yt, ys, mt, _, rt, _, dev = _tables(x, (
         ("x", x, rows, cols, _ROWS), ("gamma", gamma, cols, 1, _OPTIONAL), ("beta", beta, cols, 1, _OPTIONAL), ("y", y, rows, cols, _ROWS),
         ("mean", mean, rows, 1, _OPTIONAL | _FLOAT32), ("rstd", rstd, rows, 1, _OPTIONAL | _FLOAT32)))
-    status = library().grawa_layernorm_forward(code, xt, gt, bt, yt, mt, rt, rows, cols, xs, ys, len(x), eps, _stream_on(stream, dev))
+    status = library().grawa_layernorm_forward(code, xt, gt, bt, yt, mt, rt, rows, cols, xs >> 4, ys >> 4, len(x), eps, _stream_on(stream, dev))
     _raise(status, "grawa_layernorm_forward")
 
 
@@ -548,17 +548,20 @@ def grawa_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, *, acc
         ("dy", dy, rows, cols, _ROWS), ("x", x, rows, cols, _ROWS), ("gamma", gamma, cols, 1, _OPTIONAL), ("mean", mean, rows, 1, _FLOAT32),
         ("rstd", rstd, rows, 1, _FLOAT32), ("dx", dx, rows, cols, _ROWS | _OPTIONAL), ("dgamma", dgamma, cols, 1, _OPTIONAL),
         ("dbeta", dbeta, cols, 1, _OPTIONAL)))
-    if dx is not None and dxs != xs:
+    if dx is not None and dxs >> 4 != xs >> 4:
         raise ValueError("dx: expected the row stride of x")
-    need = lib.grawa_layernorm_backward_workspace_bytes(rows, cols, M) if dgamma is not None or dbeta is not None else 0
-    keep = _scratch(workspace, need, stream)
-    status = lib.grawa_layernorm_backward(code, yt, xt, gt, mt, rt, dxt, dgt, dbt, rows, cols, xs, ys, M, 1 if accumulate else 0,
+    keep = workspace
+    if keep is None and (dgamma is not None or dbeta is not None):
+        size = 4 if code == 0 else 2                          # aligned: no address, stride or row end inside a 16-byte word
+        inside = (xs | ys | (dxs if dx is not None else 0)) & 15 | (cols | xs >> 4 | ys >> 4) * size & 15
+        keep = _scratch(None, lib.grawa_layernorm_backward_workspace_bytes(rows, cols, M, 0 if inside else 1), stream)
+    status = lib.grawa_layernorm_backward(code, yt, xt, gt, mt, rt, dxt, dgt, dbt, rows, cols, xs >> 4, ys >> 4, M, 1 if accumulate else 0,
                                           *_scratch_args(keep), _stream_on(stream, dev))
     _raise(status, "grawa_layernorm_backward")
 
 
-def grawa_layernorm_backward_workspace_bytes(rows: int, cols: int, M: int) -> int:
-    return int(library().grawa_layernorm_backward_workspace_bytes(rows, cols, M))
+def grawa_layernorm_backward_workspace_bytes(rows: int, cols: int, M: int, aligned: bool = False) -> int:
+    return int(library().grawa_layernorm_backward_workspace_bytes(rows, cols, M, 1 if aligned else 0))
 
 
 def _ffn_sizes(x, w_gate):
@@ -580,7 +583,7 @@ def grawa_gated_ffn_forward(x, w_gate, w_up, h, *, activation="silu", gate_out=N
         ("gate_out", gate_out, rows, d_hidden, _OPTIONAL), ("up_out", up_out, rows, d_hidden, _OPTIONAL)))
     keep = workspace
     if keep is None:
-        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, 0 if xa | ga | ua else 1), stream)
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, 0 if (xa | ga | ua) & 15 else 1), stream)
     status = lib.grawa_gated_ffn_forward(code, act, xt, gt, ut, ht, got, uot, rows, d_in, d_hidden, M, *_scratch_args(keep), _stream_on(stream, dev))
     _raise(status, "grawa_gated_ffn_forward")
 
@@ -598,7 +601,7 @@ def grawa_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, 
         ("dw_gate", dw_gate, d_hidden, d_in, _OPTIONAL), ("dw_up", dw_up, d_hidden, d_in, _OPTIONAL)))
     keep = workspace
     if keep is None:
-        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, 0 if t[4] | t[6] | t[8] else 1), stream)
+        keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, 0 if (t[4] | t[6] | t[8]) & 15 else 1), stream)
     status = lib.grawa_gated_ffn_backward(t[0], act, *t[1:-1:2], rows, d_in, d_hidden, M, 1 if accumulate else 0, *_scratch_args(keep),
                                           _stream_on(stream, t[-1]))
     _raise(status, "grawa_gated_ffn_backward")

@@ -22,9 +22,9 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 }
 
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
-// padded, all with one row stride; else contiguous tensors of rows * cols elements, and in place of the stride the bits
-// below 16 that any of the addresses has.
-bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kind, int device, uint64_t* address, int64_t* stride)
+// padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0.  Below the
+// stride, in the lowest 4 bits of *layout: the bits below 16 that any of the addresses has.
+bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kind, int device, uint64_t* address, int64_t* layout)
 {
     const char* name;
     PyObject* bufs;
@@ -32,7 +32,8 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
     int mode;
     if (!PyArg_ParseTuple(spec, "sOLLi", &name, &bufs, &rows, &cols, &mode)) return false;
     *address = 0;
-    *stride = (mode & kRows) ? cols : 0;
+    int64_t stride = (mode & kRows) ? cols : 0, low = 0;
+    *layout = stride << 4;
     if (bufs == Py_None) return (mode & kOptional) ? true : fail(PyExc_TypeError, name, "expected a list of tensors, got None");
     PyObject* list = PySequence_Fast(bufs, "expected a list of tensors");
     if (list == nullptr) return false;
@@ -56,23 +57,24 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
             }
             if (cols > 1 && t.stride(1) != 1) { ok = fail(PyExc_ValueError, name, "the elements of a row must be contiguous"); break; }
             if (rows > 1) {                                   // of a single row the stride says nothing
-                if (m > 0 && t.stride(0) != *stride) { ok = fail(PyExc_ValueError, name, "all workers need one row stride"); break; }
-                *stride = t.stride(0);
+                if (m > 0 && t.stride(0) != stride) { ok = fail(PyExc_ValueError, name, "all workers need one row stride"); break; }
+                stride = t.stride(0);
             }
         } else if (t.numel() != rows * cols || !t.is_contiguous()) {
             ok = fail(PyExc_ValueError, name, "expected contiguous tensors of " + std::to_string(rows * cols) + " elements");
             break;
         }
         t_tables[index][m] = reinterpret_cast<uint64_t>(t.data_ptr());
-        if (!(mode & kRows)) *stride |= static_cast<int64_t>(t_tables[index][m] & 15);
+        low |= static_cast<int64_t>(t_tables[index][m] & 15);
     }
     Py_DECREF(list);
     *address = reinterpret_cast<uint64_t>(t_tables[index]);
+    *layout = stride << 4 | low;
     return ok;
 }
 
 // tables(first, device, specs): the storage type code of `first` (a list of tensors, one a worker) and, for each
-// spec, the address of its pointer table (0 for None) and its row stride, or the low bits of its addresses.
+// spec, the address of its pointer table (0 for None) and its layout, 16 * row stride + the low bits of its addresses.
 PyObject* tables(PyObject*, PyObject* args)
 {
     PyObject *first, *specs;
@@ -100,13 +102,13 @@ PyObject* tables(PyObject*, PyObject* args)
         PyTuple_SET_ITEM(out, 0, PyLong_FromLong(code));
         for (Py_ssize_t i = 0; i < count; ++i) {
             uint64_t address = 0;
-            int64_t stride = 0;
-            if (!one_table(PyTuple_GET_ITEM(specs, i), static_cast<int>(i), workers, kind, device, &address, &stride)) {
+            int64_t layout = 0;
+            if (!one_table(PyTuple_GET_ITEM(specs, i), static_cast<int>(i), workers, kind, device, &address, &layout)) {
                 Py_DECREF(out);
                 return nullptr;
             }
             PyTuple_SET_ITEM(out, 1 + 2 * i, PyLong_FromUnsignedLongLong(address));
-            PyTuple_SET_ITEM(out, 2 + 2 * i, PyLong_FromLongLong(stride));
+            PyTuple_SET_ITEM(out, 2 + 2 * i, PyLong_FromLongLong(layout));
         }
         return out;
     } catch (const std::exception& e) {

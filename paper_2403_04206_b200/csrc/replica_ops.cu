@@ -162,9 +162,11 @@ static int64_t norm_slots(int64_t cols, int64_t elem)
 // the additions does not change from call to call).  Few rows go to one CTA, and a moderate number to one
 // cluster, which then write the gradients themselves: the second launch costs more than a few rows one after
 // the other (called from Python, the second launch and its scratch take 6 us of the host's time).
-constexpr int kMostCluster = 8, kClusterSteps = 8;            // CTAs, and turns of each (some 0.8 us)
+constexpr int kMostCluster = 8;                               // CTAs
+// Turns of each at most: some 0.8 us a turn with the rows staged ahead, and twice that without.
+static int cluster_turns(RowMode mode) { return mode == kWhole ? 6 : 2; }
 struct NormSplit { int parts; bool cluster; };
-static NormSplit norm_split(int64_t rows, int64_t cols, int M, int64_t elem)
+static NormSplit norm_split(int64_t rows, int64_t cols, int M, int64_t elem, RowMode mode)
 {
     const NormLayout l = norm_layout(cols, elem);
     if (l.words == 0) {
@@ -173,7 +175,7 @@ static NormSplit norm_split(int64_t rows, int64_t cols, int M, int64_t elem)
     }
     const int64_t steps = l.lanes > 32 ? rows : ceil_div(rows, kNormThreads / l.lanes);
     if (steps <= 4) return {1, false};
-    if (steps <= kMostCluster * kClusterSteps) return {static_cast<int>(std::min<int64_t>(kMostCluster, ceil_div(steps, 2))), true};
+    if (steps <= kMostCluster * cluster_turns(mode)) return {static_cast<int>(std::min<int64_t>(kMostCluster, ceil_div(steps, 2))), true};
     // as many CTAs as their registers and stages let an SM hold at once
     const int elems = l.words * (16 / static_cast<int>(elem));
     const int64_t per_sm = l.lanes > 32 ? std::max(1, 512 / l.lanes) : norm_ctas(elems, static_cast<int>(elem));
@@ -588,12 +590,12 @@ grawa_status grawa_layernorm_forward(grawa_dtype dtype, const void* const* x, co
     return norm_forward<float>(a, M, mode, stream);
 }
 
-size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M)
+size_t grawa_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols, int M, int aligned)
 {
     if (!shape_ok(rows, cols, cols, cols, M, 4)) return 0;
     size_t most = 0;                                          // of the storage types
     for (const int64_t elem : {int64_t{2}, int64_t{4}}) {
-        const NormSplit s = norm_split(rows, cols, M, elem);
+        const NormSplit s = norm_split(rows, cols, M, elem, aligned ? kWhole : kUnits);
         if (s.parts > 1 && !s.cluster) most = std::max(most, static_cast<size_t>(M) * s.parts * 2 * norm_slots(cols, elem) * sizeof(float));
     }
     return most;
@@ -617,8 +619,13 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     if (dgamma && !b.add(dgamma, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     if (dbeta && !b.add(dbeta, M, 1, cols, cols, elem, true)) return GRAWA_ERR_INVALID_ARG;
     const bool weights = dgamma || dbeta;
-    const NormSplit split = norm_split(rows, cols, M, elem);
-    const size_t need = weights && rows > 0 && split.parts > 1 && !split.cluster ? grawa_layernorm_backward_workspace_bytes(rows, cols, M) : 0;
+    const auto by = [&](int64_t bytes) {
+        return rows_by(x, M, rows, cols, x_stride, elem, bytes) && rows_by(dy, M, rows, cols, y_stride, elem, bytes) &&
+               (!dx || rows_by(dx, M, rows, cols, x_stride, elem, bytes));
+    };
+    const RowMode mode = by(16) ? kWhole : by(4) ? kUnits : kHalves;
+    const NormSplit split = norm_split(rows, cols, M, elem, mode);
+    const size_t need = weights && rows > 0 && split.parts > 1 && !split.cluster ? grawa_layernorm_backward_workspace_bytes(rows, cols, M, mode == kWhole) : 0;
     if (need) {
         if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return GRAWA_ERR_WORKSPACE;
         const void* ws = workspace;
@@ -641,11 +648,6 @@ grawa_status grawa_layernorm_backward(grawa_dtype dtype, const void* const* dy, 
     a.cluster = split.cluster;
     a.has_gamma = gamma != nullptr; a.has_dx = dx != nullptr; a.has_dgamma = dgamma != nullptr; a.has_dbeta = dbeta != nullptr;
     a.accumulate = accumulate != 0;
-    const auto by = [&](int64_t bytes) {
-        return rows_by(x, M, rows, cols, x_stride, elem, bytes) && rows_by(dy, M, rows, cols, y_stride, elem, bytes) &&
-               (!dx || rows_by(dx, M, rows, cols, x_stride, elem, bytes));
-    };
-    const RowMode mode = by(16) ? kWhole : by(4) ? kUnits : kHalves;
     const NormLayout l = norm_layout(cols, elem);
     a.slots = static_cast<int>(norm_slots(cols, elem));
     a.lanes = l.words ? l.lanes : a.slots;

@@ -56,8 +56,9 @@ def norm_backward(dtype=1, dy=X, x=R, gamma=D, mean=E, rstd=F, dx=Y, dgamma=G, d
 
 def test_layernorm_backward_refusals():
     assert norm_backward(rows=0, acc=1) == OK
-    need = grawa.grawa_layernorm_backward_workspace_bytes(1000, 100, 2)
-    assert need > 0 and grawa.grawa_layernorm_backward_workspace_bytes(4, 100, 2) == 0
+    size = grawa.grawa_layernorm_backward_workspace_bytes
+    need = size(1000, 100, 2)
+    assert need > 0 and size(4, 100, 2) == 0 and size(150, 768, 2) > 0 and size(150, 768, 2, aligned=True) == 0
     for bad in ((-1, 100, 2), (10, 0, 2), (10, 100, 0), (10, 100, 65)):
         assert grawa.grawa_layernorm_backward_workspace_bytes(*bad) == 0
     for kw in (dict(ws=None), dict(ws=0x90_0000_0008), dict(ws_bytes=need - 1), dict(ws_bytes=0)):
