@@ -90,14 +90,15 @@ __device__ __forceinline__ float inverse_root(float v)
 //            4 x 8192 x 4096 bf16: 95 us, 103 to 113 us without).
 //   kUnits   units of 4 bytes (fp32 rows anywhere; 16-bit rows of even length at even addresses): a lane's four
 //            units of a word are `lanes` units apart, so that a warp's accesses are contiguous.
+//   kFull    kWhole where the row fills every word of every lane: no lane asks whether its word exists.
 //   kHalves  16-bit rows anywhere: 16-byte words put together from aligned ones.  (Single 2-byte accesses took
 //            1.8 to 2 times as long: 8 x 4745 rows of 1001 bf16, forward 117 us, here 65 us.)
-enum RowMode { kWhole = 0, kUnits = 1, kHalves = 2 };
+enum RowMode { kWhole = 0, kUnits = 1, kHalves = 2, kFull = 3 };
 
 template <typename T, int MODE>
 struct Rows {
     static constexpr int VE = kWordElems<T>, EU = 4 / static_cast<int>(sizeof(T)), HALVES = sizeof(T) / 2;
-    static constexpr int WORD = MODE == kUnits ? EU : VE;     // neighbouring elements of a lane
+    static constexpr bool whole = MODE == kWhole || MODE == kFull;
 
     // The column of element e of a lane's word i.
     static __device__ __forceinline__ int column(int i, int e, int lane, int lanes)
@@ -105,12 +106,12 @@ struct Rows {
         if constexpr (MODE == kUnits) return ((i * 4 + e / EU) * lanes + lane) * EU + e % EU;
         else return (i * lanes + lane) * VE + e;
     }
-    static __device__ __forceinline__ bool any(int i, int lane, int lanes, int cols) { return column(i, 0, lane, lanes) < cols; }
+    static __device__ __forceinline__ bool any(int i, int lane, int lanes, int cols) { return MODE == kFull || column(i, 0, lane, lanes) < cols; }
 
     // Word i of a lane that has any() of it; behind the end of the row it holds zeros.
     static __device__ __forceinline__ uint4 load(const T* row, int i, int lane, int lanes, int cols)
     {
-        if constexpr (MODE == kWhole) {
+        if constexpr (whole) {
             return __ldcs(reinterpret_cast<const uint4*>(row) + i * lanes + lane);
         } else if constexpr (MODE == kUnits) {
             const unsigned* u = reinterpret_cast<const unsigned*>(row) + i * 4 * lanes + lane;
@@ -124,7 +125,7 @@ struct Rows {
     // Its counterpart; with kHalves all lanes of a warp call it, and `segment` neighbouring lanes hold neighbouring words.
     static __device__ __forceinline__ void store(T* row, int i, int lane, int lanes, int cols, const uint4& v, int segment)
     {
-        if constexpr (MODE == kWhole) {
+        if constexpr (whole) {
             if (any(i, lane, lanes, cols)) __stcs(reinterpret_cast<uint4*>(row) + i * lanes + lane, v);
         } else if constexpr (MODE == kUnits) {
             unsigned* u = reinterpret_cast<unsigned*>(row) + i * 4 * lanes + lane;
@@ -184,7 +185,7 @@ layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
         if (!R::any(i, lane, lanes, cols)) continue;
         float f[VE];
         shifted<T>(xw[i], -mean, f);
-        if (MODE != kWhole && R::column(i, VE - 1, lane, lanes) >= cols) {          // the row ends inside this word
+        if (!R::whole && R::column(i, VE - 1, lane, lanes) >= cols) {          // the row ends inside this word
 #pragma unroll
             for (int e = 0; e < VE; ++e)
                 if (R::column(i, e, lane, lanes) >= cols) f[e] = 0.0f;
@@ -201,7 +202,7 @@ layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
     const T* beta = static_cast<const T*>(a.beta.p[m]);
     T* y = static_cast<T*>(a.y.p[m]) + (live ? row : 0) * a.y_stride;
     // parameters inside a flat vector stand anywhere, or there are none
-    const bool by_words = MODE == kWhole && a.has_gamma && a.has_beta && skip_of(gamma) == 0 && skip_of(beta) == 0;
+    const bool by_words = R::whole && a.has_gamma && a.has_beta && skip_of(gamma) == 0 && skip_of(beta) == 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const bool here = R::any(i, lane, lanes, cols);
@@ -219,7 +220,7 @@ layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
                     const int col = R::column(i, e, lane, lanes);
-                    const bool in = MODE == kWhole || col < cols;
+                    const bool in = R::whole || col < cols;
                     g[e] = a.has_gamma && in ? widen(gamma[col]) : 1.0f;
                     b[e] = a.has_beta && in ? widen(beta[col]) : 0.0f;
                 }
@@ -437,17 +438,19 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
         }
         copy_async_commit();                                  // a group a row, also where there is none
     };
-    if constexpr (MODE == kWhole) {
+    if constexpr (R::whole) {
 #pragma unroll
         for (int d = 0; d < DEPTH - 1; ++d) fetch(d, row + d * stride);
     }
     int buf = 0, slot = 0;
     float mean = row < a.rows ? means[row] : 0.0f, rstd = row < a.rows ? rstds[row] : 0.0f;
-    for (; row - group < a.rows; row += stride) {             // the same turns for all groups of the CTA
-        const int cols = row < a.rows ? a.cols : 0;
-        const long long r = row < a.rows ? row : 0;
+    // (Rows of 8 lanes: the same turns for all groups of a warp, which exchange sums together.)
+    for (; (LPR == 8 ? row - group : row) < a.rows; row += stride) {
+        const bool live = LPR != 8 || row < a.rows;
+        const int cols = live ? a.cols : 0;
+        const long long r = live ? row : 0;
         uint4 xw[NV], dw[NV];
-        if constexpr (MODE == kWhole) {
+        if constexpr (R::whole) {
             fetch(slot == 0 ? DEPTH - 1 : slot - 1, row + (DEPTH - 1) * stride);
             copy_async_wait<DEPTH - 1>();
             const uint4* from = ring + static_cast<size_t>(slot) * 2 * NV * blockDim.x + threadIdx.x;
@@ -503,7 +506,7 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
         mean = next_mean;
         rstd = next_rstd;
     }
-    if constexpr (MODE == kWhole) copy_async_wait<0>();
+    if constexpr (R::whole) copy_async_wait<0>();
     if (!a.has_dgamma && !a.has_dbeta) return;
     float2* sums;                                             // the CTA's, by slots, where they pass through shared memory
     if constexpr (LPR == 0) {

@@ -113,7 +113,9 @@ template <typename T, int MODE>
 static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStream_t stream)
 {
     constexpr int VE = kWordElems<T>;
+    constexpr int kFilled = MODE == kWhole ? kFull : MODE;    // where a row fills every word of a warp's lanes
     const int64_t words = ceil_div(a.cols, VE), per_lane = ceil_div(words, 32);
+    const bool full = a.cols == per_lane * 32 * VE;
     const auto lanes = [&](auto kernel, int lpr) {
         return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, false, a);
     };
@@ -121,14 +123,14 @@ static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStr
     if (MODE == kWhole && per_lane <= 2 && a.has_gamma && a.has_beta && a.rows * M >= 32 * kSms * kAheadCtas &&
         all_aligned(a.gamma.p, M, 16) && all_aligned(a.beta.p, M, 16))
         return per_lane == 1 ? launch_norm_short<T, 1>(a, M, stream) : launch_norm_short<T, 2>(a, M, stream);
-    if (per_lane <= 1) return lanes(layernorm_forward_kernel<T, 1, 32, MODE>, 32);
-    if (per_lane <= 2) return lanes(layernorm_forward_kernel<T, 2, 32, MODE>, 32);
-    if (per_lane <= 3) return lanes(layernorm_forward_kernel<T, 3, 32, MODE>, 32);
-    if (per_lane <= 4) return lanes(layernorm_forward_kernel<T, 4, 32, MODE>, 32);
-    if (per_lane <= 6) return lanes(layernorm_forward_kernel<T, 6, 32, MODE>, 32);
-    if (per_lane <= 8) return lanes(layernorm_forward_kernel<T, 8, 32, MODE>, 32);
-    if (per_lane <= 12) return lanes(layernorm_forward_kernel<T, 12, 32, MODE>, 32);
-    if (per_lane <= 16) return lanes(layernorm_forward_kernel<T, 16, 32, MODE>, 32);
+    if (per_lane <= 1) return lanes(full && per_lane == 1 ? layernorm_forward_kernel<T, 1, 32, kFilled> : layernorm_forward_kernel<T, 1, 32, MODE>, 32);
+    if (per_lane <= 2) return lanes(full && per_lane == 2 ? layernorm_forward_kernel<T, 2, 32, kFilled> : layernorm_forward_kernel<T, 2, 32, MODE>, 32);
+    if (per_lane <= 3) return lanes(full && per_lane == 3 ? layernorm_forward_kernel<T, 3, 32, kFilled> : layernorm_forward_kernel<T, 3, 32, MODE>, 32);
+    if (per_lane <= 4) return lanes(full && per_lane == 4 ? layernorm_forward_kernel<T, 4, 32, kFilled> : layernorm_forward_kernel<T, 4, 32, MODE>, 32);
+    if (per_lane <= 6) return lanes(full && per_lane == 6 ? layernorm_forward_kernel<T, 6, 32, kFilled> : layernorm_forward_kernel<T, 6, 32, MODE>, 32);
+    if (per_lane <= 8) return lanes(full && per_lane == 8 ? layernorm_forward_kernel<T, 8, 32, kFilled> : layernorm_forward_kernel<T, 8, 32, MODE>, 32);
+    if (per_lane <= 12) return lanes(full && per_lane == 12 ? layernorm_forward_kernel<T, 12, 32, kFilled> : layernorm_forward_kernel<T, 12, 32, MODE>, 32);
+    if (per_lane <= 16) return lanes(full && per_lane == 16 ? layernorm_forward_kernel<T, 16, 32, kFilled> : layernorm_forward_kernel<T, 16, 32, MODE>, 32);
     constexpr int kBlockWords = 4;                            // a thread's, where a CTA holds the row
     if (words <= kNormMaxBlock * kBlockWords)
         return launch(layernorm_forward_kernel<T, kBlockWords, 0, MODE>, dim3(static_cast<unsigned>(a.rows), M),
@@ -186,7 +188,7 @@ template <typename T, int NV, int LPR, int MODE>
 static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
 {
     auto* const kernel = layernorm_backward_kernel<T, NV, LPR, MODE>;
-    size_t smem = MODE == kWhole ? NormStage<NV>::bytes_a_thread * block : 0;
+    size_t smem = MODE == kWhole || MODE == kFull ? NormStage<NV>::bytes_a_thread * block : 0;
     if (LPR == 0 && a.cluster) smem = std::max(smem, sizeof(float2) * a.slots);
     if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     return launch_clusters(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a.cluster ? a.parts : 1u, a);
@@ -197,7 +199,18 @@ static grawa_status launch_norm_backward(const NormBackwardArgs& a, int M, cudaS
 {
     const NormLayout l = norm_layout(a.cols, sizeof(T));      // its words are one of the kernels below
     constexpr int kStep = sizeof(T) == 4 ? 2 : 1;
+    // Where a row fills every word of every lane.  (16-bit rows lose by it: without the branches the compiler has more
+    // values live than there are registers for; 8 x 6304 x 768 bf16: 53 us, 47 with them.)
+    constexpr int kFilled = MODE == kWhole && sizeof(T) == 4 ? kFull : MODE;
+    const bool full = kFilled == kFull && a.cols == static_cast<int64_t>(l.words) * l.lanes * kWordElems<T>;
     if (l.lanes == 8) return launch_norm_rows<T, 1, 8, MODE>(a, M, kNormThreads, stream);
+    if (full && l.lanes == 32) {
+        if (l.words == kStep) return launch_norm_rows<T, kStep, 32, kFilled>(a, M, kNormThreads, stream);
+        if (l.words == 2 * kStep) return launch_norm_rows<T, 2 * kStep, 32, kFilled>(a, M, kNormThreads, stream);
+        if (l.words == 3 * kStep) return launch_norm_rows<T, 3 * kStep, 32, kFilled>(a, M, kNormThreads, stream);
+        return launch_norm_rows<T, 4 * kStep, 32, kFilled>(a, M, kNormThreads, stream);
+    }
+    if (full && l.lanes > 32) return launch_norm_rows<T, 2 * kStep, 0, kFilled>(a, M, l.lanes, stream);
     if (l.lanes == 32) {
         if (l.words == kStep) return launch_norm_rows<T, kStep, 32, MODE>(a, M, kNormThreads, stream);
         if (l.words == 2 * kStep) return launch_norm_rows<T, 2 * kStep, 32, MODE>(a, M, kNormThreads, stream);
