@@ -272,7 +272,8 @@ grawa_status grawa_step_host_typed(grawa_dtype dtype, grawa_variant variant, voi
  *     of a row and the next row are neither read nor written.
  *   - Work is enqueued on `stream`, nothing synchronises, no call allocates device memory or keeps
  *     anything for the next one, and results are bitwise reproducible.  Calls may be captured into a
- *     CUDA graph.  A workspace belongs to its call until the call's work is done: calls (or replays of
+ *     CUDA graph (a program's first call with an operator and type before the capture: the driver loads
+ *     a kernel's code on its first launch).  A workspace belongs to its call until the call's work is done: calls (or replays of
  *     captured calls) that may overlap on the GPU need different ones.
  */
 
@@ -356,7 +357,8 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned);
 
 /* Synchronises `stream` and reports whether a bounded device wait of a gated feed-forward call on the current
- * device ran out since the last report: GRAWA_OK, or GRAWA_ERR_TIMEOUT (that call's outputs are incomplete). */
+ * device ran out since the last report: GRAWA_OK, or GRAWA_ERR_TIMEOUT (that call's outputs are incomplete).
+ * Not for a stream that is being captured. */
 grawa_status grawa_gated_ffn_status(grawa_stream_t stream);
 
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not

@@ -497,17 +497,24 @@ def _scratch(workspace, need, stream):
         return torch.empty(need, dtype=torch.uint8, device="cuda")
 
 
-def _scratch_args(workspace):
+def _on_device(buf, device, name):
+    if buf.get_device() != device:
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device ({device}), got {buf.device}")
+
+
+def _scratch_args(workspace, device):
     if workspace is None:
         return None, 0
+    _on_device(workspace, device, "workspace")
     return _addr(workspace), workspace.numel() * workspace.element_size()
 
 
-def _counter(offset_counter):
+def _counter(offset_counter, device):
     if offset_counter is None or isinstance(offset_counter, int):
         return offset_counter
-    if offset_counter.element_size() != 8 or offset_counter.is_floating_point() or not offset_counter.is_cuda:
+    if offset_counter.element_size() != 8 or offset_counter.is_floating_point():
         raise TypeError("offset_counter: expected a 64-bit integer device tensor")
+    _on_device(offset_counter, device, "offset_counter")
     return _addr(offset_counter)
 
 
@@ -516,7 +523,7 @@ def grawa_dropout_forward(x, y, p, seed, offset=0, *, residual=None, offset_coun
     of (seed, offset + counter, worker, element) and never stored; see grawa_dropout_forward in grawa.h."""
     n = x[0].numel()
     code, xt, _, rt, _, yt, _, dev = _tables(x, (("x", x, n, 1, 0), ("residual", residual, n, 1, _OPTIONAL), ("y", y, n, 1, 0)))
-    status = library().grawa_dropout_forward(code, xt, rt, yt, n, len(x), p, seed, offset, _counter(offset_counter), _stream_on(stream, dev))
+    status = library().grawa_dropout_forward(code, xt, rt, yt, n, len(x), p, seed, offset, _counter(offset_counter, dev), _stream_on(stream, dev))
     _raise(status, "grawa_dropout_forward")
 
 
@@ -524,7 +531,7 @@ def grawa_dropout_backward(dy, dx, p, seed, offset=0, *, offset_counter=None, st
     """dx = dy where the forward call with these p, seed, offset and counter kept the element, scaled; else 0."""
     n = dy[0].numel()
     code, yt, _, xt, _, dev = _tables(dy, (("dy", dy, n, 1, 0), ("dx", dx, n, 1, 0)))
-    status = library().grawa_dropout_backward(code, yt, xt, n, len(dy), p, seed, offset, _counter(offset_counter), _stream_on(stream, dev))
+    status = library().grawa_dropout_backward(code, yt, xt, n, len(dy), p, seed, offset, _counter(offset_counter, dev), _stream_on(stream, dev))
     _raise(status, "grawa_dropout_backward")
 
 
@@ -556,7 +563,7 @@ def grawa_layernorm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, *, acc
         inside = (xs | ys | (dxs if dx is not None else 0)) & 15 | (cols | xs >> 4 | ys >> 4) * size & 15
         keep = _scratch(None, lib.grawa_layernorm_backward_workspace_bytes(rows, cols, M, 0 if inside else 1), stream)
     status = lib.grawa_layernorm_backward(code, yt, xt, gt, mt, rt, dxt, dgt, dbt, rows, cols, xs >> 4, ys >> 4, M, 1 if accumulate else 0,
-                                          *_scratch_args(keep), _stream_on(stream, dev))
+                                          *_scratch_args(keep, dev), _stream_on(stream, dev))
     _raise(status, "grawa_layernorm_backward")
 
 
@@ -584,7 +591,7 @@ def grawa_gated_ffn_forward(x, w_gate, w_up, h, *, activation="silu", gate_out=N
     keep = workspace
     if keep is None:
         keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 0, 0 if (xa | ga | ua) & 15 else 1), stream)
-    status = lib.grawa_gated_ffn_forward(code, act, xt, gt, ut, ht, got, uot, rows, d_in, d_hidden, M, *_scratch_args(keep), _stream_on(stream, dev))
+    status = lib.grawa_gated_ffn_forward(code, act, xt, gt, ut, ht, got, uot, rows, d_in, d_hidden, M, *_scratch_args(keep, dev), _stream_on(stream, dev))
     _raise(status, "grawa_gated_ffn_forward")
 
 
@@ -602,7 +609,7 @@ def grawa_gated_ffn_backward(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, 
     keep = workspace
     if keep is None:
         keep = _scratch(None, lib.grawa_gated_ffn_workspace_bytes(rows, d_in, d_hidden, M, 1, 0 if (t[4] | t[6] | t[8]) & 15 else 1), stream)
-    status = lib.grawa_gated_ffn_backward(t[0], act, *t[1:-1:2], rows, d_in, d_hidden, M, 1 if accumulate else 0, *_scratch_args(keep),
+    status = lib.grawa_gated_ffn_backward(t[0], act, *t[1:-1:2], rows, d_in, d_hidden, M, 1 if accumulate else 0, *_scratch_args(keep, t[-1]),
                                           _stream_on(stream, t[-1]))
     _raise(status, "grawa_gated_ffn_backward")
 

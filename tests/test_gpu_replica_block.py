@@ -125,3 +125,83 @@ def test_the_chain_captured_and_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(y, want[offset]))
     assert grawa.grawa_gated_ffn_status() == 0
+
+
+def test_two_host_threads_on_their_own_streams():
+    """The same calls from two threads at once give the bits that one thread gets."""
+    import threading
+
+    import paper_2403_04206_b200 as grawa
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rows, width, hidden, turns = 200, 264, 300, 30
+
+    def draw(*shape):
+        return [torch.randn(*shape, generator=gen, device="cuda").bfloat16() for _ in range(M)]
+
+    inputs = [dict(x=draw(rows, width), wg=draw(hidden, width), wu=draw(hidden, width), dh=draw(rows, hidden), gamma=draw(width), beta=draw(width)) for _ in range(2)]
+
+    def chain(d):
+        n, dx, dn = ([torch.empty_like(t) for t in d["x"]] for _ in range(3))
+        h, a, u, y = ([torch.empty_like(t) for t in d["dh"]] for _ in range(4))
+        mean, rstd = ([torch.empty(rows, device="cuda") for _ in range(M)] for _ in range(2))
+        dwg, dwu, dg, db = ([torch.empty_like(t) for t in d[k]] for k in ("wg", "wu", "gamma", "beta"))
+        grawa.grawa_layernorm_forward(d["x"], d["gamma"], d["beta"], n, EPS, mean=mean, rstd=rstd)
+        grawa.grawa_gated_ffn_forward(n, d["wg"], d["wu"], h, activation="gelu", gate_out=a, up_out=u)
+        grawa.grawa_dropout_forward(h, y, P, SEED, 1, residual=d["dh"])
+        grawa.grawa_gated_ffn_backward(d["dh"], n, d["wg"], d["wu"], a, u, dn, dwg, dwu, activation="gelu")
+        grawa.grawa_layernorm_backward(dn, d["x"], d["gamma"], mean, rstd, dx, dg, db)
+        return n + y + dx + dwg + dwu + dg + db
+
+    want = [chain(d) for d in inputs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()) as _:
+                for _ in range(turns):
+                    got = chain(inputs[k])
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(p, q) for p, q in zip(got, want[k])):
+                        wrong.append(k)
+        except Exception as e:                                # noqa: BLE001  (told to the test's own thread)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and grawa.grawa_gated_ffn_status() == 0
+
+
+def test_scratch_and_counters_of_the_caller():
+    import paper_2403_04206_b200 as grawa
+    rows, width, hidden = 300, 96, 128
+    x, dy = ([torch.randn(rows, width, device="cuda").bfloat16()] for _ in range(2))
+    stats = [[torch.zeros(rows, device="cuda")], [torch.ones(rows, device="cuda")]]
+    dx, dg, db = [torch.empty_like(x[0])], [torch.empty(width, device="cuda").bfloat16()], [torch.empty(width, device="cuda").bfloat16()]
+    need = grawa.grawa_layernorm_backward_workspace_bytes(rows, width, 1, aligned=True)
+    assert need > 0
+    own = torch.full((need,), 255, dtype=torch.uint8, device="cuda")             # NaN everywhere: its contents do not matter
+    grawa.grawa_layernorm_backward(dy, x, None, *stats, dx, dg, db, workspace=own)
+    first = [t.clone() for t in (dx[0], dg[0], db[0])]
+    grawa.grawa_layernorm_backward(dy, x, None, *stats, dx, dg, db)
+    assert all(torch.equal(a, b) for a, b in zip(first, (dx[0], dg[0], db[0])))
+    with pytest.raises(grawa.GrawaError, match="workspace"):
+        grawa.grawa_layernorm_backward(dy, x, None, *stats, dx, dg, db, workspace=own[:need - 16])
+    with pytest.raises(ValueError, match="workspace"):
+        grawa.grawa_layernorm_backward(dy, x, None, *stats, dx, dg, db, workspace=own.cpu())
+    w = [[torch.randn(hidden, width, device="cuda").bfloat16()] for _ in range(2)]
+    h = [[torch.randn(rows, hidden, device="cuda").bfloat16()] for _ in range(3)]
+    dw = [[torch.empty_like(w[0][0])] for _ in range(2)]
+    need = grawa.grawa_gated_ffn_workspace_bytes(rows, width, hidden, 1, backward=True)
+    own = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    grawa.grawa_gated_ffn_backward(h[0], x, *w, h[1], h[2], dx, *dw, workspace=own)
+    first = [t.clone() for t in (dx[0], dw[0][0], dw[1][0])]
+    grawa.grawa_gated_ffn_backward(h[0], x, *w, h[1], h[2], dx, *dw)
+    assert all(torch.equal(a, b) for a, b in zip(first, (dx[0], dw[0][0], dw[1][0])))
+    y = [torch.empty_like(x[0])]
+    for bad, error in ((torch.zeros(1, dtype=torch.int64), ValueError), (torch.zeros(1, device="cuda"), TypeError), (torch.zeros(1, dtype=torch.int32, device="cuda"), TypeError)):
+        with pytest.raises(error, match="offset_counter"):
+            grawa.grawa_dropout_forward(x, y, P, SEED, offset_counter=bad)
