@@ -75,6 +75,7 @@ template <typename T, int kDropCols, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(kDropThreads)
 dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
+    stream_order();
     constexpr int VE = 16 / static_cast<int>(sizeof(T));
     constexpr int kChunk = kDropThreads * kDropCols * VE;
     const int m = blockIdx.y;

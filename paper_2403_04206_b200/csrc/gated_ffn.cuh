@@ -386,7 +386,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     __syncthreads();
     pair_sync();                                              // both CTAs' barriers are ready before either is used
     order_after();
-    asm volatile("griddepcontrol.wait;" ::: "memory");        // what is in front on the stream has written the operands
+    stream_order();                                           // (what is above touches no operand)
     const unsigned tmem = tmem_slot;
 
     Unit u;
@@ -544,7 +544,7 @@ template <typename T, bool FORWARD>
 __global__ void __launch_bounds__(kJoinThreads)
 gemm_join_kernel(const __grid_constant__ GemmArgs a, int part)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    stream_order();
     constexpr int kSums = FORWARD ? 8 : 4;                    // of a thread: 4 columns, of a and of u
     __shared__ float sums[FORWARD ? 2 : 1][32][33];
     const GemmPart& p = a.part[part];
@@ -635,6 +635,7 @@ template <typename T, int NT, int MODE>
 __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 4 : MODE == kFewShifted ? 2 : 3)
 gated_few_kernel(const __grid_constant__ FewArgs a)
 {
+    stream_order();
     constexpr int kWarps = kFewThreads / 32;
     __shared__ float sums[kWarps][2][NT * 8][kFewCols + 1];
     const int m = blockIdx.y, col0 = blockIdx.x * kFewCols;
@@ -730,6 +731,7 @@ template <typename T, int STEP>
 __global__ void __launch_bounds__(kGatedThreads)
 gated_grad_kernel(const __grid_constant__ GatedGradArgs a)
 {
+    stream_order();
     const int m = blockIdx.y, lane = threadIdx.x & 31, per_row = STEP == 8 ? a.pitch / 8 : (a.pitch + 255) / 256 * 32;
     const long long at = static_cast<long long>(blockIdx.x) * kGatedThreads + threadIdx.x;
     const long long row = at / per_row;
@@ -796,6 +798,7 @@ struct PackArgs {
 static __global__ void __launch_bounds__(kGatedThreads)
 pack_rows_kernel(const __grid_constant__ PackArgs a)
 {
+    stream_order();
     const int m = blockIdx.y, per_row = a.pitch / 8;
     const long long at = static_cast<long long>(blockIdx.x) * kGatedThreads + threadIdx.x;
     if (at >= a.rows * per_row) return;

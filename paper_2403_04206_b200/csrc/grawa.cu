@@ -32,7 +32,7 @@ static int64_t g_pull_tile = 0;           // 0 = one pass of the register kernel
 static int64_t g_pull_variant = 0;
 static int64_t g_bulk_tile = 0;           // 0 = chosen from M so that at least three stages fit
 static int64_t g_kernel_timing = 0;
-static int64_t g_pdl = 1;
+static std::atomic<int64_t> g_pdl{1};
 static int64_t g_pull_preload = 1;
 static int64_t g_pull_wide = 1;             // fp32 register kernel: 32-byte accesses when every base is 32-byte aligned
 static int64_t g_pull16_staged = 1;         // 16-bit storage, 5..16 workers: shared-memory staged kernel (1) or register kernel (0)
@@ -41,6 +41,8 @@ static int64_t g_sumsq_prefetch_waves = 1;
 static int64_t g_sumsq_ctas_per_sm = 0;   // 0 = one CTA per work item
 static int64_t g_pull_ctas_per_sm = 0;    // 0 = one CTA per work item
 static thread_local std::string t_cuda_error;
+
+bool dependent_launch() { return g_pdl.load() != 0; }
 
 grawa_status cuda_fail(cudaError_t err, const char* what)
 {

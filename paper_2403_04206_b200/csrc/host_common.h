@@ -10,6 +10,7 @@
 namespace grawa {
 
 extern std::atomic<int64_t> g_launches;                              // kernels launched since the library was loaded
+bool dependent_launch();                                             // the "dependent_launch" option
 grawa_status cuda_fail(cudaError_t err, const char* what);           // keeps the text for grawa_last_cuda_error()
 
 #define GRAWA_CUDA_TRY(expr)                                        \

@@ -164,6 +164,7 @@ template <typename T, int NV, int LPR, int MODE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock)
 layernorm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
+    stream_order();
     using R = Rows<T, MODE>;
     constexpr int VE = R::VE, LANES = LPR ? LPR : 32;
     const int m = blockIdx.y;
@@ -247,6 +248,7 @@ template <typename T, int NV>
 __global__ void __launch_bounds__(kNormThreads)
 layernorm_forward_short_kernel(const __grid_constant__ NormForwardArgs a)
 {
+    stream_order();
     constexpr int VE = kWordElems<T>, kWarps = kNormThreads / 32;
     __shared__ uint4 ring[kAheadDepth][NV][kNormThreads];
     const int m = blockIdx.y, lane = threadIdx.x % 32, words = a.cols / VE;
@@ -317,6 +319,7 @@ template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormLongThreads)
 layernorm_forward_long_kernel(const __grid_constant__ NormForwardArgs a)
 {
+    stream_order();
     constexpr int VE = WHOLE ? kWordElems<T> : 1;
     const int m = blockIdx.y, words = a.cols / VE;
     const long long row = blockIdx.x;
@@ -406,6 +409,7 @@ template <typename T, int NV, int LPR, int MODE>
 __global__ void __launch_bounds__(LPR ? kNormThreads : kNormMaxBlock, LPR == 32 ? norm_ctas(NV * kWordElems<T>, sizeof(T)) : 1)
 layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
 {
+    stream_order();
     using R = Rows<T, MODE>;
     constexpr int VE = R::VE, EPT = NV * VE, LANES = LPR ? LPR : 32, GROUPS = LPR ? kNormThreads / LANES : 1;
     constexpr int DEPTH = NormStage<NV>::depth;
@@ -572,6 +576,7 @@ template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormLongThreads)
 layernorm_backward_long_kernel(const __grid_constant__ NormBackwardArgs a)
 {
+    stream_order();
     constexpr int VE = WHOLE ? kWordElems<T> : 1;
     const int m = blockIdx.y, words = a.cols / VE;
     const long long row = blockIdx.x;
@@ -614,6 +619,7 @@ template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kNormThreads)
 layernorm_columns_kernel(const __grid_constant__ NormBackwardArgs a)
 {
+    stream_order();
     constexpr int VE = WHOLE ? kWordElems<T> : 1, kWarps = kNormThreads / 32;
     __shared__ float2 acc[kWarps][32 * VE];
     const int m = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = blockIdx.x * 32 + lane, part = blockIdx.z;
@@ -654,7 +660,7 @@ template <typename T>
 __global__ void __launch_bounds__(32 * kFinishGroups)
 layernorm_finish_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    stream_order();
     __shared__ float2 acc[kFinishGroups][32];
     const int m = blockIdx.y, lane = threadIdx.x & 31, group = threadIdx.x >> 5, slot = blockIdx.x * 32 + lane;
     float2 s = make_float2(0.0f, 0.0f);

@@ -36,7 +36,7 @@ static grawa_status launch_dropout(const DropoutArgs& a, int M, bool vec, bool r
     if (ctas > 0x7fffffff) return GRAWA_ERR_INVALID_ARG;
     auto* const kernel = vec ? (residual ? dropout_kernel<T, COLS, true, true> : dropout_kernel<T, COLS, true, false>)
                              : (residual ? dropout_kernel<T, COLS, false, true> : dropout_kernel<T, COLS, false, false>);
-    return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0, stream, false, a);
+    return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kDropThreads, 0, stream, a);
 }
 
 template <typename T>
@@ -106,7 +106,7 @@ template <typename T, int NV>
 static grawa_status launch_norm_short(const NormForwardArgs& a, int M, cudaStream_t stream)
 {
     const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows, kNormThreads / 32), static_cast<int64_t>(kSms) * kAheadCtas / M));
-    return launch(layernorm_forward_short_kernel<T, NV>, dim3(static_cast<unsigned>(ctas), M), kNormThreads, 0, stream, false, a);
+    return launch_clusters(layernorm_forward_short_kernel<T, NV>, dim3(static_cast<unsigned>(ctas), M), kNormThreads, 0, stream, false, 1u, a);
 }
 
 template <typename T, int MODE>
@@ -117,7 +117,7 @@ static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStr
     const int64_t words = ceil_div(a.cols, VE), per_lane = ceil_div(words, 32);
     const bool full = a.cols == per_lane * 32 * VE;
     const auto lanes = [&](auto kernel, int lpr) {
-        return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, false, a);
+        return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kNormThreads / lpr)), M), kNormThreads, 0, stream, a);
     };
     if (words <= 8) return lanes(layernorm_forward_kernel<T, 1, 8, MODE>, 8);
     if (MODE == kWhole && per_lane <= 2 && a.has_gamma && a.has_beta && a.rows * M >= 32 * kSms * kAheadCtas &&
@@ -134,8 +134,8 @@ static grawa_status launch_norm_forward(const NormForwardArgs& a, int M, cudaStr
     constexpr int kBlockWords = 4;                            // a thread's, where a CTA holds the row
     if (words <= kNormMaxBlock * kBlockWords)
         return launch(layernorm_forward_kernel<T, kBlockWords, 0, MODE>, dim3(static_cast<unsigned>(a.rows), M),
-                      static_cast<int>(ceil_div(words, 32 * kBlockWords)) * 32, 0, stream, false, a);
-    return launch(layernorm_forward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+                      static_cast<int>(ceil_div(words, 32 * kBlockWords)) * 32, 0, stream, a);
+    return launch(layernorm_forward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, a);
 }
 
 // How the backward pass lays a row out: NV words in each of `lanes` lanes (8, 32, or a CTA's threads), rows too long for
@@ -219,11 +219,11 @@ static grawa_status launch_norm_backward(const NormBackwardArgs& a, int M, cudaS
     }
     if (l.lanes > 32) return launch_norm_rows<T, 2 * kStep, 0, MODE>(a, M, l.lanes, stream);
     if (a.has_dx) {
-        const grawa_status st = launch(layernorm_backward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, false, a);
+        const grawa_status st = launch(layernorm_backward_long_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(a.rows), M), kNormLongThreads, 0, stream, a);
         if (st != GRAWA_OK) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
-    return launch(layernorm_columns_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32 * (MODE == kWhole ? kWordElems<T> : 1))), M, a.parts), kNormThreads, 0, stream, false, a);
+    return launch(layernorm_columns_kernel<T, MODE == kWhole>, dim3(static_cast<unsigned>(ceil_div(a.cols, 32 * (MODE == kWhole ? kWordElems<T> : 1))), M, a.parts), kNormThreads, 0, stream, a);
 }
 
 template <typename T>
@@ -237,7 +237,7 @@ static grawa_status norm_backward(const NormBackwardArgs& a, int M, RowMode mode
         if (st != GRAWA_OK || a.parts == 1 || a.cluster) return st;
     }
     if (!a.has_dgamma && !a.has_dbeta) return GRAWA_OK;
-    return launch(layernorm_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.slots, 32)), M), 32 * kFinishGroups, 0, stream, true, a);
+    return launch(layernorm_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.slots, 32)), M), 32 * kFinishGroups, 0, stream, a);
 }
 
 template <typename T>
@@ -328,7 +328,7 @@ static grawa_status make_operands(Operand* const* ops, const void* const* const*
     }
     if (packed == 0) return GRAWA_OK;
     a.rows = rows; a.cols = static_cast<int>(cols); a.pitch = static_cast<int>(pitch_of(cols));
-    return launch(pack_rows_kernel, dim3(static_cast<unsigned>(ceil_div(rows * (a.pitch / 8), kGatedThreads)), M, packed), kGatedThreads, 0, stream, false, a);
+    return launch(pack_rows_kernel, dim3(static_cast<unsigned>(ceil_div(rows * (a.pitch / 8), kGatedThreads)), M, packed), kGatedThreads, 0, stream, a);
 }
 static grawa_status make_operand(Operand* op, const void* const* table, int64_t rows, int64_t cols, int M, void* scratch, cudaStream_t stream)
 {
@@ -474,11 +474,11 @@ static grawa_status launch_gemm(GemmArgs& a, cudaStream_t stream)
     const int pairs = static_cast<int>(std::min<int64_t>(units, kSms / 2));
     set_shares(a, pairs);
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(gemm_kernel<T, FORWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
-    grawa_status st = launch(gemm_kernel<T, FORWARD>, dim3(static_cast<unsigned>(2 * pairs)), kGemmThreads, kGemmSmem, stream, true, a);
+    grawa_status st = launch(gemm_kernel<T, FORWARD>, dim3(static_cast<unsigned>(2 * pairs)), kGemmThreads, kGemmSmem, stream, a);
     for (int part = 0; part < 2 && st == GRAWA_OK; ++part)
         if (a.part[part].splits > 1)
             st = launch(gemm_join_kernel<T, FORWARD>, dim3(static_cast<unsigned>(a.part[part].tiles), kTileM / 32, (FORWARD ? kHalf : kTileN) / 32), kJoinThreads,
-                        0, stream, true, a, part);
+                        0, stream, a, part);
     return st;
 }
 template <bool FORWARD>
@@ -495,7 +495,7 @@ template <typename T, int NT>
 static grawa_status launch_few(const FewArgs& a, int M, FewMode mode, cudaStream_t stream)
 {
     auto* const kernel = mode == kFewWhole ? gated_few_kernel<T, NT, kFewWhole> : mode == kFewShifted ? gated_few_kernel<T, NT, kFewShifted> : gated_few_kernel<T, NT, kFewAny>;
-    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.d_hidden, kFewCols)), M), kFewThreads, 0, stream, false, a);
+    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.d_hidden, kFewCols)), M), kFewThreads, 0, stream, a);
 }
 template <typename T>
 static grawa_status launch_few(const FewArgs& a, int M, FewMode mode, cudaStream_t stream)
@@ -780,7 +780,7 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
     const int step = by(16) ? 8 : by(4) ? 2 : 1;
     const int64_t threads = rows * (step == 8 ? pitch / 8 : ceil_div(pitch, 256) * 32);
     const auto elementwise = [&](auto kernel) {
-        return launch(kernel, dim3(static_cast<unsigned>(ceil_div(threads, kGatedThreads)), M), kGatedThreads, 0, stream, false, e);
+        return launch(kernel, dim3(static_cast<unsigned>(ceil_div(threads, kGatedThreads)), M), kGatedThreads, 0, stream, e);
     };
     const auto of_type = [&](auto type) {
         using T = decltype(type);
