@@ -293,3 +293,56 @@ def test_binding_refuses_wrong_tensors(grawa):
         grawa.grawa_gated_ffn_forward(c.x, c.wg, c.wu, [h[0], h[0]])
     with pytest.raises(ValueError):
         grawa.grawa_gated_ffn_forward([t.cpu() for t in c.x], c.wg, c.wu, h)
+
+
+def test_results_past_two_to_the_31_elements(grawa):
+    """Small integers: every sum stays below 2^24, so float32 holds it however it is added up."""
+    rows, d_in, hidden, kind = 131077, 8, 16400, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(12)
+
+    def draw(*shape, low=-2):
+        return torch.randint(low, 3, shape, generator=gen, device="cuda", dtype=torch.int8).to(kind)
+
+    x, wg, wu = draw(rows, d_in), draw(hidden, d_in), draw(hidden, d_in)
+    h, gate, up = (torch.full((rows, hidden), 9.0, device="cuda", dtype=kind) for _ in range(3))
+    grawa.grawa_gated_ffn_forward([x], [wg], [wu], [h], activation="relu", gate_out=[gate], up_out=[up])
+    chunks = [slice(i, min(i + 8192, rows)) for i in range(0, rows, 8192)]
+    for c in chunks:
+        a, u = x[c].float() @ wg.float().T, x[c].float() @ wu.float().T
+        for name, got, want in (("h", h, a.clamp(min=0) * u), ("gate", gate, a), ("up", up, u)):
+            same(got[c], want, kind, f"{name} of rows from {c.start}")
+    del h
+    dh, gate[:], up[:] = draw(rows, hidden), draw(rows, hidden, low=0), draw(rows, hidden)
+    dx, dwg, dwu = (torch.full_like(t, 9.0) for t in (x, wg, wu))
+    grawa.grawa_gated_ffn_backward([dh], [x], [wg], [wu], [gate], [up], [dx], [dwg], [dwu], activation="relu")
+    assert grawa.grawa_gated_ffn_status() == 0
+    sums = [torch.zeros(hidden, d_in, device="cuda") for _ in range(2)]
+    for c in chunks:
+        da, du = dh[c].float() * up[c].float() * (gate[c] > 0), dh[c].float() * gate[c].float()
+        same(dx[c], da @ wg.float() + du @ wu.float(), kind, f"dx of rows from {c.start}")
+        for s, d in zip(sums, (da, du)):
+            s += d.T @ x[c].float()
+    same(dwg, sums[0], kind, "dw_gate")
+    same(dwu, sums[1], kind, "dw_up")
+
+
+@pytest.mark.parametrize("rows,d_in,hidden,lead", [(70, 61, 133, 0), (70, 64, 133, 3), (300, 127, 250, 1)])
+def test_scratch_full_of_nan_and_shared_inputs(grawa, rows, d_in, hidden, lead):
+    """Operands laid out again in the scratch, whose rows are then longer than the operands': what lies behind them is
+    not read.  Both workers read the same tensors."""
+    c = Case(1, rows, d_in, hidden, torch.bfloat16, 13, True, lead)
+    two = Case(2, rows, d_in, hidden, torch.bfloat16, 13, True, lead)
+    for name in ("wg", "wu", "x", "dh", "a", "u"):
+        setattr(two, name, getattr(c, name) * 2)
+
+    def scratch(backward):
+        need = grawa.grawa_gated_ffn_workspace_bytes(rows, d_in, hidden, 2, backward=backward, aligned=False)
+        return torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+
+    h, a, u = two.forward(grawa, "relu", workspace=scratch(False))
+    dx, dwg, dwu = two.backward(grawa, "relu", workspace=scratch(True))
+    (wh, _), (wa, _), (wu, _) = gated_ffn64("relu", c.x[0], c.wg[0], c.wu[0])
+    (wdx, _), (wdg, _), (wdu, _) = gated_ffn_backward64("relu", c.dh[0], c.x[0], c.wg[0], c.wu[0], c.a[0], c.u[0], torch.bfloat16)
+    for m in range(2):
+        for name, got, want in (("h", h, wh), ("gate", a, wa), ("up", u, wu), ("dx", dx, wdx), ("dw_gate", dwg, wdg), ("dw_up", dwu, wdu)):
+            same(got[m], want, torch.bfloat16, f"{name} of worker {m}")

@@ -230,3 +230,33 @@ def test_gradients_against_differences(grawa, cols):
                 moved.view(-1)[j] += sign * step
                 v.append(value(*[moved if k == which else a for k, a in enumerate(args)]))
             assert abs((v[0] - v[1]) / (2 * step) - grad.reshape(-1)[j].item()) < tol
+
+
+@pytest.mark.parametrize("apart", [2 ** 31 + 8, 2 ** 31 + 5])                      # whole words, and rows at odd places
+def test_rows_further_apart_than_two_to_the_31_elements(grawa, apart):
+    rows, cols, kind = 3, 771 - 3 * (apart % 8 == 0), torch.bfloat16
+
+    def far(values=None):
+        t = torch.empty((rows - 1) * apart + cols, dtype=kind, device="cuda").as_strided((rows, cols), (apart, 1))
+        return t if values is None else t.copy_(values)
+
+    d = make(1, rows, cols, kind, 9)
+    x, dy, y = far(d["x"][0]), far(d["dy"][0]), far()
+    mean, rstd = ([torch.empty(rows, device="cuda")] for _ in range(2))
+    grawa.grawa_layernorm_forward([x], d["gamma"], d["beta"], [y], EPS, mean=mean, rstd=rstd)
+    want, _, _, compute, _ = layernorm64(x, d["gamma"][0], d["beta"][0], EPS)
+    check(y, want, kind, compute, "y")
+    out = [[torch.empty(cols, dtype=kind, device="cuda")] for _ in range(2)]
+    dx = y                                                                         # (its values are checked: the buffer serves again)
+    grawa.grawa_layernorm_backward([dy], [x], d["gamma"], mean, rstd, [dx], *out)
+    (wx, ex), *weights = layernorm_backward64(dy, x, d["gamma"][0], mean[0], rstd[0])
+    check(dx, wx, kind, ex, "dx")
+    for name, o, (w, e) in zip(("dgamma", "dbeta"), out, weights):
+        check(o[0], w, kind, e, name)
+
+
+def test_workers_that_share_their_inputs(grawa):
+    d = make(1, 40, 130, torch.float16, 10)
+    d = {k: v * 3 for k, v in d.items()}                                           # the same tensors for three workers
+    mean, rstd = check_forward(grawa, d, torch.float16)
+    check_backward(grawa, d, mean, rstd, torch.float16)
