@@ -352,7 +352,7 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
 
 /* Bytes of scratch of a forward (backward = 0) or backward call.  `aligned` != 0: x, w_gate and w_up of every
  * worker are 16-byte aligned; they are then read in place when d_in is a multiple of 8, and otherwise laid out
- * again in the scratch (but not by a forward call of up to 8 rows).  Sums that are split among the SMs keep their
+ * again in the scratch (but not by a forward call of up to 16 rows).  Sums that are split among the SMs keep their
  * parts there, and a backward call da and du.  0 on invalid arguments. */
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned);
 
@@ -440,8 +440,8 @@ int grawa_trace_read(uint64_t *rows_out, int max_rows);
  *                  while capturing a CUDA graph.  Default 0.
  *   "dependent_launch" 1 (default) = the kernels of a step are launched with programmatic
  *                  stream serialisation, so each one's launch overlaps the tail of the one
- *                  before it on the stream (it still waits for that kernel's results);
- *                  0 = plain stream order.
+ *                  before it on the stream (it still waits for that kernel's results); so are
+ *                  those of the replica operators; 0 = plain stream order.
  *   "pull_preload"  1 (default) = a device-buffer step's centre+pull kernel loads its first
  *                  parameters ahead of its wait for the weights; 0 = after it.
  *   "pull_prefetch_waves", "sumsq_prefetch_waves" (0..8; defaults 3 and 1) on short steps the CTAs
