@@ -188,9 +188,13 @@ template <typename T, int NV, int LPR, int MODE>
 static grawa_status launch_norm_rows(const NormBackwardArgs& a, int M, int block, cudaStream_t stream)
 {
     auto* const kernel = layernorm_backward_kernel<T, NV, LPR, MODE>;
-    size_t smem = MODE == kWhole || MODE == kFull ? NormStage<NV>::bytes_a_thread * block : 0;
-    if (LPR == 0 && a.cluster) smem = std::max(smem, sizeof(float2) * a.slots);
-    if (smem > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    constexpr size_t kThread = MODE == kWhole || MODE == kFull ? NormStage<NV>::bytes_a_thread : 0;
+    constexpr size_t kSums = LPR == 0 ? sizeof(float2) * NV * kWordElems<T> : 0;      // a thread's column sums, where a cluster reads them
+    const size_t smem = std::max(kThread, a.cluster ? kSums : 0) * block;
+    // The limit belongs to the kernel, not to the call: the largest that any call needs, so that no host thread lowers it
+    // between another one's setting and its launch.
+    constexpr size_t kLimit = std::max(kThread, kSums) * (LPR ? kNormThreads : kNormMaxBlock);
+    if (kLimit > 0) GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kLimit)));
     return launch_clusters(kernel, dim3(static_cast<unsigned>(a.parts), M), block, smem, stream, false, a.cluster ? a.parts : 1u, a);
 }
 
