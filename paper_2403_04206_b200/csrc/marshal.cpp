@@ -1,6 +1,8 @@
 // Pointer tables of the replica operators for the Python binding: checks the tensors of a call and writes
 // their addresses into host arrays, in one call from Python (attribute by attribute in Python, the checks of
-// a call with 24 tensors take longer than its launch).  Marshalling only; no tensor is created or changed.
+// a call with 24 tensors take longer than its launch).  Marshalling only; no tensor is created or changed.  The arrays
+// are bytes objects that belong to the call (ctypes passes their address): between this module's checks and the C
+// call Python may run anything, another call with other tables included.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <Python.h>
@@ -11,7 +13,6 @@
 namespace {
 
 constexpr int kMaxWorkers = 64, kMaxTables = 12;
-thread_local uint64_t t_tables[kMaxTables][kMaxWorkers];      // read by the C call that follows on this thread
 
 enum Mode { kRows = 1, kOptional = 2, kFloat32 = 4 };
 
@@ -23,21 +24,26 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
 // padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0.  Below the
-// stride, in the lowest 4 bits of *layout: the bits below 16 that any of the addresses has.
-bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kind, int device, uint64_t* address, int64_t* layout)
+// stride, in the lowest 4 bits of *layout: the bits below 16 that any of the addresses has.  *table: bytes, or the
+// integer 0 for None.
+bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int device, PyObject** table, int64_t* layout)
 {
     const char* name;
     PyObject* bufs;
     long long rows, cols;
     int mode;
     if (!PyArg_ParseTuple(spec, "sOLLi", &name, &bufs, &rows, &cols, &mode)) return false;
-    *address = 0;
     int64_t stride = (mode & kRows) ? cols : 0, low = 0;
     *layout = stride << 4;
-    if (bufs == Py_None) return (mode & kOptional) ? true : fail(PyExc_TypeError, name, "expected a list of tensors, got None");
+    if (bufs == Py_None) {
+        if (!(mode & kOptional)) return fail(PyExc_TypeError, name, "expected a list of tensors, got None");
+        *table = PyLong_FromLong(0);
+        return *table != nullptr;
+    }
     PyObject* list = PySequence_Fast(bufs, "expected a list of tensors");
     if (list == nullptr) return false;
     bool ok = true;
+    uint64_t address[kMaxWorkers];
     if (PySequence_Fast_GET_SIZE(list) != workers)
         ok = fail(PyExc_ValueError, name, "one entry per worker is needed (" + std::to_string(workers) + "), got " + std::to_string(PySequence_Fast_GET_SIZE(list)));
     if (mode & kFloat32) kind = at::kFloat;
@@ -64,17 +70,18 @@ bool one_table(PyObject* spec, int index, Py_ssize_t workers, at::ScalarType kin
             ok = fail(PyExc_ValueError, name, "expected contiguous tensors of " + std::to_string(rows * cols) + " elements");
             break;
         }
-        t_tables[index][m] = reinterpret_cast<uint64_t>(t.data_ptr());
-        low |= static_cast<int64_t>(t_tables[index][m] & 15);
+        address[m] = reinterpret_cast<uint64_t>(t.data_ptr());
+        low |= static_cast<int64_t>(address[m] & 15);
     }
     Py_DECREF(list);
-    *address = reinterpret_cast<uint64_t>(t_tables[index]);
+    if (!ok) return false;
     *layout = stride << 4 | low;
-    return ok;
+    *table = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(address), static_cast<Py_ssize_t>(workers * sizeof(uint64_t)));
+    return *table != nullptr;
 }
 
 // tables(first, device, specs): the storage type code of `first` (a list of tensors, one a worker) and, for each
-// spec, the address of its pointer table (0 for None) and its layout, 16 * row stride + the low bits of its addresses.
+// spec, its pointer table (bytes; 0 for None) and its layout, 16 * row stride + the low bits of its addresses.
 PyObject* tables(PyObject*, PyObject* args)
 {
     PyObject *first, *specs;
@@ -101,13 +108,13 @@ PyObject* tables(PyObject*, PyObject* args)
         if (out == nullptr) return nullptr;
         PyTuple_SET_ITEM(out, 0, PyLong_FromLong(code));
         for (Py_ssize_t i = 0; i < count; ++i) {
-            uint64_t address = 0;
+            PyObject* table = nullptr;
             int64_t layout = 0;
-            if (!one_table(PyTuple_GET_ITEM(specs, i), static_cast<int>(i), workers, kind, device, &address, &layout)) {
+            if (!one_table(PyTuple_GET_ITEM(specs, i), workers, kind, device, &table, &layout)) {
                 Py_DECREF(out);
                 return nullptr;
             }
-            PyTuple_SET_ITEM(out, 1 + 2 * i, PyLong_FromUnsignedLongLong(address));
+            PyTuple_SET_ITEM(out, 1 + 2 * i, table);
             PyTuple_SET_ITEM(out, 2 + 2 * i, PyLong_FromLongLong(layout));
         }
         return out;

@@ -1,4 +1,4 @@
-"""Host side of the replica operators: calls from several threads."""
+"""Host side of the replica operators: calls from several threads, and calls that come in the middle of another."""
 import threading
 
 import pytest
@@ -63,3 +63,26 @@ def test_row_lengths_of_one_kernel_from_several_threads(grawa):
     assert not wrong, wrong
     for k in range(threads):
         assert all(torch.equal(a[0], b) for a, b in zip(outs[k], want[k % 2]))
+
+
+def test_a_call_in_the_middle_of_another(grawa, monkeypatch):
+    """What Python runs between a call's checks and its launch (a finalizer, for one) may make calls of its own."""
+    from paper_2403_04206_b200 import binding
+    outer, inner = (norm_inputs(300, 100, torch.bfloat16, seed) for seed in (1, 2))
+    want, got, other, extra = (norm_outputs(d) for d in (outer, outer, inner, inner))
+    norm_backward(grawa, outer, want)
+    norm_backward(grawa, inner, other)
+    assert grawa.grawa_layernorm_backward_workspace_bytes(300, 100, 1, aligned=False) > 0
+    scratch, nested = binding._scratch, []
+
+    def interrupted(*args):
+        if not nested:
+            nested.append(True)
+            norm_backward(grawa, inner, extra)
+        return scratch(*args)
+
+    monkeypatch.setattr(binding, "_scratch", interrupted)
+    norm_backward(grawa, outer, got)
+    assert nested
+    for a, b in zip(want + other, got + extra):
+        assert torch.equal(a[0], b[0])
