@@ -3,16 +3,22 @@
 // a call with 24 tensors take longer than its launch).  Marshalling only; no tensor is created or changed.  The arrays
 // are bytes objects that belong to the call (ctypes passes their address): between this module's checks and the C
 // call Python may run anything, another call with other tables included.
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <Python.h>
 
 #include <cstdint>
+#include <memory>
 #include <string>
 
 namespace {
 
 constexpr int kMaxWorkers = 64, kMaxTables = 12;
+
+// A reference that is given back on every way out (questions to a tensor may throw).
+struct GiveBack { void operator()(PyObject* o) const { Py_DECREF(o); } };
+using Ref = std::unique_ptr<PyObject, GiveBack>;
 
 enum Mode { kRows = 1, kOptional = 2, kFloat32 = 4 };
 
@@ -40,7 +46,8 @@ bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int devi
         *table = PyLong_FromLong(0);
         return *table != nullptr;
     }
-    PyObject* list = PySequence_Fast(bufs, "expected a list of tensors");
+    const Ref held(PySequence_Fast(bufs, "expected a list of tensors"));
+    PyObject* const list = held.get();
     if (list == nullptr) return false;
     bool ok = true;
     uint64_t address[kMaxWorkers];
@@ -73,7 +80,6 @@ bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int devi
         address[m] = reinterpret_cast<uint64_t>(t.data_ptr());
         low |= static_cast<int64_t>(address[m] & 15);
     }
-    Py_DECREF(list);
     if (!ok) return false;
     *layout = stride << 4 | low;
     *table = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(address), static_cast<Py_ssize_t>(workers * sizeof(uint64_t)));
@@ -94,30 +100,30 @@ PyObject* tables(PyObject*, PyObject* args)
             PyErr_Format(PyExc_ValueError, "1 to %d workers are possible, got %zd", kMaxWorkers, workers);
             return nullptr;
         }
-        PyObject* item = PySequence_GetItem(first, 0);
+        const Ref item(PySequence_GetItem(first, 0));
         if (item == nullptr) return nullptr;
-        const bool tensor = THPVariable_Check(item);
-        const at::ScalarType kind = tensor ? THPVariable_Unpack(item).scalar_type() : at::kByte;
-        Py_DECREF(item);
+        const bool tensor = THPVariable_Check(item.get());
+        const at::ScalarType kind = tensor ? THPVariable_Unpack(item.get()).scalar_type() : at::kByte;
         const int code = kind == at::kFloat ? 0 : kind == at::kBFloat16 ? 1 : kind == at::kHalf ? 2 : -1;
         if (code < 0) {
             PyErr_SetString(PyExc_TypeError, "expected CUDA tensors of float32, bfloat16 or float16");
             return nullptr;
         }
-        PyObject* out = PyTuple_New(1 + 2 * count);
+        Ref result(PyTuple_New(1 + 2 * count));
+        PyObject* const out = result.get();
         if (out == nullptr) return nullptr;
         PyTuple_SET_ITEM(out, 0, PyLong_FromLong(code));
         for (Py_ssize_t i = 0; i < count; ++i) {
             PyObject* table = nullptr;
             int64_t layout = 0;
-            if (!one_table(PyTuple_GET_ITEM(specs, i), workers, kind, device, &table, &layout)) {
-                Py_DECREF(out);
-                return nullptr;
-            }
+            if (!one_table(PyTuple_GET_ITEM(specs, i), workers, kind, device, &table, &layout)) return nullptr;
             PyTuple_SET_ITEM(out, 1 + 2 * i, table);
             PyTuple_SET_ITEM(out, 2 + 2 * i, PyLong_FromLongLong(layout));
         }
-        return out;
+        return result.release();
+    } catch (python_error& e) {                               // raised by a tensor's own Python code
+        e.restore();
+        return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
