@@ -29,7 +29,9 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 }
 
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
-// padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0.  Below the
+// padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0: matrices
+// [rows, cols] (a transposed one has as many elements, in another order), or, where cols is 1 or the tensor is no matrix, any
+// that hold as many.  Below the
 // stride, in the lowest 4 bits of *layout: the bits below 16 that any of the addresses has.  *table: bytes, or the
 // integer 0 for None.
 bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int device, PyObject** table, int64_t* layout)
@@ -75,6 +77,10 @@ bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int devi
             }
         } else if (t.numel() != rows * cols || !t.is_contiguous()) {
             ok = fail(PyExc_ValueError, name, "expected contiguous tensors of " + std::to_string(rows * cols) + " elements");
+            break;
+        }
+        if (!(mode & kRows) && t.dim() == 2 && t.size(0) > 1 && t.size(1) > 1 && cols > 1 && (t.size(0) != rows || t.size(1) != cols)) {
+            ok = fail(PyExc_ValueError, name, "expected shape [" + std::to_string(rows) + ", " + std::to_string(cols) + "]");
             break;
         }
         address[m] = reinterpret_cast<uint64_t>(t.data_ptr());
