@@ -515,6 +515,8 @@ def _counter(offset_counter, device):
     if offset_counter.element_size() != 8 or offset_counter.is_floating_point():
         raise TypeError("offset_counter: expected a 64-bit integer device tensor")
     _on_device(offset_counter, device, "offset_counter")
+    if offset_counter.numel() < 1:
+        raise ValueError("offset_counter: expected one element")
     return _addr(offset_counter)
 
 

@@ -58,3 +58,12 @@ def test_a_matrix_of_another_shape_is_refused():
         assert len(tables(*shape)) == 3
     vector = [Shaped(2, 24)]                                  # where a vector is meant, any shape of as many elements will do
     assert len(_marshal.tables(vector, 0, (("x", vector, 48, 1, 0),))) == 3
+
+
+def test_a_counter_without_elements_is_refused():
+    """Its address is 0, which would stand for no counter at all."""
+    from paper_2403_04206_b200 import binding
+    with pytest.raises(ValueError, match="offset_counter"):
+        binding._counter(torch.empty(0, dtype=torch.int64), -1)
+    one = torch.zeros(1, dtype=torch.int64)                   # (get_device() of a CPU tensor is -1)
+    assert binding._counter(one, -1) == one.data_ptr() and binding._counter(None, -1) is None
