@@ -267,9 +267,10 @@ grawa_status grawa_step_host_typed(grawa_dtype dtype, grawa_variant variant, voi
  *     stored in `dtype`, aligned to the element size; 16-byte aligned rows take the vector kernels.
  *     Tables are read during the call only.
  *   - Arithmetic is fp32 on exactly widened elements; each stored value is rounded to nearest-even once.
- *   - No output may overlap another buffer of the call (rows of one row stride that lie between each
- *     other do not overlap); overlap visible from the pointers is rejected.  Elements between the end
- *     of a row and the next row are neither read nor written.
+ *   - No output may overlap another buffer of the call; overlap visible from the pointers is rejected.
+ *     A buffer of one row, or of rows of the same stride, that lies between the rows of another does not
+ *     overlap it; rows of two different strides between each other are rejected.  Elements between the
+ *     end of a row and the next row are neither read nor written.
  *   - Work is enqueued on `stream`, nothing synchronises, no call allocates device memory or keeps
  *     anything for the next one, and results are bitwise reproducible.  Calls may be captured into a
  *     CUDA graph (a program's first call with an operator and type before the capture: the driver loads

@@ -14,8 +14,9 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 // The buffers of a call.  add() takes one buffer a worker, `rows` rows of `cols` elements `stride` elements
-// apart; clash() says whether an output shares a byte with any other buffer of the call.  Rows that lie
-// between the rows of another buffer of the same stride are no overlap.
+// apart; clash() says whether an output shares a byte with any other buffer of the call.  A buffer of one row, or of rows
+// of the same stride, that lies between the rows of another is no overlap.  (Rows of two strides that lie
+// between each other are taken for one.)
 class Buffers {
 public:
     static constexpr int kMost = 10 * GRAWA_MAX_WORKERS;
@@ -38,9 +39,10 @@ public:
         for (int i = 0; i < count_; ++i)
             for (int j = i + 1; j < count_ && item_[j].lo < item_[i].hi; ++j) {
                 if (!item_[i].output && !item_[j].output) continue;
-                if (item_[i].stride && item_[i].stride == item_[j].stride) {
-                    const uintptr_t d = (item_[j].lo - item_[i].lo) % item_[i].stride;
-                    if (d >= item_[i].row && d + item_[j].row <= item_[i].stride) continue;
+                const uintptr_t stride = item_[i].stride;
+                if (stride && (item_[j].stride == stride || item_[j].stride == 0)) {
+                    const uintptr_t d = (item_[j].lo - item_[i].lo) % stride;
+                    if (d >= item_[i].row && d + item_[j].row <= stride) continue;
                 }
                 return true;
             }

@@ -1,4 +1,5 @@
-"""Host side of the replica operators: calls from several threads, and calls that come in the middle of another."""
+"""Host side of the replica operators: calls from several threads, calls that come in the middle of another, and buffers
+that stand between the rows of others."""
 import threading
 
 import pytest
@@ -86,3 +87,37 @@ def test_a_call_in_the_middle_of_another(grawa, monkeypatch):
     assert nested
     for a, b in zip(want + other, got + extra):
         assert torch.equal(a[0], b[0])
+
+
+def test_buffers_in_the_padding_of_others(grawa):
+    """Parameters, statistics and gradients that stand between the rows of an output share nothing with it."""
+    rows, cols, stride = 9, 40, 200
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.randn(rows, cols, generator=gen, device="cuda") for _ in range(2))
+    gamma, beta = (torch.randn(cols, generator=gen, device="cuda") for _ in range(2))
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    grawa.grawa_layernorm_forward([x], [gamma], [beta], [y], mean=[mean], rstd=[rstd])
+    grawa.grawa_layernorm_backward([dy], [x], [gamma], [mean], [rstd], [dx], [dgamma], [dbeta])
+
+    flat = torch.full((rows, stride), 7.0, device="cuda")      # row 0: y and gamma; row 3: y, beta and mean; last row: y, beta ...
+    rows_of = flat[:, :cols]
+    g, b, mu, s = flat[0, cols:2 * cols], flat[3, 100:100 + cols], flat[3, 150:150 + rows], flat[7, stride - rows:]
+    g.copy_(gamma)
+    b.copy_(beta)
+    grawa.grawa_layernorm_forward([x], [g], [b], [rows_of], mean=[mu], rstd=[s])
+    for got, want in ((rows_of, y), (mu, mean), (s, rstd), (g, gamma), (b, beta)):
+        assert torch.equal(got, want)
+    flat.fill_(7.0)
+    x_rows = flat[:, :cols]
+    x_rows.copy_(x)
+    dg, db, out = flat[2, cols:2 * cols], flat[2, 2 * cols:3 * cols], flat[:, 148:148 + cols]
+    grawa.grawa_layernorm_backward([dy], [x_rows], [gamma], [mean], [rstd], [out], [dg], [db])
+    for got, want in ((out, dx), (dg, dgamma), (db, dbeta), (x_rows, x)):
+        assert torch.equal(got, want)
+    untouched = torch.ones_like(flat, dtype=torch.bool)
+    untouched[:, :cols] = untouched[:, 148:148 + cols] = untouched[2, cols:3 * cols] = False
+    assert (flat[untouched] == 7.0).all()
+    for bad in (flat[2, cols - 1:2 * cols - 1], flat.view(-1)[3 * stride - cols + 1:3 * stride + 1]):
+        with pytest.raises(grawa.GrawaError):                 # one element of it in a row, in front or behind
+            grawa.grawa_layernorm_forward([x], [bad], [beta], [rows_of])
