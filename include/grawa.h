@@ -43,8 +43,9 @@
  *     gradients) gives that worker weight 0, the rest are normalised among themselves (uniform
  *     1/M if none is finite), and the step's status word is set; see grawa_last_step_status.
  *   - Errors detectable on the host return a negative code before anything is enqueued.
- *     Nothing on the device traps.  The only device-side waits are the bulk-copy kernel's waits
- *     for its own copies; each is bounded and reports GRAWA_ERR_TIMEOUT instead of hanging.
+ *     Nothing on the device traps.  The only device-side waits are the bulk-copy kernel's and the gated
+ *     feed-forward product's waits for their own copies and products; each is bounded and reports
+ *     GRAWA_ERR_TIMEOUT instead of hanging.
  *   - A plan (and its device memory) lives until grawa_clear_plans(); a program that meets many
  *     different shapes or streams should call it now and then.  Steps that share a plan (same
  *     device, stream, shape) must not overlap on the GPU; the stream order guarantees that.
@@ -70,7 +71,7 @@ typedef enum grawa_status {
     GRAWA_ERR_CUDA = -2,        /* a CUDA runtime call failed; text in grawa_last_cuda_error()    */
     GRAWA_ERR_NONFINITE = -3,   /* a gradient score was NaN/Inf (fallback weights were applied)   */
     GRAWA_ERR_WORKSPACE = -4,   /* caller-supplied workspace missing, misaligned or too small     */
-    GRAWA_ERR_TIMEOUT = -5,     /* a bounded device-side wait ran out (bulk-copy variant only)    */
+    GRAWA_ERR_TIMEOUT = -5,     /* a bounded device-side wait ran out (bulk-copy variant, product) */
     GRAWA_ERR_TOO_LARGE = -6    /* problem larger than the built-in scratch of grawa_sumsq_static */
 } grawa_status;
 
@@ -361,6 +362,11 @@ size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hid
  * device ran out since the last report: GRAWA_OK, or GRAWA_ERR_TIMEOUT (that call's outputs are incomplete).
  * Not for a stream that is being captured. */
 grawa_status grawa_gated_ffn_status(grawa_stream_t stream);
+
+/* Self-test of those waits: launches one pair of CTAs of the product kernel whose operands are never fetched.  Its
+ * waits give up after 2 ms of wall time, it returns with the context still usable, and grawa_gated_ffn_status then
+ * reports GRAWA_ERR_TIMEOUT.  Touches no caller memory. */
+grawa_status grawa_selftest_gated_ffn_wait(grawa_stream_t stream);
 
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not
  * exceed it (for example M = 16 workers of up to 134 million elements each). */

@@ -123,6 +123,8 @@ def library() -> ctypes.CDLL:
     lib.grawa_gated_ffn_workspace_bytes.restype = sz
     lib.grawa_gated_ffn_status.argtypes = [vp]
     lib.grawa_gated_ffn_status.restype = ci
+    lib.grawa_selftest_gated_ffn_wait.argtypes = [vp]
+    lib.grawa_selftest_gated_ffn_wait.restype = ci
     _lib = lib
     return lib
 
@@ -623,6 +625,11 @@ def grawa_gated_ffn_workspace_bytes(rows: int, d_in: int, d_hidden: int, M: int,
 def grawa_gated_ffn_status(stream=None) -> int:
     """Synchronises the stream and returns 0, or -5 when a bounded wait of a gated feed-forward call ran out."""
     return int(library().grawa_gated_ffn_status(_stream(stream)))
+
+
+def grawa_selftest_gated_ffn_wait(*, stream=None) -> None:
+    """Launches the product kernel's bounded-wait self-test; grawa_gated_ffn_status then reports -5."""
+    _raise(library().grawa_selftest_gated_ffn_wait(_stream(stream)), "grawa_selftest_gated_ffn_wait")
 
 
 def grawa_workspace_bytes(n: int, M: int, layer_offsets=None) -> int:

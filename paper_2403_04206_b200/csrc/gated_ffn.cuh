@@ -28,8 +28,11 @@
 // of which 130 are the elementwise kernel at 7.1 TB/s and the products run at 1440 TFLOP/s until the power limit
 // lowers the clock (cuBLAS 1170 to 1230 us for the products alone).
 //
-// Every wait is bounded: a CTA whose wait runs out records it in g_ffn_status, waits (bounded) for its own
-// copies and products in flight, frees its tensor memory and returns.
+// Every wait for a barrier in shared memory is bounded: a CTA whose wait runs out records it in g_ffn_status, waits
+// (bounded) for its own copies and products in flight, frees its tensor memory and returns.  A warp decides as one: its
+// lanes leave together or go on together, as the instructions that take a whole warp need.  (Not bounded by the kernel: the
+// two waits of the pair for each other, which both CTAs reach for that reason, and the allocation of tensor
+// memory, which waits for whoever holds it on the SM to end.)
 #pragma once
 #include <cuda.h>
 
@@ -76,7 +79,7 @@ struct GemmArgs {
 };
 
 __device__ int g_ffn_status = 0;            // 1: a wait ran out since the word was read
-constexpr unsigned long long kGemmWaitLimitNs = 2000000000ull;
+constexpr unsigned long long kGemmWaitLimitNs = 2000000000ull, kStarvedLimitNs = 2000000ull;
 
 // ------------------------------------------------------------------ barriers, copies, tensor memory
 
@@ -119,7 +122,9 @@ __device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity)
         : "memory");
     return ok != 0;
 }
-// False when the limit passed, or another wait of the CTA gave up (`gave_up`, which may be NULL).
+// False when the limit passed, or another wait of the CTA gave up (`gave_up`, which may be NULL).  Lanes of a warp may get
+// different answers.
+template <unsigned long long LIMIT>
 __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, volatile int* gave_up)
 {
     if (barrier_try(bar, parity)) return true;
@@ -127,7 +132,7 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
     for (;;) {
         if (barrier_try(bar, parity)) return true;
         if (gave_up && *gave_up) return false;
-        if (nanoseconds() - t0 > kGemmWaitLimitNs) {
+        if (nanoseconds() - t0 > LIMIT) {
             if (gave_up) *gave_up = 1;
             atomicOr(&g_ffn_status, 1);
             return false;
@@ -164,6 +169,11 @@ __device__ __forceinline__ void mma_commit(unsigned bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                  "h"(static_cast<unsigned short>(3))
                  : "memory");
+}
+// The same in this CTA alone, for a thread that gives up: its pair's other CTA waits for nothing more.
+__device__ __forceinline__ void mma_commit_here(unsigned bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void pair_sync()
 {
@@ -357,10 +367,12 @@ __device__ __forceinline__ void move_stage(const GemmPart& a, unsigned char* sta
     __syncwarp();
 }
 
-template <typename T, bool FORWARD>
+// STARVED: for the self-test of the bounded waits only; nothing is copied, so that the first wait for operands runs out.
+template <typename T, bool FORWARD, bool STARVED = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs a)
 {
+    constexpr unsigned long long kLimit = STARVED ? kStarvedLimitNs : kGemmWaitLimitNs;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kStages + 5];
     __shared__ unsigned tmem_slot;
@@ -390,7 +402,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
     const unsigned tmem = tmem_slot;
 
     Unit u;
-    if (warp == 0 && lane == 0) {
+    if (!STARVED && warp == 0 && lane == 0) {
         const unsigned leader_full = in_leader(full);
         int fills = 0;
         bool ok = true;
@@ -400,7 +412,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
             const int half_blocks = a.part[u.part].half_blocks;
             for (int kb = u.begin; kb < u.end; ++kb, ++fills) {
                 const int s = fills % kStages;
-                if (fills >= kStages && !barrier_wait(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) { ok = false; break; }
+                if (fills >= kStages && !barrier_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) { ok = false; break; }
                 const unsigned bar = leader_full + 8 * s, sa = ring + s * kStageBytes, sb = sa + kABytes;
                 if (rank == 0) barrier_expect(full + 8 * s, 2 * kStageBytes);           // the bytes of both CTAs
                 if (FORWARD) {
@@ -421,10 +433,10 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         }
         // The last arrivals at this CTA's barriers come before it leaves.
         if (ok)
-            for (int f = max(0, fills - kStages); f < fills && ok; ++f) ok = barrier_wait(empty + 8 * (f % kStages), (f / kStages) & 1, &gave_up);
+            for (int f = max(0, fills - kStages); f < fills && ok; ++f) ok = barrier_wait<kLimit>(empty + 8 * (f % kStages), (f / kStages) & 1, &gave_up);
         // After a wait ran out, copies in flight still write shared memory: the first CTA sees those of both.
         if (!ok && rank == 0)
-            for (int f = max(0, fills - kStages); f < fills; ++f) barrier_wait(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
+            for (int f = max(0, fills - kStages); f < fills; ++f) barrier_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
     } else if (warp == 1 && lane == 0 && rank == 0) {
         constexpr unsigned kShape = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTileN >> 3) << 17 | (kTileM >> 4) << 24;
         constexpr unsigned kAMn = 1u << 15, kBMn = 1u << 16, kAlongK = 32 >> 4, kAlongMn = 2048 >> 4;   // 16 k further in a K- or an MN-major tile
@@ -434,11 +446,11 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
             const bool a_mn = !FORWARD && u.part == kWeightGrad, b_mn = !FORWARD;
             const unsigned shape = kShape | (a_mn ? kAMn : 0u) | (b_mn ? kBMn : 0u), a_step = a_mn ? kAlongMn : kAlongK, b_step = b_mn ? kAlongMn : kAlongK;
             const unsigned d = tmem + (turn & 1) * kTileN;
-            if (turn >= 2 && !barrier_wait(ready + 8 * (turn & 1), (turn / 2 - 1) & 1, &gave_up)) { ok = false; break; }
+            if (turn >= 2 && !barrier_wait<kLimit>(ready + 8 * (turn & 1), (turn / 2 - 1) & 1, &gave_up)) { ok = false; break; }
             order_after();
             for (int kb = u.begin; kb < u.end; ++kb, ++used) {
                 const int s = used % kStages;
-                if (!barrier_wait(full + 8 * s, (used / kStages) & 1, &gave_up)) { ok = false; break; }
+                if (!barrier_wait<kLimit>(full + 8 * s, (used / kStages) & 1, &gave_up)) { ok = false; break; }
                 order_after();
                 const unsigned sa = ring + s * kStageBytes, sb = sa + kABytes;
                 const unsigned long long da = matrix_descriptor(sa, a_mn ? 8192 : 16), db = matrix_descriptor(sb, b_mn ? 8192 : 16);
@@ -449,8 +461,8 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
             if (ok) mma_commit(done + 8 * (turn & 1));
         }
         if (!ok) {
-            mma_commit(drain);
-            barrier_wait(drain, 0, nullptr);
+            mma_commit_here(drain);
+            barrier_wait<kLimit>(drain, 0, nullptr);
         }
     } else if (warp >= 2) {
         const int quarter = warp & 3;                         // the lanes of tensor memory that this warp may read
@@ -459,7 +471,7 @@ gemm_kernel(const __grid_constant__ GemmArgs a)
         unsigned char* stage = raw + (ring - smem_address(raw)) + kStages * kStageBytes + (warp - 2) * kStoreBytes;
         for (int turn = 0; next_unit<FORWARD>(a, turn, u); ++turn) {
             const GemmPart& p = a.part[u.part];
-            if (!barrier_wait(done + 8 * (turn & 1), (turn / 2) & 1, &gave_up)) break;
+            if (!__all_sync(0xffffffffu, barrier_wait<kLimit>(done + 8 * (turn & 1), (turn / 2) & 1, &gave_up))) break;
             __syncwarp();
             order_after();
             const unsigned d = tmem + (turn & 1) * kTileN + (static_cast<unsigned>(quarter * 32) << 16);

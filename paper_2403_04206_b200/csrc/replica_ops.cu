@@ -834,6 +834,16 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
     return st;
 }
 
+grawa_status grawa_selftest_gated_ffn_wait(grawa_stream_t stream)
+{
+    auto* const kernel = gemm_kernel<__nv_bfloat16, true, true>;
+    GemmArgs a{};                                             // two tiles of one worker, of four steps; no operands, no outputs
+    a.workers = 1;
+    a.part[0] = gemm_part(1, 2 * kTileM, kHalf, kHalf, 4 * kTileK, 1);
+    GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem));
+    return launch(kernel, dim3(2), kGemmThreads, kGemmSmem, stream, a);
+}
+
 grawa_status grawa_gated_ffn_status(grawa_stream_t stream)
 {
     int word = 0, zero = 0;
