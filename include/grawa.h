@@ -359,8 +359,9 @@ grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, c
 size_t grawa_gated_ffn_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_hidden, int M, int backward, int aligned);
 
 /* Synchronises `stream` and reports whether a bounded device wait of a gated feed-forward call on the current
- * device ran out since the last report: GRAWA_OK, or GRAWA_ERR_TIMEOUT (that call's outputs are incomplete).
- * Not for a stream that is being captured. */
+ * device ran out since the last report on this stream (since the library was loaded, for the first): GRAWA_OK, or
+ * GRAWA_ERR_TIMEOUT (that call's outputs are incomplete).  The call may have run on another stream: every stream that
+ * asks is told once.  Not for a stream that is being captured. */
 grawa_status grawa_gated_ffn_status(grawa_stream_t stream);
 
 /* Self-test of those waits: launches one pair of CTAs of the product kernel whose operands are never fetched.  Its

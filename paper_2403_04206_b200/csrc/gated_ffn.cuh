@@ -28,7 +28,7 @@
 // of which 130 are the elementwise kernel at 7.1 TB/s and the products run at 1440 TFLOP/s until the power limit
 // lowers the clock (cuBLAS 1170 to 1230 us for the products alone).
 //
-// Every wait for a barrier in shared memory is bounded: a CTA whose wait runs out records it in g_ffn_status, waits
+// Every wait for a barrier in shared memory is bounded: a CTA whose wait runs out counts it in g_ffn_timeouts, waits
 // (bounded) for its own copies and products in flight, frees its tensor memory and returns.  A warp decides as one: its
 // lanes leave together or go on together, as the instructions that take a whole warp need.  (Not bounded by the kernel: the
 // two waits of the pair for each other, which both CTAs reach for that reason, and the allocation of tensor
@@ -78,7 +78,7 @@ struct GemmArgs {
     int activation, accumulate;
 };
 
-__device__ int g_ffn_status = 0;            // 1: a wait ran out since the word was read
+__device__ unsigned g_ffn_timeouts = 0;     // waits that ran out, never set back: no report can be lost between two readers
 constexpr unsigned long long kGemmWaitLimitNs = 2000000000ull, kStarvedLimitNs = 2000000ull;
 
 // ------------------------------------------------------------------ barriers, copies, tensor memory
@@ -134,7 +134,7 @@ __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, vola
         if (gave_up && *gave_up) return false;
         if (nanoseconds() - t0 > LIMIT) {
             if (gave_up) *gave_up = 1;
-            atomicOr(&g_ffn_status, 1);
+            atomicAdd(&g_ffn_timeouts, 1u);
             return false;
         }
     }

@@ -4,6 +4,9 @@
 
 #include <cmath>
 #include <cstring>
+#include <map>
+#include <mutex>
+#include <new>
 #include <utility>
 
 #include "dropout.cuh"
@@ -846,13 +849,24 @@ grawa_status grawa_selftest_gated_ffn_wait(grawa_stream_t stream)
 
 grawa_status grawa_gated_ffn_status(grawa_stream_t stream)
 {
-    int word = 0, zero = 0;
-    GRAWA_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, g_ffn_status, sizeof word, 0, cudaMemcpyDeviceToHost, stream));
+    // What each stream's reports have seen of its device's count.  A call's own stream is not known to the count (a captured
+    // call may run on any), so every stream is told of every wait that ran out, once.
+    static std::mutex mutex;
+    static auto& seen = *new std::map<std::pair<int, cudaStream_t>, unsigned>;
+    int device = 0;
+    unsigned count = 0;
+    GRAWA_CUDA_TRY(cudaGetDevice(&device));
+    GRAWA_CUDA_TRY(cudaMemcpyFromSymbolAsync(&count, g_ffn_timeouts, sizeof count, 0, cudaMemcpyDeviceToHost, stream));
     GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
-    if (word == 0) return GRAWA_OK;
-    GRAWA_CUDA_TRY(cudaMemcpyToSymbolAsync(g_ffn_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, stream));
-    GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
-    return GRAWA_ERR_TIMEOUT;
+    try {
+        const std::lock_guard<std::mutex> lock(mutex);
+        unsigned& last = seen[{device, stream}];
+        if (static_cast<int>(count - last) <= 0) return GRAWA_OK;      // (another thread's report may have seen more)
+        last = count;
+        return GRAWA_ERR_TIMEOUT;
+    } catch (const std::bad_alloc&) {
+        return cuda_fail(cudaErrorMemoryAllocation, "grawa_gated_ffn_status");
+    }
 }
 
 }  // extern "C"

@@ -45,4 +45,17 @@ def test_on_a_stream_between_calls(grawa):
         grawa.grawa_selftest_gated_ffn_wait()
         second = forward(grawa, x, w_gate, w_up)
         assert grawa.grawa_gated_ffn_status() == -5
-    assert torch.equal(first, want) and torch.equal(second, want) and grawa.grawa_gated_ffn_status() == 0
+    assert torch.equal(first, want) and torch.equal(second, want)
+    grawa.grawa_gated_ffn_status()                            # (tells this stream of it)
+
+
+def test_every_stream_is_told_once(grawa):
+    """One caller's report does not take away another's."""
+    streams = [torch.cuda.Stream() for _ in range(3)] + [torch.cuda.current_stream()]
+    for s in streams:
+        grawa.grawa_gated_ffn_status(s)
+    for _ in range(2):
+        grawa.grawa_selftest_gated_ffn_wait(stream=streams[0])
+        torch.cuda.synchronize()
+        assert [grawa.grawa_gated_ffn_status(s) for s in streams] == [-5] * 4
+        assert [grawa.grawa_gated_ffn_status(s) for s in streams] == [0] * 4
