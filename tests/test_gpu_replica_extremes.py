@@ -1,0 +1,78 @@
+"""The replica operators at the ends of their values' ranges, element by element against the definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from replica_util import activation64, bound
+
+pytestmark = pytest.mark.gpu
+HALF = [torch.bfloat16, torch.float16]
+# The smallest subnormals are 2^-133 and 2^-24; below the normal numbers a store rounds to a multiple of them.  (bound() has the
+# half of it for float16 alone.)
+HALF_SUBNORMAL = {torch.bfloat16: 2.0 ** -134, torch.float16: 0.0}
+
+
+@pytest.fixture(scope="module")
+def grawa():
+    import paper_2403_04206_b200 as g
+    return g
+
+
+def gates(low, high, kind):
+    """Every value of a 16-bit type between low < high <= 0, as a column: weights of a gate whose input is 1."""
+    values = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(kind)
+    values = values[(values.double() >= low) & (values.double() <= high)]
+    return values[torch.argsort(values.double())].cuda()[:, None].contiguous()
+
+
+def value64(act, a):
+    """The activation with its relative accuracy in the tail (0.5 (1 + erf) cancels there)."""
+    if act == "gelu":
+        return 0.5 * a * torch.erfc(-a / math.sqrt(2.0))
+    return activation64(act, a)[0]
+
+
+# The exponential's argument is rounded once or twice (2^-24 of it each), and the fast exponential adds 2 + 1.16 |argument|
+# units of 2^-23 in relative error; the rest (quotient, polynomial, products) is below 2^-20.
+def relative(argument):
+    return 2.0 ** -20 + 2.0 ** -23 * (2.0 + 2.2 * argument.abs())
+
+
+@pytest.mark.parametrize("kind", HALF)
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("act,low", [("gelu", -12.0)])
+def test_forward_of_each_gate_value(grawa, kind, rows, act, low):
+    """h = act(a) with a exact: a row of one element that is 1, and u = 1."""
+    w = gates(low, 0.0, kind)
+    x, up = torch.ones(rows, 1, dtype=kind, device="cuda"), torch.ones_like(w)
+    h = torch.empty(rows, len(w), dtype=kind, device="cuda")
+    grawa.grawa_gated_ffn_forward([x], [w], [up], [h], activation=act)
+    a = w.double().T
+    want = value64(act, a)
+    lim = bound(want, kind, relative(a * a / 2 if act == "gelu" else a) * want.abs()) + HALF_SUBNORMAL[kind]
+    over = ((h.double() - want).abs() - lim)
+    at = over.flatten().argmax().item() % len(w)
+    assert (over <= 0).all(), f"at {a[0, at].item()}: got {h[0, at].item()}, expected {want[0, at].item()}"
+
+
+@pytest.mark.parametrize("kind", HALF)
+@pytest.mark.parametrize("act,low", [("gelu", -12.0)])
+def test_backward_of_each_gate_value(grawa, kind, act, low):
+    """One row, x = dh = u = 1: the weights' gradients are da and du themselves, which are rounded once."""
+    gate = gates(low, 0.0, kind).T.contiguous()
+    hidden = gate.shape[1]
+    one, ones, w = torch.ones(1, 1, dtype=kind, device="cuda"), torch.ones_like(gate), torch.ones(hidden, 1, dtype=kind, device="cuda")
+    dwg, dwu = torch.empty_like(w), torch.empty_like(w)
+    grawa.grawa_gated_ffn_backward([ones], [one], [w], [w], [gate], [ones], None, [dwg], [dwu], activation=act)
+    a = gate.double()[0]
+    rel = relative(a * a / 2 if act == "gelu" else a)
+    value = value64(act, a)
+    assert ((dwu[:, 0].double() - value).abs() <= bound(value, kind, rel * value.abs()) + HALF_SUBNORMAL[kind]).all()
+    if act == "gelu":
+        terms = [0.5 * torch.erfc(-a / math.sqrt(2.0)), a * torch.exp(-a * a / 2) / math.sqrt(2.0 * math.pi)]
+    else:                                                     # s (1 + a (1 - s)): the two terms cancel near their zero
+        s = torch.sigmoid(a)
+        terms = [s, s * a * torch.sigmoid(-a)]
+    slope, size = terms[0] + terms[1], terms[0].abs() + terms[1].abs()
+    assert ((dwg[:, 0].double() - slope).abs() <= bound(slope, kind, 2 * rel * size) + HALF_SUBNORMAL[kind]).all()
