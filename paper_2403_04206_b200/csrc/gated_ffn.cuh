@@ -236,9 +236,16 @@ __device__ __forceinline__ float2 normal_distribution(float a)
     const float tail = t * q * e;
     return make_float2(a >= 0.0f ? 1.0f - tail : tail, 0.39894228040143268f * e);
 }
+// The logistic function at a, and at -a (1 minus it, without cancellation).  From exp(-|a|), so that the divisor stays
+// between 1 and 2: with exp(-a) in it the quotient is 0 from a = -87.3 on, where it is still a normal number.
+__device__ __forceinline__ float2 logistic(float a)
+{
+    const float e = __expf(-fabsf(a)), r = __fdividef(1.0f, 1.0f + e);
+    return a >= 0.0f ? make_float2(r, e * r) : make_float2(e * r, r);
+}
 __device__ __forceinline__ float activation(int kind, float a)
 {
-    if (kind == kSilu) return __fdividef(a, 1.0f + __expf(-a));
+    if (kind == kSilu) return a * logistic(a).x;
     if (kind == kGelu) return a * normal_distribution(a).x;
     return a <= 0.0f ? 0.0f : a;
 }
@@ -260,8 +267,8 @@ __device__ __forceinline__ void gated_product(int kind, float (&v)[16], const fl
 __device__ __forceinline__ float2 activation_slope(int kind, float a)
 {
     if (kind == kSilu) {
-        const float s = __fdividef(1.0f, 1.0f + __expf(-a));
-        return make_float2(a * s, s * (1.0f + a * (1.0f - s)));
+        const float2 s = logistic(a);
+        return make_float2(a * s.x, s.x * fmaf(a, s.y, 1.0f));
     }
     if (kind == kGelu) {
         const float2 d = normal_distribution(a);

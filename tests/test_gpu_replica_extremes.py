@@ -41,7 +41,7 @@ def relative(argument):
 
 @pytest.mark.parametrize("kind", HALF)
 @pytest.mark.parametrize("rows", [1, 40])
-@pytest.mark.parametrize("act,low", [("gelu", -12.0)])
+@pytest.mark.parametrize("act,low", [("gelu", -12.0), ("silu", -90.0)])
 def test_forward_of_each_gate_value(grawa, kind, rows, act, low):
     """h = act(a) with a exact: a row of one element that is 1, and u = 1."""
     w = gates(low, 0.0, kind)
@@ -57,7 +57,7 @@ def test_forward_of_each_gate_value(grawa, kind, rows, act, low):
 
 
 @pytest.mark.parametrize("kind", HALF)
-@pytest.mark.parametrize("act,low", [("gelu", -12.0)])
+@pytest.mark.parametrize("act,low", [("gelu", -12.0), ("silu", -90.0)])
 def test_backward_of_each_gate_value(grawa, kind, act, low):
     """One row, x = dh = u = 1: the weights' gradients are da and du themselves, which are rounded once."""
     gate = gates(low, 0.0, kind).T.contiguous()
