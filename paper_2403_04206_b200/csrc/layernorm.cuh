@@ -495,7 +495,8 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
         if (a.has_dx) {
             s = row_sum<LPR>(s, buf);
             buf ^= 1;
-            const float mg = -s.x * a.inv_cols * rstd, mgh = -s.y * a.inv_cols * rstd * rstd;
+            // (f rstd is taken first: rstd^2, and mean(g h) rstd^2, may be past fp32's range where dx is far inside it)
+            const float mg = -s.x * a.inv_cols * rstd, mgh = -s.y * a.inv_cols * rstd;
             T* dx = static_cast<T*>(a.dx.p[m]) + r * a.x_stride;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -505,7 +506,7 @@ layernorm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
                     shifted<T>(xw[i], -mean, f);
                     unpack<T>(dw[i], d);
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e], mgh, mg));
+                    for (int e = 0; e < VE; ++e) f[e] = fmaf(d[e] * gm[i * VE + e], rstd, fmaf(f[e] * rstd, mgh, mg));
                     v = pack<T>(f);
                 }
                 R::store(dx, i, lane, lanes, cols, v, LANES);

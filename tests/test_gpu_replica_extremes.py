@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from replica_util import activation64, bound
+from replica_util import activation64, bound, layernorm_backward64
 
 pytestmark = pytest.mark.gpu
 HALF = [torch.bfloat16, torch.float16]
@@ -76,3 +76,28 @@ def test_backward_of_each_gate_value(grawa, kind, act, low):
         terms = [s, s * a * torch.sigmoid(-a)]
     slope, size = terms[0] + terms[1], terms[0].abs() + terms[1].abs()
     assert ((dwg[:, 0].double() - slope).abs() <= bound(slope, kind, 2 * rel * size) + HALF_SUBNORMAL[kind]).all()
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [60, 768, 2000, 20000])
+@pytest.mark.parametrize("scale,dy_scale", [(2.0 ** -60, 2.0 ** 14), (2.0 ** 50, 2.0 ** -34)])
+def test_layernorm_gradients_of_tiny_and_huge_rows(grawa, kind, cols, scale, dy_scale):
+    """The gradients are of the size of dy / sigma, which the types hold, though its square or the mean's products with it
+    are not: rows of standard deviation 2^-60 and 2^50, without eps."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    rows = 9
+    h, gamma = normal(rows, cols), (1.0 + 0.3 * normal(cols)).to(kind)
+    x = (h * scale).to(kind)
+    dy = ((normal(rows, cols) + h) * dy_scale).to(kind)        # so that mean(g h) is of dy's size
+    mean = x.double().mean(-1)
+    rstd = (1.0 / (x.double() - mean[:, None]).square().mean(-1).sqrt()).float()
+    mean = mean.float()
+    dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    grawa.grawa_layernorm_backward([dy], [x], [gamma], [mean], [rstd], [dx], [dgamma], [dbeta])
+    for name, got, (want, e) in zip(("dx", "dgamma", "dbeta"), (dx, dgamma, dbeta), layernorm_backward64(dy, x, gamma, mean, rstd)):
+        err = (got.double() - want).abs()
+        assert torch.isfinite(got).all() and (err <= bound(want, kind, e)).all(), f"{name}: off by {(err / want.abs().max()).max().item()} of the largest"
