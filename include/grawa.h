@@ -260,18 +260,23 @@ grawa_status grawa_step_host_typed(grawa_dtype dtype, grawa_variant variant, voi
  * Replica operators: layers of the local phase (the forward and backward passes whose accumulated
  * gradients the step entry points read) run for all M workers in one call.  The paper leaves the
  * model to the caller; these operators exist for callers who keep M replicas as flat vectors on one
- * GPU: a layer's weights are read in place, at any element offset inside the workers' parameter
+ * GPU: a layer's weights are passed where they stand, at any element offset inside the workers' parameter
  * vectors, and its gradients are written to, or added to (G_k = sum over samples, Eq. 3), the
- * workers' gradient vectors.
+ * workers' gradient vectors.  (The product's tensor-core kernel cannot read weights that are not 16-byte
+ * aligned, or whose rows are not a multiple of 8 elements: such a call copies them to its workspace first, unless it
+ * is a forward call of up to 16 rows.)
  *
  *   - Tables (x, y, gamma, ...) are HOST arrays of M DEVICE pointers on the current device, elements
  *     stored in `dtype`, aligned to the element size; 16-byte aligned rows take the vector kernels.
  *     Tables are read during the call only.
  *   - Arithmetic is fp32 on exactly widened elements; each stored value is rounded to nearest-even once.
+ *     (The gated product's backward pass rounds two values on the way, see there; its activations carry the
+ *     fast exponential's relative error, 2^-22 for every unit of the exponent and 2^-20 at least.)
  *   - No output may overlap another buffer of the call; overlap visible from the pointers is rejected.
  *     A buffer of one row, or of rows of the same stride, that lies between the rows of another does not
- *     overlap it; rows of two different strides between each other are rejected.  Elements between the
- *     end of a row and the next row are neither read nor written.
+ *     overlap it; rows of two different strides between each other are rejected.
+ *   - What stands in front of, behind or between the rows of a buffer has no influence on a result and is
+ *     never written.  It may be read: the aligned 16-byte words that hold a row's ends are read whole.
  *   - Work is enqueued on `stream`, nothing synchronises, no call allocates device memory or keeps
  *     anything for the next one, and results are bitwise reproducible.  Calls may be captured into a
  *     CUDA graph (a program's first call with an operator and type before the capture: the driver loads
@@ -342,7 +347,9 @@ grawa_status grawa_gated_ffn_forward(grawa_dtype dtype, grawa_activation act, co
 
 /* Its gradients from dh and the forward call's a (gate) and u (up), with da = dh u act'(a) and du = dh act(a):
  *   dx = da Wg + du Wu,  dWg = da^T x,  dWu = du^T x.
- * da and du are rounded to `dtype` on the way (the tensor cores' operands).  dx may be NULL, dw_gate and dw_up
+ * da and du are rounded to `dtype` on the way (the tensor cores' operands), which makes the gradients' error 1.4
+ * times that of one rounding at the end; with GRAWA_F16 a da or du past 65504 is infinite and one below 2^-25 is
+ * zero, as if it were stored (scale dh against that).  dx may be NULL, dw_gate and dw_up
  * both may be, not all three.  accumulate != 0 adds dw_gate and dw_up to what the buffers hold (one rounding of
  * the sum), 0 overwrites them; rows = 0 overwrites with zeros.  The slope of GRAWA_RELU at 0 is 0. */
 grawa_status grawa_gated_ffn_backward(grawa_dtype dtype, grawa_activation act, const void *const *dh,

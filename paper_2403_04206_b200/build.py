@@ -24,7 +24,8 @@ OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_ho
 MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 
-# IEEE arithmetic throughout: no fast-math.
+# No fast-math: arithmetic is IEEE but for the approximate functions that the sources call by name (the activations of the gated
+# feed-forward product, the reciprocal root of layer norm).
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]
 

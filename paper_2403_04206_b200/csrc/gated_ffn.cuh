@@ -23,7 +23,7 @@
 // Where a product has fewer tiles than there are pairs of SMs, its sum is split among them and the parts, in fp32,
 // are added by a second kernel in a fixed order.
 //
-// Measured (B200), 4 workers x 4096 tokens, 2048 -> 5632, bf16: forward 590 to 640 us with a, u and h stored (1180 to 1280
+// Measured (B200), 4 workers x 4096 tokens, 2048 -> 5632, bf16: forward 590 to 635 us with a, u and h stored (1190 to 1280
 // TFLOP/s; cuBLAS takes 570 to 605 for the two projections alone, under the same power limit); backward 1250 to 1400 us,
 // of which 130 are the elementwise kernel at 7.1 TB/s and the products run at 1440 TFLOP/s until the power limit
 // lowers the clock (cuBLAS 1170 to 1230 us for the products alone).
@@ -620,7 +620,8 @@ gemm_join_kernel(const __grid_constant__ GemmArgs a, int part)
 // matrix instruction (multiply-adds of the plain cores, two products an instruction, were the bound from 2 rows on:
 // 4 x 5 tokens, 768 -> 2048, 11.3 us).  As the order along the sum is free, a lane's operands are 16 neighbouring bytes of
 // a row, in the weights and in x alike: four lanes read 64 bytes of a row, where they stand, at any alignment (the
-// tcgen05 path would lay unaligned weights out again first).  x comes from the L1 cache.
+// tcgen05 path would lay unaligned weights out again first).  x comes from the L1 cache.  Four CTAs an SM hold the kernel of up
+// to 8 rows to 64 registers, where weights that start anywhere spill 48 bytes: 4 x 5 tokens, 768 -> 2048, 8.2 us for 3.9 of bytes.
 struct FewArgs {
     In x, w_gate, w_up;
     Out h, gate, up;                       // gate and up may be NULL

@@ -10,11 +10,16 @@
 //
 // Rows are handled by 8 lanes, a warp or a CTA, whichever holds the row in its registers; a warp alone holds
 // up to 4096 16-bit elements (no barriers, and every lane has up to 256 bytes of loads in flight).  Longer
-// rows are read again from L2 instead.
+// rows are read again, from L2 as far as it still holds them (in the backward pass by two kernels, the second of which finds
+// nothing left there).
 //
-// Measured (B200, 6.54 TB/s copy): forward of 4 x 8192 x 4096 bf16 97 us = 5.5 TB/s (84 %), of 8 x 6184 x 768 fp32 52 us
-// = 5.8 TB/s; backward of 8 x 6304 x 768 bf16 47 us = 5.0 TB/s (76 %, its issue slots 68 % busy: 26 instructions an
-// element, held to 128 registers by the column sums), of the same in fp32 78 us = 5.9 TB/s.
+// Measured (B200, 6.54 TB/s copy), in shares of the copy rate: forward of 4 x 8192 x 4096 bf16 98 us (84 %), 16-bit rows of
+// 1024 to 12000 elements 75 to 87 %, of 256 69 %, of 768 67 to 85 % (27 to 35 us for 8 x 6184 rows from run to run), fp32 86 to
+// 90 %; backward of 8 x 6304 x 768 bf16 47 us (75 %; 26 instructions an element when counted, one more since, held
+// to 128 registers by the column sums, 23 % of the warps active, issue slots 68 % busy: no unit is full), 256 to 4096 columns 70 to 76 %,
+// fp32 88 %.  Far from it: backward rows of 8192 (57 us, 61 %: a barrier a row, one CTA an SM) and, above what a CTA's registers
+// hold, of 12000 (104 us for 34.9, x and dy read twice); 16-bit rows that do not start on 16 bytes, forward 64 us for 23.3 and
+// backward 119 for 34.9 (8 x 4745 x 1001: two words read and shifted for every one, and no staging in the backward pass).
 #pragma once
 #include <cooperative_groups.h>
 

@@ -30,10 +30,9 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
 // padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0: matrices
-// [rows, cols] (a transposed one has as many elements, in another order), or, where cols is 1 or the tensor is no matrix, any
-// that hold as many.  Below the
-// stride, in the lowest 4 bits of *layout: the bits below 16 that any of the addresses has.  *table: bytes, or the
-// integer 0 for None.
+// [rows, cols] (a transposed one has as many elements, in another order), or, where cols is 1 or the tensor is no
+// matrix, any that hold as many.  Below the stride, in the lowest 4 bits of *layout: the bits below 16 that any of the
+// addresses has.  *table: bytes, or the integer 0 for None.
 bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int device, PyObject** table, int64_t* layout)
 {
     const char* name;

@@ -495,7 +495,9 @@ static grawa_status launch_gemm(grawa_dtype dtype, GemmArgs& a, cudaStream_t str
 }
 
 // Up to kFewRows rows go by the kernel for a few rows.  (4 workers, 2048 -> 5632, bf16: 31 us for 1 row and 39 for 16,
-// against 55 and 50 by the tensor cores' tiles; 24 rows 67 against 49.)
+// against 55 and 50 by the tensor cores' tiles; 24 rows 67 against 49.  Narrow weights leave most SMs idle, and it still
+// wins: 1 worker, 4096 -> 64, 5.5 to 13 us against 16 to 18; only a very long sum loses, 12288 -> 17 at odd places 21 to 32
+// against 16.)
 static bool takes_few(int64_t rows) { return rows <= kFewRows; }
 
 template <typename T, int NT>
