@@ -460,9 +460,9 @@ _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 
 def _tables(first, specs):
-    """Storage type code, then pointer table (bytes, read by the C call, or 0) and layout (16 * row stride + the low 4 bits of the addresses; stride 0 for contiguous
-    tensors) of each spec (name, tensors or None, rows, cols, mode), from the native marshaller, which checks types, sizes,
-    contiguity and that all tensors are on the current device; last the device."""
+    """Storage type code, then pointer table (bytes, read by the C call, or 0) and layout (16 * row stride + the low 4 bits of
+    the addresses; stride 0 for contiguous tensors) of each spec (name, tensors or None, rows, cols, mode), from the native
+    marshaller, which checks types, sizes, shapes, contiguity and that all tensors are on the current device; last the device."""
     global _marshal
     import torch
     if _marshal is None:

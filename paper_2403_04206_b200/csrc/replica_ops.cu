@@ -853,14 +853,14 @@ grawa_status grawa_gated_ffn_status(grawa_stream_t stream)
 {
     // What each stream's reports have seen of its device's count.  A call's own stream is not known to the count (a captured
     // call may run on any), so every stream is told of every wait that ran out, once.
-    static std::mutex mutex;
-    static auto& seen = *new std::map<std::pair<int, cudaStream_t>, unsigned>;
     int device = 0;
     unsigned count = 0;
     GRAWA_CUDA_TRY(cudaGetDevice(&device));
     GRAWA_CUDA_TRY(cudaMemcpyFromSymbolAsync(&count, g_ffn_timeouts, sizeof count, 0, cudaMemcpyDeviceToHost, stream));
     GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
     try {
+        static std::mutex mutex;
+        static auto& seen = *new std::map<std::pair<int, cudaStream_t>, unsigned>;
         const std::lock_guard<std::mutex> lock(mutex);
         unsigned& last = seen[{device, stream}];
         if (static_cast<int>(count - last) <= 0) return GRAWA_OK;      // (another thread's report may have seen more)

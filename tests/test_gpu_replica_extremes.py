@@ -101,3 +101,16 @@ def test_layernorm_gradients_of_tiny_and_huge_rows(grawa, kind, cols, scale, dy_
     for name, got, (want, e) in zip(("dx", "dgamma", "dbeta"), (dx, dgamma, dbeta), layernorm_backward64(dy, x, gamma, mean, rstd)):
         err = (got.double() - want).abs()
         assert torch.isfinite(got).all() and (err <= bound(want, kind, e)).all(), f"{name}: off by {(err / want.abs().max()).max().item()} of the largest"
+
+
+def test_half_precision_limits_of_the_gated_gradients(grawa):
+    """da and du are values of the storage type: past 65504 infinite in half, and what bfloat16 holds in bfloat16."""
+    for kind, finite in ((torch.float16, False), (torch.bfloat16, True)):
+        def full(rows, cols, value):
+            return torch.full((rows, cols), value, dtype=kind, device="cuda")
+
+        x, dh, gate, up, w = full(1, 8, 2.0 ** -10), full(1, 16, 512.0), full(1, 16, 1.0), full(1, 16, 256.0), full(16, 8, 1.0)
+        dx, dwg, dwu = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+        grawa.grawa_gated_ffn_backward([dh], [x], [w], [w], [gate], [up], [dx], [dwg], [dwu], activation="relu")
+        assert (dwu == 0.5).all()                             # du = 512
+        assert (dwg == (128.0 if finite else math.inf)).all() and torch.isfinite(dx).all() == finite      # da = 2^17
