@@ -376,6 +376,92 @@ grawa_status grawa_gated_ffn_status(grawa_stream_t stream);
  * reports GRAWA_ERR_TIMEOUT.  Touches no caller memory. */
 grawa_status grawa_selftest_gated_ffn_wait(grawa_stream_t stream);
 
+/* Pairs of elements that a rotation by position turns: (i, i + rotary / 2) or (2 i, 2 i + 1), i < rotary / 2. */
+typedef enum grawa_pairing { GRAWA_PAIR_HALVES = 0, GRAWA_PAIR_NEIGHBOURS = 1 } grawa_pairing;
+
+/* Norms of the query and key heads with the rotation by position, in one pass.  For each head x of head_dim elements in
+ * each row, with its weight w (of the query heads, or of the key heads):
+ *   s = 1 / sqrt(mean x^2 + eps),  z = w x s,  y = z with its leading `rotary` elements turned in pairs, pair i by the
+ *   angle position * frequencies[i]:  (a, b) -> (a cos - b sin, b cos + a sin).
+ * q, q_out: `rows` rows of q_heads heads behind each other, q_stride / q_out_stride elements from row to row; k, k_out
+ * likewise (all may be NULL with k_heads = 0).  q_weight, k_weight: head_dim elements a worker, anywhere; either may be
+ * NULL (1).  head_dim in [1, 256], any; rotary even, 0 to head_dim.  q_out_m may be the same buffer as q_m where their
+ * strides are equal, k_out_m as k_m (a backward pass needs what q and k held before).
+ * positions: DEVICE, `rows` int64 a worker; NULL: the row number modulo `period` (>= 1).  frequencies: DEVICE,
+ * rotary / 2 fp64 values, for all workers (NULL with rotary = 0).  Angles are taken and reduced in fp64, squares summed
+ * in fp32.  eps >= 0.  rows = 0 is a no-op.  Heads, rows and rotated halves of whole 16-byte words at 16-byte
+ * boundaries take the vector kernels. */
+grawa_status grawa_head_rotary_forward(grawa_dtype dtype, grawa_pairing pairing, const void *const *q, const void *const *k,
+                                       const void *const *q_weight, const void *const *k_weight, void *const *q_out,
+                                       void *const *k_out, const int64_t *const *positions, const double *frequencies,
+                                       int64_t rows, int64_t q_heads, int64_t k_heads, int64_t head_dim, int64_t rotary,
+                                       int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride,
+                                       int64_t period, int M, float eps, grawa_stream_t stream);
+
+/* Its gradients from dq_out and dk_out (row strides q_out_stride, k_out_stride): with dz = dy turned back, h = x s, g = dz w,
+ *   dx = s (g - h mean(g h)),  dw = sum over rows and heads of dz h.
+ * dq has row stride q_stride, dk k_stride; dq_m may be the same buffer as dq_out_m where the strides are equal, dk_m as
+ * dk_out_m.  dq, dk, dq_weight, dk_weight: any of them may be NULL, not all.  accumulate != 0 adds dq_weight and dk_weight
+ * to what the buffers hold (one rounding of the sum), 0 overwrites them; rows = 0 overwrites with zeros.
+ * workspace: DEVICE scratch, 16-byte aligned, of grawa_head_rotary_backward_workspace_bytes(rows, M) bytes (none without
+ * dq_weight and dk_weight, or for up to 8 rows); it needs no particular contents. */
+grawa_status grawa_head_rotary_backward(grawa_dtype dtype, grawa_pairing pairing, const void *const *dq_out,
+                                        const void *const *dk_out, const void *const *q, const void *const *k,
+                                        const void *const *q_weight, const void *const *k_weight, void *const *dq,
+                                        void *const *dk, void *const *dq_weight, void *const *dk_weight,
+                                        const int64_t *const *positions, const double *frequencies, int64_t rows,
+                                        int64_t q_heads, int64_t k_heads, int64_t head_dim, int64_t rotary, int64_t q_stride,
+                                        int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, int64_t period, int M,
+                                        float eps, int accumulate, void *workspace, size_t workspace_bytes,
+                                        grawa_stream_t stream);
+
+/* 0 on invalid arguments. */
+size_t grawa_head_rotary_backward_workspace_bytes(int64_t rows, int M);
+
+/* Attention within a window and to a few first tokens.  Sequences of tokens lie behind each other in a worker's rows.  Query
+ * i of the sequence [a, b) sees key j of the same sequence when
+ *   j <= i + right   and   (j >= i - left   or   j < a + sinks),
+ * so right = 0 is causal, and left, right >= rows see everything.  For each query head, with its key head's k and v (that
+ * of query head h is h / (q_heads / kv_heads)):
+ *   S_ij = scale q_i k_j,  lse_i = log sum_j exp S_ij,  out_i = sum_j exp(S_ij - lse_i) v_j   over the keys that i sees.
+ * q, out: `rows` rows of q_heads heads of head_dim elements, q_stride / out_stride elements from row to row; k, v likewise
+ * of kv_heads heads, which divides q_heads.  dtype GRAWA_BF16 or GRAWA_F16 (the tensor cores' operands; fp32 is refused);
+ * head_dim a multiple of 8 up to 128; bases 16-byte aligned and strides multiples of 8 elements (others are refused).
+ * lse: DEVICE, fp32, [q_heads][rows] a worker, for the backward pass; may be NULL.
+ * offsets: DEVICE, sequences + 1 int64 a worker, not decreasing: sequence s is the rows [offsets[s], offsets[s + 1]), empty
+ * ones included.  Rows in front of the first and behind the last are in none; out and lse keep what they hold there.
+ * (Offsets that decrease or leave [0, rows] give some runs of rows instead; nothing outside the buffers is touched.)
+ * NULL: sequences of `period` (>= 1) rows, the last one what is left; `period` is not used otherwise.
+ * left, right, sinks >= 0; scale > 0.  rows = 0 is a no-op.
+ * Sums and statistics are fp32; exp(S - m), with m within 2^8 of the largest so far, is rounded to `dtype` for the product with v.
+ * A row's result depends on no key or value that it does not see, whatever those hold, infinities and NaN included. */
+grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void *const *q, const void *const *k, const void *const *v,
+                                            void *const *out, float *const *lse, const int64_t *const *offsets,
+                                            int64_t sequences, int64_t period, int64_t left, int64_t right, int64_t sinks,
+                                            int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                            int64_t q_stride, int64_t k_stride, int64_t v_stride, int64_t out_stride, int M,
+                                            float scale, grawa_stream_t stream);
+
+/* Its gradients from dout (row stride out_stride) and the forward call's out and lse, with P_ij = exp(S_ij - lse_i) and
+ * dS_ij = P_ij (dout_i v_j - dout_i out_i):
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i,
+ * those of a key head summed over its query heads.  dq has row stride q_stride, dk k_stride, dv v_stride.  dq may be NULL,
+ * dk and dv both may be, not all three.  Rows of no sequence keep what they hold.  P and dS are rounded to `dtype` for the
+ * products (with GRAWA_F16 scaled by powers of two that keep them in its range).
+ * workspace: DEVICE scratch, 256-byte aligned, of grawa_window_attention_backward_workspace_bytes(...) bytes; it needs no
+ * particular contents. */
+grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void *const *dout, const void *const *q,
+                                             const void *const *k, const void *const *v, const void *const *out,
+                                             const float *const *lse, void *const *dq, void *const *dk, void *const *dv,
+                                             const int64_t *const *offsets, int64_t sequences, int64_t period, int64_t left,
+                                             int64_t right, int64_t sinks, int64_t rows, int64_t q_heads, int64_t kv_heads,
+                                             int64_t head_dim, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                             int64_t out_stride, int M, float scale, void *workspace, size_t workspace_bytes,
+                                             grawa_stream_t stream);
+
+/* 0 on invalid arguments. */
+size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int M);
+
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not
  * exceed it (for example M = 16 workers of up to 134 million elements each). */
 #define GRAWA_STATIC_MAX_PARTIALS 131072

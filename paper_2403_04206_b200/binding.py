@@ -125,6 +125,18 @@ def library() -> ctypes.CDLL:
     lib.grawa_gated_ffn_status.restype = ci
     lib.grawa_selftest_gated_ffn_wait.argtypes = [vp]
     lib.grawa_selftest_gated_ffn_wait.restype = ci
+    lib.grawa_head_rotary_forward.argtypes = [ci, ci] + [vp] * 8 + [i64] * 10 + [ci, cf, vp]
+    lib.grawa_head_rotary_forward.restype = ci
+    lib.grawa_head_rotary_backward.argtypes = [ci, ci] + [vp] * 12 + [i64] * 10 + [ci, cf, ci, vp, sz, vp]
+    lib.grawa_head_rotary_backward.restype = ci
+    lib.grawa_head_rotary_backward_workspace_bytes.argtypes = [i64, ci]
+    lib.grawa_head_rotary_backward_workspace_bytes.restype = sz
+    lib.grawa_window_attention_forward.argtypes = [ci] + [vp] * 6 + [i64] * 13 + [ci, cf, vp]
+    lib.grawa_window_attention_forward.restype = ci
+    lib.grawa_window_attention_backward.argtypes = [ci] + [vp] * 10 + [i64] * 13 + [ci, cf, vp, sz, vp]
+    lib.grawa_window_attention_backward.restype = ci
+    lib.grawa_window_attention_backward_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.grawa_window_attention_backward_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -455,8 +467,9 @@ def grawa_sumsq_static(grads, sumsq_out, *, stream=None, n=None) -> None:
 # ------------------------------------------------------------------ replica operators
 
 _marshal = None
-_ROWS, _OPTIONAL, _FLOAT32 = 1, 2, 4          # modes of a table, as in csrc/marshal.cpp
+_ROWS, _OPTIONAL, _FLOAT32, _INT64 = 1, 2, 4, 8          # modes of a table, as in csrc/marshal.cpp; << 8: the head dimension
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+_PAIRINGS = {"halves": 0, "neighbours": 1}
 
 
 def _tables(first, specs):
@@ -630,6 +643,130 @@ def grawa_gated_ffn_status(stream=None) -> int:
 def grawa_selftest_gated_ffn_wait(*, stream=None) -> None:
     """Launches the product kernel's bounded-wait self-test; grawa_gated_ffn_status then reports -5."""
     _raise(library().grawa_selftest_gated_ffn_wait(_stream(stream)), "grawa_selftest_gated_ffn_wait")
+
+
+def _heads(t, name):
+    shape = t[0].shape
+    if len(shape) != 3:
+        raise ValueError(f"{name}: expected 3-D tensors [rows, heads, head_dim]")
+    return shape
+
+
+def _frequencies(frequencies, device):
+    """Address and number of the rotated elements."""
+    if frequencies is None:
+        return None, 0
+    if str(frequencies.dtype) != "torch.float64":
+        raise TypeError(f"frequencies: expected float64, got {frequencies.dtype}")
+    _on_device(frequencies, device, "frequencies")
+    return _addr(frequencies), 2 * frequencies.numel()
+
+
+def _head_specs(q, k):
+    """Sizes (rows, query heads, key heads, head_dim) and the modes of tables of heads."""
+    rows, heads, dim = _heads(q, "q")
+    kv_heads = 0
+    if k is not None:
+        kv_heads = _heads(k, "k")[1]
+        if kv_heads == 0:
+            raise ValueError("k: expected at least one head")
+    return rows, heads, kv_heads, dim, _ROWS | dim << 8
+
+
+def grawa_head_rotary_forward(q, k, q_weight, k_weight, q_out, k_out, frequencies, *, positions=None, period=None, pairing="halves", eps=1e-6,
+                              stream=None) -> None:
+    """RMS norm of each head of q and k (lists of [rows, heads, head_dim], rows may be padded) with the weights ([head_dim], or
+    None), then the rotation of the leading 2 * len(frequencies) elements (float64, device; None: none) by the rows' positions ([rows]
+    int64; None: the row number, modulo ``period`` if given).  k, k_weight and k_out may be None; q_out may be q, k_out k."""
+    rows, heads, kv_heads, dim, mode = _head_specs(q, k)
+    code, qt, qs, kt, ks, qw, _, kw, _, qo, qos, ko, kos, pos, _, dev = _tables(q, (
+        ("q", q, rows, heads * dim, mode), ("k", k, rows, kv_heads * dim, mode | _OPTIONAL), ("q_weight", q_weight, dim, 1, _OPTIONAL),
+        ("k_weight", k_weight, dim, 1, _OPTIONAL), ("q_out", q_out, rows, heads * dim, mode),
+        ("k_out", k_out, rows, kv_heads * dim, mode if kv_heads else mode | _OPTIONAL), ("positions", positions, rows, 1, _OPTIONAL | _INT64)))
+    f, rotary = _frequencies(frequencies, dev)
+    status = library().grawa_head_rotary_forward(code, _PAIRINGS[pairing], qt, kt, qw, kw, qo, ko, pos, f, rows, heads, kv_heads, dim, rotary, qs >> 4, ks >> 4,
+                                                 qos >> 4, kos >> 4, (rows or 1) if period is None else period, len(q), eps, _stream_on(stream, dev))
+    _raise(status, "grawa_head_rotary_forward")
+
+
+def grawa_head_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, dq, dk, dq_weight, dk_weight, frequencies, *, positions=None, period=None,
+                               pairing="halves", eps=1e-6, accumulate=False, workspace=None, stream=None) -> None:
+    """Gradients of grawa_head_rotary_forward; dq, dk, dq_weight and dk_weight may each be None.  dq and dk need the row strides of q
+    and k, and may be dq_out and dk_out where those have them too.  accumulate adds the weights' gradients to what the buffers hold."""
+    lib, M = library(), len(q)
+    rows, heads, kv_heads, dim, mode = _head_specs(q, k)
+    optional = mode | _OPTIONAL
+    code, qo, qos, ko, kos, qt, qs, kt, ks, qw, _, kw, _, dqt, dqs, dkt, dks, dqw, _, dkw, _, pos, _, dev = _tables(q, (
+        ("dq_out", dq_out, rows, heads * dim, mode), ("dk_out", dk_out, rows, kv_heads * dim, mode if kv_heads else optional),
+        ("q", q, rows, heads * dim, mode), ("k", k, rows, kv_heads * dim, optional), ("q_weight", q_weight, dim, 1, _OPTIONAL),
+        ("k_weight", k_weight, dim, 1, _OPTIONAL), ("dq", dq, rows, heads * dim, optional), ("dk", dk, rows, kv_heads * dim, optional),
+        ("dq_weight", dq_weight, dim, 1, _OPTIONAL), ("dk_weight", dk_weight, dim, 1, _OPTIONAL), ("positions", positions, rows, 1, _OPTIONAL | _INT64)))
+    for name, t, s, of in (("dq", dq, dqs, qs), ("dk", dk, dks, ks)):
+        if t is not None and s >> 4 != of >> 4:
+            raise ValueError(f"{name}: expected the row stride of {name[1:]}")
+    f, rotary = _frequencies(frequencies, dev)
+    keep = workspace
+    if keep is None and (dq_weight is not None or dk_weight is not None):
+        keep = _scratch(None, lib.grawa_head_rotary_backward_workspace_bytes(rows, M), stream)
+    status = lib.grawa_head_rotary_backward(code, _PAIRINGS[pairing], qo, ko, qt, kt, qw, kw, dqt, dkt, dqw, dkw, pos, f, rows, heads, kv_heads, dim, rotary,
+                                            qs >> 4, ks >> 4, qos >> 4, kos >> 4, (rows or 1) if period is None else period, M, eps, 1 if accumulate else 0,
+                                            *_scratch_args(keep, dev), _stream_on(stream, dev))
+    _raise(status, "grawa_head_rotary_backward")
+
+
+def grawa_head_rotary_backward_workspace_bytes(rows: int, M: int) -> int:
+    return int(library().grawa_head_rotary_backward_workspace_bytes(rows, M))
+
+
+def _window(rows, offsets, period, left, right, sinks):
+    """offsets' length, then sequences, period, left, right and sinks as the C calls take them (None: no limit)."""
+    length = offsets[0].numel() if offsets is not None else 0
+    if offsets is not None and length < 1:
+        raise ValueError("offsets: expected at least one element")
+    every = rows or 1
+    return length, (max(0, length - 1), every if period is None else period, every if left is None else left, every if right is None else right, sinks)
+
+
+def grawa_window_attention_forward(q, k, v, out, *, lse=None, offsets=None, period=None, left=None, right=0, sinks=0, scale=None, stream=None) -> None:
+    """Attention of q ([rows, heads, head_dim]) over k and v ([rows, kv_heads, head_dim]) of each worker, bfloat16 or float16, rows
+    may be padded: a row sees the keys of its sequence from ``left`` rows in front of it (None: all) to ``right`` behind it (0:
+    causal, None: all), and of the sequence's first ``sinks`` rows those up to there.  Sequences: offsets ([sequences + 1] int64) or
+    ``period`` rows each (None: one).  lse ([heads, rows] float32) is filled for the backward pass when given."""
+    rows, heads, kv_heads, dim, mode = _head_specs(q, k)
+    length, window = _window(rows, offsets, period, left, right, sinks)
+    code, qt, qs, kt, ks, vt, vs, ot, os, lt, _, off, _, dev = _tables(q, (
+        ("q", q, rows, heads * dim, mode), ("k", k, rows, kv_heads * dim, mode), ("v", v, rows, kv_heads * dim, mode), ("out", out, rows, heads * dim, mode),
+        ("lse", lse, heads, rows, _OPTIONAL | _FLOAT32), ("offsets", offsets, length, 1, _OPTIONAL | _INT64)))
+    status = library().grawa_window_attention_forward(code, qt, kt, vt, ot, lt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4, os >> 4,
+                                                      len(q), dim ** -0.5 if scale is None else scale, _stream_on(stream, dev))
+    _raise(status, "grawa_window_attention_forward")
+
+
+def grawa_window_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, *, offsets=None, period=None, left=None, right=0, sinks=0, scale=None,
+                                    workspace=None, stream=None) -> None:
+    """Gradients of grawa_window_attention_forward from dout and its out and lse; dq may be None, dk and dv both may be.  dout needs
+    the row stride of out, dq, dk and dv those of q, k and v.  Without a workspace the call takes one from torch's allocator."""
+    lib, M = library(), len(q)
+    rows, heads, kv_heads, dim, mode = _head_specs(q, k)
+    length, window = _window(rows, offsets, period, left, right, sinks)
+    wide, narrow, optional = heads * dim, kv_heads * dim, mode | _OPTIONAL
+    code, gt, gs, qt, qs, kt, ks, vt, vs, ot, os, lt, _, dqt, dqs, dkt, dks, dvt, dvs, off, _, dev = _tables(q, (
+        ("dout", dout, rows, wide, mode), ("q", q, rows, wide, mode), ("k", k, rows, narrow, mode), ("v", v, rows, narrow, mode),
+        ("out", out, rows, wide, mode), ("lse", lse, heads, rows, _FLOAT32), ("dq", dq, rows, wide, optional), ("dk", dk, rows, narrow, optional),
+        ("dv", dv, rows, narrow, optional), ("offsets", offsets, length, 1, _OPTIONAL | _INT64)))
+    for name, t, s, of, other in (("dout", dout, gs, os, "out"), ("dq", dq, dqs, qs, "q"), ("dk", dk, dks, ks, "k"), ("dv", dv, dvs, vs, "v")):
+        if t is not None and s >> 4 != of >> 4:
+            raise ValueError(f"{name}: expected the row stride of {other}")
+    keep = workspace
+    if keep is None:
+        keep = _scratch(None, lib.grawa_window_attention_backward_workspace_bytes(rows, heads, M), stream)
+    status = lib.grawa_window_attention_backward(code, gt, qt, kt, vt, ot, lt, dqt, dkt, dvt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4,
+                                                 os >> 4, M, dim ** -0.5 if scale is None else scale, *_scratch_args(keep, dev), _stream_on(stream, dev))
+    _raise(status, "grawa_window_attention_backward")
+
+
+def grawa_window_attention_backward_workspace_bytes(rows: int, q_heads: int, M: int) -> int:
+    return int(library().grawa_window_attention_backward_workspace_bytes(rows, q_heads, M))
 
 
 def grawa_workspace_bytes(n: int, M: int, layer_offsets=None) -> int:

@@ -14,11 +14,10 @@ TRACE_LIB_PATH = os.path.join(_HERE, "libgrawa_trace.so")
 SOURCES = [os.path.join(CSRC, "grawa.cu")]
 HEADERS = [os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "center_pull_bulk.cuh"), os.path.join(CSRC, "kernels_16bit.cuh"), os.path.join(CSRC, "center_pull_staged_any.cuh"),
            os.path.join(CSRC, "host_common.h"), os.path.join(_ROOT, "include", "grawa.h")]
-# The replica operators have no debug or trace code of their own: one object, linked into every variant.
-OPS_OBJECT = os.path.join(_HERE, "_build", "replica_ops.o")
-OPS_SOURCE = os.path.join(CSRC, "replica_ops.cu")
-OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "dropout.cuh", "layernorm.cuh", "gated_ffn.cuh", "host_common.h")] + [
-    os.path.join(_ROOT, "include", "grawa.h")]
+# The replica operators have no debug or trace code of their own: objects that are linked into every variant.
+OPS_SOURCES = [os.path.join(CSRC, s) for s in ("replica_ops.cu", "attention_ops.cu")]
+OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "tensor_core.cuh", "dropout.cuh", "layernorm.cuh", "gated_ffn.cuh",
+                                               "head_rotary.cuh", "attention_rows.cuh", "host_common.h")] + [os.path.join(_ROOT, "include", "grawa.h")]
 
 # The binding's marshaller of pointer tables (a CPython module that reads torch tensors).
 MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
@@ -41,7 +40,7 @@ def is_stale(path: str = LIB_PATH) -> bool:
     if not os.path.exists(path):
         return True
     t = os.path.getmtime(path)
-    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS + [OPS_SOURCE] + OPS_HEADERS)
+    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS + OPS_SOURCES + OPS_HEADERS)
 
 
 def _run(cmd) -> str:
@@ -51,17 +50,22 @@ def _run(cmd) -> str:
     return res.stderr
 
 
-def _build_ops(force: bool, verbose: bool = False) -> str:
-    """The object of the replica operators, compiled when missing or older than its sources."""
-    if force or not os.path.exists(OPS_OBJECT) or any(os.path.getmtime(p) > os.path.getmtime(OPS_OBJECT) for p in [OPS_SOURCE] + OPS_HEADERS):
-        os.makedirs(os.path.dirname(OPS_OBJECT), exist_ok=True)
-        tmp = OPS_OBJECT + f".tmp{os.getpid()}.o"
+def _build_ops(force: bool, verbose: bool = False) -> list:
+    """The objects of the replica operators, each compiled when missing or older than its sources."""
+    objects = []
+    for source in OPS_SOURCES:
+        made = os.path.join(_HERE, "_build", os.path.splitext(os.path.basename(source))[0] + ".o")
+        objects.append(made)
+        if not force and os.path.exists(made) and all(os.path.getmtime(p) <= os.path.getmtime(made) for p in [source] + OPS_HEADERS):
+            continue
+        os.makedirs(os.path.dirname(made), exist_ok=True)
+        tmp = made + f".tmp{os.getpid()}.o"
         flags = [f for f in NVCC_FLAGS if f != "-shared"] + (["-Xptxas", "-v"] if verbose else [])
-        log = _run([_nvcc()] + flags + ["-c", "-o", tmp, OPS_SOURCE])
+        log = _run([_nvcc()] + flags + ["-c", "-o", tmp, source])
         if verbose:
             print(log)
-        os.replace(tmp, OPS_OBJECT)
-    return OPS_OBJECT
+        os.replace(tmp, made)
+    return objects
 
 
 def build_marshal(force: bool = False) -> str:
@@ -81,7 +85,7 @@ def build_marshal(force: bool = False) -> str:
 def _build_variant(path: str, define: str, force: bool) -> str:
     if force or is_stale(path):
         tmp = path + f".tmp{os.getpid()}"
-        _run([_nvcc()] + NVCC_FLAGS + [define, "-o", tmp] + SOURCES + [_build_ops(False)])
+        _run([_nvcc()] + NVCC_FLAGS + [define, "-o", tmp] + SOURCES + _build_ops(False))
         os.replace(tmp, path)
     return path
 
@@ -97,7 +101,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
     if force or is_stale():
         tmp = LIB_PATH + f".tmp{os.getpid()}"
         ops = _build_ops(force, verbose)
-        log = _run([_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES + [ops])
+        log = _run([_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES + ops)
         if verbose:
             print(log)
         os.replace(tmp, LIB_PATH)

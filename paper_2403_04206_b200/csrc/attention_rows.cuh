@@ -1,0 +1,206 @@
+// Attention within a window, row by row: what a query sees, and a warp's way from one row of the operands to one row of the
+// results, in fp32 throughout.
+//
+// Sequences lie behind each other in a worker's rows.  Query i of the sequence [start, end) sees key j of the same sequence
+// when  j <= i + right  and  (j >= i - left  or  j < start + sinks).  So a query's keys are one run of rows and some of the
+// sequence's first ones, and a key's queries are one run of rows:
+//   keys of i     [lo, hi] and [start, sinks_end),  lo = max(start, i - left), hi = min(end - 1, i + right), sinks_end <= lo
+//   queries of j  [lo, hi],  lo = max(start, j - right), hi = end - 1 for a first key, else min(end - 1, j + left)
+//
+//   forward   S_ij = scale q_i k_j,  lse_i = log sum_j exp S_ij,  P_ij = exp(S_ij - lse_i),  out_i = sum_j P_ij v_j
+//   backward  delta_i = dout_i out_i,  dS_ij = P_ij (dout_i v_j - delta_i),
+//             dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+// (k_j and v_j of a head are those of key head  head / (heads / kv_heads); a key's sums run over all of its query heads).
+#pragma once
+#include "replica_common.cuh"
+
+namespace grawa {
+namespace replica {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttentionArgs {
+    In q, k, v, dout, out, lse;             // dout, out (as stored by the forward call) and lse in the backward pass
+    Out to[3];                              // forward: out, lse (may be NULL); backward: dq, dk, dv
+    In offsets;                             // 64-bit integers, or NULL: sequences of `period` rows
+    long long q_stride, k_stride, v_stride, out_stride;      // elements from row to row; dq has q's, dk k's, dv v's, dout out's
+    int rows, heads, kv_heads, group, dim;  // group: query heads of a key head
+    int sequences, period;
+    int left, right, sinks;                 // each at most `rows`
+    float scale;
+};
+
+struct Sequence { int start, end; };        // start > end - 1: the row belongs to none
+
+// The sequence of a row.  Offsets that decrease or leave the rows give some run of rows that holds this one.
+__device__ __forceinline__ Sequence sequence_of(const AttentionArgs& a, int m, int row)
+{
+    const long long* offsets = static_cast<const long long*>(a.offsets.p[m]);
+    if (offsets == nullptr) {
+        const int start = row - row % a.period;
+        return {start, a.period > a.rows - start ? a.rows : start + a.period};
+    }
+    if (row >= a.rows || offsets[0] > row || offsets[a.sequences] <= row) return {0, 0};
+    int lo = 0, hi = a.sequences;           // offsets[lo] <= row < offsets[hi]
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (offsets[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    const long long start = offsets[lo], end = offsets[hi];
+    return {start < 0 ? 0 : static_cast<int>(start), end > a.rows ? a.rows : static_cast<int>(end)};
+}
+
+struct Keys { int lo, hi, start, sinks_end; };
+__device__ __forceinline__ Keys keys_of(const AttentionArgs& a, const Sequence& s, int i)
+{
+    Keys k;
+    k.start = s.start;
+    k.lo = a.left >= i - s.start ? s.start : i - a.left;
+    k.hi = a.right >= s.end - 1 - i ? s.end - 1 : i + a.right;
+    k.sinks_end = a.sinks >= k.lo - s.start ? k.lo : s.start + a.sinks;
+    return k;
+}
+struct Queries { int lo, hi; };
+__device__ __forceinline__ Queries queries_of(const AttentionArgs& a, const Sequence& s, int j)
+{
+    const bool first = j - s.start < a.sinks;
+    return {a.right >= j - s.start ? s.start : j - a.right, first || a.left >= s.end - 1 - j ? s.end - 1 : j + a.left};
+}
+
+// ------------------------------------------------------------------ a warp's rows
+
+// Lane l holds elements 4 l to 4 l + 3 of a row of up to 128 (a multiple of 8).
+template <typename T>
+__device__ __forceinline__ void load_row(const void* base, long long stride, int row, int head, int dim, float (&x)[4])
+{
+    const int at = threadIdx.x % 32 * 4;
+    if (at < dim) {
+        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const T*>(base) + row * stride + static_cast<long long>(head) * dim + at);
+        unpack_pair(w.x, x, T{});
+        unpack_pair(w.y, x + 2, T{});
+    } else {
+        x[0] = x[1] = x[2] = x[3] = 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_row(void* base, long long stride, int row, int head, int dim, const float (&x)[4])
+{
+    const int at = threadIdx.x % 32 * 4;
+    if (at < dim)
+        *reinterpret_cast<uint2*>(static_cast<T*>(base) + row * stride + static_cast<long long>(head) * dim + at) =
+            make_uint2(pack_pair(x[0], x[1], T{}), pack_pair(x[2], x[3], T{}));
+}
+__device__ __forceinline__ float dot_row(const float (&x)[4], const float (&y)[4])
+{
+    return lanes_sum<32>(fmaf(x[0], y[0], fmaf(x[1], y[1], fmaf(x[2], y[2], x[3] * y[3]))));
+}
+__device__ __forceinline__ void add_row(float (&x)[4], float f, const float (&y)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[e], x[e]);
+}
+
+template <typename T>
+__device__ __noinline__ void attention_row(const AttentionArgs& a, int m, int h, int i)
+{
+    const Keys keys = keys_of(a, sequence_of(a, m, i), i);
+    const float c = a.scale * kLog2e;
+    float q[4], o[4] = {}, top = -INFINITY, total = 0.0f;
+    load_row<T>(a.q.p[m], a.q_stride, i, h, a.dim, q);
+    for (int part = 0; part < 2; ++part)
+        for (int j = part ? keys.lo : keys.start, end = part ? keys.hi + 1 : keys.sinks_end; j < end; ++j) {
+            float k[4], v[4];
+            load_row<T>(a.k.p[m], a.k_stride, j, h / a.group, a.dim, k);
+            load_row<T>(a.v.p[m], a.v_stride, j, h / a.group, a.dim, v);
+            const float s = dot_row(q, k) * c, next = fmaxf(top, s), ref = next == -INFINITY ? 0.0f : next;
+            const float f = exp2f(top - ref), p = exp2f(s - ref);
+            total = fmaf(total, f, p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(p, v[e], o[e] * f);
+            top = next;
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] /= total;
+    store_row<T>(a.to[0].p[m], a.out_stride, i, h, a.dim, o);
+    if (a.to[1].p[m] && threadIdx.x % 32 == 0) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + i] = (top + log2f(total)) * kLn2;
+}
+
+template <typename T>
+__device__ __forceinline__ float delta_of(const AttentionArgs& a, int m, int h, int i, const float (&dout)[4])
+{
+    float out[4];
+    load_row<T>(a.out.p[m], a.out_stride, i, h, a.dim, out);
+    return dot_row(dout, out);
+}
+__device__ __forceinline__ float lse_of(const AttentionArgs& a, int m, int h, int i)
+{
+    return static_cast<const float*>(a.lse.p[m])[static_cast<long long>(h) * a.rows + i] * kLog2e;
+}
+
+template <typename T>
+__device__ __noinline__ void attention_query_grad_row(const AttentionArgs& a, int m, int h, int i)
+{
+    const Keys keys = keys_of(a, sequence_of(a, m, i), i);
+    const float c = a.scale * kLog2e, lse = lse_of(a, m, h, i);
+    float q[4], dout[4], dq[4] = {};
+    load_row<T>(a.q.p[m], a.q_stride, i, h, a.dim, q);
+    load_row<T>(a.dout.p[m], a.out_stride, i, h, a.dim, dout);
+    const float delta = delta_of<T>(a, m, h, i, dout);
+    for (int part = 0; part < 2; ++part)
+        for (int j = part ? keys.lo : keys.start, end = part ? keys.hi + 1 : keys.sinks_end; j < end; ++j) {
+            float k[4], v[4];
+            load_row<T>(a.k.p[m], a.k_stride, j, h / a.group, a.dim, k);
+            load_row<T>(a.v.p[m], a.v_stride, j, h / a.group, a.dim, v);
+            add_row(dq, exp2f(dot_row(q, k) * c - lse) * (dot_row(dout, v) - delta), k);
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dq[e] *= a.scale;
+    store_row<T>(a.to[0].p[m], a.q_stride, i, h, a.dim, dq);
+}
+
+// dk and dv of a key, or (where the flag is false) not that one.
+template <typename T>
+__device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int m, int kv, int j, bool want_k, bool want_v)
+{
+    const Queries queries = queries_of(a, sequence_of(a, m, j), j);
+    const float c = a.scale * kLog2e;
+    float k[4], v[4], dk[4] = {}, dv[4] = {};
+    load_row<T>(a.k.p[m], a.k_stride, j, kv, a.dim, k);
+    load_row<T>(a.v.p[m], a.v_stride, j, kv, a.dim, v);
+    for (int h = kv * a.group; h < (kv + 1) * a.group; ++h)
+        for (int i = queries.lo; i <= queries.hi; ++i) {
+            float q[4], dout[4];
+            load_row<T>(a.q.p[m], a.q_stride, i, h, a.dim, q);
+            load_row<T>(a.dout.p[m], a.out_stride, i, h, a.dim, dout);
+            const float p = exp2f(dot_row(q, k) * c - lse_of(a, m, h, i));
+            add_row(dv, p, dout);
+            if (want_k) add_row(dk, p * (dot_row(dout, v) - delta_of<T>(a, m, h, i, dout)), q);
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dk[e] *= a.scale;
+    if (want_k) store_row<T>(a.to[1].p[m], a.k_stride, j, kv, a.dim, dk);
+    if (want_v) store_row<T>(a.to[2].p[m], a.v_stride, j, kv, a.dim, dv);
+}
+
+// ------------------------------------------------------------------ one warp a row
+
+constexpr int kRowThreads = 128;
+enum RowPass { kRowForward = 0, kRowQueryGrad = 1, kRowKeyGrad = 2 };
+
+template <typename T, int PASS>
+__global__ void __launch_bounds__(kRowThreads)
+attention_rows_kernel(const __grid_constant__ AttentionArgs a)
+{
+    stream_order();
+    const int row = blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32, h = blockIdx.y, m = blockIdx.z;
+    if (row >= a.rows) return;
+    const Sequence s = sequence_of(a, m, row);
+    if (s.start >= s.end) return;
+    if constexpr (PASS == kRowForward) attention_row<T>(a, m, h, row);
+    else if constexpr (PASS == kRowQueryGrad) attention_query_grad_row<T>(a, m, h, row);
+    else attention_key_grad_row<T>(a, m, h, row, true, true);
+}
+
+}  // namespace replica
+}  // namespace grawa

@@ -1,0 +1,381 @@
+// Norms of the query and key heads with the rotation by position, of all M workers in one call, and their gradients.
+//
+//   forward   s = 1 / sqrt(mean x^2 + eps) over a head's elements, z = w x s, y = R z
+//   backward  dz = R^T dy, dw = sum over rows and heads of dz x s, g = dz w, dx = s (g - x s mean(g x s))
+//
+// R turns the leading `2 half` elements in pairs, pair i by the angle position * frequency[i].  The angle is taken and
+// reduced to a fraction of a turn in 64 bits: in 32, a position of a million leaves 0.06 radians of error.
+//
+// One pass: a head lies in the registers of a few neighbouring lanes, which hold both elements of each pair, so that the
+// rotation exchanges nothing and a sum of squares is a few shuffles.  A warp takes one row after the other, works its
+// angles out once (a pair's sine and cosine in one lane, shared through shared memory), and uses them for all of the row's
+// query and key heads.  Bound by memory: forward reads and writes each element once, backward reads two and writes one.
+#pragma once
+#include "replica_common.cuh"
+
+namespace grawa {
+namespace replica {
+
+// How a lane holds its share of a head, in two runs a[] and b[] of n elements:
+//   kPairWords  words a and b are word j and the word `half` elements behind it: pairs of halves, (a[e], b[e]);
+//               lanes behind the rotated part hold two neighbouring words
+//   kPairNext   two neighbouring words: pairs of neighbours, (a[2i], a[2i + 1]) and (b[2i], b[2i + 1])
+//   kPairAny    single elements, at any address and of any number: pair lane + 32 t for t < 4, then what is not rotated
+enum HeadMode { kPairWords = 0, kPairNext = 1, kPairAny = 2 };
+constexpr int kHeadDim = 256;               // largest head
+constexpr int kHeadThreads = 256;
+
+struct HeadArgs {
+    In x[2], w[2], dy[2];                   // queries, keys; w may be NULL (1); dy in the backward pass
+    Out y[2];                               // forward: results; backward: dx
+    Out dw[2];                              // backward
+    In positions;                           // 64-bit integers, or NULL: row number modulo `period`
+    const double* frequencies;
+    float* partial;                         // backward, parts > 1: [worker][part][2][kHeadDim]
+    long long rows, period;
+    long long x_stride[2], y_stride[2];     // backward: of x and dx, and of dy
+    int heads[2];
+    int dim, half, neighbours, words;       // words: of a head (kPairWords, kPairNext)
+    int chunks, per_chunk;                  // forward: a row's groups of heads are shared out among so many warps
+    int parts;                              // backward: CTAs a worker
+    int has_w[2], has_dw[2], has_dx[2], accumulate;
+    float eps, inv_dim;
+};
+
+template <typename T, int MODE> constexpr int kHeadRun = MODE == kPairAny ? 8 : kWordElems<T>;
+
+// The places of a lane's elements in a head, and their loads and stores.
+template <typename T, int MODE>
+struct HeadLane {
+    static constexpr int N = kHeadRun<T, MODE>;
+    int first[2];                           // words: of a[] and b[]; kPairAny: unused
+    int dim, half, neighbours, lane;
+    bool has[2];
+
+    __device__ __forceinline__ HeadLane(const HeadArgs& a, int l) : dim(a.dim), half(a.half), neighbours(a.neighbours), lane(l)
+    {
+        if constexpr (MODE == kPairWords) {
+            const int turned = a.half / N;
+            first[0] = l < turned ? l : 2 * turned + 2 * (l - turned);
+            first[1] = l < turned ? l + turned : first[0] + 1;
+        } else {
+            first[0] = 2 * l;
+            first[1] = 2 * l + 1;
+        }
+        has[0] = MODE == kPairAny || first[0] < a.words;
+        has[1] = MODE == kPairAny || first[1] < a.words;
+    }
+    // kPairAny: the place of element t of a[] (which = 0) or b[], or -1.
+    __device__ __forceinline__ int place(int t, int which) const
+    {
+        if (t < 4) {
+            const int p = lane + 32 * t;
+            return p >= half ? -1 : neighbours ? 2 * p + which : p + which * half;
+        }
+        const int e = 2 * half + lane + 32 * (2 * (t - 4) + which);
+        return e < dim ? e : -1;
+    }
+    __device__ __forceinline__ void load(const T* head, float (&a)[N], float (&b)[N]) const
+    {
+        if constexpr (MODE == kPairAny) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const int i = place(t, 0), j = place(t, 1);
+                a[t] = i >= 0 ? widen(head[i]) : 0.0f;
+                b[t] = j >= 0 ? widen(head[j]) : 0.0f;
+            }
+        } else {
+            const uint4* w = reinterpret_cast<const uint4*>(head);
+            unpack<T>(has[0] ? w[first[0]] : make_uint4(0, 0, 0, 0), a);
+            unpack<T>(has[1] ? w[first[1]] : make_uint4(0, 0, 0, 0), b);
+        }
+    }
+    __device__ __forceinline__ void store(T* head, const float (&a)[N], const float (&b)[N]) const
+    {
+        if constexpr (MODE == kPairAny) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const int i = place(t, 0), j = place(t, 1);
+                if (i >= 0) head[i] = narrow<T>(a[t]);
+                if (j >= 0) head[j] = narrow<T>(b[t]);
+            }
+        } else {
+            uint4* w = reinterpret_cast<uint4*>(head);
+            if (has[0]) w[first[0]] = pack<T>(a);
+            if (has[1]) w[first[1]] = pack<T>(b);
+        }
+    }
+    // The same places of a vector of kHeadDim floats in shared memory (what lies behind the head's end is not used).
+    __device__ __forceinline__ void from_shared(const float* v, float (&a)[N], float (&b)[N]) const
+    {
+        if constexpr (MODE == kPairAny) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const int i = place(t, 0), j = place(t, 1);
+                a[t] = i >= 0 ? v[i] : 0.0f;
+                b[t] = j >= 0 ? v[j] : 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; e += 4) {
+                const float4 x = has[0] ? *reinterpret_cast<const float4*>(v + first[0] * N + e) : make_float4(0, 0, 0, 0);
+                const float4 y = has[1] ? *reinterpret_cast<const float4*>(v + first[1] * N + e) : make_float4(0, 0, 0, 0);
+                a[e] = x.x; a[e + 1] = x.y; a[e + 2] = x.z; a[e + 3] = x.w;
+                b[e] = y.x; b[e + 1] = y.y; b[e + 2] = y.z; b[e + 3] = y.w;
+            }
+        }
+    }
+    __device__ __forceinline__ void to_shared(float* v, const float (&a)[N], const float (&b)[N]) const
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int i = MODE == kPairAny ? place(e, 0) : has[0] ? first[0] * N + e : -1;
+            const int j = MODE == kPairAny ? place(e, 1) : has[1] ? first[1] * N + e : -1;
+            if (i >= 0) v[i] = a[e];
+            if (j >= 0) v[j] = b[e];
+        }
+    }
+    // Cosine and sine of the lane's N pairs from the warp's table (1 and 0 where nothing turns).
+    __device__ __forceinline__ void angles(const float2* table, float (&c)[N], float (&s)[N]) const
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            int p;
+            if constexpr (MODE == kPairAny) p = e < 4 ? lane + 32 * e : half;
+            else if constexpr (MODE == kPairWords) p = first[0] * N + e;
+            else p = first[e * 2 / N] * (N / 2) + e % (N / 2);
+            const float2 t = p < half ? table[p] : make_float2(1.0f, 0.0f);
+            c[e] = t.x;
+            s[e] = t.y;
+        }
+    }
+    // The pairs turned by their angles, or back (sign -1).
+    static __device__ __forceinline__ void turn(float (&a)[N], float (&b)[N], const float (&c)[N], const float (&s)[N], float sign)
+    {
+        if constexpr (MODE == kPairNext) {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float x = a[2 * i], y = a[2 * i + 1], u = b[2 * i], v = b[2 * i + 1], sx = sign * s[i], su = sign * s[N / 2 + i];
+                a[2 * i] = x * c[i] - y * sx;
+                a[2 * i + 1] = y * c[i] + x * sx;
+                b[2 * i] = u * c[N / 2 + i] - v * su;
+                b[2 * i + 1] = v * c[N / 2 + i] + u * su;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = a[e], y = b[e], t = sign * s[e];
+                a[e] = x * c[e] - y * t;
+                b[e] = y * c[e] + x * t;
+            }
+        }
+    }
+};
+
+// Cosine and sine of a row's pairs into the warp's table.
+__device__ __forceinline__ void fill_angles(const HeadArgs& a, int m, long long row, int lane, float2* table)
+{
+    const long long* given = static_cast<const long long*>(a.positions.p[m]);
+    const double position = static_cast<double>(given ? given[row] : row % a.period);
+    __syncwarp();                                             // the row in front has been read
+    for (int p = lane; p < a.half; p += 32) {
+        const double turns = position * a.frequencies[p] * 0.15915494309189533577;       // 1 / (2 pi)
+        float s, c;
+        sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s, &c);
+        table[p] = make_float2(c, s);
+    }
+    __syncwarp();
+}
+
+template <typename T>
+__device__ __forceinline__ void load_weights(const HeadArgs& a, int which, int m, float* to)
+{
+    const T* w = static_cast<const T*>(a.w[which].p[m]);
+    for (int e = threadIdx.x; e < a.dim; e += kHeadThreads) to[e] = a.has_w[which] ? widen(w[e]) : 1.0f;
+}
+
+// LPH: lanes a head.  A unit of work is a chunk of a row's heads.
+template <typename T, int LPH, int MODE>
+__global__ void __launch_bounds__(kHeadThreads)
+head_rotary_forward_kernel(const __grid_constant__ HeadArgs a)
+{
+    constexpr int N = kHeadRun<T, MODE>, kPer = 32 / LPH, kWarps = kHeadThreads / 32;
+    __shared__ __align__(16) float weights[2][kHeadDim];
+    __shared__ float2 tables[kWarps][kHeadDim / 2];
+    stream_order();
+    const int m = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32, slot = lane / LPH;
+    const HeadLane<T, MODE> at(a, lane % LPH);
+    load_weights<T>(a, 0, m, weights[0]);
+    if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
+    __syncthreads();
+    const long long units = a.rows * a.chunks;
+    for (long long u = static_cast<long long>(blockIdx.x) * kWarps + warp; u < units; u += static_cast<long long>(gridDim.x) * kWarps) {
+        const long long row = u / a.chunks;
+        const int begin = static_cast<int>(u % a.chunks) * a.per_chunk, end = min(begin + a.per_chunk, a.heads[0] + a.heads[1]);
+        fill_angles(a, m, row, lane, tables[warp]);
+        float c[N], s[N];
+        at.angles(tables[warp], c, s);
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            const int from = which ? max(begin, a.heads[0]) - a.heads[0] : begin, to = which ? end - a.heads[0] : min(end, a.heads[0]);
+            if (from >= to) continue;
+            float wa[N], wb[N];
+            at.from_shared(weights[which], wa, wb);
+            const T* in = static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which];
+            T* out = static_cast<T*>(a.y[which].p[m]) + row * a.y_stride[which];
+#pragma unroll 2
+            for (int h0 = from; h0 < to; h0 += kPer) {
+                const int h = h0 + slot;
+                const bool mine = h < to;
+                float x[N], y[N], sum = 0.0f;
+                if (mine) at.load(in + static_cast<long long>(h) * a.dim, x, y);
+                else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = y[e] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
+                const float r = rsqrtf(fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps));
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    x[e] = x[e] * r * wa[e];
+                    y[e] = y[e] * r * wb[e];
+                }
+                at.turn(x, y, c, s, 1.0f);
+                if (mine) at.store(out + static_cast<long long>(h) * a.dim, x, y);
+            }
+        }
+    }
+}
+
+// The sums over a CTA of what its lanes hold for each element of a weight, in a fixed order, into kHeadDim floats.
+template <typename T, int LPH, int MODE>
+__device__ __forceinline__ void sum_weights(const HeadLane<T, MODE>& at, float (&da)[kHeadRun<T, MODE>], float (&db)[kHeadRun<T, MODE>], float* shared, float* to,
+                                            int dim)
+{
+    constexpr int N = kHeadRun<T, MODE>, kWarps = kHeadThreads / 32;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+#pragma unroll
+        for (int d = LPH; d < 32; d *= 2) {
+            da[e] += __shfl_xor_sync(0xffffffffu, da[e], d);
+            db[e] += __shfl_xor_sync(0xffffffffu, db[e], d);
+        }
+    __syncthreads();
+    if (threadIdx.x % 32 < LPH) at.to_shared(shared + threadIdx.x / 32 * kHeadDim, da, db);
+    __syncthreads();
+    for (int e = threadIdx.x; e < dim; e += kHeadThreads) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += shared[w * kHeadDim + e];
+        to[e] = v;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void put_weight(const HeadArgs& a, int which, int m, int e, float v)
+{
+    T* to = static_cast<T*>(a.dw[which].p[m]) + e;
+    *to = narrow<T>(a.accumulate ? widen(*to) + v : v);
+}
+
+template <typename T, int LPH, int MODE>
+__global__ void __launch_bounds__(kHeadThreads, 2)
+head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
+{
+    constexpr int N = kHeadRun<T, MODE>, kPer = 32 / LPH, kWarps = kHeadThreads / 32;
+    __shared__ __align__(16) float weights[2][kHeadDim];
+    __shared__ float2 tables[kWarps][kHeadDim / 2];
+    __shared__ float sums[kWarps * kHeadDim];
+    stream_order();
+    const int m = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32, slot = lane / LPH;
+    const HeadLane<T, MODE> at(a, lane % LPH);
+    load_weights<T>(a, 0, m, weights[0]);
+    if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
+    __syncthreads();
+    float da[2][N] = {}, db[2][N] = {};
+    for (long long row = static_cast<long long>(blockIdx.x) * kWarps + warp; row < a.rows; row += static_cast<long long>(gridDim.x) * kWarps) {
+        fill_angles(a, m, row, lane, tables[warp]);
+        float c[N], s[N];
+        at.angles(tables[warp], c, s);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float wa[N], wb[N];
+            at.from_shared(weights[which], wa, wb);
+            const T* in = static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which];
+            const T* grad = static_cast<const T*>(a.dy[which].p[m]) + row * a.y_stride[which];
+            T* out = static_cast<T*>(a.y[which].p[m]) + row * a.x_stride[which];
+#pragma unroll 1
+            for (int h0 = 0; h0 < a.heads[which]; h0 += kPer) {
+                const int h = h0 + slot;
+                const bool mine = h < a.heads[which];
+                float x[N], y[N], u[N], v[N], square = 0.0f, along = 0.0f;
+                if (mine) {
+                    at.load(in + static_cast<long long>(h) * a.dim, x, y);
+                    at.load(grad + static_cast<long long>(h) * a.dim, u, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = y[e] = u[e] = v[e] = 0.0f;
+                }
+                at.turn(u, v, c, s, -1.0f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));
+                const float r = rsqrtf(fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps));
+#pragma unroll
+                for (int e = 0; e < N; ++e) {                 // x s first: s^2 may be past fp32's range where dx is inside it
+                    x[e] *= r;
+                    y[e] *= r;
+                    da[which][e] = fmaf(u[e], x[e], da[which][e]);
+                    db[which][e] = fmaf(v[e], y[e], db[which][e]);
+                    u[e] *= wa[e];
+                    v[e] *= wb[e];
+                    along = fmaf(u[e], x[e], fmaf(v[e], y[e], along));
+                }
+                along = lanes_sum<LPH>(along) * a.inv_dim;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    u[e] = (u[e] - x[e] * along) * r;
+                    v[e] = (v[e] - y[e] * along) * r;
+                }
+                if (mine && a.has_dx[which]) at.store(out + static_cast<long long>(h) * a.dim, u, v);
+            }
+        }
+    }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (!a.has_dw[which]) continue;
+        if (a.parts > 1) {
+            sum_weights<T, LPH, MODE>(at, da[which], db[which], sums, a.partial + ((static_cast<size_t>(m) * a.parts + blockIdx.x) * 2 + which) * kHeadDim, a.dim);
+        } else {
+            sum_weights<T, LPH, MODE>(at, da[which], db[which], sums, weights[which], a.dim);
+            for (int e = threadIdx.x; e < a.dim; e += kHeadThreads) put_weight<T>(a, which, m, e, weights[which][e]);     // its own sums
+        }
+    }
+}
+
+// The parts' sums, added in their order: 32 elements a CTA, kHeadGroups runs of parts side by side.
+constexpr int kHeadGroups = 16;
+template <typename T>
+__global__ void __launch_bounds__(32 * kHeadGroups)
+head_rotary_finish_kernel(const __grid_constant__ HeadArgs a)
+{
+    __shared__ float sums[kHeadGroups][32];
+    stream_order();
+    const int m = blockIdx.y, which = blockIdx.z, lane = threadIdx.x % 32, group = threadIdx.x / 32, e = blockIdx.x * 32 + lane;
+    if (!a.has_dw[which]) return;
+    const int run = (a.parts + kHeadGroups - 1) / kHeadGroups, last = min(a.parts, (group + 1) * run);
+    float v = 0.0f;
+    if (e < a.dim)
+#pragma unroll 4
+        for (int p = group * run; p < last; ++p) v += a.partial[((static_cast<size_t>(m) * a.parts + p) * 2 + which) * kHeadDim + e];
+    sums[group][lane] = v;
+    __syncthreads();
+    if (group || e >= a.dim) return;
+    v = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kHeadGroups; ++g) v += sums[g][lane];
+    put_weight<T>(a, which, m, e, v);
+}
+
+}  // namespace replica
+}  // namespace grawa

@@ -20,7 +20,7 @@ constexpr int kMaxWorkers = 64, kMaxTables = 12;
 struct GiveBack { void operator()(PyObject* o) const { Py_DECREF(o); } };
 using Ref = std::unique_ptr<PyObject, GiveBack>;
 
-enum Mode { kRows = 1, kOptional = 2, kFloat32 = 4 };
+enum Mode { kRows = 1, kOptional = 2, kFloat32 = 4, kInt64 = 8, kHeadDimShift = 8 };
 
 bool fail(PyObject* type, const char* name, const std::string& text)
 {
@@ -31,7 +31,8 @@ bool fail(PyObject* type, const char* name, const std::string& text)
 // One table: (name, tensors or None, rows, cols, mode).  mode kRows: 2-D tensors [rows, cols] whose rows may be
 // padded, all with one row stride; else contiguous tensors of rows * cols elements, whose stride is given as 0: matrices
 // [rows, cols] (a transposed one has as many elements, in another order), or, where cols is 1 or the tensor is no
-// matrix, any that hold as many.  Below the stride, in the lowest 4 bits of *layout: the bits below 16 that any of the
+// matrix, any that hold as many.  With a head dimension d in the mode's upper bits (and kRows), 3-D tensors
+// [rows, cols / d, d] whose heads lie behind each other.  Below the stride, in the lowest 4 bits of *layout: the bits below 16 that any of the
 // addresses has.  *table: bytes, or the integer 0 for None.
 bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int device, PyObject** table, int64_t* layout)
 {
@@ -55,6 +56,8 @@ bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int devi
     if (PySequence_Fast_GET_SIZE(list) != workers)
         ok = fail(PyExc_ValueError, name, "one entry per worker is needed (" + std::to_string(workers) + "), got " + std::to_string(PySequence_Fast_GET_SIZE(list)));
     if (mode & kFloat32) kind = at::kFloat;
+    if (mode & kInt64) kind = at::kLong;
+    const int64_t dim = mode >> kHeadDimShift;
     for (Py_ssize_t m = 0; ok && m < workers; ++m) {
         PyObject* item = PySequence_Fast_GET_ITEM(list, m);
         if (!THPVariable_Check(item)) { ok = fail(PyExc_TypeError, name, "expected tensors"); break; }
@@ -65,11 +68,15 @@ bool one_table(PyObject* spec, Py_ssize_t workers, at::ScalarType kind, int devi
             break;
         }
         if (mode & kRows) {
-            if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols) {
-                ok = fail(PyExc_ValueError, name, "expected shape [" + std::to_string(rows) + ", " + std::to_string(cols) + "]");
+            if (dim ? t.dim() != 3 || t.size(0) != rows || t.size(1) != cols / dim || t.size(2) != dim : t.dim() != 2 || t.size(0) != rows || t.size(1) != cols) {
+                ok = fail(PyExc_ValueError, name, "expected shape [" + std::to_string(rows) + ", " +
+                          (dim ? std::to_string(cols / dim) + ", " + std::to_string(dim) : std::to_string(cols)) + "]");
                 break;
             }
-            if (cols > 1 && t.stride(1) != 1) { ok = fail(PyExc_ValueError, name, "the elements of a row must be contiguous"); break; }
+            if (dim ? (dim > 1 && t.stride(2) != 1) || (cols > dim && t.stride(1) != dim) : cols > 1 && t.stride(1) != 1) {
+                ok = fail(PyExc_ValueError, name, "the elements of a row must be contiguous");
+                break;
+            }
             if (rows > 1) {                                   // of a single row the stride says nothing
                 if (m > 0 && t.stride(0) != stride) { ok = fail(PyExc_ValueError, name, "all workers need one row stride"); break; }
                 stride = t.stride(0);

@@ -2,6 +2,8 @@
 #pragma once
 #include "host_common.h"
 
+#include <cudaTypedefs.h>
+
 #include <algorithm>
 #include <cstdint>
 
@@ -19,7 +21,7 @@ inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintp
 // between each other are taken for one.)
 class Buffers {
 public:
-    static constexpr int kMost = 10 * GRAWA_MAX_WORKERS;
+    static constexpr int kMost = 12 * GRAWA_MAX_WORKERS;
 
     // false: a NULL entry, or one that is not aligned to its element size
     bool add(const void* const* table, int M, int64_t rows, int64_t cols, int64_t stride, int64_t elem, bool output)
@@ -54,6 +56,22 @@ private:
     Item item_[kMost];
     int count_ = 0;
 };
+
+template <typename P, typename S>
+inline void copy_table(P& to, S* const* from, int M)
+{
+    for (int m = 0; m < M; ++m) to.p[m] = const_cast<void*>(static_cast<const void*>(from ? from[m] : nullptr));
+}
+
+inline bool all_aligned(const void* const* table, int M, size_t bytes)
+{
+    bool ok = true;
+    for (int m = 0; m < M && table; ++m) ok = ok && aligned(table[m], bytes);
+    return ok;
+}
+
+// The driver's encoder of tensor maps.
+grawa_status map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out);
 
 // One launch over grid (gx, gy, gz), in clusters of `cluster` CTAs along x.  `overlap`, with the "dependent_launch" option:
 // its launch may overlap the end of the kernel in front of it on the stream, whose results it waits for by itself

@@ -1,7 +1,5 @@
 // Host side of the replica operators: argument checks, the choice of a kernel, launches, and their part of
 // the C ABI in include/grawa.h.  No call allocates device memory or keeps anything from one call to the next.
-#include <cudaTypedefs.h>
-
 #include <cmath>
 #include <cstring>
 #include <map>
@@ -16,19 +14,6 @@
 
 namespace grawa {
 namespace replica {
-
-template <typename P, typename S>
-static void copy_table(P& to, S* const* from, int M)
-{
-    for (int m = 0; m < M; ++m) to.p[m] = const_cast<void*>(static_cast<const void*>(from ? from[m] : nullptr));
-}
-
-static bool all_aligned(const void* const* table, int M, size_t bytes)
-{
-    bool ok = true;
-    for (int m = 0; m < M && table; ++m) ok = ok && aligned(table[m], bytes);
-    return ok;
-}
 
 // ------------------------------------------------------------------ dropout
 
@@ -258,7 +243,7 @@ static grawa_status norm_forward(const NormForwardArgs& a, int M, RowMode mode, 
 // ------------------------------------------------------------------ gated feed-forward product
 
 // The driver's encoder of tensor maps, looked up once through the runtime (the library does not link the driver).
-static grawa_status map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out)
+grawa_status map_encoder(PFN_cuTensorMapEncodeTiled_v12000* out)
 {
     static const auto found = [] {
         void* fn = nullptr;
