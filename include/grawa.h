@@ -43,9 +43,9 @@
  *     gradients) gives that worker weight 0, the rest are normalised among themselves (uniform
  *     1/M if none is finite), and the step's status word is set; see grawa_last_step_status.
  *   - Errors detectable on the host return a negative code before anything is enqueued.
- *     Nothing on the device traps.  The only device-side waits are the bulk-copy kernel's and the gated
- *     feed-forward product's waits for their own copies and products; each is bounded and reports
- *     GRAWA_ERR_TIMEOUT instead of hanging.
+ *     Nothing on the device traps.  The only device-side waits are the bulk-copy kernel's, the gated
+ *     feed-forward product's and the attention kernels' waits for their own copies and products; each is
+ *     bounded and reports GRAWA_ERR_TIMEOUT instead of hanging.
  *   - A plan (and its device memory) lives until grawa_clear_plans(); a program that meets many
  *     different shapes or streams should call it now and then.  Steps that share a plan (same
  *     device, stream, shape) must not overlap on the GPU; the stream order guarantees that.
@@ -461,6 +461,10 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void *cons
 
 /* 0 on invalid arguments. */
 size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int M);
+
+/* As grawa_gated_ffn_status and grawa_selftest_gated_ffn_wait, for the attention calls: their kernels' bounded waits. */
+grawa_status grawa_window_attention_status(grawa_stream_t stream);
+grawa_status grawa_selftest_window_attention_wait(grawa_stream_t stream);
 
 /* Largest number of partial sums grawa_sumsq_static can hold: M * ceil(n / 16384) must not
  * exceed it (for example M = 16 workers of up to 134 million elements each). */

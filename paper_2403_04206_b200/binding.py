@@ -137,6 +137,10 @@ def library() -> ctypes.CDLL:
     lib.grawa_window_attention_backward.restype = ci
     lib.grawa_window_attention_backward_workspace_bytes.argtypes = [i64, i64, ci]
     lib.grawa_window_attention_backward_workspace_bytes.restype = sz
+    lib.grawa_window_attention_status.argtypes = [vp]
+    lib.grawa_window_attention_status.restype = ci
+    lib.grawa_selftest_window_attention_wait.argtypes = [vp]
+    lib.grawa_selftest_window_attention_wait.restype = ci
     _lib = lib
     return lib
 
@@ -767,6 +771,16 @@ def grawa_window_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, *, offs
 
 def grawa_window_attention_backward_workspace_bytes(rows: int, q_heads: int, M: int) -> int:
     return int(library().grawa_window_attention_backward_workspace_bytes(rows, q_heads, M))
+
+
+def grawa_window_attention_status(stream=None) -> int:
+    """Synchronises the stream and returns 0, or -5 when a bounded wait of an attention call ran out."""
+    return int(library().grawa_window_attention_status(_stream(stream)))
+
+
+def grawa_selftest_window_attention_wait(*, stream=None) -> None:
+    """Launches the attention kernel's bounded-wait self-test; grawa_window_attention_status then reports -5."""
+    _raise(library().grawa_selftest_window_attention_wait(_stream(stream)), "grawa_selftest_window_attention_wait")
 
 
 def grawa_workspace_bytes(n: int, M: int, layer_offsets=None) -> int:

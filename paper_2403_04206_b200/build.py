@@ -15,9 +15,9 @@ SOURCES = [os.path.join(CSRC, "grawa.cu")]
 HEADERS = [os.path.join(CSRC, "kernels.cuh"), os.path.join(CSRC, "center_pull_bulk.cuh"), os.path.join(CSRC, "kernels_16bit.cuh"), os.path.join(CSRC, "center_pull_staged_any.cuh"),
            os.path.join(CSRC, "host_common.h"), os.path.join(_ROOT, "include", "grawa.h")]
 # The replica operators have no debug or trace code of their own: objects that are linked into every variant.
-OPS_SOURCES = [os.path.join(CSRC, s) for s in ("replica_ops.cu", "attention_ops.cu")]
+OPS_SOURCES = [os.path.join(CSRC, s) for s in ("replica_ops.cu", "head_rotary_ops.cu", "attention_ops.cu")]
 OPS_HEADERS = [os.path.join(CSRC, h) for h in ("replica_common.cuh", "replica_host.h", "tensor_core.cuh", "dropout.cuh", "layernorm.cuh", "gated_ffn.cuh",
-                                               "head_rotary.cuh", "attention_rows.cuh", "host_common.h")] + [os.path.join(_ROOT, "include", "grawa.h")]
+                                               "head_rotary.cuh", "attention_rows.cuh", "attention.cuh", "host_common.h")] + [os.path.join(_ROOT, "include", "grawa.h")]
 
 # The binding's marshaller of pointer tables (a CPython module that reads torch tensors).
 MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
@@ -51,21 +51,25 @@ def _run(cmd) -> str:
 
 
 def _build_ops(force: bool, verbose: bool = False) -> list:
-    """The objects of the replica operators, each compiled when missing or older than its sources."""
-    objects = []
-    for source in OPS_SOURCES:
+    """The objects of the replica operators, each compiled when missing or older than its sources, side by side."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    def one(source):
         made = os.path.join(_HERE, "_build", os.path.splitext(os.path.basename(source))[0] + ".o")
-        objects.append(made)
         if not force and os.path.exists(made) and all(os.path.getmtime(p) <= os.path.getmtime(made) for p in [source] + OPS_HEADERS):
-            continue
+            return made, ""
         os.makedirs(os.path.dirname(made), exist_ok=True)
         tmp = made + f".tmp{os.getpid()}.o"
         flags = [f for f in NVCC_FLAGS if f != "-shared"] + (["-Xptxas", "-v"] if verbose else [])
         log = _run([_nvcc()] + flags + ["-c", "-o", tmp, source])
-        if verbose:
-            print(log)
         os.replace(tmp, made)
-    return objects
+        return made, log
+
+    with ThreadPoolExecutor(len(OPS_SOURCES)) as pool:
+        done = list(pool.map(one, OPS_SOURCES))
+    if verbose:
+        print("".join(log for _, log in done))
+    return [made for made, _ in done]
 
 
 def build_marshal(force: bool = False) -> str:

@@ -1,0 +1,729 @@
+// Attention within a window on the tensor cores (the masks and formulas stand in attention_rows.cuh).
+//
+// Every kernel here gives a CTA 128 rows of one head, a tile, and lets it walk over the rows that the tile's rows see or
+// are seen by, some at a time: the first keys of the sequence that the tile's first row belongs to, then one run of rows (of
+// the tile's other sequences, which begin inside it, all rows lie in that run).  Rows are packed, so a tile may hold the ends of
+// some sequences and the starts of others; the mask of a row is two intervals, which a thread turns into bits where a
+// step is not visible throughout.  One thread fetches operands by TMA, one issues tcgen05.mma, and each thread of the other warps has
+// one row of the tile: its scores come from tensor memory, and what it makes of them goes back there as the next product's
+// operand, so nothing but tiles of q, k, v and dout passes through shared memory.
+//
+//   forward    S = Q K^T, P = exp2(S c - m), O += P V.  m is a row's largest score so far, but is only moved when that grows
+//              by more than 2^8 (P stays below 2^8), so that O, which lies in tensor memory, is rarely scaled.
+//   dq         S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K
+//   dk, dv     S^T = K Q^T, dP^T = V dO^T, dV += P^T dO, dK += dS^T Q, over all query heads of the key head
+//
+// dq and dk, dv are two kernels that both compute the scores: seven products instead of five, but no sum is made by atomics,
+// whose order would change the results.  lse and delta = dout out come from a small kernel in front (two floats a row).
+//
+// A masked element of P and dS is an exact zero.  Where the value it multiplies is not finite the product is NaN all the same, and spoils
+// rows that do not see it: a row with such a result is computed again by its warp alone (attention_rows.cuh).
+//
+// Every wait for a barrier in shared memory is bounded, as in the gated feed-forward product: a wait that runs out is counted
+// in g_attention_timeouts, and the CTA waits (bounded) for its copies and products in flight, frees its tensor memory
+// and returns without storing.
+#pragma once
+#include <cuda.h>
+
+#include "attention_rows.cuh"
+#include "tensor_core.cuh"
+
+namespace grawa {
+namespace replica {
+
+constexpr int kTile = 128;                  // rows of a CTA
+constexpr int kBox = 64;                    // rows, and elements of a row, of one TMA box
+constexpr int kBoxBytes = kBox * kBox * 2;
+constexpr int kAttentionWorkers = 16;       // workers a launch (their tensor maps travel as kernel parameters)
+
+struct TileArgs {
+    AttentionArgs a;
+    CUtensorMap map[4][kAttentionWorkers];  // q, k, v, dout
+    const float *lse, *delta;               // backward: [worker][head][pitch], lse in units of log 2
+    const float* longest;                   // backward, half precision: [worker][2], the squared length of the longest row of dout, of v
+    long long pitch;
+    int first_worker, workers;
+};
+
+__device__ unsigned g_attention_timeouts = 0;   // waits that ran out, never set back
+constexpr unsigned long long kAttentionWaitNs = 2000000000ull, kAttentionStarvedNs = 2000000ull;
+
+// ------------------------------------------------------------------ copies, products, tensor memory
+
+template <unsigned long long LIMIT>
+__device__ __forceinline__ bool tile_wait(unsigned bar, unsigned parity, volatile int* gave_up)
+{
+    return bounded_wait<LIMIT>(bar, parity, gave_up, &g_attention_timeouts);
+}
+__device__ __forceinline__ void arrive_here(unsigned bar) { asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void copy_box(unsigned dst, const CUtensorMap* map, int element, int head, int row, unsigned bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+                 "r"(element), "r"(head), "r"(row), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_floats(unsigned dst, const float* from, unsigned bytes, unsigned bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+// D (+)= A B^T for 16 steps along the sum, A in shared or in tensor memory.
+__device__ __forceinline__ void mma_shared(unsigned d, unsigned long long a, unsigned long long b, unsigned shape, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(shape), "r"(add ? 1u : 0u)
+        : "memory");
+}
+__device__ __forceinline__ void mma_tensor(unsigned d, unsigned a, unsigned long long b, unsigned shape, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(shape), "r"(add ? 1u : 0u)
+        : "memory");
+}
+// Arrives when every product this thread has issued so far is done.
+__device__ __forceinline__ void mma_done(unsigned bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int COLS>
+__device__ __forceinline__ void tensor_alloc(unsigned slot)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "n"(COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <int COLS>
+__device__ __forceinline__ void tensor_free(unsigned tmem)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLS));
+}
+#define GRAWA_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define GRAWA_RW8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+#define GRAWA_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of this warp's 32 lanes: a thread gets 32 neighbouring values of its row, for use after tensor_wait on them.
+__device__ __forceinline__ void tensor_load(unsigned at, unsigned (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : GRAWA_R8(r, 0), GRAWA_R8(r, 8), GRAWA_R8(r, 16), GRAWA_R8(r, 24)
+        : "r"(at));
+}
+__device__ __forceinline__ void tensor_wait(unsigned (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : GRAWA_RW8(r, 0), GRAWA_RW8(r, 8), GRAWA_RW8(r, 16), GRAWA_RW8(r, 24) : : "memory");
+}
+__device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31};" ::GRAWA_W8(r, 0),
+        GRAWA_W8(r, 8), GRAWA_W8(r, 16), GRAWA_W8(r, 24), "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::GRAWA_W8(r, 0), GRAWA_W8(r, 8),
+                 "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Bits [lo, hi] of a word, either end of which may lie outside it.
+__device__ __forceinline__ unsigned bits_between(int lo, int hi)
+{
+    const unsigned up = lo <= 0 ? ~0u : lo > 31 ? 0u : ~0u << lo;
+    const unsigned down = hi >= 31 ? ~0u : hi < 0 ? 0u : ~0u >> (31 - hi);
+    return up & down;
+}
+
+// ------------------------------------------------------------------ a tile's way
+
+// What the rows of a tile see, or are seen by, in all.
+struct Reach { int min_lo, max_lo, min_hi, max_hi, min_start; };
+
+__device__ __forceinline__ void reach_init(Reach& r) { r.min_lo = r.min_hi = r.min_start = 0x7fffffff, r.max_lo = r.max_hi = -1; }
+__device__ __forceinline__ void reach_add(Reach& r, bool valid, int lo, int hi, int start)    // a whole warp
+{
+    const int big = 0x7fffffff;
+    const int a = __reduce_min_sync(0xffffffffu, valid ? lo : big), b = __reduce_max_sync(0xffffffffu, valid ? lo : -1);
+    const int c = __reduce_min_sync(0xffffffffu, valid ? hi : big), d = __reduce_max_sync(0xffffffffu, valid ? hi : -1);
+    const int e = __reduce_min_sync(0xffffffffu, valid ? start : big);
+    if (threadIdx.x % 32 == 0) {
+        atomicMin(&r.min_lo, a), atomicMax(&r.max_lo, b), atomicMin(&r.min_hi, c), atomicMax(&r.max_hi, d);
+        atomicMin(&r.min_start, e);
+    }
+}
+
+// The key rows that a tile of queries walks over, `step` rows at a time.
+struct KeyWalk {
+    int first, main, sink_steps, steps;     // rows of the first step among the first keys, and of the first other one
+    __device__ __forceinline__ KeyWalk(const Reach& r, int sinks, int step)
+    {
+        first = r.min_start;
+        main = r.min_lo;
+        const int end = sinks >= main - first ? main : first + sinks;
+        sink_steps = 0;
+        if (end > first) {
+            if (main - first <= step) main = first;           // one run of rows costs no more
+            else sink_steps = (end - first + step - 1) / step;
+        }
+        steps = r.max_hi >= main ? sink_steps + (r.max_hi - main) / step + 1 : 0;
+    }
+    __device__ __forceinline__ int row(int i, int step) const { return i < sink_steps ? first + i * step : main + (i - sink_steps) * step; }
+};
+// Which of 32 keys from row j on a query sees, in a step that ends in front of row `limit`.
+__device__ __forceinline__ unsigned seen_keys(const Keys& k, int j, int limit)
+{
+    const int hi = min(k.hi, limit - 1);
+    return bits_between(k.lo - j, hi - j) | bits_between(k.start - j, min(k.sinks_end - 1, hi) - j);
+}
+
+// A row of results on its way from tensor memory: `cols` columns at `from` (a multiple of 32), times f, to memory where there are
+// elements; whether all were finite.
+template <typename T>
+__device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T* to, int elements, bool valid)
+{
+    bool fine = true;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 32) {
+        unsigned r[32];
+        tensor_load(from + c, r);
+        tensor_wait(r);
+        float v[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            v[e] = __uint_as_float(r[e]) * f;
+            fine = fine && fabsf(v[e]) <= 3.0e38f;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 8)
+            if (valid && c + e < elements) *reinterpret_cast<uint4*>(to + c + e) = pack<T>(v + e);
+    }
+    return fine;
+}
+
+// ------------------------------------------------------------------ forward
+
+// DP: elements of a head as the products take them, 64 or 128 (what lies behind the head's end is zero).  Two CTAs an SM, so
+// that the scores' products of one run beside the exponentials of the other.
+constexpr int kForwardThreads = 192;        // warps 0 to 3: rows, 4: copies, 5: products
+template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 5;
+template <int DP> constexpr int kForwardSmem = (1 + kForwardStages<DP>) * kTile * DP * 2 + 1024;
+
+// STARVED: for the self-test of the bounded waits only; nothing is copied, so that the first wait for operands runs out.
+template <typename T, int DP, bool STARVED = false>
+__global__ void __launch_bounds__(kForwardThreads, 2)
+attention_forward_kernel(const __grid_constant__ TileArgs t)
+{
+    constexpr unsigned long long kLimit = STARVED ? kAttentionStarvedNs : kAttentionWaitNs;
+    constexpr int kStages = kForwardStages<DP>, kBytes = kTile * DP * 2, kHalves = DP / 64;
+    extern __shared__ unsigned char raw[];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 5];
+    __shared__ unsigned tmem_slot;
+    __shared__ int gave_up;
+    __shared__ Reach reach;
+
+    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + kBytes;
+    const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, scored = loaded + 8, weighted = scored + 8,
+                   summed = weighted + 8, drain = summed + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        reach_init(reach);
+        for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
+        barrier_init(loaded, 1);
+        barrier_init(scored, 1);
+        barrier_init(weighted, 4);
+        barrier_init(summed, 1);
+        barrier_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) tensor_alloc<256>(smem_address(&tmem_slot));
+    order_before();
+    __syncthreads();
+    order_after();
+    stream_order();
+    const unsigned tmem = tmem_slot, tmem_s = tmem, tmem_o = tmem + 128;
+
+    const AttentionArgs& a = t.a;
+    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
+    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / per, w = static_cast<int>(blockIdx.x) % per / a.heads, h = static_cast<int>(blockIdx.x) % a.heads;
+    const int m = t.first_worker + w, r0 = tile * kTile, kv = h / a.group;     // the last rows, which see most, first
+    Keys keys{};
+    bool valid = false;
+    const int row = r0 + static_cast<int>(threadIdx.x);
+    if (warp < 4) {
+        const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
+        valid = s.start < s.end;
+        if (valid) keys = keys_of(a, s, row);
+        reach_add(reach, valid, keys.lo, keys.hi, keys.start);
+    }
+    __syncthreads();
+    const Reach all = reach;
+    const KeyWalk walk(all, a.sinks, kTile);
+    const int steps = STARVED ? 1 : walk.steps;
+
+    int fills = 0;                                            // of the copying thread
+    if (!STARVED && warp == 4 && lane == 0 && steps > 0) {
+        barrier_expect(loaded, kBytes);
+#pragma unroll
+        for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][w], i / 2 * 64, h, r0 + i % 2 * kBox, loaded);
+        for (; fills < 2 * steps; ++fills) {                  // k, v, k, v, ...
+            const int s = fills % kStages, j = walk.row(fills / 2, kTile);
+            if (fills >= kStages && !tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) break;
+            barrier_expect(full + 8 * s, kBytes);
+#pragma unroll
+            for (int i = 0; i < 2 * kHalves; ++i) copy_box(ring + s * kBytes + i * kBoxBytes, &t.map[1 + fills % 2][w], i / 2 * 64, kv, j + i % 2 * kBox, full + 8 * s);
+        }
+    } else if (warp == 5 && lane == 0 && steps > 0) {
+        constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
+        constexpr unsigned kScores = kTypes | (kTile >> 3) << 17, kValues = kTypes | 1u << 16 | (DP >> 3) << 17;
+        bool ok = tile_wait<kLimit>(loaded, 0, &gave_up);
+        const unsigned long long dq = matrix_descriptor(own, 16);
+        const auto wait_fill = [&](int f) {
+            ok = ok && tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, &gave_up);
+            order_after();
+            return ok;
+        };
+        const auto scores = [&](int i) {
+            const unsigned long long dk = matrix_descriptor(ring + 2 * i % kStages * kBytes, 16);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
+                mma_shared(tmem_s, dq + at, dk + at, kScores, k > 0);
+            }
+            mma_done(empty + 8 * (2 * i % kStages));
+            mma_done(scored);
+        };
+        if (wait_fill(0)) scores(0);
+        for (int i = 0; i < steps && ok; ++i) {
+            ok = tile_wait<kLimit>(weighted, i & 1, &gave_up);
+            if (!wait_fill(2 * i + 1)) break;
+            const int s = (2 * i + 1) % kStages;
+            const unsigned long long dv = matrix_descriptor(ring + s * kBytes, 2 * kBoxBytes);
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k) mma_tensor(tmem_o, tmem_s + k * 8, dv + k * (2048 >> 4), kValues, i > 0 || k > 0);
+            mma_done(empty + 8 * s);
+            if (i + 1 < steps) {
+                if (wait_fill(2 * i + 2)) scores(i + 1);
+            } else {
+                mma_done(summed);
+            }
+        }
+        if (!ok) {
+            mma_done(drain);
+            tile_wait<kLimit>(drain, 0, nullptr);
+        }
+    } else if (warp < 4 && steps > 0) {
+        const unsigned at = static_cast<unsigned>(warp * 32) << 16;        // this warp's lanes of tensor memory
+        const float c = a.scale * kLog2e;
+        float top = -INFINITY, total = 0.0f;
+        bool ok = true;
+        for (int i = 0; i < steps && ok; ++i) {
+            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(scored, i & 1, &gave_up));
+            if (!ok) break;
+            __syncwarp();
+            order_after();
+            unsigned s[4][32];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tensor_load(tmem_s + at + q * 32, s[q]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tensor_wait(s[q]);
+            const int j = walk.row(i, kTile), limit = i < walk.sink_steps ? all.min_lo : 0x7fffffff;
+            if (i < walk.sink_steps || j < all.max_lo || j + kTile - 1 > all.min_hi) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned seen = seen_keys(keys, j + q * 32, limit);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(seen >> e & 1)) s[q][e] = 0xff800000u;       // -infinity
+                }
+            }
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) most[e % 4] = fmaxf(most[e % 4], __uint_as_float(s[q][e]));
+            const float here = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c;
+            const bool grows = here > top + 8.0f;             // (from -infinity: always)
+            if (__any_sync(0xffffffffu, grows)) {
+                const float f = grows ? exp2_fast(top - here) : 1.0f;
+                if (grows) top = here;
+                total *= f;
+                if (i > 0) {
+#pragma unroll 1
+                    for (int d = 0; d < DP; d += 32) {
+                        unsigned o[32];
+                        tensor_load(tmem_o + at + d, o);
+                        tensor_wait(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tensor_store(tmem_o + at + d, o);
+                    }
+                }
+            }
+            const float ref = top == -INFINITY ? 0.0f : top;  // nothing seen yet: exp2 of -infinity is to be zero, not NaN
+            float sum[2] = {};
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                unsigned p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float x = exp2_fast(fmaf(__uint_as_float(s[2 * q + e / 16][e % 16 * 2]), c, -ref));
+                    const float y = exp2_fast(fmaf(__uint_as_float(s[2 * q + e / 16][e % 16 * 2 + 1]), c, -ref));
+                    sum[0] += x;
+                    sum[1] += y;
+                    p[e] = pack_pair(x, y, T{});
+                }
+                tensor_store(tmem_s + at + q * 32, p);
+            }
+            total += sum[0] + sum[1];
+            tensor_stored();
+            order_before();
+            __syncwarp();
+            if (lane == 0) arrive_here(weighted);
+        }
+        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(summed, 0, &gave_up));
+        if (ok) {
+            __syncwarp();
+            order_after();
+            T* to = static_cast<T*>(a.to[0].p[m]) + row * a.out_stride + static_cast<long long>(h) * a.dim;
+            const bool fine = store_result<T>(tmem_o + at, DP, 1.0f / total, to, a.dim, valid);
+            if (valid && a.to[1].p[m]) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + row] = (top + log2f(total)) * kLn2;
+            __syncwarp();
+            for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1) attention_row<T>(a, m, h, r0 + warp * 32 + __ffs(todo) - 1);
+        }
+    }
+    __syncwarp();
+    order_before();
+    __syncthreads();
+    order_after();
+    if (gave_up && fills > 0) {                               // copies in flight write shared memory: none is left behind
+        tile_wait<kLimit>(loaded, 0, nullptr);
+        for (int f = max(0, fills - kStages); f < fills; ++f) tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
+    }
+    if (warp == 5) tensor_free<256>(tmem);
+}
+
+// ------------------------------------------------------------------ backward
+
+// lse (in units of log 2) and delta = dout out of every row, in rows of `pitch`, a multiple of 64: rows that belong to no sequence, or to no
+// row at all, get infinity (P = 0) and 0.  For half precision also the longest rows of dout and v, from the last kv_heads
+// CTAs along y.  A CTA takes 64 rows of one head, 16 lanes a row.
+struct StatsArgs {
+    AttentionArgs a;
+    float *lse, *delta;
+    unsigned* longest;                      // NULL unless half precision; set to 0 before
+    long long pitch;
+};
+constexpr int kStatsThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kStatsThreads)
+attention_stats_kernel(const __grid_constant__ StatsArgs t)
+{
+    __shared__ float deltas[64];
+    __shared__ unsigned most;
+    stream_order();
+    const AttentionArgs& a = t.a;
+    const int r0 = blockIdx.x * 64, m = blockIdx.z, group = threadIdx.x / 16, word = threadIdx.x % 16;
+    const bool values = static_cast<int>(blockIdx.y) >= a.heads;
+    const int h = values ? blockIdx.y - a.heads : blockIdx.y;
+    if (threadIdx.x == 0) most = 0;
+    __syncthreads();
+    const T* x = static_cast<const T*>(values ? a.v.p[m] : a.dout.p[m]);
+    const T* y = static_cast<const T*>(a.out.p[m]);
+    float longest = 0.0f;
+    const int begin = a.offsets.p[m] ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), static_cast<const long long*>(a.offsets.p[m])[0]))) : 0;
+    const int end = a.offsets.p[m] ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), static_cast<const long long*>(a.offsets.p[m])[a.sequences]))) : a.rows;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = r0 + group + 16 * i;
+        const bool in = row >= begin && row < end;
+        float u[8] = {}, v[8] = {}, dot = 0.0f, square = 0.0f;
+        if (in && word * 8 < a.dim) {
+            unpack<T>(*reinterpret_cast<const uint4*>(x + row * (values ? a.v_stride : a.out_stride) + static_cast<long long>(h) * a.dim + word * 8), u);
+            if (!values) unpack<T>(*reinterpret_cast<const uint4*>(y + row * a.out_stride + static_cast<long long>(h) * a.dim + word * 8), v);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            dot = fmaf(u[e], v[e], dot);
+            square = fmaf(u[e], u[e], square);
+        }
+        dot = lanes_sum<16>(dot);
+        if (t.longest) longest = fmaxf(longest, lanes_sum<16>(square));    // (NaN does not count: such rows are done again)
+        if (!values && word == 0) deltas[group + 16 * i] = in ? dot : 0.0f;
+    }
+    if (t.longest && word == 0) atomicMax(&most, __float_as_uint(longest));
+    __syncthreads();
+    if (!values && threadIdx.x < 64) {
+        const int row = r0 + threadIdx.x;
+        const long long at = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
+        const bool in = row >= begin && row < end;
+        t.delta[at] = deltas[threadIdx.x];
+        t.lse[at] = in ? lse_of(a, m, h, row) : INFINITY;
+    }
+    if (t.longest && threadIdx.x == 0) atomicMax(t.longest + 2 * m + (values ? 1 : 0), most);
+}
+
+// The power of two that half precision's dS carries: with it the bound of |dS|, twice the product of the longest rows
+// of dout and v, lies in [2^14, 2^15).
+__device__ __forceinline__ int grad_exponent(const TileArgs& t, int m)
+{
+    if (t.longest == nullptr) return 0;
+    const float most = 2.0f * sqrtf(t.longest[2 * m]) * sqrtf(t.longest[2 * m + 1]);
+    if (!(most > 0.0f && most < INFINITY)) return 0;
+    return max(-100, min(100, 14 - ilogbf(most)));
+}
+
+constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, two groups that take steps in turn; 8: copies, 9: products
+constexpr int kStep = 64;                   // rows of a step
+template <int DP> constexpr int kBackwardStages = DP == 128 ? 4 : 6;
+template <int DP> constexpr int kSlotBytes = 2 * kStep * DP * 2;                   // two operands
+template <int DP> constexpr int kBackwardSmem = 2 * kTile * DP * 2 + kBackwardStages<DP> * (kSlotBytes<DP> + 2 * kStep * 4) + 1024;
+
+// KEYS: dk and dv of a tile of keys, walking over queries; else dq of a tile of queries, walking over keys.  Tensor memory: the
+// sums in columns 0 to 255 (dv, dk; or dq), then for each of the two groups 64 columns of scores (then P) and 64 of
+// dP (then dS).
+template <typename T, int DP, bool KEYS>
+__global__ void __launch_bounds__(kBackwardThreads, 1)
+attention_backward_kernel(const __grid_constant__ TileArgs t)
+{
+    constexpr unsigned long long kLimit = kAttentionWaitNs;
+    constexpr bool kHalf = TypeCode<T>::value == 0;
+    constexpr float kWeightExponent = kHalf ? 14.0f : 0.0f;               // of two, on P in half precision
+    constexpr int kStages = kBackwardStages<DP>, kSlot = kSlotBytes<DP>, kOwn = kTile * DP * 2, kHalves = DP / 64;
+    extern __shared__ unsigned char raw[];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 7];
+    __shared__ unsigned tmem_slot, spoiled[2][4];
+    __shared__ int gave_up;
+    __shared__ Reach reach;
+
+    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + 2 * kOwn, stats = ring + kStages * kSlot;
+    const float* stats_at = reinterpret_cast<const float*>(raw + (stats - smem_address(raw)));
+    const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, scored = loaded + 8, weighted = scored + 16,
+                   summed = weighted + 16, drain = summed + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        reach_init(reach);
+        for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
+        barrier_init(loaded, 1);
+        for (int b = 0; b < 2; ++b) { barrier_init(scored + 8 * b, 1); barrier_init(weighted + 8 * b, 4); }
+        barrier_init(summed, 1);
+        barrier_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 8) spoiled[threadIdx.x / 4][threadIdx.x % 4] = 0;
+    if (warp == 9) tensor_alloc<512>(smem_address(&tmem_slot));
+    order_before();
+    __syncthreads();
+    order_after();
+    stream_order();
+    const unsigned tmem = tmem_slot;
+
+    const AttentionArgs& a = t.a;
+    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
+    const int turn = static_cast<int>(blockIdx.x) / per, tile = KEYS ? turn : tiles - 1 - turn;    // the longest walks first, without a window
+    const int w = static_cast<int>(blockIdx.x) % per / heads, h = static_cast<int>(blockIdx.x) % heads;
+    const int m = t.first_worker + w, r0 = tile * kTile, kv = KEYS ? h : h / a.group;
+    const int row = r0 + static_cast<int>(threadIdx.x) % kTile, group = warp / 4;
+    bool valid = false;
+    Keys keys{};
+    if (warp < 8) {
+        const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
+        valid = s.start < s.end;
+        if (valid && KEYS) {
+            const Queries q = queries_of(a, s, row);
+            keys = Keys{q.lo, q.hi, 0, 0};
+        } else if (valid) {
+            keys = keys_of(a, s, row);
+        }
+        if (warp < 4) reach_add(reach, valid, keys.lo, keys.hi, keys.start);
+    }
+    __syncthreads();
+    const Reach all = reach;
+    const KeyWalk walk(all, a.sinks, kStep);
+    // Queries are walked in steps that start at multiples of 64 rows, where the rows of lse and delta start on 256 bytes.
+    const int first = KEYS ? all.min_lo / kStep * kStep : 0, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
+    const int steps = KEYS ? turns * a.group : walk.steps;
+    const auto row_of = [&](int i) { return KEYS ? first + i % turns * kStep : walk.row(i, kStep); };
+    const auto head_of = [&](int i) { return KEYS ? h * a.group + i / turns : kv; };
+
+    int fills = 0;                                            // of the copying thread
+    if (warp == 8 && lane == 0 && steps > 0) {
+        barrier_expect(loaded, 2 * kOwn);
+#pragma unroll
+        for (int i = 0; i < 4 * kHalves; ++i) {               // k and v, or q and dout
+            const int which = i / (2 * kHalves), j = i % (2 * kHalves);
+            copy_box(own + i * kBoxBytes, &t.map[KEYS ? 1 + which : 3 * which][w], j / 2 * 64, h, r0 + j % 2 * kBox, loaded);
+        }
+        for (; fills < steps; ++fills) {
+            const int s = fills % kStages, r = row_of(fills), hs = head_of(fills);
+            if (fills >= kStages && !tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) break;
+            barrier_expect(full + 8 * s, kSlot + (KEYS ? 2 * kStep * 4 : 0));
+#pragma unroll
+            for (int i = 0; i < 2 * kHalves; ++i) {           // q and dout, or k and v
+                const int which = i / kHalves;
+                copy_box(ring + s * kSlot + i * kBoxBytes, &t.map[KEYS ? 3 * which : 1 + which][w], i % kHalves * 64, hs, r, full + 8 * s);
+            }
+            if (KEYS) {
+                const long long from = (static_cast<long long>(m) * a.heads + hs) * t.pitch + r;
+                copy_floats(stats + s * 2 * kStep * 4, t.lse + from, kStep * 4, full + 8 * s);
+                copy_floats(stats + s * 2 * kStep * 4 + kStep * 4, t.delta + from, kStep * 4, full + 8 * s);
+            }
+        }
+    } else if (warp == 9 && lane == 0 && steps > 0) {
+        constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
+        constexpr unsigned kScores = kTypes | (kStep >> 3) << 17, kSums = kTypes | 1u << 16 | (DP >> 3) << 17;
+        bool ok = tile_wait<kLimit>(loaded, 0, &gave_up);
+        const unsigned long long dx = matrix_descriptor(own, 16), dy = matrix_descriptor(own + kOwn, 16);
+        const auto scores = [&](int i) {
+            const int s = i % kStages, b = i & 1;
+            ok = ok && tile_wait<kLimit>(full + 8 * s, (i / kStages) & 1, &gave_up);
+            if (!ok) return;
+            order_after();
+            const unsigned long long du = matrix_descriptor(ring + s * kSlot, 16), dw = matrix_descriptor(ring + s * kSlot + kSlot / 2, 16);
+            const unsigned to = tmem + 256 + b * 128;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+                mma_shared(to, dx + ((k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4), du + ((k / 4 * kBoxBytes + k % 4 * 32) >> 4), kScores, k > 0);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+                mma_shared(to + 64, dy + ((k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4), dw + ((k / 4 * kBoxBytes + k % 4 * 32) >> 4), kScores, k > 0);
+            mma_done(scored + 8 * b);
+        };
+        scores(0);
+        for (int i = 0; i < steps && ok; ++i) {
+            const int s = i % kStages, b = i & 1;
+            if (i + 1 < steps) scores(i + 1);
+            ok = ok && tile_wait<kLimit>(weighted + 8 * b, (i >> 1) & 1, &gave_up);
+            if (!ok) break;
+            order_after();
+            const unsigned long long du = matrix_descriptor(ring + s * kSlot, kBoxBytes), dw = matrix_descriptor(ring + s * kSlot + kSlot / 2, kBoxBytes);
+            const unsigned from = tmem + 256 + b * 128;
+            if (KEYS) {
+#pragma unroll
+                for (int k = 0; k < kStep / 16; ++k) mma_tensor(tmem, from + k * 8, dw + k * (2048 >> 4), kSums, i > 0 || k > 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kStep / 16; ++k) mma_tensor(tmem + (KEYS ? 128 : 0), from + 64 + k * 8, du + k * (2048 >> 4), kSums, i > 0 || k > 0);
+            mma_done(empty + 8 * s);
+        }
+        if (ok) mma_done(summed);
+        else {
+            mma_done(drain);
+            tile_wait<kLimit>(drain, 0, nullptr);
+        }
+    } else if (warp < 8 && steps > 0) {
+        const unsigned at = static_cast<unsigned>(warp % 4 * 32) << 16;
+        const float c = a.scale * kLog2e;
+        const int exponent = kHalf ? grad_exponent(t, m) : 0;
+        const float to_grad = kHalf ? exp2f(static_cast<float>(exponent) - kWeightExponent) : 1.0f;
+        float lse = 0.0f, delta = 0.0f;
+        if (!KEYS && valid) {
+            const long long from = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
+            lse = t.lse[from] - static_cast<float>(exponent);  // P with dS's power of two
+            delta = t.delta[from];
+        }
+        bool ok = true;
+        for (int i = group; i < steps && ok; i += 2) {
+            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(scored + 8 * group, (i >> 1) & 1, &gave_up));
+            if (!ok) break;
+            __syncwarp();
+            order_after();
+            const unsigned from = tmem + 256 + group * 128 + at;
+            const int r = row_of(i), limit = !KEYS && i < walk.sink_steps ? all.min_lo : 0x7fffffff;
+            const bool masked = (!KEYS && i < walk.sink_steps) || r < all.max_lo || r + kStep - 1 > all.min_hi;
+            const float* column = stats_at + i % kStages * 2 * kStep;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                unsigned s[32], g[32], p[16], d[16];
+                tensor_load(from + q * 32, s);
+                tensor_load(from + 64 + q * 32, g);
+                tensor_wait(s);
+                tensor_wait(g);
+                float v[32], x[32];
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    float l[4] = {lse, lse, lse, lse}, dl[4] = {delta, delta, delta, delta};
+                    if (KEYS) {
+                        const float4 u = *reinterpret_cast<const float4*>(column + q * 32 + e), y = *reinterpret_cast<const float4*>(column + kStep + q * 32 + e);
+                        l[0] = u.x - kWeightExponent; l[1] = u.y - kWeightExponent; l[2] = u.z - kWeightExponent; l[3] = u.w - kWeightExponent;
+                        dl[0] = y.x; dl[1] = y.y; dl[2] = y.z; dl[3] = y.w;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v[e + j] = exp2_fast(fmaf(__uint_as_float(s[e + j]), c, -l[j]));
+                        x[e + j] = v[e + j] * (__uint_as_float(g[e + j]) - dl[j]);
+                        if (KEYS && kHalf) x[e + j] *= to_grad;
+                    }
+                }
+                if (masked) {
+                    const unsigned seen = KEYS ? bits_between(keys.lo - r - q * 32, keys.hi - r - q * 32) : seen_keys(keys, r + q * 32, limit);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(seen >> e & 1)) v[e] = x[e] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (KEYS) p[e] = pack_pair(v[2 * e], v[2 * e + 1], T{});
+                    d[e] = pack_pair(x[2 * e], x[2 * e + 1], T{});
+                }
+                if (KEYS) tensor_store(from + q * 16, p);
+                tensor_store(from + 64 + q * 16, d);
+            }
+            tensor_stored();
+            order_before();
+            __syncwarp();
+            if (lane == 0) arrive_here(weighted + 8 * group);
+        }
+        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(summed, 0, &gave_up));
+        if (ok) {
+            __syncwarp();
+            order_after();
+            const float of_grad = a.scale * (kHalf ? exp2f(static_cast<float>(-exponent)) : 1.0f);
+            bool fine = true;
+            if (KEYS) {                                       // one group dv, the other dk
+                const int which = group ? 1 : 2;
+                T* to = static_cast<T*>(a.to[which].p[m]) + row * (group ? a.k_stride : a.v_stride) + static_cast<long long>(h) * a.dim;
+                fine = store_result<T>(tmem + group * 128 + at, DP, group ? of_grad : exp2f(-kWeightExponent), to, a.dim, valid);
+            } else {                                          // half of the columns each
+                T* to = static_cast<T*>(a.to[0].p[m]) + row * a.q_stride + static_cast<long long>(h) * a.dim + group * (DP / 2);
+                fine = store_result<T>(tmem + group * (DP / 2) + at, DP / 2, of_grad, to, a.dim - group * (DP / 2), valid);
+            }
+            const unsigned todo = __ballot_sync(0xffffffffu, valid && !fine);
+            if (lane == 0) spoiled[group][warp % 4] = todo;
+        }
+    }
+    __syncwarp();
+    order_before();
+    __syncthreads();
+    order_after();
+    if (gave_up && fills > 0) {                               // copies in flight write shared memory: none is left behind
+        tile_wait<kLimit>(loaded, 0, nullptr);
+        for (int f = max(0, fills - kStages); f < fills; ++f) tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
+    }
+    if (warp == 9) tensor_free<512>(tmem);
+    if (warp < 4)
+        for (unsigned todo = spoiled[0][warp] | spoiled[1][warp]; todo; todo &= todo - 1) {
+            const int lost = __ffs(todo) - 1, r = r0 + warp * 32 + lost;
+            if (KEYS) attention_key_grad_row<T>(a, m, h, r, spoiled[1][warp] >> lost & 1, spoiled[0][warp] >> lost & 1);
+            else attention_query_grad_row<T>(a, m, h, r);
+        }
+}
+
+}  // namespace replica
+}  // namespace grawa

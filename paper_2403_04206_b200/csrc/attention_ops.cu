@@ -1,163 +1,13 @@
-// Host side of the attention operators (head norms with rotation, attention within a window): argument checks, the choice of
-// a kernel, launches, and their part of the C ABI in include/grawa.h.  No call allocates device memory or keeps anything
-// from one call to the next.
+// Host side of attention within a window: argument checks, the choice of a kernel, launches, and its part of the C ABI in
+// include/grawa.h.  No call allocates device memory or keeps anything from one call to the next.
 #include <cmath>
+#include <utility>
 
-#include "attention_rows.cuh"
-#include "head_rotary.cuh"
+#include "attention.cuh"
 #include "replica_host.h"
 
 namespace grawa {
 namespace replica {
-
-// ------------------------------------------------------------------ head norms with rotation
-
-// What both directions are told about the heads.
-struct HeadShape {
-    grawa_dtype dtype;
-    grawa_pairing pairing;
-    int64_t rows, q_heads, k_heads, head_dim, rotary;
-    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
-    const int64_t* const* positions;
-    const double* frequencies;
-    int64_t period;
-    int M;
-    float eps;
-};
-
-static bool stride_ok(int64_t rows, int64_t cols, int64_t stride)
-{
-    return stride >= cols && stride <= (int64_t{1} << 58) / std::max<int64_t>(1, rows);
-}
-
-static bool head_shape_ok(const HeadShape& s)
-{
-    constexpr int64_t kMostHeads = 1 << 16;
-    if (!dtype_known(s.dtype) || (s.pairing != GRAWA_PAIR_HALVES && s.pairing != GRAWA_PAIR_NEIGHBOURS) || s.M < 1 || s.M > GRAWA_MAX_WORKERS) return false;
-    if (s.rows < 0 || s.rows > 0x7fffffff || s.q_heads < 1 || s.q_heads > kMostHeads || s.k_heads < 0 || s.k_heads > kMostHeads) return false;
-    if (s.head_dim < 1 || s.head_dim > kHeadDim || s.rotary < 0 || s.rotary > s.head_dim || s.rotary % 2 != 0) return false;
-    if (!stride_ok(s.rows, s.q_heads * s.head_dim, s.q_stride) || !stride_ok(s.rows, s.q_heads * s.head_dim, s.q_out_stride)) return false;
-    if (s.k_heads && (!stride_ok(s.rows, s.k_heads * s.head_dim, s.k_stride) || !stride_ok(s.rows, s.k_heads * s.head_dim, s.k_out_stride))) return false;
-    if (!(s.eps >= 0.0f) || std::isinf(s.eps)) return false;
-    if (s.rotary && (!s.frequencies || !aligned(s.frequencies, 8) || (!s.positions && s.period < 1))) return false;
-    return true;
-}
-
-// The buffers that both directions read beside their heads.
-static bool add_head_inputs(Buffers& b, const HeadShape& s, const void* const* q_weight, const void* const* k_weight)
-{
-    const int64_t elem = type_bytes(s.dtype);
-    if (q_weight && !b.add(q_weight, s.M, 1, s.head_dim, s.head_dim, elem, false)) return false;
-    if (s.k_heads && k_weight && !b.add(k_weight, s.M, 1, s.head_dim, s.head_dim, elem, false)) return false;
-    if (s.rotary == 0) return true;
-    const void* f = s.frequencies;
-    if (!b.add(&f, 1, 1, s.rotary / 2, s.rotary / 2, 8, false)) return false;
-    return !s.positions || b.add(reinterpret_cast<const void* const*>(s.positions), s.M, 1, s.rows, s.rows, 8, false);
-}
-
-// Heads that are read, and written in place or elsewhere: `in` may be the same buffer as `out` where their strides are equal.
-static bool add_in_and_out(Buffers& b, const void* const* in, int64_t in_stride, void* const* out, int64_t out_stride, const HeadShape& s, int64_t heads)
-{
-    const int64_t elem = type_bytes(s.dtype), cols = heads * s.head_dim;
-    const void* apart[GRAWA_MAX_WORKERS];
-    int others = 0;
-    for (int m = 0; m < s.M; ++m)
-        if (!out || in[m] != out[m] || (s.rows > 1 && in_stride != out_stride)) apart[others++] = in[m];
-    return b.add(apart, others, s.rows, cols, in_stride, elem, false) && (!out || b.add(out, s.M, s.rows, cols, out_stride, elem, true));
-}
-
-static HeadArgs head_args(const HeadShape& s, const void* const* q, const void* const* k, const void* const* q_weight, const void* const* k_weight)
-{
-    HeadArgs a{};
-    copy_table(a.x[0], q, s.M);
-    copy_table(a.w[0], q_weight, s.M);
-    if (s.k_heads) {
-        copy_table(a.x[1], k, s.M);
-        copy_table(a.w[1], k_weight, s.M);
-    }
-    if (s.rotary) copy_table(a.positions, s.positions, s.M);
-    a.frequencies = s.frequencies;
-    a.rows = s.rows; a.period = std::max<int64_t>(1, s.period);
-    a.x_stride[0] = s.q_stride; a.x_stride[1] = s.k_stride;
-    a.y_stride[0] = s.q_out_stride; a.y_stride[1] = s.k_out_stride;
-    a.heads[0] = static_cast<int>(s.q_heads); a.heads[1] = static_cast<int>(s.k_heads);
-    a.dim = static_cast<int>(s.head_dim); a.half = static_cast<int>(s.rotary / 2);
-    a.neighbours = s.pairing == GRAWA_PAIR_NEIGHBOURS;
-    a.words = static_cast<int>(s.head_dim * type_bytes(s.dtype) / 16);
-    a.has_w[0] = q_weight != nullptr; a.has_w[1] = k_weight != nullptr;
-    a.eps = s.eps; a.inv_dim = 1.0f / static_cast<float>(s.head_dim);
-    return a;
-}
-
-// How the heads are held by the lanes: in whole 16-byte words where all rows, heads and rotated halves are made of them.
-static HeadMode head_mode(const HeadArgs& a, grawa_dtype dtype, int M, bool backward)
-{
-    const int64_t elem = type_bytes(dtype), word = 16 / elem;
-    bool whole = a.dim % word == 0;
-    for (int i = 0; i < 2 && whole; ++i) {
-        if (a.heads[i] == 0) continue;
-        whole = all_aligned(a.x[i].p, M, 16) && all_aligned(a.y[i].p, M, 16) && (!backward || all_aligned(a.dy[i].p, M, 16));
-        if (a.rows > 1) whole = whole && a.x_stride[i] % word == 0 && a.y_stride[i] % word == 0;
-    }
-    if (!whole) return kPairAny;
-    if (a.neighbours) return kPairNext;
-    return a.half % word == 0 ? kPairWords : kPairAny;
-}
-
-// Calls f with the number of lanes a head takes, each of which holds two of its words.
-template <typename T, typename F>
-static grawa_status with_lanes(int words, const F& f)
-{
-    if (words <= 4) return f(std::integral_constant<int, 2>{});
-    if (words <= 8) return f(std::integral_constant<int, 4>{});
-    if (words <= 16) return f(std::integral_constant<int, 8>{});
-    if (words <= 32) return f(std::integral_constant<int, 16>{});
-    return f(std::integral_constant<int, sizeof(T) == 4 ? 32 : 16>{});     // (16-bit heads have up to 32 words)
-}
-
-template <typename T>
-static grawa_status head_forward(HeadArgs& a, int M, HeadMode mode, cudaStream_t stream)
-{
-    const auto run = [&](auto kernel, int per) {
-        constexpr int kWarps = kHeadThreads / 32;
-        const int64_t steps = ceil_div(a.heads[0] + a.heads[1], per);
-        // rows whose warps would not fill the SMs are shared out among several each, down to one step of `per` heads
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, int64_t{kSms} * 32 / (a.rows * M)));
-        a.per_chunk = static_cast<int>(ceil_div(steps, want)) * per;
-        a.chunks = static_cast<int>(ceil_div(a.heads[0] + a.heads[1], a.per_chunk));
-        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows * a.chunks, kWarps), static_cast<int64_t>(kSms) * 32 / M));
-        return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kHeadThreads, 0, stream, a);
-    };
-    if (mode == kPairAny) return run(head_rotary_forward_kernel<T, 32, kPairAny>, 1);
-    return with_lanes<T>(a.words, [&](auto lanes) {
-        constexpr int L = decltype(lanes)::value;
-        return mode == kPairWords ? run(head_rotary_forward_kernel<T, L, kPairWords>, 32 / L) : run(head_rotary_forward_kernel<T, L, kPairNext>, 32 / L);
-    });
-}
-
-// CTAs a worker's rows are split over in the backward pass (a rule on the sizes alone, so that the order of the additions
-// does not change from call to call): two an SM, which is what their registers allow.
-static int head_parts(int64_t rows, int M)
-{
-    return static_cast<int>(std::max<int64_t>(1, std::min(ceil_div(rows, kHeadThreads / 32), static_cast<int64_t>(2 * kSms / M))));
-}
-
-template <typename T>
-static grawa_status head_backward(const HeadArgs& a, int M, HeadMode mode, cudaStream_t stream)
-{
-    const auto run = [&](auto kernel) {
-        return launch_clusters(kernel, dim3(static_cast<unsigned>(a.parts), M), kHeadThreads, 0, stream, false, 1u, a);
-    };
-    grawa_status st;
-    if (mode == kPairAny) st = run(head_rotary_backward_kernel<T, 32, kPairAny>);
-    else
-        st = with_lanes<T>(a.words, [&](auto lanes) {
-            constexpr int L = decltype(lanes)::value;
-            return mode == kPairWords ? run(head_rotary_backward_kernel<T, L, kPairWords>) : run(head_rotary_backward_kernel<T, L, kPairNext>);
-        });
-    if (st != GRAWA_OK || a.parts == 1 || (!a.has_dw[0] && !a.has_dw[1])) return st;
-    return launch(head_rotary_finish_kernel<T>, dim3(static_cast<unsigned>(ceil_div(a.dim, 32)), M, 2), 32 * kHeadGroups, 0, stream, a);
-}
 
 // ------------------------------------------------------------------ attention within a window
 
@@ -173,7 +23,8 @@ struct AttentionShape {
 static bool attention_shape_ok(const AttentionShape& s)
 {
     if ((s.dtype != GRAWA_BF16 && s.dtype != GRAWA_F16) || s.M < 1 || s.M > GRAWA_MAX_WORKERS) return false;
-    if (s.rows < 0 || s.rows > 0x7fffffff - 1024 || s.q_heads < 1 || s.q_heads > 0xffff || s.kv_heads < 1 || s.q_heads % s.kv_heads != 0) return false;
+    if (s.rows < 0 || s.rows > 0x7fffffff - 1024 || s.q_heads < 1 || s.q_heads > 0x7fff || s.kv_heads < 1 || s.q_heads % s.kv_heads != 0) return false;
+    if (ceil_div(s.rows, kTile) * s.q_heads * std::min(s.M, kAttentionWorkers) > 0x7fffffff) return false;          // CTAs of a launch
     if (s.head_dim < 8 || s.head_dim > 128 || s.head_dim % 8 != 0) return false;
     if (s.left < 0 || s.right < 0 || s.sinks < 0 || !(s.scale > 0.0f) || std::isinf(s.scale)) return false;
     if (s.offsets ? s.sequences < 0 || s.sequences > 0x7fffffff - 1 : s.period < 1) return false;
@@ -212,11 +63,78 @@ static AttentionArgs attention_args(const AttentionShape& s, const void* const* 
     return a;
 }
 
-template <int PASS>
-static grawa_status launch_rows(const AttentionArgs& a, grawa_dtype dtype, int M, int heads, cudaStream_t stream)
+// Map of a worker's heads as [row][head][element], for boxes of 64 elements of one head by 64 rows.
+static grawa_status encode_heads(CUtensorMap* map, grawa_dtype dtype, const void* base, const AttentionShape& s, int64_t heads, int64_t stride)
 {
-    auto* const kernel = dtype == GRAWA_BF16 ? attention_rows_kernel<__nv_bfloat16, PASS> : attention_rows_kernel<__half, PASS>;
-    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(a.rows, kRowThreads / 32)), heads, M), kRowThreads, 0, stream, a);
+    PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+    const grawa_status st = map_encoder(&encode);
+    if (st != GRAWA_OK) return st;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(s.head_dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(s.rows)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(s.head_dim) * 2, static_cast<cuuint64_t>(stride) * 2};
+    const cuuint32_t box[3] = {kBox, 1, kBox}, step[3] = {1, 1, 1};
+    const CUresult res = encode(map, dtype == GRAWA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims,
+                                strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return res == CUDA_SUCCESS ? GRAWA_OK : cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+}
+
+// The workers [first, first + count) of a launch, with the maps of q, k, v and (backward) dout.
+static grawa_status set_workers(TileArgs& t, const AttentionShape& s, int first, int count)
+{
+    t.first_worker = first;
+    t.workers = count;
+    grawa_status st = GRAWA_OK;
+    for (int w = 0; w < count && st == GRAWA_OK; ++w) {
+        const int m = first + w;
+        st = encode_heads(&t.map[0][w], s.dtype, t.a.q.p[m], s, s.q_heads, s.q_stride);
+        if (st == GRAWA_OK) st = encode_heads(&t.map[1][w], s.dtype, t.a.k.p[m], s, s.kv_heads, s.k_stride);
+        if (st == GRAWA_OK) st = encode_heads(&t.map[2][w], s.dtype, t.a.v.p[m], s, s.kv_heads, s.v_stride);
+        if (st == GRAWA_OK && t.a.dout.p[m]) st = encode_heads(&t.map[3][w], s.dtype, t.a.dout.p[m], s, s.q_heads, s.out_stride);
+    }
+    return st;
+}
+
+template <typename Kernel>
+static grawa_status launch_tiles(Kernel kernel, const TileArgs& t, int heads, int threads, int smem, cudaStream_t stream)
+{
+    GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(t.a.rows, kTile) * heads * t.workers)), threads, smem, stream, t);
+}
+template <typename T>
+static grawa_status launch_forward(const TileArgs& t, cudaStream_t stream)
+{
+    return t.a.dim <= 64 ? launch_tiles(attention_forward_kernel<T, 64>, t, t.a.heads, kForwardThreads, kForwardSmem<64>, stream)
+                         : launch_tiles(attention_forward_kernel<T, 128>, t, t.a.heads, kForwardThreads, kForwardSmem<128>, stream);
+}
+template <typename T, bool KEYS>
+static grawa_status launch_backward(const TileArgs& t, cudaStream_t stream)
+{
+    const int heads = KEYS ? t.a.kv_heads : t.a.heads;
+    return t.a.dim <= 64 ? launch_tiles(attention_backward_kernel<T, 64, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<64>, stream)
+                         : launch_tiles(attention_backward_kernel<T, 128, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<128>, stream);
+}
+
+// The places of a backward call's scratch: lse and delta of every row, and the longest rows.
+struct AttentionScratch {
+    int64_t pitch;
+    size_t lse, delta, longest, bytes;                        // offsets, and the whole
+};
+static AttentionScratch attention_scratch(int64_t rows, int64_t q_heads, int M)
+{
+    AttentionScratch s{};
+    s.pitch = ceil_div(rows, kStep) * kStep;
+    const size_t table = static_cast<size_t>(M) * q_heads * s.pitch * sizeof(float);        // a multiple of 256 bytes
+    s.delta = table;
+    s.longest = 2 * table;
+    s.bytes = 2 * table + (static_cast<size_t>(M) * 2 * sizeof(float) + 255) / 256 * 256;
+    return s;
+}
+
+template <typename T>
+static grawa_status attention_stats(const StatsArgs& t, int M, cudaStream_t stream)
+{
+    const int heads = t.a.heads + (t.longest ? t.a.kv_heads : 0);
+    return launch(attention_stats_kernel<T>, dim3(static_cast<unsigned>(t.pitch / 64), heads, M), kStatsThreads, 0, stream, t);
 }
 
 }  // namespace replica
@@ -226,79 +144,6 @@ using namespace grawa;
 using namespace grawa::replica;
 
 extern "C" {
-
-grawa_status grawa_head_rotary_forward(grawa_dtype dtype, grawa_pairing pairing, const void* const* q, const void* const* k, const void* const* q_weight,
-                                       const void* const* k_weight, void* const* q_out, void* const* k_out, const int64_t* const* positions,
-                                       const double* frequencies, int64_t rows, int64_t q_heads, int64_t k_heads, int64_t head_dim, int64_t rotary,
-                                       int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, int64_t period, int M, float eps,
-                                       grawa_stream_t stream)
-{
-    const HeadShape s{dtype, pairing, rows, q_heads, k_heads, head_dim, rotary, q_stride, k_stride, q_out_stride, k_out_stride, positions, frequencies, period, M, eps};
-    if (!head_shape_ok(s) || !q || !q_out || (k_heads && (!k || !k_out))) return GRAWA_ERR_INVALID_ARG;
-    if (rows == 0) return GRAWA_OK;
-    Buffers b;
-    if (!add_head_inputs(b, s, q_weight, k_weight) || !add_in_and_out(b, q, q_stride, q_out, q_out_stride, s, q_heads)) return GRAWA_ERR_INVALID_ARG;
-    if (k_heads && !add_in_and_out(b, k, k_stride, k_out, k_out_stride, s, k_heads)) return GRAWA_ERR_INVALID_ARG;
-    if (b.clash()) return GRAWA_ERR_INVALID_ARG;
-    HeadArgs a = head_args(s, q, k, q_weight, k_weight);
-    copy_table(a.y[0], q_out, M);
-    if (k_heads) copy_table(a.y[1], k_out, M);
-    const HeadMode mode = head_mode(a, dtype, M, false);
-    if (dtype == GRAWA_BF16) return head_forward<__nv_bfloat16>(a, M, mode, stream);
-    if (dtype == GRAWA_F16) return head_forward<__half>(a, M, mode, stream);
-    return head_forward<float>(a, M, mode, stream);
-}
-
-size_t grawa_head_rotary_backward_workspace_bytes(int64_t rows, int M)
-{
-    if (M < 1 || M > GRAWA_MAX_WORKERS || rows < 0 || rows > 0x7fffffff) return 0;
-    const int parts = head_parts(rows, M);
-    return parts > 1 ? static_cast<size_t>(M) * parts * 2 * kHeadDim * sizeof(float) : 0;
-}
-
-grawa_status grawa_head_rotary_backward(grawa_dtype dtype, grawa_pairing pairing, const void* const* dq_out, const void* const* dk_out, const void* const* q,
-                                        const void* const* k, const void* const* q_weight, const void* const* k_weight, void* const* dq, void* const* dk,
-                                        void* const* dq_weight, void* const* dk_weight, const int64_t* const* positions, const double* frequencies,
-                                        int64_t rows, int64_t q_heads, int64_t k_heads, int64_t head_dim, int64_t rotary, int64_t q_stride,
-                                        int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, int64_t period, int M, float eps, int accumulate,
-                                        void* workspace, size_t workspace_bytes, grawa_stream_t stream)
-{
-    const HeadShape s{dtype, pairing, rows, q_heads, k_heads, head_dim, rotary, q_stride, k_stride, q_out_stride, k_out_stride, positions, frequencies, period, M, eps};
-    if (!head_shape_ok(s) || !q || !dq_out || (k_heads && (!k || !dk_out)) || (!k_heads && (dk || dk_weight))) return GRAWA_ERR_INVALID_ARG;
-    if (!dq && !dk && !dq_weight && !dk_weight) return GRAWA_ERR_INVALID_ARG;
-    if (rows == 0 && (accumulate || (!dq_weight && !dk_weight))) return GRAWA_OK;
-    const int64_t elem = type_bytes(dtype);
-    Buffers b;
-    if (!add_head_inputs(b, s, q_weight, k_weight) || !b.add(q, M, rows, q_heads * head_dim, q_stride, elem, false) ||
-        !add_in_and_out(b, dq_out, q_out_stride, dq, q_stride, s, q_heads)) return GRAWA_ERR_INVALID_ARG;
-    if (k_heads && (!b.add(k, M, rows, k_heads * head_dim, k_stride, elem, false) || !add_in_and_out(b, dk_out, k_out_stride, dk, k_stride, s, k_heads)))
-        return GRAWA_ERR_INVALID_ARG;
-    if (dq_weight && !b.add(dq_weight, M, 1, head_dim, head_dim, elem, true)) return GRAWA_ERR_INVALID_ARG;
-    if (dk_weight && !b.add(dk_weight, M, 1, head_dim, head_dim, elem, true)) return GRAWA_ERR_INVALID_ARG;
-    const size_t need = dq_weight || dk_weight ? grawa_head_rotary_backward_workspace_bytes(rows, M) : 0;
-    if (need) {
-        if (!workspace || !aligned(workspace, 16) || workspace_bytes < need) return GRAWA_ERR_WORKSPACE;
-        const void* ws = workspace;
-        if (!b.add(&ws, 1, 1, static_cast<int64_t>(need), static_cast<int64_t>(need), 1, true)) return GRAWA_ERR_INVALID_ARG;
-    }
-    if (b.clash()) return GRAWA_ERR_INVALID_ARG;
-    HeadArgs a = head_args(s, q, k, q_weight, k_weight);
-    copy_table(a.dy[0], dq_out, M);
-    if (k_heads) copy_table(a.dy[1], dk_out, M);
-    copy_table(a.y[0], dq, M);
-    copy_table(a.y[1], dk, M);
-    copy_table(a.dw[0], dq_weight, M);
-    copy_table(a.dw[1], dk_weight, M);
-    a.has_dx[0] = dq != nullptr; a.has_dx[1] = dk != nullptr;
-    a.has_dw[0] = dq_weight != nullptr; a.has_dw[1] = dk_weight != nullptr;
-    a.accumulate = accumulate != 0;
-    a.parts = head_parts(rows, M);
-    a.partial = static_cast<float*>(workspace);
-    const HeadMode mode = head_mode(a, dtype, M, true);
-    if (dtype == GRAWA_BF16) return head_backward<__nv_bfloat16>(a, M, mode, stream);
-    if (dtype == GRAWA_F16) return head_backward<__half>(a, M, mode, stream);
-    return head_backward<float>(a, M, mode, stream);
-}
 
 grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void* const* q, const void* const* k, const void* const* v, void* const* out,
                                             float* const* lse, const int64_t* const* offsets, int64_t sequences, int64_t period, int64_t left,
@@ -314,15 +159,22 @@ grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void* const
         !add_heads(b, out, s, q_heads, out_stride, true) || !add_offsets(b, s)) return GRAWA_ERR_INVALID_ARG;
     if (lse && !b.add(reinterpret_cast<const void* const*>(lse), M, 1, q_heads * rows, q_heads * rows, 4, true)) return GRAWA_ERR_INVALID_ARG;
     if (b.clash()) return GRAWA_ERR_INVALID_ARG;
-    AttentionArgs a = attention_args(s, q, k, v);
-    copy_table(a.to[0], out, M);
-    copy_table(a.to[1], lse, M);
-    return launch_rows<kRowForward>(a, dtype, M, a.heads, stream);
+    TileArgs t{};
+    t.a = attention_args(s, q, k, v);
+    copy_table(t.a.to[0], out, M);
+    copy_table(t.a.to[1], lse, M);
+    grawa_status st = GRAWA_OK;
+    for (int first = 0; first < M && st == GRAWA_OK; first += kAttentionWorkers) {
+        st = set_workers(t, s, first, std::min(kAttentionWorkers, M - first));
+        if (st == GRAWA_OK) st = dtype == GRAWA_BF16 ? launch_forward<__nv_bfloat16>(t, stream) : launch_forward<__half>(t, stream);
+    }
+    return st;
 }
 
 size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int M)
 {
-    return 0;
+    if (M < 1 || M > GRAWA_MAX_WORKERS || rows < 0 || rows > 0x7fffffff - 1024 || q_heads < 1 || q_heads > 0x7fff) return 0;
+    return attention_scratch(rows, q_heads, M).bytes;
 }
 
 grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* const* dout, const void* const* q, const void* const* k, const void* const* v,
@@ -348,17 +200,45 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* cons
         if (!b.add(&ws, 1, 1, static_cast<int64_t>(need), static_cast<int64_t>(need), 1, true)) return GRAWA_ERR_INVALID_ARG;
     }
     if (b.clash()) return GRAWA_ERR_INVALID_ARG;
-    AttentionArgs a = attention_args(s, q, k, v);
-    copy_table(a.dout, dout, M);
-    copy_table(a.out, out, M);
-    copy_table(a.lse, lse, M);
-    copy_table(a.to[0], dq, M);
-    copy_table(a.to[1], dk, M);
-    copy_table(a.to[2], dv, M);
-    grawa_status st = GRAWA_OK;
-    if (dq) st = launch_rows<kRowQueryGrad>(a, dtype, M, a.heads, stream);
-    if (dk && st == GRAWA_OK) st = launch_rows<kRowKeyGrad>(a, dtype, M, a.kv_heads, stream);
+    const AttentionScratch scratch = attention_scratch(rows, q_heads, M);
+    char* const base = static_cast<char*>(workspace);
+    TileArgs t{};
+    t.a = attention_args(s, q, k, v);
+    copy_table(t.a.dout, dout, M);
+    copy_table(t.a.out, out, M);
+    copy_table(t.a.lse, lse, M);
+    copy_table(t.a.to[0], dq, M);
+    copy_table(t.a.to[1], dk, M);
+    copy_table(t.a.to[2], dv, M);
+    t.lse = reinterpret_cast<float*>(base);
+    t.delta = reinterpret_cast<float*>(base + scratch.delta);
+    t.longest = dtype == GRAWA_F16 ? reinterpret_cast<float*>(base + scratch.longest) : nullptr;
+    t.pitch = scratch.pitch;
+    StatsArgs stats{t.a, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + scratch.delta),
+                    dtype == GRAWA_F16 ? reinterpret_cast<unsigned*>(base + scratch.longest) : nullptr, scratch.pitch};
+    if (stats.longest) GRAWA_CUDA_TRY(cudaMemsetAsync(stats.longest, 0, static_cast<size_t>(M) * 2 * sizeof(float), stream));
+    grawa_status st = dtype == GRAWA_BF16 ? attention_stats<__nv_bfloat16>(stats, M, stream) : attention_stats<__half>(stats, M, stream);
+    for (int first = 0; first < M && st == GRAWA_OK; first += kAttentionWorkers) {
+        st = set_workers(t, s, first, std::min(kAttentionWorkers, M - first));
+        if (st == GRAWA_OK && dk) st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, true>(t, stream) : launch_backward<__half, true>(t, stream);
+        if (st == GRAWA_OK && dq) st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, false>(t, stream) : launch_backward<__half, false>(t, stream);
+    }
     return st;
+}
+
+grawa_status grawa_selftest_window_attention_wait(grawa_stream_t stream)
+{
+    TileArgs t{};                                             // one row of one head; nothing is read or written
+    t.a.rows = t.a.heads = t.a.kv_heads = t.a.group = t.a.period = 1;
+    t.a.dim = 64;
+    t.a.scale = 1.0f;
+    t.workers = 1;
+    return launch_tiles(attention_forward_kernel<__nv_bfloat16, 64, true>, t, 1, kForwardThreads, kForwardSmem<64>, stream);
+}
+
+grawa_status grawa_window_attention_status(grawa_stream_t stream)
+{
+    return timeout_status(stream, g_attention_timeouts, "grawa_window_attention_status");
 }
 
 }  // extern "C"

@@ -183,24 +183,5 @@ __device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int 
     if (want_v) store_row<T>(a.to[2].p[m], a.v_stride, j, kv, a.dim, dv);
 }
 
-// ------------------------------------------------------------------ one warp a row
-
-constexpr int kRowThreads = 128;
-enum RowPass { kRowForward = 0, kRowQueryGrad = 1, kRowKeyGrad = 2 };
-
-template <typename T, int PASS>
-__global__ void __launch_bounds__(kRowThreads)
-attention_rows_kernel(const __grid_constant__ AttentionArgs a)
-{
-    stream_order();
-    const int row = blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32, h = blockIdx.y, m = blockIdx.z;
-    if (row >= a.rows) return;
-    const Sequence s = sequence_of(a, m, row);
-    if (s.start >= s.end) return;
-    if constexpr (PASS == kRowForward) attention_row<T>(a, m, h, row);
-    else if constexpr (PASS == kRowQueryGrad) attention_query_grad_row<T>(a, m, h, row);
-    else attention_key_grad_row<T>(a, m, h, row, true, true);
-}
-
 }  // namespace replica
 }  // namespace grawa

@@ -6,6 +6,10 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <map>
+#include <mutex>
+#include <new>
+#include <utility>
 
 namespace grawa {
 namespace replica {
@@ -14,6 +18,12 @@ inline bool dtype_known(grawa_dtype d) { return d == GRAWA_F32 || d == GRAWA_BF1
 inline int64_t type_bytes(grawa_dtype d) { return d == GRAWA_F32 ? 4 : 2; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// Are rows `stride` elements apart, of `cols`, apart from each other and of a possible size in all?
+inline bool stride_ok(int64_t rows, int64_t cols, int64_t stride)
+{
+    return stride >= cols && stride <= (int64_t{1} << 58) / std::max<int64_t>(1, rows);
+}
 
 // The buffers of a call.  add() takes one buffer a worker, `rows` rows of `cols` elements `stride` elements
 // apart; clash() says whether an output shares a byte with any other buffer of the call.  A buffer of one row, or of rows
@@ -106,6 +116,30 @@ template <typename... KArgs, typename... Args>
 grawa_status launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, const Args&... args)
 {
     return launch_clusters(kernel, grid, block, smem, stream, true, 1u, args...);
+}
+
+// Whether a device's count of waits that ran out (a symbol of the calling file) has grown since the last report on this stream.
+// Each file that includes this has its own record, of its own symbol.
+static inline grawa_status timeout_status(cudaStream_t stream, const unsigned& counter, const char* what)
+{
+    // What each stream's reports have seen of its device's count.  A call's own stream is not known to the count (a captured
+    // call may run on any), so every stream is told of every wait that ran out, once.
+    int device = 0;
+    unsigned count = 0;
+    GRAWA_CUDA_TRY(cudaGetDevice(&device));
+    GRAWA_CUDA_TRY(cudaMemcpyFromSymbolAsync(&count, counter, sizeof count, 0, cudaMemcpyDeviceToHost, stream));
+    GRAWA_CUDA_TRY(cudaStreamSynchronize(stream));
+    try {
+        static std::mutex mutex;
+        static auto& seen = *new std::map<std::pair<int, cudaStream_t>, unsigned>;
+        const std::lock_guard<std::mutex> lock(mutex);
+        unsigned& last = seen[{device, stream}];
+        if (static_cast<int>(count - last) <= 0) return GRAWA_OK;      // (another thread's report may have seen more)
+        last = count;
+        return GRAWA_ERR_TIMEOUT;
+    } catch (const std::bad_alloc&) {
+        return cuda_fail(cudaErrorMemoryAllocation, what);
+    }
 }
 
 }  // namespace replica

@@ -79,9 +79,19 @@ def attention_backward(dtype=1, dout=T[6], q=T[0], k=T[1], v=T[2], out=T[3], lse
 
 
 @pytest.mark.parametrize("kw", SHAPE_REFUSALS + [dict(dout=None), dict(lse=None), dict(dq=None, dk=None, dv=None), dict(dk=None), dict(dv=None), dict(dq=T[0]),
-                                                 dict(dk=T[1]), dict(dv=T[8]), dict(dv=T[4]), dict(dq=T[6]), dict(dq=table(0x80_0000_0008))], ids=str)
+                                                 dict(dk=T[1]), dict(dv=T[8]), dict(dv=T[4]), dict(dq=T[6]), dict(dq=table(0x80_0000_0008)), dict(ws=T[0][0]),
+                                                 dict(ws=T[7][0])], ids=str)
 def test_attention_backward_refusals(kw):
     assert attention_backward(**kw) == BAD
+
+
+def test_attention_scratch():
+    size = grawa.grawa_window_attention_backward_workspace_bytes
+    need = size(10, 4, 2)
+    assert need > 0 and size(-1, 4, 2) == 0 and size(10, 0, 2) == 0 and size(10, 4, 65) == 0 and size(10, 4, 0) == 0
+    for kw in (dict(ws=None), dict(ws=WS + 16), dict(ws_bytes=need - 1)):
+        assert attention_backward(**kw) == NO_SPACE, kw
+    assert attention_forward(rows=0) == OK and attention_backward(rows=0, ws=None) == OK
 
 
 def test_binding_refuses_tensors_it_cannot_pass():
