@@ -460,7 +460,8 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void *cons
                                              grawa_stream_t stream);
 
 /* 0 on invalid arguments. */
-size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int M);
+size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                                       int64_t sinks, int M);
 
 /* As grawa_gated_ffn_status and grawa_selftest_gated_ffn_wait, for the attention calls: their kernels' bounded waits. */
 grawa_status grawa_window_attention_status(grawa_stream_t stream);

@@ -135,7 +135,7 @@ def library() -> ctypes.CDLL:
     lib.grawa_window_attention_forward.restype = ci
     lib.grawa_window_attention_backward.argtypes = [ci] + [vp] * 10 + [i64] * 13 + [ci, cf, vp, sz, vp]
     lib.grawa_window_attention_backward.restype = ci
-    lib.grawa_window_attention_backward_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.grawa_window_attention_backward_workspace_bytes.argtypes = [i64] * 5 + [ci]
     lib.grawa_window_attention_backward_workspace_bytes.restype = sz
     lib.grawa_window_attention_status.argtypes = [vp]
     lib.grawa_window_attention_status.restype = ci
@@ -763,14 +763,14 @@ def grawa_window_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, *, offs
             raise ValueError(f"{name}: expected the row stride of {other}")
     keep = workspace
     if keep is None:
-        keep = _scratch(None, lib.grawa_window_attention_backward_workspace_bytes(rows, heads, M), stream)
+        keep = _scratch(None, lib.grawa_window_attention_backward_workspace_bytes(rows, heads, kv_heads, dim, sinks, M), stream)
     status = lib.grawa_window_attention_backward(code, gt, qt, kt, vt, ot, lt, dqt, dkt, dvt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4,
                                                  os >> 4, M, dim ** -0.5 if scale is None else scale, *_scratch_args(keep, dev), _stream_on(stream, dev))
     _raise(status, "grawa_window_attention_backward")
 
 
-def grawa_window_attention_backward_workspace_bytes(rows: int, q_heads: int, M: int) -> int:
-    return int(library().grawa_window_attention_backward_workspace_bytes(rows, q_heads, M))
+def grawa_window_attention_backward_workspace_bytes(rows: int, q_heads: int, kv_heads: int, head_dim: int, sinks: int, M: int) -> int:
+    return int(library().grawa_window_attention_backward_workspace_bytes(rows, q_heads, kv_heads, head_dim, sinks, M))
 
 
 def grawa_window_attention_status(stream=None) -> int:

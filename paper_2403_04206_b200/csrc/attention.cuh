@@ -42,6 +42,8 @@ struct TileArgs {
     const float *lse, *delta;               // backward: [worker][head][pitch], lse in units of log 2
     const float* longest;                   // backward, half precision: [worker][2], the squared length of the longest row of dout, of v
     long long pitch;
+    float* partial;                         // backward, where chunks of queries are set apart (or NULL): [worker][key head][chunk][dv, dk][first key][dim]
+    int chunks, far;                        // far: this launch is of the chunks
     int first_worker, workers;
 };
 
@@ -190,10 +192,19 @@ __device__ __forceinline__ unsigned seen_keys(const Keys& k, int j, int limit)
     return bits_between(k.lo - j, hi - j) | bits_between(k.start - j, min(k.sinks_end - 1, hi) - j);
 }
 
-// A row of results on its way from tensor memory: `cols` columns at `from` (a multiple of 32), times f, to memory where there are
-// elements; whether all were finite.
+// 8 results to memory.
 template <typename T>
-__device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T* to, int elements, bool valid)
+__device__ __forceinline__ void store_eight(T* to, const float* v) { *reinterpret_cast<uint4*>(to) = pack<T>(v); }
+__device__ __forceinline__ void store_eight(float* to, const float* v)
+{
+    reinterpret_cast<uint4*>(to)[0] = pack<float>(v);
+    reinterpret_cast<uint4*>(to)[1] = pack<float>(v + 4);
+}
+
+// A row of results on its way from tensor memory: `cols` columns at `from` (a multiple of 32), with what `add` adds to the 32 from
+// a column on, times f, to memory where there are elements; whether all were finite.
+template <typename T, typename F>
+__device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T* to, int elements, bool valid, const F& add)
 {
     bool fine = true;
 #pragma unroll 1
@@ -203,13 +214,16 @@ __device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T
         tensor_wait(r);
         float v[32];
 #pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+        add(v, c);
+#pragma unroll
         for (int e = 0; e < 32; ++e) {
-            v[e] = __uint_as_float(r[e]) * f;
+            v[e] *= f;
             fine = fine && fabsf(v[e]) <= 3.0e38f;
         }
 #pragma unroll
         for (int e = 0; e < 32; e += 8)
-            if (valid && c + e < elements) *reinterpret_cast<uint4*>(to + c + e) = pack<T>(v + e);
+            if (valid && c + e < elements) store_eight(to + c + e, v + e);
     }
     return fine;
 }
@@ -400,7 +414,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             __syncwarp();
             order_after();
             T* to = static_cast<T*>(a.to[0].p[m]) + row * a.out_stride + static_cast<long long>(h) * a.dim;
-            const bool fine = store_result<T>(tmem_o + at, DP, 1.0f / total, to, a.dim, valid);
+            const bool fine = store_result(tmem_o + at, DP, 1.0f / total, to, a.dim, valid, [](float (&)[32], int) {});
             if (valid && a.to[1].p[m]) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + row] = (top + log2f(total)) * kLn2;
             __syncwarp();
             for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1) attention_row<T>(a, m, h, r0 + warp * 32 + __ffs(todo) - 1);
@@ -488,15 +502,29 @@ __device__ __forceinline__ int grad_exponent(const TileArgs& t, int m)
     return max(-100, min(100, 14 - ilogbf(most)));
 }
 
-constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, two groups that take steps in turn; 8: copies, 9: products
-constexpr int kStep = 64;                   // rows of a step
-template <int DP> constexpr int kBackwardStages = DP == 128 ? 4 : 6;
-template <int DP> constexpr int kSlotBytes = 2 * kStep * DP * 2;                   // two operands
-template <int DP> constexpr int kBackwardSmem = 2 * kTile * DP * 2 + kBackwardStages<DP> * (kSlotBytes<DP> + 2 * kStep * 4) + 1024;
+// The gradient of a sequence's first keys runs over all of its queries.  So that no tile walks much longer than the others, the
+// queries are cut into chunks at multiples of kChunk rows, and those from row far_from() on are left to CTAs that take one chunk
+// each, with the sequence's first keys as their tile, and write sums in fp32; the tiles that hold those keys add them.  (2 x 16384
+// tokens, 16 query heads on 4 of 128, a window of 1024, 4 first keys: 1370 us without, when a window without first keys took 724.)
+constexpr int kChunk = 1024;
+__device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& s)
+{
+    const long long reach = static_cast<long long>(s.start) + a.sinks + a.left;
+    return static_cast<int>(min((reach + kChunk - 1) / kChunk * kChunk, 0x7fffffffll));
+}
 
-// KEYS: dk and dv of a tile of keys, walking over queries; else dq of a tile of queries, walking over keys.  Tensor memory: the
-// sums in columns 0 to 255 (dv, dk; or dq), then for each of the two groups 64 columns of scores (then P) and 64 of
-// dP (then dS).
+constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
+constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
+template <bool KEYS> constexpr int kSlotsU = KEYS ? 2 : 3;                        // of the operand that the scores take
+constexpr int kSlotsW = 2;                                                         // of the one that dP takes
+template <int DP, bool KEYS> constexpr int kBackwardSmem = (2 + kSlotsU<KEYS> + kSlotsW) * kTile * DP * 2 + (KEYS ? kSlotsU<KEYS> * 2 * kStep * 4 : 0) + 1024;
+
+// KEYS: dk and dv of a tile of keys, walking over queries; else dq of a tile of queries, walking over keys.  The scores of a
+// step are S = X U^T and dP = Y W^T with the tile's own X and Y; its sums take P W (dv) and dS U (dk, or dq).  While the
+// tensor cores work on one of them, the warps turn the other into an operand.
+//
+// Tensor memory, in columns: KEYS: dv 0, dk 128, S (then P) 256, dP (then dS) 384.  Else dq 0, S (then dS) 128 and 256 in turn, dP 384.
+// A warp's half of an operand stands where its half of the scores stood.
 template <typename T, int DP, bool KEYS>
 __global__ void __launch_bounds__(kBackwardThreads, 1)
 attention_backward_kernel(const __grid_constant__ TileArgs t)
@@ -504,24 +532,30 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     constexpr unsigned long long kLimit = kAttentionWaitNs;
     constexpr bool kHalf = TypeCode<T>::value == 0;
     constexpr float kWeightExponent = kHalf ? 14.0f : 0.0f;               // of two, on P in half precision
-    constexpr int kStages = kBackwardStages<DP>, kSlot = kSlotBytes<DP>, kOwn = kTile * DP * 2, kHalves = DP / 64;
+    constexpr int kU = kSlotsU<KEYS>, kW = kSlotsW, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS ? 1 : 2;
+    constexpr unsigned kTmemSum = KEYS ? 128 : 0, kTmemScores = KEYS ? 256 : 128, kTmemGrads = 384;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 7];
+    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 8];
     __shared__ unsigned tmem_slot, spoiled[2][4];
     __shared__ int gave_up;
     __shared__ Reach reach;
 
-    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + 2 * kOwn, stats = ring + kStages * kSlot;
+    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring_u = own + 2 * kBytes, ring_w = ring_u + kU * kBytes, stats = ring_w + kW * kBytes;
     const float* stats_at = reinterpret_cast<const float*>(raw + (stats - smem_address(raw)));
-    const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, scored = loaded + 8, weighted = scored + 16,
-                   summed = weighted + 16, drain = summed + 8;
+    const unsigned full_u = smem_address(bars), empty_u = full_u + 8 * kU, full_w = empty_u + 8 * kU, empty_w = full_w + 8 * kW, loaded = empty_w + 8 * kW,
+                   scored = loaded + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8, drain = summed + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
         reach_init(reach);
-        for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
+        for (int s = 0; s < kU; ++s) { barrier_init(full_u + 8 * s, 1); barrier_init(empty_u + 8 * s, 1); }
+        for (int s = 0; s < kW; ++s) { barrier_init(full_w + 8 * s, 1); barrier_init(empty_w + 8 * s, 1); }
         barrier_init(loaded, 1);
-        for (int b = 0; b < 2; ++b) { barrier_init(scored + 8 * b, 1); barrier_init(weighted + 8 * b, 4); }
+        barrier_init(scored, 1);                              // S of a step (in each of its places) is there
+        barrier_init(scored + 8, 1);
+        barrier_init(graded, 1);                              // dP is there
+        barrier_init(weighted, 8);                            // P is there (KEYS)
+        barrier_init(differed, 8);                            // dS is there
         barrier_init(summed, 1);
         barrier_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -538,89 +572,123 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
     const int turn = static_cast<int>(blockIdx.x) / per, tile = KEYS ? turn : tiles - 1 - turn;    // the longest walks first, without a window
     const int w = static_cast<int>(blockIdx.x) % per / heads, h = static_cast<int>(blockIdx.x) % heads;
-    const int m = t.first_worker + w, r0 = tile * kTile, kv = KEYS ? h : h / a.group;
-    const int row = r0 + static_cast<int>(threadIdx.x) % kTile, group = warp / 4;
+    const int m = t.first_worker + w, kv = KEYS ? h : h / a.group, half = warp / 4;
+    const bool far = KEYS && t.far;                           // a chunk of queries and the first keys of the sequence that it begins in
+    const Sequence chunk = far ? sequence_of(a, m, turn * kChunk) : Sequence{0, 0};
+    const int r0 = far ? chunk.start : tile * kTile, row = r0 + static_cast<int>(threadIdx.x) % kTile;
     bool valid = false;
     Keys keys{};
+    int from_chunk = 0, to_chunk = 0;                         // chunks whose sums are added to this row's
     if (warp < 8) {
-        const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
-        valid = s.start < s.end;
-        if (valid && KEYS) {
-            const Queries q = queries_of(a, s, row);
-            keys = Keys{q.lo, q.hi, 0, 0};
-        } else if (valid) {
-            keys = keys_of(a, s, row);
+        if (far) {
+            valid = chunk.start < chunk.end && turn * kChunk >= far_from(a, chunk) && row < chunk.end && row - chunk.start < a.sinks;
+            keys = Keys{turn * kChunk, min(turn * kChunk + kChunk, chunk.end) - 1, 0, 0};
+        } else {
+            const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
+            valid = s.start < s.end;
+            if (valid && KEYS) {
+                const Queries q = queries_of(a, s, row);
+                keys = Keys{q.lo, q.hi, s.start, 0};
+                if (t.partial && row - s.start < a.sinks && far_from(a, s) < s.end) {
+                    keys.hi = far_from(a, s) - 1;
+                    from_chunk = far_from(a, s) / kChunk;
+                    to_chunk = (s.end - 1) / kChunk + 1;
+                }
+            } else if (valid) {
+                keys = keys_of(a, s, row);
+            }
         }
         if (warp < 4) reach_add(reach, valid, keys.lo, keys.hi, keys.start);
     }
     __syncthreads();
     const Reach all = reach;
     const KeyWalk walk(all, a.sinks, kStep);
-    // Queries are walked in steps that start at multiples of 64 rows, where the rows of lse and delta start on 256 bytes.
-    const int first = KEYS ? all.min_lo / kStep * kStep : 0, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
+    // Queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes.
+    const int first = KEYS ? all.min_lo / 64 * 64 : 0, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
     const int steps = KEYS ? turns * a.group : walk.steps;
     const auto row_of = [&](int i) { return KEYS ? first + i % turns * kStep : walk.row(i, kStep); };
     const auto head_of = [&](int i) { return KEYS ? h * a.group + i / turns : kv; };
 
-    int fills = 0;                                            // of the copying thread
+    int fills_u = 0, fills_w = 0;                             // of the copying thread
     if (warp == 8 && lane == 0 && steps > 0) {
-        barrier_expect(loaded, 2 * kOwn);
+        const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
 #pragma unroll
-        for (int i = 0; i < 4 * kHalves; ++i) {               // k and v, or q and dout
-            const int which = i / (2 * kHalves), j = i % (2 * kHalves);
-            copy_box(own + i * kBoxBytes, &t.map[KEYS ? 1 + which : 3 * which][w], j / 2 * 64, h, r0 + j % 2 * kBox, loaded);
-        }
-        for (; fills < steps; ++fills) {
-            const int s = fills % kStages, r = row_of(fills), hs = head_of(fills);
-            if (fills >= kStages && !tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) break;
-            barrier_expect(full + 8 * s, kSlot + (KEYS ? 2 * kStep * 4 : 0));
-#pragma unroll
-            for (int i = 0; i < 2 * kHalves; ++i) {           // q and dout, or k and v
-                const int which = i / kHalves;
-                copy_box(ring + s * kSlot + i * kBoxBytes, &t.map[KEYS ? 3 * which : 1 + which][w], i % kHalves * 64, hs, r, full + 8 * s);
-            }
+            for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
+        };
+        barrier_expect(loaded, 2 * kBytes);
+        copy_tile(own, &t.map[KEYS ? 1 : 0][w], h, r0, loaded);              // X: k or q
+        copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][w], h, r0, loaded);     // Y: v or dout
+        for (int i = 0; i < steps; ++i) {
+            const int u = i % kU, v = i % kW, r = row_of(i), hs = head_of(i);
+            if (i >= kU && !tile_wait<kLimit>(empty_u + 8 * u, (i / kU - 1) & 1, &gave_up)) break;
+            barrier_expect(full_u + 8 * u, kBytes + (KEYS ? 2 * kStep * 4 : 0));
+            copy_tile(ring_u + u * kBytes, &t.map[KEYS ? 0 : 1][w], hs, r, full_u + 8 * u);
             if (KEYS) {
                 const long long from = (static_cast<long long>(m) * a.heads + hs) * t.pitch + r;
-                copy_floats(stats + s * 2 * kStep * 4, t.lse + from, kStep * 4, full + 8 * s);
-                copy_floats(stats + s * 2 * kStep * 4 + kStep * 4, t.delta + from, kStep * 4, full + 8 * s);
+                copy_floats(stats + u * 2 * kStep * 4, t.lse + from, kStep * 4, full_u + 8 * u);
+                copy_floats(stats + u * 2 * kStep * 4 + kStep * 4, t.delta + from, kStep * 4, full_u + 8 * u);
             }
+            ++fills_u;
+            if (i >= kW && !tile_wait<kLimit>(empty_w + 8 * v, (i / kW - 1) & 1, &gave_up)) break;
+            barrier_expect(full_w + 8 * v, kBytes);
+            copy_tile(ring_w + v * kBytes, &t.map[KEYS ? 3 : 2][w], hs, r, full_w + 8 * v);
+            ++fills_w;
         }
     } else if (warp == 9 && lane == 0 && steps > 0) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kStep >> 3) << 17, kSums = kTypes | 1u << 16 | (DP >> 3) << 17;
         bool ok = tile_wait<kLimit>(loaded, 0, &gave_up);
-        const unsigned long long dx = matrix_descriptor(own, 16), dy = matrix_descriptor(own + kOwn, 16);
-        const auto scores = [&](int i) {
-            const int s = i % kStages, b = i & 1;
-            ok = ok && tile_wait<kLimit>(full + 8 * s, (i / kStages) & 1, &gave_up);
-            if (!ok) return;
+        const auto await = [&](unsigned bar, int phase) {
+            ok = ok && tile_wait<kLimit>(bar, phase & 1, &gave_up);
             order_after();
-            const unsigned long long du = matrix_descriptor(ring + s * kSlot, 16), dw = matrix_descriptor(ring + s * kSlot + kSlot / 2, 16);
-            const unsigned to = tmem + 256 + b * 128;
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-                mma_shared(to, dx + ((k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4), du + ((k / 4 * kBoxBytes + k % 4 * 32) >> 4), kScores, k > 0);
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-                mma_shared(to + 64, dy + ((k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4), dw + ((k / 4 * kBoxBytes + k % 4 * 32) >> 4), kScores, k > 0);
-            mma_done(scored + 8 * b);
+            return ok;
         };
-        scores(0);
-        for (int i = 0; i < steps && ok; ++i) {
-            const int s = i % kStages, b = i & 1;
-            if (i + 1 < steps) scores(i + 1);
-            ok = ok && tile_wait<kLimit>(weighted + 8 * b, (i >> 1) & 1, &gave_up);
-            if (!ok) break;
-            order_after();
-            const unsigned long long du = matrix_descriptor(ring + s * kSlot, kBoxBytes), dw = matrix_descriptor(ring + s * kSlot + kSlot / 2, kBoxBytes);
-            const unsigned from = tmem + 256 + b * 128;
-            if (KEYS) {
+        // The scores of a step: both operands in shared memory, the sum along the head's elements.
+        const auto scores = [&](unsigned to, unsigned tile_at, unsigned slot) {
+            const unsigned long long x = matrix_descriptor(tile_at, 16), y = matrix_descriptor(slot, 16);
 #pragma unroll
-                for (int k = 0; k < kStep / 16; ++k) mma_tensor(tmem, from + k * 8, dw + k * (2048 >> 4), kSums, i > 0 || k > 0);
+            for (int k = 0; k < DP / 16; ++k) {
+                const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
+                mma_shared(to, x + at, y + at, kScores, k > 0);
             }
+        };
+        // What a step adds to a sum: 128 columns of scores as 16-bit operands in two halves, the sum along the step's rows.
+        const auto add = [&](unsigned to, unsigned from, unsigned slot, bool more) {
+            const unsigned long long y = matrix_descriptor(slot, 2 * kBoxBytes);
 #pragma unroll
-            for (int k = 0; k < kStep / 16; ++k) mma_tensor(tmem + (KEYS ? 128 : 0), from + 64 + k * 8, du + k * (2048 >> 4), kSums, i > 0 || k > 0);
-            mma_done(empty + 8 * s);
+            for (int k = 0; k < kStep / 16; ++k) mma_tensor(to, from + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), kSums, more || k > 0);
+        };
+        const auto step_s = [&](int i) {
+            if (i >= steps || !await(full_u + 8 * (i % kU), i / kU)) return;
+            scores(tmem + kTmemScores + i % kScoreSets * 128, own, ring_u + i % kU * kBytes);
+            mma_done(scored + 8 * (i % kScoreSets));
+        };
+        const auto step_p = [&](int i) {
+            if (i >= steps || !await(full_w + 8 * (i % kW), i / kW)) return;
+            scores(tmem + kTmemGrads, own + kBytes, ring_w + i % kW * kBytes);
+            mma_done(graded);
+            if (!KEYS) mma_done(empty_w + 8 * (i % kW));
+        };
+        step_s(0);
+        step_p(0);
+        if (!KEYS) step_s(1);
+        for (int i = 0; i < steps && ok; ++i) {
+            if (KEYS) {
+                if (!await(weighted, i)) break;
+                add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > 0);
+                mma_done(empty_w + 8 * (i % kW));
+                step_s(i + 1);
+                if (!await(differed, i)) break;
+                add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > 0);
+                mma_done(empty_u + 8 * (i % kU));
+                step_p(i + 1);
+            } else {
+                if (!await(differed, i)) break;
+                step_p(i + 1);
+                add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > 0);
+                mma_done(empty_u + 8 * (i % kU));
+                step_s(i + 2);
+            }
         }
         if (ok) mma_done(summed);
         else {
@@ -639,82 +707,130 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             delta = t.delta[from];
         }
         bool ok = true;
-        for (int i = group; i < steps && ok; i += 2) {
-            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(scored + 8 * group, (i >> 1) & 1, &gave_up));
-            if (!ok) break;
+        const auto await = [&](unsigned bar, int phase) {
+            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
             __syncwarp();
             order_after();
-            const unsigned from = tmem + 256 + group * 128 + at;
+            return ok;
+        };
+        for (int i = 0; i < steps; ++i) {
+            const unsigned s_at = tmem + kTmemScores + i % kScoreSets * 128 + half * 64 + at, g_at = tmem + kTmemGrads + half * 64 + at;
             const int r = row_of(i), limit = !KEYS && i < walk.sink_steps ? all.min_lo : 0x7fffffff;
             const bool masked = (!KEYS && i < walk.sink_steps) || r < all.max_lo || r + kStep - 1 > all.min_hi;
-            const float* column = stats_at + i % kStages * 2 * kStep;
+            const float* column = stats_at + i % kU * 2 * kStep + half * 64;
+            if (!await(scored + 8 * (i % kScoreSets), i / kScoreSets)) break;
+            if (KEYS && !await(full_u + 8 * (i % kU), i / kU)) break;          // (long past: for the sight of lse and delta)
+            float p[2][32];
+            unsigned seen[2] = {~0u, ~0u};
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                unsigned s[32], g[32], p[16], d[16];
-                tensor_load(from + q * 32, s);
-                tensor_load(from + 64 + q * 32, g);
+                unsigned s[32];
+                tensor_load(s_at + q * 32, s);
                 tensor_wait(s);
-                tensor_wait(g);
-                float v[32], x[32];
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                    float l[4] = {lse, lse, lse, lse}, dl[4] = {delta, delta, delta, delta};
+                    float l[4] = {lse, lse, lse, lse};
                     if (KEYS) {
-                        const float4 u = *reinterpret_cast<const float4*>(column + q * 32 + e), y = *reinterpret_cast<const float4*>(column + kStep + q * 32 + e);
+                        const float4 u = *reinterpret_cast<const float4*>(column + q * 32 + e);
                         l[0] = u.x - kWeightExponent; l[1] = u.y - kWeightExponent; l[2] = u.z - kWeightExponent; l[3] = u.w - kWeightExponent;
-                        dl[0] = y.x; dl[1] = y.y; dl[2] = y.z; dl[3] = y.w;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[q][e + j] = exp2_fast(fmaf(__uint_as_float(s[e + j]), c, -l[j]));
+                }
+                if (masked) {
+                    const int from = r + half * 64 + q * 32;
+                    seen[q] = KEYS ? bits_between(keys.lo - from, keys.hi - from) : seen_keys(keys, from, limit);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(seen[q] >> e & 1)) p[q][e] = 0.0f;
+                }
+                if (KEYS) {
+                    unsigned o[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = pack_pair(p[q][2 * e], p[q][2 * e + 1], T{});
+                    tensor_store(s_at + q * 16, o);
+                }
+            }
+            if (KEYS) {
+                tensor_stored();
+                order_before();
+                __syncwarp();
+                if (lane == 0) arrive_here(weighted);
+            }
+            if (!await(graded, i)) break;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                unsigned g[32], o[16];
+                tensor_load(g_at + q * 32, g);
+                tensor_wait(g);
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    float d[4] = {delta, delta, delta, delta};
+                    if (KEYS) {
+                        const float4 u = *reinterpret_cast<const float4*>(column + kStep + q * 32 + e);
+                        d[0] = u.x; d[1] = u.y; d[2] = u.z; d[3] = u.w;
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        v[e + j] = exp2_fast(fmaf(__uint_as_float(s[e + j]), c, -l[j]));
-                        x[e + j] = v[e + j] * (__uint_as_float(g[e + j]) - dl[j]);
-                        if (KEYS && kHalf) x[e + j] *= to_grad;
+                        float x = p[q][e + j] * (__uint_as_float(g[e + j]) - d[j]);
+                        if (KEYS && kHalf) x *= to_grad;
+                        p[q][e + j] = x;
                     }
                 }
-                if (masked) {
-                    const unsigned seen = KEYS ? bits_between(keys.lo - r - q * 32, keys.hi - r - q * 32) : seen_keys(keys, r + q * 32, limit);
+                if (masked) {                                 // (0 times what is not finite)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (!(seen >> e & 1)) v[e] = x[e] = 0.0f;
+                        if (!(seen[q] >> e & 1)) p[q][e] = 0.0f;
                 }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    if (KEYS) p[e] = pack_pair(v[2 * e], v[2 * e + 1], T{});
-                    d[e] = pack_pair(x[2 * e], x[2 * e + 1], T{});
-                }
-                if (KEYS) tensor_store(from + q * 16, p);
-                tensor_store(from + 64 + q * 16, d);
+                for (int e = 0; e < 16; ++e) o[e] = pack_pair(p[q][2 * e], p[q][2 * e + 1], T{});
+                tensor_store((KEYS ? g_at : s_at) + q * 16, o);
             }
             tensor_stored();
             order_before();
             __syncwarp();
-            if (lane == 0) arrive_here(weighted + 8 * group);
+            if (lane == 0) arrive_here(differed);
         }
-        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(summed, 0, &gave_up));
-        if (ok) {
-            __syncwarp();
-            order_after();
+        if (ok && await(summed, 0)) {
             const float of_grad = a.scale * (kHalf ? exp2f(static_cast<float>(-exponent)) : 1.0f);
             bool fine = true;
-            if (KEYS) {                                       // one group dv, the other dk
-                const int which = group ? 1 : 2;
-                T* to = static_cast<T*>(a.to[which].p[m]) + row * (group ? a.k_stride : a.v_stride) + static_cast<long long>(h) * a.dim;
-                fine = store_result<T>(tmem + group * 128 + at, DP, group ? of_grad : exp2f(-kWeightExponent), to, a.dim, valid);
+            if (KEYS) {                                       // half of the warps dv, the others dk
+                const long long partial_row = static_cast<long long>(a.sinks) * a.dim, partial_chunk = 2 * partial_row;
+                const long long partial_head = (static_cast<long long>(m) * a.kv_heads + h) * t.chunks * partial_chunk + half * partial_row;
+                const auto add = [&](float (&v)[32], int col) {
+                    for (int k = from_chunk; k < to_chunk; ++k) {
+                        const float* more = t.partial + partial_head + k * partial_chunk + static_cast<long long>(row - keys.start) * a.dim + col;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            if (col + e < a.dim) {
+                                const float4 x = *reinterpret_cast<const float4*>(more + e);
+                                v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
+                            }
+                    }
+                };
+                if (far) {
+                    float* to = t.partial + partial_head + turn * partial_chunk + static_cast<long long>(row - chunk.start) * a.dim;
+                    store_result(tmem + half * 128 + at, DP, 1.0f, to, a.dim, valid, [](float (&)[32], int) {});
+                } else {
+                    T* to = static_cast<T*>(a.to[half ? 1 : 2].p[m]) + row * (half ? a.k_stride : a.v_stride) + static_cast<long long>(h) * a.dim;
+                    fine = store_result(tmem + half * 128 + at, DP, half ? of_grad : exp2f(-kWeightExponent), to, a.dim, valid, add);
+                }
             } else {                                          // half of the columns each
-                T* to = static_cast<T*>(a.to[0].p[m]) + row * a.q_stride + static_cast<long long>(h) * a.dim + group * (DP / 2);
-                fine = store_result<T>(tmem + group * (DP / 2) + at, DP / 2, of_grad, to, a.dim - group * (DP / 2), valid);
+                T* to = static_cast<T*>(a.to[0].p[m]) + row * a.q_stride + static_cast<long long>(h) * a.dim + half * (DP / 2);
+                fine = store_result(tmem + half * (DP / 2) + at, DP / 2, of_grad, to, a.dim - half * (DP / 2), valid, [](float (&)[32], int) {});
             }
             const unsigned todo = __ballot_sync(0xffffffffu, valid && !fine);
-            if (lane == 0) spoiled[group][warp % 4] = todo;
+            if (lane == 0) spoiled[half][warp % 4] = todo;
         }
     }
     __syncwarp();
     order_before();
     __syncthreads();
     order_after();
-    if (gave_up && fills > 0) {                               // copies in flight write shared memory: none is left behind
+    if (gave_up && fills_u > 0) {                             // copies in flight write shared memory: none is left behind
         tile_wait<kLimit>(loaded, 0, nullptr);
-        for (int f = max(0, fills - kStages); f < fills; ++f) tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
+        for (int f = max(0, fills_u - kU); f < fills_u; ++f) tile_wait<kLimit>(full_u + 8 * (f % kU), (f / kU) & 1, nullptr);
+        for (int f = max(0, fills_w - kW); f < fills_w; ++f) tile_wait<kLimit>(full_w + 8 * (f % kW), (f / kW) & 1, nullptr);
     }
     if (warp == 9) tensor_free<512>(tmem);
     if (warp < 4)

@@ -98,7 +98,7 @@ template <typename Kernel>
 static grawa_status launch_tiles(Kernel kernel, const TileArgs& t, int heads, int threads, int smem, cudaStream_t stream)
 {
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    return launch(kernel, dim3(static_cast<unsigned>(ceil_div(t.a.rows, kTile) * heads * t.workers)), threads, smem, stream, t);
+    return launch(kernel, dim3(static_cast<unsigned>((t.far ? t.chunks : ceil_div(t.a.rows, kTile)) * heads * t.workers)), threads, smem, stream, t);
 }
 template <typename T>
 static grawa_status launch_forward(const TileArgs& t, cudaStream_t stream)
@@ -110,23 +110,27 @@ template <typename T, bool KEYS>
 static grawa_status launch_backward(const TileArgs& t, cudaStream_t stream)
 {
     const int heads = KEYS ? t.a.kv_heads : t.a.heads;
-    return t.a.dim <= 64 ? launch_tiles(attention_backward_kernel<T, 64, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<64>, stream)
-                         : launch_tiles(attention_backward_kernel<T, 128, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<128>, stream);
+    return t.a.dim <= 64 ? launch_tiles(attention_backward_kernel<T, 64, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<64, KEYS>, stream)
+                         : launch_tiles(attention_backward_kernel<T, 128, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<128, KEYS>, stream);
 }
 
-// The places of a backward call's scratch: lse and delta of every row, and the longest rows.
+// The places of a backward call's scratch: lse and delta of every row, the longest rows, and the sums of chunks of queries for the
+// first keys.
 struct AttentionScratch {
-    int64_t pitch;
-    size_t lse, delta, longest, bytes;                        // offsets, and the whole
+    int64_t pitch, chunks;                                    // chunks: 0 where none are set apart
+    size_t delta, longest, partial, bytes;                    // offsets (lse stands first), and the whole
 };
-static AttentionScratch attention_scratch(int64_t rows, int64_t q_heads, int M)
+// Chunks are set apart for up to a tile of first keys.  (Where the window leaves no query beyond the first chunk, none has work.)
+static AttentionScratch attention_scratch(int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t sinks, int M)
 {
     AttentionScratch s{};
-    s.pitch = ceil_div(rows, kStep) * kStep;
+    s.pitch = ceil_div(rows, 64) * 64 + 64;                   // a step of queries starts at a multiple of 64 rows
+    s.chunks = sinks > 0 && sinks <= kTile && rows > kChunk ? ceil_div(rows, kChunk) : 0;
     const size_t table = static_cast<size_t>(M) * q_heads * s.pitch * sizeof(float);        // a multiple of 256 bytes
     s.delta = table;
     s.longest = 2 * table;
-    s.bytes = 2 * table + (static_cast<size_t>(M) * 2 * sizeof(float) + 255) / 256 * 256;
+    s.partial = 2 * table + (static_cast<size_t>(M) * 2 * sizeof(float) + 255) / 256 * 256;
+    s.bytes = s.partial + static_cast<size_t>(M) * kv_heads * s.chunks * 2 * std::min<int64_t>(sinks, kTile) * head_dim * sizeof(float);
     return s;
 }
 
@@ -171,10 +175,11 @@ grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void* const
     return st;
 }
 
-size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int M)
+size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t sinks, int M)
 {
-    if (M < 1 || M > GRAWA_MAX_WORKERS || rows < 0 || rows > 0x7fffffff - 1024 || q_heads < 1 || q_heads > 0x7fff) return 0;
-    return attention_scratch(rows, q_heads, M).bytes;
+    if (M < 1 || M > GRAWA_MAX_WORKERS || rows < 0 || rows > 0x7fffffff - 1024 || q_heads < 1 || q_heads > 0x7fff || kv_heads < 1 || kv_heads > q_heads ||
+        head_dim < 8 || head_dim > 128 || sinks < 0) return 0;
+    return attention_scratch(rows, q_heads, kv_heads, head_dim, sinks, M).bytes;
 }
 
 grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* const* dout, const void* const* q, const void* const* k, const void* const* v,
@@ -193,14 +198,14 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* cons
         !b.add(reinterpret_cast<const void* const*>(lse), M, 1, q_heads * rows, q_heads * rows, 4, false)) return GRAWA_ERR_INVALID_ARG;
     if (dq && !add_heads(b, dq, s, q_heads, q_stride, true)) return GRAWA_ERR_INVALID_ARG;
     if (dk && (!add_heads(b, dk, s, kv_heads, k_stride, true) || !add_heads(b, dv, s, kv_heads, v_stride, true))) return GRAWA_ERR_INVALID_ARG;
-    const size_t need = grawa_window_attention_backward_workspace_bytes(rows, q_heads, M);
+    const AttentionScratch scratch = attention_scratch(rows, q_heads, kv_heads, head_dim, sinks, M);
+    const size_t need = scratch.bytes;
     if (need) {
         if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return GRAWA_ERR_WORKSPACE;
         const void* ws = workspace;
         if (!b.add(&ws, 1, 1, static_cast<int64_t>(need), static_cast<int64_t>(need), 1, true)) return GRAWA_ERR_INVALID_ARG;
     }
     if (b.clash()) return GRAWA_ERR_INVALID_ARG;
-    const AttentionScratch scratch = attention_scratch(rows, q_heads, M);
     char* const base = static_cast<char*>(workspace);
     TileArgs t{};
     t.a = attention_args(s, q, k, v);
@@ -214,13 +219,17 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* cons
     t.delta = reinterpret_cast<float*>(base + scratch.delta);
     t.longest = dtype == GRAWA_F16 ? reinterpret_cast<float*>(base + scratch.longest) : nullptr;
     t.pitch = scratch.pitch;
+    t.chunks = static_cast<int>(scratch.chunks);
+    t.partial = t.chunks > 0 && int64_t{t.a.left} + t.a.sinks < rows - kChunk ? reinterpret_cast<float*>(base + scratch.partial) : nullptr;
     StatsArgs stats{t.a, reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + scratch.delta),
                     dtype == GRAWA_F16 ? reinterpret_cast<unsigned*>(base + scratch.longest) : nullptr, scratch.pitch};
     if (stats.longest) GRAWA_CUDA_TRY(cudaMemsetAsync(stats.longest, 0, static_cast<size_t>(M) * 2 * sizeof(float), stream));
     grawa_status st = dtype == GRAWA_BF16 ? attention_stats<__nv_bfloat16>(stats, M, stream) : attention_stats<__half>(stats, M, stream);
     for (int first = 0; first < M && st == GRAWA_OK; first += kAttentionWorkers) {
         st = set_workers(t, s, first, std::min(kAttentionWorkers, M - first));
-        if (st == GRAWA_OK && dk) st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, true>(t, stream) : launch_backward<__half, true>(t, stream);
+        for (t.far = t.partial ? 1 : 0; t.far >= 0 && st == GRAWA_OK && dk; --t.far)
+            st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, true>(t, stream) : launch_backward<__half, true>(t, stream);
+        t.far = 0;
         if (st == GRAWA_OK && dq) st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, false>(t, stream) : launch_backward<__half, false>(t, stream);
     }
     return st;

@@ -87,8 +87,11 @@ def test_attention_backward_refusals(kw):
 
 def test_attention_scratch():
     size = grawa.grawa_window_attention_backward_workspace_bytes
-    need = size(10, 4, 2)
-    assert need > 0 and size(-1, 4, 2) == 0 and size(10, 0, 2) == 0 and size(10, 4, 65) == 0 and size(10, 4, 0) == 0
+    need = size(10, 4, 2, 64, 1, 2)
+    assert need > 0 and size(2000, 4, 2, 64, 1, 2) > size(2000, 4, 2, 64, 0, 2) == size(2000, 4, 2, 64, 129, 2)
+    for bad in ((-1, 4, 2, 64, 1, 2), (10, 0, 2, 64, 1, 2), (10, 4, 0, 64, 1, 2), (10, 4, 2, 0, 1, 2), (10, 4, 2, 64, -1, 2), (10, 4, 2, 64, 1, 0),
+                (10, 4, 2, 64, 1, 65)):
+        assert size(*bad) == 0
     for kw in (dict(ws=None), dict(ws=WS + 16), dict(ws_bytes=need - 1)):
         assert attention_backward(**kw) == NO_SPACE, kw
     assert attention_forward(rows=0) == OK and attention_backward(rows=0, ws=None) == OK

@@ -89,6 +89,9 @@ CASES = [
     dict(rows=650, heads=2, kv_heads=2, dim=128, period=1),                                     # sequences of one token
     dict(rows=650, heads=8, kv_heads=2, dim=128, period=640, left=300, scale=1.0),              # sharp rows
     dict(rows=2050, heads=1, kv_heads=1, dim=128, left=ALL),
+    dict(rows=3500, heads=2, kv_heads=1, dim=64, left=100, sinks=4),                            # first keys whose queries lie in more than one chunk
+    dict(rows=3500, heads=2, kv_heads=2, dim=128, left=300, right=5, sinks=128, lengths=[[200, 3000, 300], [5, 1000, 2490]]),
+    dict(rows=3300, heads=1, kv_heads=1, dim=64, left=0, sinks=200, period=1600),
 ]
 
 
@@ -157,7 +160,7 @@ def test_parts_alone_and_the_callers_scratch():
     want = [t.clone() for t in c.dq + c.dk + c.dv]
     for t in c.dq + c.dk + c.dv:
         t.fill_(3.0)
-    need = grawa.grawa_window_attention_backward_workspace_bytes(300, 4, 2)
+    need = grawa.grawa_window_attention_backward_workspace_bytes(300, 4, 2, 64, 1, 2)
     scratch = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")       # NaN, in every type
     args = (c.dout, c.q, c.k, c.v, c.out, c.lse)
     grawa.grawa_window_attention_backward(*args, None, c.dk, c.dv, workspace=scratch[:need], **c.window)
