@@ -39,7 +39,7 @@ constexpr int kAttentionWorkers = 16;       // workers a launch (their tensor ma
 struct TileArgs {
     AttentionArgs a;
     CUtensorMap map[4][kAttentionWorkers];  // q, k, v, dout
-    const float *lse, *delta;               // backward: [worker][head][pitch], lse in units of log 2
+    const float *lse, *delta;               // backward: [worker][head][pitch], -lse in units of log 2, and -delta
     const float* longest;                   // backward, half precision: [worker][2], the squared length of the longest row of dout, of v
     long long pitch;
     float* partial;                         // backward, where chunks of queries are set apart (or NULL): [worker][key head][chunk][dv, dk][first key][dim]
@@ -86,6 +86,14 @@ __device__ __forceinline__ void mma_tensor(unsigned d, unsigned a, unsigned long
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(shape), "r"(add ? 1u : 0u)
         : "memory");
+}
+// One lane of a whole warp, the same every time.  Products are issued by warps that stay together up to here: what they are given is
+// then the same in all lanes to the compiler too, and goes to the tensor cores without a detour for each.
+__device__ __forceinline__ bool one_lane()
+{
+    unsigned one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
 }
 // Arrives when every product this thread has issued so far is done.
 __device__ __forceinline__ void mma_done(unsigned bar)
@@ -135,11 +143,84 @@ __device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[16
 }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two floats side by side, for instructions that take two at once.
+struct Two { unsigned long long v; };
+__device__ __forceinline__ Two two(float a, float b)
+{
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ Two two(const unsigned* bits) { return two(__uint_as_float(bits[0]), __uint_as_float(bits[1])); }
+__device__ __forceinline__ void apart(Two x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ Two fma_two(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two add_two(Two a, Two b)
+{
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two mul_two(Two a, Two b)
+{
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ float max_three(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two powers of two without the special function unit, which makes 16 a cycle and SM: x = n + f with n = floor x (Cody and Waite's
+// reduction), 2^f = 1 + f (c1 + ... + c5 f^4) with coefficients fitted for this file on [0, 1) by least squares whose weights
+// were moved until the relative errors were level (8e-8; 1.5e-7 with the roundings), and n added to the exponent.  Below -127 it is 0.
+// NaN gives a number past 3e38, as its bits lie.
+__device__ __forceinline__ void exp2_two(Two x, float& a, float& b)
+{
+    constexpr float kShift = 12582912.0f;                     // 1.5 * 2^23: the sum's last bits are the integer
+    float u, v;
+    apart(x, u, v);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-127.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-127.0f));
+    x = two(u, v);
+    Two n, f, p;
+    asm("add.rm.f32x2 %0, %1, %2;" : "=l"(n.v) : "l"(x.v), "l"(two(kShift, kShift).v));
+    f = fma_two(add_two(n, two(-kShift, -kShift)), two(-1.0f, -1.0f), x);
+    p = fma_two(f, two(0.0018671303987503052f, 0.0018671303987503052f), two(0.009017029777169228f, 0.009017029777169228f));
+    p = fma_two(f, p, two(0.05579991266131401f, 0.05579991266131401f));
+    p = fma_two(f, p, two(0.24016444385051727f, 0.24016444385051727f));
+    p = fma_two(f, p, two(0.6931512951850891f, 0.6931512951850891f));
+    p = fma_two(f, p, two(1.0f, 1.0f));
+    float s, t;
+    apart(n, s, t);
+    apart(p, u, v);
+    a = __uint_as_float(__float_as_uint(u) + (__float_as_uint(s) << 23));
+    b = __uint_as_float(__float_as_uint(v) + (__float_as_uint(t) << 23));
+}
+// Powers of two of pair `pair` of a run of them: some pairs go by the polynomial, so that the units work side by side.
+template <int EVERY>
+__device__ __forceinline__ void exp2_shared(int pair, Two x, float& a, float& b)
+{
+    if (EVERY > 0 && pair % (EVERY > 0 ? EVERY : 1) == EVERY - 1) {
+        exp2_two(x, a, b);
+    } else {
+        apart(x, a, b);
+        a = exp2_fast(a);
+        b = exp2_fast(b);
+    }
 }
 
 // Bits [lo, hi] of a word, either end of which may lie outside it.
@@ -232,6 +313,7 @@ __device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T
 
 // DP: elements of a head as the products take them, 64 or 128 (what lies behind the head's end is zero).  Two CTAs an SM, so
 // that the scores' products of one run beside the exponentials of the other.
+constexpr int kForwardPolynomial = 4;       // one in so many pairs of exponentials goes by the polynomial
 constexpr int kForwardThreads = 192;        // warps 0 to 3: rows, 4: copies, 5: products
 template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 5;
 template <int DP> constexpr int kForwardSmem = (1 + kForwardStages<DP>) * kTile * DP * 2 + 1024;
@@ -252,7 +334,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + kBytes;
     const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, scored = loaded + 8, weighted = scored + 8,
                    summed = weighted + 8, drain = summed + 8;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
         reach_init(reach);
@@ -301,43 +383,48 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
             for (int i = 0; i < 2 * kHalves; ++i) copy_box(ring + s * kBytes + i * kBoxBytes, &t.map[1 + fills % 2][w], i / 2 * 64, kv, j + i % 2 * kBox, full + 8 * s);
         }
-    } else if (warp == 5 && lane == 0 && steps > 0) {
+    } else if (warp == 5 && steps > 0) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kTile >> 3) << 17, kValues = kTypes | 1u << 16 | (DP >> 3) << 17;
-        bool ok = tile_wait<kLimit>(loaded, 0, &gave_up);
-        const unsigned long long dq = matrix_descriptor(own, 16);
-        const auto wait_fill = [&](int f) {
-            ok = ok && tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, &gave_up);
+        bool ok = true;
+        const auto await = [&](unsigned bar, int phase) {
+            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
             order_after();
             return ok;
         };
-        const auto scores = [&](int i) {
-            const unsigned long long dk = matrix_descriptor(ring + 2 * i % kStages * kBytes, 16);
+        const auto step_s = [&](int i) {
+            const int s = 2 * i % kStages;
+            if (i >= steps || !await(full + 8 * s, 2 * i / kStages)) return;
+            const unsigned long long dq = matrix_descriptor(own, 16), dk = matrix_descriptor(ring + s * kBytes, 16);
+            if (one_lane()) {
 #pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-                const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
-                mma_shared(tmem_s, dq + at, dk + at, kScores, k > 0);
+                for (int k = 0; k < DP / 16; ++k) {
+                    const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
+                    mma_shared(tmem_s, dq + at, dk + at, kScores, k > 0);
+                }
+                mma_done(empty + 8 * s);
+                mma_done(scored);
             }
-            mma_done(empty + 8 * (2 * i % kStages));
-            mma_done(scored);
+            __syncwarp();
         };
-        if (wait_fill(0)) scores(0);
+        await(loaded, 0);
+        step_s(0);
         for (int i = 0; i < steps && ok; ++i) {
-            ok = tile_wait<kLimit>(weighted, i & 1, &gave_up);
-            if (!wait_fill(2 * i + 1)) break;
             const int s = (2 * i + 1) % kStages;
+            if (!await(full + 8 * s, (2 * i + 1) / kStages) || !await(weighted, i)) break;
             const unsigned long long dv = matrix_descriptor(ring + s * kBytes, 2 * kBoxBytes);
+            if (one_lane()) {
 #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k) mma_tensor(tmem_o, tmem_s + k * 8, dv + k * (2048 >> 4), kValues, i > 0 || k > 0);
-            mma_done(empty + 8 * s);
-            if (i + 1 < steps) {
-                if (wait_fill(2 * i + 2)) scores(i + 1);
-            } else {
-                mma_done(summed);
+                for (int k = 0; k < kTile / 16; ++k) mma_tensor(tmem_o, tmem_s + k * 8, dv + k * (2048 >> 4), kValues, i > 0 || k > 0);
+                mma_done(empty + 8 * s);
+                if (i + 1 == steps) mma_done(summed);
             }
+            __syncwarp();
+            step_s(i + 1);
         }
         if (!ok) {
-            mma_done(drain);
+            if (one_lane()) mma_done(drain);
+            __syncwarp();
             tile_wait<kLimit>(drain, 0, nullptr);
         }
     } else if (warp < 4 && steps > 0) {
@@ -369,7 +456,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int e = 0; e < 32; ++e) most[e % 4] = fmaxf(most[e % 4], __uint_as_float(s[q][e]));
+                for (int e = 0; e < 32; e += 2) most[e / 2 % 4] = max_three(most[e / 2 % 4], __uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1]));
             const float here = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c;
             const bool grows = here > top + 8.0f;             // (from -infinity: always)
             if (__any_sync(0xffffffffu, grows)) {
@@ -389,21 +476,22 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 }
             }
             const float ref = top == -INFINITY ? 0.0f : top;  // nothing seen yet: exp2 of -infinity is to be zero, not NaN
-            float sum[2] = {};
+            Two sum[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                unsigned p[32];
+            for (int q = 0; q < 4; ++q) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float x = exp2_fast(fmaf(__uint_as_float(s[2 * q + e / 16][e % 16 * 2]), c, -ref));
-                    const float y = exp2_fast(fmaf(__uint_as_float(s[2 * q + e / 16][e % 16 * 2 + 1]), c, -ref));
-                    sum[0] += x;
-                    sum[1] += y;
-                    p[e] = pack_pair(x, y, T{});
+                for (int e = 0; e < 16; ++e) {
+                    float x, y;
+                    exp2_shared<kForwardPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), two(-ref, -ref)), x, y);
+                    sum[e % 2] = add_two(sum[e % 2], two(x, y));
+                    s[q][e] = pack_pair(x, y, T{});
                 }
-                tensor_store(tmem_s + at + q * 32, p);
+                tensor_store(tmem_s + at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
             }
-            total += sum[0] + sum[1];
+            float parts[4];
+            apart(sum[0], parts[0], parts[1]);
+            apart(sum[1], parts[2], parts[3]);
+            total += (parts[0] + parts[1]) + (parts[2] + parts[3]);
             tensor_stored();
             order_before();
             __syncwarp();
@@ -433,8 +521,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 
 // ------------------------------------------------------------------ backward
 
-// lse (in units of log 2) and delta = dout out of every row, in rows of `pitch`, a multiple of 64: rows that belong to no sequence, or to no
-// row at all, get infinity (P = 0) and 0.  For half precision also the longest rows of dout and v, from the last kv_heads
+// -lse (in units of log 2) and -delta = -dout out of every row, in rows of `pitch`, a multiple of 64: rows that belong to no sequence,
+// or to no row at all, get -infinity (P = 0) and 0.  For half precision also the longest rows of dout and v, from the last kv_heads
 // CTAs along y.  A CTA takes 64 rows of one head, 16 lanes a row.
 struct StatsArgs {
     AttentionArgs a;
@@ -478,7 +566,7 @@ attention_stats_kernel(const __grid_constant__ StatsArgs t)
         }
         dot = lanes_sum<16>(dot);
         if (t.longest) longest = fmaxf(longest, lanes_sum<16>(square));    // (NaN does not count: such rows are done again)
-        if (!values && word == 0) deltas[group + 16 * i] = in ? dot : 0.0f;
+        if (!values && word == 0) deltas[group + 16 * i] = in ? -dot : 0.0f;
     }
     if (t.longest && word == 0) atomicMax(&most, __float_as_uint(longest));
     __syncthreads();
@@ -487,7 +575,7 @@ attention_stats_kernel(const __grid_constant__ StatsArgs t)
         const long long at = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
         const bool in = row >= begin && row < end;
         t.delta[at] = deltas[threadIdx.x];
-        t.lse[at] = in ? lse_of(a, m, h, row) : INFINITY;
+        t.lse[at] = in ? -lse_of(a, m, h, row) : -INFINITY;
     }
     if (t.longest && threadIdx.x == 0) atomicMax(t.longest + 2 * m + (values ? 1 : 0), most);
 }
@@ -515,6 +603,7 @@ __device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& 
 
 constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
+constexpr int kPolynomial = 2;              // one in so many pairs of exponentials goes by the polynomial
 template <bool KEYS> constexpr int kSlotsU = KEYS ? 2 : 3;                        // of the operand that the scores take
 constexpr int kSlotsW = 2;                                                         // of the one that dP takes
 template <int DP, bool KEYS> constexpr int kBackwardSmem = (2 + kSlotsU<KEYS> + kSlotsW) * kTile * DP * 2 + (KEYS ? kSlotsU<KEYS> * 2 * kStep * 4 : 0) + 1024;
@@ -544,7 +633,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     const float* stats_at = reinterpret_cast<const float*>(raw + (stats - smem_address(raw)));
     const unsigned full_u = smem_address(bars), empty_u = full_u + 8 * kU, full_w = empty_u + 8 * kU, empty_w = full_w + 8 * kW, loaded = empty_w + 8 * kW,
                    scored = loaded + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8, drain = summed + 8;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
         reach_init(reach);
@@ -634,12 +723,12 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             copy_tile(ring_w + v * kBytes, &t.map[KEYS ? 3 : 2][w], hs, r, full_w + 8 * v);
             ++fills_w;
         }
-    } else if (warp == 9 && lane == 0 && steps > 0) {
+    } else if (warp == 9 && steps > 0) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kStep >> 3) << 17, kSums = kTypes | 1u << 16 | (DP >> 3) << 17;
-        bool ok = tile_wait<kLimit>(loaded, 0, &gave_up);
+        bool ok = true;
         const auto await = [&](unsigned bar, int phase) {
-            ok = ok && tile_wait<kLimit>(bar, phase & 1, &gave_up);
+            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
             order_after();
             return ok;
         };
@@ -659,40 +748,70 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             for (int k = 0; k < kStep / 16; ++k) mma_tensor(to, from + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), kSums, more || k > 0);
         };
         const auto step_s = [&](int i) {
-            if (i >= steps || !await(full_u + 8 * (i % kU), i / kU)) return;
-            scores(tmem + kTmemScores + i % kScoreSets * 128, own, ring_u + i % kU * kBytes);
-            mma_done(scored + 8 * (i % kScoreSets));
+            if (i >= steps || !ok) return;
+            if (one_lane()) {
+                scores(tmem + kTmemScores + i % kScoreSets * 128, own, ring_u + i % kU * kBytes);
+                mma_done(scored + 8 * (i % kScoreSets));
+            }
+            __syncwarp();
         };
         const auto step_p = [&](int i) {
-            if (i >= steps || !await(full_w + 8 * (i % kW), i / kW)) return;
-            scores(tmem + kTmemGrads, own + kBytes, ring_w + i % kW * kBytes);
-            mma_done(graded);
-            if (!KEYS) mma_done(empty_w + 8 * (i % kW));
+            if (i >= steps || !ok) return;
+            if (one_lane()) {
+                scores(tmem + kTmemGrads, own + kBytes, ring_w + i % kW * kBytes);
+                mma_done(graded);
+                if (!KEYS) mma_done(empty_w + 8 * (i % kW));
+            }
+            __syncwarp();
         };
+        // The waits for operands come in front of those for the warps, while earlier products run.
+        const auto wait_u = [&](int i) { if (i < steps) await(full_u + 8 * (i % kU), i / kU); };
+        const auto wait_w = [&](int i) { if (i < steps) await(full_w + 8 * (i % kW), i / kW); };
+        await(loaded, 0);
+        wait_u(0);
         step_s(0);
+        wait_w(0);
         step_p(0);
-        if (!KEYS) step_s(1);
+        if (!KEYS) {
+            wait_u(1);
+            step_s(1);
+        }
         for (int i = 0; i < steps && ok; ++i) {
             if (KEYS) {
+                wait_u(i + 1);
                 if (!await(weighted, i)) break;
-                add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > 0);
-                mma_done(empty_w + 8 * (i % kW));
+                if (one_lane()) {
+                    add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > 0);
+                    mma_done(empty_w + 8 * (i % kW));
+                }
+                __syncwarp();
                 step_s(i + 1);
+                wait_w(i + 1);
                 if (!await(differed, i)) break;
-                add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > 0);
-                mma_done(empty_u + 8 * (i % kU));
+                if (one_lane()) {
+                    add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > 0);
+                    mma_done(empty_u + 8 * (i % kU));
+                    if (i + 1 == steps) mma_done(summed);
+                }
+                __syncwarp();
                 step_p(i + 1);
             } else {
+                wait_w(i + 1);
                 if (!await(differed, i)) break;
+                if (one_lane()) {
+                    add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > 0);
+                    mma_done(empty_u + 8 * (i % kU));
+                    if (i + 1 == steps) mma_done(summed);
+                }
+                __syncwarp();
                 step_p(i + 1);
-                add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > 0);
-                mma_done(empty_u + 8 * (i % kU));
+                wait_u(i + 2);                                // (its slot has only been free since the step before's sum)
                 step_s(i + 2);
             }
         }
-        if (ok) mma_done(summed);
-        else {
-            mma_done(drain);
+        if (!ok) {
+            if (one_lane()) mma_done(drain);
+            __syncwarp();
             tile_wait<kLimit>(drain, 0, nullptr);
         }
     } else if (warp < 8 && steps > 0) {
@@ -703,7 +822,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         float lse = 0.0f, delta = 0.0f;
         if (!KEYS && valid) {
             const long long from = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
-            lse = t.lse[from] - static_cast<float>(exponent);  // P with dS's power of two
+            lse = t.lse[from] + static_cast<float>(exponent);  // P with dS's power of two
             delta = t.delta[from];
         }
         bool ok = true;
@@ -720,35 +839,39 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             const float* column = stats_at + i % kU * 2 * kStep + half * 64;
             if (!await(scored + 8 * (i % kScoreSets), i / kScoreSets)) break;
             if (KEYS && !await(full_u + 8 * (i % kU), i / kU)) break;          // (long past: for the sight of lse and delta)
-            float p[2][32];
+            Two p[2][16];
             unsigned seen[2] = {~0u, ~0u};
+            ulonglong2 columns = {0, 0};                      // what four neighbouring columns' queries share
+            {
+                unsigned s[2][32];
+                tensor_load(s_at, s[0]);
+                tensor_load(s_at + 32, s[1]);
+                tensor_wait(s[0]);
+                tensor_wait(s[1]);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                unsigned s[32];
-                tensor_load(s_at + q * 32, s);
-                tensor_wait(s);
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float l[4] = {lse, lse, lse, lse};
-                    if (KEYS) {
-                        const float4 u = *reinterpret_cast<const float4*>(column + q * 32 + e);
-                        l[0] = u.x - kWeightExponent; l[1] = u.y - kWeightExponent; l[2] = u.z - kWeightExponent; l[3] = u.w - kWeightExponent;
+                for (int q = 0; q < 2; ++q) {
+                    if (masked) {
+                        const int from = r + half * 64 + q * 32;
+                        seen[q] = KEYS ? bits_between(keys.lo - from, keys.hi - from) : seen_keys(keys, from, limit);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) p[q][e + j] = exp2_fast(fmaf(__uint_as_float(s[e + j]), c, -l[j]));
-                }
-                if (masked) {
-                    const int from = r + half * 64 + q * 32;
-                    seen[q] = KEYS ? bits_between(keys.lo - from, keys.hi - from) : seen_keys(keys, from, limit);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(seen[q] >> e & 1)) p[q][e] = 0.0f;
-                }
-                if (KEYS) {
-                    unsigned o[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = pack_pair(p[q][2 * e], p[q][2 * e + 1], T{});
-                    tensor_store(s_at + q * 16, o);
+                    for (int e = 0; e < 16; ++e) {
+                        Two shift = two(lse, lse);
+                        if (KEYS) {
+                            if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + q * 32 + 2 * e);
+                            shift.v = e % 2 ? columns.y : columns.x;
+                            if (kHalf) shift = add_two(shift, two(kWeightExponent, kWeightExponent));
+                        }
+                        float x, y;
+                        exp2_shared<kPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
+                        if (masked) {
+                            x = seen[q] >> (2 * e) & 1 ? x : 0.0f;
+                            y = seen[q] >> (2 * e + 1) & 1 ? y : 0.0f;
+                        }
+                        p[q][e] = two(x, y);
+                        s[q][e] = pack_pair(x, y, T{});
+                    }
+                    if (KEYS) tensor_store(s_at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
                 }
             }
             if (KEYS) {
@@ -758,33 +881,33 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 if (lane == 0) arrive_here(weighted);
             }
             if (!await(graded, i)) break;
+            {
+                unsigned g[2][32];
+                tensor_load(g_at, g[0]);
+                tensor_load(g_at + 32, g[1]);
+                tensor_wait(g[0]);
+                tensor_wait(g[1]);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                unsigned g[32], o[16];
-                tensor_load(g_at + q * 32, g);
-                tensor_wait(g);
+                for (int q = 0; q < 2; ++q) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    float d[4] = {delta, delta, delta, delta};
-                    if (KEYS) {
-                        const float4 u = *reinterpret_cast<const float4*>(column + kStep + q * 32 + e);
-                        d[0] = u.x; d[1] = u.y; d[2] = u.z; d[3] = u.w;
+                    for (int e = 0; e < 16; ++e) {
+                        Two shift = two(delta, delta);
+                        if (KEYS) {
+                            if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + kStep + q * 32 + 2 * e);
+                            shift.v = e % 2 ? columns.y : columns.x;
+                        }
+                        Two d = mul_two(p[q][e], add_two(two(g[q] + 2 * e), shift));
+                        if (KEYS && kHalf) d = mul_two(d, two(to_grad, to_grad));
+                        float x, y;
+                        apart(d, x, y);
+                        if (masked) {                         // (0 times what is not finite)
+                            x = seen[q] >> (2 * e) & 1 ? x : 0.0f;
+                            y = seen[q] >> (2 * e + 1) & 1 ? y : 0.0f;
+                        }
+                        g[q][e] = pack_pair(x, y, T{});
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float x = p[q][e + j] * (__uint_as_float(g[e + j]) - d[j]);
-                        if (KEYS && kHalf) x *= to_grad;
-                        p[q][e + j] = x;
-                    }
+                    tensor_store((KEYS ? g_at : s_at) + q * 16, reinterpret_cast<const unsigned(&)[16]>(g[q]));
                 }
-                if (masked) {                                 // (0 times what is not finite)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(seen[q] >> e & 1)) p[q][e] = 0.0f;
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = pack_pair(p[q][2 * e], p[q][2 * e + 1], T{});
-                tensor_store((KEYS ? g_at : s_at) + q * 16, o);
             }
             tensor_stored();
             order_before();
