@@ -68,6 +68,7 @@ __device__ __forceinline__ void copy_floats(unsigned dst, const float* from, uns
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // D (+)= A B^T for 16 steps along the sum, A in shared or in tensor memory.
 __device__ __forceinline__ void mma_shared(unsigned d, unsigned long long a, unsigned long long b, unsigned shape, bool add)
 {
@@ -273,40 +274,56 @@ __device__ __forceinline__ unsigned seen_keys(const Keys& k, int j, int limit)
     return bits_between(k.lo - j, hi - j) | bits_between(k.start - j, min(k.sinks_end - 1, hi) - j);
 }
 
+// 32 rows of results on their way from tensor memory to memory, a warp's own: columns [from_col, from_col + cols) of the row's
+// `elements`, at `tensor` on, with what `add` adds to the 32 values from a column on, times f.  A thread has a row, but whole
+// 128-byte rows are what memory takes well: 64 columns at a time pass through 4 KB of shared memory, in 16-byte pieces that are
+// permuted so that neither direction meets bank conflicts.  Rows without their bit in `valid` are not stored.  Returns whether
+// all of this thread's values were finite.
+template <typename T, typename F>
+__device__ __forceinline__ bool store_rows(unsigned tensor, int from_col, int cols, float f, unsigned char* stage, T* to, long long stride, int elements, unsigned valid,
+                                           const F& add)
+{
+    const int lane = threadIdx.x % 32, piece = lane % 8, first = lane / 8;
+    bool fine = true;
+#pragma unroll 1
+    for (int c = 0; c < cols; c += 64) {
+#pragma unroll
+        for (int q = 0; q < 64; q += 32) {
+            if (q >= cols) break;                             // (half of a 64-element head)
+            unsigned r[32];
+            tensor_load(tensor + c + q, r);
+            tensor_wait(r);
+            float v[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+            add(v, from_col + c + q);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                v[e] *= f;
+                fine = fine && fabsf(v[e]) <= 3.0e38f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<uint4*>(stage + lane * 128 + (((q / 8 + e) ^ (lane & 7)) * 16)) = pack<T>(v + 8 * e);
+        }
+        __syncwarp();
+        const int col = from_col + c + piece * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = first + 4 * i;
+            const uint4 word = *reinterpret_cast<const uint4*>(stage + row * 128 + ((piece ^ (row & 7)) * 16));
+            if (valid >> row & 1 && col < elements && c + piece * 8 < cols) *reinterpret_cast<uint4*>(to + row * stride + col) = word;
+        }
+        __syncwarp();
+    }
+    return fine;
+}
+
 // 8 results to memory.
-template <typename T>
-__device__ __forceinline__ void store_eight(T* to, const float* v) { *reinterpret_cast<uint4*>(to) = pack<T>(v); }
 __device__ __forceinline__ void store_eight(float* to, const float* v)
 {
     reinterpret_cast<uint4*>(to)[0] = pack<float>(v);
     reinterpret_cast<uint4*>(to)[1] = pack<float>(v + 4);
-}
-
-// A row of results on its way from tensor memory: `cols` columns at `from` (a multiple of 32), with what `add` adds to the 32 from
-// a column on, times f, to memory where there are elements; whether all were finite.
-template <typename T, typename F>
-__device__ __forceinline__ bool store_result(unsigned from, int cols, float f, T* to, int elements, bool valid, const F& add)
-{
-    bool fine = true;
-#pragma unroll 1
-    for (int c = 0; c < cols; c += 32) {
-        unsigned r[32];
-        tensor_load(from + c, r);
-        tensor_wait(r);
-        float v[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
-        add(v, c);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            v[e] *= f;
-            fine = fine && fabsf(v[e]) <= 3.0e38f;
-        }
-#pragma unroll
-        for (int e = 0; e < 32; e += 8)
-            if (valid && c + e < elements) store_eight(to + c + e, v + e);
-    }
-    return fine;
 }
 
 // ------------------------------------------------------------------ forward
@@ -346,17 +363,23 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
         barrier_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    const AttentionArgs& a = t.a;
+    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
+    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / per, w = static_cast<int>(blockIdx.x) % per / a.heads, h = static_cast<int>(blockIdx.x) % a.heads;
+    const int m = t.first_worker + w, r0 = tile * kTile, kv = h / a.group;     // the last rows, which see most, first
+    if (warp == 4 && lane < 3) prefetch_map(&t.map[lane][w]);
     if (warp == 5) tensor_alloc<256>(smem_address(&tmem_slot));
     order_before();
     __syncthreads();
     order_after();
     stream_order();
     const unsigned tmem = tmem_slot, tmem_s = tmem, tmem_o = tmem + 128;
+    if (!STARVED && warp == 4 && lane == 0) {                 // (whether or not any row belongs to a sequence)
+        barrier_expect(loaded, kBytes);
+#pragma unroll
+        for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][w], i / 2 * 64, h, r0 + i % 2 * kBox, loaded);
+    }
 
-    const AttentionArgs& a = t.a;
-    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
-    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / per, w = static_cast<int>(blockIdx.x) % per / a.heads, h = static_cast<int>(blockIdx.x) % a.heads;
-    const int m = t.first_worker + w, r0 = tile * kTile, kv = h / a.group;     // the last rows, which see most, first
     Keys keys{};
     bool valid = false;
     const int row = r0 + static_cast<int>(threadIdx.x);
@@ -373,9 +396,6 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 
     int fills = 0;                                            // of the copying thread
     if (!STARVED && warp == 4 && lane == 0 && steps > 0) {
-        barrier_expect(loaded, kBytes);
-#pragma unroll
-        for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][w], i / 2 * 64, h, r0 + i % 2 * kBox, loaded);
         for (; fills < 2 * steps; ++fills) {                  // k, v, k, v, ...
             const int s = fills % kStages, j = walk.row(fills / 2, kTile);
             if (fills >= kStages && !tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) break;
@@ -447,9 +467,10 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const unsigned seen = seen_keys(keys, j + q * 32, limit);
+                    if (__all_sync(0xffffffffu, seen == ~0u)) continue;
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (!(seen >> e & 1)) s[q][e] = 0xff800000u;       // -infinity
+                        if (!(seen & 1u << e)) s[q][e] = 0xff800000u;      // -infinity
                 }
             }
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -501,8 +522,10 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
         if (ok) {
             __syncwarp();
             order_after();
-            T* to = static_cast<T*>(a.to[0].p[m]) + row * a.out_stride + static_cast<long long>(h) * a.dim;
-            const bool fine = store_result(tmem_o + at, DP, 1.0f / total, to, a.dim, valid, [](float (&)[32], int) {});
+            // (the tile of q has done its part; a warp's rows of it are 4 KB of each half)
+            T* to = static_cast<T*>(a.to[0].p[m]) + static_cast<long long>(r0 + warp * 32) * a.out_stride + static_cast<long long>(h) * a.dim;
+            const bool fine = store_rows(tmem_o + at, 0, DP, 1.0f / total, raw + (own - smem_address(raw)) + warp * 4096, to, a.out_stride, a.dim,
+                                         __ballot_sync(0xffffffffu, valid), [](float (&)[32], int) {});
             if (valid && a.to[1].p[m]) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + row] = (top + log2f(total)) * kLn2;
             __syncwarp();
             for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1) attention_row<T>(a, m, h, r0 + warp * 32 + __ffs(todo) - 1);
@@ -512,7 +535,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     order_before();
     __syncthreads();
     order_after();
-    if (gave_up && fills > 0) {                               // copies in flight write shared memory: none is left behind
+    if (!STARVED && warp == 4 && lane == 0 && (gave_up || steps == 0)) {       // copies in flight write shared memory: none is left behind
         tile_wait<kLimit>(loaded, 0, nullptr);
         for (int f = max(0, fills - kStages); f < fills; ++f) tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
     }
@@ -650,6 +673,12 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (threadIdx.x < 8) spoiled[threadIdx.x / 4][threadIdx.x % 4] = 0;
+    const AttentionArgs& a = t.a;
+    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
+    const int turn = static_cast<int>(blockIdx.x) / per, tile = KEYS ? turn : tiles - 1 - turn;    // the longest walks first, without a window
+    const int w = static_cast<int>(blockIdx.x) % per / heads, h = static_cast<int>(blockIdx.x) % heads;
+    const int m = t.first_worker + w, kv = KEYS ? h : h / a.group, half = warp / 4;
+    if (warp == 8 && lane < 4) prefetch_map(&t.map[lane][w]);
     if (warp == 9) tensor_alloc<512>(smem_address(&tmem_slot));
     order_before();
     __syncthreads();
@@ -657,14 +686,18 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     stream_order();
     const unsigned tmem = tmem_slot;
 
-    const AttentionArgs& a = t.a;
-    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
-    const int turn = static_cast<int>(blockIdx.x) / per, tile = KEYS ? turn : tiles - 1 - turn;    // the longest walks first, without a window
-    const int w = static_cast<int>(blockIdx.x) % per / heads, h = static_cast<int>(blockIdx.x) % heads;
-    const int m = t.first_worker + w, kv = KEYS ? h : h / a.group, half = warp / 4;
     const bool far = KEYS && t.far;                           // a chunk of queries and the first keys of the sequence that it begins in
     const Sequence chunk = far ? sequence_of(a, m, turn * kChunk) : Sequence{0, 0};
     const int r0 = far ? chunk.start : tile * kTile, row = r0 + static_cast<int>(threadIdx.x) % kTile;
+    const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
+#pragma unroll
+        for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
+    };
+    if (warp == 8 && lane == 0) {                             // (whether or not any row belongs to a sequence)
+        barrier_expect(loaded, 2 * kBytes);
+        copy_tile(own, &t.map[KEYS ? 1 : 0][w], h, r0, loaded);              // X: k or q
+        copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][w], h, r0, loaded);     // Y: v or dout
+    }
     bool valid = false;
     Keys keys{};
     int from_chunk = 0, to_chunk = 0;                         // chunks whose sums are added to this row's
@@ -700,13 +733,6 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
 
     int fills_u = 0, fills_w = 0;                             // of the copying thread
     if (warp == 8 && lane == 0 && steps > 0) {
-        const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
-#pragma unroll
-            for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
-        };
-        barrier_expect(loaded, 2 * kBytes);
-        copy_tile(own, &t.map[KEYS ? 1 : 0][w], h, r0, loaded);              // X: k or q
-        copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][w], h, r0, loaded);     // Y: v or dout
         for (int i = 0; i < steps; ++i) {
             const int u = i % kU, v = i % kW, r = row_of(i), hs = head_of(i);
             if (i >= kU && !tile_wait<kLimit>(empty_u + 8 * u, (i / kU - 1) & 1, &gave_up)) break;
@@ -865,8 +891,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                         float x, y;
                         exp2_shared<kPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
                         if (masked) {
-                            x = seen[q] >> (2 * e) & 1 ? x : 0.0f;
-                            y = seen[q] >> (2 * e + 1) & 1 ? y : 0.0f;
+                            x = seen[q] & 1u << (2 * e) ? x : 0.0f;
+                            y = seen[q] & 2u << (2 * e) ? y : 0.0f;
                         }
                         p[q][e] = two(x, y);
                         s[q][e] = pack_pair(x, y, T{});
@@ -901,8 +927,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                         float x, y;
                         apart(d, x, y);
                         if (masked) {                         // (0 times what is not finite)
-                            x = seen[q] >> (2 * e) & 1 ? x : 0.0f;
-                            y = seen[q] >> (2 * e + 1) & 1 ? y : 0.0f;
+                            x = seen[q] & 1u << (2 * e) ? x : 0.0f;
+                            y = seen[q] & 2u << (2 * e) ? y : 0.0f;
                         }
                         g[q][e] = pack_pair(x, y, T{});
                     }
@@ -917,6 +943,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         if (ok && await(summed, 0)) {
             const float of_grad = a.scale * (kHalf ? exp2f(static_cast<float>(-exponent)) : 1.0f);
             bool fine = true;
+            const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
+            unsigned char* const stage = raw + (own - smem_address(raw)) + warp * 4096;        // (the tile's own operands have done their part)
             if (KEYS) {                                       // half of the warps dv, the others dk
                 const long long partial_row = static_cast<long long>(a.sinks) * a.dim, partial_chunk = 2 * partial_row;
                 const long long partial_head = (static_cast<long long>(m) * a.kv_heads + h) * t.chunks * partial_chunk + half * partial_row;
@@ -933,14 +961,23 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 };
                 if (far) {
                     float* to = t.partial + partial_head + turn * partial_chunk + static_cast<long long>(row - chunk.start) * a.dim;
-                    store_result(tmem + half * 128 + at, DP, 1.0f, to, a.dim, valid, [](float (&)[32], int) {});
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 32) {
+                        unsigned v[32];
+                        tensor_load(tmem + half * 128 + at + c, v);
+                        tensor_wait(v);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            if (valid && c + e < a.dim) store_eight(to + c + e, reinterpret_cast<const float*>(v + e));
+                    }
                 } else {
-                    T* to = static_cast<T*>(a.to[half ? 1 : 2].p[m]) + row * (half ? a.k_stride : a.v_stride) + static_cast<long long>(h) * a.dim;
-                    fine = store_result(tmem + half * 128 + at, DP, half ? of_grad : exp2f(-kWeightExponent), to, a.dim, valid, add);
+                    const long long stride = half ? a.k_stride : a.v_stride;
+                    T* to = static_cast<T*>(a.to[half ? 1 : 2].p[m]) + (r0 + warp % 4 * 32) * stride + static_cast<long long>(h) * a.dim;
+                    fine = store_rows(tmem + half * 128 + at, 0, DP, half ? of_grad : exp2f(-kWeightExponent), stage, to, stride, a.dim, rows_valid, add);
                 }
             } else {                                          // half of the columns each
-                T* to = static_cast<T*>(a.to[0].p[m]) + row * a.q_stride + static_cast<long long>(h) * a.dim + half * (DP / 2);
-                fine = store_result(tmem + half * (DP / 2) + at, DP / 2, of_grad, to, a.dim - half * (DP / 2), valid, [](float (&)[32], int) {});
+                T* to = static_cast<T*>(a.to[0].p[m]) + (r0 + warp % 4 * 32) * a.q_stride + static_cast<long long>(h) * a.dim;
+                fine = store_rows(tmem + half * (DP / 2) + at, half * (DP / 2), DP / 2, of_grad, stage, to, a.q_stride, a.dim, rows_valid, [](float (&)[32], int) {});
             }
             const unsigned todo = __ballot_sync(0xffffffffu, valid && !fine);
             if (lane == 0) spoiled[half][warp % 4] = todo;
@@ -950,7 +987,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     order_before();
     __syncthreads();
     order_after();
-    if (gave_up && fills_u > 0) {                             // copies in flight write shared memory: none is left behind
+    if (warp == 8 && lane == 0 && (gave_up || steps == 0)) {  // copies in flight write shared memory: none is left behind
         tile_wait<kLimit>(loaded, 0, nullptr);
         for (int f = max(0, fills_u - kU); f < fills_u; ++f) tile_wait<kLimit>(full_u + 8 * (f % kU), (f / kU) & 1, nullptr);
         for (int f = max(0, fills_w - kW); f < fills_w; ++f) tile_wait<kLimit>(full_w + 8 * (f % kW), (f / kW) & 1, nullptr);
