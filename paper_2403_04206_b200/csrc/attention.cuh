@@ -55,7 +55,7 @@ constexpr unsigned long long kAttentionWaitNs = 2000000000ull, kAttentionStarved
 template <unsigned long long LIMIT>
 __device__ __forceinline__ bool tile_wait(unsigned bar, unsigned parity, volatile int* gave_up)
 {
-    return bounded_wait<LIMIT>(bar, parity, gave_up, &g_attention_timeouts);
+    return bounded_wait<LIMIT, false>(bar, parity, gave_up, &g_attention_timeouts);
 }
 __device__ __forceinline__ void arrive_here(unsigned bar) { asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void copy_box(unsigned dst, const CUtensorMap* map, int element, int head, int row, unsigned bar)
@@ -127,6 +127,16 @@ __device__ __forceinline__ void tensor_load(unsigned at, unsigned (&r)[32])
 __device__ __forceinline__ void tensor_wait(unsigned (&r)[32])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : GRAWA_RW8(r, 0), GRAWA_RW8(r, 8), GRAWA_RW8(r, 16), GRAWA_RW8(r, 24) : : "memory");
+}
+__device__ __forceinline__ void tensor_load(unsigned at, unsigned (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : GRAWA_R8(r, 0), GRAWA_R8(r, 8)
+                 : "r"(at));
+}
+__device__ __forceinline__ void tensor_wait(unsigned (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : GRAWA_RW8(r, 0), GRAWA_RW8(r, 8) : : "memory");
 }
 __device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[32])
 {
@@ -237,17 +247,51 @@ __device__ __forceinline__ unsigned bits_between(int lo, int hi)
 // What the rows of a tile see, or are seen by, in all.
 struct Reach { int min_lo, max_lo, min_hi, max_hi, min_start; };
 
-__device__ __forceinline__ void reach_init(Reach& r) { r.min_lo = r.min_hi = r.min_start = 0x7fffffff, r.max_lo = r.max_hi = -1; }
-__device__ __forceinline__ void reach_add(Reach& r, bool valid, int lo, int hi, int start)    // a whole warp
+// Of the tile's rows [r0, r0 + 128), by a whole warp.  As sequences and windows only move forward, the ends come from few rows: the
+// first and the last that belong to a sequence, the first sequence's first row that is no first key, and the last sequence's
+// first row in the tile.  `rows` says of a row and its sequence what it sees.
+template <typename F>
+__device__ __forceinline__ Reach reach_of(const AttentionArgs& a, int m, int r0, int lane, const F& rows)
 {
-    const int big = 0x7fffffff;
-    const int a = __reduce_min_sync(0xffffffffu, valid ? lo : big), b = __reduce_max_sync(0xffffffffu, valid ? lo : -1);
-    const int c = __reduce_min_sync(0xffffffffu, valid ? hi : big), d = __reduce_max_sync(0xffffffffu, valid ? hi : -1);
-    const int e = __reduce_min_sync(0xffffffffu, valid ? start : big);
-    if (threadIdx.x % 32 == 0) {
-        atomicMin(&r.min_lo, a), atomicMax(&r.max_lo, b), atomicMin(&r.min_hi, c), atomicMax(&r.max_hi, d);
-        atomicMin(&r.min_start, e);
+    const long long* offsets = static_cast<const long long*>(a.offsets.p[m]);
+    int begin = r0, end = min(r0 + kTile, a.rows);            // the rows that belong to a sequence
+    if (offsets) {
+        begin = static_cast<int>(max(static_cast<long long>(begin), min(static_cast<long long>(end), offsets[0])));
+        end = static_cast<int>(min(static_cast<long long>(end), max(static_cast<long long>(begin), offsets[a.sequences])));
     }
+    const Sequence s = begin < end ? sequence_of(a, m, lane == 0 ? begin : end - 1) : Sequence{0, 0};
+    const Sequence first{__shfl_sync(0xffffffffu, s.start, 0), __shfl_sync(0xffffffffu, s.end, 0)}, last{__shfl_sync(0xffffffffu, s.start, 1), __shfl_sync(0xffffffffu, s.end, 1)};
+    const int inner = max(begin, a.sinks >= end - first.start ? end : first.start + a.sinks);
+    const int row = lane == 0 ? begin : lane == 1 ? end - 1 : lane == 2 ? (inner < min(end, first.end) ? inner : begin) : max(begin, last.start);
+    Keys k{};
+    const bool in = begin < end && rows(lane == 0 || lane == 2 ? first : last, row, k);
+    Reach r;
+    r.min_lo = __reduce_min_sync(0xffffffffu, in ? k.lo : 0x7fffffff), r.max_lo = __reduce_max_sync(0xffffffffu, in ? k.lo : -1);
+    r.min_hi = __reduce_min_sync(0xffffffffu, in ? k.hi : 0x7fffffff), r.max_hi = __reduce_max_sync(0xffffffffu, in ? k.hi : -1);
+    r.min_start = __reduce_min_sync(0xffffffffu, in ? k.start : 0x7fffffff);
+    return r;
+}
+// What queries see.
+struct QueryRows {
+    const AttentionArgs& a;
+    __device__ __forceinline__ bool operator()(const Sequence& s, int row, Keys& k) const
+    {
+        if (s.start >= s.end) return false;
+        k = keys_of(a, s, row);
+        return true;
+    }
+};
+template <typename F>
+__device__ __forceinline__ bool own_keys(const AttentionArgs& a, int m, int row, const F& rows, Keys& k)
+{
+    return rows(row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0}, row, k);
+}
+
+// The tiles of all heads and workers, those of one place in the rows side by side; each CTA takes one in `gridDim.x`, in an order that
+// turns round every time, so that walks that get shorter from place to place come to about the same for all CTAs.
+__device__ __forceinline__ int tile_of_round(int round)
+{
+    return round * static_cast<int>(gridDim.x) + static_cast<int>(round % 2 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
 }
 
 // The key rows that a tile of queries walks over, `step` rows at a time.
@@ -276,45 +320,45 @@ __device__ __forceinline__ unsigned seen_keys(const Keys& k, int j, int limit)
 
 // 32 rows of results on their way from tensor memory to memory, a warp's own: columns [from_col, from_col + cols) of the row's
 // `elements`, at `tensor` on, with what `add` adds to the 32 values from a column on, times f.  A thread has a row, but whole
-// 128-byte rows are what memory takes well: 64 columns at a time pass through 4 KB of shared memory, in 16-byte pieces that are
-// permuted so that neither direction meets bank conflicts.  Rows without their bit in `valid` are not stored.  Returns whether
+// sectors of neighbouring rows are what memory takes well: CHUNK columns at a time pass through 64 CHUNK bytes of shared memory, in
+// 16-byte pieces that are permuted against bank conflicts.  Rows without their bit in `valid` are not stored.  Returns whether
 // all of this thread's values were finite.
-template <typename T, typename F>
+template <typename T, int CHUNK, typename F>
 __device__ __forceinline__ bool store_rows(unsigned tensor, int from_col, int cols, float f, unsigned char* stage, T* to, long long stride, int elements, unsigned valid,
                                            const F& add)
 {
-    const int lane = threadIdx.x % 32, piece = lane % 8, first = lane / 8;
+    constexpr int kPieces = CHUNK / 8, kRows = 32 / kPieces, kTurn = 8 / kPieces;        // rows a store; rows in 128 bytes
+    const int lane = threadIdx.x % 32, piece = lane % kPieces, first = lane / kPieces;
     bool fine = true;
 #pragma unroll 1
-    for (int c = 0; c < cols; c += 64) {
+    for (int c = 0; c < cols; c += 32) {
+        unsigned r[32];
+        tensor_load(tensor + c, r);
+        tensor_wait(r);
+        float v[32];
 #pragma unroll
-        for (int q = 0; q < 64; q += 32) {
-            if (q >= cols) break;                             // (half of a 64-element head)
-            unsigned r[32];
-            tensor_load(tensor + c + q, r);
-            tensor_wait(r);
-            float v[32];
+        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+        add(v, from_col + c);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
-            add(v, from_col + c + q);
+        for (int e = 0; e < 32; ++e) {
+            v[e] *= f;
+            fine = fine && fabsf(v[e]) <= 3.0e38f;
+        }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                v[e] *= f;
-                fine = fine && fabsf(v[e]) <= 3.0e38f;
+        for (int k = 0; k < 32; k += CHUNK) {
+#pragma unroll
+            for (int e = 0; e < kPieces; ++e)
+                *reinterpret_cast<uint4*>(stage + lane * CHUNK * 2 + ((e ^ lane / kTurn % kPieces) * 16)) = pack<T>(v + k + 8 * e);
+            __syncwarp();
+            const int col = from_col + c + k + piece * 8;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int row = first + kRows * i;
+                const uint4 word = *reinterpret_cast<const uint4*>(stage + row * CHUNK * 2 + ((piece ^ row / kTurn % kPieces) * 16));
+                if (valid >> row & 1 && col < elements) *reinterpret_cast<uint4*>(to + row * stride + col) = word;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                *reinterpret_cast<uint4*>(stage + lane * 128 + (((q / 8 + e) ^ (lane & 7)) * 16)) = pack<T>(v + 8 * e);
+            __syncwarp();
         }
-        __syncwarp();
-        const int col = from_col + c + piece * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = first + 4 * i;
-            const uint4 word = *reinterpret_cast<const uint4*>(stage + row * 128 + ((piece ^ (row & 7)) * 16));
-            if (valid >> row & 1 && col < elements && c + piece * 8 < cols) *reinterpret_cast<uint4*>(to + row * stride + col) = word;
-        }
-        __syncwarp();
     }
     return fine;
 }
@@ -329,11 +373,14 @@ __device__ __forceinline__ void store_eight(float* to, const float* v)
 // ------------------------------------------------------------------ forward
 
 // DP: elements of a head as the products take them, 64 or 128 (what lies behind the head's end is zero).  Two CTAs an SM, so
-// that the scores' products of one run beside the exponentials of the other.
+// that the products of one run beside the exponentials of the other; each takes one tile after the other, and fetches the next one's
+// queries while it works.  Two threads share a row, one half of a step's scores each: what they wait for one after the other (scores,
+// their exponentials, the sum) bounds a CTA.
 constexpr int kForwardPolynomial = 4;       // one in so many pairs of exponentials goes by the polynomial
-constexpr int kForwardThreads = 192;        // warps 0 to 3: rows, 4: copies, 5: products
-template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 5;
-template <int DP> constexpr int kForwardSmem = (1 + kForwardStages<DP>) * kTile * DP * 2 + 1024;
+constexpr int kForwardThreads = 320;        // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
+template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 4;
+constexpr int kForwardChunk = 16;           // columns of results on their way
+template <int DP> constexpr int kForwardSmem = (1 + kForwardStages<DP>) * kTile * DP * 2 + 8 * 64 * kForwardChunk + 1024;
 
 // STARVED: for the self-test of the bounded waits only; nothing is copied, so that the first wait for operands runs out.
 template <typename T, int DP, bool STARVED = false>
@@ -343,67 +390,74 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     constexpr unsigned long long kLimit = STARVED ? kAttentionStarvedNs : kAttentionWaitNs;
     constexpr int kStages = kForwardStages<DP>, kBytes = kTile * DP * 2, kHalves = DP / 64;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 5];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 14];
     __shared__ unsigned tmem_slot;
     __shared__ int gave_up;
-    __shared__ Reach reach;
+    __shared__ float most_of[2][2][kTile], total_of[2][kTile];             // a row's largest score in each half, of two steps in turn; its sums
 
-    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + kBytes;
-    const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, scored = loaded + 8, weighted = scored + 8,
-                   summed = weighted + 8, drain = summed + 8;
+    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + kBytes, out = ring + kStages * kBytes;
+    const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, used = loaded + 8, scored = used + 8,
+                   weighted = scored + 8, summed = weighted + 8, drain = summed + 8, maxed = drain + 8, totaled = maxed + 32;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
-        reach_init(reach);
         for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
-        barrier_init(loaded, 1);
-        barrier_init(scored, 1);
-        barrier_init(weighted, 4);
-        barrier_init(summed, 1);
+        barrier_init(loaded, 1);                              // q is there
+        barrier_init(used, 1);                                // q has done its part
+        barrier_init(scored, 1);                              // S of a step is there
+        barrier_init(weighted, 8);                            // P is there
+        barrier_init(summed, 1);                              // O of a tile is there
         barrier_init(drain, 1);
+        for (int s = 0; s < 4; ++s) { barrier_init(maxed + 8 * s, 2); barrier_init(totaled + 8 * s, 2); }        // between the two warps of 32 rows
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    const AttentionArgs& a = t.a;
-    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
-    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / per, w = static_cast<int>(blockIdx.x) % per / a.heads, h = static_cast<int>(blockIdx.x) % a.heads;
-    const int m = t.first_worker + w, r0 = tile * kTile, kv = h / a.group;     // the last rows, which see most, first
-    if (warp == 4 && lane < 3) prefetch_map(&t.map[lane][w]);
-    if (warp == 5) tensor_alloc<256>(smem_address(&tmem_slot));
+    if (warp == 8 && lane < 3 * t.workers) prefetch_map(&t.map[lane % 3][lane / 3]);
+    if (warp == 9) tensor_alloc<256>(smem_address(&tmem_slot));
     order_before();
     __syncthreads();
     order_after();
     stream_order();
     const unsigned tmem = tmem_slot, tmem_s = tmem, tmem_o = tmem + 128;
-    if (!STARVED && warp == 4 && lane == 0) {                 // (whether or not any row belongs to a sequence)
-        barrier_expect(loaded, kBytes);
-#pragma unroll
-        for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][w], i / 2 * 64, h, r0 + i % 2 * kBox, loaded);
-    }
 
-    Keys keys{};
-    bool valid = false;
-    const int row = r0 + static_cast<int>(threadIdx.x);
-    if (warp < 4) {
-        const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
-        valid = s.start < s.end;
-        if (valid) keys = keys_of(a, s, row);
-        reach_add(reach, valid, keys.lo, keys.hi, keys.start);
-    }
-    __syncthreads();
-    const Reach all = reach;
-    const KeyWalk walk(all, a.sinks, kTile);
-    const int steps = STARVED ? 1 : walk.steps;
+    const AttentionArgs& a = t.a;
+    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile, units = tiles * per;
+    struct Place { int w, m, h, r0; };
+    const auto place_of = [&](int unit) {                     // the last rows, which see most, first
+        const int in = unit % per, w = in / a.heads;
+        return Place{w, t.first_worker + w, in % a.heads, (tiles - 1 - unit / per) * kTile};
+    };
+    int fills = 0, loads = 0;                                 // of the copying thread
 
-    int fills = 0;                                            // of the copying thread
-    if (!STARVED && warp == 4 && lane == 0 && steps > 0) {
-        for (; fills < 2 * steps; ++fills) {                  // k, v, k, v, ...
-            const int s = fills % kStages, j = walk.row(fills / 2, kTile);
-            if (fills >= kStages && !tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up)) break;
-            barrier_expect(full + 8 * s, kBytes);
+    if (!STARVED && warp == 8) {
+        bool ok = true;
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const Place at = place_of(unit);
+            const KeyWalk walk(reach_of(a, at.m, at.r0, lane, QueryRows{a}), a.sinks, kTile);
+            if (walk.steps == 0) continue;
+            if (lane == 0) {
+                ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
+                if (ok) {
+                    barrier_expect(loaded, kBytes);
 #pragma unroll
-            for (int i = 0; i < 2 * kHalves; ++i) copy_box(ring + s * kBytes + i * kBoxBytes, &t.map[1 + fills % 2][w], i / 2 * 64, kv, j + i % 2 * kBox, full + 8 * s);
+                    for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][at.w], i / 2 * 64, at.h, at.r0 + i % 2 * kBox, loaded);
+                    ++loads;
+                }
+                for (int i = 0; i < 2 * walk.steps && ok; ++i) {             // k, v, k, v, ...
+                    const int s = fills % kStages, j = walk.row(i / 2, kTile);
+                    ok = fills < kStages || tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up);
+                    if (!ok) break;
+                    barrier_expect(full + 8 * s, kBytes);
+#pragma unroll
+                    for (int b = 0; b < 2 * kHalves; ++b)
+                        copy_box(ring + s * kBytes + b * kBoxBytes, &t.map[1 + i % 2][at.w], b / 2 * 64, at.h / a.group, j + b % 2 * kBox, full + 8 * s);
+                    ++fills;
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
         }
-    } else if (warp == 5 && steps > 0) {
+    } else if (warp == 9) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kTile >> 3) << 17, kValues = kTypes | 1u << 16 | (DP >> 3) << 17;
         bool ok = true;
@@ -412,134 +466,171 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             order_after();
             return ok;
         };
-        const auto step_s = [&](int i) {
-            const int s = 2 * i % kStages;
-            if (i >= steps || !await(full + 8 * s, 2 * i / kStages)) return;
-            const unsigned long long dq = matrix_descriptor(own, 16), dk = matrix_descriptor(ring + s * kBytes, 16);
-            if (one_lane()) {
+        int n = 0, tile = 0;                                  // steps and tiles so far
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const Place at = place_of(unit);
+            const int steps = STARVED ? 1 : KeyWalk(reach_of(a, at.m, at.r0, lane, QueryRows{a}), a.sinks, kTile).steps;
+            if (steps == 0) continue;
+            const auto scores = [&](int i) {
+                const int f = 2 * (n + i), s = f % kStages;
+                if (i >= steps || !await(full + 8 * s, f / kStages)) return;
+                const unsigned long long dq = matrix_descriptor(own, 16), dk = matrix_descriptor(ring + s * kBytes, 16);
+                if (one_lane()) {
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
-                    mma_shared(tmem_s, dq + at, dk + at, kScores, k > 0);
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const unsigned along = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
+                        mma_shared(tmem_s, dq + along, dk + along, kScores, k > 0);
+                    }
+                    mma_done(empty + 8 * s);
+                    mma_done(scored);
+                    if (i + 1 == steps) mma_done(used);
                 }
-                mma_done(empty + 8 * s);
-                mma_done(scored);
-            }
-            __syncwarp();
-        };
-        await(loaded, 0);
-        step_s(0);
-        for (int i = 0; i < steps && ok; ++i) {
-            const int s = (2 * i + 1) % kStages;
-            if (!await(full + 8 * s, (2 * i + 1) / kStages) || !await(weighted, i)) break;
-            const unsigned long long dv = matrix_descriptor(ring + s * kBytes, 2 * kBoxBytes);
-            if (one_lane()) {
+                __syncwarp();
+            };
+            await(loaded, tile);
+            scores(0);
+            for (int i = 0; i < steps && ok; ++i) {
+                const int f = 2 * (n + i) + 1, s = f % kStages;
+                if (!await(full + 8 * s, f / kStages) || !await(weighted, n + i)) break;
+                const unsigned long long dv = matrix_descriptor(ring + s * kBytes, 2 * kBoxBytes);
+                if (one_lane()) {
 #pragma unroll
-                for (int k = 0; k < kTile / 16; ++k) mma_tensor(tmem_o, tmem_s + k * 8, dv + k * (2048 >> 4), kValues, i > 0 || k > 0);
-                mma_done(empty + 8 * s);
-                if (i + 1 == steps) mma_done(summed);
+                    for (int k = 0; k < kTile / 16; ++k) mma_tensor(tmem_o, tmem_s + k / 4 * 64 + k % 4 * 8, dv + k * (2048 >> 4), kValues, i > 0 || k > 0);
+                    mma_done(empty + 8 * s);
+                    if (i + 1 == steps) mma_done(summed);
+                }
+                __syncwarp();
+                scores(i + 1);
             }
-            __syncwarp();
-            step_s(i + 1);
+            n += steps;
+            ++tile;
         }
         if (!ok) {
             if (one_lane()) mma_done(drain);
             __syncwarp();
             tile_wait<kLimit>(drain, 0, nullptr);
         }
-    } else if (warp < 4 && steps > 0) {
-        const unsigned at = static_cast<unsigned>(warp * 32) << 16;        // this warp's lanes of tensor memory
+    } else if (warp < 8) {
+        const int quarter = warp % 4, half = warp / 4, line = quarter * 32 + lane;
+        const unsigned lanes = static_cast<unsigned>(quarter * 32) << 16, s_at = tmem_s + lanes + half * 64, o_at = tmem_o + lanes + half * (DP / 2);
+        unsigned char* const stage = raw + (out - smem_address(raw)) + warp * 64 * kForwardChunk;
         const float c = a.scale * kLog2e;
-        float top = -INFINITY, total = 0.0f;
         bool ok = true;
-        for (int i = 0; i < steps && ok; ++i) {
-            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(scored, i & 1, &gave_up));
-            if (!ok) break;
-            __syncwarp();
-            order_after();
-            unsigned s[4][32];
+        const auto await = [&](unsigned bar, int phase) {
+            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
+            return ok;
+        };
+        int n = 0, tile = 0;
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const Place at = place_of(unit);
+            const Reach all = reach_of(a, at.m, at.r0, lane, QueryRows{a});
+            const KeyWalk walk(all, a.sinks, kTile);
+            const int steps = STARVED ? 1 : walk.steps;
+            if (steps == 0) continue;
+            Keys keys{};
+            const bool valid = own_keys(a, at.m, at.r0 + line, QueryRows{a}, keys);
+            float top = -INFINITY, total = 0.0f;
+            for (int i = 0; i < steps; ++i, ++n) {
+                if (!await(scored, n)) break;
+                order_after();
+                unsigned s[2][32];
+                tensor_load(s_at, s[0]);
+                tensor_load(s_at + 32, s[1]);
+                tensor_wait(s[0]);
+                tensor_wait(s[1]);
+                const int j = walk.row(i, kTile), limit = i < walk.sink_steps ? all.min_lo : 0x7fffffff;
+                if (i < walk.sink_steps || j < all.max_lo || j + kTile - 1 > all.min_hi) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tensor_load(tmem_s + at + q * 32, s[q]);
+                    for (int q = 0; q < 2; ++q) {
+                        const unsigned seen = seen_keys(keys, j + half * 64 + q * 32, limit);
+                        if (__all_sync(0xffffffffu, seen == ~0u)) continue;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tensor_wait(s[q]);
-            const int j = walk.row(i, kTile), limit = i < walk.sink_steps ? all.min_lo : 0x7fffffff;
-            if (i < walk.sink_steps || j < all.max_lo || j + kTile - 1 > all.min_hi) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const unsigned seen = seen_keys(keys, j + q * 32, limit);
-                    if (__all_sync(0xffffffffu, seen == ~0u)) continue;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(seen & 1u << e)) s[q][e] = 0xff800000u;      // -infinity
-                }
-            }
-            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) most[e / 2 % 4] = max_three(most[e / 2 % 4], __uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1]));
-            const float here = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c;
-            const bool grows = here > top + 8.0f;             // (from -infinity: always)
-            if (__any_sync(0xffffffffu, grows)) {
-                const float f = grows ? exp2_fast(top - here) : 1.0f;
-                if (grows) top = here;
-                total *= f;
-                if (i > 0) {
-#pragma unroll 1
-                    for (int d = 0; d < DP; d += 32) {
-                        unsigned o[32];
-                        tensor_load(tmem_o + at + d, o);
-                        tensor_wait(o);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tensor_store(tmem_o + at + d, o);
+                        for (int e = 0; e < 32; ++e)
+                            if (!(seen & 1u << e)) s[q][e] = 0xff800000u;  // -infinity
                     }
                 }
-            }
-            const float ref = top == -INFINITY ? 0.0f : top;  // nothing seen yet: exp2 of -infinity is to be zero, not NaN
-            Two sum[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float x, y;
-                    exp2_shared<kForwardPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), two(-ref, -ref)), x, y);
-                    sum[e % 2] = add_two(sum[e % 2], two(x, y));
-                    s[q][e] = pack_pair(x, y, T{});
+                    for (int e = 0; e < 32; e += 2) most[e / 2 % 4] = max_three(most[e / 2 % 4], __uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1]));
+                most[0] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                most_of[n % 2][half][line] = most[0];
+                __syncwarp();
+                if (lane == 0) arrive_here(maxed + 8 * quarter);
+                if (!await(maxed + 8 * quarter, n)) break;
+                const float here = fmaxf(most[0], most_of[n % 2][1 - half][line]) * c;
+                const bool grows = here > top + 8.0f;         // (from -infinity: always)
+                if (__any_sync(0xffffffffu, grows)) {
+                    const float f = grows ? exp2_fast(top - here) : 1.0f;
+                    if (grows) top = here;
+                    total *= f;
+                    if (i > 0) {
+#pragma unroll 1
+                        for (int d = 0; d < DP / 2; d += 16) {
+                            unsigned o[16];
+                            tensor_load(o_at + d, o);
+                            tensor_wait(o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tensor_store(o_at + d, o);
+                        }
+                    }
                 }
-                tensor_store(tmem_s + at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
+                const float ref = top == -INFINITY ? 0.0f : top;             // nothing seen yet: exp2 of -infinity is to be zero, not NaN
+                Two sum[2] = {two(0.0f, 0.0f), two(0.0f, 0.0f)};
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float x, y;
+                        exp2_shared<kForwardPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), two(-ref, -ref)), x, y);
+                        sum[e % 2] = add_two(sum[e % 2], two(x, y));
+                        s[q][e] = pack_pair(x, y, T{});
+                    }
+                    tensor_store(s_at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
+                }
+                tensor_stored();
+                order_before();
+                __syncwarp();
+                if (lane == 0) arrive_here(weighted);
+                float parts[4];
+                apart(sum[0], parts[0], parts[1]);
+                apart(sum[1], parts[2], parts[3]);
+                total += (parts[0] + parts[1]) + (parts[2] + parts[3]);
             }
-            float parts[4];
-            apart(sum[0], parts[0], parts[1]);
-            apart(sum[1], parts[2], parts[3]);
-            total += (parts[0] + parts[1]) + (parts[2] + parts[3]);
-            tensor_stored();
-            order_before();
+            if (!ok) break;
+            total_of[half][line] = total;
             __syncwarp();
-            if (lane == 0) arrive_here(weighted);
-        }
-        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(summed, 0, &gave_up));
-        if (ok) {
-            __syncwarp();
+            if (lane == 0) arrive_here(totaled + 8 * quarter);
+            if (!await(totaled + 8 * quarter, tile) || !await(summed, tile)) break;
             order_after();
-            // (the tile of q has done its part; a warp's rows of it are 4 KB of each half)
-            T* to = static_cast<T*>(a.to[0].p[m]) + static_cast<long long>(r0 + warp * 32) * a.out_stride + static_cast<long long>(h) * a.dim;
-            const bool fine = store_rows(tmem_o + at, 0, DP, 1.0f / total, raw + (own - smem_address(raw)) + warp * 4096, to, a.out_stride, a.dim,
-                                         __ballot_sync(0xffffffffu, valid), [](float (&)[32], int) {});
-            if (valid && a.to[1].p[m]) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + row] = (top + log2f(total)) * kLn2;
+            total = total_of[0][line] + total_of[1][line];
+            T* to = static_cast<T*>(a.to[0].p[at.m]) + static_cast<long long>(at.r0 + quarter * 32) * a.out_stride + static_cast<long long>(at.h) * a.dim;
+            const bool fine = store_rows<T, kForwardChunk>(o_at, half * (DP / 2), DP / 2, 1.0f / total, stage, to, a.out_stride, a.dim,
+                                                           __ballot_sync(0xffffffffu, valid), [](float (&)[32], int) {});
+            order_before();
+            if (half == 0 && valid && a.to[1].p[at.m])
+                static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (top + log2f(total)) * kLn2;
             __syncwarp();
-            for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1) attention_row<T>(a, m, h, r0 + warp * 32 + __ffs(todo) - 1);
+            for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
+                attention_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, half * (DP / 2), half * (DP / 2) + DP / 2);
+            ++tile;
         }
     }
     __syncwarp();
     order_before();
     __syncthreads();
     order_after();
-    if (!STARVED && warp == 4 && lane == 0 && (gave_up || steps == 0)) {       // copies in flight write shared memory: none is left behind
-        tile_wait<kLimit>(loaded, 0, nullptr);
+    if (gave_up && loads > 0) {                               // copies in flight write shared memory: none is left behind
+        tile_wait<kLimit>(loaded, (loads - 1) & 1, nullptr);
         for (int f = max(0, fills - kStages); f < fills; ++f) tile_wait<kLimit>(full + 8 * (f % kStages), (f / kStages) & 1, nullptr);
     }
-    if (warp == 5) tensor_free<256>(tmem);
+    if (warp == 9) tensor_free<256>(tmem);
 }
 
 // ------------------------------------------------------------------ backward
@@ -627,9 +718,28 @@ __device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& 
 constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
 constexpr int kPolynomial = 2;              // one in so many pairs of exponentials goes by the polynomial
+constexpr int kBackwardChunk = 32;          // columns of results on their way
 template <bool KEYS> constexpr int kSlotsU = KEYS ? 2 : 3;                        // of the operand that the scores take
-constexpr int kSlotsW = 2;                                                         // of the one that dP takes
-template <int DP, bool KEYS> constexpr int kBackwardSmem = (2 + kSlotsU<KEYS> + kSlotsW) * kTile * DP * 2 + (KEYS ? kSlotsU<KEYS> * 2 * kStep * 4 : 0) + 1024;
+template <bool KEYS> constexpr int kSlotsW = KEYS ? 2 : 1;                        // of the one that dP takes
+template <int DP, bool KEYS>
+constexpr int kBackwardSmem = (2 + kSlotsU<KEYS> + kSlotsW<KEYS>) * kTile * DP * 2 + (KEYS ? kSlotsU<KEYS> * 2 * kStep * 4 : 0) + 8 * 64 * kBackwardChunk + 1024;
+
+// What keys are seen by; where first keys' far queries are set apart (`chunked`), sinks_end is the end of the sequence that has some.
+struct KeyRows {
+    const AttentionArgs& a;
+    bool chunked;
+    __device__ __forceinline__ bool operator()(const Sequence& s, int row, Keys& k) const
+    {
+        if (s.start >= s.end) return false;
+        const Queries q = queries_of(a, s, row);
+        k = Keys{q.lo, q.hi, s.start, 0};
+        if (chunked && row - s.start < a.sinks && far_from(a, s) < s.end) {
+            k.hi = far_from(a, s) - 1;
+            k.sinks_end = s.end;
+        }
+        return true;
+    }
+};
 
 // KEYS: dk and dv of a tile of keys, walking over queries; else dq of a tile of queries, walking over keys.  The scores of a
 // step are S = X U^T and dP = Y W^T with the tile's own X and Y; its sums take P W (dv) and dS U (dk, or dq).  While the
@@ -644,41 +754,36 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     constexpr unsigned long long kLimit = kAttentionWaitNs;
     constexpr bool kHalf = TypeCode<T>::value == 0;
     constexpr float kWeightExponent = kHalf ? 14.0f : 0.0f;               // of two, on P in half precision
-    constexpr int kU = kSlotsU<KEYS>, kW = kSlotsW, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS ? 1 : 2;
+    constexpr int kU = kSlotsU<KEYS>, kW = kSlotsW<KEYS>, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS ? 1 : 2;
     constexpr unsigned kTmemSum = KEYS ? 128 : 0, kTmemScores = KEYS ? 256 : 128, kTmemGrads = 384;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 8];
-    __shared__ unsigned tmem_slot, spoiled[2][4];
+    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 9];
+    __shared__ unsigned tmem_slot;
     __shared__ int gave_up;
-    __shared__ Reach reach;
 
-    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring_u = own + 2 * kBytes, ring_w = ring_u + kU * kBytes, stats = ring_w + kW * kBytes;
+    const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring_u = own + 2 * kBytes, ring_w = ring_u + kU * kBytes, out = ring_w + kW * kBytes,
+                   stats = out + 8 * 64 * kBackwardChunk;
     const float* stats_at = reinterpret_cast<const float*>(raw + (stats - smem_address(raw)));
     const unsigned full_u = smem_address(bars), empty_u = full_u + 8 * kU, full_w = empty_u + 8 * kU, empty_w = full_w + 8 * kW, loaded = empty_w + 8 * kW,
-                   scored = loaded + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8, drain = summed + 8;
+                   used = loaded + 8, scored = used + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8,
+                   drain = summed + 8;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
-        reach_init(reach);
         for (int s = 0; s < kU; ++s) { barrier_init(full_u + 8 * s, 1); barrier_init(empty_u + 8 * s, 1); }
         for (int s = 0; s < kW; ++s) { barrier_init(full_w + 8 * s, 1); barrier_init(empty_w + 8 * s, 1); }
-        barrier_init(loaded, 1);
+        barrier_init(loaded, 1);                              // X and Y are there
+        barrier_init(used, 1);                                // they have done their part
         barrier_init(scored, 1);                              // S of a step (in each of its places) is there
         barrier_init(scored + 8, 1);
         barrier_init(graded, 1);                              // dP is there
         barrier_init(weighted, 8);                            // P is there (KEYS)
         barrier_init(differed, 8);                            // dS is there
-        barrier_init(summed, 1);
+        barrier_init(summed, 1);                              // a tile's sums are there
         barrier_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (threadIdx.x < 8) spoiled[threadIdx.x / 4][threadIdx.x % 4] = 0;
-    const AttentionArgs& a = t.a;
-    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = (a.rows + kTile - 1) / kTile;
-    const int turn = static_cast<int>(blockIdx.x) / per, tile = KEYS ? turn : tiles - 1 - turn;    // the longest walks first, without a window
-    const int w = static_cast<int>(blockIdx.x) % per / heads, h = static_cast<int>(blockIdx.x) % heads;
-    const int m = t.first_worker + w, kv = KEYS ? h : h / a.group, half = warp / 4;
-    if (warp == 8 && lane < 4) prefetch_map(&t.map[lane][w]);
+    if (warp == 8 && lane < 4 * t.workers) prefetch_map(&t.map[lane % 4][lane / 4]);
     if (warp == 9) tensor_alloc<512>(smem_address(&tmem_slot));
     order_before();
     __syncthreads();
@@ -686,70 +791,78 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     stream_order();
     const unsigned tmem = tmem_slot;
 
-    const bool far = KEYS && t.far;                           // a chunk of queries and the first keys of the sequence that it begins in
-    const Sequence chunk = far ? sequence_of(a, m, turn * kChunk) : Sequence{0, 0};
-    const int r0 = far ? chunk.start : tile * kTile, row = r0 + static_cast<int>(threadIdx.x) % kTile;
-    const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
-#pragma unroll
-        for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
+    const AttentionArgs& a = t.a;
+    const bool far = KEYS && t.far;                           // chunks of queries against the first keys of the sequences that they begin in
+    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = far ? t.chunks : (a.rows + kTile - 1) / kTile, units = tiles * per;
+    // A tile and its walk, the same for all warps.  (The longest walks come first, where there is no window.)
+    struct Place {
+        int w, m, h, turn, r0, steps, first, turns;
+        Reach all;
+        KeyWalk walk;
+        __device__ __forceinline__ int row(int i) const { return KEYS ? first + i % turns * kStep : walk.row(i, kStep); }
     };
-    if (warp == 8 && lane == 0) {                             // (whether or not any row belongs to a sequence)
-        barrier_expect(loaded, 2 * kBytes);
-        copy_tile(own, &t.map[KEYS ? 1 : 0][w], h, r0, loaded);              // X: k or q
-        copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][w], h, r0, loaded);     // Y: v or dout
-    }
-    bool valid = false;
-    Keys keys{};
-    int from_chunk = 0, to_chunk = 0;                         // chunks whose sums are added to this row's
-    if (warp < 8) {
-        if (far) {
-            valid = chunk.start < chunk.end && turn * kChunk >= far_from(a, chunk) && row < chunk.end && row - chunk.start < a.sinks;
-            keys = Keys{turn * kChunk, min(turn * kChunk + kChunk, chunk.end) - 1, 0, 0};
+    const auto place_of = [&](int unit) {
+        const int in = unit % per, turn = unit / per, w = in / heads, m = t.first_worker + w;
+        int r0 = (KEYS ? turn : tiles - 1 - turn) * kTile;
+        Reach all;
+        if (far) {                                            // all first keys see the whole chunk, where it is far from them
+            const Sequence s = sequence_of(a, m, turn * kChunk);
+            r0 = s.start;
+            all = Reach{turn * kChunk, turn * kChunk, min(turn * kChunk + kChunk, s.end) - 1, 0, s.start};
+            all.max_hi = s.start < s.end && turn * kChunk >= far_from(a, s) ? all.min_hi : -1;
+        } else if (KEYS) {
+            all = reach_of(a, m, r0, lane, KeyRows{a, t.partial != nullptr});
         } else {
-            const Sequence s = row < a.rows ? sequence_of(a, m, row) : Sequence{0, 0};
-            valid = s.start < s.end;
-            if (valid && KEYS) {
-                const Queries q = queries_of(a, s, row);
-                keys = Keys{q.lo, q.hi, s.start, 0};
-                if (t.partial && row - s.start < a.sinks && far_from(a, s) < s.end) {
-                    keys.hi = far_from(a, s) - 1;
-                    from_chunk = far_from(a, s) / kChunk;
-                    to_chunk = (s.end - 1) / kChunk + 1;
-                }
-            } else if (valid) {
-                keys = keys_of(a, s, row);
-            }
+            all = reach_of(a, m, r0, lane, QueryRows{a});
         }
-        if (warp < 4) reach_add(reach, valid, keys.lo, keys.hi, keys.start);
-    }
-    __syncthreads();
-    const Reach all = reach;
-    const KeyWalk walk(all, a.sinks, kStep);
-    // Queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes.
-    const int first = KEYS ? all.min_lo / 64 * 64 : 0, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
-    const int steps = KEYS ? turns * a.group : walk.steps;
-    const auto row_of = [&](int i) { return KEYS ? first + i % turns * kStep : walk.row(i, kStep); };
-    const auto head_of = [&](int i) { return KEYS ? h * a.group + i / turns : kv; };
+        const KeyWalk walk(all, a.sinks, kStep);
+        // queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes
+        const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
+        return Place{w, m, in % heads, turn, r0, KEYS ? turns * a.group : walk.steps, first, turns, all, walk};
+    };
+    int fills_u = 0, fills_w = 0, loads = 0;                  // of the copying thread
 
-    int fills_u = 0, fills_w = 0;                             // of the copying thread
-    if (warp == 8 && lane == 0 && steps > 0) {
-        for (int i = 0; i < steps; ++i) {
-            const int u = i % kU, v = i % kW, r = row_of(i), hs = head_of(i);
-            if (i >= kU && !tile_wait<kLimit>(empty_u + 8 * u, (i / kU - 1) & 1, &gave_up)) break;
-            barrier_expect(full_u + 8 * u, kBytes + (KEYS ? 2 * kStep * 4 : 0));
-            copy_tile(ring_u + u * kBytes, &t.map[KEYS ? 0 : 1][w], hs, r, full_u + 8 * u);
-            if (KEYS) {
-                const long long from = (static_cast<long long>(m) * a.heads + hs) * t.pitch + r;
-                copy_floats(stats + u * 2 * kStep * 4, t.lse + from, kStep * 4, full_u + 8 * u);
-                copy_floats(stats + u * 2 * kStep * 4 + kStep * 4, t.delta + from, kStep * 4, full_u + 8 * u);
+    if (warp == 8) {
+        const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
+#pragma unroll
+            for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
+        };
+        bool ok = true;
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const Place at = place_of(unit);
+            if (at.steps == 0) continue;
+            if (lane == 0) {
+                ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
+                if (ok) {
+                    barrier_expect(loaded, 2 * kBytes);
+                    copy_tile(own, &t.map[KEYS ? 1 : 0][at.w], at.h, at.r0, loaded);             // X: k or q
+                    copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][at.w], at.h, at.r0, loaded);    // Y: v or dout
+                    ++loads;
+                }
+                for (int i = 0; i < at.steps && ok; ++i) {
+                    const int u = fills_u % kU, v = fills_w % kW, r = at.row(i), hs = KEYS ? at.h * a.group + i / at.turns : at.h / a.group;
+                    ok = fills_u < kU || tile_wait<kLimit>(empty_u + 8 * u, (fills_u / kU - 1) & 1, &gave_up);
+                    if (!ok) break;
+                    barrier_expect(full_u + 8 * u, kBytes + (KEYS ? 2 * kStep * 4 : 0));
+                    copy_tile(ring_u + u * kBytes, &t.map[KEYS ? 0 : 1][at.w], hs, r, full_u + 8 * u);
+                    if (KEYS) {
+                        const long long from = (static_cast<long long>(at.m) * a.heads + hs) * t.pitch + r;
+                        copy_floats(stats + u * 2 * kStep * 4, t.lse + from, kStep * 4, full_u + 8 * u);
+                        copy_floats(stats + u * 2 * kStep * 4 + kStep * 4, t.delta + from, kStep * 4, full_u + 8 * u);
+                    }
+                    ++fills_u;
+                    ok = fills_w < kW || tile_wait<kLimit>(empty_w + 8 * v, (fills_w / kW - 1) & 1, &gave_up);
+                    if (!ok) break;
+                    barrier_expect(full_w + 8 * v, kBytes);
+                    copy_tile(ring_w + v * kBytes, &t.map[KEYS ? 3 : 2][at.w], hs, r, full_w + 8 * v);
+                    ++fills_w;
+                }
             }
-            ++fills_u;
-            if (i >= kW && !tile_wait<kLimit>(empty_w + 8 * v, (i / kW - 1) & 1, &gave_up)) break;
-            barrier_expect(full_w + 8 * v, kBytes);
-            copy_tile(ring_w + v * kBytes, &t.map[KEYS ? 3 : 2][w], hs, r, full_w + 8 * v);
-            ++fills_w;
+            ok = __shfl_sync(0xffffffffu, ok, 0);
         }
-    } else if (warp == 9 && steps > 0) {
+    } else if (warp == 9) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kStep >> 3) << 17, kSums = kTypes | 1u << 16 | (DP >> 3) << 17;
         bool ok = true;
@@ -763,8 +876,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             const unsigned long long x = matrix_descriptor(tile_at, 16), y = matrix_descriptor(slot, 16);
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
-                const unsigned at = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
-                mma_shared(to, x + at, y + at, kScores, k > 0);
+                const unsigned along = (k / 4 * 2 * kBoxBytes + k % 4 * 32) >> 4;
+                mma_shared(to, x + along, y + along, kScores, k > 0);
             }
         };
         // What a step adds to a sum: 128 columns of scores as 16-bit operands in two halves, the sum along the step's rows.
@@ -773,232 +886,264 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
             for (int k = 0; k < kStep / 16; ++k) mma_tensor(to, from + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), kSums, more || k > 0);
         };
-        const auto step_s = [&](int i) {
-            if (i >= steps || !ok) return;
-            if (one_lane()) {
-                scores(tmem + kTmemScores + i % kScoreSets * 128, own, ring_u + i % kU * kBytes);
-                mma_done(scored + 8 * (i % kScoreSets));
-            }
-            __syncwarp();
-        };
-        const auto step_p = [&](int i) {
-            if (i >= steps || !ok) return;
-            if (one_lane()) {
-                scores(tmem + kTmemGrads, own + kBytes, ring_w + i % kW * kBytes);
-                mma_done(graded);
-                if (!KEYS) mma_done(empty_w + 8 * (i % kW));
-            }
-            __syncwarp();
-        };
-        // The waits for operands come in front of those for the warps, while earlier products run.
-        const auto wait_u = [&](int i) { if (i < steps) await(full_u + 8 * (i % kU), i / kU); };
-        const auto wait_w = [&](int i) { if (i < steps) await(full_w + 8 * (i % kW), i / kW); };
-        await(loaded, 0);
-        wait_u(0);
-        step_s(0);
-        wait_w(0);
-        step_p(0);
-        if (!KEYS) {
-            wait_u(1);
-            step_s(1);
-        }
-        for (int i = 0; i < steps && ok; ++i) {
-            if (KEYS) {
-                wait_u(i + 1);
-                if (!await(weighted, i)) break;
+        int n = 0, tile = 0;                                  // steps and tiles so far
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const int steps = place_of(unit).steps, end = n + steps;
+            if (steps == 0) continue;
+            // Steps are numbered through all tiles here.  The waits for operands come in front of those for the warps, while earlier
+            // products run.
+            const auto wait_u = [&](int i) { if (i < end) await(full_u + 8 * (i % kU), i / kU); };
+            const auto wait_w = [&](int i) { if (i < end) await(full_w + 8 * (i % kW), i / kW); };
+            const auto step_s = [&](int i) {
+                if (i >= end || !ok) return;
                 if (one_lane()) {
-                    add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > 0);
-                    mma_done(empty_w + 8 * (i % kW));
+                    scores(tmem + kTmemScores + i % kScoreSets * 128, own, ring_u + i % kU * kBytes);
+                    mma_done(scored + 8 * (i % kScoreSets));
                 }
                 __syncwarp();
-                step_s(i + 1);
-                wait_w(i + 1);
-                if (!await(differed, i)) break;
+            };
+            const auto step_p = [&](int i) {
+                if (i >= end || !ok) return;
                 if (one_lane()) {
-                    add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > 0);
-                    mma_done(empty_u + 8 * (i % kU));
-                    if (i + 1 == steps) mma_done(summed);
+                    scores(tmem + kTmemGrads, own + kBytes, ring_w + i % kW * kBytes);
+                    mma_done(graded);
+                    if (!KEYS) mma_done(empty_w + 8 * (i % kW));
+                    if (i + 1 == end) mma_done(used);         // (the last scores have gone before)
                 }
                 __syncwarp();
-                step_p(i + 1);
-            } else {
-                wait_w(i + 1);
-                if (!await(differed, i)) break;
-                if (one_lane()) {
-                    add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > 0);
-                    mma_done(empty_u + 8 * (i % kU));
-                    if (i + 1 == steps) mma_done(summed);
-                }
-                __syncwarp();
-                step_p(i + 1);
-                wait_u(i + 2);                                // (its slot has only been free since the step before's sum)
-                step_s(i + 2);
+            };
+            await(loaded, tile);
+            wait_u(n);
+            step_s(n);
+            if (!KEYS) {
+                wait_u(n + 1);
+                step_s(n + 1);
             }
+            wait_w(n);
+            step_p(n);
+            for (int i = n; i < end && ok; ++i) {
+                if (KEYS) {
+                    wait_u(i + 1);
+                    if (!await(weighted, i)) break;
+                    if (one_lane()) {
+                        add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > n);
+                        mma_done(empty_w + 8 * (i % kW));
+                    }
+                    __syncwarp();
+                    step_s(i + 1);
+                    wait_w(i + 1);
+                    if (!await(differed, i)) break;
+                    if (one_lane()) {
+                        add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > n);
+                        mma_done(empty_u + 8 * (i % kU));
+                        if (i + 1 == end) mma_done(summed);
+                    }
+                    __syncwarp();
+                    step_p(i + 1);
+                } else {
+                    wait_w(i + 1);
+                    if (!await(differed, i)) break;
+                    if (one_lane()) {
+                        add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > n);
+                        mma_done(empty_u + 8 * (i % kU));
+                        if (i + 1 == end) mma_done(summed);
+                    }
+                    __syncwarp();
+                    step_p(i + 1);
+                    wait_u(i + 2);                            // (its slot has only been free since the step before's sum)
+                    step_s(i + 2);
+                }
+            }
+            n = end;
+            ++tile;
         }
         if (!ok) {
             if (one_lane()) mma_done(drain);
             __syncwarp();
             tile_wait<kLimit>(drain, 0, nullptr);
         }
-    } else if (warp < 8 && steps > 0) {
-        const unsigned at = static_cast<unsigned>(warp % 4 * 32) << 16;
+    } else if (warp < 8) {
+        const int quarter = warp % 4, half = warp / 4;
+        const unsigned lanes = static_cast<unsigned>(quarter * 32) << 16;
+        unsigned char* const stage = raw + (out - smem_address(raw)) + warp * 64 * kBackwardChunk;
         const float c = a.scale * kLog2e;
-        const int exponent = kHalf ? grad_exponent(t, m) : 0;
-        const float to_grad = kHalf ? exp2f(static_cast<float>(exponent) - kWeightExponent) : 1.0f;
-        float lse = 0.0f, delta = 0.0f;
-        if (!KEYS && valid) {
-            const long long from = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
-            lse = t.lse[from] + static_cast<float>(exponent);  // P with dS's power of two
-            delta = t.delta[from];
-        }
         bool ok = true;
         const auto await = [&](unsigned bar, int phase) {
-            ok = __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
-            __syncwarp();
+            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
             order_after();
             return ok;
         };
-        for (int i = 0; i < steps; ++i) {
-            const unsigned s_at = tmem + kTmemScores + i % kScoreSets * 128 + half * 64 + at, g_at = tmem + kTmemGrads + half * 64 + at;
-            const int r = row_of(i), limit = !KEYS && i < walk.sink_steps ? all.min_lo : 0x7fffffff;
-            const bool masked = (!KEYS && i < walk.sink_steps) || r < all.max_lo || r + kStep - 1 > all.min_hi;
-            const float* column = stats_at + i % kU * 2 * kStep + half * 64;
-            if (!await(scored + 8 * (i % kScoreSets), i / kScoreSets)) break;
-            if (KEYS && !await(full_u + 8 * (i % kU), i / kU)) break;          // (long past: for the sight of lse and delta)
-            Two p[2][16];
-            unsigned seen[2] = {~0u, ~0u};
-            ulonglong2 columns = {0, 0};                      // what four neighbouring columns' queries share
-            {
-                unsigned s[2][32];
-                tensor_load(s_at, s[0]);
-                tensor_load(s_at + 32, s[1]);
-                tensor_wait(s[0]);
-                tensor_wait(s[1]);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    if (masked) {
-                        const int from = r + half * 64 + q * 32;
-                        seen[q] = KEYS ? bits_between(keys.lo - from, keys.hi - from) : seen_keys(keys, from, limit);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        Two shift = two(lse, lse);
-                        if (KEYS) {
-                            if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + q * 32 + 2 * e);
-                            shift.v = e % 2 ? columns.y : columns.x;
-                            if (kHalf) shift = add_two(shift, two(kWeightExponent, kWeightExponent));
-                        }
-                        float x, y;
-                        exp2_shared<kPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
-                        if (masked) {
-                            x = seen[q] & 1u << (2 * e) ? x : 0.0f;
-                            y = seen[q] & 2u << (2 * e) ? y : 0.0f;
-                        }
-                        p[q][e] = two(x, y);
-                        s[q][e] = pack_pair(x, y, T{});
-                    }
-                    if (KEYS) tensor_store(s_at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
-                }
+        int n = 0, tile = 0;
+        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const Place at = place_of(unit);
+            if (at.steps == 0) continue;
+            const int row = at.r0 + quarter * 32 + lane;
+            Keys keys{};
+            bool valid;
+            if (far) {
+                const Sequence s = sequence_of(a, at.m, at.turn * kChunk);
+                keys = Keys{at.all.min_lo, at.all.max_hi, s.start, 0};
+                valid = row < s.end && row - s.start < a.sinks;
+            } else if (KEYS) {
+                valid = own_keys(a, at.m, row, KeyRows{a, t.partial != nullptr}, keys);
+            } else {
+                valid = own_keys(a, at.m, row, QueryRows{a}, keys);
             }
-            if (KEYS) {
+            const int exponent = kHalf ? grad_exponent(t, at.m) : 0;
+            const float to_grad = kHalf ? exp2f(static_cast<float>(exponent) - kWeightExponent) : 1.0f;
+            float lse = 0.0f, delta = 0.0f;
+            if (!KEYS && valid) {
+                const long long from = (static_cast<long long>(at.m) * a.heads + at.h) * t.pitch + row;
+                lse = t.lse[from] + static_cast<float>(exponent);  // P with dS's power of two
+                delta = t.delta[from];
+            }
+            for (int i = 0; i < at.steps; ++i, ++n) {
+                const unsigned s_at = tmem + kTmemScores + n % kScoreSets * 128 + half * 64 + lanes, g_at = tmem + kTmemGrads + half * 64 + lanes;
+                const int r = at.row(i), limit = !KEYS && i < at.walk.sink_steps ? at.all.min_lo : 0x7fffffff;
+                const bool masked = (!KEYS && i < at.walk.sink_steps) || r < at.all.max_lo || r + kStep - 1 > at.all.min_hi;
+                const float* column = stats_at + n % kU * 2 * kStep + half * 64;
+                if (!await(scored + 8 * (n % kScoreSets), n / kScoreSets)) break;
+                if (KEYS && !await(full_u + 8 * (n % kU), n / kU)) break;      // (long past: for the sight of lse and delta)
+                Two p[2][16];
+                unsigned seen[2] = {~0u, ~0u};
+                ulonglong2 columns = {0, 0};                  // what four neighbouring columns' queries share
+                {
+                    unsigned s[2][32];
+                    tensor_load(s_at, s[0]);
+                    tensor_load(s_at + 32, s[1]);
+                    tensor_wait(s[0]);
+                    tensor_wait(s[1]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        if (masked) {
+                            const int from = r + half * 64 + q * 32;
+                            seen[q] = KEYS ? bits_between(keys.lo - from, keys.hi - from) : seen_keys(keys, from, limit);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            Two shift = two(lse, lse);
+                            if (KEYS) {
+                                if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + q * 32 + 2 * e);
+                                shift.v = e % 2 ? columns.y : columns.x;
+                                if (kHalf) shift = add_two(shift, two(kWeightExponent, kWeightExponent));
+                            }
+                            float x, y;
+                            exp2_shared<kPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
+                            if (masked) {
+                                x = seen[q] & 1u << (2 * e) ? x : 0.0f;
+                                y = seen[q] & 2u << (2 * e) ? y : 0.0f;
+                            }
+                            p[q][e] = two(x, y);
+                            s[q][e] = pack_pair(x, y, T{});
+                        }
+                        if (KEYS) tensor_store(s_at + q * 16, reinterpret_cast<const unsigned(&)[16]>(s[q]));
+                    }
+                }
+                if (KEYS) {
+                    tensor_stored();
+                    order_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_here(weighted);
+                }
+                if (!await(graded, n)) break;
+                {
+                    unsigned g[2][32];
+                    tensor_load(g_at, g[0]);
+                    tensor_load(g_at + 32, g[1]);
+                    tensor_wait(g[0]);
+                    tensor_wait(g[1]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            Two shift = two(delta, delta);
+                            if (KEYS) {
+                                if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + kStep + q * 32 + 2 * e);
+                                shift.v = e % 2 ? columns.y : columns.x;
+                            }
+                            Two d = mul_two(p[q][e], add_two(two(g[q] + 2 * e), shift));
+                            if (KEYS && kHalf) d = mul_two(d, two(to_grad, to_grad));
+                            float x, y;
+                            apart(d, x, y);
+                            if (masked) {                     // (0 times what is not finite)
+                                x = seen[q] & 1u << (2 * e) ? x : 0.0f;
+                                y = seen[q] & 2u << (2 * e) ? y : 0.0f;
+                            }
+                            g[q][e] = pack_pair(x, y, T{});
+                        }
+                        tensor_store((KEYS ? g_at : s_at) + q * 16, reinterpret_cast<const unsigned(&)[16]>(g[q]));
+                    }
+                }
                 tensor_stored();
                 order_before();
                 __syncwarp();
-                if (lane == 0) arrive_here(weighted);
+                if (lane == 0) arrive_here(differed);
             }
-            if (!await(graded, i)) break;
-            {
-                unsigned g[2][32];
-                tensor_load(g_at, g[0]);
-                tensor_load(g_at + 32, g[1]);
-                tensor_wait(g[0]);
-                tensor_wait(g[1]);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        Two shift = two(delta, delta);
-                        if (KEYS) {
-                            if (e % 2 == 0) columns = *reinterpret_cast<const ulonglong2*>(column + kStep + q * 32 + 2 * e);
-                            shift.v = e % 2 ? columns.y : columns.x;
-                        }
-                        Two d = mul_two(p[q][e], add_two(two(g[q] + 2 * e), shift));
-                        if (KEYS && kHalf) d = mul_two(d, two(to_grad, to_grad));
-                        float x, y;
-                        apart(d, x, y);
-                        if (masked) {                         // (0 times what is not finite)
-                            x = seen[q] & 1u << (2 * e) ? x : 0.0f;
-                            y = seen[q] & 2u << (2 * e) ? y : 0.0f;
-                        }
-                        g[q][e] = pack_pair(x, y, T{});
-                    }
-                    tensor_store((KEYS ? g_at : s_at) + q * 16, reinterpret_cast<const unsigned(&)[16]>(g[q]));
-                }
-            }
-            tensor_stored();
-            order_before();
-            __syncwarp();
-            if (lane == 0) arrive_here(differed);
-        }
-        if (ok && await(summed, 0)) {
+            if (!await(summed, tile)) break;
             const float of_grad = a.scale * (kHalf ? exp2f(static_cast<float>(-exponent)) : 1.0f);
-            bool fine = true;
             const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
-            unsigned char* const stage = raw + (own - smem_address(raw)) + warp * 4096;        // (the tile's own operands have done their part)
+            const auto nothing = [](float (&)[32], int) {};
             if (KEYS) {                                       // half of the warps dv, the others dk
                 const long long partial_row = static_cast<long long>(a.sinks) * a.dim, partial_chunk = 2 * partial_row;
-                const long long partial_head = (static_cast<long long>(m) * a.kv_heads + h) * t.chunks * partial_chunk + half * partial_row;
-                const auto add = [&](float (&v)[32], int col) {
-                    for (int k = from_chunk; k < to_chunk; ++k) {
-                        const float* more = t.partial + partial_head + k * partial_chunk + static_cast<long long>(row - keys.start) * a.dim + col;
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            if (col + e < a.dim) {
-                                const float4 x = *reinterpret_cast<const float4*>(more + e);
-                                v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
-                            }
-                    }
-                };
+                const long long partial_head = (static_cast<long long>(at.m) * a.kv_heads + at.h) * t.chunks * partial_chunk + half * partial_row;
                 if (far) {
-                    float* to = t.partial + partial_head + turn * partial_chunk + static_cast<long long>(row - chunk.start) * a.dim;
+                    float* to = t.partial + partial_head + at.turn * partial_chunk + static_cast<long long>(row - keys.start) * a.dim;
 #pragma unroll 1
-                    for (int c = 0; c < DP; c += 32) {
+                    for (int d = 0; d < DP; d += 32) {
                         unsigned v[32];
-                        tensor_load(tmem + half * 128 + at + c, v);
+                        tensor_load(tmem + half * 128 + lanes + d, v);
                         tensor_wait(v);
 #pragma unroll
                         for (int e = 0; e < 32; e += 8)
-                            if (valid && c + e < a.dim) store_eight(to + c + e, reinterpret_cast<const float*>(v + e));
+                            if (valid && d + e < a.dim) store_eight(to + d + e, reinterpret_cast<const float*>(v + e));
                     }
                 } else {
+                    const int from_chunk = (keys.hi + 1) / kChunk, to_chunk = valid && keys.sinks_end > 0 ? (keys.sinks_end - 1) / kChunk + 1 : 0;
+                    const auto add = [&](float (&v)[32], int col) {
+                        for (int k = from_chunk; k < to_chunk; ++k) {
+                            const float* more = t.partial + partial_head + k * partial_chunk + static_cast<long long>(row - keys.start) * a.dim + col;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                if (col + e < a.dim) {
+                                    const float4 x = *reinterpret_cast<const float4*>(more + e);
+                                    v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
+                                }
+                        }
+                    };
                     const long long stride = half ? a.k_stride : a.v_stride;
-                    T* to = static_cast<T*>(a.to[half ? 1 : 2].p[m]) + (r0 + warp % 4 * 32) * stride + static_cast<long long>(h) * a.dim;
-                    fine = store_rows(tmem + half * 128 + at, 0, DP, half ? of_grad : exp2f(-kWeightExponent), stage, to, stride, a.dim, rows_valid, add);
+                    T* to = static_cast<T*>(a.to[half ? 1 : 2].p[at.m]) + (at.r0 + quarter * 32) * stride + static_cast<long long>(at.h) * a.dim;
+                    const bool fine = store_rows<T, kBackwardChunk>(tmem + half * 128 + lanes, 0, DP, half ? of_grad : exp2f(-kWeightExponent), stage, to, stride,
+                                                                    a.dim, rows_valid, add);
+                    __syncwarp();
+                    for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
+                        attention_key_grad_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, half != 0);
                 }
             } else {                                          // half of the columns each
-                T* to = static_cast<T*>(a.to[0].p[m]) + (r0 + warp % 4 * 32) * a.q_stride + static_cast<long long>(h) * a.dim;
-                fine = store_rows(tmem + half * (DP / 2) + at, half * (DP / 2), DP / 2, of_grad, stage, to, a.q_stride, a.dim, rows_valid, [](float (&)[32], int) {});
+                const int d = half * (DP / 2);
+                T* to = static_cast<T*>(a.to[0].p[at.m]) + (at.r0 + quarter * 32) * a.q_stride + static_cast<long long>(at.h) * a.dim;
+                const bool fine = store_rows<T, kBackwardChunk>(tmem + d + lanes, d, DP / 2, of_grad, stage, to, a.q_stride, a.dim, rows_valid, nothing);
+                __syncwarp();
+                for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
+                    attention_query_grad_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, d, d + DP / 2);
             }
-            const unsigned todo = __ballot_sync(0xffffffffu, valid && !fine);
-            if (lane == 0) spoiled[half][warp % 4] = todo;
+            order_before();
+            ++tile;
         }
     }
     __syncwarp();
     order_before();
     __syncthreads();
     order_after();
-    if (warp == 8 && lane == 0 && (gave_up || steps == 0)) {  // copies in flight write shared memory: none is left behind
-        tile_wait<kLimit>(loaded, 0, nullptr);
+    if (gave_up && loads > 0) {                               // copies in flight write shared memory: none is left behind
+        tile_wait<kLimit>(loaded, (loads - 1) & 1, nullptr);
         for (int f = max(0, fills_u - kU); f < fills_u; ++f) tile_wait<kLimit>(full_u + 8 * (f % kU), (f / kU) & 1, nullptr);
         for (int f = max(0, fills_w - kW); f < fills_w; ++f) tile_wait<kLimit>(full_w + 8 * (f % kW), (f / kW) & 1, nullptr);
     }
     if (warp == 9) tensor_free<512>(tmem);
-    if (warp < 4)
-        for (unsigned todo = spoiled[0][warp] | spoiled[1][warp]; todo; todo &= todo - 1) {
-            const int lost = __ffs(todo) - 1, r = r0 + warp * 32 + lost;
-            if (KEYS) attention_key_grad_row<T>(a, m, h, r, spoiled[1][warp] >> lost & 1, spoiled[0][warp] >> lost & 1);
-            else attention_query_grad_row<T>(a, m, h, r);
-        }
 }
 
 }  // namespace replica

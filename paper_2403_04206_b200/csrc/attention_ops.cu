@@ -24,7 +24,7 @@ static bool attention_shape_ok(const AttentionShape& s)
 {
     if ((s.dtype != GRAWA_BF16 && s.dtype != GRAWA_F16) || s.M < 1 || s.M > GRAWA_MAX_WORKERS) return false;
     if (s.rows < 0 || s.rows > 0x7fffffff - 1024 || s.q_heads < 1 || s.q_heads > 0x7fff || s.kv_heads < 1 || s.q_heads % s.kv_heads != 0) return false;
-    if (ceil_div(s.rows, kTile) * s.q_heads * std::min(s.M, kAttentionWorkers) > 0x7fffffff) return false;          // CTAs of a launch
+    if (ceil_div(s.rows, kTile) * s.q_heads * std::min(s.M, kAttentionWorkers) > 0x7fffffff - 4096) return false;          // tiles of a launch
     if (s.head_dim < 8 || s.head_dim > 128 || s.head_dim % 8 != 0) return false;
     if (s.left < 0 || s.right < 0 || s.sinks < 0 || !(s.scale > 0.0f) || std::isinf(s.scale)) return false;
     if (s.offsets ? s.sequences < 0 || s.sequences > 0x7fffffff - 1 : s.period < 1) return false;
@@ -94,24 +94,26 @@ static grawa_status set_workers(TileArgs& t, const AttentionShape& s, int first,
     return st;
 }
 
+// As many CTAs as the SMs hold, `per_sm` each, or one a tile.
 template <typename Kernel>
-static grawa_status launch_tiles(Kernel kernel, const TileArgs& t, int heads, int threads, int smem, cudaStream_t stream)
+static grawa_status launch_tiles(Kernel kernel, const TileArgs& t, int heads, int per_sm, int threads, int smem, cudaStream_t stream)
 {
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    return launch(kernel, dim3(static_cast<unsigned>((t.far ? t.chunks : ceil_div(t.a.rows, kTile)) * heads * t.workers)), threads, smem, stream, t);
+    const int64_t units = (t.far ? t.chunks : ceil_div(t.a.rows, kTile)) * heads * t.workers;
+    return launch(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(units, kSms * per_sm))), threads, smem, stream, t);
 }
 template <typename T>
 static grawa_status launch_forward(const TileArgs& t, cudaStream_t stream)
 {
-    return t.a.dim <= 64 ? launch_tiles(attention_forward_kernel<T, 64>, t, t.a.heads, kForwardThreads, kForwardSmem<64>, stream)
-                         : launch_tiles(attention_forward_kernel<T, 128>, t, t.a.heads, kForwardThreads, kForwardSmem<128>, stream);
+    return t.a.dim <= 64 ? launch_tiles(attention_forward_kernel<T, 64>, t, t.a.heads, 2, kForwardThreads, kForwardSmem<64>, stream)
+                         : launch_tiles(attention_forward_kernel<T, 128>, t, t.a.heads, 2, kForwardThreads, kForwardSmem<128>, stream);
 }
 template <typename T, bool KEYS>
 static grawa_status launch_backward(const TileArgs& t, cudaStream_t stream)
 {
     const int heads = KEYS ? t.a.kv_heads : t.a.heads;
-    return t.a.dim <= 64 ? launch_tiles(attention_backward_kernel<T, 64, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<64, KEYS>, stream)
-                         : launch_tiles(attention_backward_kernel<T, 128, KEYS>, t, heads, kBackwardThreads, kBackwardSmem<128, KEYS>, stream);
+    return t.a.dim <= 64 ? launch_tiles(attention_backward_kernel<T, 64, KEYS>, t, heads, 1, kBackwardThreads, kBackwardSmem<64, KEYS>, stream)
+                         : launch_tiles(attention_backward_kernel<T, 128, KEYS>, t, heads, 1, kBackwardThreads, kBackwardSmem<128, KEYS>, stream);
 }
 
 // The places of a backward call's scratch: lse and delta of every row, the longest rows, and the sums of chunks of queries for the
@@ -242,7 +244,7 @@ grawa_status grawa_selftest_window_attention_wait(grawa_stream_t stream)
     t.a.dim = 64;
     t.a.scale = 1.0f;
     t.workers = 1;
-    return launch_tiles(attention_forward_kernel<__nv_bfloat16, 64, true>, t, 1, kForwardThreads, kForwardSmem<64>, stream);
+    return launch_tiles(attention_forward_kernel<__nv_bfloat16, 64, true>, t, 1, 1, kForwardThreads, kForwardSmem<64>, stream);
 }
 
 grawa_status grawa_window_attention_status(grawa_stream_t stream)

@@ -84,10 +84,10 @@ __device__ __forceinline__ void load_row(const void* base, long long stride, int
     }
 }
 template <typename T>
-__device__ __forceinline__ void store_row(void* base, long long stride, int row, int head, int dim, const float (&x)[4])
+__device__ __forceinline__ void store_row(void* base, long long stride, int row, int head, int dim, const float (&x)[4], int from, int to)
 {
     const int at = threadIdx.x % 32 * 4;
-    if (at < dim)
+    if (at < dim && at >= from && at < to)
         *reinterpret_cast<uint2*>(static_cast<T*>(base) + row * stride + static_cast<long long>(head) * dim + at) =
             make_uint2(pack_pair(x[0], x[1], T{}), pack_pair(x[2], x[3], T{}));
 }
@@ -101,8 +101,9 @@ __device__ __forceinline__ void add_row(float (&x)[4], float f, const float (&y)
     for (int e = 0; e < 4; ++e) x[e] = fmaf(f, y[e], x[e]);
 }
 
+// Elements [from, to) of out_i, and with the first of them lse_i.
 template <typename T>
-__device__ __noinline__ void attention_row(const AttentionArgs& a, int m, int h, int i)
+__device__ __noinline__ void attention_row(const AttentionArgs& a, int m, int h, int i, int from, int to)
 {
     const Keys keys = keys_of(a, sequence_of(a, m, i), i);
     const float c = a.scale * kLog2e;
@@ -122,8 +123,8 @@ __device__ __noinline__ void attention_row(const AttentionArgs& a, int m, int h,
         }
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] /= total;
-    store_row<T>(a.to[0].p[m], a.out_stride, i, h, a.dim, o);
-    if (a.to[1].p[m] && threadIdx.x % 32 == 0) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + i] = (top + log2f(total)) * kLn2;
+    store_row<T>(a.to[0].p[m], a.out_stride, i, h, a.dim, o, from, to);
+    if (a.to[1].p[m] && from == 0 && threadIdx.x % 32 == 0) static_cast<float*>(a.to[1].p[m])[static_cast<long long>(h) * a.rows + i] = (top + log2f(total)) * kLn2;
 }
 
 template <typename T>
@@ -138,8 +139,9 @@ __device__ __forceinline__ float lse_of(const AttentionArgs& a, int m, int h, in
     return static_cast<const float*>(a.lse.p[m])[static_cast<long long>(h) * a.rows + i] * kLog2e;
 }
 
+// Elements [from, to) of dq_i.
 template <typename T>
-__device__ __noinline__ void attention_query_grad_row(const AttentionArgs& a, int m, int h, int i)
+__device__ __noinline__ void attention_query_grad_row(const AttentionArgs& a, int m, int h, int i, int from, int to)
 {
     const Keys keys = keys_of(a, sequence_of(a, m, i), i);
     const float c = a.scale * kLog2e, lse = lse_of(a, m, h, i);
@@ -156,16 +158,16 @@ __device__ __noinline__ void attention_query_grad_row(const AttentionArgs& a, in
         }
 #pragma unroll
     for (int e = 0; e < 4; ++e) dq[e] *= a.scale;
-    store_row<T>(a.to[0].p[m], a.q_stride, i, h, a.dim, dq);
+    store_row<T>(a.to[0].p[m], a.q_stride, i, h, a.dim, dq, from, to);
 }
 
-// dk and dv of a key, or (where the flag is false) not that one.
+// dk_j, or dv_j.
 template <typename T>
-__device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int m, int kv, int j, bool want_k, bool want_v)
+__device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int m, int kv, int j, bool want_k)
 {
     const Queries queries = queries_of(a, sequence_of(a, m, j), j);
     const float c = a.scale * kLog2e;
-    float k[4], v[4], dk[4] = {}, dv[4] = {};
+    float k[4], v[4], sum[4] = {};
     load_row<T>(a.k.p[m], a.k_stride, j, kv, a.dim, k);
     load_row<T>(a.v.p[m], a.v_stride, j, kv, a.dim, v);
     for (int h = kv * a.group; h < (kv + 1) * a.group; ++h)
@@ -174,13 +176,12 @@ __device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int 
             load_row<T>(a.q.p[m], a.q_stride, i, h, a.dim, q);
             load_row<T>(a.dout.p[m], a.out_stride, i, h, a.dim, dout);
             const float p = exp2f(dot_row(q, k) * c - lse_of(a, m, h, i));
-            add_row(dv, p, dout);
-            if (want_k) add_row(dk, p * (dot_row(dout, v) - delta_of<T>(a, m, h, i, dout)), q);
+            if (want_k) add_row(sum, p * (dot_row(dout, v) - delta_of<T>(a, m, h, i, dout)), q);
+            else add_row(sum, p, dout);
         }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dk[e] *= a.scale;
-    if (want_k) store_row<T>(a.to[1].p[m], a.k_stride, j, kv, a.dim, dk);
-    if (want_v) store_row<T>(a.to[2].p[m], a.v_stride, j, kv, a.dim, dv);
+    for (int e = 0; e < 4; ++e) sum[e] *= want_k ? a.scale : 1.0f;
+    store_row<T>(a.to[want_k ? 1 : 2].p[m], want_k ? a.k_stride : a.v_stride, j, kv, a.dim, sum, 0, a.dim);
 }
 
 }  // namespace replica

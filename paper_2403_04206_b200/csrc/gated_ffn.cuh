@@ -99,7 +99,7 @@ __device__ __forceinline__ void barrier_arrive(unsigned cluster_bar)
 template <unsigned long long LIMIT>
 __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity, volatile int* gave_up)
 {
-    return bounded_wait<LIMIT>(bar, parity, gave_up, &g_ffn_timeouts);
+    return bounded_wait<LIMIT, true>(bar, parity, gave_up, &g_ffn_timeouts);
 }
 // Copies into this CTA's shared memory that complete on a barrier of the pair's first CTA.
 __device__ __forceinline__ void copy_2d(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar)

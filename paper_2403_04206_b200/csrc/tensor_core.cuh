@@ -23,27 +23,38 @@ __device__ __forceinline__ void barrier_expect(unsigned bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// PAIR: arrivals may come from the other CTA of a pair (a wider acquire, which takes longer).
+template <bool PAIR>
 __device__ __forceinline__ bool barrier_try(unsigned bar, unsigned parity)
 {
     unsigned ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
     return ok != 0;
 }
 // False when the limit passed, or another wait of the CTA gave up (`gave_up`, which may be NULL).  Lanes of a warp may get
 // different answers.  `timeouts`: the device's count of waits that ran out.
-template <unsigned long long LIMIT>
+template <unsigned long long LIMIT, bool PAIR>
 __device__ __forceinline__ bool bounded_wait(unsigned bar, unsigned parity, volatile int* gave_up, unsigned* timeouts)
 {
-    if (barrier_try(bar, parity)) return true;
+    if (barrier_try<PAIR>(bar, parity)) return true;
     const unsigned long long t0 = nanoseconds();
     for (;;) {
-        if (barrier_try(bar, parity)) return true;
+        if (barrier_try<PAIR>(bar, parity)) return true;
         if (gave_up && *gave_up) return false;
         if (nanoseconds() - t0 > LIMIT) {
             if (gave_up) *gave_up = 1;
