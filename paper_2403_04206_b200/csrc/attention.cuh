@@ -45,6 +45,7 @@ struct TileArgs {
     float* partial;                         // backward, where chunks of queries are set apart (or NULL): [worker][key head][chunk][dv, dk][first key][dim]
     int chunks, far;                        // far: this launch is of the chunks
     int first_worker, workers;
+    Divisor per, per_worker;                // tiles of one place in the rows: of all heads and workers of the launch, of one worker
 };
 
 __device__ unsigned g_attention_timeouts = 0;   // waits that ran out, never set back
@@ -376,7 +377,7 @@ __device__ __forceinline__ void store_eight(float* to, const float* v)
 // that the products of one run beside the exponentials of the other; each takes one tile after the other, and fetches the next one's
 // queries while it works.  Two threads share a row, one half of a step's scores each: what they wait for one after the other (scores,
 // their exponentials, the sum) bounds a CTA.
-constexpr int kForwardPolynomial = 4;       // one in so many pairs of exponentials goes by the polynomial
+constexpr int kForwardPolynomial = 8;       // one in so many pairs of exponentials goes by the polynomial
 constexpr int kForwardThreads = 320;        // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 4;
 constexpr int kForwardChunk = 16;           // columns of results on their way
@@ -420,22 +421,32 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     const unsigned tmem = tmem_slot, tmem_s = tmem, tmem_o = tmem + 128;
 
     const AttentionArgs& a = t.a;
-    const int per = a.heads * t.workers, tiles = (a.rows + kTile - 1) / kTile, units = tiles * per;
-    struct Place { int w, m, h, r0; };
-    const auto place_of = [&](int unit) {                     // the last rows, which see most, first
-        const int in = unit % per, w = in / a.heads;
-        return Place{w, t.first_worker + w, in % a.heads, (tiles - 1 - unit / per) * kTile};
+    const int tiles = (a.rows + kTile - 1) / kTile, units = tiles * static_cast<int>(t.per.by);
+    // A tile and its walk, the same for all warps; steps = -1: there are no more tiles.
+    struct Place { int w, m, h, r0, steps; Reach all; KeyWalk walk; };
+    const auto next_place = [&](int& round) {
+        for (; round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
+            const int r0 = (tiles - 1 - turn) * kTile;        // the last rows, which see most, first
+            const Reach all = reach_of(a, m, r0, lane, QueryRows{a});
+            const KeyWalk walk(all, a.sinks, kTile);
+            const int steps = STARVED ? 1 : walk.steps;
+            if (steps == 0) continue;
+            ++round;
+            return Place{w, m, in - w * a.heads, r0, steps, all, walk};
+        }
+        return Place{0, 0, 0, 0, -1, Reach{}, KeyWalk(Reach{}, 0, kTile)};
     };
+    int round = 0;
     int fills = 0, loads = 0;                                 // of the copying thread
 
     if (!STARVED && warp == 8) {
         bool ok = true;
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const Place at = place_of(unit);
-            const KeyWalk walk(reach_of(a, at.m, at.r0, lane, QueryRows{a}), a.sinks, kTile);
-            if (walk.steps == 0) continue;
+        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
+            const KeyWalk& walk = at.walk;
+            const int kv = a.group_size.quotient(at.h);
             if (lane == 0) {
                 ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
                 if (ok) {
@@ -451,7 +462,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                     barrier_expect(full + 8 * s, kBytes);
 #pragma unroll
                     for (int b = 0; b < 2 * kHalves; ++b)
-                        copy_box(ring + s * kBytes + b * kBoxBytes, &t.map[1 + i % 2][at.w], b / 2 * 64, at.h / a.group, j + b % 2 * kBox, full + 8 * s);
+                        copy_box(ring + s * kBytes + b * kBoxBytes, &t.map[1 + i % 2][at.w], b / 2 * 64, kv, j + b % 2 * kBox, full + 8 * s);
                     ++fills;
                 }
             }
@@ -467,12 +478,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             return ok;
         };
         int n = 0, tile = 0;                                  // steps and tiles so far
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const Place at = place_of(unit);
-            const int steps = STARVED ? 1 : KeyWalk(reach_of(a, at.m, at.r0, lane, QueryRows{a}), a.sinks, kTile).steps;
-            if (steps == 0) continue;
+        for (int steps = next_place(round).steps; ok && steps >= 0; steps = next_place(round).steps) {
             const auto scores = [&](int i) {
                 const int f = 2 * (n + i), s = f % kStages;
                 if (i >= steps || !await(full + 8 * s, f / kStages)) return;
@@ -523,16 +529,16 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             return ok;
         };
         int n = 0, tile = 0;
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const Place at = place_of(unit);
-            const Reach all = reach_of(a, at.m, at.r0, lane, QueryRows{a});
-            const KeyWalk walk(all, a.sinks, kTile);
-            const int steps = STARVED ? 1 : walk.steps;
-            if (steps == 0) continue;
-            Keys keys{};
-            const bool valid = own_keys(a, at.m, at.r0 + line, QueryRows{a}, keys);
+        Place next = next_place(round);
+        Keys next_keys{};
+        bool next_valid = next.steps >= 0 && own_keys(a, next.m, next.r0 + line, QueryRows{a}, next_keys);
+        while (ok && next.steps >= 0) {
+            const Place at = next;
+            const Reach& all = at.all;
+            const KeyWalk& walk = at.walk;
+            const Keys keys = next_keys;
+            const bool valid = next_valid;
+            const int steps = at.steps;
             float top = -INFINITY, total = 0.0f;
             for (int i = 0; i < steps; ++i, ++n) {
                 if (!await(scored, n)) break;
@@ -555,9 +561,10 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 }
                 float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int q = 0; q < 2; ++q) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) most[e / 2 % 4] = max_three(most[e / 2 % 4], __uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1]));
+                }
                 most[0] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
                 most_of[n % 2][half][line] = most[0];
                 __syncwarp();
@@ -607,6 +614,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             total_of[half][line] = total;
             __syncwarp();
             if (lane == 0) arrive_here(totaled + 8 * quarter);
+            next = next_place(round);                         // (while the last product runs)
+            next_valid = next.steps >= 0 && own_keys(a, next.m, next.r0 + line, QueryRows{a}, next_keys);
             if (!await(totaled + 8 * quarter, tile) || !await(summed, tile)) break;
             order_after();
             total = total_of[0][line] + total_of[1][line];
@@ -637,7 +646,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 
 // -lse (in units of log 2) and -delta = -dout out of every row, in rows of `pitch`, a multiple of 64: rows that belong to no sequence,
 // or to no row at all, get -infinity (P = 0) and 0.  For half precision also the longest rows of dout and v, from the last kv_heads
-// CTAs along y.  A CTA takes 64 rows of one head, 16 lanes a row.
+// CTAs along y.  A CTA takes 64 rows of one head.
 struct StatsArgs {
     AttentionArgs a;
     float *lse, *delta;
@@ -646,49 +655,61 @@ struct StatsArgs {
 };
 constexpr int kStatsThreads = 256;
 
-template <typename T>
+// LANES a row (8 or 16), each 8 elements of it.
+template <typename T, int LANES>
 __global__ void __launch_bounds__(kStatsThreads)
 attention_stats_kernel(const __grid_constant__ StatsArgs t)
 {
+    constexpr int kAtOnce = kStatsThreads / LANES, kTurns = 64 / kAtOnce;
     __shared__ float deltas[64];
     __shared__ unsigned most;
     stream_order();
     const AttentionArgs& a = t.a;
-    const int r0 = blockIdx.x * 64, m = blockIdx.z, group = threadIdx.x / 16, word = threadIdx.x % 16;
+    const int r0 = blockIdx.x * 64, m = blockIdx.z, group = threadIdx.x / LANES, word = threadIdx.x % LANES;
     const bool values = static_cast<int>(blockIdx.y) >= a.heads;
     const int h = values ? blockIdx.y - a.heads : blockIdx.y;
     if (threadIdx.x == 0) most = 0;
-    __syncthreads();
-    const T* x = static_cast<const T*>(values ? a.v.p[m] : a.dout.p[m]);
-    const T* y = static_cast<const T*>(a.out.p[m]);
-    float longest = 0.0f;
-    const int begin = a.offsets.p[m] ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), static_cast<const long long*>(a.offsets.p[m])[0]))) : 0;
-    const int end = a.offsets.p[m] ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), static_cast<const long long*>(a.offsets.p[m])[a.sequences]))) : a.rows;
+    if (t.longest) __syncthreads();
+    const long long stride = values ? a.v_stride : a.out_stride;
+    const T* x = static_cast<const T*>(values ? a.v.p[m] : a.dout.p[m]) + static_cast<long long>(h) * a.dim + word * 8;
+    const T* y = static_cast<const T*>(a.out.p[m]) + static_cast<long long>(h) * a.dim + word * 8;
+    const long long* offsets = static_cast<const long long*>(a.offsets.p[m]);
+    const int begin = offsets ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), offsets[0]))) : 0;
+    const int end = offsets ? static_cast<int>(max(0ll, min(static_cast<long long>(a.rows), offsets[a.sequences]))) : a.rows;
+    uint4 u[kTurns] = {}, v[kTurns] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = r0 + group + 16 * i;
-        const bool in = row >= begin && row < end;
-        float u[8] = {}, v[8] = {}, dot = 0.0f, square = 0.0f;
-        if (in && word * 8 < a.dim) {
-            unpack<T>(*reinterpret_cast<const uint4*>(x + row * (values ? a.v_stride : a.out_stride) + static_cast<long long>(h) * a.dim + word * 8), u);
-            if (!values) unpack<T>(*reinterpret_cast<const uint4*>(y + row * a.out_stride + static_cast<long long>(h) * a.dim + word * 8), v);
+    for (int i = 0; i < kTurns; ++i) {
+        const int row = r0 + group + kAtOnce * i;
+        if (row >= begin && row < end && word * 8 < a.dim) {
+            u[i] = *reinterpret_cast<const uint4*>(x + row * stride);
+            if (!values) v[i] = *reinterpret_cast<const uint4*>(y + row * stride);
         }
+    }
+    float longest = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        float p[8], q[8], dot = 0.0f, square = 0.0f;
+        unpack<T>(u[i], p);
+        unpack<T>(v[i], q);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            dot = fmaf(u[e], v[e], dot);
-            square = fmaf(u[e], u[e], square);
+            dot = fmaf(p[e], q[e], dot);
+            square = fmaf(p[e], p[e], square);
         }
-        dot = lanes_sum<16>(dot);
-        if (t.longest) longest = fmaxf(longest, lanes_sum<16>(square));    // (NaN does not count: such rows are done again)
-        if (!values && word == 0) deltas[group + 16 * i] = in ? -dot : 0.0f;
+        if (!values) dot = lanes_sum<LANES>(dot);
+        if (t.longest) longest = fmaxf(longest, lanes_sum<LANES>(square));   // (NaN does not count: such rows are done again)
+        if (!values && word == 0) deltas[group + kAtOnce * i] = -dot;
     }
-    if (t.longest && word == 0) atomicMax(&most, __float_as_uint(longest));
+    if (t.longest) {
+        const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(longest));
+        if (threadIdx.x % 32 == 0) atomicMax(&most, bits);
+    }
     __syncthreads();
     if (!values && threadIdx.x < 64) {
         const int row = r0 + threadIdx.x;
         const long long at = (static_cast<long long>(m) * a.heads + h) * t.pitch + row;
         const bool in = row >= begin && row < end;
-        t.delta[at] = deltas[threadIdx.x];
+        t.delta[at] = in ? deltas[threadIdx.x] : 0.0f;
         t.lse[at] = in ? -lse_of(a, m, h, row) : -INFINITY;
     }
     if (t.longest && threadIdx.x == 0) atomicMax(t.longest + 2 * m + (values ? 1 : 0), most);
@@ -717,7 +738,7 @@ __device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& 
 
 constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
-constexpr int kPolynomial = 2;              // one in so many pairs of exponentials goes by the polynomial
+constexpr int kPolynomial = 4;              // one in so many pairs of exponentials goes by the polynomial
 constexpr int kBackwardChunk = 32;          // columns of results on their way
 template <bool KEYS> constexpr int kSlotsU = KEYS ? 2 : 3;                        // of the operand that the scores take
 template <bool KEYS> constexpr int kSlotsW = KEYS ? 2 : 1;                        // of the one that dP takes
@@ -793,33 +814,50 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
 
     const AttentionArgs& a = t.a;
     const bool far = KEYS && t.far;                           // chunks of queries against the first keys of the sequences that they begin in
-    const int heads = KEYS ? a.kv_heads : a.heads, per = heads * t.workers, tiles = far ? t.chunks : (a.rows + kTile - 1) / kTile, units = tiles * per;
-    // A tile and its walk, the same for all warps.  (The longest walks come first, where there is no window.)
+    const int heads = KEYS ? a.kv_heads : a.heads, tiles = far ? t.chunks : (a.rows + kTile - 1) / kTile, units = tiles * static_cast<int>(t.per.by);
+    // A tile and its walk, the same for all warps; steps = -1: there are no more tiles.  (The longest walks come first, where there is no
+    // window.)
     struct Place {
-        int w, m, h, turn, r0, steps, first, turns;
+        int w, m, h, turn, r0, steps, first, turns;           // KEYS: `turns` steps from row `first` on, for each query head
         Reach all;
         KeyWalk walk;
-        __device__ __forceinline__ int row(int i) const { return KEYS ? first + i % turns * kStep : walk.row(i, kStep); }
     };
-    const auto place_of = [&](int unit) {
-        const int in = unit % per, turn = unit / per, w = in / heads, m = t.first_worker + w;
-        int r0 = (KEYS ? turn : tiles - 1 - turn) * kTile;
-        Reach all;
-        if (far) {                                            // all first keys see the whole chunk, where it is far from them
-            const Sequence s = sequence_of(a, m, turn * kChunk);
-            r0 = s.start;
-            all = Reach{turn * kChunk, turn * kChunk, min(turn * kChunk + kChunk, s.end) - 1, 0, s.start};
-            all.max_hi = s.start < s.end && turn * kChunk >= far_from(a, s) ? all.min_hi : -1;
-        } else if (KEYS) {
-            all = reach_of(a, m, r0, lane, KeyRows{a, t.partial != nullptr});
-        } else {
-            all = reach_of(a, m, r0, lane, QueryRows{a});
+    const auto next_place = [&](int& round) {
+        for (; round * static_cast<int>(gridDim.x) < units; ++round) {
+            const int unit = tile_of_round(round);
+            if (unit >= units) continue;
+            const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
+            int r0 = (KEYS ? turn : tiles - 1 - turn) * kTile;
+            Reach all;
+            if (far) {                                        // all first keys see the whole chunk, where it is far from them
+                const Sequence s = sequence_of(a, m, turn * kChunk);
+                r0 = s.start;
+                all = Reach{turn * kChunk, turn * kChunk, min(turn * kChunk + kChunk, s.end) - 1, 0, s.start};
+                all.max_hi = s.start < s.end && turn * kChunk >= far_from(a, s) ? all.min_hi : -1;
+            } else if (KEYS) {
+                all = reach_of(a, m, r0, lane, KeyRows{a, t.partial != nullptr});
+            } else {
+                all = reach_of(a, m, r0, lane, QueryRows{a});
+            }
+            const KeyWalk walk(all, a.sinks, kStep);
+            // queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes
+            const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
+            const int steps = KEYS ? turns * a.group : walk.steps;
+            if (steps == 0) continue;
+            ++round;
+            return Place{w, m, in - w * heads, turn, r0, steps, first, turns, all, walk};
         }
-        const KeyWalk walk(all, a.sinks, kStep);
-        // queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes
-        const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
-        return Place{w, m, in % heads, turn, r0, KEYS ? turns * a.group : walk.steps, first, turns, all, walk};
+        return Place{0, 0, 0, 0, 0, -1, 0, 0, Reach{}, KeyWalk(Reach{}, 0, kStep)};
     };
+    const auto own_row = [&](const Place& at, int row, Keys& keys) {
+        if (far) {
+            const Sequence s = sequence_of(a, at.m, at.turn * kChunk);
+            keys = Keys{at.all.min_lo, at.all.max_hi, s.start, 0};
+            return row < s.end && row - s.start < a.sinks;
+        }
+        return KEYS ? own_keys(a, at.m, row, KeyRows{a, t.partial != nullptr}, keys) : own_keys(a, at.m, row, QueryRows{a}, keys);
+    };
+    int round = 0;
     int fills_u = 0, fills_w = 0, loads = 0;                  // of the copying thread
 
     if (warp == 8) {
@@ -828,11 +866,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
         };
         bool ok = true;
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const Place at = place_of(unit);
-            if (at.steps == 0) continue;
+        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
+            const int kv = KEYS ? at.h : a.group_size.quotient(at.h);
             if (lane == 0) {
                 ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
                 if (ok) {
@@ -841,8 +876,9 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     copy_tile(own + kBytes, &t.map[KEYS ? 2 : 3][at.w], at.h, at.r0, loaded);    // Y: v or dout
                     ++loads;
                 }
-                for (int i = 0; i < at.steps && ok; ++i) {
-                    const int u = fills_u % kU, v = fills_w % kW, r = at.row(i), hs = KEYS ? at.h * a.group + i / at.turns : at.h / a.group;
+                for (int i = 0, turn = 0, hs = KEYS ? kv * a.group : kv; i < at.steps && ok; ++i, ++turn) {
+                    if (KEYS && turn == at.turns) turn = 0, ++hs;            // the next query head
+                    const int u = fills_u % kU, v = fills_w % kW, r = KEYS ? at.first + turn * kStep : at.walk.row(i, kStep);
                     ok = fills_u < kU || tile_wait<kLimit>(empty_u + 8 * u, (fills_u / kU - 1) & 1, &gave_up);
                     if (!ok) break;
                     barrier_expect(full_u + 8 * u, kBytes + (KEYS ? 2 * kStep * 4 : 0));
@@ -887,11 +923,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             for (int k = 0; k < kStep / 16; ++k) mma_tensor(to, from + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), kSums, more || k > 0);
         };
         int n = 0, tile = 0;                                  // steps and tiles so far
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const int steps = place_of(unit).steps, end = n + steps;
-            if (steps == 0) continue;
+        for (int steps = next_place(round).steps; ok && steps >= 0; steps = next_place(round).steps) {
+            const int end = n + steps;
             // Steps are numbered through all tiles here.  The waits for operands come in front of those for the warps, while earlier
             // products run.
             const auto wait_u = [&](int i) { if (i < end) await(full_u + 8 * (i % kU), i / kU); };
@@ -976,23 +1009,10 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             return ok;
         };
         int n = 0, tile = 0;
-        for (int round = 0; ok && round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const Place at = place_of(unit);
-            if (at.steps == 0) continue;
+        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
             const int row = at.r0 + quarter * 32 + lane;
             Keys keys{};
-            bool valid;
-            if (far) {
-                const Sequence s = sequence_of(a, at.m, at.turn * kChunk);
-                keys = Keys{at.all.min_lo, at.all.max_hi, s.start, 0};
-                valid = row < s.end && row - s.start < a.sinks;
-            } else if (KEYS) {
-                valid = own_keys(a, at.m, row, KeyRows{a, t.partial != nullptr}, keys);
-            } else {
-                valid = own_keys(a, at.m, row, QueryRows{a}, keys);
-            }
+            const bool valid = own_row(at, row, keys);
             const int exponent = kHalf ? grad_exponent(t, at.m) : 0;
             const float to_grad = kHalf ? exp2f(static_cast<float>(exponent) - kWeightExponent) : 1.0f;
             float lse = 0.0f, delta = 0.0f;
@@ -1001,9 +1021,10 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 lse = t.lse[from] + static_cast<float>(exponent);  // P with dS's power of two
                 delta = t.delta[from];
             }
-            for (int i = 0; i < at.steps; ++i, ++n) {
+            for (int i = 0, turn = 0; i < at.steps; ++i, ++n, ++turn) {
+                if (KEYS && turn == at.turns) turn = 0;
                 const unsigned s_at = tmem + kTmemScores + n % kScoreSets * 128 + half * 64 + lanes, g_at = tmem + kTmemGrads + half * 64 + lanes;
-                const int r = at.row(i), limit = !KEYS && i < at.walk.sink_steps ? at.all.min_lo : 0x7fffffff;
+                const int r = KEYS ? at.first + turn * kStep : at.walk.row(i, kStep), limit = !KEYS && i < at.walk.sink_steps ? at.all.min_lo : 0x7fffffff;
                 const bool masked = (!KEYS && i < at.walk.sink_steps) || r < at.all.max_lo || r + kStep - 1 > at.all.min_hi;
                 const float* column = stats_at + n % kU * 2 * kStep + half * 64;
                 if (!await(scored + 8 * (n % kScoreSets), n / kScoreSets)) break;

@@ -56,7 +56,8 @@ static AttentionArgs attention_args(const AttentionShape& s, const void* const* 
     a.rows = static_cast<int>(s.rows); a.heads = static_cast<int>(s.q_heads); a.kv_heads = static_cast<int>(s.kv_heads);
     a.group = a.heads / a.kv_heads; a.dim = static_cast<int>(s.head_dim);
     a.sequences = static_cast<int>(s.offsets ? s.sequences : 0);
-    a.period = static_cast<int>(std::min(s.offsets ? s.rows : s.period, s.rows));
+    a.period = divisor(static_cast<unsigned>(std::min(s.offsets ? s.rows : s.period, s.rows)));
+    a.group_size = divisor(static_cast<unsigned>(a.group));
     a.left = static_cast<int>(std::min(s.left, s.rows)); a.right = static_cast<int>(std::min(s.right, s.rows));
     a.sinks = static_cast<int>(std::min(s.sinks, s.rows));
     a.scale = s.scale;
@@ -100,7 +101,10 @@ static grawa_status launch_tiles(Kernel kernel, const TileArgs& t, int heads, in
 {
     GRAWA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     const int64_t units = (t.far ? t.chunks : ceil_div(t.a.rows, kTile)) * heads * t.workers;
-    return launch(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(units, kSms * per_sm))), threads, smem, stream, t);
+    TileArgs args = t;
+    args.per = divisor(static_cast<unsigned>(heads * t.workers));
+    args.per_worker = divisor(static_cast<unsigned>(heads));
+    return launch(kernel, dim3(static_cast<unsigned>(std::min<int64_t>(units, kSms * per_sm))), threads, smem, stream, args);
 }
 template <typename T>
 static grawa_status launch_forward(const TileArgs& t, cudaStream_t stream)
@@ -140,7 +144,8 @@ template <typename T>
 static grawa_status attention_stats(const StatsArgs& t, int M, cudaStream_t stream)
 {
     const int heads = t.a.heads + (t.longest ? t.a.kv_heads : 0);
-    return launch(attention_stats_kernel<T>, dim3(static_cast<unsigned>(t.pitch / 64), heads, M), kStatsThreads, 0, stream, t);
+    auto* const kernel = t.a.dim <= 64 ? attention_stats_kernel<T, 8> : attention_stats_kernel<T, 16>;
+    return launch(kernel, dim3(static_cast<unsigned>(t.pitch / 64), heads, M), kStatsThreads, 0, stream, t);
 }
 
 }  // namespace replica
@@ -240,7 +245,8 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* cons
 grawa_status grawa_selftest_window_attention_wait(grawa_stream_t stream)
 {
     TileArgs t{};                                             // one row of one head; nothing is read or written
-    t.a.rows = t.a.heads = t.a.kv_heads = t.a.group = t.a.period = 1;
+    t.a.rows = t.a.heads = t.a.kv_heads = t.a.group = 1;
+    t.a.period = t.a.group_size = divisor(1);
     t.a.dim = 64;
     t.a.scale = 1.0f;
     t.workers = 1;

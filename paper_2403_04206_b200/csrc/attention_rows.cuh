@@ -19,13 +19,27 @@ namespace replica {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// Division by a number that the host knows, of numbers below 2^31 (round-up multiplier of 33 bits, whose highest is the number itself).
+struct Divisor {
+    unsigned by, multiplier, shift;
+    __device__ __forceinline__ int quotient(int n) const { return static_cast<int>((__umulhi(static_cast<unsigned>(n), multiplier) + static_cast<unsigned>(n)) >> shift); }
+    __device__ __forceinline__ int remainder(int n) const { return n - quotient(n) * static_cast<int>(by); }
+};
+inline Divisor divisor(unsigned by)
+{
+    unsigned shift = 0;
+    while ((1ull << shift) < by) ++shift;
+    return {by, static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - by)) / by + 1), shift};
+}
+
 struct AttentionArgs {
     In q, k, v, dout, out, lse;             // dout, out (as stored by the forward call) and lse in the backward pass
     Out to[3];                              // forward: out, lse (may be NULL); backward: dq, dk, dv
     In offsets;                             // 64-bit integers, or NULL: sequences of `period` rows
     long long q_stride, k_stride, v_stride, out_stride;      // elements from row to row; dq has q's, dk k's, dv v's, dout out's
     int rows, heads, kv_heads, group, dim;  // group: query heads of a key head
-    int sequences, period;
+    int sequences;
+    Divisor period, group_size;
     int left, right, sinks;                 // each at most `rows`
     float scale;
 };
@@ -37,8 +51,8 @@ __device__ __forceinline__ Sequence sequence_of(const AttentionArgs& a, int m, i
 {
     const long long* offsets = static_cast<const long long*>(a.offsets.p[m]);
     if (offsets == nullptr) {
-        const int start = row - row % a.period;
-        return {start, a.period > a.rows - start ? a.rows : start + a.period};
+        const int start = row - a.period.remainder(row), length = static_cast<int>(a.period.by);
+        return {start, length > a.rows - start ? a.rows : start + length};
     }
     if (row >= a.rows || offsets[0] > row || offsets[a.sequences] <= row) return {0, 0};
     int lo = 0, hi = a.sequences;           // offsets[lo] <= row < offsets[hi]

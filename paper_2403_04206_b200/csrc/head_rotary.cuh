@@ -36,7 +36,7 @@ struct HeadArgs {
     long long x_stride[2], y_stride[2];     // backward: of x and dx, and of dy
     int heads[2];
     int dim, half, neighbours, words;       // words: of a head (kPairWords, kPairNext)
-    int chunks, per_chunk;                  // forward: a row's groups of heads are shared out among so many warps
+    int chunks, per_chunk;                  // forward: a row's steps are shared out among so many warps, so many each
     int parts;                              // backward: CTAs a worker
     int has_w[2], has_dw[2], has_dx[2], accumulate;
     float eps, inv_dim;
@@ -88,6 +88,35 @@ struct HeadLane {
             const uint4* w = reinterpret_cast<const uint4*>(head);
             unpack<T>(has[0] ? w[first[0]] : make_uint4(0, 0, 0, 0), a);
             unpack<T>(has[1] ? w[first[1]] : make_uint4(0, 0, 0, 0), b);
+        }
+    }
+    // A lane's share on its way: words as they are, single elements widened.
+    struct Held {
+        uint4 a, b;
+        float x[MODE == kPairAny ? N : 1], y[MODE == kPairAny ? N : 1];
+    };
+    __device__ __forceinline__ void fetch(const T* head, bool mine, Held& to) const
+    {
+        if constexpr (MODE == kPairAny) {
+            if (mine) load(head, to.x, to.y);
+            else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) to.x[e] = to.y[e] = 0.0f;
+            }
+        } else {
+            const uint4* w = reinterpret_cast<const uint4*>(head);
+            to.a = mine && has[0] ? __ldcs(w + first[0]) : make_uint4(0, 0, 0, 0);
+            to.b = mine && has[1] ? __ldcs(w + first[1]) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    static __device__ __forceinline__ void open(const Held& from, float (&a)[N], float (&b)[N])
+    {
+        if constexpr (MODE == kPairAny) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) a[e] = from.x[e], b[e] = from.y[e];
+        } else {
+            unpack<T>(from.a, a);
+            unpack<T>(from.b, b);
         }
     }
     __device__ __forceinline__ void store(T* head, const float (&a)[N], const float (&b)[N]) const
@@ -194,57 +223,71 @@ __device__ __forceinline__ void load_weights(const HeadArgs& a, int which, int m
     for (int e = threadIdx.x; e < a.dim; e += kHeadThreads) to[e] = a.has_w[which] ? widen(w[e]) : 1.0f;
 }
 
-// LPH: lanes a head.  A unit of work is a chunk of a row's heads.
+// A row's heads in steps of `per` neighbouring ones, those of the queries first.
+struct HeadSteps {
+    int q_steps, steps;
+    __device__ __forceinline__ HeadSteps(const HeadArgs& a, int per) : q_steps((a.heads[0] + per - 1) / per), steps(q_steps + (a.heads[1] + per - 1) / per) {}
+};
+
+// LPH: lanes a head.  A unit of work is a chunk of a row's steps, whose loads are under way kHeadAhead steps ahead, the first ones while the
+// row's angles are worked out (4 x 8192 rows of 32 + 8 heads of 128 bf16: 148 us with each step's loads in front of it).
+template <int MODE> constexpr int kHeadAhead = MODE == kPairAny ? 1 : 4;
 template <typename T, int LPH, int MODE>
-__global__ void __launch_bounds__(kHeadThreads)
+__global__ void __launch_bounds__(kHeadThreads, 2)
 head_rotary_forward_kernel(const __grid_constant__ HeadArgs a)
 {
-    constexpr int N = kHeadRun<T, MODE>, kPer = 32 / LPH, kWarps = kHeadThreads / 32;
+    constexpr int N = kHeadRun<T, MODE>, kPer = 32 / LPH, kWarps = kHeadThreads / 32, kAhead = kHeadAhead<MODE>;
     __shared__ __align__(16) float weights[2][kHeadDim];
     __shared__ float2 tables[kWarps][kHeadDim / 2];
     stream_order();
     const int m = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32, slot = lane / LPH;
     const HeadLane<T, MODE> at(a, lane % LPH);
-    load_weights<T>(a, 0, m, weights[0]);
-    if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
-    __syncthreads();
+    const HeadSteps all(a, kPer);
     const long long units = a.rows * a.chunks;
-    for (long long u = static_cast<long long>(blockIdx.x) * kWarps + warp; u < units; u += static_cast<long long>(gridDim.x) * kWarps) {
+    bool ready = false;                                       // the weights
+    for (long long u = static_cast<long long>(blockIdx.x) * kWarps + warp; u - warp < units; u += static_cast<long long>(gridDim.x) * kWarps) {
         const long long row = u / a.chunks;
-        const int begin = static_cast<int>(u % a.chunks) * a.per_chunk, end = min(begin + a.per_chunk, a.heads[0] + a.heads[1]);
+        const int begin = u < units ? static_cast<int>(u % a.chunks) * a.per_chunk : 0, end = u < units ? min(begin + a.per_chunk, all.steps) : 0;
+        const T* in[2] = {static_cast<const T*>(a.x[0].p[m]) + row * a.x_stride[0], static_cast<const T*>(a.x[1].p[m]) + row * a.x_stride[1]};
+        typename HeadLane<T, MODE>::Held held[kAhead];
+        const auto fetch = [&](int step, typename HeadLane<T, MODE>::Held& to) {
+            const int which = step >= all.q_steps, h = (step - (which ? all.q_steps : 0)) * kPer + slot;
+            if (step < end) at.fetch(in[which] + static_cast<long long>(h) * a.dim, h < a.heads[which], to);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(begin + i, held[i]);
+        if (!ready) {                                         // (all warps of the CTA come here for the first time together)
+            load_weights<T>(a, 0, m, weights[0]);
+            if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
+            __syncthreads();
+            ready = true;
+        }
+        if (begin >= end) continue;
         fill_angles(a, m, row, lane, tables[warp]);
         float c[N], s[N];
         at.angles(tables[warp], c, s);
 #pragma unroll 1
-        for (int which = 0; which < 2; ++which) {
-            const int from = which ? max(begin, a.heads[0]) - a.heads[0] : begin, to = which ? end - a.heads[0] : min(end, a.heads[0]);
-            if (from >= to) continue;
-            float wa[N], wb[N];
-            at.from_shared(weights[which], wa, wb);
-            const T* in = static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which];
-            T* out = static_cast<T*>(a.y[which].p[m]) + row * a.y_stride[which];
-#pragma unroll 2
-            for (int h0 = from; h0 < to; h0 += kPer) {
-                const int h = h0 + slot;
-                const bool mine = h < to;
-                float x[N], y[N], sum = 0.0f;
-                if (mine) at.load(in + static_cast<long long>(h) * a.dim, x, y);
-                else {
+        for (int first = begin; first < end; first += kAhead)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = y[e] = 0.0f;
-                }
+            for (int i = 0; i < kAhead; ++i) {
+                const int step = first + i;
+                if (step >= end) break;
+                const int which = step >= all.q_steps, h = (step - (which ? all.q_steps : 0)) * kPer + slot;
+                float x[N], y[N], wa[N], wb[N], sum = 0.0f;
+                at.open(held[i], x, y);
+                fetch(step + kAhead, held[i]);
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
                 const float r = rsqrtf(fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps));
+                at.from_shared(weights[which], wa, wb);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     x[e] = x[e] * r * wa[e];
                     y[e] = y[e] * r * wb[e];
                 }
                 at.turn(x, y, c, s, 1.0f);
-                if (mine) at.store(out + static_cast<long long>(h) * a.dim, x, y);
+                if (h < a.heads[which]) at.store(static_cast<T*>(a.y[which].p[m]) + row * a.y_stride[which] + static_cast<long long>(h) * a.dim, x, y);
             }
-        }
     }
 }
 
@@ -284,43 +327,45 @@ __global__ void __launch_bounds__(kHeadThreads, 2)
 head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
 {
     constexpr int N = kHeadRun<T, MODE>, kPer = 32 / LPH, kWarps = kHeadThreads / 32;
+    using Lane = HeadLane<T, MODE>;
     __shared__ __align__(16) float weights[2][kHeadDim];
     __shared__ float2 tables[kWarps][kHeadDim / 2];
     __shared__ float sums[kWarps * kHeadDim];
     stream_order();
     const int m = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32, slot = lane / LPH;
-    const HeadLane<T, MODE> at(a, lane % LPH);
+    const Lane at(a, lane % LPH);
     load_weights<T>(a, 0, m, weights[0]);
     if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
     __syncthreads();
     float da[2][N] = {}, db[2][N] = {};
     for (long long row = static_cast<long long>(blockIdx.x) * kWarps + warp; row < a.rows; row += static_cast<long long>(gridDim.x) * kWarps) {
+        typename Lane::Held held[2];                          // x and dy of the next step, on their way
+        const auto fetch = [&](int which, int h0) {
+            const int h = h0 + slot;
+            const long long place = static_cast<long long>(h) * a.dim;
+            at.fetch(static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which] + place, h < a.heads[which], held[0]);
+            at.fetch(static_cast<const T*>(a.dy[which].p[m]) + row * a.y_stride[which] + place, h < a.heads[which], held[1]);
+        };
+        fetch(0, 0);
         fill_angles(a, m, row, lane, tables[warp]);
         float c[N], s[N];
         at.angles(tables[warp], c, s);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            float wa[N], wb[N];
-            at.from_shared(weights[which], wa, wb);
-            const T* in = static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which];
-            const T* grad = static_cast<const T*>(a.dy[which].p[m]) + row * a.y_stride[which];
             T* out = static_cast<T*>(a.y[which].p[m]) + row * a.x_stride[which];
 #pragma unroll 1
             for (int h0 = 0; h0 < a.heads[which]; h0 += kPer) {
                 const int h = h0 + slot;
-                const bool mine = h < a.heads[which];
-                float x[N], y[N], u[N], v[N], square = 0.0f, along = 0.0f;
-                if (mine) {
-                    at.load(in + static_cast<long long>(h) * a.dim, x, y);
-                    at.load(grad + static_cast<long long>(h) * a.dim, u, v);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = y[e] = u[e] = v[e] = 0.0f;
-                }
+                float x[N], y[N], u[N], v[N], wa[N], wb[N], square = 0.0f, along = 0.0f;
+                Lane::open(held[0], x, y);
+                Lane::open(held[1], u, v);
+                if (h0 + kPer < a.heads[which]) fetch(which, h0 + kPer);
+                else if (which == 0 && a.heads[1]) fetch(1, 0);
                 at.turn(u, v, c, s, -1.0f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));
                 const float r = rsqrtf(fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps));
+                at.from_shared(weights[which], wa, wb);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {                 // x s first: s^2 may be past fp32's range where dx is inside it
                     x[e] *= r;
@@ -337,7 +382,7 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
                     u[e] = (u[e] - x[e] * along) * r;
                     v[e] = (v[e] - y[e] * along) * r;
                 }
-                if (mine && a.has_dx[which]) at.store(out + static_cast<long long>(h) * a.dim, u, v);
+                if (h < a.heads[which] && a.has_dx[which]) at.store(out + static_cast<long long>(h) * a.dim, u, v);
             }
         }
     }

@@ -107,17 +107,18 @@ static grawa_status with_lanes(int words, const F& f)
     return f(std::integral_constant<int, sizeof(T) == 4 ? 32 : 16>{});     // (16-bit heads have up to 32 words)
 }
 
+constexpr int kHeadCtas = 8;                                  // an SM's, at most: some turns of each
 template <typename T>
 static grawa_status head_forward(HeadArgs& a, int M, HeadMode mode, cudaStream_t stream)
 {
     const auto run = [&](auto kernel, int per) {
         constexpr int kWarps = kHeadThreads / 32;
-        const int64_t steps = ceil_div(a.heads[0] + a.heads[1], per);
+        const int64_t steps = ceil_div(a.heads[0], per) + ceil_div(a.heads[1], per);
         // rows whose warps would not fill the SMs are shared out among several each, down to one step of `per` heads
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, int64_t{kSms} * 32 / (a.rows * M)));
-        a.per_chunk = static_cast<int>(ceil_div(steps, want)) * per;
-        a.chunks = static_cast<int>(ceil_div(a.heads[0] + a.heads[1], a.per_chunk));
-        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows * a.chunks, kWarps), static_cast<int64_t>(kSms) * 32 / M));
+        a.per_chunk = static_cast<int>(ceil_div(steps, want));
+        a.chunks = static_cast<int>(ceil_div(steps, a.per_chunk));
+        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows * a.chunks, kWarps), static_cast<int64_t>(kSms) * kHeadCtas / M));
         return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kHeadThreads, 0, stream, a);
     };
     if (mode == kPairAny) return run(head_rotary_forward_kernel<T, 32, kPairAny>, 1);
