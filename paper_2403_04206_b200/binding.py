@@ -660,10 +660,8 @@ def _frequencies(frequencies, device):
     """Address and number of the rotated elements."""
     if frequencies is None:
         return None, 0
-    if str(frequencies.dtype) != "torch.float64":
-        raise TypeError(f"frequencies: expected float64, got {frequencies.dtype}")
-    _on_device(frequencies, device, "frequencies")
-    return _addr(frequencies), 2 * frequencies.numel()
+    address, count = _marshal.vector("frequencies", frequencies, device)
+    return address, 2 * count
 
 
 def _head_specs(q, k):

@@ -20,8 +20,10 @@ namespace replica {
 //   kPairWords  words a and b are word j and the word `half` elements behind it: pairs of halves, (a[e], b[e]);
 //               lanes behind the rotated part hold two neighbouring words
 //   kPairNext   two neighbouring words: pairs of neighbours, (a[2i], a[2i + 1]) and (b[2i], b[2i + 1])
-//   kPairAny    single elements, at any address and of any number: pair lane + 32 t for t < 4, then what is not rotated
-enum HeadMode { kPairWords = 0, kPairNext = 1, kPairAny = 2 };
+//   kPairAny    single elements, at any address and of any number: pair lane + 32 t for t < n / 2, then what is not rotated;
+//               kPairAnyShort for heads of up to 128 elements (n = 4), kPairAny for longer ones (n = 8)
+enum HeadMode { kPairWords = 0, kPairNext = 1, kPairAny = 2, kPairAnyShort = 3 };
+template <int MODE> constexpr bool kSingles = MODE >= kPairAny;
 constexpr int kHeadDim = 256;               // largest head
 constexpr int kHeadThreads = 256;
 
@@ -32,7 +34,7 @@ struct HeadArgs {
     In positions;                           // 64-bit integers, or NULL: row number modulo `period`
     const double* frequencies;
     float* partial;                         // backward, parts > 1: [worker][part][2][kHeadDim]
-    long long rows, period;
+    unsigned rows, period;
     long long x_stride[2], y_stride[2];     // backward: of x and dx, and of dy
     int heads[2];
     int dim, half, neighbours, words;       // words: of a head (kPairWords, kPairNext)
@@ -42,13 +44,13 @@ struct HeadArgs {
     float eps, inv_dim;
 };
 
-template <typename T, int MODE> constexpr int kHeadRun = MODE == kPairAny ? 8 : kWordElems<T>;
+template <typename T, int MODE> constexpr int kHeadRun = MODE == kPairAny ? 8 : MODE == kPairAnyShort ? 4 : kWordElems<T>;
 
 // The places of a lane's elements in a head, and their loads and stores.
 template <typename T, int MODE>
 struct HeadLane {
     static constexpr int N = kHeadRun<T, MODE>;
-    int first[2];                           // words: of a[] and b[]; kPairAny: unused
+    int first[2];                           // words: of a[] and b[]
     int dim, half, neighbours, lane;
     bool has[2];
 
@@ -62,22 +64,22 @@ struct HeadLane {
             first[0] = 2 * l;
             first[1] = 2 * l + 1;
         }
-        has[0] = MODE == kPairAny || first[0] < a.words;
-        has[1] = MODE == kPairAny || first[1] < a.words;
+        has[0] = kSingles<MODE> || first[0] < a.words;
+        has[1] = kSingles<MODE> || first[1] < a.words;
     }
-    // kPairAny: the place of element t of a[] (which = 0) or b[], or -1.
+    // Single elements: the place of element t of a[] (which = 0) or b[], or -1.
     __device__ __forceinline__ int place(int t, int which) const
     {
-        if (t < 4) {
+        if (t < N / 2) {
             const int p = lane + 32 * t;
             return p >= half ? -1 : neighbours ? 2 * p + which : p + which * half;
         }
-        const int e = 2 * half + lane + 32 * (2 * (t - 4) + which);
+        const int e = 2 * half + lane + 32 * (2 * (t - N / 2) + which);
         return e < dim ? e : -1;
     }
     __device__ __forceinline__ void load(const T* head, float (&a)[N], float (&b)[N]) const
     {
-        if constexpr (MODE == kPairAny) {
+        if constexpr (kSingles<MODE>) {
 #pragma unroll
             for (int t = 0; t < N; ++t) {
                 const int i = place(t, 0), j = place(t, 1);
@@ -93,11 +95,11 @@ struct HeadLane {
     // A lane's share on its way: words as they are, single elements widened.
     struct Held {
         uint4 a, b;
-        float x[MODE == kPairAny ? N : 1], y[MODE == kPairAny ? N : 1];
+        float x[kSingles<MODE> ? N : 1], y[kSingles<MODE> ? N : 1];
     };
     __device__ __forceinline__ void fetch(const T* head, bool mine, Held& to) const
     {
-        if constexpr (MODE == kPairAny) {
+        if constexpr (kSingles<MODE>) {
             if (mine) load(head, to.x, to.y);
             else {
 #pragma unroll
@@ -111,7 +113,7 @@ struct HeadLane {
     }
     static __device__ __forceinline__ void open(const Held& from, float (&a)[N], float (&b)[N])
     {
-        if constexpr (MODE == kPairAny) {
+        if constexpr (kSingles<MODE>) {
 #pragma unroll
             for (int e = 0; e < N; ++e) a[e] = from.x[e], b[e] = from.y[e];
         } else {
@@ -121,7 +123,7 @@ struct HeadLane {
     }
     __device__ __forceinline__ void store(T* head, const float (&a)[N], const float (&b)[N]) const
     {
-        if constexpr (MODE == kPairAny) {
+        if constexpr (kSingles<MODE>) {
 #pragma unroll
             for (int t = 0; t < N; ++t) {
                 const int i = place(t, 0), j = place(t, 1);
@@ -137,7 +139,7 @@ struct HeadLane {
     // The same places of a vector of kHeadDim floats in shared memory (what lies behind the head's end is not used).
     __device__ __forceinline__ void from_shared(const float* v, float (&a)[N], float (&b)[N]) const
     {
-        if constexpr (MODE == kPairAny) {
+        if constexpr (kSingles<MODE>) {
 #pragma unroll
             for (int t = 0; t < N; ++t) {
                 const int i = place(t, 0), j = place(t, 1);
@@ -158,8 +160,8 @@ struct HeadLane {
     {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int i = MODE == kPairAny ? place(e, 0) : has[0] ? first[0] * N + e : -1;
-            const int j = MODE == kPairAny ? place(e, 1) : has[1] ? first[1] * N + e : -1;
+            const int i = kSingles<MODE> ? place(e, 0) : has[0] ? first[0] * N + e : -1;
+            const int j = kSingles<MODE> ? place(e, 1) : has[1] ? first[1] * N + e : -1;
             if (i >= 0) v[i] = a[e];
             if (j >= 0) v[j] = b[e];
         }
@@ -170,7 +172,7 @@ struct HeadLane {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             int p;
-            if constexpr (MODE == kPairAny) p = e < 4 ? lane + 32 * e : half;
+            if constexpr (kSingles<MODE>) p = e < N / 2 ? lane + 32 * e : half;
             else if constexpr (MODE == kPairWords) p = first[0] * N + e;
             else p = first[e * 2 / N] * (N / 2) + e % (N / 2);
             const float2 t = p < half ? table[p] : make_float2(1.0f, 0.0f);
@@ -202,7 +204,7 @@ struct HeadLane {
 };
 
 // Cosine and sine of a row's pairs into the warp's table.
-__device__ __forceinline__ void fill_angles(const HeadArgs& a, int m, long long row, int lane, float2* table)
+__device__ __forceinline__ void fill_angles(const HeadArgs& a, int m, unsigned row, int lane, float2* table)
 {
     const long long* given = static_cast<const long long*>(a.positions.p[m]);
     const double position = static_cast<double>(given ? given[row] : row % a.period);
@@ -229,8 +231,27 @@ struct HeadSteps {
     __device__ __forceinline__ HeadSteps(const HeadArgs& a, int per) : q_steps((a.heads[0] + per - 1) / per), steps(q_steps + (a.heads[1] + per - 1) / per) {}
 };
 
-// LPH: lanes a head.  A unit of work is a chunk of a row's steps, whose loads are under way kHeadAhead steps ahead, the first ones while the
-// row's angles are worked out (4 x 8192 rows of 32 + 8 heads of 128 bf16: 148 us with each step's loads in front of it).
+// Where a warp stands in its chunks of rows: a chunk is a run of a row's steps.
+struct HeadWalk {
+    unsigned unit, row;
+    int step, end;
+    __device__ __forceinline__ void enter(const HeadArgs& a, int steps)
+    {
+        row = a.chunks == 1 ? unit : unit / a.chunks;
+        step = a.chunks == 1 ? 0 : static_cast<int>(unit - row * a.chunks) * a.per_chunk;
+        end = min(step + a.per_chunk, steps);
+    }
+    __device__ __forceinline__ bool inside(const HeadArgs& a) const { return unit < a.rows * static_cast<unsigned>(a.chunks); }
+    __device__ __forceinline__ void advance(const HeadArgs& a, int steps)
+    {
+        if (++step < end) return;
+        unit += gridDim.x * (kHeadThreads / 32);
+        enter(a, steps);
+    }
+};
+
+// LPH: lanes a head.  A step's loads are under way while the kHeadAhead steps in front of it are worked on, whatever rows they belong to
+// (4 x 8192 rows of 32 + 8 heads of 128 bf16: 148 us with each step's loads in front of it).
 template <int MODE> constexpr int kHeadAhead = MODE == kPairAny ? 1 : 4;
 template <typename T, int LPH, int MODE>
 __global__ void __launch_bounds__(kHeadThreads, 2)
@@ -243,51 +264,50 @@ head_rotary_forward_kernel(const __grid_constant__ HeadArgs a)
     const int m = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32, slot = lane / LPH;
     const HeadLane<T, MODE> at(a, lane % LPH);
     const HeadSteps all(a, kPer);
-    const long long units = a.rows * a.chunks;
-    bool ready = false;                                       // the weights
-    for (long long u = static_cast<long long>(blockIdx.x) * kWarps + warp; u - warp < units; u += static_cast<long long>(gridDim.x) * kWarps) {
-        const long long row = u / a.chunks;
-        const int begin = u < units ? static_cast<int>(u % a.chunks) * a.per_chunk : 0, end = u < units ? min(begin + a.per_chunk, all.steps) : 0;
-        const T* in[2] = {static_cast<const T*>(a.x[0].p[m]) + row * a.x_stride[0], static_cast<const T*>(a.x[1].p[m]) + row * a.x_stride[1]};
-        typename HeadLane<T, MODE>::Held held[kAhead];
-        const auto fetch = [&](int step, typename HeadLane<T, MODE>::Held& to) {
-            const int which = step >= all.q_steps, h = (step - (which ? all.q_steps : 0)) * kPer + slot;
-            if (step < end) at.fetch(in[which] + static_cast<long long>(h) * a.dim, h < a.heads[which], to);
-        };
+    HeadWalk now, ahead;
+    now.unit = blockIdx.x * kWarps + warp;
+    now.enter(a, all.steps);
+    ahead = now;
+    typename HeadLane<T, MODE>::Held held[kAhead];
+    const auto fetch = [&](typename HeadLane<T, MODE>::Held& to) {
+        if (!ahead.inside(a)) return;
+        const int which = ahead.step >= all.q_steps, h = (ahead.step - (which ? all.q_steps : 0)) * kPer + slot;
+        at.fetch(static_cast<const T*>(a.x[which].p[m]) + ahead.row * a.x_stride[which] + static_cast<long long>(h) * a.dim, h < a.heads[which], to);
+        ahead.advance(a, all.steps);
+    };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) fetch(begin + i, held[i]);
-        if (!ready) {                                         // (all warps of the CTA come here for the first time together)
-            load_weights<T>(a, 0, m, weights[0]);
-            if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
-            __syncthreads();
-            ready = true;
-        }
-        if (begin >= end) continue;
-        fill_angles(a, m, row, lane, tables[warp]);
-        float c[N], s[N];
-        at.angles(tables[warp], c, s);
-#pragma unroll 1
-        for (int first = begin; first < end; first += kAhead)
+    for (int i = 0; i < kAhead; ++i) fetch(held[i]);
+    load_weights<T>(a, 0, m, weights[0]);
+    if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
+    __syncthreads();
+    float c[N], s[N];
+    unsigned turned = ~0u;                                    // the unit that c and s are of
+    while (now.inside(a)) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int step = first + i;
-                if (step >= end) break;
-                const int which = step >= all.q_steps, h = (step - (which ? all.q_steps : 0)) * kPer + slot;
-                float x[N], y[N], wa[N], wb[N], sum = 0.0f;
-                at.open(held[i], x, y);
-                fetch(step + kAhead, held[i]);
-#pragma unroll
-                for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
-                const float r = rsqrtf(fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps));
-                at.from_shared(weights[which], wa, wb);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    x[e] = x[e] * r * wa[e];
-                    y[e] = y[e] * r * wb[e];
-                }
-                at.turn(x, y, c, s, 1.0f);
-                if (h < a.heads[which]) at.store(static_cast<T*>(a.y[which].p[m]) + row * a.y_stride[which] + static_cast<long long>(h) * a.dim, x, y);
+        for (int i = 0; i < kAhead; ++i) {
+            if (!now.inside(a)) break;
+            if (now.unit != turned) {
+                fill_angles(a, m, now.row, lane, tables[warp]);
+                at.angles(tables[warp], c, s);
+                turned = now.unit;
             }
+            const int which = now.step >= all.q_steps, h = (now.step - (which ? all.q_steps : 0)) * kPer + slot;
+            float x[N], y[N], wa[N], wb[N], sum = 0.0f;
+            at.open(held[i], x, y);
+            fetch(held[i]);
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
+            const float r = rsqrtf(fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps));
+            at.from_shared(weights[which], wa, wb);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                x[e] = x[e] * r * wa[e];
+                y[e] = y[e] * r * wb[e];
+            }
+            at.turn(x, y, c, s, 1.0f);
+            if (h < a.heads[which]) at.store(static_cast<T*>(a.y[which].p[m]) + now.row * a.y_stride[which] + static_cast<long long>(h) * a.dim, x, y);
+            now.advance(a, all.steps);
+        }
     }
 }
 
@@ -338,15 +358,16 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
     if (a.heads[1]) load_weights<T>(a, 1, m, weights[1]);
     __syncthreads();
     float da[2][N] = {}, db[2][N] = {};
-    for (long long row = static_cast<long long>(blockIdx.x) * kWarps + warp; row < a.rows; row += static_cast<long long>(gridDim.x) * kWarps) {
-        typename Lane::Held held[2];                          // x and dy of the next step, on their way
-        const auto fetch = [&](int which, int h0) {
-            const int h = h0 + slot;
-            const long long place = static_cast<long long>(h) * a.dim;
-            at.fetch(static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which] + place, h < a.heads[which], held[0]);
-            at.fetch(static_cast<const T*>(a.dy[which].p[m]) + row * a.y_stride[which] + place, h < a.heads[which], held[1]);
-        };
-        fetch(0, 0);
+    typename Lane::Held held[2];                              // x and dy of the next step, on their way
+    const auto fetch = [&](unsigned row, int which, int h0) {
+        const int h = h0 + slot;
+        const long long place = static_cast<long long>(h) * a.dim;
+        at.fetch(static_cast<const T*>(a.x[which].p[m]) + row * a.x_stride[which] + place, h < a.heads[which], held[0]);
+        at.fetch(static_cast<const T*>(a.dy[which].p[m]) + row * a.y_stride[which] + place, h < a.heads[which], held[1]);
+    };
+    const unsigned start = blockIdx.x * kWarps + warp, stride = gridDim.x * kWarps;
+    if (start < a.rows) fetch(start, 0, 0);
+    for (unsigned row = start; row < a.rows; row += stride) {
         fill_angles(a, m, row, lane, tables[warp]);
         float c[N], s[N];
         at.angles(tables[warp], c, s);
@@ -359,8 +380,9 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
                 float x[N], y[N], u[N], v[N], wa[N], wb[N], square = 0.0f, along = 0.0f;
                 Lane::open(held[0], x, y);
                 Lane::open(held[1], u, v);
-                if (h0 + kPer < a.heads[which]) fetch(which, h0 + kPer);
-                else if (which == 0 && a.heads[1]) fetch(1, 0);
+                if (h0 + kPer < a.heads[which]) fetch(row, which, h0 + kPer);
+                else if (which == 0 && a.heads[1]) fetch(row, 1, 0);
+                else if (row + stride < a.rows) fetch(row + stride, 0, 0);
                 at.turn(u, v, c, s, -1.0f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));

@@ -69,7 +69,7 @@ static HeadArgs head_args(const HeadShape& s, const void* const* q, const void* 
     }
     if (s.rotary) copy_table(a.positions, s.positions, s.M);
     a.frequencies = s.frequencies;
-    a.rows = s.rows; a.period = std::max<int64_t>(1, s.period);
+    a.rows = static_cast<unsigned>(s.rows); a.period = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(s.period, 0x7fffffff)));
     a.x_stride[0] = s.q_stride; a.x_stride[1] = s.k_stride;
     a.y_stride[0] = s.q_out_stride; a.y_stride[1] = s.k_out_stride;
     a.heads[0] = static_cast<int>(s.q_heads); a.heads[1] = static_cast<int>(s.k_heads);
@@ -91,9 +91,9 @@ static HeadMode head_mode(const HeadArgs& a, grawa_dtype dtype, int M, bool back
         whole = all_aligned(a.x[i].p, M, 16) && all_aligned(a.y[i].p, M, 16) && (!backward || all_aligned(a.dy[i].p, M, 16));
         if (a.rows > 1) whole = whole && a.x_stride[i] % word == 0 && a.y_stride[i] % word == 0;
     }
-    if (!whole) return kPairAny;
-    if (a.neighbours) return kPairNext;
-    return a.half % word == 0 ? kPairWords : kPairAny;
+    if (whole && a.neighbours) return kPairNext;
+    if (whole && a.half % word == 0) return kPairWords;
+    return a.dim <= 128 ? kPairAnyShort : kPairAny;
 }
 
 // Calls f with the number of lanes a head takes, each of which holds two of its words.
@@ -107,7 +107,7 @@ static grawa_status with_lanes(int words, const F& f)
     return f(std::integral_constant<int, sizeof(T) == 4 ? 32 : 16>{});     // (16-bit heads have up to 32 words)
 }
 
-constexpr int kHeadCtas = 8;                                  // an SM's, at most: some turns of each
+constexpr int kHeadCtas = 4;                                  // an SM's, at most: some turns of each
 template <typename T>
 static grawa_status head_forward(HeadArgs& a, int M, HeadMode mode, cudaStream_t stream)
 {
@@ -115,13 +115,14 @@ static grawa_status head_forward(HeadArgs& a, int M, HeadMode mode, cudaStream_t
         constexpr int kWarps = kHeadThreads / 32;
         const int64_t steps = ceil_div(a.heads[0], per) + ceil_div(a.heads[1], per);
         // rows whose warps would not fill the SMs are shared out among several each, down to one step of `per` heads
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, int64_t{kSms} * 32 / (a.rows * M)));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(steps, int64_t{kSms} * 32 / (int64_t{a.rows} * M)));
         a.per_chunk = static_cast<int>(ceil_div(steps, want));
         a.chunks = static_cast<int>(ceil_div(steps, a.per_chunk));
-        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(a.rows * a.chunks, kWarps), static_cast<int64_t>(kSms) * kHeadCtas / M));
+        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(int64_t{a.rows} * a.chunks, kWarps), static_cast<int64_t>(kSms) * kHeadCtas / M));
         return launch(kernel, dim3(static_cast<unsigned>(ctas), M), kHeadThreads, 0, stream, a);
     };
     if (mode == kPairAny) return run(head_rotary_forward_kernel<T, 32, kPairAny>, 1);
+    if (mode == kPairAnyShort) return run(head_rotary_forward_kernel<T, 32, kPairAnyShort>, 1);
     return with_lanes<T>(a.words, [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         return mode == kPairWords ? run(head_rotary_forward_kernel<T, L, kPairWords>, 32 / L) : run(head_rotary_forward_kernel<T, L, kPairNext>, 32 / L);
@@ -143,6 +144,7 @@ static grawa_status head_backward(const HeadArgs& a, int M, HeadMode mode, cudaS
     };
     grawa_status st;
     if (mode == kPairAny) st = run(head_rotary_backward_kernel<T, 32, kPairAny>);
+    else if (mode == kPairAnyShort) st = run(head_rotary_backward_kernel<T, 32, kPairAnyShort>);
     else
         st = with_lanes<T>(a.words, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;

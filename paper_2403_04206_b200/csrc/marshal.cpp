@@ -142,7 +142,33 @@ PyObject* tables(PyObject*, PyObject* args)
     }
 }
 
-PyMethodDef methods[] = {{"tables", tables, METH_VARARGS, "Checked pointer tables of a replica operator's tensors."}, {nullptr, nullptr, 0, nullptr}};
+// vector(name, tensor, device): address and number of elements of a contiguous float64 tensor on the device.
+PyObject* vector(PyObject*, PyObject* args)
+{
+    const char* name;
+    PyObject* item;
+    int device;
+    if (!PyArg_ParseTuple(args, "sOi", &name, &item, &device)) return nullptr;
+    try {
+        if (!THPVariable_Check(item)) { fail(PyExc_TypeError, name, "expected a tensor"); return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(item);
+        if (t.scalar_type() != at::kDouble) { fail(PyExc_TypeError, name, std::string("expected ") + c10::toString(at::kDouble) + ", got " + c10::toString(t.scalar_type())); return nullptr; }
+        if (!t.is_cuda() || t.get_device() != device) {
+            fail(PyExc_ValueError, name, "expected a tensor on the current CUDA device (" + std::to_string(device) + "), got " + t.device().str());
+            return nullptr;
+        }
+        if (!t.is_contiguous()) { fail(PyExc_ValueError, name, "expected a contiguous tensor"); return nullptr; }
+        return Py_BuildValue("KL", static_cast<unsigned long long>(reinterpret_cast<uint64_t>(t.data_ptr())), static_cast<long long>(t.numel()));
+    } catch (python_error& e) {                               // raised by a tensor's own Python code
+        e.restore();
+        return nullptr;
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+PyMethodDef methods[] = {{"vector", vector, METH_VARARGS, "Checked address and size of one float64 vector."}, {"tables", tables, METH_VARARGS, "Checked pointer tables of a replica operator's tensors."}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
