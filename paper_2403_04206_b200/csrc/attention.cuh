@@ -44,6 +44,7 @@ struct TileArgs {
     long long pitch;
     float* partial;                         // backward, where chunks of queries are set apart (or NULL): [worker][key head][chunk][dv, dk][first key][dim]
     int chunks, far;                        // far: this launch is of the chunks
+    int beside;                             // backward: this launch needs nothing of the one in front, only of those before that
     int first_worker, workers;
     Divisor per, per_worker;                // tiles of one place in the rows: of all heads and workers of the launch, of one worker
 };
@@ -740,10 +741,11 @@ constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
 constexpr int kPolynomial = 4;              // one in so many pairs of exponentials goes by the polynomial
 constexpr int kBackwardChunk = 32;          // columns of results on their way
-template <bool KEYS> constexpr int kSlotsU = KEYS ? 2 : 3;                        // of the operand that the scores take
-template <bool KEYS> constexpr int kSlotsW = KEYS ? 2 : 1;                        // of the one that dP takes
+template <int DP, bool KEYS> constexpr int kSlotsU = KEYS && DP == 128 ? 2 : 3;   // of the operand that the scores take
+template <int DP, bool KEYS> constexpr int kSlotsW = KEYS || DP == 64 ? 2 : 1;    // of the one that dP takes
 template <int DP, bool KEYS>
-constexpr int kBackwardSmem = (2 + kSlotsU<KEYS> + kSlotsW<KEYS>) * kTile * DP * 2 + (KEYS ? kSlotsU<KEYS> * 2 * kStep * 4 : 0) + 8 * 64 * kBackwardChunk + 1024;
+constexpr int kBackwardSmem = (2 + kSlotsU<DP, KEYS> + kSlotsW<DP, KEYS>) * kTile * DP * 2 + (KEYS ? kSlotsU<DP, KEYS> * 2 * kStep * 4 : 0) +
+                              8 * 64 * kBackwardChunk + 1024;
 
 // What keys are seen by; where first keys' far queries are set apart (`chunked`), sinks_end is the end of the sequence that has some.
 struct KeyRows {
@@ -766,8 +768,9 @@ struct KeyRows {
 // step are S = X U^T and dP = Y W^T with the tile's own X and Y; its sums take P W (dv) and dS U (dk, or dq).  While the
 // tensor cores work on one of them, the warps turn the other into an operand.
 //
-// Tensor memory, in columns: KEYS: dv 0, dk 128, S (then P) 256, dP (then dS) 384.  Else dq 0, S (then dS) 128 and 256 in turn, dP 384.
-// A warp's half of an operand stands where its half of the scores stood.
+// Tensor memory, in columns: KEYS: dv 0, dk 128 (64 with heads of 64), S (then P) 256 (and 128 in turn, with heads of 64), dP (then dS)
+// 384.  Else dq 0, S (then dS) 128 and 256 in turn, dP 384.  A warp's half of an operand stands where its half of the scores stood.
+// Where there are two places for S, a step's scores are there before the step in front is done.
 template <typename T, int DP, bool KEYS>
 __global__ void __launch_bounds__(kBackwardThreads, 1)
 attention_backward_kernel(const __grid_constant__ TileArgs t)
@@ -775,8 +778,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     constexpr unsigned long long kLimit = kAttentionWaitNs;
     constexpr bool kHalf = TypeCode<T>::value == 0;
     constexpr float kWeightExponent = kHalf ? 14.0f : 0.0f;               // of two, on P in half precision
-    constexpr int kU = kSlotsU<KEYS>, kW = kSlotsW<KEYS>, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS ? 1 : 2;
-    constexpr unsigned kTmemSum = KEYS ? 128 : 0, kTmemScores = KEYS ? 256 : 128, kTmemGrads = 384;
+    constexpr int kU = kSlotsU<DP, KEYS>, kW = kSlotsW<DP, KEYS>, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS && DP == 128 ? 1 : 2;
+    constexpr unsigned kTmemSum = KEYS ? DP : 0, kTmemScores = kScoreSets == 1 ? 256 : 128, kTmemGrads = 384;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 9];
     __shared__ unsigned tmem_slot;
@@ -809,7 +812,9 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     order_before();
     __syncthreads();
     order_after();
-    stream_order();
+    // The launch in front has waited for all before it, so that a launch that needs nothing of it may run beside it, and waits at its end.
+    if (t.beside) let_next_start();
+    else stream_order();
     const unsigned tmem = tmem_slot;
 
     const AttentionArgs& a = t.a;
@@ -950,7 +955,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             await(loaded, tile);
             wait_u(n);
             step_s(n);
-            if (!KEYS) {
+            if (kScoreSets == 2) {
                 wait_u(n + 1);
                 step_s(n + 1);
             }
@@ -958,14 +963,15 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             step_p(n);
             for (int i = n; i < end && ok; ++i) {
                 if (KEYS) {
-                    wait_u(i + 1);
+                    if (kScoreSets == 1) wait_u(i + 1);
                     if (!await(weighted, i)) break;
                     if (one_lane()) {
-                        add(tmem, tmem + kTmemScores, ring_w + i % kW * kBytes, i > n);
+                        add(tmem, tmem + kTmemScores + i % kScoreSets * 128, ring_w + i % kW * kBytes, i > n);
                         mma_done(empty_w + 8 * (i % kW));
                     }
                     __syncwarp();
-                    step_s(i + 1);
+                    if (kScoreSets == 2) wait_u(i + 2);
+                    step_s(i + kScoreSets);
                     wait_w(i + 1);
                     if (!await(differed, i)) break;
                     if (one_lane()) {
@@ -1116,7 +1122,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll 1
                     for (int d = 0; d < DP; d += 32) {
                         unsigned v[32];
-                        tensor_load(tmem + half * 128 + lanes + d, v);
+                        tensor_load(tmem + half * kTmemSum + lanes + d, v);
                         tensor_wait(v);
 #pragma unroll
                         for (int e = 0; e < 32; e += 8)
@@ -1137,7 +1143,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     };
                     const long long stride = half ? a.k_stride : a.v_stride;
                     T* to = static_cast<T*>(a.to[half ? 1 : 2].p[at.m]) + (at.r0 + quarter * 32) * stride + static_cast<long long>(at.h) * a.dim;
-                    const bool fine = store_rows<T, kBackwardChunk>(tmem + half * 128 + lanes, 0, DP, half ? of_grad : exp2f(-kWeightExponent), stage, to, stride,
+                    const bool fine = store_rows<T, kBackwardChunk>(tmem + half * kTmemSum + lanes, 0, DP, half ? of_grad : exp2f(-kWeightExponent), stage, to, stride,
                                                                     a.dim, rows_valid, add);
                     __syncwarp();
                     for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
@@ -1165,6 +1171,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         for (int f = max(0, fills_w - kW); f < fills_w; ++f) tile_wait<kLimit>(full_w + 8 * (f % kW), (f / kW) & 1, nullptr);
     }
     if (warp == 9) tensor_free<512>(tmem);
+    if (t.beside) wait_for_previous();
 }
 
 }  // namespace replica

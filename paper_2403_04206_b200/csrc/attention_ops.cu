@@ -234,10 +234,21 @@ grawa_status grawa_window_attention_backward(grawa_dtype dtype, const void* cons
     grawa_status st = dtype == GRAWA_BF16 ? attention_stats<__nv_bfloat16>(stats, M, stream) : attention_stats<__half>(stats, M, stream);
     for (int first = 0; first < M && st == GRAWA_OK; first += kAttentionWorkers) {
         st = set_workers(t, s, first, std::min(kAttentionWorkers, M - first));
-        for (t.far = t.partial ? 1 : 0; t.far >= 0 && st == GRAWA_OK && dk; --t.far)
-            st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, true>(t, stream) : launch_backward<__half, true>(t, stream);
-        t.far = 0;
-        if (st == GRAWA_OK && dq) st = dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, false>(t, stream) : launch_backward<__half, false>(t, stream);
+        // dq needs nothing of dk and dv: its kernel runs beside the one in front, wherever that leaves SMs free.  (3 x 1001 tokens, 6 heads on 2 of
+        // 80: 59 us one after the other.)  The chunks' sums come before the tiles that add them.
+        const auto keys = [&](int far) {
+            t.far = far;
+            t.beside = 0;
+            return dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, true>(t, stream) : launch_backward<__half, true>(t, stream);
+        };
+        const auto queries = [&] {
+            t.far = 0;
+            t.beside = dk != nullptr;
+            return dtype == GRAWA_BF16 ? launch_backward<__nv_bfloat16, false>(t, stream) : launch_backward<__half, false>(t, stream);
+        };
+        if (st == GRAWA_OK && dk) st = keys(t.partial ? 1 : 0);
+        if (st == GRAWA_OK && dq) st = queries();
+        if (st == GRAWA_OK && dk && t.partial) st = keys(0);
     }
     return st;
 }
