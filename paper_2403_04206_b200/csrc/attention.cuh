@@ -4,9 +4,10 @@
 // are seen by, some at a time: the first keys of the sequence that the tile's first row belongs to, then one run of rows (of
 // the tile's other sequences, which begin inside it, all rows lie in that run).  Rows are packed, so a tile may hold the ends of
 // some sequences and the starts of others; the mask of a row is two intervals, which a thread turns into bits where a
-// step is not visible throughout.  One thread fetches operands by TMA, one issues tcgen05.mma, and each thread of the other warps has
-// one row of the tile: its scores come from tensor memory, and what it makes of them goes back there as the next product's
-// operand, so nothing but tiles of q, k, v and dout passes through shared memory.
+// step is not visible throughout.  One thread fetches operands by TMA, one warp issues tcgen05.mma, and the threads of eight others have
+// half of a row of the tile each: its scores come from tensor memory, and what they make of them goes back there as the next
+// product's operand, so nothing but tiles of q, k, v and dout passes through shared memory.  A step is 128 rows wide, because products
+// of two operands in shared memory take the tensor cores as long for 64 columns as for 128.
 //
 //   forward    S = Q K^T, P = exp2(S c - m), O += P V.  m is a row's largest score so far, but is only moved when that grows
 //              by more than 2^8 (P stays below 2^8), so that O, which lies in tensor memory, is rarely scaled.
@@ -18,6 +19,11 @@
 //
 // A masked element of P and dS is an exact zero.  Where the value it multiplies is not finite the product is NaN all the same, and spoils
 // rows that do not see it: a row with such a result is computed again by its warp alone (attention_rows.cuh).
+//
+// Measured (B200, back to back, where the power limit holds the clock at 1.6 GHz): 2 x 8192 tokens, 16 query heads on 8 of 128, causal, bf16:
+// forward 590 us (930 TFLOP/s, at 55 % of the tensor pipe's cycles), backward 1850 us (740); what bounds a CTA is the way of a step from
+// its scores to their exponentials to the next product, three waits of some hundred cycles each beside the arithmetic's, and
+// what bounds the SM is power.
 //
 // Every wait for a barrier in shared memory is bounded, as in the gated feed-forward product: a wait that runs out is counted
 // in g_attention_timeouts, and the CTA waits (bounded) for its copies and products in flight, frees its tensor memory
@@ -50,7 +56,7 @@ struct TileArgs {
 };
 
 __device__ unsigned g_attention_timeouts = 0;   // waits that ran out, never set back
-constexpr unsigned long long kAttentionWaitNs = 2000000000ull, kAttentionStarvedNs = 2000000ull;
+constexpr unsigned long long kAttentionWaitNs = 10000000000ull, kAttentionStarvedNs = 2000000ull;
 
 // ------------------------------------------------------------------ copies, products, tensor memory
 
@@ -378,7 +384,9 @@ __device__ __forceinline__ void store_eight(float* to, const float* v)
 // that the products of one run beside the exponentials of the other; each takes one tile after the other, and fetches the next one's
 // queries while it works.  Two threads share a row, one half of a step's scores each: what they wait for one after the other (scores,
 // their exponentials, the sum) bounds a CTA.
-constexpr int kForwardPolynomial = 8;       // one in so many pairs of exponentials goes by the polynomial
+// One in so many pairs of exponentials goes by the polynomial.  (2 x 8192 tokens, 16 heads of 64, causal: 471 us with none, 443 with one in 8,
+// 448 in 4, 516 in 2: its integer steps crowd the other pipe.)
+constexpr int kForwardPolynomial = 8;
 constexpr int kForwardThreads = 320;        // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 4;
 constexpr int kForwardChunk = 16;           // columns of results on their way
@@ -721,7 +729,7 @@ attention_stats_kernel(const __grid_constant__ StatsArgs t)
 __device__ __forceinline__ int grad_exponent(const TileArgs& t, int m)
 {
     if (t.longest == nullptr) return 0;
-    const float most = 2.0f * sqrtf(t.longest[2 * m]) * sqrtf(t.longest[2 * m + 1]);
+    const float most = 2.0f * sqrtf(__ldcg(t.longest + 2 * m)) * sqrtf(__ldcg(t.longest + 2 * m + 1));
     if (!(most > 0.0f && most < INFINITY)) return 0;
     return max(-100, min(100, 14 - ilogbf(most)));
 }
@@ -739,7 +747,8 @@ __device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& 
 
 constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
-constexpr int kPolynomial = 4;              // one in so many pairs of exponentials goes by the polynomial
+// As kForwardPolynomial.  (The same tokens, dk and dv / dq: 829 / 721 us with none, 790 / 611 with one in 4, 835 / 663 in 2.)
+constexpr int kPolynomial = 4;
 constexpr int kBackwardChunk = 32;          // columns of results on their way
 template <int DP, bool KEYS> constexpr int kSlotsU = KEYS && DP == 128 ? 2 : 3;   // of the operand that the scores take
 template <int DP, bool KEYS> constexpr int kSlotsW = KEYS || DP == 64 ? 2 : 1;    // of the one that dP takes
@@ -813,8 +822,13 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     __syncthreads();
     order_after();
     // The launch in front has waited for all before it, so that a launch that needs nothing of it may run beside it, and waits at its end.
-    if (t.beside) let_next_start();
-    else stream_order();
+    // (The fence keeps reads from what its SM may hold of older results.)
+    if (t.beside) {
+        let_next_start();
+        __threadfence();
+    } else {
+        stream_order();
+    }
     const unsigned tmem = tmem_slot;
 
     const AttentionArgs& a = t.a;
@@ -1024,8 +1038,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             float lse = 0.0f, delta = 0.0f;
             if (!KEYS && valid) {
                 const long long from = (static_cast<long long>(at.m) * a.heads + at.h) * t.pitch + row;
-                lse = t.lse[from] + static_cast<float>(exponent);  // P with dS's power of two
-                delta = t.delta[from];
+                lse = __ldcg(t.lse + from) + static_cast<float>(exponent);  // P with dS's power of two
+                delta = __ldcg(t.delta + from);
             }
             for (int i = 0, turn = 0; i < at.steps; ++i, ++n, ++turn) {
                 if (KEYS && turn == at.turns) turn = 0;

@@ -22,6 +22,7 @@ struct AttentionShape {
 
 static bool attention_shape_ok(const AttentionShape& s)
 {
+    constexpr int64_t kMostStride = int64_t{1} << 38;          // of a tensor map, in elements
     if ((s.dtype != GRAWA_BF16 && s.dtype != GRAWA_F16) || s.M < 1 || s.M > GRAWA_MAX_WORKERS) return false;
     if (s.rows < 0 || s.rows > 0x7fffffff - 1024 || s.q_heads < 1 || s.q_heads > 0x7fff || s.kv_heads < 1 || s.q_heads % s.kv_heads != 0) return false;
     if (ceil_div(s.rows, kTile) * s.q_heads * std::min(s.M, kAttentionWorkers) > 0x7fffffff - 4096) return false;          // tiles of a launch
@@ -29,9 +30,9 @@ static bool attention_shape_ok(const AttentionShape& s)
     if (s.left < 0 || s.right < 0 || s.sinks < 0 || !(s.scale > 0.0f) || std::isinf(s.scale)) return false;
     if (s.offsets ? s.sequences < 0 || s.sequences > 0x7fffffff - 1 : s.period < 1) return false;
     for (const int64_t stride : {s.q_stride, s.out_stride})
-        if (stride % 8 != 0 || !stride_ok(s.rows, s.q_heads * s.head_dim, stride)) return false;
+        if (stride % 8 != 0 || stride > kMostStride || !stride_ok(s.rows, s.q_heads * s.head_dim, stride)) return false;
     for (const int64_t stride : {s.k_stride, s.v_stride})
-        if (stride % 8 != 0 || !stride_ok(s.rows, s.kv_heads * s.head_dim, stride)) return false;
+        if (stride % 8 != 0 || stride > kMostStride || !stride_ok(s.rows, s.kv_heads * s.head_dim, stride)) return false;
     return true;
 }
 

@@ -222,3 +222,31 @@ def test_no_rows():
     c.window["period"] = None
     c.forward()
     c.backward()
+
+
+def test_rows_of_nothing_but_nan_end_and_stay_nan():
+    """A replica that has diverged: every row is NaN, and the calls return as ever."""
+    import paper_2403_04206_b200 as grawa
+    c = Case(torch.bfloat16, 3000, 2, 1, 128, seed=11)
+    for t in c.q + c.k + c.v + c.dout:
+        t.fill_(float("nan"))
+    c.forward()
+    c.backward()
+    assert grawa.grawa_window_attention_status() == 0
+    for t in c.out + c.dq + c.dk + c.dv:
+        assert t.isnan().all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_infinite_values_of_a_seen_key(dim):
+    """An infinity in a value: an infinity or NaN in that element of exactly the rows that see it, and finite numbers beside it."""
+    c = Case(torch.float16, 900, 2, 2, dim, left=200, seed=12)
+    for t in c.v:
+        t[300, 1, 5] = float("inf")
+    c.forward()
+    for m in range(c.M):
+        bad = ~torch.isfinite(c.out[m].float())
+        want = torch.zeros_like(bad)
+        want[300:501, 1, 5] = True
+        # a weight that rounds to zero gives NaN or zero times infinity: not finite either way
+        assert torch.equal(bad, want)
