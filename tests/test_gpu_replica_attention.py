@@ -250,3 +250,26 @@ def test_infinite_values_of_a_seen_key(dim):
         want[300:501, 1, 5] = True
         # a weight that rounds to zero gives NaN or zero times infinity: not finite either way
         assert torch.equal(bad, want)
+
+
+def test_rows_past_2_31_elements():
+    """q, k, v and their gradients side by side in rows so far apart that the last ones lie past 2^31 elements: the bits of packed ones."""
+    import paper_2403_04206_b200 as grawa
+    rows, stride = 17000, 131200
+    assert rows * stride > 2 ** 31
+    wide = torch.empty(rows, stride, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    at = {name: wide[:, 64 * i:64 * (i + 1)].unflatten(1, (1, 64)) for i, name in enumerate(("q", "k", "v", "dout", "out", "dq", "dk", "dv", "q2", "dq2"))}
+    own = {name: torch.randn(rows, 1, 64, generator=gen, device="cuda").bfloat16() for name in at}
+    for name in ("q", "k", "v", "dout"):
+        at[name].copy_(own[name])
+    lse = [torch.empty(1, rows, device="cuda") for _ in range(2)]
+    for t, s in zip((own, at), lse):
+        one = {k: [v] for k, v in t.items()}
+        grawa.grawa_window_attention_forward(one["q"], one["k"], one["v"], one["out"], lse=[s], left=99, sinks=3)
+        grawa.grawa_window_attention_backward(one["dout"], one["q"], one["k"], one["v"], one["out"], [s], one["dq"], one["dk"], one["dv"], left=99, sinks=3)
+        grawa.grawa_head_rotary_forward(one["q"], None, None, None, one["q2"], None, None)
+        grawa.grawa_head_rotary_backward(one["dout"], None, one["q"], None, None, None, one["dq2"], None, None, None, None)
+    assert torch.equal(*lse)
+    for name in at:
+        assert torch.equal(own[name], at[name]), name

@@ -158,3 +158,16 @@ def test_captured_and_on_another_stream():
         both()
     torch.cuda.current_stream().wait_stream(stream)
     assert all(torch.equal(a, b) for a, b in zip(results, want))
+
+
+def test_far_positions_keep_their_digits():
+    """Positions of billions: the angles are those of 64 bits (off by 2^-53 of themselves), as in 32 bits not even their sign would be."""
+    import paper_2403_04206_b200 as grawa
+    gen, M, q, k, qw, kw, f, where, _ = sizes((64, 2, 1, 64, 64, 0, 0), torch.float32, "halves", True, seed=5)
+    where["positions"] = [torch.randint(0, 1 << 32, (64,), generator=gen, device="cuda") for _ in range(M)]
+    out, k_out = [torch.empty_like(t) for t in q], [torch.empty_like(t) for t in k]
+    grawa.grawa_head_rotary_forward(q, k, qw, kw, out, k_out, f, **where)
+    for m in range(M):
+        want, error = head_rotary64(q[m], qw[m], where["positions"][m], f, "halves", EPS)
+        # two products and a reduction on either side, each 2^-53 of an angle of up to 2^32, against elements of up to 8
+        check(out[m], want, torch.float32, error + 8 * 6 * 2.0 ** (32 - 53))
