@@ -471,6 +471,7 @@ def grawa_sumsq_static(grads, sumsq_out, *, stream=None, n=None) -> None:
 # ------------------------------------------------------------------ replica operators
 
 _marshal = None
+_addresses = {}                               # of entry points
 _ROWS, _OPTIONAL, _FLOAT32, _INT64 = 1, 2, 4, 8          # modes of a table, as in csrc/marshal.cpp; << 8: the head dimension
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 _PAIRINGS = {"halves": 0, "neighbours": 1}
@@ -489,6 +490,14 @@ def _tables(first, specs):
         torch.cuda.init()
     device = torch._C._cuda_getDevice()
     return _marshal.tables(first, device, specs) + (device,)
+
+
+def _call(name, *args) -> int:
+    """Status of an entry point, called by way of the native marshaller (loaded by _tables)."""
+    address = _addresses.get(name)
+    if address is None:
+        address = _addresses[name] = ctypes.cast(getattr(library(), name), ctypes.c_void_p).value
+    return getattr(_marshal, name)(address, *args)
 
 
 def _stream_on(stream, device) -> int:
@@ -686,7 +695,7 @@ def grawa_head_rotary_forward(q, k, q_weight, k_weight, q_out, k_out, frequencie
         ("k_weight", k_weight, dim, 1, _OPTIONAL), ("q_out", q_out, rows, heads * dim, mode),
         ("k_out", k_out, rows, kv_heads * dim, mode if kv_heads else mode | _OPTIONAL), ("positions", positions, rows, 1, _OPTIONAL | _INT64)))
     f, rotary = _frequencies(frequencies, dev)
-    status = library().grawa_head_rotary_forward(code, _PAIRINGS[pairing], qt, kt, qw, kw, qo, ko, pos, f, rows, heads, kv_heads, dim, rotary, qs >> 4, ks >> 4,
+    status = _call("grawa_head_rotary_forward", code, _PAIRINGS[pairing], qt, kt, qw, kw, qo, ko, pos, f, rows, heads, kv_heads, dim, rotary, qs >> 4, ks >> 4,
                                                  qos >> 4, kos >> 4, (rows or 1) if period is None else period, len(q), eps, _stream_on(stream, dev))
     _raise(status, "grawa_head_rotary_forward")
 
@@ -710,7 +719,7 @@ def grawa_head_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, dq, dk,
     keep = workspace
     if keep is None and (dq_weight is not None or dk_weight is not None):
         keep = _scratch(None, lib.grawa_head_rotary_backward_workspace_bytes(rows, M), stream)
-    status = lib.grawa_head_rotary_backward(code, _PAIRINGS[pairing], qo, ko, qt, kt, qw, kw, dqt, dkt, dqw, dkw, pos, f, rows, heads, kv_heads, dim, rotary,
+    status = _call("grawa_head_rotary_backward", code, _PAIRINGS[pairing], qo, ko, qt, kt, qw, kw, dqt, dkt, dqw, dkw, pos, f, rows, heads, kv_heads, dim, rotary,
                                             qs >> 4, ks >> 4, qos >> 4, kos >> 4, (rows or 1) if period is None else period, M, eps, 1 if accumulate else 0,
                                             *_scratch_args(keep, dev), _stream_on(stream, dev))
     _raise(status, "grawa_head_rotary_backward")
@@ -739,7 +748,7 @@ def grawa_window_attention_forward(q, k, v, out, *, lse=None, offsets=None, peri
     code, qt, qs, kt, ks, vt, vs, ot, os, lt, _, off, _, dev = _tables(q, (
         ("q", q, rows, heads * dim, mode), ("k", k, rows, kv_heads * dim, mode), ("v", v, rows, kv_heads * dim, mode), ("out", out, rows, heads * dim, mode),
         ("lse", lse, heads, rows, _OPTIONAL | _FLOAT32), ("offsets", offsets, length, 1, _OPTIONAL | _INT64)))
-    status = library().grawa_window_attention_forward(code, qt, kt, vt, ot, lt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4, os >> 4,
+    status = _call("grawa_window_attention_forward", code, qt, kt, vt, ot, lt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4, os >> 4,
                                                       len(q), dim ** -0.5 if scale is None else scale, _stream_on(stream, dev))
     _raise(status, "grawa_window_attention_forward")
 
@@ -762,7 +771,7 @@ def grawa_window_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, *, offs
     keep = workspace
     if keep is None:
         keep = _scratch(None, lib.grawa_window_attention_backward_workspace_bytes(rows, heads, kv_heads, dim, sinks, M), stream)
-    status = lib.grawa_window_attention_backward(code, gt, qt, kt, vt, ot, lt, dqt, dkt, dvt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4,
+    status = _call("grawa_window_attention_backward", code, gt, qt, kt, vt, ot, lt, dqt, dkt, dvt, off, *window, rows, heads, kv_heads, dim, qs >> 4, ks >> 4, vs >> 4,
                                                  os >> 4, M, dim ** -0.5 if scale is None else scale, *_scratch_args(keep, dev), _stream_on(stream, dev))
     _raise(status, "grawa_window_attention_backward")
 

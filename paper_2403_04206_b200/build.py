@@ -74,7 +74,8 @@ def _build_ops(force: bool, verbose: bool = False) -> list:
 
 def build_marshal(force: bool = False) -> str:
     """Compiles the marshaller when missing or older than its source; returns its path."""
-    if force or not os.path.exists(MARSHAL_PATH) or os.path.getmtime(MARSHAL_SOURCE) > os.path.getmtime(MARSHAL_PATH):
+    header = os.path.join(_ROOT, "include", "grawa.h")
+    if force or not os.path.exists(MARSHAL_PATH) or any(os.path.getmtime(p) > os.path.getmtime(MARSHAL_PATH) for p in (MARSHAL_SOURCE, header)):
         import sysconfig
         import torch
         base = os.path.dirname(torch.__file__)

@@ -8,9 +8,14 @@
 
 #include <Python.h>
 
+#include "../../include/grawa.h"
+
 #include <cstdint>
 #include <memory>
 #include <string>
+#include <tuple>
+#include <type_traits>
+#include <utility>
 
 namespace {
 
@@ -168,7 +173,57 @@ PyObject* vector(PyObject*, PyObject* args)
     }
 }
 
-PyMethodDef methods[] = {{"vector", vector, METH_VARARGS, "Checked address and size of one float64 vector."}, {"tables", tables, METH_VARARGS, "Checked pointer tables of a replica operator's tensors."}, {nullptr, nullptr, 0, nullptr}};
+// A C value from a Python one: pointers from integers (addresses), bytes (their contents) or None, numbers from numbers.
+template <typename A>
+A c_value(PyObject* o)
+{
+    if constexpr (std::is_pointer_v<A>) {
+        if (o == Py_None) return nullptr;
+        if (PyBytes_Check(o)) return reinterpret_cast<A>(PyBytes_AS_STRING(o));
+        return reinterpret_cast<A>(PyLong_AsUnsignedLongLong(o));
+    } else if constexpr (std::is_floating_point_v<A>) {
+        return static_cast<A>(PyFloat_AsDouble(o));
+    } else {
+        return static_cast<A>(PyLong_AsLongLong(o));
+    }
+}
+template <typename... A, size_t... I>
+PyObject* call_with(grawa_status (*fn)(A...), PyObject* const* args, std::index_sequence<I...>)
+{
+    const std::tuple<A...> values{c_value<A>(args[I])...};
+    if (PyErr_Occurred()) return nullptr;
+    grawa_status status;
+    Py_BEGIN_ALLOW_THREADS
+    status = std::apply(fn, values);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+// call(address of the library's entry point, its arguments...): by way of ctypes the conversion of 25 arguments takes 2 us.
+template <typename... A>
+PyObject* call_entry(grawa_status (*)(A...), PyObject* const* args, Py_ssize_t count)
+{
+    if (count != static_cast<Py_ssize_t>(sizeof...(A)) + 1) {
+        PyErr_Format(PyExc_TypeError, "%zd arguments are needed, got %zd", static_cast<Py_ssize_t>(sizeof...(A)) + 1, count);
+        return nullptr;
+    }
+    auto* const fn = reinterpret_cast<grawa_status (*)(A...)>(PyLong_AsUnsignedLongLong(args[0]));
+    if (fn == nullptr || PyErr_Occurred()) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "expected the address of an entry point");
+        return nullptr;
+    }
+    return call_with(fn, args + 1, std::index_sequence_for<A...>{});
+}
+#define GRAWA_ENTRY(name) \
+    PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t count) { return call_entry(static_cast<decltype(&::grawa_##name)>(nullptr), args, count); }
+GRAWA_ENTRY(head_rotary_forward)
+GRAWA_ENTRY(head_rotary_backward)
+GRAWA_ENTRY(window_attention_forward)
+GRAWA_ENTRY(window_attention_backward)
+#define GRAWA_METHOD(name) {"grawa_" #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, "The entry point of this name, given its address first."}
+
+PyMethodDef methods[] = {{"vector", vector, METH_VARARGS, "Checked address and size of one float64 vector."}, {"tables", tables, METH_VARARGS, "Checked pointer tables of a replica operator's tensors."},
+                         GRAWA_METHOD(head_rotary_forward), GRAWA_METHOD(head_rotary_backward), GRAWA_METHOD(window_attention_forward),
+                         GRAWA_METHOD(window_attention_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
