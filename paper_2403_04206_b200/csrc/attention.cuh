@@ -326,6 +326,15 @@ __device__ __forceinline__ unsigned seen_keys(const Keys& k, int j, int limit)
     return bits_between(k.lo - j, hi - j) | bits_between(k.start - j, min(k.sinks_end - 1, hi) - j);
 }
 
+// The tiles of a CTA on their way from the copying warp, which works them out ahead of the others, to these.
+constexpr int kPlaces = 4;
+template <typename P>
+struct PlaceRing {
+    P* slots;                               // in shared memory
+    unsigned there, free;                   // barriers of the slots
+    __device__ __forceinline__ const P& operator[](int tile) const { return slots[tile % kPlaces]; }
+};
+
 // 32 rows of results on their way from tensor memory to memory, a warp's own: columns [from_col, from_col + cols) of the row's
 // `elements`, at `tensor` on, with what `add` adds to the 32 values from a column on, times f.  A thread has a row, but whole
 // sectors of neighbouring rows are what memory takes well: CHUNK columns at a time pass through 64 CHUNK bytes of shared memory, in
@@ -393,6 +402,11 @@ constexpr int kForwardChunk = 16;           // columns of results on their way
 template <int DP> constexpr int kForwardSmem = (1 + kForwardStages<DP>) * kTile * DP * 2 + 8 * 64 * kForwardChunk + 1024;
 
 // STARVED: for the self-test of the bounded waits only; nothing is copied, so that the first wait for operands runs out.
+struct ForwardPlace {                       // steps = -1: there are no more tiles
+    int w, m, h, r0, steps;
+    Reach all;
+    KeyWalk walk;
+};
 template <typename T, int DP, bool STARVED = false>
 __global__ void __launch_bounds__(kForwardThreads, 2)
 attention_forward_kernel(const __grid_constant__ TileArgs t)
@@ -400,7 +414,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     constexpr unsigned long long kLimit = STARVED ? kAttentionStarvedNs : kAttentionWaitNs;
     constexpr int kStages = kForwardStages<DP>, kBytes = kTile * DP * 2, kHalves = DP / 64;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStages + 14];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 14 + 2 * kPlaces];
+    __shared__ __align__(8) unsigned char place_bytes[kPlaces * sizeof(ForwardPlace)];
     __shared__ unsigned tmem_slot;
     __shared__ int gave_up;
     __shared__ float most_of[2][2][kTile], total_of[2][kTile];             // a row's largest score in each half, of two steps in turn; its sums
@@ -408,6 +423,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
     const unsigned own = (smem_address(raw) + 1023u) & ~1023u, ring = own + kBytes, out = ring + kStages * kBytes;
     const unsigned full = smem_address(bars), empty = full + 8 * kStages, loaded = empty + 8 * kStages, used = loaded + 8, scored = used + 8,
                    weighted = scored + 8, summed = weighted + 8, drain = summed + 8, maxed = drain + 8, totaled = maxed + 32;
+    const PlaceRing<ForwardPlace> places{reinterpret_cast<ForwardPlace*>(place_bytes), totaled + 32, totaled + 32 + 8 * kPlaces};
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -419,6 +435,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
         barrier_init(summed, 1);                              // O of a tile is there
         barrier_init(drain, 1);
         for (int s = 0; s < 4; ++s) { barrier_init(maxed + 8 * s, 2); barrier_init(totaled + 8 * s, 2); }        // between the two warps of 32 rows
+        for (int s = 0; s < kPlaces; ++s) { barrier_init(places.there + 8 * s, 1); barrier_init(places.free + 8 * s, 9); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8 && lane < 3 * t.workers) prefetch_map(&t.map[lane % 3][lane / 3]);
@@ -431,32 +448,45 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 
     const AttentionArgs& a = t.a;
     const int tiles = (a.rows + kTile - 1) / kTile, units = tiles * static_cast<int>(t.per.by);
-    // A tile and its walk, the same for all warps; steps = -1: there are no more tiles.
-    struct Place { int w, m, h, r0, steps; Reach all; KeyWalk walk; };
-    const auto next_place = [&](int& round) {
-        for (; round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
-            const int r0 = (tiles - 1 - turn) * kTile;        // the last rows, which see most, first
-            const Reach all = reach_of(a, m, r0, lane, QueryRows{a});
-            const KeyWalk walk(all, a.sinks, kTile);
-            const int steps = STARVED ? 1 : walk.steps;
-            if (steps == 0) continue;
-            ++round;
-            return Place{w, m, in - w * a.heads, r0, steps, all, walk};
-        }
-        return Place{0, 0, 0, 0, -1, Reach{}, KeyWalk(Reach{}, 0, kTile)};
-    };
-    int round = 0;
     int fills = 0, loads = 0;                                 // of the copying thread
+    bool ok = true;
+    const auto await = [&](unsigned bar, int phase) {         // by a whole warp
+        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
+        return ok;
+    };
+    const auto place_there = [&](int tile) { return await(places.there + 8 * (tile % kPlaces), tile / kPlaces) && places[tile].steps >= 0; };
+    const auto place_done = [&](int tile) {
+        __syncwarp();
+        if (lane == 0) arrive_here(places.free + 8 * (tile % kPlaces));
+    };
 
-    if (!STARVED && warp == 8) {
-        bool ok = true;
-        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
-            const KeyWalk& walk = at.walk;
-            const int kv = a.group_size.quotient(at.h);
+    if (warp == 8) {
+        int round = 0, placed = 0;
+        const auto place_next = [&] {                         // works the next tile out and hands it on; without steps it is none
+            ForwardPlace p{0, 0, 0, 0, -1, Reach{}, KeyWalk(Reach{}, 0, kTile)};
+            for (; p.steps <= 0 && round * static_cast<int>(gridDim.x) < units; ++round) {
+                const int unit = tile_of_round(round);
+                if (unit >= units) continue;
+                const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
+                const int r0 = (tiles - 1 - turn) * kTile;    // the last rows, which see most, first
+                const Reach all = reach_of(a, m, r0, lane, QueryRows{a});
+                const KeyWalk walk(all, a.sinks, kTile);
+                p = ForwardPlace{w, m, in - w * a.heads, r0, STARVED ? 1 : walk.steps, all, walk};
+            }
+            if (p.steps == 0) p.steps = -1;
+            if (placed >= kPlaces && !await(places.free + 8 * (placed % kPlaces), placed / kPlaces - 1)) return p;
             if (lane == 0) {
+                places.slots[placed % kPlaces] = p;
+                arrive_here(places.there + 8 * (placed % kPlaces));
+            }
+            ++placed;
+            return p;
+        };
+        ForwardPlace at = place_next();
+        while (ok && at.steps > 0) {
+            const ForwardPlace next = place_next();
+            const int kv = a.group_size.quotient(at.h);
+            if (!STARVED && ok && lane == 0) {
                 ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
                 if (ok) {
                     barrier_expect(loaded, kBytes);
@@ -464,8 +494,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                     for (int i = 0; i < 2 * kHalves; ++i) copy_box(own + i * kBoxBytes, &t.map[0][at.w], i / 2 * 64, at.h, at.r0 + i % 2 * kBox, loaded);
                     ++loads;
                 }
-                for (int i = 0; i < 2 * walk.steps && ok; ++i) {             // k, v, k, v, ...
-                    const int s = fills % kStages, j = walk.row(i / 2, kTile);
+                for (int i = 0; i < 2 * at.steps && ok; ++i) {               // k, v, k, v, ...
+                    const int s = fills % kStages, j = at.walk.row(i / 2, kTile);
                     ok = fills < kStages || tile_wait<kLimit>(empty + 8 * s, (fills / kStages - 1) & 1, &gave_up);
                     if (!ok) break;
                     barrier_expect(full + 8 * s, kBytes);
@@ -476,21 +506,19 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 }
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
+            at = next;
         }
     } else if (warp == 9) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kTile >> 3) << 17, kValues = kTypes | 1u << 16 | (DP >> 3) << 17;
-        bool ok = true;
-        const auto await = [&](unsigned bar, int phase) {
-            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
-            order_after();
-            return ok;
-        };
-        int n = 0, tile = 0;                                  // steps and tiles so far
-        for (int steps = next_place(round).steps; ok && steps >= 0; steps = next_place(round).steps) {
+        int n = 0;                                            // steps so far
+        for (int tile = 0; place_there(tile); ++tile) {
+            const int steps = places[tile].steps;
+            place_done(tile);
             const auto scores = [&](int i) {
                 const int f = 2 * (n + i), s = f % kStages;
                 if (i >= steps || !await(full + 8 * s, f / kStages)) return;
+                order_after();
                 const unsigned long long dq = matrix_descriptor(own, 16), dk = matrix_descriptor(ring + s * kBytes, 16);
                 if (one_lane()) {
 #pragma unroll
@@ -509,6 +537,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             for (int i = 0; i < steps && ok; ++i) {
                 const int f = 2 * (n + i) + 1, s = f % kStages;
                 if (!await(full + 8 * s, f / kStages) || !await(weighted, n + i)) break;
+                order_after();
                 const unsigned long long dv = matrix_descriptor(ring + s * kBytes, 2 * kBoxBytes);
                 if (one_lane()) {
 #pragma unroll
@@ -519,8 +548,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 __syncwarp();
                 scores(i + 1);
             }
+            if (!ok) break;
             n += steps;
-            ++tile;
         }
         if (!ok) {
             if (one_lane()) mma_done(drain);
@@ -532,22 +561,13 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
         const unsigned lanes = static_cast<unsigned>(quarter * 32) << 16, s_at = tmem_s + lanes + half * 64, o_at = tmem_o + lanes + half * (DP / 2);
         unsigned char* const stage = raw + (out - smem_address(raw)) + warp * 64 * kForwardChunk;
         const float c = a.scale * kLog2e;
-        bool ok = true;
-        const auto await = [&](unsigned bar, int phase) {
-            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
-            return ok;
-        };
-        int n = 0, tile = 0;
-        Place next = next_place(round);
-        Keys next_keys{};
-        bool next_valid = next.steps >= 0 && own_keys(a, next.m, next.r0 + line, QueryRows{a}, next_keys);
-        while (ok && next.steps >= 0) {
-            const Place at = next;
-            const Reach& all = at.all;
-            const KeyWalk& walk = at.walk;
-            const Keys keys = next_keys;
-            const bool valid = next_valid;
+        int n = 0;
+        for (int tile = 0; place_there(tile); ++tile) {
+            const ForwardPlace& at = places[tile];
+            const KeyWalk walk = at.walk;
             const int steps = at.steps;
+            Keys keys{};
+            const bool valid = own_keys(a, at.m, at.r0 + line, QueryRows{a}, keys);
             float top = -INFINITY, total = 0.0f;
             for (int i = 0; i < steps; ++i, ++n) {
                 if (!await(scored, n)) break;
@@ -557,8 +577,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 tensor_load(s_at + 32, s[1]);
                 tensor_wait(s[0]);
                 tensor_wait(s[1]);
-                const int j = walk.row(i, kTile), limit = i < walk.sink_steps ? all.min_lo : 0x7fffffff;
-                if (i < walk.sink_steps || j < all.max_lo || j + kTile - 1 > all.min_hi) {
+                const int j = walk.row(i, kTile), limit = i < walk.sink_steps ? at.all.min_lo : 0x7fffffff;
+                if (i < walk.sink_steps || j < at.all.max_lo || j + kTile - 1 > at.all.min_hi) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         const unsigned seen = seen_keys(keys, j + half * 64 + q * 32, limit);
@@ -623,8 +643,6 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             total_of[half][line] = total;
             __syncwarp();
             if (lane == 0) arrive_here(totaled + 8 * quarter);
-            next = next_place(round);                         // (while the last product runs)
-            next_valid = next.steps >= 0 && own_keys(a, next.m, next.r0 + line, QueryRows{a}, next_keys);
             if (!await(totaled + 8 * quarter, tile) || !await(summed, tile)) break;
             order_after();
             total = total_of[0][line] + total_of[1][line];
@@ -637,7 +655,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             __syncwarp();
             for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
                 attention_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, half * (DP / 2), half * (DP / 2) + DP / 2);
-            ++tile;
+            place_done(tile);
         }
     }
     __syncwarp();
@@ -780,6 +798,11 @@ struct KeyRows {
 // Tensor memory, in columns: KEYS: dv 0, dk 128 (64 with heads of 64), S (then P) 256 (and 128 in turn, with heads of 64), dP (then dS)
 // 384.  Else dq 0, S (then dS) 128 and 256 in turn, dP 384.  A warp's half of an operand stands where its half of the scores stood.
 // Where there are two places for S, a step's scores are there before the step in front is done.
+struct BackwardPlace {                      // steps = -1: there are no more tiles
+    int w, m, h, turn, r0, steps, first, turns;               // KEYS: `turns` steps from row `first` on, for each query head
+    Reach all;
+    KeyWalk walk;
+};
 template <typename T, int DP, bool KEYS>
 __global__ void __launch_bounds__(kBackwardThreads, 1)
 attention_backward_kernel(const __grid_constant__ TileArgs t)
@@ -790,7 +813,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     constexpr int kU = kSlotsU<DP, KEYS>, kW = kSlotsW<DP, KEYS>, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS && DP == 128 ? 1 : 2;
     constexpr unsigned kTmemSum = KEYS ? DP : 0, kTmemScores = kScoreSets == 1 ? 256 : 128, kTmemGrads = 384;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 9];
+    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 9 + 2 * kPlaces];
+    __shared__ __align__(8) unsigned char place_bytes[kPlaces * sizeof(BackwardPlace)];
     __shared__ unsigned tmem_slot;
     __shared__ int gave_up;
 
@@ -800,6 +824,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     const unsigned full_u = smem_address(bars), empty_u = full_u + 8 * kU, full_w = empty_u + 8 * kU, empty_w = full_w + 8 * kW, loaded = empty_w + 8 * kW,
                    used = loaded + 8, scored = used + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8,
                    drain = summed + 8;
+    const PlaceRing<BackwardPlace> places{reinterpret_cast<BackwardPlace*>(place_bytes), drain + 8, drain + 8 + 8 * kPlaces};
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -814,6 +839,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         barrier_init(differed, 8);                            // dS is there
         barrier_init(summed, 1);                              // a tile's sums are there
         barrier_init(drain, 1);
+        for (int s = 0; s < kPlaces; ++s) { barrier_init(places.there + 8 * s, 1); barrier_init(places.free + 8 * s, 9); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8 && lane < 4 * t.workers) prefetch_map(&t.map[lane % 4][lane / 4]);
@@ -834,41 +860,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     const AttentionArgs& a = t.a;
     const bool far = KEYS && t.far;                           // chunks of queries against the first keys of the sequences that they begin in
     const int heads = KEYS ? a.kv_heads : a.heads, tiles = far ? t.chunks : (a.rows + kTile - 1) / kTile, units = tiles * static_cast<int>(t.per.by);
-    // A tile and its walk, the same for all warps; steps = -1: there are no more tiles.  (The longest walks come first, where there is no
-    // window.)
-    struct Place {
-        int w, m, h, turn, r0, steps, first, turns;           // KEYS: `turns` steps from row `first` on, for each query head
-        Reach all;
-        KeyWalk walk;
-    };
-    const auto next_place = [&](int& round) {
-        for (; round * static_cast<int>(gridDim.x) < units; ++round) {
-            const int unit = tile_of_round(round);
-            if (unit >= units) continue;
-            const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
-            int r0 = (KEYS ? turn : tiles - 1 - turn) * kTile;
-            Reach all;
-            if (far) {                                        // all first keys see the whole chunk, where it is far from them
-                const Sequence s = sequence_of(a, m, turn * kChunk);
-                r0 = s.start;
-                all = Reach{turn * kChunk, turn * kChunk, min(turn * kChunk + kChunk, s.end) - 1, 0, s.start};
-                all.max_hi = s.start < s.end && turn * kChunk >= far_from(a, s) ? all.min_hi : -1;
-            } else if (KEYS) {
-                all = reach_of(a, m, r0, lane, KeyRows{a, t.partial != nullptr});
-            } else {
-                all = reach_of(a, m, r0, lane, QueryRows{a});
-            }
-            const KeyWalk walk(all, a.sinks, kStep);
-            // queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes
-            const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
-            const int steps = KEYS ? turns * a.group : walk.steps;
-            if (steps == 0) continue;
-            ++round;
-            return Place{w, m, in - w * heads, turn, r0, steps, first, turns, all, walk};
-        }
-        return Place{0, 0, 0, 0, 0, -1, 0, 0, Reach{}, KeyWalk(Reach{}, 0, kStep)};
-    };
-    const auto own_row = [&](const Place& at, int row, Keys& keys) {
+    const auto own_row = [&](const BackwardPlace& at, int row, Keys& keys) {
         if (far) {
             const Sequence s = sequence_of(a, at.m, at.turn * kChunk);
             keys = Keys{at.all.min_lo, at.all.max_hi, s.start, 0};
@@ -876,18 +868,62 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         }
         return KEYS ? own_keys(a, at.m, row, KeyRows{a, t.partial != nullptr}, keys) : own_keys(a, at.m, row, QueryRows{a}, keys);
     };
-    int round = 0;
     int fills_u = 0, fills_w = 0, loads = 0;                  // of the copying thread
+    bool ok = true;
+    const auto await = [&](unsigned bar, int phase) {         // by a whole warp
+        ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
+        return ok;
+    };
+    const auto place_there = [&](int tile) { return await(places.there + 8 * (tile % kPlaces), tile / kPlaces) && places[tile].steps >= 0; };
+    const auto place_done = [&](int tile) {
+        __syncwarp();
+        if (lane == 0) arrive_here(places.free + 8 * (tile % kPlaces));
+    };
 
     if (warp == 8) {
         const auto copy_tile = [&](unsigned to, const CUtensorMap* map, int head, int r, unsigned bar) {
 #pragma unroll
             for (int i = 0; i < 2 * kHalves; ++i) copy_box(to + i * kBoxBytes, map, i / 2 * 64, head, r + i % 2 * kBox, bar);
         };
-        bool ok = true;
-        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
-            const int kv = KEYS ? at.h : a.group_size.quotient(at.h);
+        int round = 0, placed = 0;
+        // Works the next tile out and hands it on; without steps it is none.  (The longest walks come first, where there is no window.)
+        const auto place_next = [&] {
+            BackwardPlace p{0, 0, 0, 0, 0, -1, 0, 0, Reach{}, KeyWalk(Reach{}, 0, kStep)};
+            for (; p.steps <= 0 && round * static_cast<int>(gridDim.x) < units; ++round) {
+                const int unit = tile_of_round(round);
+                if (unit >= units) continue;
+                const int turn = t.per.quotient(unit), in = unit - turn * static_cast<int>(t.per.by), w = t.per_worker.quotient(in), m = t.first_worker + w;
+                int r0 = (KEYS ? turn : tiles - 1 - turn) * kTile;
+                Reach all;
+                if (far) {                                    // all first keys see the whole chunk, where it is far from them
+                    const Sequence s = sequence_of(a, m, turn * kChunk);
+                    r0 = s.start;
+                    all = Reach{turn * kChunk, turn * kChunk, min(turn * kChunk + kChunk, s.end) - 1, 0, s.start};
+                    all.max_hi = s.start < s.end && turn * kChunk >= far_from(a, s) ? all.min_hi : -1;
+                } else if (KEYS) {
+                    all = reach_of(a, m, r0, lane, KeyRows{a, t.partial != nullptr});
+                } else {
+                    all = reach_of(a, m, r0, lane, QueryRows{a});
+                }
+                const KeyWalk walk(all, a.sinks, kStep);
+                // queries are walked from a multiple of 64 rows on, where the rows of lse and delta start on 256 bytes
+                const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
+                p = BackwardPlace{w, m, in - w * heads, turn, r0, KEYS ? turns * a.group : walk.steps, first, turns, all, walk};
+            }
+            if (p.steps == 0) p.steps = -1;
+            if (placed >= kPlaces && !await(places.free + 8 * (placed % kPlaces), placed / kPlaces - 1)) return p;
             if (lane == 0) {
+                places.slots[placed % kPlaces] = p;
+                arrive_here(places.there + 8 * (placed % kPlaces));
+            }
+            ++placed;
+            return p;
+        };
+        BackwardPlace at = place_next();
+        while (ok && at.steps > 0) {
+            const BackwardPlace next = place_next();
+            const int kv = KEYS ? at.h : a.group_size.quotient(at.h);
+            if (ok && lane == 0) {
                 ok = loads == 0 || tile_wait<kLimit>(used, (loads - 1) & 1, &gave_up);
                 if (ok) {
                     barrier_expect(loaded, 2 * kBytes);
@@ -916,15 +952,15 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 }
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
+            at = next;
         }
     } else if (warp == 9) {
         constexpr unsigned kTypes = 1u << 4 | TypeCode<T>::value << 7 | TypeCode<T>::value << 10 | (kTile >> 4) << 24;
         constexpr unsigned kScores = kTypes | (kStep >> 3) << 17, kSums = kTypes | 1u << 16 | (DP >> 3) << 17;
-        bool ok = true;
-        const auto await = [&](unsigned bar, int phase) {
-            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
+        const auto await_product = [&](unsigned bar, int phase) {
+            const bool there = await(bar, phase);
             order_after();
-            return ok;
+            return there;
         };
         // The scores of a step: both operands in shared memory, the sum along the head's elements.
         const auto scores = [&](unsigned to, unsigned tile_at, unsigned slot) {
@@ -941,13 +977,14 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
             for (int k = 0; k < kStep / 16; ++k) mma_tensor(to, from + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), kSums, more || k > 0);
         };
-        int n = 0, tile = 0;                                  // steps and tiles so far
-        for (int steps = next_place(round).steps; ok && steps >= 0; steps = next_place(round).steps) {
-            const int end = n + steps;
+        int n = 0;                                            // steps so far
+        for (int tile = 0; place_there(tile); ++tile) {
+            const int steps = places[tile].steps, end = n + steps;
+            place_done(tile);
             // Steps are numbered through all tiles here.  The waits for operands come in front of those for the warps, while earlier
             // products run.
-            const auto wait_u = [&](int i) { if (i < end) await(full_u + 8 * (i % kU), i / kU); };
-            const auto wait_w = [&](int i) { if (i < end) await(full_w + 8 * (i % kW), i / kW); };
+            const auto wait_u = [&](int i) { if (i < end) await_product(full_u + 8 * (i % kU), i / kU); };
+            const auto wait_w = [&](int i) { if (i < end) await_product(full_w + 8 * (i % kW), i / kW); };
             const auto step_s = [&](int i) {
                 if (i >= end || !ok) return;
                 if (one_lane()) {
@@ -966,7 +1003,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 }
                 __syncwarp();
             };
-            await(loaded, tile);
+            await_product(loaded, tile);
             wait_u(n);
             step_s(n);
             if (kScoreSets == 2) {
@@ -978,7 +1015,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             for (int i = n; i < end && ok; ++i) {
                 if (KEYS) {
                     if (kScoreSets == 1) wait_u(i + 1);
-                    if (!await(weighted, i)) break;
+                    if (!await_product(weighted, i)) break;
                     if (one_lane()) {
                         add(tmem, tmem + kTmemScores + i % kScoreSets * 128, ring_w + i % kW * kBytes, i > n);
                         mma_done(empty_w + 8 * (i % kW));
@@ -987,7 +1024,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     if (kScoreSets == 2) wait_u(i + 2);
                     step_s(i + kScoreSets);
                     wait_w(i + 1);
-                    if (!await(differed, i)) break;
+                    if (!await_product(differed, i)) break;
                     if (one_lane()) {
                         add(tmem + kTmemSum, tmem + kTmemGrads, ring_u + i % kU * kBytes, i > n);
                         mma_done(empty_u + 8 * (i % kU));
@@ -997,7 +1034,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     step_p(i + 1);
                 } else {
                     wait_w(i + 1);
-                    if (!await(differed, i)) break;
+                    if (!await_product(differed, i)) break;
                     if (one_lane()) {
                         add(tmem + kTmemSum, tmem + kTmemScores + i % 2 * 128, ring_u + i % kU * kBytes, i > n);
                         mma_done(empty_u + 8 * (i % kU));
@@ -1009,8 +1046,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     step_s(i + 2);
                 }
             }
+            if (!ok) break;
             n = end;
-            ++tile;
         }
         if (!ok) {
             if (one_lane()) mma_done(drain);
@@ -1022,14 +1059,11 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         const unsigned lanes = static_cast<unsigned>(quarter * 32) << 16;
         unsigned char* const stage = raw + (out - smem_address(raw)) + warp * 64 * kBackwardChunk;
         const float c = a.scale * kLog2e;
-        bool ok = true;
-        const auto await = [&](unsigned bar, int phase) {
-            ok = ok && __all_sync(0xffffffffu, tile_wait<kLimit>(bar, phase & 1, &gave_up));
-            order_after();
-            return ok;
-        };
-        int n = 0, tile = 0;
-        for (Place at = next_place(round); ok && at.steps >= 0; at = next_place(round)) {
+        int n = 0;
+        for (int tile = 0; place_there(tile); ++tile) {
+            const BackwardPlace& at = places[tile];
+            const KeyWalk walk = at.walk;
+            const int first = at.first, turns = at.turns, steps = at.steps;
             const int row = at.r0 + quarter * 32 + lane;
             Keys keys{};
             const bool valid = own_row(at, row, keys);
@@ -1041,14 +1075,15 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 lse = __ldcg(t.lse + from) + static_cast<float>(exponent);  // P with dS's power of two
                 delta = __ldcg(t.delta + from);
             }
-            for (int i = 0, turn = 0; i < at.steps; ++i, ++n, ++turn) {
-                if (KEYS && turn == at.turns) turn = 0;
+            for (int i = 0, turn = 0; i < steps; ++i, ++n, ++turn) {
+                if (KEYS && turn == turns) turn = 0;
                 const unsigned s_at = tmem + kTmemScores + n % kScoreSets * 128 + half * 64 + lanes, g_at = tmem + kTmemGrads + half * 64 + lanes;
-                const int r = KEYS ? at.first + turn * kStep : at.walk.row(i, kStep), limit = !KEYS && i < at.walk.sink_steps ? at.all.min_lo : 0x7fffffff;
-                const bool masked = (!KEYS && i < at.walk.sink_steps) || r < at.all.max_lo || r + kStep - 1 > at.all.min_hi;
+                const int r = KEYS ? first + turn * kStep : walk.row(i, kStep), limit = !KEYS && i < walk.sink_steps ? at.all.min_lo : 0x7fffffff;
+                const bool masked = (!KEYS && i < walk.sink_steps) || r < at.all.max_lo || r + kStep - 1 > at.all.min_hi;
                 const float* column = stats_at + n % kU * 2 * kStep + half * 64;
                 if (!await(scored + 8 * (n % kScoreSets), n / kScoreSets)) break;
                 if (KEYS && !await(full_u + 8 * (n % kU), n / kU)) break;      // (long past: for the sight of lse and delta)
+                order_after();
                 Two p[2][16];
                 unsigned seen[2] = {~0u, ~0u};
                 ulonglong2 columns = {0, 0};                  // what four neighbouring columns' queries share
@@ -1091,6 +1126,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     if (lane == 0) arrive_here(weighted);
                 }
                 if (!await(graded, n)) break;
+                order_after();
                 {
                     unsigned g[2][32];
                     tensor_load(g_at, g[0]);
@@ -1125,6 +1161,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 if (lane == 0) arrive_here(differed);
             }
             if (!await(summed, tile)) break;
+            order_after();
             const float of_grad = a.scale * (kHalf ? exp2f(static_cast<float>(-exponent)) : 1.0f);
             const unsigned rows_valid = __ballot_sync(0xffffffffu, valid);
             const auto nothing = [](float (&)[32], int) {};
@@ -1172,7 +1209,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     attention_query_grad_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, d, d + DP / 2);
             }
             order_before();
-            ++tile;
+            place_done(tile);
         }
     }
     __syncwarp();

@@ -133,11 +133,13 @@ def test_two_micro_batches_and_the_averaging_step():
 
 
 def test_the_chain_captured_and_replayed_beside_another():
-    """Two captured passes, each with scratch of its own, replayed on two streams at once: the same bits as eager ones."""
+    """Two captured passes, each with scratch of its own, replayed on two streams at once: the same bits as eager ones.  (Each is
+    captured on a stream of its own, as the library products' scratch belongs to the stream.)"""
     import paper_2403_04206_b200 as grawa
     flat, passes = inputs(2)
     p = views(flat)
     results, graphs, want = [], [], []
+    streams = [torch.cuda.Stream() for _ in passes]
     for i, one in enumerate(passes):
         grads = [torch.zeros(int(OFFSETS[-1]), dtype=torch.bfloat16, device="cuda") for _ in range(M)]
         g = views(grads)
@@ -146,14 +148,13 @@ def test_the_chain_captured_and_replayed_beside_another():
         want.append([t.clone() for t in results[-1]])
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
+        with torch.cuda.graph(graph, stream=streams[i]):
             one.run(grawa, p, g, i, True)
         graphs.append(graph)
     for t in results[0] + results[1]:
         t.zero_()
     torch.cuda.synchronize()
-    streams = [torch.cuda.Stream() for _ in graphs]
-    for _ in range(3):
+    for _ in range(20):
         for graph, stream in zip(graphs, streams):
             with torch.cuda.stream(stream):
                 graph.replay()
