@@ -653,7 +653,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
             if (half == 0 && valid && a.to[1].p[at.m])
                 static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (top + log2f(total)) * kLn2;
             __syncwarp();
-            for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine); todo; todo &= todo - 1)
+            // (a sum of weights that is NaN comes of a score that the row sees: the row is NaN)
+            for (unsigned todo = __ballot_sync(0xffffffffu, valid && !fine && !isnan(total)); todo; todo &= todo - 1)
                 attention_row<T>(a, at.m, at.h, at.r0 + quarter * 32 + __ffs(todo) - 1, half * (DP / 2), half * (DP / 2) + DP / 2);
             place_done(tile);
         }

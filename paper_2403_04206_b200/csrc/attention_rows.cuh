@@ -121,12 +121,17 @@ __device__ __forceinline__ bool any_nan(const float (&x)[4])
 }
 __device__ __forceinline__ void fill_row(float (&x)[4], float v) { x[0] = x[1] = x[2] = x[3] = v; }
 
-// Calls f for the rows [begin, end), kRowsAtOnce at a time (the last ones may lie behind the end), so that what they wait for overlaps.
+// Calls f for the rows [begin, end), kRowsAtOnce at a time (the last ones may lie behind the end), so that what they wait for overlaps; until
+// all of the sums that it makes are NaN, which they stay.
 constexpr int kRowsAtOnce = 4;
 template <typename F>
-__device__ __forceinline__ void for_rows(int begin, int end, const F& f)
+__device__ __forceinline__ void for_rows(int begin, int end, int dim, const float (&sum)[4], const F& f)
 {
-    for (int j = begin; j < end; j += kRowsAtOnce) f(j);
+    const bool none = threadIdx.x % 32 * 4 >= static_cast<unsigned>(dim);
+    for (int j = begin; j < end; j += kRowsAtOnce) {
+        f(j);
+        if (__all_sync(0xffffffffu, none || (isnan(sum[0]) && isnan(sum[1]) && isnan(sum[2]) && isnan(sum[3])))) return;
+    }
 }
 
 // Elements [from, to) of out_i, and with the first of them lse_i.  (Where q_i holds NaN, all of it is.)
@@ -142,7 +147,7 @@ __device__ __noinline__ void attention_row(const AttentionArgs& a, int m, int h,
     } else {
         for (int part = 0; part < 2; ++part) {
             const int end = part ? keys.hi + 1 : keys.sinks_end;
-            for_rows(part ? keys.lo : keys.start, end, [&](int j) {
+            for_rows(part ? keys.lo : keys.start, end, a.dim, o, [&](int j) {
                 float k[kRowsAtOnce][4], v[kRowsAtOnce][4], s[kRowsAtOnce], next = top;
 #pragma unroll
                 for (int r = 0; r < kRowsAtOnce; ++r) {
@@ -202,7 +207,7 @@ __device__ __noinline__ void attention_query_grad_row(const AttentionArgs& a, in
     } else {
         for (int part = 0; part < 2; ++part) {
             const int end = part ? keys.hi + 1 : keys.sinks_end;
-            for_rows(part ? keys.lo : keys.start, end, [&](int j) {
+            for_rows(part ? keys.lo : keys.start, end, a.dim, dq, [&](int j) {
                 float k[kRowsAtOnce][4], v[kRowsAtOnce][4];
 #pragma unroll
                 for (int r = 0; r < kRowsAtOnce; ++r) {
@@ -235,7 +240,7 @@ __device__ __noinline__ void attention_key_grad_row(const AttentionArgs& a, int 
         fill_row(sum, NAN);
     } else {
         for (int h = kv * a.group; h < (kv + 1) * a.group; ++h)
-            for_rows(queries.lo, queries.hi + 1, [&](int i) {
+            for_rows(queries.lo, queries.hi + 1, a.dim, sum, [&](int i) {
                 float q[kRowsAtOnce][4], dout[kRowsAtOnce][4];
 #pragma unroll
                 for (int r = 0; r < kRowsAtOnce; ++r) {
