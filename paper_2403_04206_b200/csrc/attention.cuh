@@ -848,14 +848,10 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     order_before();
     __syncthreads();
     order_after();
-    // The launch in front has waited for all before it, so that a launch that needs nothing of it may run beside it, and waits at its end.
-    // (The fence keeps reads from what its SM may hold of older results.)
-    if (t.beside) {
-        let_next_start();
-        __threadfence();
-    } else {
-        stream_order();
-    }
+    // The launch in front has waited for all before it, so that a launch that needs nothing of it may run beside it, and waits at its
+    // end, before it lets the next one start.  (The fence keeps reads from what the SM may hold of older results.)
+    if (t.beside) __threadfence();
+    else stream_order();
     const unsigned tmem = tmem_slot;
 
     const AttentionArgs& a = t.a;
@@ -1223,7 +1219,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         for (int f = max(0, fills_w - kW); f < fills_w; ++f) tile_wait<kLimit>(full_w + 8 * (f % kW), (f / kW) & 1, nullptr);
     }
     if (warp == 9) tensor_free<512>(tmem);
-    if (t.beside) wait_for_previous();
+    if (t.beside) stream_order();
 }
 
 }  // namespace replica
