@@ -71,7 +71,7 @@ typedef enum grawa_status {
     GRAWA_ERR_CUDA = -2,        /* a CUDA runtime call failed; text in grawa_last_cuda_error()    */
     GRAWA_ERR_NONFINITE = -3,   /* a gradient score was NaN/Inf (fallback weights were applied)   */
     GRAWA_ERR_WORKSPACE = -4,   /* caller-supplied workspace missing, misaligned or too small     */
-    GRAWA_ERR_TIMEOUT = -5,     /* a bounded device-side wait ran out (bulk-copy variant, product) */
+    GRAWA_ERR_TIMEOUT = -5,     /* a bounded device-side wait ran out (bulk copies, product, attention) */
     GRAWA_ERR_TOO_LARGE = -6    /* problem larger than the built-in scratch of grawa_sumsq_static */
 } grawa_status;
 
@@ -433,7 +433,7 @@ size_t grawa_head_rotary_backward_workspace_bytes(int64_t rows, int M);
  * (Offsets that decrease or leave [0, rows] give some runs of rows instead; nothing outside the buffers is touched.)
  * NULL: sequences of `period` (>= 1) rows, the last one what is left; `period` is not used otherwise.
  * left, right, sinks >= 0; scale > 0.  rows = 0 is a no-op.
- * Sums and statistics are fp32; exp(S - m), with m within 2^8 of the largest so far, is rounded to `dtype` for the product with v.
+ * Sums and statistics are fp32; the weights exp(S - m), at most 2^8, are rounded to `dtype` for the product with v.
  * A row's result depends on no key or value that it does not see, whatever those hold, infinities and NaN included. */
 grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void *const *q, const void *const *k, const void *const *v,
                                             void *const *out, float *const *lse, const int64_t *const *offsets,

@@ -146,14 +146,6 @@ __device__ __forceinline__ void tensor_wait(unsigned (&r)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : GRAWA_RW8(r, 0), GRAWA_RW8(r, 8) : : "memory");
 }
-__device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
-        "%23, %24, %25, %26, %27, %28, %29, %30, %31};" ::GRAWA_W8(r, 0),
-        GRAWA_W8(r, 8), GRAWA_W8(r, 16), GRAWA_W8(r, 24), "r"(at)
-        : "memory");
-}
 __device__ __forceinline__ void tensor_store(unsigned at, const unsigned (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::GRAWA_W8(r, 0), GRAWA_W8(r, 8),
