@@ -196,16 +196,19 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 // Two powers of two without the special function unit, which makes 16 a cycle and SM: x = n + f with n = floor x (Cody and Waite's
-// reduction), 2^f = 1 + f (c1 + ... + c5 f^4) with coefficients fitted for this file on [0, 1) by least squares whose weights
-// were moved until the relative errors were level (8e-8; 1.5e-7 with the roundings), and n added to the exponent.  Below -127 it is 0.
-// NaN gives a number past 3e38, as its bits lie.
+// reduction; the clamped reduction by an addition rounded down, and the sharing of the exponentials between the two units, are published
+// for softmax on this architecture), 2^f = 1 + f (c1 + ... + c5 f^4) with coefficients fitted for this file on [0, 1) by least squares whose
+// weights were moved until the relative errors were level (8e-8; 1.7e-7 at most with the roundings), times 2^n.  As of the unit, results below
+// 2^-126 are zero, those from 2^128 on infinity, and those of NaN NaN.
 __device__ __forceinline__ void exp2_two(Two x, float& a, float& b)
 {
-    constexpr float kShift = 12582912.0f;                     // 1.5 * 2^23: the sum's last bits are the integer
+    constexpr float kShift = 12583039.0f;                     // 1.5 * 2^23 + 127: the sum's last bits are n + 127, the exponent field of 2^n
     float u, v;
     apart(x, u, v);
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-127.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-127.0f));  // (field 0: zero)
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-127.0f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(128.0f));   // (field 255: infinity)
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(128.0f));
     x = two(u, v);
     Two n, f, p;
     asm("add.rm.f32x2 %0, %1, %2;" : "=l"(n.v) : "l"(x.v), "l"(two(kShift, kShift).v));
@@ -217,9 +220,8 @@ __device__ __forceinline__ void exp2_two(Two x, float& a, float& b)
     p = fma_two(f, p, two(1.0f, 1.0f));
     float s, t;
     apart(n, s, t);
-    apart(p, u, v);
-    a = __uint_as_float(__float_as_uint(u) + (__float_as_uint(s) << 23));
-    b = __uint_as_float(__float_as_uint(v) + (__float_as_uint(t) << 23));
+    p = mul_two(p, two(__uint_as_float(__float_as_uint(s) << 23), __uint_as_float(__float_as_uint(t) << 23)));
+    apart(p, a, b);
 }
 // Powers of two of pair `pair` of a run of them: some pairs go by the polynomial, so that the units work side by side.
 template <int EVERY>

@@ -1,0 +1,47 @@
+"""Attention within a window at the ends of the exponentials' range."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def one_row(kind, scores, values, dim=64):
+    """The result of one query (the last row; all rows hold it) whose scores against the keys are `scores` exactly."""
+    import paper_2403_04206_b200 as grawa
+    n = len(scores)
+    q, k, v = (torch.zeros(n, 1, dim, dtype=kind, device="cuda") for _ in range(3))
+    q[..., 0] = 1.0
+    k[:, 0, 0] = torch.as_tensor(scores, dtype=torch.float64).cuda().to(kind)
+    v[:, 0, 0] = torch.as_tensor(values, dtype=torch.float64).cuda().to(kind)
+    out, lse = torch.full_like(q, 5.0), torch.full((1, n), 5.0, device="cuda")
+    grawa.grawa_window_attention_forward([q], [k], [v], [out], lse=[lse], right=None, scale=1.0)
+    return out[:, 0, 0], lse[0]
+
+
+def test_weights_below_the_smallest_normal_number_are_zero_wherever_they_stand():
+    """Weights of 2^-126.2 (-87.5 log2 e) are zero for every key, by both ways to an exponential; those of 2^-125.5 (-87) are there."""
+    n = 200
+    for place in range(n):
+        scores, values = [-200.0] * n, [0.0] * n
+        top = (place + 100) % n
+        scores[top], scores[place], values[place] = 0.0, -87.5, 2.0 ** 127
+        out, lse = one_row(torch.bfloat16, scores, values)
+        assert (out == 0).all() and (lse == 0).all(), place
+        scores[place] = -87.0
+        out, _ = one_row(torch.bfloat16, scores, values)
+        # the bfloat16 weight and the bfloat16 result are each rounded once, the argument 125.5 carries 2 roundings of 2^-24
+        assert (out.double() / (2.0 ** 127 * math.exp(-87.0)) - 1).abs().max() < 2.0 ** -7, place
+
+
+def test_scores_whose_rounding_is_past_the_exponentials_range():
+    """Scores of 2^34, at every place of a step: a product with log2 e is off by up to 2^10 there, but the largest score's row still is
+    that of its value, and lse that score."""
+    n = 128
+    for place, turn in [(place, (37 * place + 5 * turn) % 128) for place in range(n) for turn in range(5)]:
+        scores, values = [float(-j) for j in range(n)], [float(j) for j in range(n)]
+        scores[place] = 2.0 ** 34 * (1.0 + turn / 128.0)
+        out, lse = one_row(torch.bfloat16, scores, values)
+        assert (out == values[place]).all(), (place, turn)
+        assert (lse.double() / scores[place] - 1).abs().max() < 2.0 ** -21, (place, turn, lse[0])
