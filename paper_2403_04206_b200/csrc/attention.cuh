@@ -719,7 +719,10 @@ attention_stats_kernel(const __grid_constant__ StatsArgs t)
             square = fmaf(p[e], p[e], square);
         }
         if (!values) dot = lanes_sum<LANES>(dot);
-        if (t.longest) longest = fmaxf(longest, lanes_sum<LANES>(square));   // (NaN does not count: such rows are done again)
+        if (t.longest) {                                      // rows that are not finite do not count: they are done again
+            square = lanes_sum<LANES>(square);
+            if (square < INFINITY) longest = fmaxf(longest, square);
+        }
         if (!values && word == 0) deltas[group + kAtOnce * i] = -dot;
     }
     if (t.longest) {
@@ -737,7 +740,7 @@ attention_stats_kernel(const __grid_constant__ StatsArgs t)
     if (t.longest && threadIdx.x == 0) atomicMax(t.longest + 2 * m + (values ? 1 : 0), most);
 }
 
-// The power of two that half precision's dS carries: with it the bound of |dS|, twice the product of the longest rows
+// The power of two that half precision's dS carries: with it the bound of |dS|, twice the product of the longest finite rows
 // of dout and v, lies in [2^14, 2^15).
 __device__ __forceinline__ int grad_exponent(const TileArgs& t, int m)
 {
