@@ -433,8 +433,8 @@ size_t grawa_head_rotary_backward_workspace_bytes(int64_t rows, int M);
  * (Offsets that decrease or leave [0, rows] give some runs of rows instead; nothing outside the buffers is touched.)
  * NULL: sequences of `period` (>= 1) rows, the last one what is left; `period` is not used otherwise.
  * left, right, sinks >= 0; scale > 0.  rows = 0 is a no-op.
- * Sums and statistics are fp32; the weights exp(S - m), at most 2^8, are rounded to `dtype` for the product with v
- * (and are zero below 2^-126).
+ * Sums and statistics are fp32; the weights exp(S - m), at most 2^8 (with GRAWA_F16 times 2^6), are rounded to `dtype` for the
+ * product with v (and are zero below 2^-126).
  * A row's result depends on no key or value that it does not see, whatever those hold, infinities and NaN included.  (Where rows
  * that belong to sequences hold such elements, tiles of 128 rows that walk over them are walked twice: a call with one takes up to
  * 3 times as long, one with some in every row up to 30 times.) */

@@ -9,8 +9,8 @@
 // product's operand, so nothing but tiles of q, k, v and dout passes through shared memory.  A step is 128 rows wide, because products
 // of two operands in shared memory take the tensor cores as long for 64 columns as for 128.
 //
-//   forward    S = Q K^T, P = exp2(S c - m), O += P V.  m is a row's largest score so far, but is only moved when that grows
-//              by more than 2^8 (P stays below 2^8), so that O, which lies in tensor memory, is rarely scaled.
+//   forward    S = Q K^T, P = exp2(S c - m), O += P V.  m is a row's largest score so far (6 less in half precision), but is only moved when
+//              that grows by more than 2^8 (P stays below 2^8, or 2^14), so that O, which lies in tensor memory, is rarely scaled.
 //   dq         S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //   dk, dv     S^T = K Q^T, dP^T = V dO^T, dV += P^T dO, dK += dS^T Q, over all query heads of the key head
 //
@@ -783,7 +783,10 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                     __syncwarp();
                     if (lane == 0) arrive_here(maxed + 8 * quarter);
                     if (!await(maxed + 8 * quarter, n)) break;
-                    const float here = fmaxf(most[0], most_of[n % 2][1 - half][line]) * c;
+                    float here = fmaxf(most[0], most_of[n % 2][1 - half][line]) * c;
+                    // Half precision's smallest numbers are 2^-24: the largest weight is 2^6, and none is above 2^14 before m moves.  (Not where the
+                    // rounding of larger scores could take them past its largest number.)
+                    if (TypeCode<T>::value == 0 && fabsf(here) < 1048576.0f) here -= 6.0f;
                     const bool grows = here > top + 8.0f;         // (from -infinity: always)
                     if (__any_sync(0xffffffffu, grows)) {
                         const float f = grows ? exp2_fast(top - here) : 1.0f;
@@ -857,7 +860,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                                                                });
                 order_before();
                 if (half == 0 && valid && a.to[1].p[at.m])
-                    static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (top + log2f(total / unit)) * kLn2;
+                    static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (TypeCode<T>::value ? top + log2f(total / unit) : (top + 6.0f) + log2f(total / 64.0f)) * kLn2;
                 // (a sum of weights that is NaN comes of a score that the row sees: the row is NaN)
                 if (!careful && __any_sync(0xffffffffu, valid && !fine && !isnan(total)) && lane == 0) mark_tile(marks, &more, tile);
                 place_done(tile);

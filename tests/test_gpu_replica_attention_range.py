@@ -45,3 +45,18 @@ def test_scores_whose_rounding_is_past_the_exponentials_range():
         out, lse = one_row(torch.bfloat16, scores, values)
         assert (out == values[place]).all(), (place, turn)
         assert (lse.double() / scores[place] - 1).abs().max() < 2.0 ** -21, (place, turn, lse[0])
+
+
+def test_small_weights_of_half_precision_keep_their_digits():
+    """One key with all the weight and a value of 0, and many whose weights, 2^-24 to 2^-28, are below half precision's smallest normal
+    number: their sum is the result.  The weights are carried with 2^6, which keeps most of them above 2^-24."""
+    n = 6000
+    for low in (-16.5, -17.5, -19.0):
+        out, lse = one_row(torch.float16, [0.0] + [low] * (n - 1), [0.0] + [100.0] * (n - 1))
+        total = 1.0 + (n - 1) * math.exp(low)
+        # each weight carries 2^6 and is off by at most half of half precision's smallest subnormal, 2^-25; the result by its rounding
+        want = (n - 1) * math.exp(low) * 100.0 / total
+        assert (out.double() / want - 1).abs().max() < 2.0 ** -25 / (math.exp(low) * 2.0 ** 6) + 2.0 ** -11 + 2.0 ** -16, (low, out[-1], want)
+        # 47 steps' additions to the sum, and 16 in the first step beside the large term, of 2^-24 each; the logarithm's terms are below 8 and
+        # each rounded by at most 2^-21
+        assert (lse.double() - math.log(total)).abs().max() < 70 * 2.0 ** -24 + 2 * 2.0 ** -21
