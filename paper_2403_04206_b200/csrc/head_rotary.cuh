@@ -386,7 +386,8 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
                 at.turn(u, v, c, s, -1.0f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));
-                const float r = rsqrtf(fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps));
+                float r = rsqrtf(fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps));
+                if (h >= a.heads[which]) r = 0.0f;            // no head: its zeros are to stay such, also without eps
                 at.from_shared(weights[which], wa, wb);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {                 // x s first: s^2 may be past fp32's range where dx is inside it
