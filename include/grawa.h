@@ -389,7 +389,7 @@ typedef enum grawa_pairing { GRAWA_PAIR_HALVES = 0, GRAWA_PAIR_NEIGHBOURS = 1 } 
  * strides are equal, k_out_m as k_m (a backward pass needs what q and k held before).
  * positions: DEVICE, `rows` int64 a worker; NULL: the row number modulo `period` (>= 1).  frequencies: DEVICE,
  * rotary / 2 fp64 values, for all workers (NULL with rotary = 0).  Angles are taken and reduced in fp64, squares summed
- * in fp32.  eps >= 0.  rows = 0 is a no-op.  Heads, rows and rotated halves of whole 16-byte words at 16-byte
+ * in fp32 (of scaled elements where those of a head leave its range).  eps >= 0.  rows = 0 is a no-op.  Heads, rows and rotated halves of whole 16-byte words at 16-byte
  * boundaries take the vector kernels. */
 grawa_status grawa_head_rotary_forward(grawa_dtype dtype, grawa_pairing pairing, const void *const *q, const void *const *k,
                                        const void *const *q_weight, const void *const *k_weight, void *const *q_out,

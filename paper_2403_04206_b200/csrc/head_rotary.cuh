@@ -42,6 +42,7 @@ struct HeadArgs {
     int parts;                              // backward: CTAs a worker
     int has_w[2], has_dw[2], has_dx[2], accumulate;
     float eps, inv_dim;
+    unsigned small;                         // bits of the mean square below which it is taken again, of scaled elements
 };
 
 template <typename T, int MODE> constexpr int kHeadRun = MODE == kPairAny ? 8 : MODE == kPairAnyShort ? 4 : kWordElems<T>;
@@ -225,6 +226,38 @@ __device__ __forceinline__ void load_weights(const HeadArgs& a, int which, int m
     for (int e = threadIdx.x; e < a.dim; e += kHeadThreads) to[e] = a.has_w[which] ? widen(w[e]) : 1.0f;
 }
 
+// Whether squares of a head's elements are neither past the range of 32 bits nor so small that some are missing and eps does not make up
+// for them.
+__device__ __forceinline__ bool squares_in_range(const HeadArgs& a, float mean)
+{
+    constexpr unsigned kMost = 0x7c000000u;                   // 2^121
+    return __float_as_uint(mean) - a.small <= kMost - a.small;
+}
+// 1 / sqrt(mean x^2 + eps) of a head whose lanes' elements are x and y and whose mean square and eps make `mean`, where that is not so: of
+// elements that are scaled by a power of two, `scale`.  (By the head's lanes alone, which all have the same mean.)
+template <int LPH, int N>
+__device__ __forceinline__ float scaled_norm(const HeadArgs& a, float mean, float (&x)[N], float (&y)[N], float& scale)
+{
+    const unsigned lanes = LPH == 32 ? ~0u : ((1u << LPH % 32) - 1) << (threadIdx.x % 32 / LPH * LPH);
+    const float root = sqrtf(a.eps);
+    float most = root, square = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) most = fmaxf(most, fmaxf(fabsf(x[e]), fabsf(y[e])));
+#pragma unroll
+    for (int d = LPH / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(lanes, most, d));
+    if (!(most > 0.0f && most < INFINITY)) return rsqrtf(mean);
+    scale = exp2f(static_cast<float>(-max(-126, min(126, ilogbf(most)))));
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        x[e] *= scale;
+        y[e] *= scale;
+        square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));
+    }
+#pragma unroll
+    for (int d = LPH / 2; d > 0; d >>= 1) square += __shfl_xor_sync(lanes, square, d);
+    return rsqrtf(fmaf(square, a.inv_dim, (root * scale) * (root * scale)));
+}
+
 // A row's heads in steps of `per` neighbouring ones, those of the queries first.
 struct HeadSteps {
     int q_steps, steps;
@@ -297,14 +330,25 @@ head_rotary_forward_kernel(const __grid_constant__ HeadArgs a)
             fetch(held[i]);
 #pragma unroll
             for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
-            const float r = rsqrtf(fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps));
+            const float mean = fmaf(lanes_sum<LPH>(sum), a.inv_dim, a.eps);
             at.from_shared(weights[which], wa, wb);
+            const auto finish = [&](float r) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                x[e] = x[e] * r * wa[e];
-                y[e] = y[e] * r * wb[e];
+                for (int e = 0; e < N; ++e) {
+                    x[e] = x[e] * r * wa[e];
+                    y[e] = y[e] * r * wb[e];
+                }
+                at.turn(x, y, c, s, 1.0f);
+            };
+            finish(rsqrtf(mean));
+            if (!squares_in_range(a, mean)) {                 // from the start (4 x 8192 rows of 32 + 8 heads of 128 bf16: 134 us with the question in front)
+                typename HeadLane<T, MODE>::Held again;
+                at.fetch(static_cast<const T*>(a.x[which].p[m]) + now.row * a.x_stride[which] + static_cast<long long>(h) * a.dim, h < a.heads[which], again);
+                at.open(again, x, y);
+                float scale;
+                const float r = scaled_norm<LPH>(a, mean, x, y, scale);
+                finish(r);
             }
-            at.turn(x, y, c, s, 1.0f);
             if (h < a.heads[which]) at.store(static_cast<T*>(a.y[which].p[m]) + now.row * a.y_stride[which] + static_cast<long long>(h) * a.dim, x, y);
             now.advance(a, all.steps);
         }
@@ -386,7 +430,9 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
                 at.turn(u, v, c, s, -1.0f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) square = fmaf(x[e], x[e], fmaf(y[e], y[e], square));
-                float r = rsqrtf(fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps));
+                const float mean = fmaf(lanes_sum<LPH>(square), a.inv_dim, a.eps);
+                float scale = 1.0f, r = rsqrtf(mean);
+                if (!squares_in_range(a, mean)) r = scaled_norm<LPH>(a, mean, x, y, scale);
                 if (h >= a.heads[which]) r = 0.0f;            // no head: its zeros are to stay such, also without eps
                 at.from_shared(weights[which], wa, wb);
 #pragma unroll
@@ -404,6 +450,13 @@ head_rotary_backward_kernel(const __grid_constant__ HeadArgs a)
                 for (int e = 0; e < N; ++e) {
                     u[e] = (u[e] - x[e] * along) * r;
                     v[e] = (v[e] - y[e] * along) * r;
+                }
+                if (scale != 1.0f) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        u[e] *= scale;
+                        v[e] *= scale;
+                    }
                 }
                 if (h < a.heads[which] && a.has_dx[which]) at.store(out + static_cast<long long>(h) * a.dim, u, v);
             }

@@ -78,6 +78,7 @@ static HeadArgs head_args(const HeadShape& s, const void* const* q, const void* 
     a.words = static_cast<int>(s.head_dim * type_bytes(s.dtype) / 16);
     a.has_w[0] = q_weight != nullptr; a.has_w[1] = k_weight != nullptr;
     a.eps = s.eps; a.inv_dim = 1.0f / static_cast<float>(s.head_dim);
+    a.small = s.eps < 0x1p-80f ? 0x12800000u : 0u;            // 2^-90: squares that are missing are below 2^-149 each
     return a;
 }
 
