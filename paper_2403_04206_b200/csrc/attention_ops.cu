@@ -185,8 +185,9 @@ grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void* const
 
 size_t grawa_window_attention_backward_workspace_bytes(int64_t rows, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t sinks, int M)
 {
-    if (M < 1 || M > GRAWA_MAX_WORKERS || rows < 0 || rows > 0x7fffffff - 1024 || q_heads < 1 || q_heads > 0x7fff || kv_heads < 1 || kv_heads > q_heads ||
-        head_dim < 8 || head_dim > 128 || sinks < 0) return 0;
+    if (q_heads < 1 || q_heads > 0x7fff || kv_heads < 1 || kv_heads > q_heads || head_dim < 8 || head_dim > 128) return 0;
+    const int64_t wide = q_heads * head_dim, narrow = kv_heads * head_dim;
+    if (!attention_shape_ok({GRAWA_BF16, nullptr, 0, 1, 0, 0, sinks, rows, q_heads, kv_heads, head_dim, wide, narrow, narrow, wide, M, 1.0f})) return 0;
     return attention_scratch(rows, q_heads, kv_heads, head_dim, sinks, M).bytes;
 }
 
