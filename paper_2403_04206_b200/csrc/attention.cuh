@@ -1013,7 +1013,8 @@ struct KeyRows {
 //
 // Tensor memory, in columns: KEYS: dv 0, dk 128 (64 with heads of 64), S (then P) 256 (and 128 in turn, with heads of 64), dP (then dS)
 // 384.  Else dq 0, S (then dS) 128 and 256 in turn, dP 384.  A warp's half of an operand stands where its half of the scores stood.
-// Where there are two places for S, a step's scores are there before the step in front is done.
+// Where there are two places for S, a step's scores are there before the step in front is done: a warp may be through with a step's P while
+// another is still at that of the step in front, so each place has a barrier of its own for P.
 struct BackwardPlace {                      // steps = -1: there are no more tiles
     int w, m, h, turn, r0, steps, first, turns, from, to;     // KEYS: `turns` steps from row `first` on, for each query head
     Reach all;
@@ -1029,7 +1030,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
     constexpr int kU = kSlotsU<DP, KEYS>, kW = kSlotsW<DP, KEYS>, kBytes = kTile * DP * 2, kHalves = DP / 64, kScoreSets = KEYS && DP == 128 ? 1 : 2;
     constexpr unsigned kTmemSum = KEYS ? DP : 0, kTmemScores = kScoreSets == 1 ? 256 : 128, kTmemGrads = 384;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 10 + 2 * kPlaces];
+    __shared__ __align__(8) unsigned long long bars[2 * kU + 2 * kW + 11 + 2 * kPlaces];
     __shared__ __align__(8) unsigned char place_bytes[kPlaces * sizeof(BackwardPlace)];
     __shared__ unsigned tmem_slot, marks[kMarks / 32];
     __shared__ BadRows bad_u, bad_w;
@@ -1039,7 +1040,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                    stats = out + 8 * 64 * kBackwardChunk;
     const float* stats_at = reinterpret_cast<const float*>(raw + (stats - smem_address(raw)));
     const unsigned full_u = smem_address(bars), empty_u = full_u + 8 * kU, full_w = empty_u + 8 * kU, empty_w = full_w + 8 * kW, loaded = empty_w + 8 * kW,
-                   used = loaded + 8, scored = used + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 8, summed = differed + 8,
+                   used = loaded + 8, scored = used + 8, graded = scored + 16, weighted = graded + 8, differed = weighted + 16, summed = differed + 8,
                    drain = summed + 8, scanned = drain + 8;
     const PlaceRing<BackwardPlace> places{reinterpret_cast<BackwardPlace*>(place_bytes), scanned + 8, scanned + 8 + 8 * kPlaces};
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0), lane = threadIdx.x & 31;
@@ -1053,7 +1054,8 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
         barrier_init(scored, 1);                              // S of a step (in each of its places) is there
         barrier_init(scored + 8, 1);
         barrier_init(graded, 1);                              // dP is there
-        barrier_init(weighted, 8);                            // P is there (KEYS)
+        barrier_init(weighted, 8);                            // P of a step (in each of the places of S) is there (KEYS)
+        barrier_init(weighted + 8, 8);
         barrier_init(differed, 8);                            // dS is there
         barrier_init(summed, 1);                              // a tile's sums are there
         barrier_init(drain, 1);
@@ -1236,7 +1238,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 for (int i = n; i < end && ok; ++i) {
                     if (KEYS) {
                         if (kScoreSets == 1) wait_u(i + 1);
-                        if (!await_product(weighted, i)) break;
+                        if (!await_product(weighted + 8 * (i % kScoreSets), i / kScoreSets)) break;
                         if (one_lane()) {
                             add(tmem, tmem + kTmemScores + i % kScoreSets * 128, ring_w + i % kW * kBytes, i > n);
                             mma_done(empty_w + 8 * (i % kW));
@@ -1375,7 +1377,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                         tensor_stored();
                         order_before();
                         __syncwarp();
-                        if (lane == 0) arrive_here(weighted);
+                        if (lane == 0) arrive_here(weighted + 8 * (n % kScoreSets));
                     }
                     if (!await(graded, n)) break;
                     order_after();
