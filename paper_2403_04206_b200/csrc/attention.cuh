@@ -1016,7 +1016,7 @@ struct KeyRows {
 // Where there are two places for S, a step's scores are there before the step in front is done: a warp may be through with a step's P while
 // another is still at that of the step in front, so each place has a barrier of its own for P.
 struct BackwardPlace {                      // steps = -1: there are no more tiles
-    int w, m, h, turn, r0, steps, first, turns, from, to;     // KEYS: `turns` steps from row `first` on, for each query head
+    int w, m, h, turn, r0, steps, first, turns, from, to, loose;  // KEYS: `turns` steps from row `first` on, for each query head
     Reach all;
     KeyWalk walk;
 };
@@ -1109,7 +1109,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
             int round = 0, met = 0;
             // Works the next tile out and hands it on; without steps it is none.  (The longest walks come first, where there is no window.)
             const auto place_next = [&] {
-                BackwardPlace p{0, 0, 0, 0, 0, -1, 0, 0, 0, 0, Reach{}, KeyWalk(Reach{}, 0, kStep)};
+                BackwardPlace p{0, 0, 0, 0, 0, -1, 0, 0, 0, 0, 0, Reach{}, KeyWalk(Reach{}, 0, kStep)};
                 for (; p.steps <= 0 && round * static_cast<int>(gridDim.x) < units; ++round) {
                     const int unit = tile_of_round(round);
                     if (unit >= units) continue;
@@ -1131,7 +1131,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     const int first = all.min_lo / 64 * 64, turns = all.max_hi >= all.min_lo ? (all.max_hi - first) / kStep + 1 : 0;
                     int from, to;
                     rows_of_sequences(a, m, from, to);
-                    p = BackwardPlace{w, m, in - w * heads, turn, r0, KEYS ? turns * a.group : walk.steps, first, turns, from, to, all, walk};
+                    p = BackwardPlace{w, m, in - w * heads, turn, r0, KEYS ? turns * a.group : walk.steps, first, turns, from, to, (KEYS && first < from) || (KEYS ? first + turns * kStep : walk.row(walk.steps - 1, kStep) + kStep) > to, all, walk};
                     if (careful && p.steps > 0 && !marked(marks, met++)) p.steps = 0;
                 }
                 if (p.steps == 0) p.steps = -1;
@@ -1288,7 +1288,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                 const KeyWalk walk = at.walk;
                 const int first = at.first, turns = at.turns, steps = at.steps;
                 // some of the rows that are walked over belong to no sequence
-                const bool loose = (KEYS && first < at.from) || (KEYS ? first + turns * kStep : walk.row(steps - 1, kStep) + kStep) > at.to;
+                const bool loose = at.loose;
                 const int row = at.r0 + quarter * 32 + lane;
                 Keys keys{};
                 const bool valid = own_row(at, row, keys);
