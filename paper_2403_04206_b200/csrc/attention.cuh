@@ -191,53 +191,21 @@ __device__ __forceinline__ float max_three(float a, float b, float c)
     return r;
 }
 
+// Powers of two by the special function unit, which makes 16 a cycle and SM; zero below 2^-126.  (A share of them by a polynomial of degree 5 in
+// its shadow was tried: 2 x 8192 tokens, 16 heads of 64, causal, forward 407 us with none, 433 with one pair in 8, 473 in 4; backward
+// 1153 with none, 1112 with one in 4, but 312 and 328 for 4 x 32 images of 197 tokens, and 1820 and 1885 with heads of 128 on 8.)
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Two powers of two without the special function unit, which makes 16 a cycle and SM: x = n + f with n = floor x (Cody and Waite's
-// reduction; the clamped reduction by an addition rounded down, and the sharing of the exponentials between the two units, are published
-// for softmax on this architecture), 2^f = 1 + f (c1 + ... + c5 f^4) with coefficients fitted for this file on [0, 1) by least squares whose
-// weights were moved until the relative errors were level (8e-8; 1.7e-7 at most with the roundings), times 2^n.  As of the unit, results below
-// 2^-126 are zero, those from 2^128 on infinity, and those of NaN NaN.
-__device__ __forceinline__ void exp2_two(Two x, float& a, float& b)
+__device__ __forceinline__ void exp2_fast(Two x, float& a, float& b)
 {
-    constexpr float kShift = 12583039.0f;                     // 1.5 * 2^23 + 127: the sum's last bits are n + 127, the exponent field of 2^n
-    float u, v;
-    apart(x, u, v);
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-127.0f));  // (field 0: zero)
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-127.0f));
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(128.0f));   // (field 255: infinity)
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(128.0f));
-    x = two(u, v);
-    Two n, f, p;
-    asm("add.rm.f32x2 %0, %1, %2;" : "=l"(n.v) : "l"(x.v), "l"(two(kShift, kShift).v));
-    f = fma_two(add_two(n, two(-kShift, -kShift)), two(-1.0f, -1.0f), x);
-    p = fma_two(f, two(0.0018671303987503052f, 0.0018671303987503052f), two(0.009017029777169228f, 0.009017029777169228f));
-    p = fma_two(f, p, two(0.05579991266131401f, 0.05579991266131401f));
-    p = fma_two(f, p, two(0.24016444385051727f, 0.24016444385051727f));
-    p = fma_two(f, p, two(0.6931512951850891f, 0.6931512951850891f));
-    p = fma_two(f, p, two(1.0f, 1.0f));
-    float s, t;
-    apart(n, s, t);
-    p = mul_two(p, two(__uint_as_float(__float_as_uint(s) << 23), __uint_as_float(__float_as_uint(t) << 23)));
-    apart(p, a, b);
+    apart(x, a, b);
+    a = exp2_fast(a);
+    b = exp2_fast(b);
 }
-// Powers of two of pair `pair` of a run of them: some pairs go by the polynomial, so that the units work side by side.
-template <int EVERY>
-__device__ __forceinline__ void exp2_shared(int pair, Two x, float& a, float& b)
-{
-    if (EVERY > 0 && pair % (EVERY > 0 ? EVERY : 1) == EVERY - 1) {
-        exp2_two(x, a, b);
-    } else {
-        apart(x, a, b);
-        a = exp2_fast(a);
-        b = exp2_fast(b);
-    }
-}
-
 // Bits [lo, hi] of a word, either end of which may lie outside it.
 __device__ __forceinline__ unsigned bits_between(int lo, int hi)
 {
@@ -542,9 +510,6 @@ __device__ __forceinline__ void store_eight(float* to, const float* v)
 // that the products of one run beside the exponentials of the other; each takes one tile after the other, and fetches the next one's
 // queries while it works.  Two threads share a row, one half of a step's scores each: what they wait for one after the other (scores,
 // their exponentials, the sum) bounds a CTA.
-// One in so many pairs of exponentials goes by the polynomial.  (2 x 8192 tokens, 16 heads of 64, causal: 471 us with none, 443 with one in 8,
-// 448 in 4, 516 in 2: its integer steps crowd the other pipe.)
-constexpr int kForwardPolynomial = 8;
 constexpr int kForwardThreads = 320;        // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 template <int DP> constexpr int kForwardStages = DP == 128 ? 2 : 4;
 constexpr int kForwardChunk = 16;           // columns of results on their way
@@ -813,7 +778,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 float x, y;
-                                weight(e, two(s[q] + 2 * e), x, y);
+                                weight(two(s[q] + 2 * e), x, y);
                                 sum[e % 2] = add_two(sum[e % 2], two(x, y));
                                 s[q][e] = pack_pair(x, y, T{});
                             }
@@ -821,15 +786,17 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                         }
                     };
                     if (!careful) {
-                        weigh([&](int e, Two score, float& x, float& y) { exp2_shared<kForwardPolynomial>(e, fma_two(score, two(c, c), two(-ref, -ref)), x, y); });
+                        weigh([&](Two score, float& x, float& y) {
+                            exp2_fast(fma_two(score, two(c, c), two(-ref, -ref)), x, y);
+                        });
                     } else {
-                        weigh([&](int e, Two score, float& x, float& y) {
+                        weigh([&](Two score, float& x, float& y) {
                             Two from_top = fma_two(score, two(c, c), two(-ref, -ref));
                             if (far) {
                                 apart(score, x, y);
                                 from_top = two(__fadd_rn(__fmul_rn(x, c), -ref), __fadd_rn(__fmul_rn(y, c), -ref));
                             }
-                            exp2_shared<kForwardPolynomial>(e, from_top, x, y);
+                            exp2_fast(from_top, x, y);
                             x *= unit;
                             y *= unit;
                         });
@@ -981,8 +948,6 @@ __device__ __forceinline__ int far_from(const AttentionArgs& a, const Sequence& 
 
 constexpr int kBackwardThreads = 320;       // warps 0 to 7: rows, 64 columns of a step each; 8: copies, 9: products
 constexpr int kStep = 128;                  // rows of a step: products of 64 columns take the tensor cores as long as of 128
-// As kForwardPolynomial.  (The same tokens, dk and dv / dq: 829 / 721 us with none, 790 / 611 with one in 4, 835 / 663 in 2.)
-constexpr int kPolynomial = 4;
 constexpr int kBackwardChunk = 32;          // columns of results on their way
 template <int DP, bool KEYS> constexpr int kSlotsU = KEYS && DP == 128 ? 2 : 3;   // of the operand that the scores take
 template <int DP, bool KEYS> constexpr int kSlotsW = KEYS || DP == 64 ? 2 : 1;    // of the one that dP takes
@@ -1362,7 +1327,7 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                                     if (kHalf) shift = add_two(shift, two(kWeightExponent, kWeightExponent));
                                 }
                                 float x, y;
-                                exp2_shared<kPolynomial>(e, fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
+                                exp2_fast(fma_two(two(s[q] + 2 * e), two(c, c), shift), x, y);
                                 if (masked) {
                                     x = seen[q] & 1u << (2 * e) ? x : 0.0f;
                                     y = seen[q] & 2u << (2 * e) ? y : 0.0f;

@@ -60,3 +60,23 @@ def test_small_weights_of_half_precision_keep_their_digits():
         # 47 steps' additions to the sum, and 16 in the first step beside the large term, of 2^-24 each; the logarithm's terms are below 8 and
         # each rounded by at most 2^-21
         assert (lse.double() - math.log(total)).abs().max() < 70 * 2.0 ** -24 + 2 * 2.0 ** -21
+
+
+def test_weights_of_the_backward_pass_below_the_smallest_normal_number():
+    """As above, for the weights that make dv: those of 2^-126.2 are zero wherever the key stands, those of 2^-125.5 are there."""
+    import paper_2403_04206_b200 as grawa
+    n, dim = 200, 64
+    for place in range(n):
+        for low in (-87.5, -87.0):
+            top = (place + 100) % n
+            q, k, v, dout = (torch.zeros(n, 1, dim, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+            q[..., 0] = 1.0
+            k[:, 0, 0] = -200.0
+            k[top, 0, 0], k[place, 0, 0] = 0.0, low
+            dout[n - 1, 0, 0] = 2.0 ** 127
+            out, lse, dk, dv = torch.zeros_like(q), torch.zeros(1, n, device="cuda"), torch.empty_like(k), torch.empty_like(v)
+            grawa.grawa_window_attention_backward([dout], [q], [k], [v], [out], [lse], None, [dk], [dv], right=None, scale=1.0)
+            if low == -87.5:
+                assert dv[place, 0, 0] == 0, place
+            else:                                             # the bfloat16 weight and result are each rounded once
+                assert abs(dv[place, 0, 0].item() / (2.0 ** 127 * math.exp(low)) - 1) < 2.0 ** -7, place
