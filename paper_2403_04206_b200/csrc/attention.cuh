@@ -206,6 +206,7 @@ __device__ __forceinline__ void exp2_fast(Two x, float& a, float& b)
     a = exp2_fast(a);
     b = exp2_fast(b);
 }
+
 // Bits [lo, hi] of a word, either end of which may lie outside it.
 __device__ __forceinline__ unsigned bits_between(int lo, int hi)
 {
@@ -697,7 +698,9 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 Keys keys{};
                 const bool valid = own_keys(a, at.m, at.r0 + line, QueryRows{a}, keys);
                 float top = -INFINITY, total = 0.0f;
-                bool far = false;                                 // the rounding of top, which is past 2^31, is past the exponentials' range
+                // Scores past 2^23: the rounding of the largest one's product is more than a factor of the weights should be.  Such tiles are walked
+                // a second time too, with products that are rounded before top is taken from them.
+                bool far = false, rough = false;              // of top, of any top so far
                 if (careful)
                     for (int e = 0; e < 8; ++e) mine[e] = 0;
                 for (int i = 0; i < steps; ++i, ++n) {
@@ -748,15 +751,19 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                     __syncwarp();
                     if (lane == 0) arrive_here(maxed + 8 * quarter);
                     if (!await(maxed + 8 * quarter, n)) break;
-                    float here = fmaxf(most[0], most_of[n % 2][1 - half][line]) * c;
+                    const float largest = fmaxf(most[0], most_of[n % 2][1 - half][line]), product = largest * c;
+                    float here = product;
                     // Half precision's smallest numbers are 2^-24: the largest weight is 2^6, and none is above 2^14 before m moves.  (Not where the
                     // rounding of larger scores could take them past its largest number.)
-                    if (TypeCode<T>::value == 0 && fabsf(here) < 1048576.0f) here -= 6.0f;
+                    if (TypeCode<T>::value == 0 && fabsf(product) < 1048576.0f) here -= 6.0f;
                     const bool grows = here > top + 8.0f;         // (from -infinity: always)
                     if (__any_sync(0xffffffffu, grows)) {
                         const float f = grows ? exp2_fast(top - here) : 1.0f;
-                        if (careful && grows) far = fabsf(fmaf(fmaxf(most[0], most_of[n % 2][1 - half][line]), c, -here)) > 100.0f;
-                        if (grows) top = here;
+                        if (grows) {
+                            far = fabsf(fmaf(largest, c, -product)) > 0.5f;
+                            rough = rough || far;
+                            top = here;
+                        }
                         total *= f;
                         if (i > 0) {
 #pragma unroll 1
@@ -829,7 +836,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                 if (half == 0 && valid && a.to[1].p[at.m])
                     static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (TypeCode<T>::value ? top + log2f(total / unit) : (top + 6.0f) + log2f(total / 64.0f)) * kLn2;
                 // (a sum of weights that is NaN comes of a score that the row sees: the row is NaN)
-                if (!careful && __any_sync(0xffffffffu, valid && !fine && !isnan(total)) && lane == 0) mark_tile(marks, &more, tile);
+                if (!careful && __any_sync(0xffffffffu, valid && (rough || (!fine && !isnan(total)))) && lane == 0) mark_tile(marks, &more, tile);
                 place_done(tile);
             }
             if (threadIdx.x == 0) careful_from = n;

@@ -4,15 +4,17 @@ import math
 import pytest
 import torch
 
+from replica_util import HALF_ULP
+
 pytestmark = pytest.mark.gpu
 
 
-def one_row(kind, scores, values, dim=64):
-    """The result of one query (the last row; all rows hold it) whose scores against the keys are `scores` exactly."""
+def one_row(kind, scores, values, dim=64, query=1.0):
+    """The results of `query` times the first unit vector, in each row, whose scores against the keys are `scores` times that."""
     import paper_2403_04206_b200 as grawa
     n = len(scores)
     q, k, v = (torch.zeros(n, 1, dim, dtype=kind, device="cuda") for _ in range(3))
-    q[..., 0] = 1.0
+    q[..., 0] = query
     k[:, 0, 0] = torch.as_tensor(scores, dtype=torch.float64).cuda().to(kind)
     v[:, 0, 0] = torch.as_tensor(values, dtype=torch.float64).cuda().to(kind)
     out, lse = torch.full_like(q, 5.0), torch.full((1, n), 5.0, device="cuda")
@@ -80,3 +82,22 @@ def test_weights_of_the_backward_pass_below_the_smallest_normal_number():
                 assert dv[place, 0, 0] == 0, place
             else:                                             # the bfloat16 weight and result are each rounded once
                 assert abs(dv[place, 0, 0].item() / (2.0 ** 127 * math.exp(low)) - 1) < 2.0 ** -7, place
+
+
+@pytest.mark.parametrize("power", [22, 24, 26, 28, 30])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16])
+def test_scores_whose_rounding_is_past_half_precision(kind, power):
+    """Scores of 2^22 to 2^30, where the rounding of the largest one's product with log2 e is 2^-2 to 2^6: weights are taken of what
+    the largest one is, in half precision too, whose numbers end at 2^16 and 2^-24."""
+    n = 128
+    for turn in range(64):
+        place = 2 * turn + 1
+        scores, values = [-float(j) for j in range(n)], [float(j) for j in range(n)]
+        scores[place] = 2.0 ** (power - 15) * (1.0 + turn / 64.0)
+        out, lse = one_row(kind, scores, values, query=2.0 ** 15)
+        # the weight is rounded once to the storage type before the product, the result once
+        assert ((out.double() - values[place]).abs() <= 2 * HALF_ULP[kind] * values[place]).all(), (place, out[0])
+        assert (lse.double() / (scores[place] * 2.0 ** 15) - 1).abs().max() < 2.0 ** -21, (place, lse[0])
+        scores[place - 1] = scores[place]                     # two of the same weight
+        out, lse = one_row(kind, scores, values, query=2.0 ** 15)
+        assert ((out.double() - values[place] + 0.5).abs() <= 2 * HALF_ULP[kind] * values[place]).all(), (place, out[0])
