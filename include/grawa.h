@@ -437,7 +437,7 @@ size_t grawa_head_rotary_backward_workspace_bytes(int64_t rows, int M);
  * product with v (and are zero below 2^-126).
  * A row's result depends on no key or value that it does not see, whatever those hold, infinities and NaN included.  (Where rows
  * that belong to sequences hold such elements, tiles of 128 rows that walk over them are walked twice: a call with one takes up to
- * 3 times as long, one with some in every row up to 30 times.) */
+ * 3 times as long, one with some in every row up to 30 times.  So are tiles with scores past 2^23 / 1.44.) */
 grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void *const *q, const void *const *k, const void *const *v,
                                             void *const *out, float *const *lse, const int64_t *const *offsets,
                                             int64_t sequences, int64_t period, int64_t left, int64_t right, int64_t sinks,
@@ -450,7 +450,8 @@ grawa_status grawa_window_attention_forward(grawa_dtype dtype, const void *const
  *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i,
  * those of a key head summed over its query heads.  dq has row stride q_stride, dk k_stride, dv v_stride.  dq may be NULL,
  * dk and dv both may be, not all three.  Rows of no sequence keep what they hold.  P and dS are rounded to `dtype` for the
- * products (with GRAWA_F16 scaled by powers of two that keep them in its range, for scores below 2^23).
+ * products (with GRAWA_F16 scaled by powers of two that keep them in its range).  P is off by some 2^-22 |S| of itself, the
+ * rounding of lse: scores are to be well below 2^20 in magnitude here.
  * What holds of rows that are not seen, and of the time that infinities and NaN take, holds here too.
  * workspace: DEVICE scratch, 256-byte aligned, of grawa_window_attention_backward_workspace_bytes(...) bytes; it needs no
  * particular contents. */

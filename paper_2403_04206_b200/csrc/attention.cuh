@@ -21,9 +21,8 @@
 // rows that do not see it.  Tiles with such a result are walked a second time, with care: see "what is not finite" below.
 //
 // Measured (B200, back to back, where the power limit holds the clock at 1.6 GHz): 2 x 8192 tokens, 16 query heads on 8 of 128, causal, bf16:
-// forward 590 us (930 TFLOP/s, at 55 % of the tensor pipe's cycles), backward 1850 us (740); what bounds a CTA is the way of a step from
-// its scores to their exponentials to the next product, three waits of some hundred cycles each beside the arithmetic's, and
-// what bounds the SM is power.
+// forward 590 us (930 TFLOP/s), backward 1820 us (755); what bounds a CTA is the way of a step from its scores to their exponentials to
+// the next product, three waits of some hundred cycles each beside the arithmetic's, and what bounds the SM is power.
 //
 // Every wait for a barrier in shared memory is bounded, as in the gated feed-forward product: a wait that runs out is counted
 // in g_attention_timeouts, and the CTA waits (bounded) for its copies and products in flight, frees its tensor memory
@@ -352,7 +351,8 @@ __device__ __forceinline__ bool store_rows(unsigned tensor, int from_col, int co
 // through walks those once more.  This time the threads of the rows look each step's operand of such a product over, set elements that
 // are not finite to zero where they stand in shared memory, and keep for each row they see such elements from in which columns infinity
 // of either sign (both: NaN) is to be added to the sum.  An element of P counts as positive even where it is too small for 32 bits; dS, which
-// then is zero or not finite itself, as making NaN.  Rows that belong to no sequence, which may hold anything, are zeroed on the first walk already, where a step holds some.
+// then is zero or not finite itself, as making NaN.  Rows that belong to no sequence, which may hold anything, are zeroed on the first walk
+// already, where a step holds some.
 //
 // Measured (2 x 8192 tokens, 16 query heads on 8 of 128, causal, bf16; 520 us forward, 1610 backward with finite operands): one infinity in
 // the first row of v 1390 us forward; in the last one of dout 3540 us backward; v NaN throughout 3570 us forward, dout 7900 us

@@ -13,9 +13,10 @@ namespace replica {
 constexpr int kWorkers = 64;           // GRAWA_MAX_WORKERS
 constexpr int kSms = 148;              // a B200; the shapes of the persistent grids follow it
 
-// The first thing in every kernel (but one that runs beside the launch in front of it, which does this last): waits until the kernel in front on the stream is done and its results are visible, then
-// lets the kernel behind start launching, which waits in the same way.  So a kernel's launch and ramp-up overlap the end of
-// the one in front, and nothing else does.  (Without the launch attribute both do nothing.)
+// The first thing in every kernel: waits until the kernel in front on the stream is done and its results are visible, then lets
+// the kernel behind start launching, which waits in the same way.  So a kernel's launch and ramp-up overlap the end of the one in
+// front, and nothing else does.  (Without the launch attribute both do nothing.)  A kernel that runs beside the launch in front of it,
+// as it needs nothing of that, does this last instead.
 __device__ __forceinline__ void stream_order()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
