@@ -490,7 +490,7 @@ __device__ __noinline__ void add_infinities(unsigned* mine, const unsigned short
 #pragma unroll
     for (int e = 0; e < 8; ++e) mine[e] = own.bits[e];
 }
-// Whether a walk is the second one, of noted tiles, and which those are.
+// Notes a tile for the second walk, and whether it is noted.
 __device__ __forceinline__ void mark_tile(unsigned* marks, int* more, int tile)
 {
     atomicOr(marks + tile % kMarks / 32, 1u << tile % 32);
@@ -793,9 +793,7 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                         }
                     };
                     if (!careful) {
-                        weigh([&](Two score, float& x, float& y) {
-                            exp2_fast(fma_two(score, two(c, c), two(-ref, -ref)), x, y);
-                        });
+                        weigh([&](Two score, float& x, float& y) { exp2_fast(fma_two(score, two(c, c), two(-ref, -ref)), x, y); });
                     } else {
                         weigh([&](Two score, float& x, float& y) {
                             Two from_top = fma_two(score, two(c, c), two(-ref, -ref));
@@ -834,7 +832,8 @@ attention_forward_kernel(const __grid_constant__ TileArgs t)
                                                                });
                 order_before();
                 if (half == 0 && valid && a.to[1].p[at.m])
-                    static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] = (TypeCode<T>::value ? top + log2f(total / unit) : (top + 6.0f) + log2f(total / 64.0f)) * kLn2;
+                    static_cast<float*>(a.to[1].p[at.m])[static_cast<long long>(at.h) * a.rows + at.r0 + line] =
+                        (TypeCode<T>::value ? top + log2f(total / unit) : (top + 6.0f) + log2f(total / 64.0f)) * kLn2;
                 // (a sum of weights that is NaN comes of a score that the row sees: the row is NaN)
                 if (!careful && __any_sync(0xffffffffu, valid && (rough || (!fine && !isnan(total)))) && lane == 0) mark_tile(marks, &more, tile);
                 place_done(tile);
@@ -1284,9 +1283,10 @@ attention_backward_kernel(const __grid_constant__ TileArgs t)
                     if (KEYS && !await(full_u + 8 * (n % kU), n / kU)) break;      // (long past: for the sight of lse and delta)
                     // (The products that made S, and dP of the operand that dv takes, are through with what is set to zero here.)
                     if (!careful && loose) {
-                        ok = zero_loose_rows<DP>(at.from - r, at.to - r, raw + (ring_u - smem_address(raw)) + n % kU * kBytes, full_u + 8 * (n % kU), n / kU, full_u + 8 * (n % kU), n / kU,
-                                                 &gave_up) &&
-                             (!KEYS || zero_loose_rows<DP>(at.from - r, at.to - r, raw + (ring_w - smem_address(raw)) + n % kW * kBytes, full_w + 8 * (n % kW), n / kW, graded, n, &gave_up));
+                        const int from = at.from - r, to = at.to - r;
+                        const unsigned bar_u = full_u + 8 * (n % kU), bar_w = full_w + 8 * (n % kW);
+                        ok = zero_loose_rows<DP>(from, to, raw + (ring_u - smem_address(raw)) + n % kU * kBytes, bar_u, n / kU, bar_u, n / kU, &gave_up) &&
+                             (!KEYS || zero_loose_rows<DP>(from, to, raw + (ring_w - smem_address(raw)) + n % kW * kBytes, bar_w, n / kW, graded, n, &gave_up));
                         if (!ok) break;
                     }
                     if (careful) {
